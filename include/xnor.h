@@ -398,6 +398,141 @@ xnor_status xnor_maxpool2d(const float *x, int N, int C, int H, int W, int k, in
                            int relu, float *out, void *cuda_stream);
 
 /*
+ * ---- Rows of tokens: the low-bit block of a language model ---------------------------------
+ * The counterpart of BinActiv, BinConv and the Binary-Weight convolution for rows of hidden
+ * states: a norm whose output can leave in 8 bits with scales, and products with weights of
+ * 4 bits with a scale for each group of columns.  (No counterpart in the paper.)
+ *
+ * Tensors of rows are [rows][cols] with the columns contiguous and a stride of their own, in
+ * elements, from row to row: any stride >= 0 for what is read (0: one row for all), at least
+ * cols for what is written.  They are fastest when the strides are multiples of 16 bytes.
+ * rows = 0 is allowed: nothing is read, and only xnor_rmsnorm_backward's dweight is written.
+ */
+typedef enum {
+  XNOR_F32 = 0,
+  XNOR_BF16 = 1,
+  XNOR_F16 = 2,
+  XNOR_I8 = 3,
+  XNOR_E4M3 = 4      /* 8-bit floating point, 4 exponent and 3 mantissa bits, no infinities */
+} xnor_type;
+
+/*
+ * Root-mean-square norm of rows, with the residual's addition:
+ *   h = x + residual, rounded to `type` (h = x without a residual),
+ *   rstd = 1 / sqrt(mean over the columns of h^2 + eps),   y = h rstd weight.
+ * Sums, rstd and products in fp32, y rounded once.
+ *
+ *   x         in   type [rows][cols]
+ *   residual  in   type [rows][cols] or NULL
+ *   weight    in   weight_type [cols] or NULL (ones)
+ *   sum       out  type [rows][cols] or NULL: h, what the next layers add to.  May be the same
+ *                  buffer as x or residual (with the same stride)
+ *   y         out  type [rows][cols]; may be the same buffer as x or residual
+ *   rstd      out  fp32 [rows] or NULL: what the backward pass needs
+ * xnor_rmsnorm_quant writes y in 8 bits instead, without rounding it in between:
+ *   scale = max|y| / top over the group, q = y / scale to nearest even, top = 127 (I8) or 448 (E4M3)
+ *   q         out  q_type [rows][cols], dense
+ *   scales    out  fp32 [rows][cols / group], dense; group = 0: one scale for a whole row, [rows]
+ *   A group of zeros has the scale 0.  A group with an infinity or NaN in it has such a scale (so that
+ *   all it stands for is NaN or infinite).
+ *
+ * INVALID_ARG: null (where not allowed) or misaligned pointer, rows < 0, cols < 1, a stride out of
+ * range, type none of F32, BF16, F16, weight_type neither F32 nor type, eps negative or not a number,
+ * q_type neither I8 nor E4M3, group none of 0, 32, 64, 128.  UNSUPPORTED: cols > 32768; cols not a
+ * multiple of group.
+ */
+typedef struct {
+  int rows, cols;
+  int type, weight_type;      /* xnor_type */
+  float eps;
+  long long x_stride, residual_stride, sum_stride, y_stride;
+} xnor_norm_desc;
+xnor_status xnor_rmsnorm(const void *x, const void *residual, const void *weight,
+                         const xnor_norm_desc *d, void *sum, void *y, float *rstd,
+                         void *cuda_stream);
+xnor_status xnor_rmsnorm_quant(const void *x, const void *residual, const void *weight,
+                               const xnor_norm_desc *d, int q_type, int group, void *sum, void *q,
+                               float *scales, float *rstd, void *cuda_stream);
+
+/*
+ * Backward pass of xnor_rmsnorm (and, with the rounding to 8 bits passed straight through, of
+ * xnor_rmsnorm_quant): with u = weight dy,
+ *   dx = rstd (u - h rstd^2 mean(u h)) + dsum,   dweight = sum over the rows of dy h rstd.
+ * The residual's gradient is dx too.
+ *
+ *   dy       in   type [rows][cols], stride y_stride: gradient at y
+ *   dsum     in   type [rows][cols] or NULL, stride residual_stride: gradient at sum, that
+ *                 arrives past the norm
+ *   h        in   type [rows][cols], stride x_stride: the forward call's sum (x without a residual)
+ *   weight   in   as in the forward call
+ *   rstd     in   fp32 [rows], from the forward call
+ *   dx       out  type [rows][cols], stride sum_stride; may be the same buffer as dy or dsum
+ *   dweight  out  fp32 [cols] or NULL (then work may be NULL too)
+ *   work     scratch of xnor_rmsnorm_work_elems(rows, cols) floats
+ * dweight is summed in a fixed order: the same inputs give the same bits.  d->eps is ignored.
+ * Errors as above; xnor_rmsnorm_work_elems gives 0 for sizes out of range and for no rows.
+ */
+size_t xnor_rmsnorm_work_elems(int rows, int cols);
+xnor_status xnor_rmsnorm_backward(const void *dy, const void *dsum, const void *h, const void *weight,
+                                  const float *rstd, const xnor_norm_desc *d, void *dx, float *dweight,
+                                  float *work, void *cuda_stream);
+
+/*
+ * 4-bit weights: a matrix [N][K] (N outputs, K inputs, bias-free like the filters) as codes 0 .. 15
+ * with a scale and, optionally, a zero point for each group of `group` columns of a row (the last
+ * group may be shorter): w = (code - zero) scale.
+ *
+ *   w_packed  u32 [ceil(N/16)][ceil(K/64)][32][4]: tiles of 16 rows x 64 columns.  Element
+ *             [.][.][4 g + t][j] holds the codes of rows g (bits 0, 16, 8, 24 and up) and g + 8 (bits
+ *             4, 20, 12, 28 and up), columns 32 (j/2) + 8 t + 4 (j%2) + 0, 1, 2, 3 of the tile; rows
+ *             and columns beyond the matrix hold any code.
+ *   scales    fp32 [ceil(K/group)][N]
+ *   zeros     u8   [ceil(K/group)][N], 0 .. 15, or NULL: 8 everywhere
+ * xnor_w4_quantize   w type [N][K] (F32, BF16, F16) -> w_packed, scales, zeros.
+ *     zeros NULL: scale = max|w| / 7, code = w / scale + 8; else with lo = min(w, 0) and hi = max(w, 0)
+ *     over the group scale = (hi - lo) / 15, zero = -lo / scale, code = w / scale + zero.  scale is
+ *     rounded to fp32, the quotients to the nearest whole number, exactly, ties to even.  A group of
+ *     zeros has the scale 0; one with an infinity or NaN such a scale.
+ * xnor_w4_pack        codes u8 [N][K], 0 .. 15 (higher bits are ignored) -> w_packed: weights that
+ *     were quantised elsewhere.
+ * xnor_w4_dequantize  w_packed, scales, zeros -> w type [N][K] (F32, BF16, F16), rounded once.
+ *
+ * INVALID_ARG: null or misaligned pointer, N or K < 1, group none of 32, 64, 128, type out of range.
+ * UNSUPPORTED: N > 1048560, K > 16777216.
+ */
+typedef struct {
+  int N, K, group;
+} xnor_w4_desc;
+size_t xnor_w4_packed_words(const xnor_w4_desc *d);       /* 0: bad descriptor */
+xnor_status xnor_w4_quantize(const void *w, int type, const xnor_w4_desc *d, uint32_t *w_packed,
+                             float *scales, uint8_t *zeros, void *cuda_stream);
+xnor_status xnor_w4_pack(const uint8_t *codes, const xnor_w4_desc *d, uint32_t *w_packed,
+                         void *cuda_stream);
+xnor_status xnor_w4_dequantize(const uint32_t *w_packed, const float *scales, const uint8_t *zeros,
+                               const xnor_w4_desc *d, int type, void *w, void *cuda_stream);
+
+/*
+ * Rows times 4-bit weights, from one token to whole prompts:
+ *   out[t][n] = sum over groups of scales[g][n] xs[t][g] sum over k in the group of
+ *               (code[n][k] - zero[g][n]) x[t][k]
+ *   x         in   x_type [rows][K]: BF16, F16, or I8 / E4M3 with scales
+ *   x_scales  in   fp32 [rows] (x_group = 0) or [rows][ceil(K/group)] (x_group = group), dense; only
+ *                  with I8 and E4M3 rows (xnor_rmsnorm_quant makes them), else NULL
+ *   w_packed, scales, zeros   as above
+ *   out       out  out_type [rows][N]: F32, BF16, F16, rounded once
+ * code - zero and x are exact operands; the sums of a group and over the groups are fp32.
+ * INVALID_ARG as above, and for x_scales that are missing or not wanted.  UNSUPPORTED: F32 rows, an
+ * x_group that is neither 0 nor the weights' group, rows > 1048560.
+ */
+typedef struct {
+  int rows, x_type, x_group, out_type;
+  long long x_stride, out_stride;
+} xnor_w4_rows;
+xnor_status xnor_w4_matmul(const void *x, const float *x_scales, const uint32_t *w_packed,
+                           const float *scales, const uint8_t *zeros, const xnor_w4_desc *d,
+                           const xnor_w4_rows *r, void *out, void *cuda_stream);
+
+/*
  * Which BinConv engine xnor_conv2d_forward uses.  XNOR_ENGINE_AUTO (default)
  * picks by shape: the tensor-core engine where it applies, else the CUDA-core
  * one.  Meant for tests and measurements.  This is the library's only

@@ -44,7 +44,15 @@ EXPORTS = [
     "xnor_binactiv_kbit", "xnor_conv2d_forward_kbit", "xnor_conv2d_plan",
     "xnor_bwn_input_elems", "xnor_bwn_prepare_input", "xnor_bwn_conv2d_forward",
     "xnor_bgrad_stream_elems", "xnor_binarize_weights_transposed", "xnor_binary_gradient_backward", "xnor_measure_peaks",
+    "xnor_rmsnorm", "xnor_rmsnorm_quant", "xnor_rmsnorm_work_elems", "xnor_rmsnorm_backward",
+    "xnor_w4_packed_words", "xnor_w4_quantize", "xnor_w4_pack", "xnor_w4_dequantize", "xnor_w4_matmul",
 ]
+
+XNOR_F32 = 0
+XNOR_BF16 = 1
+XNOR_F16 = 2
+XNOR_I8 = 3
+XNOR_E4M3 = 4
 
 
 class xnor_conv_desc(ctypes.Structure):
@@ -55,6 +63,20 @@ class xnor_conv_desc(ctypes.Structure):
 class xnor_conv_plan(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int) for n in
                 ("tensor_cores", "launches", "resident", "pair", "slabs", "slab_filters")]
+
+
+class xnor_norm_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("rows", "cols", "type", "weight_type")] + [("eps", ctypes.c_float)] + \
+        [(n, ctypes.c_longlong) for n in ("x_stride", "residual_stride", "sum_stride", "y_stride")]
+
+
+class xnor_w4_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("N", "K", "group")]
+
+
+class xnor_w4_rows(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("rows", "x_type", "x_group", "out_type")] + \
+        [(n, ctypes.c_longlong) for n in ("x_stride", "out_stride")]
 
 
 class XnorError(RuntimeError):
@@ -68,7 +90,8 @@ _lib = None
 _MARSHALLED = ["binarize_weights", "binactiv", "conv2d_forward", "shortcut_conv1x1",
                "conv2d_forward_binactiv", "binactiv_finish", "maxpool2d", "binactiv_kbit",
                "conv2d_forward_kbit", "bwn_prepare_input", "bwn_conv2d_forward",
-               "binarize_weights_transposed", "binary_gradient_backward"]
+               "binarize_weights_transposed", "binary_gradient_backward", "rmsnorm", "rmsnorm_quant",
+               "rmsnorm_backward", "w4_quantize", "w4_pack", "w4_dequantize", "w4_matmul"]
 
 
 class _Unloaded:
@@ -152,6 +175,25 @@ def load():
     lib.xnor_binary_gradient_backward.argtypes = [vp, vp, vp, ctypes.POINTER(xnor_conv_desc), vp, vp, vp, vp]
     lib.xnor_measure_peaks.restype = ci
     lib.xnor_measure_peaks.argtypes = [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double), vp]
+    nd, wd, cz = ctypes.POINTER(xnor_norm_desc), ctypes.POINTER(xnor_w4_desc), ctypes.c_size_t
+    lib.xnor_rmsnorm.restype = ci
+    lib.xnor_rmsnorm.argtypes = [vp, vp, vp, nd, vp, vp, vp, vp]
+    lib.xnor_rmsnorm_quant.restype = ci
+    lib.xnor_rmsnorm_quant.argtypes = [vp, vp, vp, nd, ci, ci, vp, vp, vp, vp, vp]
+    lib.xnor_rmsnorm_work_elems.restype = cz
+    lib.xnor_rmsnorm_work_elems.argtypes = [ci, ci]
+    lib.xnor_rmsnorm_backward.restype = ci
+    lib.xnor_rmsnorm_backward.argtypes = [vp, vp, vp, vp, vp, nd, vp, vp, vp, vp]
+    lib.xnor_w4_packed_words.restype = cz
+    lib.xnor_w4_packed_words.argtypes = [wd]
+    lib.xnor_w4_quantize.restype = ci
+    lib.xnor_w4_quantize.argtypes = [vp, ci, wd, vp, vp, vp, vp]
+    lib.xnor_w4_pack.restype = ci
+    lib.xnor_w4_pack.argtypes = [vp, wd, vp, vp]
+    lib.xnor_w4_dequantize.restype = ci
+    lib.xnor_w4_dequantize.argtypes = [vp, vp, vp, wd, ci, vp, vp]
+    lib.xnor_w4_matmul.restype = ci
+    lib.xnor_w4_matmul.argtypes = [vp, vp, vp, vp, vp, wd, ctypes.POINTER(xnor_w4_rows), vp, vp]
     try:
         from . import _pymarshal
     except ImportError as e:
@@ -159,6 +201,7 @@ def load():
                           "(%s)" % e) from e
     _pymarshal.bind([ctypes.cast(getattr(lib, "xnor_" + n), vp).value for n in _MARSHALLED], xnor_conv_desc,
                     _address)
+    _pymarshal.describe(xnor_w4_desc, _describe, ctypes.cast(lib.xnor_rmsnorm_work_elems, vp).value)
     _m, _lib = _pymarshal, lib       # in this order: another thread that sees _lib goes on to use _m
     return lib
 
@@ -178,6 +221,22 @@ def _ptr(t, dtype=None):
 def _address(t, dtype):
     """For the native module: the address of what is not exactly a tensor, by its Python attributes."""
     return _ptr(t, getattr(torch, dtype)).value or 0
+
+
+_SCALAR_TYPES = {torch.uint8: 0, torch.int8: 1, torch.int16: 2, torch.int32: 3, torch.int64: 4, torch.float16: 5,
+                 torch.float32: 6, torch.float64: 7, torch.bool: 11, torch.bfloat16: 15, torch.float8_e5m2: 23,
+                 torch.float8_e4m3fn: 24}            # c10::ScalarType
+
+
+def _describe(t):
+    """For the native module: what is not exactly a tensor, by its Python attributes (calls on tensors of rows)."""
+    if not t.is_cuda:
+        raise ValueError("libxnor takes device pointers: tensor is on %s" % t.device)
+    if t.dtype not in _SCALAR_TYPES:
+        raise ValueError("%s is not supported" % t.dtype)
+    index = getattr(torch.device(t.device), "index", None)
+    return (int(t.data_ptr()), _SCALAR_TYPES[t.dtype], tuple(int(n) for n in t.shape),
+            tuple(int(n) for n in t.stride()), torch.cuda.current_device() if index is None else index)
 
 
 def _stream(stream):
@@ -386,6 +445,88 @@ def xnor_shortcut_conv1x1(x, w, stride, out, stream=None):
     s = _m.shortcut_conv1x1(x, w, int(stride), out, stream)
     if s:
         raise XnorError(s, "xnor_shortcut_conv1x1")
+
+
+# ---- rows of tokens -------------------------------------------------------------------------
+# These calls take sizes, types and strides from the tensors ([rows][cols], columns contiguous, rows at any stride),
+# and run on the tensors' device; stream=None is that device's current stream.
+def xnor_rmsnorm(x, residual, weight, eps, sum, y, rstd, stream=None):
+    """y = norm(x + residual) * weight; residual, weight, sum and rstd may be None."""
+    s = _m.rmsnorm(x, residual, weight, eps, sum, y, rstd, stream)
+    if s:
+        raise XnorError(s, "xnor_rmsnorm")
+
+
+def xnor_rmsnorm_quant(x, residual, weight, eps, group, sum, q, scales, rstd, stream=None):
+    """The norm in 8 bits: q int8 or float8_e4m3fn, scales [rows][cols / group] ([rows][1] for group 0)."""
+    s = _m.rmsnorm_quant(x, residual, weight, eps, int(group), sum, q, scales, rstd, stream)
+    if s:
+        raise XnorError(s, "xnor_rmsnorm_quant")
+
+
+def xnor_rmsnorm_work_elems(rows, cols):
+    return int(load().xnor_rmsnorm_work_elems(int(rows), int(cols)))
+
+
+def xnor_rmsnorm_backward(dy, dsum, h, weight, rstd, dx, dweight, work, stream=None):
+    """dx (the residual's gradient too) and dweight; dsum, weight may be None, and dweight with work."""
+    s = _m.rmsnorm_backward(dy, dsum, h, weight, rstd, dx, dweight, work, stream)
+    if s:
+        raise XnorError(s, "xnor_rmsnorm_backward")
+
+
+def alloc_rmsnorm_quant(rows, cols, group, dtype=torch.int8, device="cuda"):
+    """(q [rows][cols], scales) for xnor_rmsnorm_quant."""
+    return (torch.empty((rows, cols), dtype=dtype, device=device),
+            torch.empty((rows, cols // group if group > 0 else 1), dtype=torch.float32, device=device))
+
+
+def alloc_rmsnorm_backward(rows, cols, device="cuda"):
+    """(dweight [cols], work scratch) for xnor_rmsnorm_backward."""
+    return (torch.empty((cols,), dtype=torch.float32, device=device),
+            torch.empty((xnor_rmsnorm_work_elems(rows, cols),), dtype=torch.float32, device=device))
+
+
+def make_w4_desc(N, K, group=128):
+    return xnor_w4_desc(N, K, group)
+
+
+def xnor_w4_packed_words(d):
+    return int(load().xnor_w4_packed_words(ctypes.byref(d)))
+
+
+def alloc_w4(d, zeros=False, device="cuda"):
+    """(w_packed, scales, zeros or None) of the matrix d."""
+    groups = -(-d.K // d.group)
+    return (torch.empty((-(-d.N // 16), -(-d.K // 64), 32, 4), dtype=torch.int32, device=device),
+            torch.empty((groups, d.N), dtype=torch.float32, device=device),
+            torch.empty((groups, d.N), dtype=torch.uint8, device=device) if zeros else None)
+
+
+def xnor_w4_quantize(w, d, w_packed, scales, zeros, stream=None):
+    s = _m.w4_quantize(w, d, w_packed, scales, zeros, stream)
+    if s:
+        raise XnorError(s, "xnor_w4_quantize")
+
+
+def xnor_w4_pack(codes, d, w_packed, stream=None):
+    s = _m.w4_pack(codes, d, w_packed, stream)
+    if s:
+        raise XnorError(s, "xnor_w4_pack")
+
+
+def xnor_w4_dequantize(w_packed, scales, zeros, d, w, stream=None):
+    s = _m.w4_dequantize(w_packed, scales, zeros, d, w, stream)
+    if s:
+        raise XnorError(s, "xnor_w4_dequantize")
+
+
+def xnor_w4_matmul(x, x_scales, w_packed, scales, zeros, d, out, stream=None):
+    """out [rows][N] = x [rows][K] times the transposed 4-bit matrix; x_scales [rows][1] or [rows][groups] with
+    8-bit rows, else None."""
+    s = _m.w4_matmul(x, x_scales, w_packed, scales, zeros, d, out, stream)
+    if s:
+        raise XnorError(s, "xnor_w4_matmul")
 
 
 # ---- buffer helpers (allocation only; torch owns the memory) -------------------------------

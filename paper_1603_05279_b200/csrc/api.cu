@@ -3,6 +3,7 @@
 
 #include "bgrad.cuh"
 #include "kbit.cuh"
+#include "rows.cuh"
 
 namespace {
 
@@ -429,6 +430,126 @@ xnor_status xnor_binary_gradient_backward(const float *g, const uint32_t *wT_pac
   if (e == cudaSuccess) e = xnor::launch_bwn_conv(g_stream, wT_packed, nullptr, nullptr, gb, grad_in, st);
   if (e != cudaSuccess) (void)cudaGetLastError();
   return from_cuda(e);
+}
+
+namespace {
+
+bool real_type(int t) { return t == XNOR_F32 || t == XNOR_BF16 || t == XNOR_F16; }
+// Whether tensors of rows may be read (stride 0: one row for all) or written with this stride.
+bool bad_read(const void *p, long long stride) { return bad_ptr(p) || stride < 0; }
+bool bad_write(const void *p, long long stride, int rows, int cols) {
+  return bad_ptr(p) || stride < 0 || (rows > 1 && stride < cols);
+}
+
+xnor_status check_norm(const xnor_norm_desc *d, const void *weight) {
+  if (!d || d->rows < 0 || d->cols < 1 || !real_type(d->type)) return XNOR_ERR_INVALID_ARG;
+  if (weight && (misaligned(weight) || (d->weight_type != XNOR_F32 && d->weight_type != d->type))) return XNOR_ERR_INVALID_ARG;
+  return d->cols > xnor::kNormMaxCols ? XNOR_ERR_UNSUPPORTED : XNOR_OK;
+}
+
+xnor_status check_norm_forward(const void *x, const void *residual, const void *weight, const xnor_norm_desc *d,
+                               const void *sum, const float *rstd) {
+  const xnor_status s = check_norm(d, weight);
+  if (s == XNOR_ERR_INVALID_ARG) return s;
+  if (!(d->eps >= 0.0f) || misaligned(rstd)) return XNOR_ERR_INVALID_ARG;
+  if (d->rows == 0) return s;
+  if (bad_read(x, d->x_stride) || (residual && bad_read(residual, d->residual_stride)) ||
+      (sum && bad_write(sum, d->sum_stride, d->rows, d->cols)))
+    return XNOR_ERR_INVALID_ARG;
+  return s;
+}
+
+bool bad_w4(const xnor_w4_desc *d) {
+  return !d || d->N < 1 || d->K < 1 || (d->group != 32 && d->group != 64 && d->group != 128);
+}
+bool large_w4(const xnor_w4_desc *d) { return d->N > 16 * 65535 || d->K > (1 << 24); }
+
+}  // namespace
+
+xnor_status xnor_rmsnorm(const void *x, const void *residual, const void *weight,
+                         const xnor_norm_desc *d, void *sum, void *y, float *rstd,
+                         void *cuda_stream) {
+  const xnor_status s = check_norm_forward(x, residual, weight, d, sum, rstd);
+  if (s == XNOR_ERR_INVALID_ARG) return s;
+  if (d->rows > 0 && bad_write(y, d->y_stride, d->rows, d->cols)) return XNOR_ERR_INVALID_ARG;
+  if (s != XNOR_OK) return s;
+  return from_cuda(xnor::launch_rmsnorm({x, residual, weight, sum, y, rstd, nullptr, nullptr, 0, 0, *d},
+                                        (cudaStream_t)cuda_stream));
+}
+
+xnor_status xnor_rmsnorm_quant(const void *x, const void *residual, const void *weight,
+                               const xnor_norm_desc *d, int q_type, int group, void *sum, void *q,
+                               float *scales, float *rstd, void *cuda_stream) {
+  const xnor_status s = check_norm_forward(x, residual, weight, d, sum, rstd);
+  if (s == XNOR_ERR_INVALID_ARG) return s;
+  if (q_type != XNOR_I8 && q_type != XNOR_E4M3) return XNOR_ERR_INVALID_ARG;
+  if (group != 0 && group != 32 && group != 64 && group != 128) return XNOR_ERR_INVALID_ARG;
+  if (d->rows > 0 && (bad_ptr(q) || bad_ptr(scales))) return XNOR_ERR_INVALID_ARG;
+  if (s != XNOR_OK) return s;
+  if (group != 0 && d->cols % group != 0) return XNOR_ERR_UNSUPPORTED;
+  return from_cuda(xnor::launch_rmsnorm({x, residual, weight, sum, nullptr, rstd, q, scales, q_type, group, *d},
+                                        (cudaStream_t)cuda_stream));
+}
+
+size_t xnor_rmsnorm_work_elems(int rows, int cols) {
+  if (rows < 0 || cols < 1 || cols > xnor::kNormMaxCols) return 0;
+  return (size_t)xnor::rmsnorm_parts(rows, cols) * (size_t)cols;
+}
+
+xnor_status xnor_rmsnorm_backward(const void *dy, const void *dsum, const void *h, const void *weight,
+                                  const float *rstd, const xnor_norm_desc *d, void *dx, float *dweight,
+                                  float *work, void *cuda_stream) {
+  const xnor_status s = check_norm(d, weight);
+  if (s == XNOR_ERR_INVALID_ARG) return s;
+  if (misaligned(dweight)) return XNOR_ERR_INVALID_ARG;
+  if (d->rows > 0 && (bad_read(dy, d->y_stride) || (dsum && bad_read(dsum, d->residual_stride)) || bad_read(h, d->x_stride) ||
+                      bad_ptr(rstd) || bad_write(dx, d->sum_stride, d->rows, d->cols) || (dweight && bad_ptr(work))))
+    return XNOR_ERR_INVALID_ARG;
+  if (s != XNOR_OK) return s;
+  return from_cuda(xnor::launch_rmsnorm_backward({dy, dsum, h, weight, rstd, dx, dweight, work, *d}, (cudaStream_t)cuda_stream));
+}
+
+size_t xnor_w4_packed_words(const xnor_w4_desc *d) {
+  if (bad_w4(d) || large_w4(d)) return 0;
+  return (size_t)xnor::w4_row_tiles(*d) * (size_t)xnor::w4_col_tiles(*d) * 128;
+}
+
+xnor_status xnor_w4_quantize(const void *w, int type, const xnor_w4_desc *d, uint32_t *w_packed,
+                             float *scales, uint8_t *zeros, void *cuda_stream) {
+  if (bad_w4(d) || !real_type(type) || bad_ptr(w) || bad_ptr(w_packed) || bad_ptr(scales) || misaligned(zeros))
+    return XNOR_ERR_INVALID_ARG;
+  if (large_w4(d)) return XNOR_ERR_UNSUPPORTED;
+  return from_cuda(xnor::launch_w4_quantize(w, type, *d, w_packed, scales, zeros, (cudaStream_t)cuda_stream));
+}
+
+xnor_status xnor_w4_pack(const uint8_t *codes, const xnor_w4_desc *d, uint32_t *w_packed,
+                         void *cuda_stream) {
+  if (bad_w4(d) || bad_ptr(codes) || bad_ptr(w_packed)) return XNOR_ERR_INVALID_ARG;
+  if (large_w4(d)) return XNOR_ERR_UNSUPPORTED;
+  return from_cuda(xnor::launch_w4_pack(codes, *d, w_packed, (cudaStream_t)cuda_stream));
+}
+
+xnor_status xnor_w4_dequantize(const uint32_t *w_packed, const float *scales, const uint8_t *zeros,
+                               const xnor_w4_desc *d, int type, void *w, void *cuda_stream) {
+  if (bad_w4(d) || !real_type(type) || bad_ptr(w) || bad_ptr(w_packed) || bad_ptr(scales) || misaligned(zeros))
+    return XNOR_ERR_INVALID_ARG;
+  if (large_w4(d)) return XNOR_ERR_UNSUPPORTED;
+  return from_cuda(xnor::launch_w4_dequantize(w_packed, scales, zeros, *d, type, w, (cudaStream_t)cuda_stream));
+}
+
+xnor_status xnor_w4_matmul(const void *x, const float *x_scales, const uint32_t *w_packed,
+                           const float *scales, const uint8_t *zeros, const xnor_w4_desc *d,
+                           const xnor_w4_rows *r, void *out, void *cuda_stream) {
+  if (bad_w4(d) || !r || r->rows < 0 || r->x_type < XNOR_F32 || r->x_type > XNOR_E4M3 || !real_type(r->out_type))
+    return XNOR_ERR_INVALID_ARG;
+  const bool bytes = r->x_type == XNOR_I8 || r->x_type == XNOR_E4M3;
+  if (bad_ptr(w_packed) || bad_ptr(scales) || misaligned(zeros)) return XNOR_ERR_INVALID_ARG;
+  if (r->rows > 0 && (bad_read(x, r->x_stride) || bad_write(out, r->out_stride, r->rows, d->N) ||
+                      (bytes ? bad_ptr(x_scales) : x_scales != nullptr)))
+    return XNOR_ERR_INVALID_ARG;
+  if (large_w4(d) || r->rows > 16 * 65535 || r->x_type == XNOR_F32 || (bytes && r->x_group != 0 && r->x_group != d->group))
+    return XNOR_ERR_UNSUPPORTED;
+  return from_cuda(xnor::launch_w4_few_rows({x, x_scales, w_packed, scales, zeros, out, *d, *r}, (cudaStream_t)cuda_stream));
 }
 
 xnor_status xnor_shortcut_conv1x1(const float *x, const float *w, int N, int C_in, int H, int W,

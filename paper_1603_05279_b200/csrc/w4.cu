@@ -1,0 +1,380 @@
+// 4-bit weights with a scale for each group of columns: quantised from real weights, laid out from given
+// codes, dequantised, and multiplied with a few rows.
+#include <algorithm>
+#include <type_traits>
+
+#include "w4.cuh"
+
+namespace xnor {
+
+namespace {
+
+// ---- layout -------------------------------------------------------------------------------
+constexpr int kLayThreads = 128;
+constexpr int kLayCols = 2 * kW4Cols;      // a block: 16 rows x 128 columns, the largest group; a thread: 16 columns
+constexpr int kQuads = kLayCols / 4;
+
+// Codes of the block, spread (w4_spread), [16 rows][quads of columns], to the packed tiles.
+__device__ __forceinline__ void write_tiles(const uint32_t (&part)[kW4Rows][kQuads + 1], int row_tile, int col_tile0,
+                                            int col_tiles, uint32_t *w) {
+  const int tile = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  if (tile >= 2 || col_tile0 + tile >= col_tiles) return;
+  uint32_t v[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int q = 16 * tile + w4_column(t, j) / 4;
+    v[j] = part[g][q] | part[g + 8][q] << 4;
+  }
+  reinterpret_cast<uint4 *>(w)[((size_t)row_tile * col_tiles + col_tile0 + tile) * 32 + lane] = make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+// round(w / s) to the nearest whole number, ties to even, of the exact quotient (|w / s| below 2^20): the
+// first guess is off by one at most where the quotient lies next to a border, and the rest w - q s is
+// exact in 32 bits.
+__device__ __forceinline__ float round_quotient(float w, float s, float inv) {
+  float q = rintf(inv > 0.0f ? w * inv : w / s);
+  const float r = fmaf(-q, s, w), twice = 2.0f * fabsf(r);
+  if (twice > s || (twice == s && ((int)q & 1))) q += r > 0.0f ? 1.0f : -1.0f;
+  return q;
+}
+
+// Thread (row r, 16 columns c ..): the scale of its group over 2, 4 or 8 neighbouring threads, then its codes.
+template <class T>
+__global__ void __launch_bounds__(kLayThreads)
+w4_quantize_kernel(const T *w, const xnor_w4_desc d, int pieces, uint32_t *w_packed, float *scales, uint8_t *zeros) {
+  __shared__ uint32_t part[kW4Rows][kQuads + 1];
+  stream_order();
+  const int r = threadIdx.x / 8, c = threadIdx.x % 8;
+  const int n = blockIdx.y * kW4Rows + r, k = blockIdx.x * kLayCols + 16 * c;
+  float v[16];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int kk = k + 8 * i, in = n < d.N ? min(8, max(0, d.K - kk)) : 0;
+    Chunk<T> a;
+    a.load(w + (in > 0 ? (size_t)n * d.K + kk : 0), pieces, in);
+    a.to_float(v + 8 * i);
+  }
+  // extremes of the group; NaN and infinity make its scale such, and its codes those of zero
+  float lo = 0.0f, hi = 0.0f;
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    lo = fminf(lo, v[i]);
+    hi = fmaxf(hi, v[i]);
+    nan |= v[i] != v[i];
+  }
+  if (nan) hi = __int_as_float(0x7FC00000);
+  const int lanes = d.group / 16;
+  for (int o = 1; o < lanes; o *= 2) {
+    const float ol = __shfl_xor_sync(0xffffffffu, lo, o), oh = __shfl_xor_sync(0xffffffffu, hi, o);
+    lo = fminf(lo, ol);
+    hi = (hi != hi || oh != oh) ? __int_as_float(0x7FC00000) : fmaxf(hi, oh);
+  }
+  float s, z = 8.0f;
+  if (zeros) s = (float)(((double)hi - (double)lo) / 15.0);
+  else s = hi != hi ? hi : __fdiv_rn(fmaxf(-lo, hi), 7.0f);
+  const bool sound = s > 0.0f && s <= 3.402823466e38f;
+  const float inv = sound && s > 1e-37f ? 1.0f / s : 0.0f;      // 0: it would overflow
+  if (zeros) z = sound ? fminf(15.0f, fmaxf(0.0f, round_quotient(-lo, s, inv))) : 8.0f;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    uint32_t code[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float u = sound ? round_quotient(v[4 * q + i], s, inv) + z : z;
+      code[i] = (uint32_t)fminf(15.0f, fmaxf(0.0f, u));
+    }
+    part[r][4 * c + q] = w4_spread(code[0], code[1], code[2], code[3]);
+  }
+  if (n < d.N && k < d.K && c % lanes == 0) {
+    const size_t at = (size_t)(k / d.group) * d.N + n;
+    scales[at] = s;
+    if (zeros) zeros[at] = (uint8_t)z;
+  }
+  __syncthreads();
+  write_tiles(part, blockIdx.y, blockIdx.x * 2, (d.K + kW4Cols - 1) / kW4Cols, w_packed);
+}
+
+__global__ void __launch_bounds__(kLayThreads)
+w4_pack_kernel(const uint8_t *codes, const xnor_w4_desc d, uint32_t *w_packed) {
+  __shared__ uint32_t part[kW4Rows][kQuads + 1];
+  stream_order();
+  const int r = threadIdx.x / 8, c = threadIdx.x % 8;
+  const int n = blockIdx.y * kW4Rows + r, k = blockIdx.x * kLayCols + 16 * c;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    uint32_t code[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int kk = k + 4 * q + i;
+      code[i] = n < d.N && kk < d.K ? load_global(codes + (size_t)n * d.K + kk) & 15u : 8u;
+    }
+    part[r][4 * c + q] = w4_spread(code[0], code[1], code[2], code[3]);
+  }
+  __syncthreads();
+  write_tiles(part, blockIdx.y, blockIdx.x * 2, (d.K + kW4Cols - 1) / kW4Cols, w_packed);
+}
+
+template <class T>
+__global__ void __launch_bounds__(kLayThreads)
+w4_dequantize_kernel(const uint32_t *w_packed, const float *scales, const uint8_t *zeros, const xnor_w4_desc d,
+                     int pieces, T *w) {
+  __shared__ uint32_t words[2][32][5];
+  stream_order();
+  const int col_tiles = (d.K + kW4Cols - 1) / kW4Cols;
+  if (threadIdx.x < 64) {
+    const int tile = threadIdx.x / 32, lane = threadIdx.x & 31, ct = blockIdx.x * 2 + tile;
+    if (ct < col_tiles) {
+      const uint4 v = load_global(reinterpret_cast<const uint4 *>(w_packed) + ((size_t)blockIdx.y * col_tiles + ct) * 32 + lane);
+      words[tile][lane][0] = v.x; words[tile][lane][1] = v.y; words[tile][lane][2] = v.z; words[tile][lane][3] = v.w;
+    }
+  }
+  __syncthreads();
+  const int r = threadIdx.x / 8, c = threadIdx.x % 8;
+  const int n = blockIdx.y * kW4Rows + r, k = blockIdx.x * kLayCols + 16 * c;
+  if (n >= d.N || k >= d.K) return;
+  const size_t at = (size_t)(k / d.group) * d.N + n;         // 16 columns lie in one group
+  const float s = load_global(scales + at);
+  const int z = zeros ? (int)load_global(zeros + at) : 8;
+  const uint32_t up = r < 8 ? 0u : 4u;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {                              // eight columns: words j and j + 1 of lane t
+    const int col = 16 * (c & 3) + 8 * h, t = (col & 31) / 8, j = 2 * (col / 32), lane = 4 * (r & 7) + t;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t word = words[c / 4][lane][j + i / 4] >> up;
+      const int shift = ((i & 1) << 4) | ((i & 2) << 2);
+      v[i] = (float)((int)((word >> shift) & 15u) - z) * s;
+    }
+    Chunk<T> a;
+    a.from_float(v);
+    a.store(w + (size_t)n * d.K + k + 8 * h, pieces, min(8, max(0, d.K - (k + 8 * h))));
+  }
+}
+
+// ---- a few rows ---------------------------------------------------------------------------
+// out[t][n] = x_scale[t] sum over groups of scale[g][n] sum over the group of (code - zero)[n][k] x[t][k].
+// Codes minus zeros and the rows' values are exact 16-bit operands of m16n8k16 products summed in 32 bits: 16
+// weight rows against 8 rows of x per step, whatever few of those exist (no extra traffic: the lanes of missing
+// rows read the last one).  Bound by the weights' bytes.  A block has 16 weight rows; its warps and the
+// blocks of its cluster divide the columns, and add their sums in shared memory in a fixed order.
+constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;
+constexpr int kMaxSplit = 8;
+
+template <class T>
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t a[4], uint32_t b0, uint32_t b1) {
+  if constexpr (std::is_same<T, __half>::value)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Eight values of x as four 16-bit pairs.  Bytes: int8 and e4m3 become 16-bit floats, exactly.
+template <int kType>
+struct RowsOf {
+  using T = __half;                       // the products' type
+  static constexpr int kBytes = 1;
+};
+template <> struct RowsOf<XNOR_BF16> { using T = __nv_bfloat16; static constexpr int kBytes = 2; };
+template <> struct RowsOf<XNOR_F16> { using T = __half; static constexpr int kBytes = 2; };
+
+template <int kType>
+__device__ __forceinline__ void load_x8(const uint8_t *row, int k, int K, bool pieces, uint32_t v[4]) {
+  constexpr int kB = RowsOf<kType>::kBytes;
+  const uint8_t *p = row + (size_t)k * kB;
+  uint32_t raw[2 * kB];
+  if (pieces && k + 8 <= K) {
+    if constexpr (kB == 2) {
+      const uint4 q = load_global(reinterpret_cast<const uint4 *>(p));
+      raw[0] = q.x; raw[1] = q.y; raw[2] = q.z; raw[3] = q.w;
+    } else {
+      const uint2 q = load_global(reinterpret_cast<const uint2 *>(p));
+      raw[0] = q.x; raw[1] = q.y;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2 * kB; ++i) raw[i] = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (k + i >= K) continue;
+      if constexpr (kB == 2) raw[i / 2] |= (uint32_t)load_global(reinterpret_cast<const uint16_t *>(p) + i) << (16 * (i & 1));
+      else raw[i / 4] |= (uint32_t)load_global(p + i) << (8 * (i & 3));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (kB == 2) v[i] = raw[i];
+    else if constexpr (kType == XNOR_I8) v[i] = i8_pair(raw[i / 2], i & 1);
+    else v[i] = e4m3_pair((raw[i / 2] >> (16 * (i & 1))) & 0xFFFFu);
+  }
+}
+
+// kN: blocks of eight rows of x that share the weights in registers.
+template <int kType, int kN>
+__global__ void __launch_bounds__(kFewThreads)
+w4_few_rows_kernel(const W4Args A, int pieces) {
+  using T = typename RowsOf<kType>::T;
+  constexpr int kTok = 8 * kN;
+  __shared__ float part[kFewWarps][kW4Rows][kTok + 1];
+  __shared__ float sums[kTok][kW4Rows];
+  stream_order();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const int N = A.d.N, K = A.d.K, group = A.d.group;
+  const int col_tiles = (K + kW4Cols - 1) / kW4Cols;
+  const int split = gridDim.x, rank = blockIdx.x;           // blocks of the cluster
+  const int row_tile = blockIdx.y;
+  const int n0 = row_tile * kW4Rows;
+  const long long tok0 = (long long)blockIdx.z * kTok;
+  const int slices = split * kFewWarps, slice = rank * kFewWarps + warp;
+  const int ct0 = (int)((long long)col_tiles * slice / slices), ct1 = (int)((long long)col_tiles * (slice + 1) / slices);
+  const int na = min(n0 + g, N - 1), nb = min(n0 + g + 8, N - 1);
+  const uint8_t *xrow[kN];
+#pragma unroll
+  for (int i = 0; i < kN; ++i)
+    xrow[i] = static_cast<const uint8_t *>(A.x) + min(tok0 + 8 * i + g, (long long)A.r.rows - 1) * A.r.x_stride * RowsOf<kType>::kBytes;
+  const uint4 *w = reinterpret_cast<const uint4 *>(A.w) + (size_t)row_tile * col_tiles * 32 + lane;
+  const bool x_groups = A.x_scales != nullptr && A.r.x_group != 0;
+  const int x_ngroups = (K + group - 1) / group;
+  float total[kN][4] = {};
+  for (int ct = ct0; ct < ct1; ++ct) {
+    const uint4 word = load_global(w + (size_t)ct * 32);
+    const uint32_t words[4] = {word.x, word.y, word.z, word.w};
+    uint32_t xv[kN][2][4];
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      load_x8<kType>(xrow[i], ct * kW4Cols + 8 * t, K, pieces, xv[i][0]);
+      load_x8<kType>(xrow[i], ct * kW4Cols + 32 + 8 * t, K, pieces, xv[i][1]);
+    }
+    float acc[kN][4] = {};
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int k = ct * kW4Cols + 32 * half, grp = min(k, K - 1) / group;
+      const size_t at = (size_t)grp * N;
+      const uint32_t za = w4_zero(A.zeros ? (uint32_t)load_global(A.zeros + at + na) : 8u, T());
+      const uint32_t zb = w4_zero(A.zeros ? (uint32_t)load_global(A.zeros + at + nb) : 8u, T());
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+        const uint32_t v = words[2 * half + jj];
+        const uint32_t a[4] = {w4_pair(v, 0, T(), za), w4_pair(v, 1, T(), zb), w4_pair(v, 2, T(), za), w4_pair(v, 3, T(), zb)};
+#pragma unroll
+        for (int i = 0; i < kN; ++i) mma_16x8x16<T>(acc[i], a, xv[i][half][2 * jj], xv[i][half][2 * jj + 1]);
+      }
+      if (half == 1 || group == 32) {
+        const float sa = load_global(A.scales + at + na), sb = load_global(A.scales + at + nb);
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+          float s0 = 1.0f, s1 = 1.0f;
+          if (x_groups) {
+            const long long t0 = min(tok0 + 8 * i + 2 * t, (long long)A.r.rows - 1), t1 = min(tok0 + 8 * i + 2 * t + 1, (long long)A.r.rows - 1);
+            s0 = load_global(A.x_scales + t0 * x_ngroups + grp);
+            s1 = load_global(A.x_scales + t1 * x_ngroups + grp);
+          }
+          total[i][0] = fmaf(acc[i][0] * s0, sa, total[i][0]);
+          total[i][1] = fmaf(acc[i][1] * s1, sa, total[i][1]);
+          total[i][2] = fmaf(acc[i][2] * s0, sb, total[i][2]);
+          total[i][3] = fmaf(acc[i][3] * s1, sb, total[i][3]);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) acc[i][q] = 0.0f;
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    part[warp][g][8 * i + 2 * t] = total[i][0];
+    part[warp][g][8 * i + 2 * t + 1] = total[i][1];
+    part[warp][g + 8][8 * i + 2 * t] = total[i][2];
+    part[warp][g + 8][8 * i + 2 * t + 1] = total[i][3];
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < kTok * kW4Rows; e += kFewThreads) {
+    const int n = e % kW4Rows, tok = e / kW4Rows;
+    float s = part[0][n][tok];
+#pragma unroll
+    for (int i = 1; i < kFewWarps; ++i) s += part[i][n][tok];
+    sums[tok][n] = s;
+  }
+  if (split > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  else __syncthreads();
+  // the cluster's blocks write the outputs in turn; each adds the blocks' sums in the same order
+  for (int e = rank * kFewThreads + threadIdx.x; e < kTok * kW4Rows; e += split * kFewThreads) {
+    const int n = e % kW4Rows, tok = e / kW4Rows;
+    float s = 0.0f;
+    if (split == 1) s = sums[tok][n];
+    else
+      for (int i = 0; i < split; ++i) {
+        uint32_t a;
+        float v;
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(&sums[tok][n])), "r"(i));
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+        s += v;
+      }
+    const long long row = tok0 + tok;
+    if (row >= A.r.rows || n0 + n >= N) continue;
+    if (A.x_scales != nullptr && !x_groups) s *= load_global(A.x_scales + row);
+    const size_t at = (size_t)(row * A.r.out_stride) + n0 + n;
+    if (A.r.out_type == XNOR_F32) static_cast<float *>(A.out)[at] = s;
+    else if (A.r.out_type == XNOR_BF16) static_cast<__nv_bfloat16 *>(A.out)[at] = __float2bfloat16_rn(s);
+    else static_cast<__half *>(A.out)[at] = __float2half_rn(s);
+  }
+  if (split > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+template <int kType>
+cudaError_t few_rows(const W4Args &a, cudaStream_t st) {
+  const int row_tiles = w4_row_tiles(a.d), col_tiles = w4_col_tiles(a.d);
+  // blocks of a cluster divide the columns while the blocks are fewer than the GPU takes at once and
+  // every warp keeps two tiles
+  int split = 1;
+  while (split < kMaxSplit && row_tiles * split < 2 * sm_count_of_current_device() && col_tiles >= 4 * split * kFewWarps) split *= 2;
+  const int pieces = rows_in_pieces(a.x, a.r.x_stride, 8, RowsOf<kType>::kBytes);
+  const int n = a.r.rows > 8 ? 2 : 1;
+  const long long token_blocks = (a.r.rows + 8ll * n - 1) / (8 * n);
+  // (a grid has at most 65535 blocks along y and z)
+  const dim3 grid((unsigned)split, (unsigned)row_tiles, (unsigned)token_blocks);
+  if (n == 1) return launch_kernel(w4_few_rows_kernel<kType, 1>, grid, kFewThreads, 0, st, (unsigned)split, a, pieces);
+  return launch_kernel(w4_few_rows_kernel<kType, 2>, grid, kFewThreads, 0, st, (unsigned)split, a, pieces);
+}
+
+dim3 lay_grid(const xnor_w4_desc &d) { return dim3((unsigned)((w4_col_tiles(d) + 1) / 2), (unsigned)w4_row_tiles(d)); }
+
+}  // namespace
+
+cudaError_t launch_w4_quantize(const void *w, int type, const xnor_w4_desc &d, uint32_t *w_packed, float *scales,
+                               uint8_t *zeros, cudaStream_t st) {
+  const int pieces = d.K % 8 == 0;
+  if (type == XNOR_F32)
+    return launch_kernel(w4_quantize_kernel<float>, lay_grid(d), kLayThreads, 0, st, 1, (const float *)w, d, pieces, w_packed, scales, zeros);
+  if (type == XNOR_BF16)
+    return launch_kernel(w4_quantize_kernel<__nv_bfloat16>, lay_grid(d), kLayThreads, 0, st, 1, (const __nv_bfloat16 *)w, d, pieces, w_packed, scales, zeros);
+  return launch_kernel(w4_quantize_kernel<__half>, lay_grid(d), kLayThreads, 0, st, 1, (const __half *)w, d, pieces, w_packed, scales, zeros);
+}
+
+cudaError_t launch_w4_pack(const uint8_t *codes, const xnor_w4_desc &d, uint32_t *w_packed, cudaStream_t st) {
+  return launch_kernel(w4_pack_kernel, lay_grid(d), kLayThreads, 0, st, 1, codes, d, w_packed);
+}
+
+cudaError_t launch_w4_dequantize(const uint32_t *w_packed, const float *scales, const uint8_t *zeros,
+                                 const xnor_w4_desc &d, int type, void *w, cudaStream_t st) {
+  const int pieces = d.K % 8 == 0;
+  if (type == XNOR_F32)
+    return launch_kernel(w4_dequantize_kernel<float>, lay_grid(d), kLayThreads, 0, st, 1, w_packed, scales, zeros, d, pieces, (float *)w);
+  if (type == XNOR_BF16)
+    return launch_kernel(w4_dequantize_kernel<__nv_bfloat16>, lay_grid(d), kLayThreads, 0, st, 1, w_packed, scales, zeros, d, pieces, (__nv_bfloat16 *)w);
+  return launch_kernel(w4_dequantize_kernel<__half>, lay_grid(d), kLayThreads, 0, st, 1, w_packed, scales, zeros, d, pieces, (__half *)w);
+}
+
+cudaError_t launch_w4_few_rows(const W4Args &a, cudaStream_t st) {
+  if (a.r.rows == 0) return cudaSuccess;
+  switch (a.r.x_type) {
+    case XNOR_BF16: return few_rows<XNOR_BF16>(a, st);
+    case XNOR_F16: return few_rows<XNOR_F16>(a, st);
+    case XNOR_I8: return few_rows<XNOR_I8>(a, st);
+    default: return few_rows<XNOR_E4M3>(a, st);
+  }
+}
+
+}  // namespace xnor

@@ -263,3 +263,41 @@ class ChainRunner:
 
     def macs(self):
         return sum(wl.macs(s) for s in self.shapes)
+
+
+class TokenBlock:
+    """Buffers and calls of a projection in a decoder's layer: the residual's addition, the norm, and the product
+    with 4-bit weights, on bfloat16 rows of tokens.
+
+    quant: None (the product reads the norm in bfloat16), "i8" or "e4m3" (in 8 bits, one scale for each row),
+    "i8_groups" or "e4m3_groups" (a scale for each of the weights' groups)."""
+
+    def __init__(self, rows, K, N, group=128, zeros=False, quant=None, eps=1e-5, device="cuda"):
+        bf16 = dict(dtype=torch.bfloat16, device=device)
+        self.eps, self.d = eps, B.make_w4_desc(N, K, group)
+        self.x, self.residual = torch.empty((rows, K), **bf16), torch.empty((rows, K), **bf16)
+        self.weight = torch.ones((K,), dtype=torch.float32, device=device)
+        self.packed, self.scales, self.zeros = B.alloc_w4(self.d, zeros, device)
+        self.out = torch.empty((rows, N), **bf16)
+        self.y = self.q = self.q_scales = None
+        self.q_group = group if quant and quant.endswith("_groups") else 0
+        if quant is None:
+            self.y = torch.empty((rows, K), **bf16)
+        else:
+            t = torch.int8 if quant.startswith("i8") else torch.float8_e4m3fn
+            self.q, self.q_scales = B.alloc_rmsnorm_quant(rows, K, self.q_group, t, device)
+
+    def load(self, w, stream=None):
+        """Real weights [N][K], quantised."""
+        B.xnor_w4_quantize(w, self.d, self.packed, self.scales, self.zeros, stream)
+
+    def forward(self, stream=None):
+        """residual += x, out = norm(residual) times the weights."""
+        if self.q is None:
+            B.xnor_rmsnorm(self.x, self.residual, self.weight, self.eps, self.residual, self.y, None, stream)
+        else:
+            B.xnor_rmsnorm_quant(self.x, self.residual, self.weight, self.eps, self.q_group, self.residual, self.q,
+                                 self.q_scales, None, stream)
+        B.xnor_w4_matmul(self.y if self.q is None else self.q, self.q_scales, self.packed, self.scales, self.zeros,
+                         self.d, self.out, stream)
+        return self.out
