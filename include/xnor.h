@@ -483,9 +483,9 @@ xnor_status xnor_rmsnorm_backward(const void *dy, const void *dsum, const void *
  * group may be shorter): w = (code - zero) scale.
  *
  *   w_packed  u32 [ceil(N/16)][ceil(K/64)][32][4]: tiles of 16 rows x 64 columns.  Element
- *             [.][.][4 g + t][j] holds the codes of rows g (bits 0, 16, 8, 24 and up) and g + 8 (bits
- *             4, 20, 12, 28 and up), columns 32 (j/2) + 8 t + 4 (j%2) + 0, 1, 2, 3 of the tile; rows
- *             and columns beyond the matrix hold any code.
+ *             [.][.][4 g + t][2 r + c] holds row g + 8 r, columns 32 c + 8 t + 0 .. 7 of the tile, column
+ *             2 i + h of the eight in bits 4 i + 16 h and up; rows and columns beyond the matrix
+ *             hold any code.
  *   scales    fp32 [ceil(K/group)][N]
  *   zeros     u8   [ceil(K/group)][N], 0 .. 15, or NULL: 8 everywhere
  * xnor_w4_quantize   w type [N][K] (F32, BF16, F16) -> w_packed, scales, zeros.

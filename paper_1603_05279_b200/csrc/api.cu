@@ -335,15 +335,16 @@ xnor_status xnor_selftest_wait_timeout(void *cuda_stream) {
 }
 
 xnor_status xnor_check_device(void *cuda_stream) {
-  int st = 0, st2 = 0, st3 = 0, st4 = 0;
+  int st = 0, st2 = 0, st3 = 0, st4 = 0, st5 = 0;
   if (cudaStreamSynchronize((cudaStream_t)cuda_stream) != cudaSuccess ||
       xnor::read_status_tc(&st) != cudaSuccess || xnor::read_status_bwn(&st2) != cudaSuccess ||
-      xnor::read_status_act(&st3) != cudaSuccess || xnor::read_status_pool(&st4) != cudaSuccess) {
+      xnor::read_status_act(&st3) != cudaSuccess || xnor::read_status_pool(&st4) != cudaSuccess ||
+      xnor::read_status_w4(&st5) != cudaSuccess) {
     (void)cudaGetLastError();
     return XNOR_ERR_CUDA;
   }
   if (st >= 1000) return XNOR_ERR_BOUNDS;
-  return (st == 0 && st2 == 0 && st3 == 0 && st4 == 0) ? XNOR_OK : XNOR_ERR_TIMEOUT;
+  return (st == 0 && st2 == 0 && st3 == 0 && st4 == 0 && st5 == 0) ? XNOR_OK : XNOR_ERR_TIMEOUT;
 }
 
 xnor_status xnor_measure_peaks(double *mma_mac_per_clk_per_sm, double *popc_per_clk_per_sm,
@@ -549,7 +550,9 @@ xnor_status xnor_w4_matmul(const void *x, const float *x_scales, const uint32_t 
     return XNOR_ERR_INVALID_ARG;
   if (large_w4(d) || r->rows > 16 * 65535 || r->x_type == XNOR_F32 || (bytes && r->x_group != 0 && r->x_group != d->group))
     return XNOR_ERR_UNSUPPORTED;
-  return from_cuda(xnor::launch_w4_few_rows({x, x_scales, w_packed, scales, zeros, out, *d, *r}, (cudaStream_t)cuda_stream));
+  const xnor::W4Args a = {x, x_scales, w_packed, scales, zeros, out, *d, *r};
+  return from_cuda(r->rows <= xnor::kW4FewRows ? xnor::launch_w4_few_rows(a, (cudaStream_t)cuda_stream)
+                                               : xnor::launch_w4_many_rows(a, (cudaStream_t)cuda_stream));
 }
 
 xnor_status xnor_shortcut_conv1x1(const float *x, const float *w, int N, int C_in, int H, int W,

@@ -161,5 +161,8 @@ struct W4Args {
   xnor_w4_rows r;
 };
 cudaError_t launch_w4_few_rows(const W4Args &a, cudaStream_t st);
+cudaError_t launch_w4_many_rows(const W4Args &a, cudaStream_t st);
+cudaError_t read_status_w4(int *status);   // of the kernel for many rows, as the others'
+constexpr int kW4FewRows = 16;             // up to here the kernel for few rows
 
 }  // namespace xnor

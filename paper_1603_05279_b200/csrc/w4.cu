@@ -12,19 +12,15 @@ namespace {
 // ---- layout -------------------------------------------------------------------------------
 constexpr int kLayThreads = 128;
 constexpr int kLayCols = 2 * kW4Cols;      // a block: 16 rows x 128 columns, the largest group; a thread: 16 columns
-constexpr int kQuads = kLayCols / 4;
+constexpr int kOctets = kLayCols / 8;
 
-// Codes of the block, spread (w4_spread), [16 rows][quads of columns], to the packed tiles.
-__device__ __forceinline__ void write_tiles(const uint32_t (&part)[kW4Rows][kQuads + 1], int row_tile, int col_tile0,
+// Words of the block, [16 rows][groups of eight columns], to the packed tiles.
+__device__ __forceinline__ void write_tiles(const uint32_t (&words)[kW4Rows][kOctets + 1], int row_tile, int col_tile0,
                                             int col_tiles, uint32_t *w) {
   const int tile = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   if (tile >= 2 || col_tile0 + tile >= col_tiles) return;
-  uint32_t v[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int q = 16 * tile + w4_column(t, j) / 4;
-    v[j] = part[g][q] | part[g + 8][q] << 4;
-  }
+  const int c = 8 * tile + t;
+  const uint32_t v[4] = {words[g][c], words[g][c + 4], words[g + 8][c], words[g + 8][c + 4]};
   reinterpret_cast<uint4 *>(w)[((size_t)row_tile * col_tiles + col_tile0 + tile) * 32 + lane] = make_uint4(v[0], v[1], v[2], v[3]);
 }
 
@@ -42,7 +38,7 @@ __device__ __forceinline__ float round_quotient(float w, float s, float inv) {
 template <class T>
 __global__ void __launch_bounds__(kLayThreads)
 w4_quantize_kernel(const T *w, const xnor_w4_desc d, int pieces, uint32_t *w_packed, float *scales, uint8_t *zeros) {
-  __shared__ uint32_t part[kW4Rows][kQuads + 1];
+  __shared__ uint32_t words[kW4Rows][kOctets + 1];
   stream_order();
   const int r = threadIdx.x / 8, c = threadIdx.x % 8;
   const int n = blockIdx.y * kW4Rows + r, k = blockIdx.x * kLayCols + 16 * c;
@@ -77,14 +73,14 @@ w4_quantize_kernel(const T *w, const xnor_w4_desc d, int pieces, uint32_t *w_pac
   const float inv = sound && s > 1e-37f ? 1.0f / s : 0.0f;      // 0: it would overflow
   if (zeros) z = sound ? fminf(15.0f, fmaxf(0.0f, round_quotient(-lo, s, inv))) : 8.0f;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    uint32_t code[4];
+  for (int q = 0; q < 2; ++q) {
+    uint32_t word = 0u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float u = sound ? round_quotient(v[4 * q + i], s, inv) + z : z;
-      code[i] = (uint32_t)fminf(15.0f, fmaxf(0.0f, u));
+    for (int i = 0; i < 8; ++i) {
+      const float u = sound ? round_quotient(v[8 * q + i], s, inv) + z : z;
+      word |= (uint32_t)fminf(15.0f, fmaxf(0.0f, u)) << w4_bit(i);
     }
-    part[r][4 * c + q] = w4_spread(code[0], code[1], code[2], code[3]);
+    words[r][2 * c + q] = word;
   }
   if (n < d.N && k < d.K && c % lanes == 0) {
     const size_t at = (size_t)(k / d.group) * d.N + n;
@@ -92,27 +88,27 @@ w4_quantize_kernel(const T *w, const xnor_w4_desc d, int pieces, uint32_t *w_pac
     if (zeros) zeros[at] = (uint8_t)z;
   }
   __syncthreads();
-  write_tiles(part, blockIdx.y, blockIdx.x * 2, (d.K + kW4Cols - 1) / kW4Cols, w_packed);
+  write_tiles(words, blockIdx.y, blockIdx.x * 2, (d.K + kW4Cols - 1) / kW4Cols, w_packed);
 }
 
 __global__ void __launch_bounds__(kLayThreads)
 w4_pack_kernel(const uint8_t *codes, const xnor_w4_desc d, uint32_t *w_packed) {
-  __shared__ uint32_t part[kW4Rows][kQuads + 1];
+  __shared__ uint32_t words[kW4Rows][kOctets + 1];
   stream_order();
   const int r = threadIdx.x / 8, c = threadIdx.x % 8;
   const int n = blockIdx.y * kW4Rows + r, k = blockIdx.x * kLayCols + 16 * c;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    uint32_t code[4];
+  for (int q = 0; q < 2; ++q) {
+    uint32_t word = 0u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int kk = k + 4 * q + i;
-      code[i] = n < d.N && kk < d.K ? load_global(codes + (size_t)n * d.K + kk) & 15u : 8u;
+    for (int i = 0; i < 8; ++i) {
+      const int kk = k + 8 * q + i;
+      word |= (n < d.N && kk < d.K ? load_global(codes + (size_t)n * d.K + kk) & 15u : 8u) << w4_bit(i);
     }
-    part[r][4 * c + q] = w4_spread(code[0], code[1], code[2], code[3]);
+    words[r][2 * c + q] = word;
   }
   __syncthreads();
-  write_tiles(part, blockIdx.y, blockIdx.x * 2, (d.K + kW4Cols - 1) / kW4Cols, w_packed);
+  write_tiles(words, blockIdx.y, blockIdx.x * 2, (d.K + kW4Cols - 1) / kW4Cols, w_packed);
 }
 
 template <class T>
@@ -136,17 +132,13 @@ w4_dequantize_kernel(const uint32_t *w_packed, const float *scales, const uint8_
   const size_t at = (size_t)(k / d.group) * d.N + n;         // 16 columns lie in one group
   const float s = load_global(scales + at);
   const int z = zeros ? (int)load_global(zeros + at) : 8;
-  const uint32_t up = r < 8 ? 0u : 4u;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {                              // eight columns: words j and j + 1 of lane t
-    const int col = 16 * (c & 3) + 8 * h, t = (col & 31) / 8, j = 2 * (col / 32), lane = 4 * (r & 7) + t;
+  for (int h = 0; h < 2; ++h) {
+    const int col = 16 * (c & 3) + 8 * h;
+    const uint32_t word = words[c / 4][w4_lane(r, col)][w4_word(r, col)];
     float v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t word = words[c / 4][lane][j + i / 4] >> up;
-      const int shift = ((i & 1) << 4) | ((i & 2) << 2);
-      v[i] = (float)((int)((word >> shift) & 15u) - z) * s;
-    }
+    for (int i = 0; i < 8; ++i) v[i] = (float)((int)((word >> w4_bit(i)) & 15u) - z) * s;
     Chunk<T> a;
     a.from_float(v);
     a.store(w + (size_t)n * d.K + k + 8 * h, pieces, min(8, max(0, d.K - (k + 8 * h))));
@@ -170,46 +162,6 @@ __device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t a[4], 
   else
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-// Eight values of x as four 16-bit pairs.  Bytes: int8 and e4m3 become 16-bit floats, exactly.
-template <int kType>
-struct RowsOf {
-  using T = __half;                       // the products' type
-  static constexpr int kBytes = 1;
-};
-template <> struct RowsOf<XNOR_BF16> { using T = __nv_bfloat16; static constexpr int kBytes = 2; };
-template <> struct RowsOf<XNOR_F16> { using T = __half; static constexpr int kBytes = 2; };
-
-template <int kType>
-__device__ __forceinline__ void load_x8(const uint8_t *row, int k, int K, bool pieces, uint32_t v[4]) {
-  constexpr int kB = RowsOf<kType>::kBytes;
-  const uint8_t *p = row + (size_t)k * kB;
-  uint32_t raw[2 * kB];
-  if (pieces && k + 8 <= K) {
-    if constexpr (kB == 2) {
-      const uint4 q = load_global(reinterpret_cast<const uint4 *>(p));
-      raw[0] = q.x; raw[1] = q.y; raw[2] = q.z; raw[3] = q.w;
-    } else {
-      const uint2 q = load_global(reinterpret_cast<const uint2 *>(p));
-      raw[0] = q.x; raw[1] = q.y;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 2 * kB; ++i) raw[i] = 0u;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (k + i >= K) continue;
-      if constexpr (kB == 2) raw[i / 2] |= (uint32_t)load_global(reinterpret_cast<const uint16_t *>(p) + i) << (16 * (i & 1));
-      else raw[i / 4] |= (uint32_t)load_global(p + i) << (8 * (i & 3));
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (kB == 2) v[i] = raw[i];
-    else if constexpr (kType == XNOR_I8) v[i] = i8_pair(raw[i / 2], i & 1);
-    else v[i] = e4m3_pair((raw[i / 2] >> (16 * (i & 1))) & 0xFFFFu);
-  }
 }
 
 // kN: blocks of eight rows of x that share the weights in registers.
@@ -255,14 +207,14 @@ w4_few_rows_kernel(const W4Args A, int pieces) {
       const size_t at = (size_t)grp * N;
       const uint32_t za = w4_zero(A.zeros ? (uint32_t)load_global(A.zeros + at + na) : 8u, T());
       const uint32_t zb = w4_zero(A.zeros ? (uint32_t)load_global(A.zeros + at + nb) : 8u, T());
+      const uint32_t va = words[half], vb = words[2 + half];
 #pragma unroll
       for (int jj = 0; jj < 2; ++jj) {
-        const uint32_t v = words[2 * half + jj];
-        const uint32_t a[4] = {w4_pair(v, 0, T(), za), w4_pair(v, 1, T(), zb), w4_pair(v, 2, T(), za), w4_pair(v, 3, T(), zb)};
+        const uint32_t a[4] = {w4_pair(va, 2 * jj, T(), za), w4_pair(vb, 2 * jj, T(), zb), w4_pair(va, 2 * jj + 1, T(), za), w4_pair(vb, 2 * jj + 1, T(), zb)};
 #pragma unroll
         for (int i = 0; i < kN; ++i) mma_16x8x16<T>(acc[i], a, xv[i][half][2 * jj], xv[i][half][2 * jj + 1]);
       }
-      if (half == 1 || group == 32) {
+      if ((half == 1 || group == 32) && (k < K || group != 32)) {       // (groups of 32: the second may not exist)
         const float sa = load_global(A.scales + at + na), sb = load_global(A.scales + at + nb);
 #pragma unroll
         for (int i = 0; i < kN; ++i) {

@@ -1,26 +1,24 @@
 // The layout of 4-bit weights (internal).
 //
 // Codes 0 .. 15 lie in tiles of 16 rows x 64 columns, 512 bytes: u32 [row tiles][column tiles][32 lanes][4].
-// Lane 4 g + t (g = 0 .. 7, t = 0 .. 3) holds rows g and g + 8 of the tile; its word j columns
-// w4_column(t, j) + i, i = 0 .. 3: row g's codes in bits 0, 16, 8, 24 and up, row g + 8's four bits above each.
-// So a lane's four words are what four m16n8k16 steps want of it in the matrix operand (the columns of a step,
-// in any order, only have to be the same as the rows' that they meet), a pair of neighbouring columns
-// becomes two 16-bit values with one mask, and words 0, 1 and 2, 3 each cover 32 neighbouring columns,
-// the smallest group.
+// A word holds eight neighbouring columns of one row, column 2 i + h in bits 4 i + 16 h and up: a mask brings two
+// neighbouring columns to where two 16-bit values have them.  Lane 4 g + t (g = 0 .. 7, t = 0 .. 3) holds, of
+// row g, columns 8 t .. and 32 + 8 t .., then the same of row g + 8.  So a lane's four words are what four
+// m16n8k16 steps want of it in the matrix operand (the columns of a step, in any order, only have to be the
+// same as those of the rows that they meet), two steps each for 32 neighbouring columns, the smallest group.
 #pragma once
 #include "rows.cuh"
 
 namespace xnor {
 
-__host__ __device__ __forceinline__ int w4_column(int t, int j) { return 32 * (j >> 1) + 8 * t + 4 * (j & 1); }
+// Lane and word of the tile that hold row r, columns c .. c + 7 (c a multiple of 8).
+__host__ __device__ __forceinline__ int w4_lane(int r, int c) { return 4 * (r & 7) + ((c & 31) >> 3); }
+__host__ __device__ __forceinline__ int w4_word(int r, int c) { return 2 * ((r >> 3) & 1) + (c >> 5); }
 
-// The part of a word that the four codes of one row make (for row g + 8: shifted up by four).
-__device__ __forceinline__ uint32_t w4_spread(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3) {
-  return c0 | c1 << 16 | c2 << 8 | c3 << 24;
-}
+__host__ __device__ __forceinline__ int w4_bit(int column) { return 4 * (column >> 1) + 16 * (column & 1); }
 
-// Two values of a word as 16-bit numbers code - zero, exact: pair 0, 1: columns 0 and 1 of rows g, g + 8; pair
-// 2, 3: columns 2 and 3.  A code put into the mantissa of 2^k is 2^k + code; `zero` holds (2^k + zero) twice.
+// Two values of a word, columns 2 pair and 2 pair + 1, as 16-bit numbers code - zero, exact.  A code put into the
+// mantissa of 2^k is 2^k + code; `zero` holds (2^k + zero) twice.
 __device__ __forceinline__ uint32_t w4_pair(uint32_t w, int pair, __nv_bfloat16, uint32_t zero) {
   const uint32_t v = ((w >> (4 * pair)) & 0x000F000Fu) | 0x43004300u;                    // 128 + code
   const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&v), *reinterpret_cast<const __nv_bfloat162 *>(&zero));
@@ -44,6 +42,46 @@ __device__ __forceinline__ uint32_t i8_pair(uint32_t four, int pair) {
 __device__ __forceinline__ uint32_t e4m3_pair(uint32_t two) {
   const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
   return (uint32_t)r.x | (uint32_t)r.y << 16;
+}
+
+// Eight values of x as four 16-bit pairs.  Bytes: int8 and e4m3 become 16-bit floats, exactly.
+template <int kType>
+struct RowsOf {
+  using T = __half;                       // the products' type
+  static constexpr int kBytes = 1;
+};
+template <> struct RowsOf<XNOR_BF16> { using T = __nv_bfloat16; static constexpr int kBytes = 2; };
+template <> struct RowsOf<XNOR_F16> { using T = __half; static constexpr int kBytes = 2; };
+
+template <int kType>
+__device__ __forceinline__ void load_x8(const uint8_t *row, int k, int K, bool pieces, uint32_t v[4]) {
+  constexpr int kB = RowsOf<kType>::kBytes;
+  const uint8_t *p = row + (size_t)k * kB;
+  uint32_t raw[2 * kB];
+  if (pieces && k + 8 <= K) {
+    if constexpr (kB == 2) {
+      const uint4 q = load_global(reinterpret_cast<const uint4 *>(p));
+      raw[0] = q.x; raw[1] = q.y; raw[2] = q.z; raw[3] = q.w;
+    } else {
+      const uint2 q = load_global(reinterpret_cast<const uint2 *>(p));
+      raw[0] = q.x; raw[1] = q.y;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2 * kB; ++i) raw[i] = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (k + i >= K) continue;
+      if constexpr (kB == 2) raw[i / 2] |= (uint32_t)load_global(reinterpret_cast<const uint16_t *>(p) + i) << (16 * (i & 1));
+      else raw[i / 4] |= (uint32_t)load_global(p + i) << (8 * (i & 3));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (kB == 2) v[i] = raw[i];
+    else if constexpr (kType == XNOR_I8) v[i] = i8_pair(raw[i / 2], i & 1);
+    else v[i] = e4m3_pair((raw[i / 2] >> (16 * (i & 1))) & 0xFFFFu);
+  }
 }
 
 }  // namespace xnor

@@ -90,11 +90,10 @@ def unpack_codes(packed, N, K):
     out = np.zeros((rt * 16, ct * 64), np.uint8)
     for lane in range(32):
         g, t = lane // 4, lane % 4
-        for j in range(4):
-            col = 32 * (j // 2) + 8 * t + 4 * (j % 2)
-            for up, row in ((0, g), (4, g + 8)):
-                for i, bit in enumerate((0, 16, 8, 24)):
-                    out[row::16, col + i::64] = (p[:, :, lane, j] >> np.uint32(bit + up)) & 15
+        for word in range(4):
+            row, col = g + 8 * (word // 2), 32 * (word % 2) + 8 * t
+            for i in range(8):
+                out[row::16, col + i::64] = (p[:, :, lane, word] >> np.uint32(4 * (i // 2) + 16 * (i % 2))) & 15
     return out[:N, :K]
 
 
@@ -107,11 +106,10 @@ def pack_codes(codes):
     p = np.zeros((rt, ct, 32, 4), np.uint32)
     for lane in range(32):
         g, t = lane // 4, lane % 4
-        for j in range(4):
-            col = 32 * (j // 2) + 8 * t + 4 * (j % 2)
-            for up, row in ((0, g), (4, g + 8)):
-                for i, bit in enumerate((0, 16, 8, 24)):
-                    p[:, :, lane, j] |= full[row::16, col + i::64] << np.uint32(bit + up)
+        for word in range(4):
+            row, col = g + 8 * (word // 2), 32 * (word % 2) + 8 * t
+            for i in range(8):
+                p[:, :, lane, word] |= full[row::16, col + i::64] << np.uint32(4 * (i // 2) + 16 * (i % 2))
     return torch.from_numpy(p.view(np.int32))
 
 

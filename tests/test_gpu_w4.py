@@ -176,7 +176,8 @@ def test_product_sizes(xname, group):
 
 
 @pytest.mark.parametrize("xname", ["bf16", "f16", "i8", "e4m3"])
-@pytest.mark.parametrize("T,N,K", [(1, 4096, 4096), (16, 2048, 1088), (40, 1024, 4096), (300, 512, 1024), (777, 384, 640), (2050, 136, 192)])
+@pytest.mark.parametrize("T,N,K", [(1, 4096, 4096), (16, 2048, 1088), (40, 1024, 4096), (300, 512, 1024), (777, 384, 640), (2050, 136, 192),
+                                   (300, 5000, 328), (1000, 2500, 1100)])
 def test_product_large(xname, T, N, K):
     x, xs, each, codes, scales, zs = operands(T, N, K, 128, T % 2 == 1, xname, T, T == 300)
     out = product(x, xs, codes, scales, zs, 128, torch.float32)
