@@ -7,16 +7,19 @@
 // are finished, are multiplied with the group's scale and added up in fp32 registers, so that no weight is
 // rounded: scaling the weights before the product would round each to the operands' 8 or 11 bits.
 //
-// A block (one per SM, persistent) computes 128 outputs x kRows rows.  A unit of work is one group and up to 128 rows:
-// the accumulators are two buffers of tensor memory, so that the tensor core fills one while the other is drained;
-// with 256 rows the buffers are the two halves of the rows, and an expanded group serves both.  (512 threads:)
-//   promotion  8 warps (256 rows) or 4: a thread holds the sums of one output row, 128 rows of x at most
-//   expansion  4 or 8 warps: a thread expands one weight row, 64 columns at a time, straight into tensor memory
-//   one warp issues the products, three bring the rows of x into a ring of stages of 64 columns
+// A block (one per SM, persistent) computes 128 outputs x kRows rows of x.  A unit of work is one group: its sums
+// have two buffers in tensor memory, so that the tensor core fills one while the other is drained.  16 or 20 warps:
+//   promotion  8 warps (4 up to 64 rows): a thread holds the sums of one output and up to 96 rows of x
+//   expansion  8 warps (4 with 192 rows): a thread expands one weight row, 64 columns at a time, straight into tensor memory
+//   one warp issues the products; one copies the rows of x, by tensor copies, into a ring of stages of 64 columns
+//   (where they cannot be copied as they are, three warps bring them through registers)
 // Where the tiles are too few for the GPU, the blocks of a cluster divide the columns, and add their sums through
 // each other's shared memory in a fixed order.  Every wait is bounded; on expiry the block records
 // XNOR_ERR_TIMEOUT, stops and frees its tensor memory.
+#include <cuda.h>
+
 #include <algorithm>
+#include <atomic>
 
 #include "umma_common.cuh"
 #include "w4.cuh"
@@ -29,35 +32,39 @@ namespace {
 
 using namespace umma;
 
-constexpr int kThreads = 512;
 constexpr int kTileN = 128;                  // outputs (weight rows) of a tile: the lanes of tensor memory
 constexpr int kChunk = 64;                   // columns of a stage
-constexpr int kMmaWarp = 12, kLoadWarp = 13, kLoadWarps = 3;
-constexpr int kABufs = 8, kACols = kChunk / 2;                 // expanded weights: 8 x 32 columns of tensor memory
-constexpr int kDCols = 128, kATmem = 2 * kDCols;               // behind the two accumulators
-constexpr int kMaxStages = 8;
+constexpr int kLoadWarps = 3;
+constexpr int kACols = kChunk / 2;           // tensor-memory columns of a chunk of expanded weights
+constexpr int kMaxABufs = 8, kStages = 8;
 constexpr uint32_t kCtrlBytes = 1024;
 constexpr int kMaxSplitTc = 8;
 
 template <int kRows>
 struct Shape {
-  static constexpr int kHalves = kRows > 128 ? 2 : 1;          // products of a unit: kUnit rows each
-  static constexpr int kUnit = kRows / kHalves;
-  static constexpr int kPromo = kHalves;                       // sets of four warps
-  static constexpr int kExpand = 3 - kHalves;
-  static constexpr uint32_t kPlane = kRows * 16 + 16;          // eight columns of all rows; 16 more keep the banks apart
-  static constexpr uint32_t kStage = 8 * kPlane;
-  static constexpr int kStages = kRows > 128 ? 6 : kMaxStages;
-  static constexpr uint32_t kScaleBytes = kPromo * 4 * 512;    // a group's scales of x, per promotion warp
-  static constexpr size_t kSmem = kCtrlBytes + kScaleBytes + (size_t)kStages * kStage;
-  static_assert(kSmem <= 232448, "shared memory");
-  static_assert(kHalves == 2 || (size_t)kStages * kStage >= (size_t)kRows * kTileN * 4, "room for the sums of a block");
+  static constexpr int kPromo = kRows > 64 ? 2 : 1;            // sets of four warps
+  static constexpr int kUnit = kRows / kPromo;                 // rows of x of a set
+  static constexpr int kExpand = kRows > 128 ? 1 : 2;
+  static constexpr int kMmaWarp = 4 * (kPromo + kExpand), kLoadWarp = kMmaWarp + 1;
+  static constexpr int kThreads = 32 * (kMmaWarp + 4);
+  static constexpr int kATmem = kRows > 128 ? 2 * kRows : 256; // behind the two accumulators
+  static constexpr int kABufs = (512 - kATmem) / kACols;
+  static constexpr uint32_t kStage = kRows * kChunk * 2;       // a row of x: 128 bytes, swizzled
+  static constexpr uint32_t kScaleBytes = 8 * 512;             // a group's scales of x, per promotion warp
+  static constexpr size_t kSmem = 1024 + kCtrlBytes + kScaleBytes + (size_t)kStages * kStage;   // (1024: to align the ring)
+  // Registers per thread as launched, and after they are dealt out anew: the promotion's hold its sums.
+  static constexpr int kRegs = kThreads == 512 ? 128 : 96;
+  static constexpr int kPromoRegs = kRows > 128 ? 152 : kRows > 64 ? 128 : 128, kOtherRegs = kRows > 128 ? 104 : kRows > 64 ? 72 : 128;
+  static_assert(kPromo * 128 * kPromoRegs + (kThreads - kPromo * 128) * kOtherRegs <= kThreads * kRegs, "registers");
+  static_assert(kSmem <= 232448 && kABufs <= kMaxABufs, "shared and tensor memory");
+  static_assert((size_t)kStages * kStage >= (size_t)kRows * kTileN * 4, "room for the sums of a block");
 };
 
 struct TcParams {
+  CUtensorMap x_map;                        // the rows of x, 64 columns x kRows rows at a time
   W4Args A;
   int col_tiles, row_tiles, token_tiles;    // chunks of columns; tiles of 128 outputs, of kRows rows
-  int split, pieces;
+  int split, pieces, copies;                // copies: x_map is there
   uint32_t idesc;
 };
 
@@ -69,15 +76,15 @@ struct Smem {
 __device__ __forceinline__ Smem carve(uint8_t *smem, uint32_t scale_bytes) {
   Smem s;
   s.afull = smem_u32(smem);
-  s.aempty = s.afull + 8 * kABufs;
-  s.bfull = s.aempty + 8 * kABufs;
-  s.bempty = s.bfull + 8 * kMaxStages;
-  s.dfull = s.bempty + 8 * kMaxStages;
+  s.aempty = s.afull + 8 * kMaxABufs;
+  s.bfull = s.aempty + 8 * kMaxABufs;
+  s.bempty = s.bfull + 8 * kStages;
+  s.dfull = s.bempty + 8 * kStages;
   s.dempty = s.dfull + 16;
-  s.tmem_slot = reinterpret_cast<uint32_t *>(smem + 16 * kABufs + 16 * kMaxStages + 32);
+  s.tmem_slot = reinterpret_cast<uint32_t *>(smem + 16 * kMaxABufs + 16 * kStages + 32);
   s.abort_flag = reinterpret_cast<volatile int *>(s.tmem_slot + 1);
   s.scales = s.afull + kCtrlBytes;
-  s.ring = s.scales + scale_bytes;
+  s.ring = (s.scales + scale_bytes + 1023u) & ~1023u;
   return s;
 }
 
@@ -86,6 +93,22 @@ __device__ __forceinline__ bool wait(const Smem &S, uint32_t bar, uint32_t parit
 }
 __device__ __forceinline__ bool wait_warp(const Smem &S, uint32_t bar, uint32_t parity) {
   return __all_sync(0xFFFFFFFFu, wait(S, bar, parity));
+}
+
+// The same as straight code, for the warps whose registers hold sums: a call would have them move around it.
+__device__ __forceinline__ bool wait_inline(const Smem &S, uint32_t bar, uint32_t parity) {
+  if (mbar_try(bar, parity)) return true;
+  const long long t0 = clock64();
+  bool ok = false;
+#pragma unroll 1
+  while (!ok && *S.abort_flag == 0) {
+    ok = mbar_try(bar, parity);
+    if (!ok && clock64() - t0 > kWaitCycles) {
+      *S.abort_flag = 1;
+      atomicExch(&g_status_w4, (int)XNOR_ERR_TIMEOUT);
+    }
+  }
+  return ok;
 }
 
 // A position in a ring of buffers and the parity of its uses.
@@ -128,59 +151,67 @@ __device__ __forceinline__ uint32_t elect_one() {
 }
 
 // ------------------------------------------------------------------ the issuing thread
+// Operand of the rows of x: 128-byte rows, swizzled in groups of eight (1024 bytes); 16 columns are 32 bytes on.
+__device__ __forceinline__ uint64_t swizzled_desc(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
 template <int kRows>
 __device__ void mma_loop(const TcParams &P, const Smem &S, const Span &span, int tiles, uint32_t tmem) {
   using Sh = Shape<kRows>;
   const int group = P.A.d.group;
-  Ring a, b, d;                                    // d: the accumulator (one half: both in turn)
-  uint32_t dpar[2] = {1u, 1u};
+  const uint32_t idesc = P.idesc;
+  const uint64_t desc0 = swizzled_desc(S.ring);
+  Ring a, b;
+  uint32_t buf = 0u, dpar = 1u;                    // the accumulator and the parity of its being drained
+  // n products of 16 columns from column 16 `from` of the chunk at hand
+  auto products = [&](int from, int n, uint32_t accumulate) {
+    const uint32_t d = tmem + buf * (uint32_t)kRows, at = tmem + (uint32_t)Sh::kATmem + a.at * kACols + 8u * (uint32_t)from;
+    const uint64_t bt = desc0 + (uint64_t)(b.at * (Sh::kStage >> 4) + 2u * (uint32_t)from);
+    mma_tmem(d, at, bt, idesc, accumulate);
+    mma_tmem(d, at + 8u, bt + 2u, idesc, 1u);
+    if (n > 2) {
+      mma_tmem(d, at + 16u, bt + 4u, idesc, 1u);
+      mma_tmem(d, at + 24u, bt + 6u, idesc, 1u);
+    }
+  };
+  auto acquire = [&]() {
+    const bool ok = wait(S, S.afull + 8u * a.at, a.parity) && wait(S, S.bfull + 8u * b.at, b.parity);
+    tc_fence_after();
+    return ok;
+  };
+  auto release = [&]() {
+    umma_commit(S.aempty + 8u * a.at);
+    umma_commit(S.bempty + 8u * b.at);
+    a.step(Sh::kABufs);
+    b.step(kStages);
+  };
   for (int tile = 0; tile < tiles; ++tile) {
-    int acquired = span.c0;                        // chunks whose buffers are known to be full
-    Ring aw = a, bw = b;
+    int c = span.c0;
+#pragma unroll 1
     for (int u = span.u0; u < span.u1; ++u) {
-      const int k0 = u * group, steps = min(group, P.col_tiles * kChunk - k0) / 16;
-      const bool ends = ((k0 + group) % kChunk) == 0 || u + 1 == span.u1;      // the unit's last chunk is done with
-      const Ring a0 = a, b0 = b;
-#pragma unroll 1
-      for (int h = 0; h < Sh::kHalves; ++h) {
-        const uint32_t buf = Sh::kHalves == 2 ? (uint32_t)h : d.at;
-        if (!wait(S, S.dempty + 8u * buf, dpar[buf])) return;
-        dpar[buf] ^= 1u;
-        tc_fence_after();
-        a = a0;
-        b = b0;
-        uint32_t accumulate = 0u;
-#pragma unroll 1
-        for (int s = 0; s < steps; s += 4 - (s + k0 / 16) % 4) {
-          const int in_chunk = (k0 / 16 + s) % 4, c = (k0 + 16 * s) / kChunk;
-          if (c >= acquired) {
-            if (!wait(S, S.afull + 8u * aw.at, aw.parity) || !wait(S, S.bfull + 8u * bw.at, bw.parity)) return;
-            tc_fence_after();
-            aw.step(kABufs);
-            bw.step(Sh::kStages);
-            acquired = c + 1;
-          }
-          const uint32_t at = tmem + (uint32_t)(kATmem + (int)a.at * kACols + in_chunk * 8);
-          const uint32_t bt = S.ring + b.at * Sh::kStage + (uint32_t)(2 * in_chunk) * Sh::kPlane + (uint32_t)(h * Sh::kUnit) * 16u;
-          const int n = min(4 - in_chunk, steps - s);
-#pragma unroll 1
-          for (int i = 0; i < n; ++i) {
-            mma_tmem(tmem + buf * kDCols, at + 8u * i, make_desc(bt + 2u * i * Sh::kPlane, Sh::kPlane, 128u), P.idesc, accumulate);
-            accumulate = 1u;
-          }
-          const bool chunk_done = in_chunk + n == 4 || (ends && s + n == steps);
-          if (chunk_done) {
-            if (h == Sh::kHalves - 1) {
-              umma_commit(S.aempty + 8u * a.at);
-              umma_commit(S.bempty + 8u * b.at);
-            }
-            a.step(kABufs);
-            b.step(Sh::kStages);
-          }
+      if (!wait(S, S.dempty + 8u * buf, dpar)) return;
+      tc_fence_after();
+      if (group == 32) {                           // half a chunk
+        const int half = u & 1;
+        if (half == 0 && !acquire()) return;
+        products(2 * half, 2, 0u);
+        if (half == 1 || u + 1 == span.u1) release();
+      } else {
+        if (!acquire()) return;
+        products(0, 4, 0u);
+        release();
+        ++c;
+        if (group == 128 && c < span.c1) {
+          if (!acquire()) return;
+          products(0, 4, 1u);
+          release();
+          ++c;
         }
-        umma_commit(S.dfull + 8u * buf);
       }
-      if (Sh::kHalves == 1) d.at ^= 1u;
+      umma_commit(S.dfull + 8u * buf);
+      buf ^= 1u;
+      if (buf == 0u) dpar ^= 1u;
     }
   }
 }
@@ -194,140 +225,137 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t r[16]) 
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 
-// Set `which` of `sets` takes every sets-th chunk.  A thread expands one weight row: eight words of a chunk, which
-// come in two chunks ahead.
+// Set `which` takes every kExpand-th chunk.  A thread expands one weight row: eight words of a chunk, which come
+// in two chunks ahead.
+struct Ahead {
+  uint2 w[4];
+  uint32_t z[2];
+};
+
 template <class T, int kRows>
 __device__ void expand_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total, int which, int quarter,
                             int lane, uint32_t tmem) {
-  constexpr int kSets = Shape<kRows>::kExpand;
+  using Sh = Shape<kRows>;
+  constexpr int kSets = Sh::kExpand;
   const int N = P.A.d.N, group = P.A.d.group, r = 32 * quarter + lane, per_tile = span.c1 - span.c0;
-  const uint32_t t_lane = tmem + ((uint32_t)(32 * quarter) << 16) + kATmem;
+  const int last_group = (P.A.d.K - 1) / group;
+  const uint32_t t_lane = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)Sh::kATmem;
   uint32_t seq = 0;                                 // chunks of all tiles in sequence: their buffers
   for (int tile = first; tile < total; tile += step, seq += (uint32_t)per_tile) {
-    const int n = (tile % P.row_tiles) * kTileN + r, nc = min(n, N - 1);
+    const int nc = min((tile % P.row_tiles) * kTileN + r, N - 1);
     const uint2 *w = reinterpret_cast<const uint2 *>(P.A.w) +
                      ((size_t)(nc / kW4Rows) * P.col_tiles * 32 + 4 * (nc & 7)) * 2 + ((nc >> 3) & 1);
-    struct Ahead { uint2 w[4]; uint32_t z[2]; };
-    auto fetch = [&](int c, Ahead &f) {
-      if (c >= span.c1) return;
+    auto fetch = [&](int i, Ahead &f) {
+      if (i >= per_tile) return;
+      const int c = span.c0 + i;
 #pragma unroll
       for (int t = 0; t < 4; ++t) f.w[t] = load_global(w + ((size_t)c * 32 + t) * 2);
       f.z[0] = f.z[1] = 8u;
       if (P.A.zeros) {
-        const int last = (P.A.d.K - 1) / group;
-        f.z[0] = load_global(P.A.zeros + (size_t)min(c * kChunk / group, last) * N + nc);
-        f.z[1] = group == 32 ? load_global(P.A.zeros + (size_t)min(2 * c + 1, last) * N + nc) : f.z[0];
+        f.z[0] = load_global(P.A.zeros + (size_t)min(c * kChunk / group, last_group) * N + nc);
+        f.z[1] = group == 32 ? load_global(P.A.zeros + (size_t)min(2 * c + 1, last_group) * N + nc) : f.z[0];
       }
     };
-    const int skip = (int)((uint32_t)(which + kSets - (int)(seq % kSets)) % kSets);     // this set's first chunk of the tile
-    Ahead f[2];
-    fetch(span.c0 + skip, f[0]);
-    fetch(span.c0 + skip + kSets, f[1]);
-#pragma unroll 1
-    for (int i = skip; i < per_tile; i += kSets) {
-      const Ahead now = f[0];
-      f[0] = f[1];
-      fetch(span.c0 + i + 2 * kSets, f[1]);
-      const uint32_t at = (seq + (uint32_t)i) % kABufs, use = (seq + (uint32_t)i) / kABufs;
-      if (!wait_warp(S, S.aempty + 8u * at, (use & 1u) ^ 1u)) return;
+    auto expand = [&](int i, const Ahead &f) {
+      const uint32_t at = (seq + (uint32_t)i) % Sh::kABufs, use = (seq + (uint32_t)i) / Sh::kABufs;
+      if (!wait_warp(S, S.aempty + 8u * at, (use & 1u) ^ 1u)) return false;
       tc_fence_after();
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const uint32_t zero = w4_zero(now.z[half], T());
+        const uint32_t zero = w4_zero(f.z[half], T());
         uint32_t v[16];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-          for (int p = 0; p < 4; ++p) v[4 * t + p] = w4_pair(half == 0 ? now.w[t].x : now.w[t].y, p, T(), zero);
-        __syncwarp();
+          for (int p = 0; p < 4; ++p) v[4 * t + p] = w4_pair(half == 0 ? f.w[t].x : f.w[t].y, p, T(), zero);
         tmem_st16(t_lane + at * kACols + 16u * half, v);
       }
       asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(S.afull + 8u * at);
+      return true;
+    };
+    const int skip = (int)(((uint32_t)(which + kSets) - seq % kSets) % kSets);     // this set's first chunk of the tile
+    Ahead f0, f1;                                   // (two by name: moving one to the other would wait for its loads)
+    fetch(skip, f0);
+    fetch(skip + kSets, f1);
+#pragma unroll 1
+    for (int i = skip; i < per_tile; i += 2 * kSets) {
+      if (!expand(i, f0)) return;
+      fetch(i + 2 * kSets, f0);
+      if (i + kSets >= per_tile) break;
+      if (!expand(i + kSets, f1)) return;
+      fetch(i + 3 * kSets, f1);
     }
   }
 }
 
 // ------------------------------------------------------------------ the rows of x
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(__cvta_generic_to_global(src)), "r"(bytes) : "memory");
+// One thread copies a stage with one tensor copy, which also fills what does not exist with zeros.
+template <int kRows>
+__device__ void copy_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total) {
+  Ring r;
+  for (int tile = first; tile < total; tile += step) {
+    const int tok0 = (tile / P.row_tiles) * kRows;
+#pragma unroll 1
+    for (int c = span.c0; c < span.c1; ++c) {
+      if (!wait(S, S.bempty + 8u * r.at, r.parity ^ 1u)) {
+        // gave up: the copies in flight must land before the block's shared memory is released
+        for (uint32_t s = 0; s < kStages; ++s)
+          for (int i = 0; i < (1 << 16) && !mbar_try(S.bfull + 8u * s, s < r.at ? r.parity : r.parity ^ 1u); ++i) {}
+        return;
+      }
+      const uint32_t bar = S.bfull + 8u * r.at;
+      mbar_arrive_expect_tx(bar, Shape<kRows>::kStage);
+      asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                   ::"r"(S.ring + r.at * Shape<kRows>::kStage), "l"(&P.x_map), "r"(c * kChunk), "r"(tok0), "r"(bar) : "memory");
+      r.step(kStages);
+    }
+  }
 }
 
-// Three warps share every stage.  Rows whose addresses allow it come in by asynchronous 16-byte copies, two stages in
-// flight; others, and 8-bit rows, which become 16-bit numbers, through registers.  Shared memory holds
-// [columns / 8][row][16 bytes], the operand layout without swizzle; missing rows and columns are zeros.
+// Three warps share every stage: rows in 8 bits become 16-bit numbers, others are at addresses that tensor copies
+// do not take.
 template <int kType, int kRows>
 __device__ void load_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total, int w, int lane) {
   using Sh = Shape<kRows>;
   const int K = P.A.d.K, piece = lane & 7;
-  const bool async = RowsOf<kType>::kBytes == 2 && P.pieces;
-  constexpr int kDepth = 2;
-  Ring fill, done;
-  int pending = 0;
-  auto finish = [&]() {                              // the oldest stage in flight is complete
-    fence_proxy_async();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(S.bfull + 8u * done.at);
-    done.step(Sh::kStages);
-    --pending;
-  };
+  Ring fill;
   for (int tile = first; tile < total; tile += step) {
     const long long tok0 = (long long)(tile / P.row_tiles) * kRows;
     const int rows = (int)min((long long)kRows, P.A.r.rows - tok0);
-    const uint8_t *x = static_cast<const uint8_t *>(P.A.x) + tok0 * P.A.r.x_stride * RowsOf<kType>::kBytes;
     const long long row_bytes = P.A.r.x_stride * RowsOf<kType>::kBytes;
+    const uint8_t *x = static_cast<const uint8_t *>(P.A.x) + tok0 * row_bytes;
 #pragma unroll 1
     for (int c = span.c0; c < span.c1; ++c) {
-      if (!wait_warp(S, S.bempty + 8u * fill.at, fill.parity ^ 1u)) {
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        return;
-      }
+      if (!wait_warp(S, S.bempty + 8u * fill.at, fill.parity ^ 1u)) return;
       const int k = c * kChunk + 8 * piece;
-      const uint32_t dst = S.ring + fill.at * Sh::kStage + (uint32_t)piece * Sh::kPlane;
-      int row = 4 * w + (lane >> 3);
-      if (async) {
-        const uint32_t bytes = (uint32_t)max(0, min(16, 2 * (K - k)));
-        const uint8_t *src = x + (long long)row * row_bytes + 2 * (bytes > 0 ? k : 0);
-#pragma unroll 4
-        for (; row < kRows; row += 4 * kLoadWarps, src += 4 * kLoadWarps * row_bytes)
-          copy16(dst + (uint32_t)row * 16u, row < rows ? src : x, row < rows ? bytes : 0u);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        ++pending;
-        if (pending > kDepth) {
-          asm volatile("cp.async.wait_group %0;" ::"n"(kDepth) : "memory");
-          finish();
-        }
-      } else {
+      const uint32_t dst = S.ring + fill.at * Sh::kStage;
 #pragma unroll 1
-        for (; row < kRows; row += 4 * kLoadWarps * 4) {
-          uint32_t v[4][4];
+      for (int row = 4 * w + (lane >> 3); row < kRows; row += 4 * kLoadWarps * 4) {
+        uint32_t v[4][4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int rr = row + 4 * kLoadWarps * i;
-            if (rr < rows) {
-              load_x8<kType>(x + (long long)rr * row_bytes, k, K, P.pieces, v[i]);
-            } else {
+        for (int i = 0; i < 4; ++i) {
+          const int rr = row + 4 * kLoadWarps * i;
+          if (rr < rows) {
+            load_x8<kType>(x + (long long)rr * row_bytes, k, K, P.pieces, v[i]);
+          } else {
 #pragma unroll
-              for (int q = 0; q < 4; ++q) v[i][q] = 0u;
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int rr = row + 4 * kLoadWarps * i;
-            if (rr < kRows) sts128(dst + (uint32_t)rr * 16u, v[i][0], v[i][1], v[i][2], v[i][3]);
+            for (int q = 0; q < 4; ++q) v[i][q] = 0u;
           }
         }
-        ++pending;
-        finish();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int rr = row + 4 * kLoadWarps * i;
+          if (rr < kRows) sts128(dst + (uint32_t)rr * 128u + (uint32_t)((piece ^ (rr & 7)) * 16), v[i][0], v[i][1], v[i][2], v[i][3]);
+        }
       }
-      fill.step(Sh::kStages);
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(S.bfull + 8u * fill.at);
+      fill.step(kStages);
     }
-  }
-  if (async) {
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    while (pending > 0) finish();
   }
 }
 
@@ -346,7 +374,7 @@ __device__ __forceinline__ float4 lds_f4(uint32_t addr) {
 }
 
 template <int kRows>
-__device__ bool promote_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total, int set, int quarter,
+__device__ void promote_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total, int set, int quarter,
                              int lane, uint32_t tmem) {
   using Sh = Shape<kRows>;
   constexpr int kUnit = Sh::kUnit;
@@ -356,7 +384,7 @@ __device__ bool promote_role(const TcParams &P, const Smem &S, const Span &span,
   const int G = (A.d.K + A.d.group - 1) / A.d.group;
   const uint32_t t_lane = tmem + ((uint32_t)(32 * quarter) << 16);
   const uint32_t my_scales = S.scales + (uint32_t)(4 * set + quarter) * 512u;
-  uint32_t parity[2] = {0u, 0u}, next = 0u;
+  uint32_t buf = 0u, parity = 0u;
   for (int tile = first; tile < total; tile += step) {
     const int n = (tile % P.row_tiles) * kTileN + 32 * quarter + lane, nc = min(n, N - 1);
     const long long tok0 = (long long)(tile / P.row_tiles) * kRows + set * kUnit;
@@ -378,36 +406,39 @@ __device__ bool promote_role(const TcParams &P, const Smem &S, const Span &span,
         }
         __syncwarp();
       }
-      const uint32_t buf = Sh::kHalves == 2 ? (uint32_t)set : next;
-      if (!wait_warp(S, S.dfull + 8u * buf, parity[buf])) return false;
-      parity[buf] ^= 1u;
-      next ^= 1u;
+      if (!__all_sync(0xFFFFFFFFu, wait_inline(S, S.dfull + 8u * buf, parity))) return;
       tc_fence_after();
+      // 32 values at a time: a load of tensor memory takes as long for 16
+      constexpr int kLoad = kRows > 64 ? 16 : 32;
 #pragma unroll
-      for (int j = 0; j < kUnit / 16; ++j) {
-        int32_t v[16];
-        __syncwarp();
-        tmem_ld16(t_lane + buf * kDCols + 16u * j, v);
+      for (int j = 0; j < kUnit / kLoad; ++j) {
+        int32_t v[kLoad];
+        const uint32_t from = t_lane + buf * (uint32_t)kRows + (uint32_t)(set * kUnit + kLoad * j);
+        tmem_ld16(from, v);
+        if constexpr (kLoad == 32) { tmem_ld16(from + 16u, v + 16); tmem_wait16(v + 16); }
         tmem_wait16(v);
-        if (j + 1 == kUnit / 16) {
+        if (j + 1 == kUnit / kLoad) {
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(S.dempty + 8u * buf);
         }
         if (x_groups) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 f = lds_f4(my_scales + 64u * j + 16u * i);
-            acc[16 * j + 4 * i] = fmaf(__int_as_float(v[4 * i]) * f.x, s, acc[16 * j + 4 * i]);
-            acc[16 * j + 4 * i + 1] = fmaf(__int_as_float(v[4 * i + 1]) * f.y, s, acc[16 * j + 4 * i + 1]);
-            acc[16 * j + 4 * i + 2] = fmaf(__int_as_float(v[4 * i + 2]) * f.z, s, acc[16 * j + 4 * i + 2]);
-            acc[16 * j + 4 * i + 3] = fmaf(__int_as_float(v[4 * i + 3]) * f.w, s, acc[16 * j + 4 * i + 3]);
+          for (int i = 0; i < kLoad / 4; ++i) {
+            const float4 f = lds_f4(my_scales + (uint32_t)(4 * kLoad * j + 16 * i));
+            float *to = acc + kLoad * j + 4 * i;
+            to[0] = fmaf(__int_as_float(v[4 * i]) * f.x, s, to[0]);
+            to[1] = fmaf(__int_as_float(v[4 * i + 1]) * f.y, s, to[1]);
+            to[2] = fmaf(__int_as_float(v[4 * i + 2]) * f.z, s, to[2]);
+            to[3] = fmaf(__int_as_float(v[4 * i + 3]) * f.w, s, to[3]);
           }
         } else {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[16 * j + i] = fmaf(__int_as_float(v[i]), s, acc[16 * j + i]);
+          for (int i = 0; i < kLoad; ++i) acc[kLoad * j + i] = fmaf(__int_as_float(v[i]), s, acc[kLoad * j + i]);
         }
       }
+      buf ^= 1u;
+      if (buf == 0u) parity ^= 1u;
     }
     if (P.split > 1) {                     // [row of x][output], for the cluster
 #pragma unroll
@@ -420,7 +451,6 @@ __device__ bool promote_role(const TcParams &P, const Smem &S, const Span &span,
         if (tok0 + i < A.r.rows) store_out(A, tok0 + i, n, xs ? acc[i] * load_global(xs + tok0 + i) : acc[i]);
     }
   }
-  return true;
 }
 
 __device__ __forceinline__ void cluster_barrier() {
@@ -428,21 +458,21 @@ __device__ __forceinline__ void cluster_barrier() {
 }
 
 template <int kType, int kRows>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Shape<kRows>::kThreads, 1)
 w4_tc_kernel(const __grid_constant__ TcParams P) {
   using Sh = Shape<kRows>;
   using T = typename RowsOf<kType>::T;
-  extern __shared__ __align__(128) uint8_t smem[];
+  extern __shared__ __align__(1024) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Smem S = carve(smem, Sh::kScaleBytes);
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kABufs; ++i) { mbar_init(S.afull + 8u * i, 4); mbar_init(S.aempty + 8u * i, 1); }
-    for (int i = 0; i < kMaxStages; ++i) { mbar_init(S.bfull + 8u * i, kLoadWarps); mbar_init(S.bempty + 8u * i, 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(S.dfull + 8u * i, 1); mbar_init(S.dempty + 8u * i, 4); }
+    for (int i = 0; i < Sh::kABufs; ++i) { mbar_init(S.afull + 8u * i, 4); mbar_init(S.aempty + 8u * i, 1); }
+    for (int i = 0; i < kStages; ++i) { mbar_init(S.bfull + 8u * i, P.copies ? 1 : kLoadWarps); mbar_init(S.bempty + 8u * i, 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(S.dfull + 8u * i, 1); mbar_init(S.dempty + 8u * i, 4 * Sh::kPromo); }
     *S.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == kMmaWarp) {
+  if (warp == Sh::kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(S.tmem_slot)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -457,15 +487,25 @@ w4_tc_kernel(const __grid_constant__ TcParams P) {
   const int rank = (int)(blockIdx.x % (unsigned)P.split), first = (int)(blockIdx.x / (unsigned)P.split), step = (int)(gridDim.x / (unsigned)P.split);
   const int total = P.row_tiles * P.token_tiles, mine = first < total ? (total - first + step - 1) / step : 0;
   const Span span(P, rank);
-  if (warp < 4 * Sh::kPromo) promote_role<kRows>(P, S, span, first, step, total, warp >> 2, warp & 3, lane, tmem);
-  else if (warp < kMmaWarp) expand_role<T, kRows>(P, S, span, first, step, total, (warp >> 2) - Sh::kPromo, warp & 3, lane, tmem);
-  else if (warp == kMmaWarp) {
-    if (elect_one()) mma_loop<kRows>(P, S, span, mine, tmem);
+  if (warp < 4 * Sh::kPromo) {
+    if constexpr (Sh::kPromoRegs != Sh::kRegs) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Sh::kPromoRegs));
+    promote_role<kRows>(P, S, span, first, step, total, warp >> 2, warp & 3, lane, tmem);
+  } else {
+    if constexpr (Sh::kOtherRegs != Sh::kRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::kOtherRegs));
+    if (warp < Sh::kMmaWarp) {
+      expand_role<T, kRows>(P, S, span, first, step, total, (warp >> 2) - Sh::kPromo, warp & 3, lane, tmem);
+    } else if (warp == Sh::kMmaWarp) {
+      if (elect_one()) mma_loop<kRows>(P, S, span, mine, tmem);
+    } else if (!P.copies) {
+      load_role<kType, kRows>(P, S, span, first, step, total, warp - Sh::kLoadWarp, lane);
+    } else if (warp == Sh::kLoadWarp) {
+      if (elect_one()) copy_role<kRows>(P, S, span, first, step, total);
+    }
     __syncwarp();
-  } else load_role<kType, kRows>(P, S, span, first, step, total, warp - kLoadWarp, lane);
+  }
   tc_fence_before();
   __syncthreads();
-  if (warp == kMmaWarp)
+  if (warp == Sh::kMmaWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
   if (P.split == 1) return;
   // a cluster has one tile; its blocks write shares of the rows, each the sums of all in the same order
@@ -474,7 +514,7 @@ w4_tc_kernel(const __grid_constant__ TcParams P) {
   const long long tok0 = (long long)(first / P.row_tiles) * kRows;
   const bool row_scale = P.A.x_scales != nullptr && P.A.r.x_group == 0;
   const int r0 = kRows * rank / P.split, r1 = kRows * (rank + 1) / P.split;
-  for (int e = r0 * kTileN + threadIdx.x; e < r1 * kTileN; e += kThreads) {
+  for (int e = r0 * kTileN + threadIdx.x; e < r1 * kTileN; e += Sh::kThreads) {
     const int n = e % kTileN;
     const long long row = tok0 + e / kTileN;
     if (row >= P.A.r.rows || n0 + n >= P.A.d.N) continue;
@@ -492,6 +532,40 @@ w4_tc_kernel(const __grid_constant__ TcParams P) {
   cluster_barrier();
 }
 
+// The driver's function that makes tensor maps, looked up once (no library is linked for it).
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+  static std::atomic<EncodeTiled> known{nullptr};
+  EncodeTiled f = known.load(std::memory_order_relaxed);
+  if (f == nullptr) {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) == cudaSuccess &&
+        found == cudaDriverEntryPointSuccess) {
+      f = (EncodeTiled)p;
+      known.store(f, std::memory_order_relaxed);
+    } else {
+      (void)cudaGetLastError();
+    }
+  }
+  return f;
+}
+
+// Whether the rows can be copied as they are, and their map.
+template <int kType>
+bool map_rows(const W4Args &a, int rows, CUtensorMap *map) {
+  if (RowsOf<kType>::kBytes != 2 || !rows_in_pieces(a.x, a.r.x_stride, 8, 2) || a.r.x_stride < a.d.K) return false;
+  const EncodeTiled encode = encode_tiled();
+  if (encode == nullptr) return false;
+  const cuuint64_t size[2] = {(cuuint64_t)a.d.K, (cuuint64_t)a.r.rows}, stride[1] = {(cuuint64_t)a.r.x_stride * 2};
+  const cuuint32_t box[2] = {kChunk, (cuuint32_t)rows}, each[2] = {1, 1};
+  return encode(map, kType == XNOR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                const_cast<void *>(a.x), size, stride, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int kType, int kRows>
 cudaError_t run(const W4Args &a, cudaStream_t st) {
   using Sh = Shape<kRows>;
@@ -503,6 +577,7 @@ cudaError_t run(const W4Args &a, cudaStream_t st) {
     attr_set = true;
   }
   TcParams P;
+  P.copies = map_rows<kType>(a, kRows, &P.x_map);
   P.A = a;
   P.col_tiles = w4_col_tiles(a.d);
   P.row_tiles = (a.d.N + kTileN - 1) / kTileN;
@@ -511,20 +586,18 @@ cudaError_t run(const W4Args &a, cudaStream_t st) {
   const int total = P.row_tiles * P.token_tiles, sms = sm_count_of_current_device();
   // blocks divide the columns while that still adds SMs and each keeps four blocks of 128 columns
   P.split = 1;
-  while (Sh::kHalves == 1 && P.split < kMaxSplitTc && 2 * P.split * total <= sms && P.col_tiles >= 16 * P.split) P.split *= 2;
+  while (P.split < kMaxSplitTc && 2 * P.split * total <= sms && P.col_tiles >= 16 * P.split) P.split *= 2;
   // instruction descriptor: D fp32, A and B bf16 or f16, both K-major, M = 128
   const uint32_t format = kType == XNOR_BF16 ? 1u : 0u;
-  P.idesc = (1u << 4) | (format << 7) | (format << 10) | ((uint32_t)(Sh::kUnit >> 3) << 17) | ((uint32_t)(kTileN >> 4) << 24);
+  P.idesc = (1u << 4) | (format << 7) | (format << 10) | ((uint32_t)(kRows >> 3) << 17) | ((uint32_t)(kTileN >> 4) << 24);
   const unsigned grid = P.split > 1 ? (unsigned)(total * P.split) : (unsigned)std::min(total, sms);
-  return launch_kernel(w4_tc_kernel<kType, kRows>, dim3(grid), kThreads, Sh::kSmem, st, (unsigned)P.split, P);
+  return launch_kernel(w4_tc_kernel<kType, kRows>, dim3(grid), Sh::kThreads, Sh::kSmem, st, (unsigned)P.split, P);
 }
 
-// 256 rows of x per block halve the expansion per product; a block of them takes no share of a cluster (its two
-// halves end one after the other), so they are for problems that fill the GPU.
 template <int kType>
 cudaError_t run_type(const W4Args &a, cudaStream_t st) {
-  const long long tiles = (a.d.N + kTileN - 1) / kTileN * ((a.r.rows + 255ll) / 256);
-  if (a.r.rows > 128 && 2 * tiles > sm_count_of_current_device()) return run<kType, 256>(a, st);
+  const long long tiles = (a.d.N + kTileN - 1) / kTileN * ((a.r.rows + 191ll) / 192);
+  if (a.r.rows > 128 && 2 * tiles > sm_count_of_current_device()) return run<kType, 192>(a, st);
   if (a.r.rows <= 32) return run<kType, 32>(a, st);
   if (a.r.rows <= 64) return run<kType, 64>(a, st);
   return run<kType, 128>(a, st);
