@@ -8,9 +8,9 @@
 // rounded: scaling the weights before the product would round each to the operands' 8 or 11 bits.
 //
 // A block (one per SM, persistent) computes 128 outputs x kRows rows of x.  A unit of work is one group: its sums
-// have two buffers in tensor memory, so that the tensor core fills one while the other is drained.  16 or 20 warps:
+// have two buffers in tensor memory, so that the tensor core fills one while the other is drained.  20 warps (16):
 //   promotion  8 warps (4 up to 64 rows): a thread holds the sums of one output and up to 96 rows of x
-//   expansion  8 warps (4 with 192 rows): a thread expands one weight row, 64 columns at a time, straight into tensor memory
+//   expansion  8 warps: a thread expands one weight row, 64 columns at a time, straight into tensor memory
 //   one warp issues the products; one copies the rows of x, by tensor copies, into a ring of stages of 64 columns
 //   (where they cannot be copied as they are, three warps bring them through registers)
 // Where the tiles are too few for the GPU, the blocks of a cluster divide the columns, and add their sums through
@@ -36,7 +36,7 @@ constexpr int kTileN = 128;                  // outputs (weight rows) of a tile:
 constexpr int kChunk = 64;                   // columns of a stage
 constexpr int kLoadWarps = 3;
 constexpr int kACols = kChunk / 2;           // tensor-memory columns of a chunk of expanded weights
-constexpr int kMaxABufs = 8, kStages = 8;
+constexpr int kMaxStages = 8;
 constexpr uint32_t kCtrlBytes = 1024;
 constexpr int kMaxSplitTc = 8;
 
@@ -44,20 +44,20 @@ template <int kRows>
 struct Shape {
   static constexpr int kPromo = kRows > 64 ? 2 : 1;            // sets of four warps
   static constexpr int kUnit = kRows / kPromo;                 // rows of x of a set
-  static constexpr int kExpand = kRows > 128 ? 1 : 2;
+  static constexpr int kExpand = 2;
   static constexpr int kMmaWarp = 4 * (kPromo + kExpand), kLoadWarp = kMmaWarp + 1;
   static constexpr int kThreads = 32 * (kMmaWarp + 4);
   static constexpr int kATmem = kRows > 128 ? 2 * kRows : 256; // behind the two accumulators
-  static constexpr int kABufs = (512 - kATmem) / kACols;
+  static constexpr int kStages = (512 - kATmem) / kACols;      // chunks: weights in tensor memory, rows of x in shared
   static constexpr uint32_t kStage = kRows * kChunk * 2;       // a row of x: 128 bytes, swizzled
   static constexpr uint32_t kScaleBytes = 8 * 512;             // a group's scales of x, per promotion warp
   static constexpr size_t kSmem = 1024 + kCtrlBytes + kScaleBytes + (size_t)kStages * kStage;   // (1024: to align the ring)
   // Registers per thread as launched, and after they are dealt out anew: the promotion's hold its sums.
   static constexpr int kRegs = kThreads == 512 ? 128 : 96;
-  static constexpr int kPromoRegs = kRows > 128 ? 152 : kRows > 64 ? 128 : 128, kOtherRegs = kRows > 128 ? 104 : kRows > 64 ? 72 : 128;
+  static constexpr int kPromoRegs = kRows > 128 ? 144 : kRows > 64 ? 128 : 128, kOtherRegs = kRows > 128 ? 64 : kRows > 64 ? 72 : 128;
   static_assert(kPromo * 128 * kPromoRegs + (kThreads - kPromo * 128) * kOtherRegs <= kThreads * kRegs, "registers");
-  static_assert(kSmem <= 232448 && kABufs <= kMaxABufs, "shared and tensor memory");
-  static_assert((size_t)kStages * kStage >= (size_t)kRows * kTileN * 4, "room for the sums of a block");
+  static_assert(kSmem <= 232448 && kStages <= kMaxStages, "shared and tensor memory");
+  static_assert((size_t)kStages * kStage >= (size_t)kRows * kTileN * 4 || kRows > 128, "room for the sums of a block");
 };
 
 struct TcParams {
@@ -69,21 +69,19 @@ struct TcParams {
 };
 
 struct Smem {
-  uint32_t afull, aempty, bfull, bempty, dfull, dempty, scales, ring;
+  uint32_t full, empty, dfull, dempty, scales, ring;
   uint32_t *tmem_slot;
   volatile int *abort_flag;
 };
 __device__ __forceinline__ Smem carve(uint8_t *smem, uint32_t scale_bytes) {
   Smem s;
-  s.afull = smem_u32(smem);
-  s.aempty = s.afull + 8 * kMaxABufs;
-  s.bfull = s.aempty + 8 * kMaxABufs;
-  s.bempty = s.bfull + 8 * kStages;
-  s.dfull = s.bempty + 8 * kStages;
+  s.full = smem_u32(smem);
+  s.empty = s.full + 8 * kMaxStages;
+  s.dfull = s.empty + 8 * kMaxStages;
   s.dempty = s.dfull + 16;
-  s.tmem_slot = reinterpret_cast<uint32_t *>(smem + 16 * kMaxABufs + 16 * kStages + 32);
+  s.tmem_slot = reinterpret_cast<uint32_t *>(smem + 16 * kMaxStages + 32);
   s.abort_flag = reinterpret_cast<volatile int *>(s.tmem_slot + 1);
-  s.scales = s.afull + kCtrlBytes;
+  s.scales = s.full + kCtrlBytes;
   s.ring = (s.scales + scale_bytes + 1023u) & ~1023u;
   return s;
 }
@@ -162,12 +160,13 @@ __device__ void mma_loop(const TcParams &P, const Smem &S, const Span &span, int
   const int group = P.A.d.group;
   const uint32_t idesc = P.idesc;
   const uint64_t desc0 = swizzled_desc(S.ring);
-  Ring a, b;
+  Ring r;
+  bool ready = false;                              // the stage at hand was seen to be full
   uint32_t buf = 0u, dpar = 1u;                    // the accumulator and the parity of its being drained
   // n products of 16 columns from column 16 `from` of the chunk at hand
   auto products = [&](int from, int n, uint32_t accumulate) {
-    const uint32_t d = tmem + buf * (uint32_t)kRows, at = tmem + (uint32_t)Sh::kATmem + a.at * kACols + 8u * (uint32_t)from;
-    const uint64_t bt = desc0 + (uint64_t)(b.at * (Sh::kStage >> 4) + 2u * (uint32_t)from);
+    const uint32_t d = tmem + buf * (uint32_t)kRows, at = tmem + (uint32_t)Sh::kATmem + r.at * kACols + 8u * (uint32_t)from;
+    const uint64_t bt = desc0 + (uint64_t)(r.at * (Sh::kStage >> 4) + 2u * (uint32_t)from);
     mma_tmem(d, at, bt, idesc, accumulate);
     mma_tmem(d, at + 8u, bt + 2u, idesc, 1u);
     if (n > 2) {
@@ -176,15 +175,17 @@ __device__ void mma_loop(const TcParams &P, const Smem &S, const Span &span, int
     }
   };
   auto acquire = [&]() {
-    const bool ok = wait(S, S.afull + 8u * a.at, a.parity) && wait(S, S.bfull + 8u * b.at, b.parity);
+    if (!ready && !wait(S, S.full + 8u * r.at, r.parity)) return false;
     tc_fence_after();
-    return ok;
+    // (the next stage's barrier is looked at before this one's products are issued)
+    Ring next = r;
+    next.step(Sh::kStages);
+    ready = mbar_try(S.full + 8u * next.at, next.parity);
+    return true;
   };
   auto release = [&]() {
-    umma_commit(S.aempty + 8u * a.at);
-    umma_commit(S.bempty + 8u * b.at);
-    a.step(Sh::kABufs);
-    b.step(kStages);
+    umma_commit(S.empty + 8u * r.at);
+    r.step(Sh::kStages);
   };
   for (int tile = 0; tile < tiles; ++tile) {
     int c = span.c0;
@@ -257,8 +258,8 @@ __device__ void expand_role(const TcParams &P, const Smem &S, const Span &span, 
       }
     };
     auto expand = [&](int i, const Ahead &f) {
-      const uint32_t at = (seq + (uint32_t)i) % Sh::kABufs, use = (seq + (uint32_t)i) / Sh::kABufs;
-      if (!wait_warp(S, S.aempty + 8u * at, (use & 1u) ^ 1u)) return false;
+      const uint32_t at = (seq + (uint32_t)i) % Sh::kStages, use = (seq + (uint32_t)i) / Sh::kStages;
+      if (!wait_warp(S, S.empty + 8u * at, (use & 1u) ^ 1u)) return false;
       tc_fence_after();
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
@@ -273,7 +274,7 @@ __device__ void expand_role(const TcParams &P, const Smem &S, const Span &span, 
       asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(S.afull + 8u * at);
+      if (lane == 0) mbar_arrive(S.full + 8u * at);
       return true;
     };
     const int skip = (int)(((uint32_t)(which + kSets) - seq % kSets) % kSets);     // this set's first chunk of the tile
@@ -295,18 +296,19 @@ __device__ void expand_role(const TcParams &P, const Smem &S, const Span &span, 
 // One thread copies a stage with one tensor copy, which also fills what does not exist with zeros.
 template <int kRows>
 __device__ void copy_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total) {
+  constexpr uint32_t kStages = Shape<kRows>::kStages;
   Ring r;
   for (int tile = first; tile < total; tile += step) {
     const int tok0 = (tile / P.row_tiles) * kRows;
 #pragma unroll 1
     for (int c = span.c0; c < span.c1; ++c) {
-      if (!wait(S, S.bempty + 8u * r.at, r.parity ^ 1u)) {
+      if (!wait(S, S.empty + 8u * r.at, r.parity ^ 1u)) {
         // gave up: the copies in flight must land before the block's shared memory is released
         for (uint32_t s = 0; s < kStages; ++s)
-          for (int i = 0; i < (1 << 16) && !mbar_try(S.bfull + 8u * s, s < r.at ? r.parity : r.parity ^ 1u); ++i) {}
+          for (int i = 0; i < (1 << 12) && !mbar_try(S.full + 8u * s, s < r.at ? r.parity : r.parity ^ 1u); ++i) {}
         return;
       }
-      const uint32_t bar = S.bfull + 8u * r.at;
+      const uint32_t bar = S.full + 8u * r.at;
       mbar_arrive_expect_tx(bar, Shape<kRows>::kStage);
       asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                    ::"r"(S.ring + r.at * Shape<kRows>::kStage), "l"(&P.x_map), "r"(c * kChunk), "r"(tok0), "r"(bar) : "memory");
@@ -329,7 +331,7 @@ __device__ void load_role(const TcParams &P, const Smem &S, const Span &span, in
     const uint8_t *x = static_cast<const uint8_t *>(P.A.x) + tok0 * row_bytes;
 #pragma unroll 1
     for (int c = span.c0; c < span.c1; ++c) {
-      if (!wait_warp(S, S.bempty + 8u * fill.at, fill.parity ^ 1u)) return;
+      if (!wait_warp(S, S.empty + 8u * fill.at, fill.parity ^ 1u)) return;
       const int k = c * kChunk + 8 * piece;
       const uint32_t dst = S.ring + fill.at * Sh::kStage;
 #pragma unroll 1
@@ -353,8 +355,8 @@ __device__ void load_role(const TcParams &P, const Smem &S, const Span &span, in
       }
       fence_proxy_async();
       __syncwarp();
-      if (lane == 0) mbar_arrive(S.bfull + 8u * fill.at);
-      fill.step(kStages);
+      if (lane == 0) mbar_arrive(S.full + 8u * fill.at);
+      fill.step(Sh::kStages);
     }
   }
 }
@@ -466,8 +468,8 @@ w4_tc_kernel(const __grid_constant__ TcParams P) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Smem S = carve(smem, Sh::kScaleBytes);
   if (threadIdx.x == 0) {
-    for (int i = 0; i < Sh::kABufs; ++i) { mbar_init(S.afull + 8u * i, 4); mbar_init(S.aempty + 8u * i, 1); }
-    for (int i = 0; i < kStages; ++i) { mbar_init(S.bfull + 8u * i, P.copies ? 1 : kLoadWarps); mbar_init(S.bempty + 8u * i, 1); }
+    // a stage is full with four expanding warps' arrivals and those that bring the rows
+    for (int i = 0; i < Sh::kStages; ++i) { mbar_init(S.full + 8u * i, 4 + (P.copies ? 1 : kLoadWarps)); mbar_init(S.empty + 8u * i, 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(S.dfull + 8u * i, 1); mbar_init(S.dempty + 8u * i, 4 * Sh::kPromo); }
     *S.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
