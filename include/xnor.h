@@ -483,9 +483,9 @@ xnor_status xnor_rmsnorm_backward(const void *dy, const void *dsum, const void *
  * group may be shorter): w = (code - zero) scale.
  *
  *   w_packed  u32 [ceil(N/16)][ceil(K/64)][32][4]: tiles of 16 rows x 64 columns.  Element
- *             [.][.][4 g + t][2 r + c] holds row g + 8 r, columns 32 c + 8 t + 0 .. 7 of the tile, column
- *             2 i + h of the eight in bits 4 i + 16 h and up; rows and columns beyond the matrix
- *             hold any code.
+ *             [.][.][4 g + (t ^ (g/2 % 4))][2 r + c] holds row g + 8 r (g < 8, r < 2), columns
+ *             32 c + 8 t + 0 .. 7 (t < 4, c < 2) of the tile, column 2 i + h of the eight in bits
+ *             4 i + 16 h and up; rows and columns beyond the matrix hold any code.
  *   scales    fp32 [ceil(K/group)][N]
  *   zeros     u8   [ceil(K/group)][N], 0 .. 15, or NULL: 8 everywhere
  * xnor_w4_quantize   w type [N][K] (F32, BF16, F16) -> w_packed, scales, zeros.

@@ -1,6 +1,7 @@
 // 4-bit weights with a scale for each group of columns: quantised from real weights, laid out from given
 // codes, dequantised, and multiplied with a few rows.
 #include <algorithm>
+#include <climits>
 #include <type_traits>
 
 #include "w4.cuh"
@@ -19,7 +20,7 @@ __device__ __forceinline__ void write_tiles(const uint32_t (&words)[kW4Rows][kOc
                                             int col_tiles, uint32_t *w) {
   const int tile = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   if (tile >= 2 || col_tile0 + tile >= col_tiles) return;
-  const int c = 8 * tile + t;
+  const int c = 8 * tile + (t ^ ((g >> 1) & 3));            // this place's columns
   const uint32_t v[4] = {words[g][c], words[g][c + 4], words[g + 8][c], words[g + 8][c + 4]};
   reinterpret_cast<uint4 *>(w)[((size_t)row_tile * col_tiles + col_tile0 + tile) * 32 + lane] = make_uint4(v[0], v[1], v[2], v[3]);
 }
@@ -135,7 +136,7 @@ w4_dequantize_kernel(const uint32_t *w_packed, const float *scales, const uint8_
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int col = 16 * (c & 3) + 8 * h;
-    const uint32_t word = words[c / 4][w4_lane(r, col)][w4_word(r, col)];
+    const uint32_t word = words[c / 4][w4_place(r, col)][w4_word(r, col)];
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (float)((int)((word >> w4_bit(i)) & 15u) - z) * s;
@@ -149,123 +150,183 @@ w4_dequantize_kernel(const uint32_t *w_packed, const float *scales, const uint8_
 // out[t][n] = x_scale[t] sum over groups of scale[g][n] sum over the group of (code - zero)[n][k] x[t][k].
 // Codes minus zeros and the rows' values are exact 16-bit operands of m16n8k16 products summed in 32 bits: 16
 // weight rows against 8 rows of x per step, whatever few of those exist (no extra traffic: the lanes of missing
-// rows read the last one).  Bound by the weights' bytes.  A block has 16 weight rows; its warps and the
-// blocks of its cluster divide the columns, and add their sums in shared memory in a fixed order.
+// rows read the last one).  Bound by the weights' bytes.  A warp multiplies kR tiles of 16 weight rows with the
+// same rows of x in its registers; the warps of a block and the blocks of its cluster divide the columns, and
+// add their sums in shared memory in a fixed order.
 constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;
 constexpr int kMaxSplit = 8;
 
+// d = a b + c
 template <class T>
-__device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t a[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, const float *c) {
   if constexpr (std::is_same<T, __half>::value)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
   else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
 
-// kN: blocks of eight rows of x that share the weights in registers.
-template <int kType, int kN>
+// kN: blocks of eight rows of x; kR: tiles of weight rows; kGroup, kZeros: as the weights have them; kU: column
+// tiles of a stage (a group of 128 stays in one: 2).
+template <int kType, int kN, int kR, int kGroup, bool kZeros>
 __global__ void __launch_bounds__(kFewThreads)
 w4_few_rows_kernel(const W4Args A, int pieces) {
   using T = typename RowsOf<kType>::T;
-  constexpr int kTok = 8 * kN;
-  __shared__ float part[kFewWarps][kW4Rows][kTok + 1];
-  __shared__ float sums[kTok][kW4Rows];
+  constexpr int kB = RowsOf<kType>::kBytes, kU = 2, kCols = kU * kW4Cols, kS = kCols / kGroup;
+  constexpr int kTok = 8 * kN, kOut = kW4Rows * kR;
+  extern __shared__ float shared[];
+  float *part = shared;                                     // [warps][kTok][kOut + 1]
+  float *sums = shared + kFewWarps * kTok * (kOut + 1);     // [kTok][kOut]
   stream_order();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const int N = A.d.N, K = A.d.K, group = A.d.group;
-  const int col_tiles = (K + kW4Cols - 1) / kW4Cols;
+  const int N = A.d.N, K = A.d.K;
+  const int col_tiles = (K + kW4Cols - 1) / kW4Cols, row_tiles = (N + kW4Rows - 1) / kW4Rows, groups = (K + kGroup - 1) / kGroup;
   const int split = gridDim.x, rank = blockIdx.x;           // blocks of the cluster
-  const int row_tile = blockIdx.y;
-  const int n0 = row_tile * kW4Rows;
+  const int n0 = blockIdx.y * kOut;
   const long long tok0 = (long long)blockIdx.z * kTok;
-  const int slices = split * kFewWarps, slice = rank * kFewWarps + warp;
-  const int ct0 = (int)((long long)col_tiles * slice / slices), ct1 = (int)((long long)col_tiles * (slice + 1) / slices);
-  const int na = min(n0 + g, N - 1), nb = min(n0 + g + 8, N - 1);
-  const uint8_t *xrow[kN];
+  // stages of two column tiles: this warp's
+  const int stages = (col_tiles + kU - 1) / kU, slices = split * kFewWarps, slice = rank * kFewWarps + warp;
+  const int st0 = (int)((long long)stages * slice / slices), st1 = (int)((long long)stages * (slice + 1) / slices);
+  const uint8_t *x[kN];
 #pragma unroll
   for (int i = 0; i < kN; ++i)
-    xrow[i] = static_cast<const uint8_t *>(A.x) + min(tok0 + 8 * i + g, (long long)A.r.rows - 1) * A.r.x_stride * RowsOf<kType>::kBytes;
-  const uint4 *w = reinterpret_cast<const uint4 *>(A.w) + (size_t)row_tile * col_tiles * 32 + lane;
-  const bool x_groups = A.x_scales != nullptr && A.r.x_group != 0;
-  const int x_ngroups = (K + group - 1) / group;
-  float total[kN][4] = {};
-  for (int ct = ct0; ct < ct1; ++ct) {
-    const uint4 word = load_global(w + (size_t)ct * 32);
-    const uint32_t words[4] = {word.x, word.y, word.z, word.w};
-    uint32_t xv[kN][2][4];
+    x[i] = static_cast<const uint8_t *>(A.x) + min(tok0 + 8 * i + g, (long long)A.r.rows - 1) * A.r.x_stride * kB;
+  const uint4 *w[kR];
+  int na[kR], nb[kR];                                       // this lane's weight rows, inside the matrix
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      load_x8<kType>(xrow[i], ct * kW4Cols + 8 * t, K, pieces, xv[i][0]);
-      load_x8<kType>(xrow[i], ct * kW4Cols + 32 + 8 * t, K, pieces, xv[i][1]);
-    }
-    float acc[kN][4] = {};
+  for (int i = 0; i < kR; ++i) {
+    w[i] = reinterpret_cast<const uint4 *>(A.w) + (size_t)min((int)blockIdx.y * kR + i, row_tiles - 1) * col_tiles * 32 + w4_place(g, 8 * t);
+    na[i] = min(n0 + kW4Rows * i + g, N - 1);
+    nb[i] = min(n0 + kW4Rows * i + g + 8, N - 1);
+  }
+  const bool x_groups = kB == 1 && A.r.x_group != 0;
+  float total[kR][kN][4] = {};
+
+  struct Stage {
+    uint4 w[kR][kU];
+    uint32_t x[kN][2 * kU][2 * kB];         // as they lie in memory: a conversion would wait for its load
+    float sa[kR][kS], sb[kR][kS];
+    uint32_t za[kR][kS], zb[kR][kS];
+  };
+  auto load = [&](int st, Stage &s) {
+    if (st >= st1) return;
+    const int k0 = st * kCols;
+    const bool whole = pieces && k0 + kCols <= K;           // else column by column at the end of the rows
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int k = ct * kW4Cols + 32 * half, grp = min(k, K - 1) / group;
-      const size_t at = (size_t)grp * N;
-      const uint32_t za = w4_zero(A.zeros ? (uint32_t)load_global(A.zeros + at + na) : 8u, T());
-      const uint32_t zb = w4_zero(A.zeros ? (uint32_t)load_global(A.zeros + at + nb) : 8u, T());
-      const uint32_t va = words[half], vb = words[2 + half];
+    for (int i = 0; i < kR; ++i)
 #pragma unroll
-      for (int jj = 0; jj < 2; ++jj) {
-        const uint32_t a[4] = {w4_pair(va, 2 * jj, T(), za), w4_pair(vb, 2 * jj, T(), zb), w4_pair(va, 2 * jj + 1, T(), za), w4_pair(vb, 2 * jj + 1, T(), zb)};
+      for (int u = 0; u < kU; ++u) s.w[i][u] = load_global(w[i] + (size_t)min(st * kU + u, col_tiles - 1) * 32);
 #pragma unroll
-        for (int i = 0; i < kN; ++i) mma_16x8x16<T>(acc[i], a, xv[i][half][2 * jj], xv[i][half][2 * jj + 1]);
+    for (int i = 0; i < kN; ++i)
+#pragma unroll
+      for (int h = 0; h < 2 * kU; ++h) {
+        if (whole) load_x8_raw<kType>(x[i], k0 + 32 * h + 8 * t, INT_MAX, true, s.x[i][h]);
+        else load_x8_raw<kType>(x[i], k0 + 32 * h + 8 * t, K, pieces, s.x[i][h]);
       }
-      if ((half == 1 || group == 32) && (k < K || group != 32)) {       // (groups of 32: the second may not exist)
-        const float sa = load_global(A.scales + at + na), sb = load_global(A.scales + at + nb);
 #pragma unroll
-        for (int i = 0; i < kN; ++i) {
-          float s0 = 1.0f, s1 = 1.0f;
-          if (x_groups) {
-            const long long t0 = min(tok0 + 8 * i + 2 * t, (long long)A.r.rows - 1), t1 = min(tok0 + 8 * i + 2 * t + 1, (long long)A.r.rows - 1);
-            s0 = load_global(A.x_scales + t0 * x_ngroups + grp);
-            s1 = load_global(A.x_scales + t1 * x_ngroups + grp);
+    for (int h = 0; h < kS; ++h) {
+      const size_t at = (size_t)min(st * kS + h, groups - 1) * N;
+#pragma unroll
+      for (int i = 0; i < kR; ++i) {
+        s.sa[i][h] = load_global(A.scales + at + na[i]);
+        s.sb[i][h] = load_global(A.scales + at + nb[i]);
+        s.za[i][h] = kZeros ? load_global(A.zeros + at + na[i]) : 8u;
+        s.zb[i][h] = kZeros ? load_global(A.zeros + at + nb[i]) : 8u;
+      }
+    }
+  };
+  auto multiply = [&](int st, const Stage &s) {
+    const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    uint32_t xv[kN][2 * kU][4];
+#pragma unroll
+    for (int n = 0; n < kN; ++n)
+#pragma unroll
+      for (int h = 0; h < 2 * kU; ++h) x8_pairs<kType>(s.x[n][h], xv[n][h]);
+#pragma unroll
+    for (int i = 0; i < kR; ++i) {
+      float acc[kN][4];
+#pragma unroll
+      for (int h = 0; h < 2 * kU; ++h) {                    // 32 columns
+        const int grp = 32 * h / kGroup;
+        const uint4 q = s.w[i][h / 2];
+        const uint32_t va = h % 2 ? q.y : q.x, vb = h % 2 ? q.w : q.z;
+        const uint32_t za = w4_zero(s.za[i][grp], T()), zb = w4_zero(s.zb[i][grp], T());
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t a[4] = {w4_pair(va, 2 * j, T(), za), w4_pair(vb, 2 * j, T(), zb), w4_pair(va, 2 * j + 1, T(), za), w4_pair(vb, 2 * j + 1, T(), zb)};
+#pragma unroll
+          for (int n = 0; n < kN; ++n)
+            mma_16x8x16<T>(acc[n], a, xv[n][h][2 * j], xv[n][h][2 * j + 1], 32 * h % kGroup == 0 && j == 0 ? none : acc[n]);
+        }
+        // a group is complete (one that does not exist is left out)
+        if ((32 * h + 32) % kGroup != 0 || st * kS + grp >= groups) continue;
+        const float sa = s.sa[i][grp], sb = s.sb[i][grp];
+#pragma unroll
+        for (int n = 0; n < kN; ++n) {
+          if (kB == 1 && x_groups) {
+            const long long last = (long long)A.r.rows - 1, t0 = min(tok0 + 8 * n + 2 * t, last), t1 = min(tok0 + 8 * n + 2 * t + 1, last);
+            const float s0 = load_global(A.x_scales + t0 * groups + st * kS + grp), s1 = load_global(A.x_scales + t1 * groups + st * kS + grp);
+            acc[n][0] *= s0; acc[n][1] *= s1; acc[n][2] *= s0; acc[n][3] *= s1;
           }
-          total[i][0] = fmaf(acc[i][0] * s0, sa, total[i][0]);
-          total[i][1] = fmaf(acc[i][1] * s1, sa, total[i][1]);
-          total[i][2] = fmaf(acc[i][2] * s0, sb, total[i][2]);
-          total[i][3] = fmaf(acc[i][3] * s1, sb, total[i][3]);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) acc[i][q] = 0.0f;
+          total[i][n][0] = fmaf(acc[n][0], sa, total[i][n][0]);
+          total[i][n][1] = fmaf(acc[n][1], sa, total[i][n][1]);
+          total[i][n][2] = fmaf(acc[n][2], sb, total[i][n][2]);
+          total[i][n][3] = fmaf(acc[n][3], sb, total[i][n][3]);
         }
       }
     }
+  };
+  // stages come in two ahead, by name (moving one to the other would wait for its loads)
+  Stage s0, s1;
+  load(st0, s0);
+  load(st0 + 1, s1);
+#pragma unroll 1
+  for (int st = st0; st < st1; st += 2) {
+    multiply(st, s0);
+    load(st + 2, s0);
+    if (st + 1 >= st1) break;
+    multiply(st + 1, s1);
+    load(st + 3, s1);
   }
 #pragma unroll
-  for (int i = 0; i < kN; ++i) {
-    part[warp][g][8 * i + 2 * t] = total[i][0];
-    part[warp][g][8 * i + 2 * t + 1] = total[i][1];
-    part[warp][g + 8][8 * i + 2 * t] = total[i][2];
-    part[warp][g + 8][8 * i + 2 * t + 1] = total[i][3];
-  }
+  for (int i = 0; i < kR; ++i)
+#pragma unroll
+    for (int n = 0; n < kN; ++n) {
+      float *p = part + (warp * kTok + 8 * n + 2 * t) * (kOut + 1) + kW4Rows * i + g;
+      p[0] = total[i][n][0];
+      p[kOut + 1] = total[i][n][1];
+      p[8] = total[i][n][2];
+      p[kOut + 1 + 8] = total[i][n][3];
+    }
   __syncthreads();
-  for (int e = threadIdx.x; e < kTok * kW4Rows; e += kFewThreads) {
-    const int n = e % kW4Rows, tok = e / kW4Rows;
-    float s = part[0][n][tok];
+  const int toks = (int)min((long long)kTok, A.r.rows - tok0);
+  for (int e = threadIdx.x; e < toks * kOut; e += kFewThreads) {
+    const int n = e % kOut, tok = e / kOut;
+    float s = part[tok * (kOut + 1) + n];
 #pragma unroll
-    for (int i = 1; i < kFewWarps; ++i) s += part[i][n][tok];
-    sums[tok][n] = s;
+    for (int i = 1; i < kFewWarps; ++i) s += part[(i * kTok + tok) * (kOut + 1) + n];
+    sums[e] = s;
   }
   if (split > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-  else __syncthreads();
+  // (without a cluster every thread reads what it wrote itself)
   // the cluster's blocks write the outputs in turn; each adds the blocks' sums in the same order
-  for (int e = rank * kFewThreads + threadIdx.x; e < kTok * kW4Rows; e += split * kFewThreads) {
-    const int n = e % kW4Rows, tok = e / kW4Rows;
+  for (int e = rank * kFewThreads + threadIdx.x; e < toks * kOut; e += split * kFewThreads) {
+    const int n = e % kOut;
     float s = 0.0f;
-    if (split == 1) s = sums[tok][n];
+    if (split == 1) s = sums[e];
     else
       for (int i = 0; i < split; ++i) {
         uint32_t a;
         float v;
-        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(&sums[tok][n])), "r"(i));
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(sums + e)), "r"(i));
         asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
         s += v;
       }
-    const long long row = tok0 + tok;
-    if (row >= A.r.rows || n0 + n >= N) continue;
+    if (n0 + n >= N) continue;
+    const long long row = tok0 + e / kOut;
     if (A.x_scales != nullptr && !x_groups) s *= load_global(A.x_scales + row);
     const size_t at = (size_t)(row * A.r.out_stride) + n0 + n;
     if (A.r.out_type == XNOR_F32) static_cast<float *>(A.out)[at] = s;
@@ -275,20 +336,34 @@ w4_few_rows_kernel(const W4Args A, int pieces) {
   if (split > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+#ifndef FEW_R1
+#define FEW_R1 1
+#define FEW_R2 2
+#define FEW_BLOCKS 1
+#endif
+template <int kType, int kN, int kR, int kGroup, bool kZeros>
+cudaError_t few_rows(const W4Args &a, cudaStream_t st) {
+  constexpr int kTok = 8 * kN, kOut = kW4Rows * kR;
+  constexpr size_t kSmem = (size_t)(kFewWarps * kTok * (kOut + 1) + kTok * kOut) * sizeof(float);
+  static_assert(kSmem <= 48 * 1024, "shared memory");
+  const int blocks = (w4_row_tiles(a.d) + kR - 1) / kR, col_tiles = w4_col_tiles(a.d);
+  // blocks of a cluster divide the columns while the blocks are fewer than the GPU has SMs and every warp
+  // keeps two tiles
+  int split = 1;
+  while (split < kMaxSplit && blocks * split < FEW_BLOCKS * sm_count_of_current_device() && col_tiles >= 4 * split * kFewWarps) split *= 2;
+  const int pieces = rows_in_pieces(a.x, a.r.x_stride, 8, RowsOf<kType>::kBytes);
+  const dim3 grid((unsigned)split, (unsigned)blocks, (unsigned)((a.r.rows + kTok - 1) / kTok));
+  return launch_kernel(w4_few_rows_kernel<kType, kN, kR, kGroup, kZeros>, grid, kFewThreads, kSmem, st, (unsigned)split, a, pieces);
+}
+template <int kType, int kN, int kR>
+cudaError_t few_rows(const W4Args &a, cudaStream_t st) {
+  if (a.d.group == 32) return a.zeros ? few_rows<kType, kN, kR, 32, true>(a, st) : few_rows<kType, kN, kR, 32, false>(a, st);
+  if (a.d.group == 64) return a.zeros ? few_rows<kType, kN, kR, 64, true>(a, st) : few_rows<kType, kN, kR, 64, false>(a, st);
+  return a.zeros ? few_rows<kType, kN, kR, 128, true>(a, st) : few_rows<kType, kN, kR, 128, false>(a, st);
+}
 template <int kType>
 cudaError_t few_rows(const W4Args &a, cudaStream_t st) {
-  const int row_tiles = w4_row_tiles(a.d), col_tiles = w4_col_tiles(a.d);
-  // blocks of a cluster divide the columns while the blocks are fewer than the GPU takes at once and
-  // every warp keeps two tiles
-  int split = 1;
-  while (split < kMaxSplit && row_tiles * split < 2 * sm_count_of_current_device() && col_tiles >= 4 * split * kFewWarps) split *= 2;
-  const int pieces = rows_in_pieces(a.x, a.r.x_stride, 8, RowsOf<kType>::kBytes);
-  const int n = a.r.rows > 8 ? 2 : 1;
-  const long long token_blocks = (a.r.rows + 8ll * n - 1) / (8 * n);
-  // (a grid has at most 65535 blocks along y and z)
-  const dim3 grid((unsigned)split, (unsigned)row_tiles, (unsigned)token_blocks);
-  if (n == 1) return launch_kernel(w4_few_rows_kernel<kType, 1>, grid, kFewThreads, 0, st, (unsigned)split, a, pieces);
-  return launch_kernel(w4_few_rows_kernel<kType, 2>, grid, kFewThreads, 0, st, (unsigned)split, a, pieces);
+  return a.r.rows <= 8 ? few_rows<kType, 1, FEW_R1>(a, st) : few_rows<kType, 2, FEW_R2>(a, st);
 }
 
 dim3 lay_grid(const xnor_w4_desc &d) { return dim3((unsigned)((w4_col_tiles(d) + 1) / 2), (unsigned)w4_row_tiles(d)); }

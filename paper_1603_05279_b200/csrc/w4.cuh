@@ -2,17 +2,19 @@
 //
 // Codes 0 .. 15 lie in tiles of 16 rows x 64 columns, 512 bytes: u32 [row tiles][column tiles][32 lanes][4].
 // A word holds eight neighbouring columns of one row, column 2 i + h in bits 4 i + 16 h and up: a mask brings two
-// neighbouring columns to where two 16-bit values have them.  Lane 4 g + t (g = 0 .. 7, t = 0 .. 3) holds, of
-// row g, columns 8 t .. and 32 + 8 t .., then the same of row g + 8.  So a lane's four words are what four
-// m16n8k16 steps want of it in the matrix operand (the columns of a step, in any order, only have to be the
-// same as those of the rows that they meet), two steps each for 32 neighbouring columns, the smallest group.
+// neighbouring columns to where two 16-bit values have them.  Place 4 g + (t ^ (g >> 1 & 3)) of a tile (g = 0 .. 7,
+// t = 0 .. 3) holds, of row g, columns 8 t .. and 32 + 8 t .., then the same of row g + 8.  So its four words are
+// what four m16n8k16 steps want of a lane in the matrix operand (the columns of a step, in any order, only have
+// to be the same as those of the rows that they meet), two steps each for 32 neighbouring columns, the smallest
+// group.  And threads that read a whole row each, from shared memory, meet in no bank: that is what t is turned
+// for.
 #pragma once
 #include "rows.cuh"
 
 namespace xnor {
 
-// Lane and word of the tile that hold row r, columns c .. c + 7 (c a multiple of 8).
-__host__ __device__ __forceinline__ int w4_lane(int r, int c) { return 4 * (r & 7) + ((c & 31) >> 3); }
+// Place and word of the tile that hold row r, columns c .. c + 7 (c a multiple of 8).
+__host__ __device__ __forceinline__ int w4_place(int r, int c) { return 4 * (r & 7) + (((c & 31) >> 3) ^ ((r >> 1) & 3)); }
 __host__ __device__ __forceinline__ int w4_word(int r, int c) { return 2 * ((r >> 3) & 1) + (c >> 5); }
 
 __host__ __device__ __forceinline__ int w4_bit(int column) { return 4 * (column >> 1) + 16 * (column & 1); }
@@ -53,11 +55,21 @@ struct RowsOf {
 template <> struct RowsOf<XNOR_BF16> { using T = __nv_bfloat16; static constexpr int kBytes = 2; };
 template <> struct RowsOf<XNOR_F16> { using T = __half; static constexpr int kBytes = 2; };
 
+// As four pairs; `raw` is what lies in memory.
 template <int kType>
-__device__ __forceinline__ void load_x8(const uint8_t *row, int k, int K, bool pieces, uint32_t v[4]) {
+__device__ __forceinline__ void x8_pairs(const uint32_t (&raw)[2 * RowsOf<kType>::kBytes], uint32_t (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (RowsOf<kType>::kBytes == 2) v[i] = raw[i];
+    else if constexpr (kType == XNOR_I8) v[i] = i8_pair(raw[i / 2], i & 1);
+    else v[i] = e4m3_pair((raw[i / 2] >> (16 * (i & 1))) & 0xFFFFu);
+  }
+}
+// Columns k .. k + 7 of a row of K as they lie in memory; some may not exist (zeros) or lie anywhere.
+template <int kType>
+__device__ __forceinline__ void load_x8_raw(const uint8_t *row, int k, int K, bool pieces, uint32_t (&raw)[2 * RowsOf<kType>::kBytes]) {
   constexpr int kB = RowsOf<kType>::kBytes;
   const uint8_t *p = row + (size_t)k * kB;
-  uint32_t raw[2 * kB];
   if (pieces && k + 8 <= K) {
     if constexpr (kB == 2) {
       const uint4 q = load_global(reinterpret_cast<const uint4 *>(p));
@@ -66,22 +78,22 @@ __device__ __forceinline__ void load_x8(const uint8_t *row, int k, int K, bool p
       const uint2 q = load_global(reinterpret_cast<const uint2 *>(p));
       raw[0] = q.x; raw[1] = q.y;
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 2 * kB; ++i) raw[i] = 0u;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (k + i >= K) continue;
-      if constexpr (kB == 2) raw[i / 2] |= (uint32_t)load_global(reinterpret_cast<const uint16_t *>(p) + i) << (16 * (i & 1));
-      else raw[i / 4] |= (uint32_t)load_global(p + i) << (8 * (i & 3));
-    }
+    return;
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (kB == 2) v[i] = raw[i];
-    else if constexpr (kType == XNOR_I8) v[i] = i8_pair(raw[i / 2], i & 1);
-    else v[i] = e4m3_pair((raw[i / 2] >> (16 * (i & 1))) & 0xFFFFu);
+  for (int i = 0; i < 2 * kB; ++i) raw[i] = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (k + i >= K) continue;
+    if constexpr (kB == 2) raw[i / 2] |= (uint32_t)load_global(reinterpret_cast<const uint16_t *>(p) + i) << (16 * (i & 1));
+    else raw[i / 4] |= (uint32_t)load_global(p + i) << (8 * (i & 3));
   }
+}
+template <int kType>
+__device__ __forceinline__ void load_x8(const uint8_t *row, int k, int K, bool pieces, uint32_t (&v)[4]) {
+  uint32_t raw[2 * RowsOf<kType>::kBytes];
+  load_x8_raw<kType>(row, k, K, pieces, raw);
+  x8_pairs<kType>(raw, v);
 }
 
 }  // namespace xnor

@@ -245,12 +245,12 @@ __device__ void expand_role(const TcParams &P, const Smem &S, const Span &span, 
   for (int tile = first; tile < total; tile += step, seq += (uint32_t)per_tile) {
     const int nc = min((tile % P.row_tiles) * kTileN + r, N - 1);
     const uint2 *w = reinterpret_cast<const uint2 *>(P.A.w) +
-                     ((size_t)(nc / kW4Rows) * P.col_tiles * 32 + 4 * (nc & 7)) * 2 + ((nc >> 3) & 1);
+                     ((size_t)(nc / kW4Rows) * P.col_tiles * 32) * 2 + ((nc >> 3) & 1);
     auto fetch = [&](int i, Ahead &f) {
       if (i >= per_tile) return;
       const int c = span.c0 + i;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) f.w[t] = load_global(w + ((size_t)c * 32 + t) * 2);
+      for (int t = 0; t < 4; ++t) f.w[t] = load_global(w + ((size_t)c * 32 + w4_place(nc, 8 * t)) * 2);
       f.z[0] = f.z[1] = 8u;
       if (P.A.zeros) {
         f.z[0] = load_global(P.A.zeros + (size_t)min(c * kChunk / group, last_group) * N + nc);

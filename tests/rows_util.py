@@ -89,7 +89,8 @@ def unpack_codes(packed, N, K):
     rt, ct = p.shape[:2]
     out = np.zeros((rt * 16, ct * 64), np.uint8)
     for lane in range(32):
-        g, t = lane // 4, lane % 4
+        g = lane // 4
+        t = (lane % 4) ^ (g // 2 % 4)
         for word in range(4):
             row, col = g + 8 * (word // 2), 32 * (word % 2) + 8 * t
             for i in range(8):
@@ -105,7 +106,8 @@ def pack_codes(codes):
     full[:N, :K] = codes
     p = np.zeros((rt, ct, 32, 4), np.uint32)
     for lane in range(32):
-        g, t = lane // 4, lane % 4
+        g = lane // 4
+        t = (lane % 4) ^ (g // 2 % 4)
         for word in range(4):
             row, col = g + 8 * (word // 2), 32 * (word % 2) + 8 * t
             for i in range(8):
