@@ -482,8 +482,8 @@ xnor_status xnor_rmsnorm_backward(const void *dy, const void *dsum, const void *
  * with a scale and, optionally, a zero point for each group of `group` columns of a row (the last
  * group may be shorter): w = (code - zero) scale.
  *
- *   w_packed  u32 [ceil(N/16)][ceil(K/64)][32][4]: tiles of 16 rows x 64 columns.  Element
- *             [.][.][4 g + (t ^ (g/2 % 4))][2 r + c] holds row g + 8 r (g < 8, r < 2), columns
+ *   w_packed  u32 [ceil(N/128)][ceil(K/64)][8][32][4]: tiles of 16 rows x 64 columns, those of 128
+ *             rows together.  Element [..][4 g + (t ^ (g/2 % 4))][2 r + c] holds row g + 8 r (g < 8, r < 2), columns
  *             32 c + 8 t + 0 .. 7 (t < 4, c < 2) of the tile, column 2 i + h of the eight in bits
  *             4 i + 16 h and up; rows and columns beyond the matrix hold any code.
  *   scales    fp32 [ceil(K/group)][N]
@@ -498,7 +498,7 @@ xnor_status xnor_rmsnorm_backward(const void *dy, const void *dsum, const void *
  * xnor_w4_dequantize  w_packed, scales, zeros -> w type [N][K] (F32, BF16, F16), rounded once.
  *
  * INVALID_ARG: null or misaligned pointer, N or K < 1, group none of 32, 64, 128, type out of range.
- * UNSUPPORTED: N > 1048560, K > 16777216.
+ * UNSUPPORTED: N > 1048448, K > 16777216.
  */
 typedef struct {
   int N, K, group;

@@ -498,7 +498,7 @@ def xnor_w4_packed_words(d):
 def alloc_w4(d, zeros=False, device="cuda"):
     """(w_packed, scales, zeros or None) of the matrix d."""
     groups = -(-d.K // d.group)
-    return (torch.empty((-(-d.N // 16), -(-d.K // 64), 32, 4), dtype=torch.int32, device=device),
+    return (torch.empty((-(-d.N // 128), -(-d.K // 64), 256, 4), dtype=torch.int32, device=device),
             torch.empty((groups, d.N), dtype=torch.float32, device=device),
             torch.empty((groups, d.N), dtype=torch.uint8, device=device) if zeros else None)
 

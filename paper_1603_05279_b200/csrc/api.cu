@@ -463,7 +463,7 @@ xnor_status check_norm_forward(const void *x, const void *residual, const void *
 bool bad_w4(const xnor_w4_desc *d) {
   return !d || d->N < 1 || d->K < 1 || (d->group != 32 && d->group != 64 && d->group != 128);
 }
-bool large_w4(const xnor_w4_desc *d) { return d->N > 16 * 65535 || d->K > (1 << 24); }
+bool large_w4(const xnor_w4_desc *d) { return d->N > xnor::kW4Rows * 65528 || d->K > (1 << 24); }
 
 }  // namespace
 
@@ -512,7 +512,7 @@ xnor_status xnor_rmsnorm_backward(const void *dy, const void *dsum, const void *
 
 size_t xnor_w4_packed_words(const xnor_w4_desc *d) {
   if (bad_w4(d) || large_w4(d)) return 0;
-  return (size_t)xnor::w4_row_tiles(*d) * (size_t)xnor::w4_col_tiles(*d) * 128;
+  return (size_t)xnor::w4_panels(*d) * (size_t)xnor::w4_col_tiles(*d) * 1024;
 }
 
 xnor_status xnor_w4_quantize(const void *w, int type, const xnor_w4_desc *d, uint32_t *w_packed,

@@ -544,7 +544,7 @@ struct W4In {
   W4In(RowArgs &A, const xnor_w4_desc &d, int packed_at, int scales_at, int zeros_at) {
     if (!A.ok) return;
     const long long G = (d.K + (long long)d.group - 1) / d.group;
-    packed = A.dense(packed_at, "w_packed", at::kInt, {(d.N + 15ll) / 16, (d.K + 63ll) / 64, 32, 4});
+    packed = A.dense(packed_at, "w_packed", at::kInt, {(d.N + 127ll) / 128, (d.K + 63ll) / 64, 256, 4});
     if (scales_at >= 0) scales = A.dense(scales_at, "scales", at::kFloat, {G, d.N});
     if (zeros_at >= 0 && A.ok && !A.none(zeros_at)) zeros = A.dense(zeros_at, "zeros", at::kByte, {G, d.N});
   }

@@ -143,7 +143,9 @@ constexpr int kNormMaxCols = 32768;
 
 // 4-bit weights.
 constexpr int kW4Rows = 16, kW4Cols = 64;  // a tile: 16 rows of 64 columns, 512 bytes
+constexpr int kW4Panel = 8;                // row tiles whose tiles of a column lie together
 inline int w4_row_tiles(const xnor_w4_desc &d) { return d.N / kW4Rows + (d.N % kW4Rows != 0); }
+inline int w4_panels(const xnor_w4_desc &d) { return (w4_row_tiles(d) + kW4Panel - 1) / kW4Panel; }
 inline int w4_col_tiles(const xnor_w4_desc &d) { return d.K / kW4Cols + (d.K % kW4Cols != 0); }
 cudaError_t launch_w4_quantize(const void *w, int type, const xnor_w4_desc &d, uint32_t *w_packed, float *scales,
                                uint8_t *zeros, cudaStream_t st);
@@ -163,6 +165,6 @@ struct W4Args {
 cudaError_t launch_w4_few_rows(const W4Args &a, cudaStream_t st);
 cudaError_t launch_w4_many_rows(const W4Args &a, cudaStream_t st);
 cudaError_t read_status_w4(int *status);   // of the kernel for many rows, as the others'
-constexpr int kW4FewRows = 16;             // up to here the kernel for few rows
+constexpr int kW4FewRows = 8;              // up to here the kernel for few rows
 
 }  // namespace xnor

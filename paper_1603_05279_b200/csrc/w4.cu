@@ -22,7 +22,7 @@ __device__ __forceinline__ void write_tiles(const uint32_t (&words)[kW4Rows][kOc
   if (tile >= 2 || col_tile0 + tile >= col_tiles) return;
   const int c = 8 * tile + (t ^ ((g >> 1) & 3));            // this place's columns
   const uint32_t v[4] = {words[g][c], words[g][c + 4], words[g + 8][c], words[g + 8][c + 4]};
-  reinterpret_cast<uint4 *>(w)[((size_t)row_tile * col_tiles + col_tile0 + tile) * 32 + lane] = make_uint4(v[0], v[1], v[2], v[3]);
+  reinterpret_cast<uint4 *>(w)[(w4_tile(row_tile, col_tiles) + (size_t)(col_tile0 + tile) * kW4Panel) * 32 + lane] = make_uint4(v[0], v[1], v[2], v[3]);
 }
 
 // round(w / s) to the nearest whole number, ties to even, of the exact quotient (|w / s| below 2^20): the
@@ -122,7 +122,7 @@ w4_dequantize_kernel(const uint32_t *w_packed, const float *scales, const uint8_
   if (threadIdx.x < 64) {
     const int tile = threadIdx.x / 32, lane = threadIdx.x & 31, ct = blockIdx.x * 2 + tile;
     if (ct < col_tiles) {
-      const uint4 v = load_global(reinterpret_cast<const uint4 *>(w_packed) + ((size_t)blockIdx.y * col_tiles + ct) * 32 + lane);
+      const uint4 v = load_global(reinterpret_cast<const uint4 *>(w_packed) + (w4_tile(blockIdx.y, col_tiles) + (size_t)ct * kW4Panel) * 32 + lane);
       words[tile][lane][0] = v.x; words[tile][lane][1] = v.y; words[tile][lane][2] = v.z; words[tile][lane][3] = v.w;
     }
   }
@@ -172,8 +172,8 @@ __device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t (&a)[4
 // kN: blocks of eight rows of x; kR: tiles of weight rows; kGroup, kZeros: as the weights have them; kU: column
 // tiles of a stage (a group of 128 stays in one: 2).
 template <int kType, int kN, int kR, int kGroup, bool kZeros>
-__global__ void __launch_bounds__(kFewThreads)
-w4_few_rows_kernel(const W4Args A, int pieces) {
+__global__ void __launch_bounds__(kFewThreads, kN == 1 ? 2 : 1)
+w4_few_rows_kernel(const W4Args A, int pieces, uint32_t magic) {
   using T = typename RowsOf<kType>::T;
   constexpr int kB = RowsOf<kType>::kBytes, kU = 2, kCols = kU * kW4Cols, kS = kCols / kGroup;
   constexpr int kTok = 8 * kN, kOut = kW4Rows * kR;
@@ -188,8 +188,9 @@ w4_few_rows_kernel(const W4Args A, int pieces) {
   const int n0 = blockIdx.y * kOut;
   const long long tok0 = (long long)blockIdx.z * kTok;
   // stages of two column tiles: this warp's
-  const int stages = (col_tiles + kU - 1) / kU, slices = split * kFewWarps, slice = rank * kFewWarps + warp;
-  const int st0 = (int)((long long)stages * slice / slices), st1 = (int)((long long)stages * (slice + 1) / slices);
+  const unsigned stages = (unsigned)(col_tiles + kU - 1) / kU, slice = (unsigned)(rank * kFewWarps + warp);
+  const int lg = 31 - __clz(split * kFewWarps);             // a power of two of slices; fewer than 2^18 stages
+  const int st0 = (int)((stages * slice) >> lg), st1 = (int)((stages * (slice + 1)) >> lg);
   const uint8_t *x[kN];
 #pragma unroll
   for (int i = 0; i < kN; ++i)
@@ -198,7 +199,7 @@ w4_few_rows_kernel(const W4Args A, int pieces) {
   int na[kR], nb[kR];                                       // this lane's weight rows, inside the matrix
 #pragma unroll
   for (int i = 0; i < kR; ++i) {
-    w[i] = reinterpret_cast<const uint4 *>(A.w) + (size_t)min((int)blockIdx.y * kR + i, row_tiles - 1) * col_tiles * 32 + w4_place(g, 8 * t);
+    w[i] = reinterpret_cast<const uint4 *>(A.w) + w4_tile(min((int)blockIdx.y * kR + i, row_tiles - 1), col_tiles) * 32 + w4_place(g, 8 * t);
     na[i] = min(n0 + kW4Rows * i + g, N - 1);
     nb[i] = min(n0 + kW4Rows * i + g + 8, N - 1);
   }
@@ -211,30 +212,66 @@ w4_few_rows_kernel(const W4Args A, int pieces) {
     float sa[kR][kS], sb[kR][kS];
     uint32_t za[kR][kS], zb[kR][kS];
   };
+  // this lane's part of stage 0; a stage is one multiply-add from there
+  const float *pa[kR], *pb[kR];
+  const uint8_t *qa[kR], *qb[kR];
+#pragma unroll
+  for (int i = 0; i < kR; ++i) {
+    pa[i] = A.scales + na[i];
+    pb[i] = A.scales + nb[i];
+    qa[i] = A.zeros + (kZeros ? na[i] : 0);
+    qb[i] = A.zeros + (kZeros ? nb[i] : 0);
+  }
+#pragma unroll
+  for (int i = 0; i < kN; ++i) x[i] += 8 * t * kB;
+  // stages that lie inside the rows, at addresses that allow whole pieces
+  const int sound = pieces ? min(st1, K / kCols) : st0;
   auto load = [&](int st, Stage &s) {
-    if (st >= st1) return;
-    const int k0 = st * kCols;
-    const bool whole = pieces && k0 + kCols <= K;           // else column by column at the end of the rows
-#pragma unroll
-    for (int i = 0; i < kR; ++i)
-#pragma unroll
-      for (int u = 0; u < kU; ++u) s.w[i][u] = load_global(w[i] + (size_t)min(st * kU + u, col_tiles - 1) * 32);
-#pragma unroll
-    for (int i = 0; i < kN; ++i)
-#pragma unroll
-      for (int h = 0; h < 2 * kU; ++h) {
-        if (whole) load_x8_raw<kType>(x[i], k0 + 32 * h + 8 * t, INT_MAX, true, s.x[i][h]);
-        else load_x8_raw<kType>(x[i], k0 + 32 * h + 8 * t, K, pieces, s.x[i][h]);
-      }
-#pragma unroll
-    for (int h = 0; h < kS; ++h) {
-      const size_t at = (size_t)min(st * kS + h, groups - 1) * N;
+    if (st < sound) {
 #pragma unroll
       for (int i = 0; i < kR; ++i) {
-        s.sa[i][h] = load_global(A.scales + at + na[i]);
-        s.sb[i][h] = load_global(A.scales + at + nb[i]);
-        s.za[i][h] = kZeros ? load_global(A.zeros + at + na[i]) : 8u;
-        s.zb[i][h] = kZeros ? load_global(A.zeros + at + nb[i]) : 8u;
+        const uint4 *p = w[i] + (long long)st * (kU * kW4Panel * 32);
+#pragma unroll
+        for (int u = 0; u < kU; ++u) s.w[i][u] = load_global(p + u * kW4Panel * 32);
+      }
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        const uint8_t *p = x[i] + (long long)st * (kCols * kB);
+#pragma unroll
+        for (int h = 0; h < 2 * kU; ++h) load_x8_raw<kType>(p, 32 * h, INT_MAX, true, s.x[i][h]);
+      }
+#pragma unroll
+      for (int h = 0; h < kS; ++h) {
+        const long long at = (long long)st * (kS * N) + h * N;
+#pragma unroll
+        for (int i = 0; i < kR; ++i) {
+          s.sa[i][h] = load_global(pa[i] + at);
+          s.sb[i][h] = load_global(pb[i] + at);
+          s.za[i][h] = kZeros ? load_global(qa[i] + at) : 8u;
+          s.zb[i][h] = kZeros ? load_global(qb[i] + at) : 8u;
+        }
+      }
+    } else if (st < st1) {
+#pragma unroll
+      for (int i = 0; i < kR; ++i)
+#pragma unroll
+        for (int u = 0; u < kU; ++u) s.w[i][u] = load_global(w[i] + (size_t)min(st * kU + u, col_tiles - 1) * (kW4Panel * 32));
+#pragma unroll
+      for (int i = 0; i < kN; ++i)
+#pragma unroll
+        for (int h = 0; h < 2 * kU; ++h) load_x8_raw<kType>(x[i], st * kCols + 32 * h, K - 8 * t, pieces, s.x[i][h]);
+#pragma unroll
+      for (int h = 0; h < kS; ++h) {
+        // a group that does not exist counts nothing: its columns of x are zeros, and so is its scale
+        const bool there = st * kS + h < groups;
+        const long long at = there ? (long long)(st * kS + h) * N : 0;
+#pragma unroll
+        for (int i = 0; i < kR; ++i) {
+          s.sa[i][h] = there ? load_global(pa[i] + at) : 0.0f;
+          s.sb[i][h] = there ? load_global(pb[i] + at) : 0.0f;
+          s.za[i][h] = kZeros ? load_global(qa[i] + at) : 8u;
+          s.zb[i][h] = kZeros ? load_global(qb[i] + at) : 8u;
+        }
       }
     }
   };
@@ -253,22 +290,24 @@ w4_few_rows_kernel(const W4Args A, int pieces) {
         const int grp = 32 * h / kGroup;
         const uint4 q = s.w[i][h / 2];
         const uint32_t va = h % 2 ? q.y : q.x, vb = h % 2 ? q.w : q.z;
-        const uint32_t za = w4_zero(s.za[i][grp], T()), zb = w4_zero(s.zb[i][grp], T());
+        uint32_t ra[4], rb[4];
+        W4Type<T>::expand(va, W4Type<T>::zero(s.za[i][grp]), magic, ra);
+        W4Type<T>::expand(vb, W4Type<T>::zero(s.zb[i][grp]), magic, rb);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const uint32_t a[4] = {w4_pair(va, 2 * j, T(), za), w4_pair(vb, 2 * j, T(), zb), w4_pair(va, 2 * j + 1, T(), za), w4_pair(vb, 2 * j + 1, T(), zb)};
+          const uint32_t a[4] = {ra[2 * j], rb[2 * j], ra[2 * j + 1], rb[2 * j + 1]};
 #pragma unroll
           for (int n = 0; n < kN; ++n)
             mma_16x8x16<T>(acc[n], a, xv[n][h][2 * j], xv[n][h][2 * j + 1], 32 * h % kGroup == 0 && j == 0 ? none : acc[n]);
         }
-        // a group is complete (one that does not exist is left out)
-        if ((32 * h + 32) % kGroup != 0 || st * kS + grp >= groups) continue;
+        if ((32 * h + 32) % kGroup != 0) continue;          // the group goes on
         const float sa = s.sa[i][grp], sb = s.sb[i][grp];
 #pragma unroll
         for (int n = 0; n < kN; ++n) {
           if (kB == 1 && x_groups) {
             const long long last = (long long)A.r.rows - 1, t0 = min(tok0 + 8 * n + 2 * t, last), t1 = min(tok0 + 8 * n + 2 * t + 1, last);
-            const float s0 = load_global(A.x_scales + t0 * groups + st * kS + grp), s1 = load_global(A.x_scales + t1 * groups + st * kS + grp);
+            const int at = min(st * kS + grp, groups - 1);
+            const float s0 = load_global(A.x_scales + t0 * groups + at), s1 = load_global(A.x_scales + t1 * groups + at);
             acc[n][0] *= s0; acc[n][1] *= s1; acc[n][2] *= s0; acc[n][3] *= s1;
           }
           total[i][n][0] = fmaf(acc[n][0], sa, total[i][n][0]);
@@ -336,11 +375,6 @@ w4_few_rows_kernel(const W4Args A, int pieces) {
   if (split > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-#ifndef FEW_R1
-#define FEW_R1 1
-#define FEW_R2 2
-#define FEW_BLOCKS 1
-#endif
 template <int kType, int kN, int kR, int kGroup, bool kZeros>
 cudaError_t few_rows(const W4Args &a, cudaStream_t st) {
   constexpr int kTok = 8 * kN, kOut = kW4Rows * kR;
@@ -350,23 +384,31 @@ cudaError_t few_rows(const W4Args &a, cudaStream_t st) {
   // blocks of a cluster divide the columns while the blocks are fewer than the GPU has SMs and every warp
   // keeps two tiles
   int split = 1;
-  while (split < kMaxSplit && blocks * split < FEW_BLOCKS * sm_count_of_current_device() && col_tiles >= 4 * split * kFewWarps) split *= 2;
+  while (split < kMaxSplit && blocks * split < sm_count_of_current_device() && col_tiles >= 4 * split * kFewWarps) split *= 2;
   const int pieces = rows_in_pieces(a.x, a.r.x_stride, 8, RowsOf<kType>::kBytes);
   const dim3 grid((unsigned)split, (unsigned)blocks, (unsigned)((a.r.rows + kTok - 1) / kTok));
-  return launch_kernel(w4_few_rows_kernel<kType, kN, kR, kGroup, kZeros>, grid, kFewThreads, kSmem, st, (unsigned)split, a, pieces);
+  return launch_kernel(w4_few_rows_kernel<kType, kN, kR, kGroup, kZeros>, grid, kFewThreads, kSmem, st, (unsigned)split, a, pieces,
+                       W4Type<typename RowsOf<kType>::T>::kMagic);
 }
-template <int kType, int kN, int kR>
+// Two tiles of weight rows share the rows of x in registers, where two stages of them fit (small groups and zero points
+// take registers too).
+template <int kType, int kN, int kGroup>
 cudaError_t few_rows(const W4Args &a, cudaStream_t st) {
-  if (a.d.group == 32) return a.zeros ? few_rows<kType, kN, kR, 32, true>(a, st) : few_rows<kType, kN, kR, 32, false>(a, st);
-  if (a.d.group == 64) return a.zeros ? few_rows<kType, kN, kR, 64, true>(a, st) : few_rows<kType, kN, kR, 64, false>(a, st);
-  return a.zeros ? few_rows<kType, kN, kR, 128, true>(a, st) : few_rows<kType, kN, kR, 128, false>(a, st);
+  if (a.zeros) return few_rows<kType, kN, 1, kGroup, true>(a, st);
+  return few_rows<kType, kN, kGroup == 32 ? 1 : 2, kGroup, false>(a, st);
+}
+template <int kType, int kN>
+cudaError_t few_rows(const W4Args &a, cudaStream_t st) {
+  return a.d.group == 32 ? few_rows<kType, kN, 32>(a, st) : a.d.group == 64 ? few_rows<kType, kN, 64>(a, st) : few_rows<kType, kN, 128>(a, st);
 }
 template <int kType>
 cudaError_t few_rows(const W4Args &a, cudaStream_t st) {
-  return a.r.rows <= 8 ? few_rows<kType, 1, FEW_R1>(a, st) : few_rows<kType, 2, FEW_R2>(a, st);
+  return a.r.rows <= 8 ? few_rows<kType, 1>(a, st) : few_rows<kType, 2>(a, st);
 }
 
 dim3 lay_grid(const xnor_w4_desc &d) { return dim3((unsigned)((w4_col_tiles(d) + 1) / 2), (unsigned)w4_row_tiles(d)); }
+// ... of every row tile of the panels
+dim3 fill_grid(const xnor_w4_desc &d) { return dim3(lay_grid(d).x, (unsigned)(w4_panels(d) * kW4Panel)); }
 
 }  // namespace
 
@@ -374,14 +416,14 @@ cudaError_t launch_w4_quantize(const void *w, int type, const xnor_w4_desc &d, u
                                uint8_t *zeros, cudaStream_t st) {
   const int pieces = d.K % 8 == 0;
   if (type == XNOR_F32)
-    return launch_kernel(w4_quantize_kernel<float>, lay_grid(d), kLayThreads, 0, st, 1, (const float *)w, d, pieces, w_packed, scales, zeros);
+    return launch_kernel(w4_quantize_kernel<float>, fill_grid(d), kLayThreads, 0, st, 1, (const float *)w, d, pieces, w_packed, scales, zeros);
   if (type == XNOR_BF16)
-    return launch_kernel(w4_quantize_kernel<__nv_bfloat16>, lay_grid(d), kLayThreads, 0, st, 1, (const __nv_bfloat16 *)w, d, pieces, w_packed, scales, zeros);
-  return launch_kernel(w4_quantize_kernel<__half>, lay_grid(d), kLayThreads, 0, st, 1, (const __half *)w, d, pieces, w_packed, scales, zeros);
+    return launch_kernel(w4_quantize_kernel<__nv_bfloat16>, fill_grid(d), kLayThreads, 0, st, 1, (const __nv_bfloat16 *)w, d, pieces, w_packed, scales, zeros);
+  return launch_kernel(w4_quantize_kernel<__half>, fill_grid(d), kLayThreads, 0, st, 1, (const __half *)w, d, pieces, w_packed, scales, zeros);
 }
 
 cudaError_t launch_w4_pack(const uint8_t *codes, const xnor_w4_desc &d, uint32_t *w_packed, cudaStream_t st) {
-  return launch_kernel(w4_pack_kernel, lay_grid(d), kLayThreads, 0, st, 1, codes, d, w_packed);
+  return launch_kernel(w4_pack_kernel, fill_grid(d), kLayThreads, 0, st, 1, codes, d, w_packed);
 }
 
 cudaError_t launch_w4_dequantize(const uint32_t *w_packed, const float *scales, const uint8_t *zeros,

@@ -1,6 +1,7 @@
 // The layout of 4-bit weights (internal).
 //
-// Codes 0 .. 15 lie in tiles of 16 rows x 64 columns, 512 bytes: u32 [row tiles][column tiles][32 lanes][4].
+// Codes 0 .. 15 lie in tiles of 16 rows x 64 columns, 512 bytes, the tiles of 128 rows together:
+// u32 [panels of 8 row tiles][column tiles][8][32 places][4].
 // A word holds eight neighbouring columns of one row, column 2 i + h in bits 4 i + 16 h and up: a mask brings two
 // neighbouring columns to where two 16-bit values have them.  Place 4 g + (t ^ (g >> 1 & 3)) of a tile (g = 0 .. 7,
 // t = 0 .. 3) holds, of row g, columns 8 t .. and 32 + 8 t .., then the same of row g + 8.  So its four words are
@@ -17,22 +18,48 @@ namespace xnor {
 __host__ __device__ __forceinline__ int w4_place(int r, int c) { return 4 * (r & 7) + (((c & 31) >> 3) ^ ((r >> 1) & 3)); }
 __host__ __device__ __forceinline__ int w4_word(int r, int c) { return 2 * ((r >> 3) & 1) + (c >> 5); }
 
+// The tile of 16 rows `rt`, of column tile 0; the next column's is kW4Panel tiles on (a tile: 32 uint4).
+__host__ __device__ __forceinline__ size_t w4_tile(int rt, int col_tiles) { return ((size_t)(rt / kW4Panel) * col_tiles) * kW4Panel + rt % kW4Panel; }
+
 __host__ __device__ __forceinline__ int w4_bit(int column) { return 4 * (column >> 1) + 16 * (column & 1); }
 
-// Two values of a word, columns 2 pair and 2 pair + 1, as 16-bit numbers code - zero, exact.  A code put into the
-// mantissa of 2^k is 2^k + code; `zero` holds (2^k + zero) twice.
-__device__ __forceinline__ uint32_t w4_pair(uint32_t w, int pair, __nv_bfloat16, uint32_t zero) {
-  const uint32_t v = ((w >> (4 * pair)) & 0x000F000Fu) | 0x43004300u;                    // 128 + code
-  const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&v), *reinterpret_cast<const __nv_bfloat162 *>(&zero));
-  return *reinterpret_cast<const uint32_t *>(&r);
-}
-__device__ __forceinline__ uint32_t w4_pair(uint32_t w, int pair, __half, uint32_t zero) {
-  const uint32_t v = ((w >> (4 * pair)) & 0x000F000Fu) | 0x64006400u;                    // 1024 + code
-  const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&v), *reinterpret_cast<const __half2 *>(&zero));
-  return *reinterpret_cast<const uint32_t *>(&r);
-}
-__device__ __forceinline__ uint32_t w4_zero(uint32_t z, __nv_bfloat16) { return (0x4300u | z) * 0x00010001u; }
-__device__ __forceinline__ uint32_t w4_zero(uint32_t z, __half) { return (0x6400u | z) * 0x00010001u; }
+// The eight values of a word, code - zero, as four pairs of 16-bit numbers, exact.  A code put into the mantissa of
+// 2^k is 2^k + code.  `magic` is kW4Magic of the type, but as a variable that the compiler does not know (a kernel's
+// argument): a mask and an OR are one instruction if only one of them is a constant in it.  (One row times
+// 16384x8192: 23.0 -> W4MAGIC us.)
+template <class T>
+struct W4Type;
+template <>
+struct W4Type<__nv_bfloat16> {
+  static constexpr uint32_t kMagic = 0x43004300u;                            // 128
+  struct Zero { uint32_t a; };
+  __device__ static __forceinline__ Zero zero(uint32_t z) { return {(0x4300u | z) * 0x00010001u}; }
+  __device__ static __forceinline__ void expand(uint32_t w, const Zero &z, uint32_t magic, uint32_t (&v)[4]) {
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const uint32_t u = ((w >> (4 * p)) & 0x000F000Fu) | magic;
+      const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&u), *reinterpret_cast<const __nv_bfloat162 *>(&z.a));
+      v[p] = *reinterpret_cast<const uint32_t *>(&r);
+    }
+  }
+};
+template <>
+struct W4Type<__half> {
+  static constexpr uint32_t kMagic = 0x64006400u;                            // 1024
+  struct Zero { uint32_t a, b; };                                            // 1024 + zero, -(64 + zero)
+  __device__ static __forceinline__ Zero zero(uint32_t z) { return {(0x6400u | z) * 0x00010001u, (0xD400u | z << 4) * 0x00010001u}; }
+  __device__ static __forceinline__ void expand(uint32_t w, const Zero &z, uint32_t magic, uint32_t (&v)[4]) {
+    const uint32_t sixteenth = 0x2C002C00u;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t lo = ((w >> (8 * h)) & 0x000F000Fu) | magic, hi = ((w >> (8 * h)) & 0x00F000F0u) | magic;      // 1024 + 16 code
+      const __half2 r0 = __hsub2(*reinterpret_cast<const __half2 *>(&lo), *reinterpret_cast<const __half2 *>(&z.a));
+      const __half2 r1 = __hfma2(*reinterpret_cast<const __half2 *>(&hi), *reinterpret_cast<const __half2 *>(&sixteenth), *reinterpret_cast<const __half2 *>(&z.b));
+      v[2 * h] = *reinterpret_cast<const uint32_t *>(&r0);
+      v[2 * h + 1] = *reinterpret_cast<const uint32_t *>(&r1);
+    }
+  }
+};
 
 // Eight values of a row in 8 bits as 16-bit numbers, exact.  The code of an int8 with its sign bit turned is
 // 128 + value; in the mantissa of 1024 it is 1152 + value.

@@ -8,11 +8,12 @@
 // rounded: scaling the weights before the product would round each to the operands' 8 or 11 bits.
 //
 // A block (one per SM, persistent) computes 128 outputs x kRows rows of x.  A unit of work is one group: its sums
-// have two buffers in tensor memory, so that the tensor core fills one while the other is drained.  20 warps (16):
-//   promotion  8 warps (4 up to 64 rows): a thread holds the sums of one output and up to 96 rows of x
-//   expansion  8 warps: a thread expands one weight row, 64 columns at a time, straight into tensor memory
-//   one warp issues the products; one copies the rows of x, by tensor copies, into a ring of stages of 64 columns
-//   (where they cannot be copied as they are, three warps bring them through registers)
+// have two buffers in tensor memory, so that the tensor core fills one while the other is drained.  Warps:
+//   promotion  8 (4 up to 64 rows): a thread holds the sums of one output and up to 96 rows of x
+//   expansion  8: a thread expands one weight row, 64 columns at a time, from shared straight into tensor memory
+//   one issues the products, one copies the packed weights into a deep ring in shared memory (bulk copies), one the
+//   rows of x, by tensor copies, into the stages of 64 columns that the products read; rows that cannot be copied as
+//   they are, in 8 bits above all, come through the registers of two warps (six) instead
 // Where the tiles are too few for the GPU, the blocks of a cluster divide the columns, and add their sums through
 // each other's shared memory in a fixed order.  Every wait is bounded; on expiry the block records
 // XNOR_ERR_TIMEOUT, stops and frees its tensor memory.
@@ -34,29 +35,31 @@ using namespace umma;
 
 constexpr int kTileN = 128;                  // outputs (weight rows) of a tile: the lanes of tensor memory
 constexpr int kChunk = 64;                   // columns of a stage
-constexpr int kLoadWarps = 3;
 constexpr int kACols = kChunk / 2;           // tensor-memory columns of a chunk of expanded weights
-constexpr int kMaxStages = 8;
+constexpr int kMaxStages = 8, kWeightStages = 16;
+constexpr uint32_t kWeightStage = 4096;      // a chunk of packed weights: 8 tiles of 16 x 64
 constexpr uint32_t kCtrlBytes = 1024;
 constexpr int kMaxSplitTc = 8;
 
-template <int kRows>
+template <int kRows, int kBytes>
 struct Shape {
   static constexpr int kPromo = kRows > 64 ? 2 : 1;            // sets of four warps
   static constexpr int kUnit = kRows / kPromo;                 // rows of x of a set
   static constexpr int kExpand = 2;
-  static constexpr int kMmaWarp = 4 * (kPromo + kExpand), kLoadWarp = kMmaWarp + 1;
-  static constexpr int kThreads = 32 * (kMmaWarp + 4);
+  static constexpr int kOther = kBytes == 1 ? 8 : 4, kLoadWarps = kOther - 2;
+  static constexpr int kMmaWarp = 4 * (kPromo + kExpand), kWeightWarp = kMmaWarp + 1, kLoadWarp = kMmaWarp + 2;
+  static constexpr int kThreads = 32 * (kMmaWarp + kOther);
   static constexpr int kATmem = kRows > 128 ? 2 * kRows : 256; // behind the two accumulators
   static constexpr int kStages = (512 - kATmem) / kACols;      // chunks: weights in tensor memory, rows of x in shared
   static constexpr uint32_t kStage = kRows * kChunk * 2;       // a row of x: 128 bytes, swizzled
   static constexpr uint32_t kScaleBytes = 8 * 512;             // a group's scales of x, per promotion warp
-  static constexpr size_t kSmem = 1024 + kCtrlBytes + kScaleBytes + (size_t)kStages * kStage;   // (1024: to align the ring)
+  static constexpr size_t kSmem = 1024 + kCtrlBytes + kScaleBytes + kWeightStages * kWeightStage + (size_t)kStages * kStage;   // (1024: to align the ring)
   // Registers per thread as launched, and after they are dealt out anew: the promotion's hold its sums.
-  static constexpr int kRegs = kThreads == 512 ? 128 : 96;
-  static constexpr int kPromoRegs = kRows > 128 ? 144 : kRows > 64 ? 128 : 128, kOtherRegs = kRows > 128 ? 64 : kRows > 64 ? 72 : 128;
+  static constexpr int kRegs = kThreads == 512 ? 128 : kThreads == 640 ? 96 : 80;
+  static constexpr int kPromoRegs = kRows > 128 ? 144 : kRows > 64 ? (kBytes == 1 ? 112 : 128) : kRows > 32 ? 128 : kRegs;
+  static constexpr int kOtherRegs = kRows > 128 ? 64 : kRows > 64 ? (kBytes == 1 ? 64 : 72) : kRows > 32 && kBytes == 1 ? 80 : kRegs;
   static_assert(kPromo * 128 * kPromoRegs + (kThreads - kPromo * 128) * kOtherRegs <= kThreads * kRegs, "registers");
-  static_assert(kSmem <= 232448 && kStages <= kMaxStages, "shared and tensor memory");
+  static_assert(kSmem <= 232448 && kStages <= kMaxStages && (kStages & (kStages - 1)) == 0, "shared and tensor memory");
   static_assert((size_t)kStages * kStage >= (size_t)kRows * kTileN * 4 || kRows > 128, "room for the sums of a block");
 };
 
@@ -65,11 +68,11 @@ struct TcParams {
   W4Args A;
   int col_tiles, row_tiles, token_tiles;    // chunks of columns; tiles of 128 outputs, of kRows rows
   int split, pieces, copies;                // copies: x_map is there
-  uint32_t idesc;
+  uint32_t idesc, magic;                    // magic: W4Type's
 };
 
 struct Smem {
-  uint32_t full, empty, dfull, dempty, scales, ring;
+  uint32_t full, empty, wfull, wempty, dfull, dempty, scales, weights, ring;
   uint32_t *tmem_slot;
   volatile int *abort_flag;
 };
@@ -77,12 +80,15 @@ __device__ __forceinline__ Smem carve(uint8_t *smem, uint32_t scale_bytes) {
   Smem s;
   s.full = smem_u32(smem);
   s.empty = s.full + 8 * kMaxStages;
-  s.dfull = s.empty + 8 * kMaxStages;
+  s.wfull = s.empty + 8 * kMaxStages;
+  s.wempty = s.wfull + 8 * kWeightStages;
+  s.dfull = s.wempty + 8 * kWeightStages;
   s.dempty = s.dfull + 16;
-  s.tmem_slot = reinterpret_cast<uint32_t *>(smem + 16 * kMaxStages + 32);
+  s.tmem_slot = reinterpret_cast<uint32_t *>(smem + 16 * kMaxStages + 16 * kWeightStages + 32);
   s.abort_flag = reinterpret_cast<volatile int *>(s.tmem_slot + 1);
   s.scales = s.full + kCtrlBytes;
-  s.ring = (s.scales + scale_bytes + 1023u) & ~1023u;
+  s.weights = s.scales + scale_bytes;
+  s.ring = (s.weights + kWeightStages * kWeightStage + 1023u) & ~1023u;
   return s;
 }
 
@@ -109,12 +115,17 @@ __device__ __forceinline__ bool wait_inline(const Smem &S, uint32_t bar, uint32_
   return ok;
 }
 
-// A position in a ring of buffers and the parity of its uses.
-struct Ring {
-  uint32_t at = 0, parity = 0;
-  __device__ __forceinline__ void step(uint32_t size) {
-    if (++at == size) { at = 0; parity ^= 1u; }
+// Every tile starts with stage 0 and accumulator 0, so that the issuing thread's addresses are constants.  `base` has
+// the parities of the stages' next uses, and changes from tile to tile with those that were used an odd number of times.
+template <int kStages>
+struct Parities {
+  uint32_t base = 0u, flip = 0u;
+  __device__ __forceinline__ explicit Parities(int chunks) {
+#pragma unroll
+    for (int s = 0; s < kStages; ++s) flip |= (uint32_t)(((chunks - s + kStages - 1) / kStages) & 1) << s;      // (chunks > 0)
   }
+  __device__ __forceinline__ uint32_t of(int i) const { return ((base >> (i % kStages)) ^ (uint32_t)(i / kStages)) & 1u; }
+  __device__ __forceinline__ void next_tile() { base ^= flip; }
 };
 
 // The columns of a block, by its rank in the cluster: whole blocks of 128, so that no group is cut.
@@ -154,65 +165,52 @@ __device__ __forceinline__ uint64_t swizzled_desc(uint32_t addr) {
   return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
-template <int kRows>
-__device__ void mma_loop(const TcParams &P, const Smem &S, const Span &span, int tiles, uint32_t tmem) {
-  using Sh = Shape<kRows>;
-  const int group = P.A.d.group;
+// One lap over the stages is straight-line code.
+template <class Sh, int kRows, int kGroup>
+__device__ __forceinline__ void mma_loop(const TcParams &P, const Smem &S, const Span &span, int tiles, uint32_t tmem) {
   const uint32_t idesc = P.idesc;
   const uint64_t desc0 = swizzled_desc(S.ring);
-  Ring r;
-  bool ready = false;                              // the stage at hand was seen to be full
-  uint32_t buf = 0u, dpar = 1u;                    // the accumulator and the parity of its being drained
-  // n products of 16 columns from column 16 `from` of the chunk at hand
-  auto products = [&](int from, int n, uint32_t accumulate) {
-    const uint32_t d = tmem + buf * (uint32_t)kRows, at = tmem + (uint32_t)Sh::kATmem + r.at * kACols + 8u * (uint32_t)from;
-    const uint64_t bt = desc0 + (uint64_t)(r.at * (Sh::kStage >> 4) + 2u * (uint32_t)from);
-    mma_tmem(d, at, bt, idesc, accumulate);
-    mma_tmem(d, at + 8u, bt + 2u, idesc, 1u);
-    if (n > 2) {
-      mma_tmem(d, at + 16u, bt + 4u, idesc, 1u);
-      mma_tmem(d, at + 24u, bt + 6u, idesc, 1u);
-    }
-  };
-  auto acquire = [&]() {
-    if (!ready && !wait(S, S.full + 8u * r.at, r.parity)) return false;
+  const int n = span.c1 - span.c0, units = span.u1 - span.u0;
+  Parities<Sh::kStages> par(n);
+  uint32_t dpar = 3u;                              // the accumulators: drained at first
+  auto drained = [&](int buf) {
+    const bool ok = wait(S, S.dempty + 8u * buf, (dpar >> buf) & 1u);
+    dpar ^= 1u << buf;
     tc_fence_after();
-    // (the next stage's barrier is looked at before this one's products are issued)
-    Ring next = r;
-    next.step(Sh::kStages);
-    ready = mbar_try(S.full + 8u * next.at, next.parity);
-    return true;
+    return ok;
   };
-  auto release = [&]() {
-    umma_commit(S.empty + 8u * r.at);
-    r.step(Sh::kStages);
+  // `count` products of 16 columns from column 16 `from` of stage s
+  auto products = [&](int s, int buf, int from, int count, uint32_t accumulate) {
+#pragma unroll
+    for (int i = 0; i < count; ++i)
+      mma_tmem(tmem + (uint32_t)(buf * kRows), tmem + (uint32_t)(Sh::kATmem + s * kACols + 8 * (from + i)),
+               desc0 + (uint64_t)((uint32_t)s * (Sh::kStage >> 4) + 2u * (uint32_t)(from + i)), idesc, i > 0 ? 1u : accumulate);
   };
-  for (int tile = 0; tile < tiles; ++tile) {
-    int c = span.c0;
+  for (int tile = 0; tile < tiles; ++tile, par.next_tile()) {
 #pragma unroll 1
-    for (int u = span.u0; u < span.u1; ++u) {
-      if (!wait(S, S.dempty + 8u * buf, dpar)) return;
-      tc_fence_after();
-      if (group == 32) {                           // half a chunk
-        const int half = u & 1;
-        if (half == 0 && !acquire()) return;
-        products(2 * half, 2, 0u);
-        if (half == 1 || u + 1 == span.u1) release();
-      } else {
-        if (!acquire()) return;
-        products(0, 4, 0u);
-        release();
-        ++c;
-        if (group == 128 && c < span.c1) {
-          if (!acquire()) return;
-          products(0, 4, 1u);
-          release();
-          ++c;
+    for (int c = 0; c < n; c += Sh::kStages) {
+#pragma unroll
+      for (int s = 0; s < Sh::kStages; ++s) {
+        if (c + s < n) {
+          const int buf = kGroup == 128 ? (s / 2) & 1 : s & 1;
+          if (kGroup == 32 ? !drained(0) : (kGroup == 64 || s % 2 == 0) && !drained(buf)) return;
+          if (!wait(S, S.full + 8u * s, par.of(c + s))) return;
+          tc_fence_after();
+          if constexpr (kGroup == 32) {
+            products(s, 0, 0, 2, 0u);
+            umma_commit(S.dfull);
+            if (2 * (c + s) + 1 < units) {
+              if (!drained(1)) return;
+              products(s, 1, 2, 2, 0u);
+              umma_commit(S.dfull + 8u);
+            }
+          } else {
+            products(s, buf, 0, 4, kGroup == 128 && s % 2 == 1 ? 1u : 0u);
+            if (kGroup == 64 || s % 2 == 1 || c + s + 1 == n) umma_commit(S.dfull + 8u * buf);
+          }
+          umma_commit(S.empty + 8u * s);
         }
       }
-      umma_commit(S.dfull + 8u * buf);
-      buf ^= 1u;
-      if (buf == 0u) dpar ^= 1u;
     }
   }
 }
@@ -226,137 +224,190 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t r[16]) 
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 
-// Set `which` takes every kExpand-th chunk.  A thread expands one weight row: eight words of a chunk, which come
-// in two chunks ahead.
-struct Ahead {
-  uint2 w[4];
-  uint32_t z[2];
-};
-
-template <class T, int kRows>
-__device__ void expand_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total, int which, int quarter,
-                            int lane, uint32_t tmem) {
-  using Sh = Shape<kRows>;
+// Set `which` takes every kExpand-th chunk of a tile.  A thread expands one weight row: the eight words of a chunk.
+template <class Sh, class T>
+__device__ __forceinline__ void expand_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total, int which,
+                                            int quarter, int lane, uint32_t tmem) {
   constexpr int kSets = Sh::kExpand;
-  const int N = P.A.d.N, group = P.A.d.group, r = 32 * quarter + lane, per_tile = span.c1 - span.c0;
+  const int N = P.A.d.N, group = P.A.d.group, r = 32 * quarter + lane, n = span.c1 - span.c0;
   const int last_group = (P.A.d.K - 1) / group;
   const uint32_t t_lane = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)Sh::kATmem;
-  uint32_t seq = 0;                                 // chunks of all tiles in sequence: their buffers
-  for (int tile = first; tile < total; tile += step, seq += (uint32_t)per_tile) {
-    const int nc = min((tile % P.row_tiles) * kTileN + r, N - 1);
-    const uint2 *w = reinterpret_cast<const uint2 *>(P.A.w) +
-                     ((size_t)(nc / kW4Rows) * P.col_tiles * 32) * 2 + ((nc >> 3) & 1);
-    auto fetch = [&](int i, Ahead &f) {
-      if (i >= per_tile) return;
-      const int c = span.c0 + i;
+  uint32_t from[4];                                 // this row's words of columns 8 t .. and 32 + 8 t ..
 #pragma unroll
-      for (int t = 0; t < 4; ++t) f.w[t] = load_global(w + ((size_t)c * 32 + w4_place(nc, 8 * t)) * 2);
+  for (int t = 0; t < 4; ++t) from[t] = S.weights + (uint32_t)((r / kW4Rows) * 512 + w4_place(r, 8 * t) * 16 + 4 * w4_word(r, 0));
+  Parities<Sh::kStages> par(n);
+  uint32_t seq = 0;                                 // chunks of all tiles in sequence: their places in the ring of weights
+  for (int tile = first; tile < total; tile += step, seq += (uint32_t)n, par.next_tile()) {
+    const int nc = min((tile % P.row_tiles) * kTileN + r, N - 1);
+    struct Zeros { uint32_t z[2]; };
+    auto fetch = [&](int i, Zeros &f) {
       f.z[0] = f.z[1] = 8u;
-      if (P.A.zeros) {
+      if (P.A.zeros && i < n) {
+        const int c = span.c0 + i;
         f.z[0] = load_global(P.A.zeros + (size_t)min(c * kChunk / group, last_group) * N + nc);
         f.z[1] = group == 32 ? load_global(P.A.zeros + (size_t)min(2 * c + 1, last_group) * N + nc) : f.z[0];
       }
     };
-    auto expand = [&](int i, const Ahead &f) {
-      const uint32_t at = (seq + (uint32_t)i) % Sh::kStages, use = (seq + (uint32_t)i) / Sh::kStages;
-      if (!wait_warp(S, S.empty + 8u * at, (use & 1u) ^ 1u)) return false;
+    auto expand = [&](int i, const Zeros &f) {
+      const uint32_t slot = (seq + (uint32_t)i) % kWeightStages, use = (seq + (uint32_t)i) / kWeightStages, s = (uint32_t)i % Sh::kStages;
+      if (!wait_warp(S, S.wfull + 8u * slot, use & 1u)) return false;
+      uint32_t w[8];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) lds64(from[t] + slot * kWeightStage, w[t], w[4 + t]);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(S.wempty + 8u * slot);
+      if (!wait_warp(S, S.empty + 8u * s, par.of(i) ^ 1u)) return false;
       tc_fence_after();
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const uint32_t zero = w4_zero(f.z[half], T());
+        const typename W4Type<T>::Zero zero = W4Type<T>::zero(f.z[half]);
         uint32_t v[16];
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 4; ++t) {
+          uint32_t e[4];
+          W4Type<T>::expand(w[4 * half + t], zero, P.magic, e);
 #pragma unroll
-          for (int p = 0; p < 4; ++p) v[4 * t + p] = w4_pair(half == 0 ? f.w[t].x : f.w[t].y, p, T(), zero);
-        tmem_st16(t_lane + at * kACols + 16u * half, v);
+          for (int p = 0; p < 4; ++p) v[4 * t + p] = e[p];
+        }
+        tmem_st16(t_lane + s * kACols + 16u * half, v);
       }
       asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(S.full + 8u * at);
+      if (lane == 0) mbar_arrive(S.full + 8u * s);
       return true;
     };
-    const int skip = (int)(((uint32_t)(which + kSets) - seq % kSets) % kSets);     // this set's first chunk of the tile
-    Ahead f0, f1;                                   // (two by name: moving one to the other would wait for its loads)
-    fetch(skip, f0);
-    fetch(skip + kSets, f1);
+    Zeros f0, f1;                                   // (two by name: moving one to the other would wait for its loads)
+    fetch(which, f0);
+    fetch(which + kSets, f1);
 #pragma unroll 1
-    for (int i = skip; i < per_tile; i += 2 * kSets) {
+    for (int i = which; i < n; i += 2 * kSets) {
       if (!expand(i, f0)) return;
       fetch(i + 2 * kSets, f0);
-      if (i + kSets >= per_tile) break;
+      if (i + kSets >= n) break;
       if (!expand(i + kSets, f1)) return;
       fetch(i + 3 * kSets, f1);
     }
   }
 }
 
-// ------------------------------------------------------------------ the rows of x
-// One thread copies a stage with one tensor copy, which also fills what does not exist with zeros.
-template <int kRows>
-__device__ void copy_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total) {
-  constexpr uint32_t kStages = Shape<kRows>::kStages;
-  Ring r;
+// One thread copies the packed weights, a chunk of 128 rows at a time.
+__device__ __forceinline__ void weight_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total) {
+  uint32_t seq = 0;
   for (int tile = first; tile < total; tile += step) {
-    const int tok0 = (tile / P.row_tiles) * kRows;
+    const uint32_t *w = P.A.w + (size_t)(tile % P.row_tiles) * P.col_tiles * (kWeightStage / 4);
 #pragma unroll 1
-    for (int c = span.c0; c < span.c1; ++c) {
-      if (!wait(S, S.empty + 8u * r.at, r.parity ^ 1u)) {
+    for (int c = span.c0; c < span.c1; ++c, ++seq) {
+      const uint32_t slot = seq % kWeightStages, use = seq / kWeightStages;
+      if (!wait(S, S.wempty + 8u * slot, (use & 1u) ^ 1u)) {
         // gave up: the copies in flight must land before the block's shared memory is released
-        for (uint32_t s = 0; s < kStages; ++s)
-          for (int i = 0; i < (1 << 12) && !mbar_try(S.full + 8u * s, s < r.at ? r.parity : r.parity ^ 1u); ++i) {}
+        for (uint32_t u = seq > kWeightStages ? seq - kWeightStages : 0u; u < seq; ++u)
+          for (int i = 0; i < (1 << 12) && !mbar_try(S.wfull + 8u * (u % kWeightStages), (u / kWeightStages) & 1u); ++i) {}
         return;
       }
-      const uint32_t bar = S.full + 8u * r.at;
-      mbar_arrive_expect_tx(bar, Shape<kRows>::kStage);
-      asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                   ::"r"(S.ring + r.at * Shape<kRows>::kStage), "l"(&P.x_map), "r"(c * kChunk), "r"(tok0), "r"(bar) : "memory");
-      r.step(kStages);
+      mbar_arrive_expect_tx(S.wfull + 8u * slot, kWeightStage);
+      bulk_copy_g2s(S.weights + slot * kWeightStage, w + (size_t)c * (kWeightStage / 4), kWeightStage, S.wfull + 8u * slot);
     }
   }
 }
 
-// Three warps share every stage: rows in 8 bits become 16-bit numbers, others are at addresses that tensor copies
-// do not take.
-template <int kType, int kRows>
-__device__ void load_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total, int w, int lane) {
-  using Sh = Shape<kRows>;
-  const int K = P.A.d.K, piece = lane & 7;
-  Ring fill;
-  for (int tile = first; tile < total; tile += step) {
+// ------------------------------------------------------------------ the rows of x
+// One thread copies a stage with one tensor copy, which also fills what does not exist with zeros.
+template <class Sh, int kRows>
+__device__ __forceinline__ void copy_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total) {
+  const int n = span.c1 - span.c0;
+  Parities<Sh::kStages> par(n);
+  for (int tile = first; tile < total; tile += step, par.next_tile()) {
+    const int tok0 = (tile / P.row_tiles) * kRows;
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+      const uint32_t s = (uint32_t)i % Sh::kStages;
+      if (!wait(S, S.empty + 8u * s, par.of(i) ^ 1u)) {
+        // gave up: what is in flight lands within microseconds; the block's shared memory is not released before
+        const long long t0 = clock64();
+        while (clock64() - t0 < (1 << 20)) {}
+        return;
+      }
+      const uint32_t bar = S.full + 8u * s;
+      mbar_arrive_expect_tx(bar, Sh::kStage);
+      asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                   ::"r"(S.ring + s * Sh::kStage), "l"(&P.x_map), "r"((span.c0 + i) * kChunk), "r"(tok0), "r"(bar) : "memory");
+    }
+  }
+}
+
+// Through registers: rows in 8 bits become 16-bit numbers, others are at addresses that tensor copies do not take.
+// The warps share every stage; a thread has eight columns of every (4 kLoadWarps)-th row, and where it can it loads them
+// a chunk ahead.
+template <class Sh, int kType, int kRows>
+__device__ __forceinline__ void load_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total, int w, int lane) {
+  constexpr int kB = RowsOf<kType>::kBytes, kStep = 4 * Sh::kLoadWarps, kPass = (kRows + kStep - 1) / kStep, kBatch = kPass < 6 ? kPass : 6;
+  const int K = P.A.d.K, n = span.c1 - span.c0, piece = lane & 7, row0 = 4 * w + (lane >> 3);
+  const long long row_bytes = P.A.r.x_stride * kB;
+  Parities<Sh::kStages> par(n);
+  for (int tile = first; tile < total; tile += step, par.next_tile()) {
     const long long tok0 = (long long)(tile / P.row_tiles) * kRows;
     const int rows = (int)min((long long)kRows, P.A.r.rows - tok0);
-    const long long row_bytes = P.A.r.x_stride * RowsOf<kType>::kBytes;
-    const uint8_t *x = static_cast<const uint8_t *>(P.A.x) + tok0 * row_bytes;
-#pragma unroll 1
-    for (int c = span.c0; c < span.c1; ++c) {
-      if (!wait_warp(S, S.empty + 8u * fill.at, fill.parity ^ 1u)) return;
-      const int k = c * kChunk + 8 * piece;
-      const uint32_t dst = S.ring + fill.at * Sh::kStage;
-#pragma unroll 1
-      for (int row = 4 * w + (lane >> 3); row < kRows; row += 4 * kLoadWarps * 4) {
-        uint32_t v[4][4];
+    const uint8_t *x = static_cast<const uint8_t *>(P.A.x) + (tok0 + row0) * row_bytes;
+    struct Batch { uint32_t v[kBatch][2 * kB]; };
+    auto load = [&](int i, int p0, Batch &b) {
+      if (i >= n) return;
+      const int k = (span.c0 + i) * kChunk + 8 * piece;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int rr = row + 4 * kLoadWarps * i;
-          if (rr < rows) {
-            load_x8<kType>(x + (long long)rr * row_bytes, k, K, P.pieces, v[i]);
-          } else {
+      for (int p = 0; p < kBatch; ++p) {
+        const int row = row0 + kStep * (p0 + p);
+        if (row < rows) {
+          load_x8_raw<kType>(x + (long long)(kStep * (p0 + p)) * row_bytes, k, K, P.pieces, b.v[p]);
+        } else {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[i][q] = 0u;
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int rr = row + 4 * kLoadWarps * i;
-          if (rr < kRows) sts128(dst + (uint32_t)rr * 128u + (uint32_t)((piece ^ (rr & 7)) * 16), v[i][0], v[i][1], v[i][2], v[i][3]);
+          for (int q = 0; q < 2 * kB; ++q) b.v[p][q] = 0u;
         }
       }
+    };
+    auto store = [&](int i, int p0, const Batch &b) {
+      const uint32_t dst = S.ring + ((uint32_t)i % Sh::kStages) * Sh::kStage;
+#pragma unroll
+      for (int p = 0; p < kBatch; ++p) {
+        const int row = row0 + kStep * (p0 + p);
+        uint32_t v[4];
+        x8_pairs<kType>(b.v[p], v);
+        if (row < kRows) sts128(dst + (uint32_t)row * 128u + (uint32_t)((piece ^ (row & 7)) * 16), v[0], v[1], v[2], v[3]);
+      }
+    };
+    auto start = [&](int i) { return wait_warp(S, S.empty + 8u * (i % Sh::kStages), par.of(i) ^ 1u); };
+    auto finish = [&](int i) {
       fence_proxy_async();
       __syncwarp();
-      if (lane == 0) mbar_arrive(S.full + 8u * fill.at);
-      fill.step(Sh::kStages);
+      if (lane == 0) mbar_arrive(S.full + 8u * (i % Sh::kStages));
+    };
+    if constexpr (kPass <= kBatch) {
+      Batch b0, b1;
+      load(0, 0, b0);
+      load(1, 0, b1);
+#pragma unroll 1
+      for (int i = 0; i < n; i += 2) {
+        if (!start(i)) return;
+        store(i, 0, b0);
+        finish(i);
+        load(i + 2, 0, b0);
+        if (i + 1 >= n) break;
+        if (!start(i + 1)) return;
+        store(i + 1, 0, b1);
+        finish(i + 1);
+        load(i + 3, 0, b1);
+      }
+    } else {
+      Batch b;
+#pragma unroll 1
+      for (int i = 0; i < n; ++i) {
+        if (!start(i)) return;
+#pragma unroll 1
+        for (int p0 = 0; p0 < kPass; p0 += kBatch) {
+          load(i, p0, b);
+          store(i, p0, b);
+        }
+        finish(i);
+      }
     }
   }
 }
@@ -375,10 +426,9 @@ __device__ __forceinline__ float4 lds_f4(uint32_t addr) {
   return make_float4(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3]));
 }
 
-template <int kRows>
-__device__ void promote_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total, int set, int quarter,
+template <class Sh, int kRows>
+__device__ __forceinline__ void promote_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total, int set, int quarter,
                              int lane, uint32_t tmem) {
-  using Sh = Shape<kRows>;
   constexpr int kUnit = Sh::kUnit;
   const W4Args &A = P.A;
   const int N = A.d.N;
@@ -386,7 +436,7 @@ __device__ void promote_role(const TcParams &P, const Smem &S, const Span &span,
   const int G = (A.d.K + A.d.group - 1) / A.d.group;
   const uint32_t t_lane = tmem + ((uint32_t)(32 * quarter) << 16);
   const uint32_t my_scales = S.scales + (uint32_t)(4 * set + quarter) * 512u;
-  uint32_t buf = 0u, parity = 0u;
+  uint32_t dpar = 0u;                               // the accumulators' parities
   for (int tile = first; tile < total; tile += step) {
     const int n = (tile % P.row_tiles) * kTileN + 32 * quarter + lane, nc = min(n, N - 1);
     const long long tok0 = (long long)(tile / P.row_tiles) * kRows + set * kUnit;
@@ -408,10 +458,12 @@ __device__ void promote_role(const TcParams &P, const Smem &S, const Span &span,
         }
         __syncwarp();
       }
-      if (!__all_sync(0xFFFFFFFFu, wait_inline(S, S.dfull + 8u * buf, parity))) return;
+      const uint32_t buf = (uint32_t)(u - span.u0) & 1u;
+      if (!__all_sync(0xFFFFFFFFu, wait_inline(S, S.dfull + 8u * buf, (dpar >> buf) & 1u))) return;
+      dpar ^= 1u << buf;
       tc_fence_after();
       // 32 values at a time: a load of tensor memory takes as long for 16
-      constexpr int kLoad = kRows > 64 ? 16 : 32;
+      constexpr int kLoad = kRows > 64 || kRows < 32 ? 16 : 32;
 #pragma unroll
       for (int j = 0; j < kUnit / kLoad; ++j) {
         int32_t v[kLoad];
@@ -439,8 +491,6 @@ __device__ void promote_role(const TcParams &P, const Smem &S, const Span &span,
           for (int i = 0; i < kLoad; ++i) acc[kLoad * j + i] = fmaf(__int_as_float(v[i]), s, acc[kLoad * j + i]);
         }
       }
-      buf ^= 1u;
-      if (buf == 0u) parity ^= 1u;
     }
     if (P.split > 1) {                     // [row of x][output], for the cluster
 #pragma unroll
@@ -460,16 +510,17 @@ __device__ __forceinline__ void cluster_barrier() {
 }
 
 template <int kType, int kRows>
-__global__ void __launch_bounds__(Shape<kRows>::kThreads, 1)
+__global__ void __launch_bounds__(Shape<kRows, RowsOf<kType>::kBytes>::kThreads, 1)
 w4_tc_kernel(const __grid_constant__ TcParams P) {
-  using Sh = Shape<kRows>;
+  using Sh = Shape<kRows, RowsOf<kType>::kBytes>;
   using T = typename RowsOf<kType>::T;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Smem S = carve(smem, Sh::kScaleBytes);
   if (threadIdx.x == 0) {
     // a stage is full with four expanding warps' arrivals and those that bring the rows
-    for (int i = 0; i < Sh::kStages; ++i) { mbar_init(S.full + 8u * i, 4 + (P.copies ? 1 : kLoadWarps)); mbar_init(S.empty + 8u * i, 1); }
+    for (int i = 0; i < Sh::kStages; ++i) { mbar_init(S.full + 8u * i, 4 + (P.copies ? 1 : Sh::kLoadWarps)); mbar_init(S.empty + 8u * i, 1); }
+    for (int i = 0; i < kWeightStages; ++i) { mbar_init(S.wfull + 8u * i, 1); mbar_init(S.wempty + 8u * i, 4); }
     for (int i = 0; i < 2; ++i) { mbar_init(S.dfull + 8u * i, 1); mbar_init(S.dempty + 8u * i, 4 * Sh::kPromo); }
     *S.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -491,17 +542,23 @@ w4_tc_kernel(const __grid_constant__ TcParams P) {
   const Span span(P, rank);
   if (warp < 4 * Sh::kPromo) {
     if constexpr (Sh::kPromoRegs != Sh::kRegs) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Sh::kPromoRegs));
-    promote_role<kRows>(P, S, span, first, step, total, warp >> 2, warp & 3, lane, tmem);
+    promote_role<Sh, kRows>(P, S, span, first, step, total, warp >> 2, warp & 3, lane, tmem);
   } else {
     if constexpr (Sh::kOtherRegs != Sh::kRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::kOtherRegs));
     if (warp < Sh::kMmaWarp) {
-      expand_role<T, kRows>(P, S, span, first, step, total, (warp >> 2) - Sh::kPromo, warp & 3, lane, tmem);
+      expand_role<Sh, T>(P, S, span, first, step, total, (warp >> 2) - Sh::kPromo, warp & 3, lane, tmem);
     } else if (warp == Sh::kMmaWarp) {
-      if (elect_one()) mma_loop<kRows>(P, S, span, mine, tmem);
+      if (elect_one()) {
+        if (P.A.d.group == 128) mma_loop<Sh, kRows, 128>(P, S, span, mine, tmem);
+        else if (P.A.d.group == 64) mma_loop<Sh, kRows, 64>(P, S, span, mine, tmem);
+        else mma_loop<Sh, kRows, 32>(P, S, span, mine, tmem);
+      }
+    } else if (warp == Sh::kWeightWarp) {
+      if (elect_one()) weight_role(P, S, span, first, step, total);
     } else if (!P.copies) {
-      load_role<kType, kRows>(P, S, span, first, step, total, warp - Sh::kLoadWarp, lane);
+      load_role<Sh, kType, kRows>(P, S, span, first, step, total, warp - Sh::kLoadWarp, lane);
     } else if (warp == Sh::kLoadWarp) {
-      if (elect_one()) copy_role<kRows>(P, S, span, first, step, total);
+      if (elect_one()) copy_role<Sh, kRows>(P, S, span, first, step, total);
     }
     __syncwarp();
   }
@@ -570,7 +627,7 @@ bool map_rows(const W4Args &a, int rows, CUtensorMap *map) {
 
 template <int kType, int kRows>
 cudaError_t run(const W4Args &a, cudaStream_t st) {
-  using Sh = Shape<kRows>;
+  using Sh = Shape<kRows, RowsOf<kType>::kBytes>;
   static bool attr_flags[64] = {};
   bool &attr_set = attr_done_for_current_device(attr_flags);
   if (!attr_set) {
@@ -581,6 +638,7 @@ cudaError_t run(const W4Args &a, cudaStream_t st) {
   TcParams P;
   P.copies = map_rows<kType>(a, kRows, &P.x_map);
   P.A = a;
+  P.magic = W4Type<typename RowsOf<kType>::T>::kMagic;
   P.col_tiles = w4_col_tiles(a.d);
   P.row_tiles = (a.d.N + kTileN - 1) / kTileN;
   P.token_tiles = (a.r.rows + kRows - 1) / kRows;
@@ -598,8 +656,11 @@ cudaError_t run(const W4Args &a, cudaStream_t st) {
 
 template <int kType>
 cudaError_t run_type(const W4Args &a, cudaStream_t st) {
-  const long long tiles = (a.d.N + kTileN - 1) / kTileN * ((a.r.rows + 191ll) / 192);
-  if (a.r.rows > 128 && 2 * tiles > sm_count_of_current_device()) return run<kType, 192>(a, st);
+  if constexpr (RowsOf<kType>::kBytes == 2) {
+    const long long tiles = (a.d.N + kTileN - 1) / kTileN * ((a.r.rows + 191ll) / 192);
+    if (a.r.rows > 128 && 2 * tiles > sm_count_of_current_device()) return run<kType, 192>(a, st);
+  }
+  if (a.r.rows <= 16) return run<kType, 16>(a, st);
   if (a.r.rows <= 32) return run<kType, 32>(a, st);
   if (a.r.rows <= 64) return run<kType, 64>(a, st);
   return run<kType, 128>(a, st);

@@ -86,32 +86,34 @@ def norm_error(D):
 def unpack_codes(packed, N, K):
     """Codes [N][K] of the packed tiles, by the documented layout alone."""
     p = packed.cpu().numpy().view(np.uint32)
-    rt, ct = p.shape[:2]
-    out = np.zeros((rt * 16, ct * 64), np.uint8)
-    for lane in range(32):
-        g = lane // 4
-        t = (lane % 4) ^ (g // 2 % 4)
+    panels, ct = p.shape[:2]
+    p = p.reshape(panels, ct, 8, 32, 4).transpose(0, 2, 1, 3, 4).reshape(panels * 8, ct, 32, 4)
+    out = np.zeros((panels * 128, ct * 64), np.uint8)
+    for place in range(32):
+        g = place // 4
+        t = (place % 4) ^ (g // 2 % 4)
         for word in range(4):
             row, col = g + 8 * (word // 2), 32 * (word % 2) + 8 * t
             for i in range(8):
-                out[row::16, col + i::64] = (p[:, :, lane, word] >> np.uint32(4 * (i // 2) + 16 * (i % 2))) & 15
+                out[row::16, col + i::64] = (p[:, :, place, word] >> np.uint32(4 * (i // 2) + 16 * (i % 2))) & 15
     return out[:N, :K]
 
 
 def pack_codes(codes):
     """The packed tiles of codes [N][K] (numpy), by the documented layout alone; 8 beyond the matrix."""
     N, K = codes.shape
-    rt, ct = -(-N // 16), -(-K // 64)
-    full = np.full((rt * 16, ct * 64), 8, np.uint32)
+    panels, ct = -(-N // 128), -(-K // 64)
+    full = np.full((panels * 128, ct * 64), 8, np.uint32)
     full[:N, :K] = codes
-    p = np.zeros((rt, ct, 32, 4), np.uint32)
-    for lane in range(32):
-        g = lane // 4
-        t = (lane % 4) ^ (g // 2 % 4)
+    p = np.zeros((panels * 8, ct, 32, 4), np.uint32)
+    for place in range(32):
+        g = place // 4
+        t = (place % 4) ^ (g // 2 % 4)
         for word in range(4):
             row, col = g + 8 * (word // 2), 32 * (word % 2) + 8 * t
             for i in range(8):
-                p[:, :, lane, word] |= full[row::16, col + i::64] << np.uint32(4 * (i // 2) + 16 * (i % 2))
+                p[:, :, place, word] |= full[row::16, col + i::64] << np.uint32(4 * (i // 2) + 16 * (i % 2))
+    p = np.ascontiguousarray(p.reshape(panels, 8, ct, 32, 4).transpose(0, 2, 1, 3, 4)).reshape(panels, ct, 256, 4)
     return torch.from_numpy(p.view(np.int32))
 
 

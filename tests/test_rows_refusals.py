@@ -57,8 +57,8 @@ def test_w4_arguments():
         assert lib.xnor_w4_dequantize(P, P, P, bad, 1, P, NULL) == INV
         assert lib.xnor_w4_packed_words(bad) == 0
         assert lib.xnor_w4_matmul(P, NULL, P, P, P, bad, ctypes.byref(B.xnor_w4_rows(1, 1, 0, 1, 100, 40)), P, NULL) == INV
-    assert lib.xnor_w4_packed_words(d()) == 3 * 2 * 128
-    for big in (d(N=1048561), d(K=(1 << 24) + 1)):
+    assert lib.xnor_w4_packed_words(d()) == 1 * 2 * 1024
+    for big in (d(N=1048449), d(K=(1 << 24) + 1)):
         assert lib.xnor_w4_quantize(P, 1, big, P, P, NULL, NULL) == UNS and lib.xnor_w4_pack(P, big, P, NULL) == UNS
         assert lib.xnor_w4_dequantize(P, P, NULL, big, 1, P, NULL) == UNS and lib.xnor_w4_packed_words(big) == 0
     assert lib.xnor_w4_quantize(P, B.XNOR_I8, d(), P, P, NULL, NULL) == INV
@@ -106,11 +106,11 @@ no(lambda: R(f(64), f(255)))                              # work too small
 no(lambda: R(f(63), f(256)))
 no(lambda: R(None, None, h=f(4, 64, t=bf)))
 d = X.make_w4_desc(40, 100, 64)
-pk, sc, z = f(3, 2, 32, 4, t=torch.int32), f(2, 40), f(2, 40, t=u8)
+pk, sc, z = f(1, 2, 256, 4, t=torch.int32), f(2, 40), f(2, 40, t=u8)
 M = lambda x=None, xs=None, p=pk, s=sc, zz=z, d=d, o=None: X.xnor_w4_matmul(f(5, 100, t=bf) if x is None else x, xs, p, s, zz, d, f(5, 40, t=bf) if o is None else o, stream=0)
 no(lambda: M(x=f(5, 99, t=bf)))
-no(lambda: M(p=f(3, 2, 32, 3, t=torch.int32)))
-no(lambda: M(p=f(3, 2, 32, 4)))
+no(lambda: M(p=f(1, 2, 256, 3, t=torch.int32)))
+no(lambda: M(p=f(1, 2, 256, 4)))
 no(lambda: M(s=f(40, 2)))
 no(lambda: M(zz=f(2, 40)))
 no(lambda: M(o=f(5, 41, t=bf)))
@@ -152,7 +152,7 @@ def test_what_the_binding_passes_on():
     from test_binding import PRELUDE
     run_child("""
 d = X.make_w4_desc(40, 100, 64)
-pk, sc, z = Like(0x100, torch.int32, (3, 2, 32, 4), (256, 128, 4, 1)), Like(0x200, torch.float32, (2, 40), (40, 1)), Like(0x300, torch.uint8, (2, 40), (40, 1))
+pk, sc, z = Like(0x100, torch.int32, (1, 2, 256, 4), (2048, 1024, 4, 1)), Like(0x200, torch.float32, (2, 40), (40, 1)), Like(0x300, torch.uint8, (2, 40), (40, 1))
 call = lambda x, xs, o, zz=z: X.xnor_w4_matmul(x, xs, pk, sc, zz, d, o, stream=0x77)
 call(Like(0x400, torch.bfloat16, (5, 100), (112, 1)), None, Like(0x500, torch.float32, (5, 40), (48, 1)))
 assert seen[-1] == (0x400, None, 0x300, (40, 100, 64), (5, 1, 0, 0, 112, 48), 0x500, 0x77), seen
