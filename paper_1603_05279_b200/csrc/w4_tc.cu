@@ -413,11 +413,30 @@ __device__ __forceinline__ void load_role(const TcParams &P, const Smem &S, cons
 }
 
 // ------------------------------------------------------------------ promotion: sums of groups -> sums of a row
-__device__ __forceinline__ void store_out(const W4Args &A, long long row, int n, float v) {
-  const size_t at = (size_t)(row * A.r.out_stride) + n;
-  if (A.r.out_type == XNOR_F32) static_cast<float *>(A.out)[at] = v;
-  else if (A.r.out_type == XNOR_BF16) static_cast<__nv_bfloat16 *>(A.out)[at] = __float2bfloat16_rn(v);
-  else static_cast<__half *>(A.out)[at] = __float2half_rn(v);
+__device__ __forceinline__ void convert(float v, float *p) { *p = v; }
+__device__ __forceinline__ void convert(float v, __nv_bfloat16 *p) { *p = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void convert(float v, __half *p) { *p = __float2half_rn(v); }
+
+// The sums of one output and kUnit rows of x, `left` of which exist: a warp stores 32 neighbouring outputs of a row.
+template <int kUnit, class Out>
+__device__ __forceinline__ void store_column(const float (&acc)[kUnit], Out *p, long long stride, int left) {
+  if (left >= kUnit) {
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i, p += stride) convert(acc[i], p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i, p += stride)
+      if (i < left) convert(acc[i], p);
+  }
+}
+
+// Four neighbouring outputs, `left` of which exist.
+template <class Out>
+__device__ __forceinline__ void store_four(const float4 &v, Out *p, int left) {
+  convert(v.x, p);
+  if (left > 1) convert(v.y, p + 1);
+  if (left > 2) convert(v.z, p + 2);
+  if (left > 3) convert(v.w, p + 3);
 }
 
 __device__ __forceinline__ float4 lds_f4(uint32_t addr) {
@@ -496,11 +515,29 @@ __device__ __forceinline__ void promote_role(const TcParams &P, const Smem &S, c
 #pragma unroll
       for (int i = 0; i < kUnit; ++i)
         sts32(S.ring + (uint32_t)(((set * kUnit + i) * kTileN + 32 * quarter + lane) * 4), __float_as_uint(acc[i]));
-    } else if (n < N) {
-      const float *xs = A.x_scales != nullptr && !x_groups ? A.x_scales : nullptr;
+    } else {
+      if (A.x_scales != nullptr && !x_groups) {                   // a scale for each row
+        __syncwarp();
 #pragma unroll
-      for (int i = 0; i < kUnit; ++i)
-        if (tok0 + i < A.r.rows) store_out(A, tok0 + i, n, xs ? acc[i] * load_global(xs + tok0 + i) : acc[i]);
+        for (int i = 0; i < (kUnit + 31) / 32; ++i) {
+          const int col = lane + 32 * i;
+          const float v = col < kUnit && tok0 + col < A.r.rows ? load_global(A.x_scales + tok0 + col) : 0.0f;
+          if (col < kUnit) sts32(my_scales + 4u * col, __float_as_uint(v));
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kUnit / 4; ++i) {
+          const float4 f = lds_f4(my_scales + 16u * i);
+          acc[4 * i] *= f.x; acc[4 * i + 1] *= f.y; acc[4 * i + 2] *= f.z; acc[4 * i + 3] *= f.w;
+        }
+      }
+      if (n < N) {
+        const long long at = tok0 * A.r.out_stride + n;
+        const int left = (int)min((long long)kUnit, A.r.rows - tok0);
+        if (A.r.out_type == XNOR_F32) store_column(acc, static_cast<float *>(A.out) + at, A.r.out_stride, left);
+        else if (A.r.out_type == XNOR_BF16) store_column(acc, static_cast<__nv_bfloat16 *>(A.out) + at, A.r.out_stride, left);
+        else store_column(acc, static_cast<__half *>(A.out) + at, A.r.out_stride, left);
+      }
     }
   }
 }
@@ -573,20 +610,31 @@ w4_tc_kernel(const __grid_constant__ TcParams P) {
   const long long tok0 = (long long)(first / P.row_tiles) * kRows;
   const bool row_scale = P.A.x_scales != nullptr && P.A.r.x_group == 0;
   const int r0 = kRows * rank / P.split, r1 = kRows * (rank + 1) / P.split;
-  for (int e = r0 * kTileN + threadIdx.x; e < r1 * kTileN; e += Sh::kThreads) {
-    const int n = e % kTileN;
-    const long long row = tok0 + e / kTileN;
-    if (row >= P.A.r.rows || n0 + n >= P.A.d.N) continue;
-    float s = 0.0f;
-    for (int i = 0; i < P.split; ++i) {
+  for (int e = r0 * (kTileN / 4) + threadIdx.x; e < r1 * (kTileN / 4); e += Sh::kThreads) {       // four outputs each
+    const int n = n0 + 4 * (e % (kTileN / 4));
+    const long long row = tok0 + e / (kTileN / 4);
+    if (row >= P.A.r.rows || n >= P.A.d.N) continue;
+    float4 v[kMaxSplitTc];
+#pragma unroll
+    for (int i = 0; i < kMaxSplitTc; ++i) {
+      if (i >= P.split) continue;
       uint32_t a;
-      float v;
-      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(S.ring + 4u * (uint32_t)e), "r"(i));
-      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
-      s += v;
+      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(S.ring + 16u * (uint32_t)e), "r"(i));
+      asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[i].x), "=f"(v[i].y), "=f"(v[i].z), "=f"(v[i].w) : "r"(a) : "memory");
     }
-    if (row_scale) s *= load_global(P.A.x_scales + row);
-    store_out(P.A, row, n0 + n, s);
+    float4 s = v[0];
+#pragma unroll
+    for (int i = 1; i < kMaxSplitTc; ++i)
+      if (i < P.split) { s.x += v[i].x; s.y += v[i].y; s.z += v[i].z; s.w += v[i].w; }
+    if (row_scale) {
+      const float f = load_global(P.A.x_scales + row);
+      s.x *= f; s.y *= f; s.z *= f; s.w *= f;
+    }
+    const long long at = row * P.A.r.out_stride + n;
+    const int left = P.A.d.N - n;
+    if (P.A.r.out_type == XNOR_F32) store_four(s, static_cast<float *>(P.A.out) + at, left);
+    else if (P.A.r.out_type == XNOR_BF16) store_four(s, static_cast<__nv_bfloat16 *>(P.A.out) + at, left);
+    else store_four(s, static_cast<__half *>(P.A.out) + at, left);
   }
   cluster_barrier();
 }
