@@ -36,28 +36,30 @@ using namespace umma;
 constexpr int kTileN = 128;                  // outputs (weight rows) of a tile: the lanes of tensor memory
 constexpr int kChunk = 64;                   // columns of a stage
 constexpr int kACols = kChunk / 2;           // tensor-memory columns of a chunk of expanded weights
-constexpr int kMaxStages = 8, kWeightStages = 16;
-constexpr uint32_t kWeightStage = 4096;      // a chunk of packed weights: 8 tiles of 16 x 64
+constexpr int kMaxStages = 8, kWeightStages = 8;
+constexpr uint32_t kWeightChunk = 4096;      // a chunk of packed weights: 8 tiles of 16 x 64
+constexpr uint32_t kWeightStage = 2 * kWeightChunk;            // chunks of two expanding sets
 constexpr uint32_t kCtrlBytes = 1024;
 constexpr int kMaxSplitTc = 8;
+constexpr int kAhead = 8;                    // groups whose scales are under way
 
 template <int kRows, int kBytes>
 struct Shape {
   static constexpr int kPromo = kRows > 64 ? 2 : 1;            // sets of four warps
   static constexpr int kUnit = kRows / kPromo;                 // rows of x of a set
-  static constexpr int kExpand = 2;
+  static constexpr int kExpand = kRows > 64 ? 2 : 4;           // sets of four warps
   static constexpr int kOther = kBytes == 1 ? 8 : 4, kLoadWarps = kOther - 2;
   static constexpr int kMmaWarp = 4 * (kPromo + kExpand), kWeightWarp = kMmaWarp + 1, kLoadWarp = kMmaWarp + 2;
   static constexpr int kThreads = 32 * (kMmaWarp + kOther);
   static constexpr int kATmem = kRows > 128 ? 2 * kRows : 256; // behind the two accumulators
   static constexpr int kStages = (512 - kATmem) / kACols;      // chunks: weights in tensor memory, rows of x in shared
   static constexpr uint32_t kStage = kRows * kChunk * 2;       // a row of x: 128 bytes, swizzled
-  static constexpr uint32_t kScaleBytes = 8 * 512;             // a group's scales of x, per promotion warp
+  static constexpr uint32_t kScaleBytes = 8 * (512 + kAhead * 128);          // per promotion warp: a group's scales of x, its outputs' of groups ahead
   static constexpr size_t kSmem = 1024 + kCtrlBytes + kScaleBytes + kWeightStages * kWeightStage + (size_t)kStages * kStage;   // (1024: to align the ring)
   // Registers per thread as launched, and after they are dealt out anew: the promotion's hold its sums.
-  static constexpr int kRegs = kThreads == 512 ? 128 : kThreads == 640 ? 96 : 80;
-  static constexpr int kPromoRegs = kRows > 128 ? 144 : kRows > 64 ? (kBytes == 1 ? 112 : 128) : kRows > 32 ? 128 : kRegs;
-  static constexpr int kOtherRegs = kRows > 128 ? 64 : kRows > 64 ? (kBytes == 1 ? 64 : 72) : kRows > 32 && kBytes == 1 ? 80 : kRegs;
+  static constexpr int kRegs = kThreads == 640 ? 96 : kThreads == 768 ? 80 : 72;
+  static constexpr int kPromoRegs = kRows > 128 ? 144 : kRows > 64 ? (kBytes == 1 ? 112 : 128) : kRows > 32 ? 128 : 96;
+  static constexpr int kOtherRegs = kRows > 128 ? 64 : kRows > 64 ? (kBytes == 1 ? 64 : 72) : kBytes == 1 ? (kRows > 32 ? 56 : 64) : (kRows > 32 ? 64 : 72);
   static_assert(kPromo * 128 * kPromoRegs + (kThreads - kPromo * 128) * kOtherRegs <= kThreads * kRegs, "registers");
   static_assert(kSmem <= 232448 && kStages <= kMaxStages && (kStages & (kStages - 1)) == 0, "shared and tensor memory");
   static_assert((size_t)kStages * kStage >= (size_t)kRows * kTileN * 4 || kRows > 128, "room for the sums of a block");
@@ -234,10 +236,10 @@ __device__ __forceinline__ void expand_role(const TcParams &P, const Smem &S, co
   const uint32_t t_lane = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)Sh::kATmem;
   uint32_t from[4];                                 // this row's words of columns 8 t .. and 32 + 8 t ..
 #pragma unroll
-  for (int t = 0; t < 4; ++t) from[t] = S.weights + (uint32_t)((r / kW4Rows) * 512 + w4_place(r, 8 * t) * 16 + 4 * w4_word(r, 0));
+  for (int t = 0; t < 4; ++t) from[t] = S.weights + (uint32_t)(which & 1) * kWeightChunk + (uint32_t)((r / kW4Rows) * 512 + w4_place(r, 8 * t) * 16 + 4 * w4_word(r, 0));
   Parities<Sh::kStages> par(n);
-  uint32_t seq = 0;                                 // chunks of all tiles in sequence: their places in the ring of weights
-  for (int tile = first; tile < total; tile += step, seq += (uint32_t)n, par.next_tile()) {
+  uint32_t seq = 0;                                 // pairs of chunks of all tiles in sequence: their places in the ring of weights
+  for (int tile = first; tile < total; tile += step, seq += (uint32_t)(n + 1) / 2u, par.next_tile()) {
     const int nc = min((tile % P.row_tiles) * kTileN + r, N - 1);
     struct Zeros { uint32_t z[2]; };
     auto fetch = [&](int i, Zeros &f) {
@@ -246,16 +248,19 @@ __device__ __forceinline__ void expand_role(const TcParams &P, const Smem &S, co
         const int c = span.c0 + i;
         f.z[0] = load_global(P.A.zeros + (size_t)min(c * kChunk / group, last_group) * N + nc);
         f.z[1] = group == 32 ? load_global(P.A.zeros + (size_t)min(2 * c + 1, last_group) * N + nc) : f.z[0];
+        // (these come from memory: fetched into the L2 well ahead)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(__cvta_generic_to_global(P.A.zeros + (size_t)min((c + 16) * kChunk / group, last_group) * N + nc)));
       }
     };
     auto expand = [&](int i, const Zeros &f) {
-      const uint32_t slot = (seq + (uint32_t)i) % kWeightStages, use = (seq + (uint32_t)i) / kWeightStages, s = (uint32_t)i % Sh::kStages;
+      const uint32_t pair = seq + (uint32_t)i / 2u, slot = pair % kWeightStages, use = pair / kWeightStages, s = (uint32_t)i % Sh::kStages;
       if (!wait_warp(S, S.wfull + 8u * slot, use & 1u)) return false;
       uint32_t w[8];
 #pragma unroll
       for (int t = 0; t < 4; ++t) lds64(from[t] + slot * kWeightStage, w[t], w[4 + t]);
       __syncwarp();
       if (lane == 0) mbar_arrive(S.wempty + 8u * slot);
+      if (i >= n) return true;                      // the last pair lacks this set's chunk
       if (!wait_warp(S, S.empty + 8u * s, par.of(i) ^ 1u)) return false;
       tc_fence_after();
 #pragma unroll
@@ -281,32 +286,37 @@ __device__ __forceinline__ void expand_role(const TcParams &P, const Smem &S, co
     fetch(which, f0);
     fetch(which + kSets, f1);
 #pragma unroll 1
-    for (int i = which; i < n; i += 2 * kSets) {
+    for (int i = which; i < ((n + 1) & ~1); i += 2 * kSets) {
       if (!expand(i, f0)) return;
       fetch(i + 2 * kSets, f0);
-      if (i + kSets >= n) break;
+      if (i + kSets >= ((n + 1) & ~1)) break;
       if (!expand(i + kSets, f1)) return;
       fetch(i + 3 * kSets, f1);
     }
   }
 }
 
-// One thread copies the packed weights, a chunk of 128 rows at a time.
+// One thread copies the packed weights, two chunks of 128 rows at a time (one at a time it took longer than the
+// rest at few rows of x: 32 rows times 16384x16384 69.9 us).
 __device__ __forceinline__ void weight_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total) {
-  uint32_t seq = 0;
+  uint32_t slot = 0u, parity = 1u, started = 0u;
   for (int tile = first; tile < total; tile += step) {
-    const uint32_t *w = P.A.w + (size_t)(tile % P.row_tiles) * P.col_tiles * (kWeightStage / 4);
+    const uint8_t *w = reinterpret_cast<const uint8_t *>(P.A.w) + ((size_t)(tile % P.row_tiles) * P.col_tiles + span.c0) * kWeightChunk;
+    uint32_t left = (uint32_t)(span.c1 - span.c0) * kWeightChunk;
 #pragma unroll 1
-    for (int c = span.c0; c < span.c1; ++c, ++seq) {
-      const uint32_t slot = seq % kWeightStages, use = seq / kWeightStages;
-      if (!wait(S, S.wempty + 8u * slot, (use & 1u) ^ 1u)) {
+    for (; left > 0u; ++started) {
+      const uint32_t bytes = min(left, kWeightStage), bar = S.wfull + 8u * slot;
+      if (!wait(S, S.wempty + 8u * slot, parity)) {
         // gave up: the copies in flight must land before the block's shared memory is released
-        for (uint32_t u = seq > kWeightStages ? seq - kWeightStages : 0u; u < seq; ++u)
+        for (uint32_t u = started > kWeightStages ? started - kWeightStages : 0u; u < started; ++u)
           for (int i = 0; i < (1 << 12) && !mbar_try(S.wfull + 8u * (u % kWeightStages), (u / kWeightStages) & 1u); ++i) {}
         return;
       }
-      mbar_arrive_expect_tx(S.wfull + 8u * slot, kWeightStage);
-      bulk_copy_g2s(S.weights + slot * kWeightStage, w + (size_t)c * (kWeightStage / 4), kWeightStage, S.wfull + 8u * slot);
+      mbar_arrive_expect_tx(bar, bytes);
+      bulk_copy_g2s(S.weights + slot * kWeightStage, w, bytes, bar);
+      w += bytes;
+      left -= bytes;
+      if (++slot == kWeightStages) { slot = 0u; parity ^= 1u; }
     }
   }
 }
@@ -454,7 +464,18 @@ __device__ __forceinline__ void promote_role(const TcParams &P, const Smem &S, c
   const bool x_groups = A.x_scales != nullptr && A.r.x_group != 0;
   const int G = (A.d.K + A.d.group - 1) / A.d.group;
   const uint32_t t_lane = tmem + ((uint32_t)(32 * quarter) << 16);
-  const uint32_t my_scales = S.scales + (uint32_t)(4 * set + quarter) * 512u;
+  const uint32_t my_scales = S.scales + (uint32_t)(4 * set + quarter) * (512u + kAhead * 128u), my_ring = my_scales + 512u + 4u * lane;
+  // Few rows of x take few instructions per group, and its scales come from memory: eight groups are under way then
+  // (32 rows times 16384x16384 69.9 -> 56.2 us, with four expanding sets).  Many rows have the time of one group's
+  // products for a load from the L2, and no slots to spare (2048 rows times 8192x8192 234 us, 240 with the ring).
+  constexpr bool kRing = kRows <= 64;
+  // A group's scale of this output, into its place of the ring; a copy or none, so that the copies count the groups
+  auto ahead = [&](int u, int nc) {
+    if (u < span.u1)
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(my_ring + 128u * ((uint32_t)u % kAhead)),
+                   "l"(__cvta_generic_to_global(A.scales + (size_t)u * N + nc)) : "memory");
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
   uint32_t dpar = 0u;                               // the accumulators' parities
   for (int tile = first; tile < total; tile += step) {
     const int n = (tile % P.row_tiles) * kTileN + 32 * quarter + lane, nc = min(n, N - 1);
@@ -462,11 +483,23 @@ __device__ __forceinline__ void promote_role(const TcParams &P, const Smem &S, c
     float acc[kUnit];
 #pragma unroll
     for (int i = 0; i < kUnit; ++i) acc[i] = 0.0f;
-    float scale = span.u0 < span.u1 ? load_global(A.scales + (size_t)span.u0 * N + nc) : 0.0f;
+    float next = 0.0f;
+    if constexpr (kRing) {
+#pragma unroll
+      for (int i = 0; i < kAhead - 1; ++i) ahead(span.u0 + i, nc);
+    } else {
+      if (span.u0 < span.u1) next = load_global(A.scales + (size_t)span.u0 * N + nc);
+    }
 #pragma unroll 1
     for (int u = span.u0; u < span.u1; ++u) {
-      const float s = scale;
-      if (u + 1 < span.u1) scale = load_global(A.scales + (size_t)(u + 1) * N + nc);
+      float s = next;
+      if constexpr (kRing) {
+        ahead(u + kAhead - 1, nc);
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+        s = __uint_as_float(lds32(my_ring + 128u * ((uint32_t)u % kAhead)));  // (each lane reads what it copied)
+      } else {
+        if (u + 1 < span.u1) next = load_global(A.scales + (size_t)(u + 1) * N + nc);
+      }
       if (x_groups) {
         __syncwarp();
 #pragma unroll
@@ -478,19 +511,24 @@ __device__ __forceinline__ void promote_role(const TcParams &P, const Smem &S, c
         __syncwarp();
       }
       const uint32_t buf = (uint32_t)(u - span.u0) & 1u;
-      if (!__all_sync(0xFFFFFFFFu, wait_inline(S, S.dfull + 8u * buf, (dpar >> buf) & 1u))) return;
+      if (!__all_sync(0xFFFFFFFFu, wait_inline(S, S.dfull + 8u * buf, (dpar >> buf) & 1u))) {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        return;
+      }
       dpar ^= 1u << buf;
       tc_fence_after();
-      // 32 values at a time: a load of tensor memory takes as long for 16
-      constexpr int kLoad = kRows > 64 || kRows < 32 ? 16 : 32;
+      // 16 values at a time; the next load is under way while these are added
+      constexpr int kLoad = 16, kLoads = kUnit / kLoad;
+      const uint32_t from = t_lane + buf * (uint32_t)kRows + (uint32_t)(set * kUnit);
+      int32_t vs[2][kLoad];
+      tmem_ld16(from, vs[0]);
 #pragma unroll
-      for (int j = 0; j < kUnit / kLoad; ++j) {
-        int32_t v[kLoad];
-        const uint32_t from = t_lane + buf * (uint32_t)kRows + (uint32_t)(set * kUnit + kLoad * j);
-        tmem_ld16(from, v);
-        if constexpr (kLoad == 32) { tmem_ld16(from + 16u, v + 16); tmem_wait16(v + 16); }
+      for (int j = 0; j < kLoads; ++j) {
+        int32_t (&v)[kLoad] = vs[j & 1];
         tmem_wait16(v);
-        if (j + 1 == kUnit / kLoad) {
+        if (j + 1 < kLoads) {
+          tmem_ld16(from + (uint32_t)(kLoad * (j + 1)), vs[(j + 1) & 1]);
+        } else {
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(S.dempty + 8u * buf);
@@ -557,7 +595,7 @@ w4_tc_kernel(const __grid_constant__ TcParams P) {
   if (threadIdx.x == 0) {
     // a stage is full with four expanding warps' arrivals and those that bring the rows
     for (int i = 0; i < Sh::kStages; ++i) { mbar_init(S.full + 8u * i, 4 + (P.copies ? 1 : Sh::kLoadWarps)); mbar_init(S.empty + 8u * i, 1); }
-    for (int i = 0; i < kWeightStages; ++i) { mbar_init(S.wfull + 8u * i, 1); mbar_init(S.wempty + 8u * i, 4); }
+    for (int i = 0; i < kWeightStages; ++i) { mbar_init(S.wfull + 8u * i, 1); mbar_init(S.wempty + 8u * i, 8); }
     for (int i = 0; i < 2; ++i) { mbar_init(S.dfull + 8u * i, 1); mbar_init(S.dempty + 8u * i, 4 * Sh::kPromo); }
     *S.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
