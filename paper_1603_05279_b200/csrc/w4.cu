@@ -227,51 +227,51 @@ w4_few_rows_kernel(const W4Args A, int pieces, uint32_t magic) {
   // stages that lie inside the rows, at addresses that allow whole pieces
   const int sound = pieces ? min(st1, K / kCols) : st0;
   auto load = [&](int st, Stage &s) {
-    if (st < sound) {
+    if (st >= sound) return;
+#pragma unroll
+    for (int i = 0; i < kR; ++i) {
+      const uint4 *p = w[i] + (long long)st * (kU * kW4Panel * 32);
+#pragma unroll
+      for (int u = 0; u < kU; ++u) s.w[i][u] = load_global(p + u * kW4Panel * 32);
+    }
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const uint8_t *p = x[i] + (long long)st * (kCols * kB);
+#pragma unroll
+      for (int h = 0; h < 2 * kU; ++h) load_x8_raw<kType>(p, 32 * h, INT_MAX, true, s.x[i][h]);
+    }
+#pragma unroll
+    for (int h = 0; h < kS; ++h) {
+      const long long at = (long long)st * (kS * N) + h * N;
 #pragma unroll
       for (int i = 0; i < kR; ++i) {
-        const uint4 *p = w[i] + (long long)st * (kU * kW4Panel * 32);
-#pragma unroll
-        for (int u = 0; u < kU; ++u) s.w[i][u] = load_global(p + u * kW4Panel * 32);
+        s.sa[i][h] = load_global(pa[i] + at);
+        s.sb[i][h] = load_global(pb[i] + at);
+        s.za[i][h] = kZeros ? load_global(qa[i] + at) : 8u;
+        s.zb[i][h] = kZeros ? load_global(qb[i] + at) : 8u;
       }
+    }
+  };
+  auto load_any = [&](int st, Stage &s) {
 #pragma unroll
-      for (int i = 0; i < kN; ++i) {
-        const uint8_t *p = x[i] + (long long)st * (kCols * kB);
+    for (int i = 0; i < kR; ++i)
 #pragma unroll
-        for (int h = 0; h < 2 * kU; ++h) load_x8_raw<kType>(p, 32 * h, INT_MAX, true, s.x[i][h]);
-      }
+      for (int u = 0; u < kU; ++u) s.w[i][u] = load_global(w[i] + (size_t)min(st * kU + u, col_tiles - 1) * (kW4Panel * 32));
 #pragma unroll
-      for (int h = 0; h < kS; ++h) {
-        const long long at = (long long)st * (kS * N) + h * N;
+    for (int i = 0; i < kN; ++i)
 #pragma unroll
-        for (int i = 0; i < kR; ++i) {
-          s.sa[i][h] = load_global(pa[i] + at);
-          s.sb[i][h] = load_global(pb[i] + at);
-          s.za[i][h] = kZeros ? load_global(qa[i] + at) : 8u;
-          s.zb[i][h] = kZeros ? load_global(qb[i] + at) : 8u;
-        }
-      }
-    } else if (st < st1) {
+      for (int h = 0; h < 2 * kU; ++h) load_x8_raw<kType>(x[i], st * kCols + 32 * h, K - 8 * t, pieces, s.x[i][h]);
 #pragma unroll
-      for (int i = 0; i < kR; ++i)
+    for (int h = 0; h < kS; ++h) {
+      // a group that does not exist counts nothing: its columns of x are zeros, and so is its scale
+      const bool there = st * kS + h < groups;
+      const long long at = there ? (long long)(st * kS + h) * N : 0;
 #pragma unroll
-        for (int u = 0; u < kU; ++u) s.w[i][u] = load_global(w[i] + (size_t)min(st * kU + u, col_tiles - 1) * (kW4Panel * 32));
-#pragma unroll
-      for (int i = 0; i < kN; ++i)
-#pragma unroll
-        for (int h = 0; h < 2 * kU; ++h) load_x8_raw<kType>(x[i], st * kCols + 32 * h, K - 8 * t, pieces, s.x[i][h]);
-#pragma unroll
-      for (int h = 0; h < kS; ++h) {
-        // a group that does not exist counts nothing: its columns of x are zeros, and so is its scale
-        const bool there = st * kS + h < groups;
-        const long long at = there ? (long long)(st * kS + h) * N : 0;
-#pragma unroll
-        for (int i = 0; i < kR; ++i) {
-          s.sa[i][h] = there ? load_global(pa[i] + at) : 0.0f;
-          s.sb[i][h] = there ? load_global(pb[i] + at) : 0.0f;
-          s.za[i][h] = kZeros ? load_global(qa[i] + at) : 8u;
-          s.zb[i][h] = kZeros ? load_global(qb[i] + at) : 8u;
-        }
+      for (int i = 0; i < kR; ++i) {
+        s.sa[i][h] = there ? load_global(pa[i] + at) : 0.0f;
+        s.sb[i][h] = there ? load_global(pb[i] + at) : 0.0f;
+        s.za[i][h] = kZeros ? load_global(qa[i] + at) : 8u;
+        s.zb[i][h] = kZeros ? load_global(qb[i] + at) : 8u;
       }
     }
   };
@@ -323,12 +323,18 @@ w4_few_rows_kernel(const W4Args A, int pieces, uint32_t magic) {
   load(st0, s0);
   load(st0 + 1, s1);
 #pragma unroll 1
-  for (int st = st0; st < st1; st += 2) {
+  for (int st = st0; st < sound; st += 2) {
     multiply(st, s0);
     load(st + 2, s0);
-    if (st + 1 >= st1) break;
+    if (st + 1 >= sound) break;
     multiply(st + 1, s1);
     load(st + 3, s1);
+  }
+  // what is left: the ragged end of the rows, or all of them
+#pragma unroll 1
+  for (int st = max(st0, sound); st < st1; ++st) {
+    load_any(st, s0);
+    multiply(st, s0);
   }
 #pragma unroll
   for (int i = 0; i < kR; ++i)

@@ -20,6 +20,7 @@
 #include <cuda.h>
 
 #include <algorithm>
+#include <climits>
 #include <atomic>
 
 #include "umma_common.cuh"
@@ -358,30 +359,35 @@ __device__ __forceinline__ void load_role(const TcParams &P, const Smem &S, cons
   for (int tile = first; tile < total; tile += step, par.next_tile()) {
     const long long tok0 = (long long)(tile / P.row_tiles) * kRows;
     const int rows = (int)min((long long)kRows, P.A.r.rows - tok0);
-    const uint8_t *x = static_cast<const uint8_t *>(P.A.x) + (tok0 + row0) * row_bytes;
+    const uint8_t *x = static_cast<const uint8_t *>(P.A.x) + tok0 * row_bytes;
+    // (a row that does not exist is its last one's: no output reads it)
     struct Batch { uint32_t v[kBatch][2 * kB]; };
-    auto load = [&](int i, int p0, Batch &b) {
-      if (i >= n) return;
-      const int k = (span.c0 + i) * kChunk + 8 * piece;
+    auto whole = [&](int i) { return P.pieces && (span.c0 + i + 1) * kChunk <= K; };
+    auto load = [&](int i, int p0, Batch &b) {       // of a whole chunk, at addresses for whole pieces: nothing but loads
+      if (i >= n || !whole(i)) return;
+      const uint8_t *from = x + ((span.c0 + i) * kChunk + 8 * piece) * kB;
 #pragma unroll
-      for (int p = 0; p < kBatch; ++p) {
-        const int row = row0 + kStep * (p0 + p);
-        if (row < rows) {
-          load_x8_raw<kType>(x + (long long)(kStep * (p0 + p)) * row_bytes, k, K, P.pieces, b.v[p]);
-        } else {
-#pragma unroll
-          for (int q = 0; q < 2 * kB; ++q) b.v[p][q] = 0u;
-        }
-      }
+      for (int p = 0; p < kBatch; ++p)
+        load_x8_raw<kType>(from + (long long)min(row0 + kStep * (p0 + p), rows - 1) * row_bytes, 0, INT_MAX, true, b.v[p]);
+    };
+    auto put = [&](int i, int row, const uint32_t (&raw)[2 * kB]) {
+      uint32_t v[4];
+      x8_pairs<kType>(raw, v);
+      if (row < kRows)
+        sts128(S.ring + ((uint32_t)i % Sh::kStages) * Sh::kStage + (uint32_t)row * 128u + (uint32_t)((piece ^ (row & 7)) * 16), v[0], v[1], v[2], v[3]);
     };
     auto store = [&](int i, int p0, const Batch &b) {
-      const uint32_t dst = S.ring + ((uint32_t)i % Sh::kStages) * Sh::kStage;
+      if (whole(i)) {
 #pragma unroll
-      for (int p = 0; p < kBatch; ++p) {
-        const int row = row0 + kStep * (p0 + p);
-        uint32_t v[4];
-        x8_pairs<kType>(b.v[p], v);
-        if (row < kRows) sts128(dst + (uint32_t)row * 128u + (uint32_t)((piece ^ (row & 7)) * 16), v[0], v[1], v[2], v[3]);
+        for (int p = 0; p < kBatch; ++p) put(i, row0 + kStep * (p0 + p), b.v[p]);
+      } else {
+#pragma unroll 1
+        for (int p = 0; p < kBatch; ++p) {
+          uint32_t raw[2 * kB];
+          const int row = row0 + kStep * (p0 + p);
+          load_x8_raw<kType>(x + (long long)min(row, rows - 1) * row_bytes, (span.c0 + i) * kChunk + 8 * piece, K, P.pieces, raw);
+          put(i, row, raw);
+        }
       }
     };
     auto start = [&](int i) { return wait_warp(S, S.empty + 8u * (i % Sh::kStages), par.of(i) ^ 1u); };
@@ -600,6 +606,8 @@ w4_tc_kernel(const __grid_constant__ TcParams P) {
     *S.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  if (warp == Sh::kLoadWarp && lane == 0 && P.copies)
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&P.x_map) : "memory");
   if (warp == Sh::kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(S.tmem_slot)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
