@@ -1,12 +1,22 @@
 // Root-mean-square norm of rows with the residual's addition, in the rows' type or in 8 bits with scales, and
 // its backward pass.  Every row is read once: its values stay in the registers of a team of threads.
+//
+// HBM bounds them.  The forward pass gets there with enough loads under way in registers (8192x4096 bf16 with residual
+// 43.7 us, 0.94 of the copy bandwidth); a ring of rows in shared memory, filled by bulk copies, took longer there (59:
+// fewer warps for the same work).  The backward pass, which has the sums of the weight's gradient in its registers too,
+// needs that ring for long rows in numbers (4096x4096 39 -> 34 us): persistent blocks, one row at a time.
 #include <algorithm>
 
 #include "rows.cuh"
+#include "umma_common.cuh"
 
 namespace xnor {
 
+__device__ int g_status_norm = 0;
+
 namespace {
+
+using namespace umma;
 
 // ---- reductions over a team (a power of two of threads, 32 and more, of a block) ---------------
 struct Team {
@@ -59,16 +69,29 @@ int weight_kind(const void *w, const xnor_norm_desc &d) {
   return w == nullptr ? 0 : d.weight_type == XNOR_F32 ? 1 : 2;
 }
 
-// y / s to nearest even.  The reciprocal is within an ulp of the quotient's factor except where it overflows.
-struct Divide {
-  float s, inv;
-  bool tiny;
-  __device__ __forceinline__ explicit Divide(float s_) : s(s_) {
-    tiny = s > 0.0f && s < 1e-37f;
-    inv = s > 0.0f ? 1.0f / s : 0.0f;
+// The scale of a group whose largest magnitude is m (as bits), and what its values are multiplied with.  Both are within
+// two roundings of m / top and its reciprocal, at a few instructions (two IEEE divisions took a tenth of the time of
+// e4m3 rows); where the reciprocal would overflow or the scale lose bits, they are divided.
+__device__ __forceinline__ float scale_of(uint32_t m, bool i8, float &inv) {
+  const float v = __uint_as_float(m), top = i8 ? 127.0f : 448.0f;
+  if (m < 0x08800000u && m > 0u) {           // below 2^-110
+    inv = -1.0f;
+    return __fdiv_rn(v, top);
   }
-  __device__ __forceinline__ float operator()(float y) const { return tiny ? y / s : y * inv; }
-};
+  float r;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+  inv = m > 0u && m < 0x7F800000u ? top * r : 0.0f;        // a group of zeros, infinite or NaN: zeros (NaN)
+  return v * (i8 ? 1.0f / 127.0f : 1.0f / 448.0f);
+}
+__device__ __forceinline__ void divide(float (&y)[8], float s, float inv) {
+  if (inv < 0.0f) {
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) y[i] = s > 0.0f ? y[i] / s : 0.0f;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] *= inv;
+}
 
 __device__ __forceinline__ uint32_t pack_i8(float a, float b, float c, float d) {
   auto q = [](float v) { return (uint32_t)(uint8_t)(int8_t)min(127, max(-127, __float2int_rn(v))); };
@@ -80,9 +103,119 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
   return lo | hi << 16;
 }
 
-// Forward.  Chunk c = rank + v * team of a row belongs to one thread; kV chunks per thread cover the row.
+// Forward: what follows the loads of a row.  Chunk c = rank + v * team of a row belongs to one thread; kV chunks per
+// thread cover the row.  `read` is called when every thread of the block has its values.
+template <class T, int kV, bool kQuant>
+__device__ __forceinline__ void finish_row(const NormArgs &A, const Team &team, long long row, bool real, const int (&in)[kV], Chunk<T> (&xc)[kV],
+                                           const Chunk<T> (&rc)[kV], const Weights<T> (&wc)[kV], int weights, int pieces, float *red,
+                                           uint32_t *red_max) {
+  const int D = A.d.cols;
+  // (16-bit values stay packed and are converted twice: half the registers, so twice the rows under way)
+  float ss = 0.0f;
+#pragma unroll
+  for (int v = 0; v < kV; ++v) {
+    float h[8];
+    xc[v].to_float(h);
+    if (A.residual) {
+      float r[8];
+      rc[v].to_float(r);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[i] += r[i];
+      // the norm is of the sum as it is stored, which is what later layers and the backward pass read
+      xc[v].from_float(h);
+      xc[v].to_float(h);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ss = fmaf(h[i], h[i], ss);
+  }
+  if (A.sum) {
+    T *sum = static_cast<T *>(A.sum) + (real ? row * A.d.sum_stride : 0);
+#pragma unroll
+    for (int v = 0; v < kV; ++v) xc[v].store(sum + 8 * (team.rank + v * team.size), pieces, in[v]);
+  }
+  ss = team.reduce(ss, red, Add());
+  const float rstd = 1.0f / sqrtf(ss / (float)D + A.d.eps);
+  if (A.rstd && real && team.rank == 0) A.rstd[row] = rstd;
+  auto normed = [&](int v, float (&y)[8]) {
+    xc[v].to_float(y);
+    float w[8];
+    if constexpr (kV > 2) {                   // (long rows: not held over the sum, whose latency other rows fill)
+      Weights<T> late;
+      late.load(A.weight, weights, 8 * (team.rank + v * team.size), in[v]);
+      late.to_float(weights, w);
+    } else {
+      wc[v].to_float(weights, w);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = y[i] * rstd * w[i];
+  };
+  if constexpr (!kQuant) {
+    T *y = static_cast<T *>(A.y) + (real ? row * A.d.y_stride : 0);
+#pragma unroll
+    for (int v = 0; v < kV; ++v) {
+      float u[8];
+      normed(v, u);
+      xc[v].from_float(u);
+      xc[v].store(y + 8 * (team.rank + v * team.size), pieces, in[v]);
+    }
+  } else {
+    const bool i8 = A.q_type == XNOR_I8;
+    float u[kV <= 2 ? kV : 1][8];             // (many chunks: formed again)
+    uint32_t m[kV];
+#pragma unroll
+    for (int v = 0; v < kV; ++v) {
+      float (&y)[8] = u[kV <= 2 ? v : 0];
+      normed(v, y);
+      m[v] = 0u;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m[v] = max(m[v], magnitude(y[i]));
+    }
+    const int lanes = A.group / 8, lg = 31 - __clz(max(A.group, 1));      // threads of a group: 4, 8 or 16, in one warp
+    if (A.group == 0) {
+      uint32_t all = m[0];
+#pragma unroll
+      for (int v = 1; v < kV; ++v) all = max(all, m[v]);
+      all = team.reduce(all, red_max, Max());
+#pragma unroll
+      for (int v = 0; v < kV; ++v) m[v] = all;
+    } else {
+#pragma unroll
+      for (int v = 0; v < kV; ++v)
+#pragma unroll
+        for (int o = 1; o < 16; o *= 2) {
+          const uint32_t other = __shfl_xor_sync(0xffffffffu, m[v], o);
+          if (o < lanes) m[v] = max(m[v], other);
+        }
+    }
+    uint8_t *q = static_cast<uint8_t *>(A.q) + (real ? row * D : 0);
+#pragma unroll
+    for (int v = 0; v < kV; ++v) {
+      const int chunk = team.rank + v * team.size;
+      float inv;
+      const float s = scale_of(m[v], i8, inv);
+      if (A.group == 0) {
+        if (v == 0 && team.rank == 0 && real) A.scales[row] = s;
+      } else if (in[v] > 0 && (chunk & (lanes - 1)) == 0) {
+        A.scales[row * (D >> lg) + (chunk >> (lg - 3))] = s;
+      }
+      float (&y)[8] = u[kV <= 2 ? v : 0];
+      if constexpr (kV > 2) normed(v, y);
+      divide(y, s, inv);
+      const uint32_t lo = i8 ? pack_i8(y[0], y[1], y[2], y[3]) : pack_e4m3(y[0], y[1], y[2], y[3]);
+      const uint32_t hi = i8 ? pack_i8(y[4], y[5], y[6], y[7]) : pack_e4m3(y[4], y[5], y[6], y[7]);
+      if ((D & 7) == 0) {
+        if (in[v] > 0) *reinterpret_cast<uint2 *>(q + 8 * chunk) = make_uint2(lo, hi);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < in[v]) q[8 * chunk + i] = (uint8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
+      }
+    }
+  }
+}
+
 template <class T, int kV, int kMost, bool kQuant>
-__global__ void __launch_bounds__(kMost)
+__global__ void __launch_bounds__(kMost, kMost <= 512 && sizeof(T) == 2 ? 2 : 1)
 rmsnorm_kernel(const NormArgs A, int team_size, int weights, int pieces) {
   __shared__ float red[kMost / 32];
   __shared__ uint32_t red_max[kMost / 32];
@@ -104,173 +237,201 @@ rmsnorm_kernel(const NormArgs A, int team_size, int weights, int pieces) {
     xc[v].load(x + c, pieces, in[v]);
     if (A.residual) rc[v].load(res + c, pieces, in[v]);
   }
+  if constexpr (kV <= 2) {
 #pragma unroll
-  for (int v = 0; v < kV; ++v) wc[v].load(A.weight, weights, 8 * (team.rank + v * team.size), in[v]);
-  float h[kV][8], ss = 0.0f;
-#pragma unroll
-  for (int v = 0; v < kV; ++v) {
-    xc[v].to_float(h[v]);
-    if (A.residual) {
-      float r[8];
-      rc[v].to_float(r);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) h[v][i] += r[i];
-      // the norm is of the sum as it is stored, which is what later layers and the backward pass read
-      xc[v].from_float(h[v]);
-      xc[v].to_float(h[v]);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) ss = fmaf(h[v][i], h[v][i], ss);
+    for (int v = 0; v < kV; ++v) wc[v].load(A.weight, weights, 8 * (team.rank + v * team.size), in[v]);
   }
-  if (A.sum) {
-    T *sum = static_cast<T *>(A.sum) + (real ? row * A.d.sum_stride : 0);
-#pragma unroll
-    for (int v = 0; v < kV; ++v) xc[v].store(sum + 8 * (team.rank + v * team.size), pieces, in[v]);
+  finish_row<T, kV, kQuant>(A, team, row, real, in, xc, rc, wc, weights, pieces, red, red_max);
+}
+
+// ---- rows through a ring in shared memory -----------------------------------------------------
+constexpr int kMaxStages = 8;
+constexpr int kRingControl = 128;          // barriers and the abort flag
+
+// Blocks take rows b, b + grid, ...; thread 0 copies each row's tensors, `tensors` of them, into a stage.
+struct RowRing {
+  uint32_t bars, data, row_bytes, stage_bytes, stages;
+  volatile int *abort_flag;
+  int count;                               // rows of this block
+
+  __device__ __forceinline__ RowRing(uint8_t *smem, int rows, uint32_t row_bytes_, int tensors, int stages_)
+      : bars(smem_u32(smem)), data(smem_u32(smem) + kRingControl), row_bytes(row_bytes_), stage_bytes(row_bytes_ * (uint32_t)tensors),
+        stages((uint32_t)stages_), abort_flag(reinterpret_cast<volatile int *>(smem + 8 * kMaxStages)) {
+    count = (int)blockIdx.x < rows ? (rows - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
+    if (threadIdx.x == 0) {
+      for (uint32_t s = 0; s < stages; ++s) mbar_init(bars + 8u * s, 1);
+      *abort_flag = 0;
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
   }
-  ss = team.reduce(ss, red, Add());
-  const float rstd = 1.0f / sqrtf(ss / (float)D + A.d.eps);
-  if (A.rstd && real && team.rank == 0) A.rstd[row] = rstd;
-#pragma unroll
-  for (int v = 0; v < kV; ++v) {
-    float w[8];
-    wc[v].to_float(weights, w);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) h[v][i] = h[v][i] * rstd * w[i];
+  __device__ __forceinline__ long long row(int i) const { return blockIdx.x + (long long)i * gridDim.x; }
+  __device__ __forceinline__ uint32_t stage(int i) const { return data + ((uint32_t)i % stages) * stage_bytes; }
+  __device__ __forceinline__ void expect(int i) const { mbar_arrive_expect_tx(bars + 8u * ((uint32_t)i % stages), stage_bytes); }
+  __device__ __forceinline__ void copy(int i, int tensor, const void *from) const {
+    bulk_copy_g2s(stage(i) + (uint32_t)tensor * row_bytes, from, row_bytes, bars + 8u * ((uint32_t)i % stages));
   }
-  if constexpr (!kQuant) {
-    T *y = static_cast<T *>(A.y) + (real ? row * A.d.y_stride : 0);
+  // Waits for row i of this block; false (for every thread): given up.
+  __device__ __forceinline__ bool wait(int i) const {
+    const bool ok = mbar_wait(bars + 8u * ((uint32_t)i % stages), ((uint32_t)i / stages) & 1u, abort_flag, &g_status_norm);
+    return ok;
+  }
+  // After giving up at row i: the copies in flight must land before the block's shared memory is released.
+  __device__ __forceinline__ void drain(int i) const {
+    for (int k = i; k < count && k < i + (int)stages; ++k)
+      for (int n = 0; n < (1 << 12) && !mbar_try(bars + 8u * ((uint32_t)k % stages), ((uint32_t)k / stages) & 1u); ++n) {}
+  }
+};
+
+template <class T>
+__device__ __forceinline__ void load_shared(Chunk<T> &c, uint32_t addr) {
 #pragma unroll
-    for (int v = 0; v < kV; ++v) {
-      xc[v].from_float(h[v]);
-      xc[v].store(y + 8 * (team.rank + v * team.size), pieces, in[v]);
-    }
-  } else {
-    const float top = A.q_type == XNOR_I8 ? 127.0f : 448.0f;
-    uint32_t m[kV];
-#pragma unroll
-    for (int v = 0; v < kV; ++v) {
-      m[v] = 0u;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) m[v] = max(m[v], magnitude(h[v][i]));
-    }
-    const int lanes = A.group / 8;            // threads of a group: 4, 8 or 16, in one warp
-    if (A.group == 0) {
-      uint32_t all = m[0];
-#pragma unroll
-      for (int v = 1; v < kV; ++v) all = max(all, m[v]);
-      all = team.reduce(all, red_max, Max());
-#pragma unroll
-      for (int v = 0; v < kV; ++v) m[v] = all;
-    } else {
-#pragma unroll
-      for (int v = 0; v < kV; ++v)
-        for (int o = 1; o < lanes; o *= 2) m[v] = max(m[v], __shfl_xor_sync(0xffffffffu, m[v], o));
-    }
-    uint8_t *q = static_cast<uint8_t *>(A.q) + (real ? row * D : 0);
-#pragma unroll
-    for (int v = 0; v < kV; ++v) {
-      const int chunk = team.rank + v * team.size;
-      const float s = __fdiv_rn(__uint_as_float(m[v]), top);
-      if (A.group == 0) {
-        if (v == 0 && team.rank == 0 && real) A.scales[row] = s;
-      } else if (in[v] > 0 && (chunk & (lanes - 1)) == 0) {
-        A.scales[row * (D / A.group) + chunk / lanes] = s;
-      }
-      const Divide by(s);
-      float u[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) u[i] = by(h[v][i]);
-      const bool i8 = A.q_type == XNOR_I8;
-      const uint32_t lo = i8 ? pack_i8(u[0], u[1], u[2], u[3]) : pack_e4m3(u[0], u[1], u[2], u[3]);
-      const uint32_t hi = i8 ? pack_i8(u[4], u[5], u[6], u[7]) : pack_e4m3(u[4], u[5], u[6], u[7]);
-      if ((D & 7) == 0) {
-        if (in[v] > 0) *reinterpret_cast<uint2 *>(q + 8 * chunk) = make_uint2(lo, hi);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i < in[v]) q[8 * chunk + i] = (uint8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
-      }
-    }
+  for (int i = 0; i < Chunk<T>::kWords / 4; ++i) {
+    uint32_t v[4];
+    lds128(addr + 16u * i, v);
+    c.w[4 * i] = v[0]; c.w[4 * i + 1] = v[1]; c.w[4 * i + 2] = v[2]; c.w[4 * i + 3] = v[3];
   }
 }
 
 // Backward.  With u = w dy: dx = rstd (u - h (rstd^2 / D) sum(u h)) (+ dsum), dw = sum over rows of dy h rstd.
 // A block takes rows b, b + grid, ...; the sums of dw stay in registers and leave as one row of partial sums
 // per block, which rmsnorm_dweight_kernel adds in the blocks' order.
+template <class T, int kV>
+struct BackwardRow {
+  Chunk<T> h[kV], y[kV], s[kV];
+  float rstd;
+};
+
+template <class T, int kV, class Read>
+__device__ __forceinline__ void finish_backward(const NormBackwardArgs &A, const Team &team, long long row, const int (&in)[kV],
+                                                const BackwardRow<T, kV> &r, const Weights<T> (&wc)[kV], int weights, int pieces,
+                                                float (&dw)[kV][8], float *sums, Read &&read) {
+  T *dx = static_cast<T *>(A.dx) + row * A.d.sum_stride;
+  float dot = 0.0f;
+#pragma unroll
+  for (int v = 0; v < kV; ++v) {
+    float hv[8], yv[8], w[8];
+    r.h[v].to_float(hv);
+    r.y[v].to_float(yv);
+    wc[v].to_float(weights, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      dot = fmaf(yv[i] * w[i], hv[i], dot);
+      dw[v][i] = fmaf(yv[i], hv[i] * r.rstd, dw[v][i]);
+    }
+  }
+  dot = team.reduce(dot, sums, Add());
+  read();
+  const float k = dot * (r.rstd * r.rstd / (float)A.d.cols);
+#pragma unroll
+  for (int v = 0; v < kV; ++v) {
+    float hv[8], yv[8], w[8], sv[8], o[8];
+    r.h[v].to_float(hv);
+    r.y[v].to_float(yv);
+    wc[v].to_float(weights, w);
+    if (A.dsum) r.s[v].to_float(sv);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      o[i] = r.rstd * fmaf(-hv[i], k, yv[i] * w[i]);
+      if (A.dsum) o[i] += sv[i];
+    }
+    Chunk<T> oc;
+    oc.from_float(o);
+    oc.store(dx + 8 * (team.rank + v * team.size), pieces, in[v]);
+  }
+}
+
+// This block's partial sums of dw.
+template <int kV>
+__device__ __forceinline__ void store_partial(const NormBackwardArgs &A, const Team &team, const int (&in)[kV], const float (&dw)[kV][8]) {
+  if (A.work == nullptr) return;
+  float *part = A.work + (size_t)blockIdx.x * A.d.cols;
+#pragma unroll
+  for (int v = 0; v < kV; ++v) {
+    Chunk<float> f;
+    f.from_float(dw[v]);
+    f.store(part + 8 * (team.rank + v * team.size), (A.d.cols & 7) == 0, in[v]);
+  }
+}
+
 template <class T, int kV, int kMost>
-__global__ void __launch_bounds__(kMost)
+__global__ void __launch_bounds__(kMost, kV == 1 ? 2 : 1)
 rmsnorm_backward_kernel(const NormBackwardArgs A, int weights, int pieces) {
   __shared__ float red[2][kMost / 32];
   const Team team((int)blockDim.x);
-  const int D = A.d.cols;
   int in[kV];
 #pragma unroll
-  for (int v = 0; v < kV; ++v) in[v] = min(8, max(0, D - 8 * (team.rank + v * team.size)));
+  for (int v = 0; v < kV; ++v) in[v] = min(8, max(0, A.d.cols - 8 * (team.rank + v * team.size)));
   stream_order();
   Weights<T> wc[kV];
-  float dw[kV][8];
+  float dw[kV][8] = {};
 #pragma unroll
-  for (int v = 0; v < kV; ++v) {
-    wc[v].load(A.weight, weights, 8 * (team.rank + v * team.size), in[v]);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) dw[v][i] = 0.0f;
-  }
+  for (int v = 0; v < kV; ++v) wc[v].load(A.weight, weights, 8 * (team.rank + v * team.size), in[v]);
   int turn = 0;
+#pragma unroll 1
   for (long long row = blockIdx.x; row < A.d.rows; row += gridDim.x, turn ^= 1) {
     const T *h = static_cast<const T *>(A.h) + row * A.d.x_stride;
     const T *dy = static_cast<const T *>(A.dy) + row * A.d.y_stride;
     const T *ds = static_cast<const T *>(A.dsum) + (A.dsum ? row * A.d.residual_stride : 0);
-    T *dx = static_cast<T *>(A.dx) + row * A.d.sum_stride;
-    Chunk<T> hc[kV], yc[kV], sc[kV];
+    BackwardRow<T, kV> r;
 #pragma unroll
     for (int v = 0; v < kV; ++v) {
       const int c = 8 * (team.rank + v * team.size);
-      hc[v].load(h + c, pieces, in[v]);
-      yc[v].load(dy + c, pieces, in[v]);
-      if (A.dsum) sc[v].load(ds + c, pieces, in[v]);
+      r.h[v].load(h + c, pieces, in[v]);
+      r.y[v].load(dy + c, pieces, in[v]);
+      if (A.dsum) r.s[v].load(ds + c, pieces, in[v]);
     }
-    const float rstd = load_global(A.rstd + row);
-    float dot = 0.0f;
+    r.rstd = load_global(A.rstd + row);
+    finish_backward<T, kV>(A, team, row, in, r, wc, weights, pieces, dw, red[turn], [] {});
+  }
+  store_partial<kV>(A, team, in, dw);
+}
+
+template <class T, int kV, int kMost>
+__global__ void __launch_bounds__(kMost, kV == 1 ? 2 : 1)
+rmsnorm_backward_ring_kernel(const NormBackwardArgs A, int weights, int stages) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ float red[2][kMost / 32];
+  const Team team((int)blockDim.x);
+  const RowRing ring(smem, A.d.rows, (uint32_t)A.d.cols * sizeof(T), A.dsum ? 3 : 2, stages);
+  int in[kV];
+#pragma unroll
+  for (int v = 0; v < kV; ++v) in[v] = min(8, max(0, A.d.cols - 8 * (team.rank + v * team.size)));
+  stream_order();
+  auto fetch = [&](int i) {
+    if (threadIdx.x != 0 || i >= ring.count) return;
+    ring.expect(i);
+    ring.copy(i, 0, static_cast<const T *>(A.h) + ring.row(i) * A.d.x_stride);
+    ring.copy(i, 1, static_cast<const T *>(A.dy) + ring.row(i) * A.d.y_stride);
+    if (A.dsum) ring.copy(i, 2, static_cast<const T *>(A.dsum) + ring.row(i) * A.d.residual_stride);
+  };
+  for (int i = 0; i < stages; ++i) fetch(i);
+  Weights<T> wc[kV];
+  float dw[kV][8] = {};
+#pragma unroll
+  for (int v = 0; v < kV; ++v) wc[v].load(A.weight, weights, 8 * (team.rank + v * team.size), in[v]);
+  float next = ring.count > 0 ? load_global(A.rstd + ring.row(0)) : 0.0f;
+#pragma unroll 1
+  for (int i = 0; i < ring.count; ++i) {
+    const float rstd = next;
+    if (i + 1 < ring.count) next = load_global(A.rstd + ring.row(i + 1));
+    if (__syncthreads_or(!ring.wait(i))) {         // (all give up together)
+      if (threadIdx.x == 0) ring.drain(i);
+      return;
+    }
+    BackwardRow<T, kV> r;
+    r.rstd = rstd;
 #pragma unroll
     for (int v = 0; v < kV; ++v) {
-      float hv[8], yv[8], w[8];
-      hc[v].to_float(hv);
-      yc[v].to_float(yv);
-      wc[v].to_float(weights, w);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        dot = fmaf(yv[i] * w[i], hv[i], dot);
-        dw[v][i] = fmaf(yv[i], hv[i] * rstd, dw[v][i]);
-      }
+      if (in[v] == 0) { r.h[v].zero(); r.y[v].zero(); r.s[v].zero(); continue; }
+      const uint32_t at = ring.stage(i) + 8u * (uint32_t)sizeof(T) * (uint32_t)(team.rank + v * team.size);
+      load_shared(r.h[v], at);
+      load_shared(r.y[v], at + ring.row_bytes);
+      if (A.dsum) load_shared(r.s[v], at + 2u * ring.row_bytes);
     }
-    dot = team.reduce(dot, red[turn], Add());
-    const float k = dot * (rstd * rstd / (float)D);
-#pragma unroll
-    for (int v = 0; v < kV; ++v) {
-      float hv[8], yv[8], w[8], sv[8], o[8];
-      hc[v].to_float(hv);
-      yc[v].to_float(yv);
-      wc[v].to_float(weights, w);
-      if (A.dsum) sc[v].to_float(sv);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        o[i] = rstd * fmaf(-hv[i], k, yv[i] * w[i]);
-        if (A.dsum) o[i] += sv[i];
-      }
-      Chunk<T> oc;
-      oc.from_float(o);
-      oc.store(dx + 8 * (team.rank + v * team.size), pieces, in[v]);
-    }
+    finish_backward<T, kV>(A, team, ring.row(i), in, r, wc, weights, 1, dw, red[i & 1], [&] { fetch(i + stages); });
   }
-  if (A.work == nullptr) return;
-  float *part = A.work + (size_t)blockIdx.x * D;
-#pragma unroll
-  for (int v = 0; v < kV; ++v) {
-    const int c = 8 * (team.rank + v * team.size);
-    Chunk<float> f;
-    f.from_float(dw[v]);
-    f.store(part + c, (D & 7) == 0, in[v]);
-  }
+  store_partial<kV>(A, team, in, dw);
 }
 
 // dweight[c] = sum over the partial rows, in their order: eight threads of a column take every eighth row each.
@@ -298,27 +459,70 @@ rmsnorm_dweight_kernel(const float *part, int parts, int D, float *__restrict__ 
 struct Deal {
   int per_thread, most, team;       // team: a power of two of whole warps
 };
-Deal deal(int cols) {
+enum Pass { kForward, kQuantized, kBackward };
+// Chunks per thread, measured: 8192x4096 with residual 59 us with one, 47 with two, 43.7 with four (32 bits: 51, 43.6,
+// 46.4); e4m3 2048x4096 23, 16.6, 19.2; backward 4096x4096 50 with one, 34 with two.
+Deal deal(int cols, Pass pass, size_t elem) {
   const int chunks = (cols + 7) / 8;
   Deal d;
-  d.per_thread = chunks <= 512 ? 1 : chunks <= 1024 ? 2 : 4;
+  d.per_thread = chunks <= 256 ? 1 : chunks <= (pass == kForward && elem == 2 ? 256 : 1024) ? 2 : 4;
   d.most = chunks <= 2048 ? 512 : 1024;
   d.team = 32;
   while (d.team * d.per_thread < chunks) d.team *= 2;
   return d;
 }
 
-template <class T, int kV, int kMost>
-cudaError_t run(const NormArgs &a, const Deal &l, cudaStream_t st) {
+// Blocks per SM of the backward pass, by the registers that their threads take.
+int blocks_per_sm(const Deal &l) { return std::max(1, std::min(8, (l.per_thread == 1 ? 1024 : 512) / l.team)); }
+
+// The ring kernels' stages; 0: not for these rows (short ones, whose copies would be small, few of them, or two of
+// their stages do not fit).  `tensors`: read per row.
+struct Ring {
+  int stages;
+  size_t smem;
+};
+Ring ring_of(int rows, int cols, size_t elem, int tensors, bool pieces) {
+  const size_t row = (size_t)cols * elem, stage = row * (size_t)tensors;
+  const Deal l = deal(cols, kBackward, elem);
+  Ring r = {0, 0};
+  if (!pieces || row < 4096 || l.team < 64 || l.most > 512 || rows < 4 * (int)kSms) return r;
+  const size_t room = 200 * 1024 / (size_t)blocks_per_sm(l) - 2048;
+  r.stages = (int)std::min<size_t>(kMaxStages, room / stage);
+  if (r.stages < 2) r.stages = 0;
+  r.smem = kRingControl + (size_t)r.stages * stage;
+  return r;
+}
+
+template <class K>
+cudaError_t allow_shared(K *kernel, bool (&flags)[64]) {
+  bool &set = attr_done_for_current_device(flags);
+  if (set) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+  if (e != cudaSuccess) (void)cudaGetLastError();
+  set = e == cudaSuccess;
+  return e;
+}
+
+template <class T, int kV, int kMost, bool kQuant>
+cudaError_t run(const NormArgs &a, const Deal &l, int pieces, cudaStream_t st) {
+  const int w = weight_kind<T>(a.weight, a.d);
   const int threads = std::max(l.team, 128), per_block = threads / l.team;
   const dim3 grid((unsigned)((a.d.rows + (long long)per_block - 1) / per_block));
+  return launch_kernel(rmsnorm_kernel<T, kV, kMost, kQuant>, grid, (unsigned)threads, 0, st, 1, a, l.team, w, pieces);
+}
+
+template <class T, int kV, int kMost>
+cudaError_t run(const NormArgs &a, const Deal &l, cudaStream_t st) {
   const int pieces = rows_in_pieces(a.x, a.d.x_stride, a.d.cols, sizeof(T)) &&
                      rows_in_pieces(a.residual, a.d.residual_stride, a.d.cols, sizeof(T)) &&
                      rows_in_pieces(a.sum, a.d.sum_stride, a.d.cols, sizeof(T)) &&
                      rows_in_pieces(a.y, a.d.y_stride, a.d.cols, sizeof(T));
-  const int w = weight_kind<T>(a.weight, a.d);
-  if (a.q) return launch_kernel(rmsnorm_kernel<T, kV, kMost, true>, grid, (unsigned)threads, 0, st, 1, a, l.team, w, pieces);
-  return launch_kernel(rmsnorm_kernel<T, kV, kMost, false>, grid, (unsigned)threads, 0, st, 1, a, l.team, w, pieces);
+  return a.q ? run<T, kV, kMost, true>(a, l, pieces, st) : run<T, kV, kMost, false>(a, l, pieces, st);
+}
+
+// Blocks, and with them rows of partial sums, of the backward pass.  (They do not depend on the device.)
+int backward_blocks(int rows, int cols) {
+  return std::min(rows, blocks_per_sm(deal(cols, kBackward, 2)) * (int)kSms);
 }
 
 template <class T, int kV, int kMost>
@@ -327,13 +531,26 @@ cudaError_t run(const NormBackwardArgs &a, const Deal &l, cudaStream_t st) {
                      rows_in_pieces(a.dy, a.d.y_stride, a.d.cols, sizeof(T)) &&
                      rows_in_pieces(a.dsum, a.d.residual_stride, a.d.cols, sizeof(T)) &&
                      rows_in_pieces(a.dx, a.d.sum_stride, a.d.cols, sizeof(T));
-  return launch_kernel(rmsnorm_backward_kernel<T, kV, kMost>, dim3((unsigned)rmsnorm_parts(a.d.rows, a.d.cols)), (unsigned)l.team, 0,
-                       st, 1, a, weight_kind<T>(a.weight, a.d), pieces);
+  const int w = weight_kind<T>(a.weight, a.d), blocks = backward_blocks(a.d.rows, a.d.cols);
+  if constexpr (kMost <= 512) {
+    const Ring ring = ring_of(a.d.rows, a.d.cols, sizeof(T), a.dsum ? 3 : 2, pieces);
+    if (ring.stages > 0) {
+      static bool flags[64] = {};
+      const cudaError_t e = allow_shared(rmsnorm_backward_ring_kernel<T, kV, kMost>, flags);
+      if (e != cudaSuccess) return e;
+      return launch_kernel(rmsnorm_backward_ring_kernel<T, kV, kMost>, dim3((unsigned)blocks), (unsigned)l.team, ring.smem, st, 1, a, w,
+                           ring.stages);
+    }
+  }
+  return launch_kernel(rmsnorm_backward_kernel<T, kV, kMost>, dim3((unsigned)blocks), (unsigned)l.team, 0, st, 1, a, w, pieces);
 }
+
+Pass pass_of(const NormArgs &a) { return a.q ? kQuantized : kForward; }
+Pass pass_of(const NormBackwardArgs &) { return kBackward; }
 
 template <class T, class Args>
 cudaError_t run_type(const Args &a, cudaStream_t st) {
-  const Deal l = deal(a.d.cols);
+  const Deal l = deal(a.d.cols, pass_of(a), sizeof(T));
   if (l.most > 512) return run<T, 4, 1024>(a, l, st);
   return l.per_thread == 1 ? run<T, 1, 512>(a, l, st) : l.per_thread == 2 ? run<T, 2, 512>(a, l, st) : run<T, 4, 512>(a, l, st);
 }
@@ -345,9 +562,15 @@ cudaError_t run_any(const Args &a, cudaStream_t st) {
 
 }  // namespace
 
-int rmsnorm_parts(int rows, int cols) {
-  const int per_sm = std::max(1, std::min(8, 1024 / deal(cols).team));
-  return std::min(rows, per_sm * (int)kSms);
+int rmsnorm_parts(int rows, int cols) { return backward_blocks(rows, cols); }
+
+cudaError_t read_status_norm(int *status) {
+  cudaError_t e = cudaMemcpyFromSymbol(status, g_status_norm, sizeof(int));
+  if (e == cudaSuccess && *status != 0) {
+    const int zero = 0;
+    e = cudaMemcpyToSymbol(g_status_norm, &zero, sizeof(int));
+  }
+  return e;
 }
 
 cudaError_t launch_rmsnorm(const NormArgs &a, cudaStream_t st) { return a.d.rows == 0 ? cudaSuccess : run_any(a, st); }

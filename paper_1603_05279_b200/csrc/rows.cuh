@@ -138,6 +138,7 @@ struct NormBackwardArgs {
   xnor_norm_desc d;
 };
 cudaError_t launch_rmsnorm_backward(const NormBackwardArgs &a, cudaStream_t st);
+cudaError_t read_status_norm(int *status);
 int rmsnorm_parts(int rows, int cols);     // rows of partial sums in the workspace
 constexpr int kNormMaxCols = 32768;
 

@@ -90,8 +90,9 @@ def test_norm_of_zeros_nan_and_infinity():
 
 
 def check_quant(x, r, w, group, q, s, total):
-    """q and its scales against 64 bits: y is off by norm_error, the scale by that and a division (U), so the
-    quotient, at most `top`, by twice that of its magnitude and a division; then half a step of the output."""
+    """q and its scales against 64 bits: y is off by norm_error, the scale by that, a constant and a product (2 U); the
+    quotient by both errors, those of an approximate reciprocal (2 U) and two products (2 U), relative to its
+    magnitude; then half a step of the output."""
     h = x if r is None else (x.float() + r.float()).to(x.dtype)
     if total is not None:
         assert torch.equal(total, h)
@@ -99,14 +100,14 @@ def check_quant(x, r, w, group, q, s, total):
     top = 127.0 if q.dtype == torch.int8 else 448.0
     y = norm64(h, w)[1].view(T, -1, group or D)
     s64 = y.abs().amax(2) / top
-    e = norm_error(D) + U
+    e = norm_error(D) + 2 * U
     assert ((s.double() - s64).abs() <= e * s64).all()
     v = torch.where(s64[:, :, None] > 0, y / s64[:, :, None], 0.0)
     d = (q.float().double().view_as(v) - v).abs()
     if q.dtype == torch.int8:
-        bound = 0.5 + (2 * e + 2 * U) * v.abs()
+        bound = 0.5 + (2 * e + 4 * U) * v.abs()
     else:
-        bound = (2.0 ** -4 * v.abs()).clamp(min=2.0 ** -10) + (2 * e + 2 * U) * v.abs()      # subnormal below 2^-6
+        bound = (2.0 ** -4 * v.abs()).clamp(min=2.0 ** -10) + (2 * e + 4 * U) * v.abs()      # subnormal below 2^-6
     assert (d <= bound).all(), (d - bound).max()
 
 

@@ -27,7 +27,7 @@ def check(b):
     h = (b.x0.float() + b.residual0.float()).to(torch.bfloat16)
     assert torch.equal(b.residual, h)
     y = norm64(h, b.weight)[1]
-    e = norm_error(K) + U
+    e = norm_error(K) + 4 * U
     if b.q is None:
         assert ((b.y.double() - y).abs() <= (half_step(torch.bfloat16) + 2 * e) * y.abs() + 1e-40).all()
         x, each = b.y, 1.0
