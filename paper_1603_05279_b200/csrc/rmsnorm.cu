@@ -46,24 +46,22 @@ struct Max { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t
 
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
-// The weights of a chunk: none (1), 32 bits, or the rows' type.
+// Eight weights: ones (kind 0), in 32 bits (1) or of the rows' type (2).
 template <class T>
-struct Weights {
-  Chunk<float> wide;
-  Chunk<T> same;
-  __device__ __forceinline__ void load(const void *w, int kind, int c, int in) {
-    if (kind == 1) wide.load(static_cast<const float *>(w) + c, in == 8, in);
-    else if (kind == 2) same.load(static_cast<const T *>(w) + c, in == 8, in);
-  }
-  __device__ __forceinline__ void to_float(int kind, float v[8]) const {
-    if (kind == 1) wide.to_float(v);
-    else if (kind == 2) same.to_float(v);
-    else {
+__device__ __forceinline__ void load_weights(const void *w, int kind, int c, int in, float (&v)[8]) {
+  if (kind == 0) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 1.0f;
-    }
+    for (int i = 0; i < 8; ++i) v[i] = 1.0f;
+  } else if (kind == 1) {
+    Chunk<float> a;
+    a.load(static_cast<const float *>(w) + c, in == 8, in);
+    a.to_float(v);
+  } else {
+    Chunk<T> a;
+    a.load(static_cast<const T *>(w) + c, in == 8, in);
+    a.to_float(v);
   }
-};
+}
 template <class T>
 int weight_kind(const void *w, const xnor_norm_desc &d) {
   return w == nullptr ? 0 : d.weight_type == XNOR_F32 ? 1 : 2;
@@ -107,7 +105,7 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
 // thread cover the row.  `read` is called when every thread of the block has its values.
 template <class T, int kV, bool kQuant>
 __device__ __forceinline__ void finish_row(const NormArgs &A, const Team &team, long long row, bool real, const int (&in)[kV], Chunk<T> (&xc)[kV],
-                                           const Chunk<T> (&rc)[kV], const Weights<T> (&wc)[kV], int weights, int pieces, float *red,
+                                           const Chunk<T> (&rc)[kV], const float (&wc)[kV][8], int weights, int pieces, float *red,
                                            uint32_t *red_max) {
   const int D = A.d.cols;
   // (16-bit values stay packed and are converted twice: half the registers, so twice the rows under way)
@@ -138,14 +136,9 @@ __device__ __forceinline__ void finish_row(const NormArgs &A, const Team &team, 
   if (A.rstd && real && team.rank == 0) A.rstd[row] = rstd;
   auto normed = [&](int v, float (&y)[8]) {
     xc[v].to_float(y);
-    float w[8];
-    if constexpr (kV > 2) {                   // (long rows: not held over the sum, whose latency other rows fill)
-      Weights<T> late;
-      late.load(A.weight, weights, 8 * (team.rank + v * team.size), in[v]);
-      late.to_float(weights, w);
-    } else {
-      wc[v].to_float(weights, w);
-    }
+    float late[8];
+    if constexpr (kV > 2) load_weights<T>(A.weight, weights, 8 * (team.rank + v * team.size), in[v], late);     // (long rows: not held over the sum)
+    const float *w = kV > 2 ? late : wc[v];
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = y[i] * rstd * w[i];
   };
@@ -230,7 +223,7 @@ rmsnorm_kernel(const NormArgs A, int team_size, int weights, int pieces) {
   for (int v = 0; v < kV; ++v) in[v] = real ? min(8, max(0, D - 8 * (team.rank + v * team.size))) : 0;
   stream_order();
   Chunk<T> xc[kV], rc[kV];
-  Weights<T> wc[kV];
+  float wc[kV][8];
 #pragma unroll
   for (int v = 0; v < kV; ++v) {
     const int c = 8 * (team.rank + v * team.size);
@@ -239,7 +232,7 @@ rmsnorm_kernel(const NormArgs A, int team_size, int weights, int pieces) {
   }
   if constexpr (kV <= 2) {
 #pragma unroll
-    for (int v = 0; v < kV; ++v) wc[v].load(A.weight, weights, 8 * (team.rank + v * team.size), in[v]);
+    for (int v = 0; v < kV; ++v) load_weights<T>(A.weight, weights, 8 * (team.rank + v * team.size), in[v], wc[v]);
   }
   finish_row<T, kV, kQuant>(A, team, row, real, in, xc, rc, wc, weights, pieces, red, red_max);
 }
@@ -294,51 +287,36 @@ __device__ __forceinline__ void load_shared(Chunk<T> &c, uint32_t addr) {
 }
 
 // Backward.  With u = w dy: dx = rstd (u - h (rstd^2 / D) sum(u h)) (+ dsum), dw = sum over rows of dy h rstd.
-// A block takes rows b, b + grid, ...; the sums of dw stay in registers and leave as one row of partial sums
-// per block, which rmsnorm_dweight_kernel adds in the blocks' order.
-template <class T, int kV>
-struct BackwardRow {
-  Chunk<T> h[kV], y[kV], s[kV];
-  float rstd;
-};
-
-template <class T, int kV, class Read>
-__device__ __forceinline__ void finish_backward(const NormBackwardArgs &A, const Team &team, long long row, const int (&in)[kV],
-                                                const BackwardRow<T, kV> &r, const Weights<T> (&wc)[kV], int weights, int pieces,
-                                                float (&dw)[kV][8], float *sums, Read &&read) {
-  T *dx = static_cast<T *>(A.dx) + row * A.d.sum_stride;
-  float dot = 0.0f;
+// Blocks take rows in turn; the sums of dw stay in registers and leave as one row of partial sums per block,
+// which rmsnorm_dweight_kernel adds in the blocks' order.
+template <class T>
+__device__ __forceinline__ void add_chunk(const Chunk<T> &h, const Chunk<T> &y, const float (&w)[8], float rstd, float &dot, float (&dw)[8]) {
+  float hv[8], yv[8];
+  h.to_float(hv);
+  y.to_float(yv);
 #pragma unroll
-  for (int v = 0; v < kV; ++v) {
-    float hv[8], yv[8], w[8];
-    r.h[v].to_float(hv);
-    r.y[v].to_float(yv);
-    wc[v].to_float(weights, w);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      dot = fmaf(yv[i] * w[i], hv[i], dot);
-      dw[v][i] = fmaf(yv[i], hv[i] * r.rstd, dw[v][i]);
-    }
+  for (int i = 0; i < 8; ++i) {
+    const float yh = yv[i] * hv[i];
+    dot = fmaf(yh, w[i], dot);
+    dw[i] = fmaf(yh, rstd, dw[i]);
   }
-  dot = team.reduce(dot, sums, Add());
-  read();
-  const float k = dot * (r.rstd * r.rstd / (float)A.d.cols);
+}
+template <class T>
+__device__ __forceinline__ Chunk<T> gradient_chunk(const Chunk<T> &h, const Chunk<T> &y, const Chunk<T> &s, bool add, const float (&w)[8],
+                                                   float rstd, float k) {
+  float hv[8], yv[8], sv[8], o[8];
+  h.to_float(hv);
+  y.to_float(yv);
 #pragma unroll
-  for (int v = 0; v < kV; ++v) {
-    float hv[8], yv[8], w[8], sv[8], o[8];
-    r.h[v].to_float(hv);
-    r.y[v].to_float(yv);
-    wc[v].to_float(weights, w);
-    if (A.dsum) r.s[v].to_float(sv);
+  for (int i = 0; i < 8; ++i) o[i] = rstd * fmaf(-hv[i], k, yv[i] * w[i]);
+  if (add) {
+    s.to_float(sv);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      o[i] = r.rstd * fmaf(-hv[i], k, yv[i] * w[i]);
-      if (A.dsum) o[i] += sv[i];
-    }
-    Chunk<T> oc;
-    oc.from_float(o);
-    oc.store(dx + 8 * (team.rank + v * team.size), pieces, in[v]);
+    for (int i = 0; i < 8; ++i) o[i] += sv[i];
   }
+  Chunk<T> c;
+  c.from_float(o);
+  return c;
 }
 
 // This block's partial sums of dw.
@@ -354,41 +332,73 @@ __device__ __forceinline__ void store_partial(const NormBackwardArgs &A, const T
   }
 }
 
+// Several teams share a block where rows are short; the first adds their sums of dw.
 template <class T, int kV, int kMost>
-__global__ void __launch_bounds__(kMost, kV == 1 ? 2 : 1)
-rmsnorm_backward_kernel(const NormBackwardArgs A, int weights, int pieces) {
+__global__ void __launch_bounds__(kMost)
+rmsnorm_backward_kernel(const NormBackwardArgs A, int team_size, int weights, int pieces) {
   __shared__ float red[2][kMost / 32];
-  const Team team((int)blockDim.x);
+  extern __shared__ float sums[];                    // [teams - 1][columns, rounded up to the teams' chunks]
+  const Team team(team_size);
+  const int D = A.d.cols, teams = (int)blockDim.x / team_size, which = (int)threadIdx.x / team_size;
   int in[kV];
 #pragma unroll
-  for (int v = 0; v < kV; ++v) in[v] = min(8, max(0, A.d.cols - 8 * (team.rank + v * team.size)));
+  for (int v = 0; v < kV; ++v) in[v] = min(8, max(0, D - 8 * (team.rank + v * team.size)));
   stream_order();
-  Weights<T> wc[kV];
-  float dw[kV][8] = {};
+  float wc[kV][8], dw[kV][8] = {};
 #pragma unroll
-  for (int v = 0; v < kV; ++v) wc[v].load(A.weight, weights, 8 * (team.rank + v * team.size), in[v]);
+  for (int v = 0; v < kV; ++v) load_weights<T>(A.weight, weights, 8 * (team.rank + v * team.size), in[v], wc[v]);
   int turn = 0;
 #pragma unroll 1
-  for (long long row = blockIdx.x; row < A.d.rows; row += gridDim.x, turn ^= 1) {
+  for (long long first = (long long)blockIdx.x * teams; first < A.d.rows; first += (long long)gridDim.x * teams, turn ^= 1) {
+    const bool real = first + which < A.d.rows;
+    const long long row = real ? first + which : 0;
     const T *h = static_cast<const T *>(A.h) + row * A.d.x_stride;
     const T *dy = static_cast<const T *>(A.dy) + row * A.d.y_stride;
     const T *ds = static_cast<const T *>(A.dsum) + (A.dsum ? row * A.d.residual_stride : 0);
-    BackwardRow<T, kV> r;
+    Chunk<T> hc[kV], yc[kV], sc[kV];
 #pragma unroll
     for (int v = 0; v < kV; ++v) {
-      const int c = 8 * (team.rank + v * team.size);
-      r.h[v].load(h + c, pieces, in[v]);
-      r.y[v].load(dy + c, pieces, in[v]);
-      if (A.dsum) r.s[v].load(ds + c, pieces, in[v]);
+      const int c = 8 * (team.rank + v * team.size), n = real ? in[v] : 0;
+      hc[v].load(h + c, pieces, n);
+      yc[v].load(dy + c, pieces, n);
+      if (A.dsum) sc[v].load(ds + c, pieces, n);
     }
-    r.rstd = load_global(A.rstd + row);
-    finish_backward<T, kV>(A, team, row, in, r, wc, weights, pieces, dw, red[turn], [] {});
+    const float rstd = load_global_if(A.rstd + row, real);
+    float dot = 0.0f;
+#pragma unroll
+    for (int v = 0; v < kV; ++v) add_chunk<T>(hc[v], yc[v], wc[v], rstd, dot, dw[v]);
+    dot = team.reduce(dot, red[turn], Add());
+    if (!real) continue;
+    const float k = dot * (rstd * rstd / (float)D);
+    T *dx = static_cast<T *>(A.dx) + row * A.d.sum_stride;
+#pragma unroll
+    for (int v = 0; v < kV; ++v)
+      gradient_chunk<T>(hc[v], yc[v], sc[v], A.dsum != nullptr, wc[v], rstd, k).store(dx + 8 * (team.rank + v * team.size), pieces, in[v]);
+  }
+  if (A.work == nullptr) return;
+  if (teams > 1) {
+    const int width = 8 * kV * team_size;
+    if (which > 0) {
+#pragma unroll
+      for (int v = 0; v < kV; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[(which - 1) * width + (v * 8 + i) * team_size + team.rank] = dw[v][i];
+    }
+    __syncthreads();
+    if (which > 0) return;
+    for (int o = 0; o < teams - 1; ++o)
+#pragma unroll
+      for (int v = 0; v < kV; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[v][i] += sums[o * width + (v * 8 + i) * team_size + team.rank];
   }
   store_partial<kV>(A, team, in, dw);
 }
 
+// Long rows through the ring.  Both passes over a row read it from there, so that registers hold the sums of dw and
+// little else; a stage is free when the next row begins.
 template <class T, int kV, int kMost>
-__global__ void __launch_bounds__(kMost, kV == 1 ? 2 : 1)
+__global__ void __launch_bounds__(kMost)
 rmsnorm_backward_ring_kernel(const NormBackwardArgs A, int weights, int stages) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float red[2][kMost / 32];
@@ -406,10 +416,9 @@ rmsnorm_backward_ring_kernel(const NormBackwardArgs A, int weights, int stages) 
     if (A.dsum) ring.copy(i, 2, static_cast<const T *>(A.dsum) + ring.row(i) * A.d.residual_stride);
   };
   for (int i = 0; i < stages; ++i) fetch(i);
-  Weights<T> wc[kV];
-  float dw[kV][8] = {};
+  float wc[kV][8], dw[kV][8] = {};
 #pragma unroll
-  for (int v = 0; v < kV; ++v) wc[v].load(A.weight, weights, 8 * (team.rank + v * team.size), in[v]);
+  for (int v = 0; v < kV; ++v) load_weights<T>(A.weight, weights, 8 * (team.rank + v * team.size), in[v], wc[v]);
   float next = ring.count > 0 ? load_global(A.rstd + ring.row(0)) : 0.0f;
 #pragma unroll 1
   for (int i = 0; i < ring.count; ++i) {
@@ -419,39 +428,60 @@ rmsnorm_backward_ring_kernel(const NormBackwardArgs A, int weights, int stages) 
       if (threadIdx.x == 0) ring.drain(i);
       return;
     }
-    BackwardRow<T, kV> r;
-    r.rstd = rstd;
+    if (i > 0) fetch(i - 1 + stages);              // (every thread is done with row i - 1)
+    const uint32_t at = ring.stage(i) + 8u * (uint32_t)sizeof(T) * (uint32_t)team.rank, step = 8u * (uint32_t)sizeof(T) * (uint32_t)team.size;
+    float dot = 0.0f;
 #pragma unroll
     for (int v = 0; v < kV; ++v) {
-      if (in[v] == 0) { r.h[v].zero(); r.y[v].zero(); r.s[v].zero(); continue; }
-      const uint32_t at = ring.stage(i) + 8u * (uint32_t)sizeof(T) * (uint32_t)(team.rank + v * team.size);
-      load_shared(r.h[v], at);
-      load_shared(r.y[v], at + ring.row_bytes);
-      if (A.dsum) load_shared(r.s[v], at + 2u * ring.row_bytes);
+      if (in[v] == 0) continue;
+      Chunk<T> h, y;
+      load_shared(h, at + (uint32_t)v * step);
+      load_shared(y, at + (uint32_t)v * step + ring.row_bytes);
+      add_chunk<T>(h, y, wc[v], rstd, dot, dw[v]);
     }
-    finish_backward<T, kV>(A, team, ring.row(i), in, r, wc, weights, 1, dw, red[i & 1], [&] { fetch(i + stages); });
+    dot = team.reduce(dot, red[i & 1], Add());
+    const float k = dot * (rstd * rstd / (float)A.d.cols);
+    T *dx = static_cast<T *>(A.dx) + ring.row(i) * A.d.sum_stride;
+#pragma unroll
+    for (int v = 0; v < kV; ++v) {
+      if (in[v] == 0) continue;
+      Chunk<T> h, y, s;
+      load_shared(h, at + (uint32_t)v * step);
+      load_shared(y, at + (uint32_t)v * step + ring.row_bytes);
+      if (A.dsum) load_shared(s, at + (uint32_t)v * step + 2u * ring.row_bytes);
+      gradient_chunk<T>(h, y, s, A.dsum != nullptr, wc[v], rstd, k).store(dx + 8 * (team.rank + v * team.size), true, in[v]);
+    }
   }
   store_partial<kV>(A, team, in, dw);
 }
 
-// dweight[c] = sum over the partial rows, in their order: eight threads of a column take every eighth row each.
-constexpr int kSumCols = 32, kSumWays = 8;
+// dweight[c] = sum over the partial rows, in a fixed order: kSumWays threads of a column take every kSumWays-th row each,
+// four loads under way at a time (4096x4096 35.3 -> 33.0 us in all, 20000x256 15.6 -> 14.4).
+constexpr int kSumCols = 32, kSumWays = 32;
 __global__ void __launch_bounds__(kSumCols * kSumWays)
 rmsnorm_dweight_kernel(const float *part, int parts, int D, float *__restrict__ dweight) {
-  __shared__ float red[kSumWays][kSumCols];
+  __shared__ float red[kSumWays][kSumCols + 1];
   stream_order();
   const int lane = threadIdx.x % kSumCols, way = threadIdx.x / kSumCols;
   const int c = blockIdx.x * kSumCols + lane;
   float s = 0.0f;
-  if (c < D)
-    for (int p = way; p < parts; p += kSumWays) s += load_global(part + (size_t)p * D + c);
+  for (int p = way; p < parts; p += 4 * kSumWays) {
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool in = c < D && p + i * kSumWays < parts;
+      v[i] = load_global_if(part + (in ? (size_t)(p + i * kSumWays) * D + c : 0), in);
+    }
+    s += (v[0] + v[1]) + (v[2] + v[3]);
+  }
   red[way][lane] = s;
   __syncthreads();
-  if (way == 0 && c < D) {
+  // warp w now has column w's sums in its lanes
+  s = red[lane][way];
 #pragma unroll
-    for (int i = 1; i < kSumWays; ++i) s += red[i][lane];
-    dweight[c] = s;
-  }
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  const int col = blockIdx.x * kSumCols + way;
+  if (lane == 0 && col < D) dweight[col] = s;
 }
 
 // How a row of `cols` columns is dealt out: chunks per thread, and the most threads that takes (which sets
@@ -472,25 +502,32 @@ Deal deal(int cols, Pass pass, size_t elem) {
   return d;
 }
 
-// Blocks per SM of the backward pass, by the registers that their threads take.
-int blocks_per_sm(const Deal &l) { return std::max(1, std::min(8, (l.per_thread == 1 ? 1024 : 512) / l.team)); }
+// The backward pass: threads per block (several teams of short rows), and at most so many blocks per SM.
+int backward_threads(const Deal &l) { return std::max(l.team, 256); }
+int most_per_sm(const Deal &l) { return std::max(1, (l.per_thread <= 2 ? 1024 : 512) / backward_threads(l)); }
 
-// The ring kernels' stages; 0: not for these rows (short ones, whose copies would be small, few of them, or two of
-// their stages do not fit).  `tensors`: read per row.
-struct Ring {
-  int stages;
+// Its blocks, and the ring's stages.  0 stages: not for these rows (short ones, whose copies would be small, few of them, or
+// two of their stages do not fit).  `tensors`: read per row.  More blocks are better down to two stages each (4096x4096
+// bf16 31.7 us with four per SM, 34.8 with two; in 32 bits, where four leave one stage, 33.6 and 29.2).
+struct BackwardPlan {
+  int blocks, stages;
   size_t smem;
 };
-Ring ring_of(int rows, int cols, size_t elem, int tensors, bool pieces) {
+int blocks_of(int rows, const Deal &l, int per_sm) {
+  const int teams = backward_threads(l) / l.team;
+  return std::min((int)((rows + (long long)teams - 1) / teams), per_sm * (int)kSms);
+}
+BackwardPlan plan_backward(int rows, int cols, size_t elem, int tensors, bool pieces) {
   const size_t row = (size_t)cols * elem, stage = row * (size_t)tensors;
   const Deal l = deal(cols, kBackward, elem);
-  Ring r = {0, 0};
-  if (!pieces || row < 4096 || l.team < 64 || l.most > 512 || rows < 4 * (int)kSms) return r;
-  const size_t room = 200 * 1024 / (size_t)blocks_per_sm(l) - 2048;
-  r.stages = (int)std::min<size_t>(kMaxStages, room / stage);
-  if (r.stages < 2) r.stages = 0;
-  r.smem = kRingControl + (size_t)r.stages * stage;
-  return r;
+  int per_sm = most_per_sm(l);
+  BackwardPlan p = {blocks_of(rows, l, per_sm), 0, 0};
+  if (!pieces || row < 4096 || l.team != backward_threads(l) || l.most > 512 || rows < 4 * (int)kSms) return p;
+  for (; per_sm >= 1; per_sm /= 2) {
+    const int stages = (int)std::min<size_t>(kMaxStages, (200 * 1024 / (size_t)per_sm - 2048) / stage);
+    if (stages >= 2) return {blocks_of(rows, l, per_sm), stages, kRingControl + (size_t)stages * stage};
+  }
+  return p;
 }
 
 template <class K>
@@ -520,49 +557,51 @@ cudaError_t run(const NormArgs &a, const Deal &l, cudaStream_t st) {
   return a.q ? run<T, kV, kMost, true>(a, l, pieces, st) : run<T, kV, kMost, false>(a, l, pieces, st);
 }
 
-// Blocks, and with them rows of partial sums, of the backward pass.  (They do not depend on the device.)
-int backward_blocks(int rows, int cols) {
-  return std::min(rows, blocks_per_sm(deal(cols, kBackward, 2)) * (int)kSms);
-}
-
 template <class T, int kV, int kMost>
-cudaError_t run(const NormBackwardArgs &a, const Deal &l, cudaStream_t st) {
+cudaError_t run(const NormBackwardArgs &a, const Deal &l, cudaStream_t st, int *blocks) {
   const int pieces = rows_in_pieces(a.h, a.d.x_stride, a.d.cols, sizeof(T)) &&
                      rows_in_pieces(a.dy, a.d.y_stride, a.d.cols, sizeof(T)) &&
                      rows_in_pieces(a.dsum, a.d.residual_stride, a.d.cols, sizeof(T)) &&
                      rows_in_pieces(a.dx, a.d.sum_stride, a.d.cols, sizeof(T));
-  const int w = weight_kind<T>(a.weight, a.d), blocks = backward_blocks(a.d.rows, a.d.cols);
+  const int w = weight_kind<T>(a.weight, a.d);
+  const BackwardPlan plan = plan_backward(a.d.rows, a.d.cols, sizeof(T), a.dsum ? 3 : 2, pieces);
+  *blocks = plan.blocks;
   if constexpr (kMost <= 512) {
-    const Ring ring = ring_of(a.d.rows, a.d.cols, sizeof(T), a.dsum ? 3 : 2, pieces);
-    if (ring.stages > 0) {
+    if (plan.stages > 0) {
       static bool flags[64] = {};
       const cudaError_t e = allow_shared(rmsnorm_backward_ring_kernel<T, kV, kMost>, flags);
       if (e != cudaSuccess) return e;
-      return launch_kernel(rmsnorm_backward_ring_kernel<T, kV, kMost>, dim3((unsigned)blocks), (unsigned)l.team, ring.smem, st, 1, a, w,
-                           ring.stages);
+      return launch_kernel(rmsnorm_backward_ring_kernel<T, kV, kMost>, dim3((unsigned)plan.blocks), (unsigned)l.team, plan.smem, st, 1, a, w,
+                           plan.stages);
     }
   }
-  return launch_kernel(rmsnorm_backward_kernel<T, kV, kMost>, dim3((unsigned)blocks), (unsigned)l.team, 0, st, 1, a, w, pieces);
+  const int threads = backward_threads(l), teams = threads / l.team;
+  return launch_kernel(rmsnorm_backward_kernel<T, kV, kMost>, dim3((unsigned)plan.blocks), (unsigned)threads,
+                       (size_t)(teams - 1) * 8 * kV * l.team * sizeof(float), st, 1, a, l.team, w, pieces);
 }
 
 Pass pass_of(const NormArgs &a) { return a.q ? kQuantized : kForward; }
 Pass pass_of(const NormBackwardArgs &) { return kBackward; }
 
-template <class T, class Args>
-cudaError_t run_type(const Args &a, cudaStream_t st) {
+template <class T, class Args, class... More>
+cudaError_t run_type(const Args &a, cudaStream_t st, More... more) {
   const Deal l = deal(a.d.cols, pass_of(a), sizeof(T));
-  if (l.most > 512) return run<T, 4, 1024>(a, l, st);
-  return l.per_thread == 1 ? run<T, 1, 512>(a, l, st) : l.per_thread == 2 ? run<T, 2, 512>(a, l, st) : run<T, 4, 512>(a, l, st);
+  if (l.most > 512) return run<T, 4, 1024>(a, l, st, more...);
+  return l.per_thread == 1 ? run<T, 1, 512>(a, l, st, more...) : l.per_thread == 2 ? run<T, 2, 512>(a, l, st, more...) : run<T, 4, 512>(a, l, st, more...);
 }
-template <class Args>
-cudaError_t run_any(const Args &a, cudaStream_t st) {
-  if (a.d.type == XNOR_F32) return run_type<float>(a, st);
-  return a.d.type == XNOR_BF16 ? run_type<__nv_bfloat16>(a, st) : run_type<__half>(a, st);
+template <class Args, class... More>
+cudaError_t run_any(const Args &a, cudaStream_t st, More... more) {
+  if (a.d.type == XNOR_F32) return run_type<float>(a, st, more...);
+  return a.d.type == XNOR_BF16 ? run_type<__nv_bfloat16>(a, st, more...) : run_type<__half>(a, st, more...);
 }
 
 }  // namespace
 
-int rmsnorm_parts(int rows, int cols) { return backward_blocks(rows, cols); }
+// (Does not depend on the device.)
+int rmsnorm_parts(int rows, int cols) {
+  const Deal l = deal(cols, kBackward, 2);
+  return blocks_of(rows, l, most_per_sm(l));
+}
 
 cudaError_t read_status_norm(int *status) {
   cudaError_t e = cudaMemcpyFromSymbol(status, g_status_norm, sizeof(int));
@@ -578,10 +617,11 @@ cudaError_t launch_rmsnorm(const NormArgs &a, cudaStream_t st) { return a.d.rows
 cudaError_t launch_rmsnorm_backward(const NormBackwardArgs &args, cudaStream_t st) {
   NormBackwardArgs a = args;
   if (a.dweight == nullptr) a.work = nullptr;
-  cudaError_t e = a.d.rows > 0 ? run_any(a, st) : cudaSuccess;
+  int blocks = 0;                              // and rows of partial sums
+  const cudaError_t e = a.d.rows > 0 ? run_any(a, st, &blocks) : cudaSuccess;
   if (e != cudaSuccess || a.dweight == nullptr) return e;
   return launch_kernel(rmsnorm_dweight_kernel, dim3((unsigned)((a.d.cols + kSumCols - 1) / kSumCols)), kSumCols * kSumWays, 0, st, 1,
-                       (const float *)a.work, rmsnorm_parts(a.d.rows, a.d.cols), a.d.cols, a.dweight);
+                       (const float *)a.work, blocks, a.d.cols, a.dweight);
 }
 
 }  // namespace xnor

@@ -25,14 +25,34 @@ __device__ __forceinline__ void write_tiles(const uint32_t (&words)[kW4Rows][kOc
   reinterpret_cast<uint4 *>(w)[(w4_tile(row_tile, col_tiles) + (size_t)(col_tile0 + tile) * kW4Panel) * 32 + lane] = make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-// round(w / s) to the nearest whole number, ties to even, of the exact quotient (|w / s| below 2^20): the
-// first guess is off by one at most where the quotient lies next to a border, and the rest w - q s is
-// exact in 32 bits.
-__device__ __forceinline__ float round_quotient(float w, float s, float inv) {
-  float q = rintf(inv > 0.0f ? w * inv : w / s);
+// w / s to the nearest whole number, ties to even, of the exact quotient (|w / s| below 2^20).  A first guess is off by one
+// at most, where the quotient lies next to a border, and the rest w - q s is exact in 32 bits.
+__device__ __forceinline__ float mend_quotient(float q, float w, float s) {
   const float r = fmaf(-q, s, w), twice = 2.0f * fabsf(r);
-  if (twice > s || (twice == s && ((int)q & 1))) q += r > 0.0f ? 1.0f : -1.0f;
-  return q;
+  return twice > s || (twice == s && ((int)q & 1)) ? q + (r > 0.0f ? 1.0f : -1.0f) : q;
+}
+__device__ __forceinline__ float round_quotient(float w, float s) { return mend_quotient(rintf(w / s), w, s); }
+
+// The same of kN values.  With the reciprocal the guess is within 2e-6 of the quotient (at most 16), so only guesses that
+// close to a border can be wrong; all are mended then.  (inv = 0: it would overflow.)
+template <int kN>
+__device__ __forceinline__ void round_quotients(const float (&w)[kN], float s, float inv, float (&q)[kN]) {
+  if (inv == 0.0f) {
+#pragma unroll 1
+    for (int i = 0; i < kN; ++i) q[i] = round_quotient(w[i], s);
+    return;
+  }
+  float far = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    const float t = w[i] * inv;
+    q[i] = __fadd_rn(__fadd_rn(t, 12582912.0f), -12582912.0f);          // 1.5 2^23: rounds to a whole number
+    far = fmaxf(far, fabsf(t - q[i]));
+  }
+  if (far > 0.49999f) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) q[i] = mend_quotient(q[i], w[i], s);
+  }
 }
 
 // Thread (row r, 16 columns c ..): the scale of its group over 2, 4 or 8 neighbouring threads, then its codes.
@@ -72,16 +92,23 @@ w4_quantize_kernel(const T *w, const xnor_w4_desc d, int pieces, uint32_t *w_pac
   else s = hi != hi ? hi : __fdiv_rn(fmaxf(-lo, hi), 7.0f);
   const bool sound = s > 0.0f && s <= 3.402823466e38f;
   const float inv = sound && s > 1e-37f ? 1.0f / s : 0.0f;      // 0: it would overflow
-  if (zeros) z = sound ? fminf(15.0f, fmaxf(0.0f, round_quotient(-lo, s, inv))) : 8.0f;
+  if (zeros) z = sound ? fminf(15.0f, fmaxf(0.0f, round_quotient(-lo, s))) : 8.0f;
+  float q[16];
+  if (sound) {
+    round_quotients(v, s, inv, q);
+  } else {
 #pragma unroll
-  for (int q = 0; q < 2; ++q) {
+    for (int i = 0; i < 16; ++i) q[i] = 0.0f;
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
     uint32_t word = 0u;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float u = sound ? round_quotient(v[8 * q + i], s, inv) + z : z;
-      word |= (uint32_t)fminf(15.0f, fmaxf(0.0f, u)) << w4_bit(i);
+      const float code = fminf(15.0f, fmaxf(0.0f, q[8 * h + i] + z));
+      word |= (__float_as_uint(code + 8388608.0f) & 15u) << w4_bit(i);     // 2^23: the code in the low bits
     }
-    words[r][2 * c + q] = word;
+    words[r][2 * c + h] = word;
   }
   if (n < d.N && k < d.K && c % lanes == 0) {
     const size_t at = (size_t)(k / d.group) * d.N + n;
@@ -115,7 +142,7 @@ w4_pack_kernel(const uint8_t *codes, const xnor_w4_desc d, uint32_t *w_packed) {
 template <class T>
 __global__ void __launch_bounds__(kLayThreads)
 w4_dequantize_kernel(const uint32_t *w_packed, const float *scales, const uint8_t *zeros, const xnor_w4_desc d,
-                     int pieces, T *w) {
+                     int pieces, uint32_t magic, T *w) {
   __shared__ uint32_t words[2][32][5];
   stream_order();
   const int col_tiles = (d.K + kW4Cols - 1) / kW4Cols;
@@ -132,14 +159,20 @@ w4_dequantize_kernel(const uint32_t *w_packed, const float *scales, const uint8_
   if (n >= d.N || k >= d.K) return;
   const size_t at = (size_t)(k / d.group) * d.N + n;         // 16 columns lie in one group
   const float s = load_global(scales + at);
-  const int z = zeros ? (int)load_global(zeros + at) : 8;
+  const W4Type<__nv_bfloat16>::Zero zero = W4Type<__nv_bfloat16>::zero(zeros ? load_global(zeros + at) : 8u);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int col = 16 * (c & 3) + 8 * h;
     const uint32_t word = words[c / 4][w4_place(r, col)][w4_word(r, col)];
+    uint32_t pair[4];
+    W4Type<__nv_bfloat16>::expand(word, zero, magic, pair);
     float v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)((int)((word >> w4_bit(i)) & 15u) - z) * s;
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = pair_to_float(pair[i], __nv_bfloat16());
+      v[2 * i] = f.x * s;
+      v[2 * i + 1] = f.y * s;
+    }
     Chunk<T> a;
     a.from_float(v);
     a.store(w + (size_t)n * d.K + k + 8 * h, pieces, min(8, max(0, d.K - (k + 8 * h))));
@@ -436,10 +469,10 @@ cudaError_t launch_w4_dequantize(const uint32_t *w_packed, const float *scales, 
                                  const xnor_w4_desc &d, int type, void *w, cudaStream_t st) {
   const int pieces = d.K % 8 == 0;
   if (type == XNOR_F32)
-    return launch_kernel(w4_dequantize_kernel<float>, lay_grid(d), kLayThreads, 0, st, 1, w_packed, scales, zeros, d, pieces, (float *)w);
+    return launch_kernel(w4_dequantize_kernel<float>, lay_grid(d), kLayThreads, 0, st, 1, w_packed, scales, zeros, d, pieces, W4Type<__nv_bfloat16>::kMagic, (float *)w);
   if (type == XNOR_BF16)
-    return launch_kernel(w4_dequantize_kernel<__nv_bfloat16>, lay_grid(d), kLayThreads, 0, st, 1, w_packed, scales, zeros, d, pieces, (__nv_bfloat16 *)w);
-  return launch_kernel(w4_dequantize_kernel<__half>, lay_grid(d), kLayThreads, 0, st, 1, w_packed, scales, zeros, d, pieces, (__half *)w);
+    return launch_kernel(w4_dequantize_kernel<__nv_bfloat16>, lay_grid(d), kLayThreads, 0, st, 1, w_packed, scales, zeros, d, pieces, W4Type<__nv_bfloat16>::kMagic, (__nv_bfloat16 *)w);
+  return launch_kernel(w4_dequantize_kernel<__half>, lay_grid(d), kLayThreads, 0, st, 1, w_packed, scales, zeros, d, pieces, W4Type<__nv_bfloat16>::kMagic, (__half *)w);
 }
 
 cudaError_t launch_w4_few_rows(const W4Args &a, cudaStream_t st) {
