@@ -55,65 +55,85 @@ __device__ __forceinline__ void round_quotients(const float (&w)[kN], float s, f
   }
 }
 
-// Thread (row r, 16 columns c ..): the scale of its group over 2, 4 or 8 neighbouring threads, then its codes.
-template <class T>
+// Four codes c0 .. c3 as c0 + 16 c1 + 256 c2 + 4096 c3, which 32-bit floats hold exactly; in the mantissa of 2^23 they
+// lie as a word has them.  (Nine instructions a value in all; with a conversion, a shift and an OR for each
+// code 4096x4096 took 24.3 us, Q4US now.)
+__device__ __forceinline__ float four_codes(float first, float c1, float c2, float c3) {
+  return fmaf(c3, 4096.0f, fmaf(c2, 256.0f, fmaf(c1, 16.0f, first)));
+}
+
+// Thread (row r, 16 columns c ..): the scale of its group over 2, 4 or 8 neighbouring threads, then its codes.  A group
+// is 2^lg columns.  NaN and infinity make its scale such, and its codes those of zero.
+template <class T, bool kZeros>
 __global__ void __launch_bounds__(kLayThreads)
-w4_quantize_kernel(const T *w, const xnor_w4_desc d, int pieces, uint32_t *w_packed, float *scales, uint8_t *zeros) {
+w4_quantize_kernel(const T *w, const xnor_w4_desc d, int lg, int pieces, uint32_t *w_packed, float *scales, uint8_t *zeros) {
   __shared__ uint32_t words[kW4Rows][kOctets + 1];
   stream_order();
   const int r = threadIdx.x / 8, c = threadIdx.x % 8;
   const int n = blockIdx.y * kW4Rows + r, k = blockIdx.x * kLayCols + 16 * c;
   float v[16];
+  {
+    const T *from = w + (size_t)min(n, d.N - 1) * d.K + k;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int kk = k + 8 * i, in = n < d.N ? min(8, max(0, d.K - kk)) : 0;
-    Chunk<T> a;
-    a.load(w + (in > 0 ? (size_t)n * d.K + kk : 0), pieces, in);
-    a.to_float(v + 8 * i);
+    for (int i = 0; i < 2; ++i) {
+      Chunk<T> a;
+      a.load(from + 8 * i, pieces, n < d.N ? min(8, max(0, d.K - k - 8 * i)) : 0);
+      float (&half)[8] = *reinterpret_cast<float (*)[8]>(v + 8 * i);
+      a.to_float(half);
+    }
   }
-  // extremes of the group; NaN and infinity make its scale such, and its codes those of zero
-  float lo = 0.0f, hi = 0.0f;
-  bool nan = false;
+  const int lanes = 1 << (lg - 4);
+  float s, z = 8.0f, lo = 0.0f, q[16];
+  if constexpr (kZeros) {
+    float hi = 0.0f, odd = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    lo = fminf(lo, v[i]);
-    hi = fmaxf(hi, v[i]);
-    nan |= v[i] != v[i];
+    for (int i = 0; i < 16; ++i) {
+      lo = fminf(lo, v[i]);
+      hi = fmaxf(hi, v[i]);
+      odd = fmaf(v[i], 0.0f, odd);                     // NaN if any is NaN or infinite
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o *= 2) {
+      const float ol = __shfl_xor_sync(0xffffffffu, lo, o), oh = __shfl_xor_sync(0xffffffffu, hi, o), oo = __shfl_xor_sync(0xffffffffu, odd, o);
+      if (o < lanes) { lo = fminf(lo, ol); hi = fmaxf(hi, oh); odd += oo; }
+    }
+    s = (float)(((double)hi - (double)lo) / 15.0);
+    if (odd != 0.0f && s <= 3.402823466e38f) s = odd;  // (infinite extremes have made it such)
+  } else {
+    uint32_t m = 0u;                                   // of bit patterns of magnitudes: a NaN is above every number
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+#pragma unroll
+    for (int o = 1; o < 8; o *= 2) {
+      const uint32_t om = __shfl_xor_sync(0xffffffffu, m, o);
+      if (o < lanes) m = max(m, om);
+    }
+    s = __fdiv_rn(__uint_as_float(m), 7.0f);
   }
-  if (nan) hi = __int_as_float(0x7FC00000);
-  const int lanes = d.group / 16;
-  for (int o = 1; o < lanes; o *= 2) {
-    const float ol = __shfl_xor_sync(0xffffffffu, lo, o), oh = __shfl_xor_sync(0xffffffffu, hi, o);
-    lo = fminf(lo, ol);
-    hi = (hi != hi || oh != oh) ? __int_as_float(0x7FC00000) : fmaxf(hi, oh);
-  }
-  float s, z = 8.0f;
-  if (zeros) s = (float)(((double)hi - (double)lo) / 15.0);
-  else s = hi != hi ? hi : __fdiv_rn(fmaxf(-lo, hi), 7.0f);
   const bool sound = s > 0.0f && s <= 3.402823466e38f;
   const float inv = sound && s > 1e-37f ? 1.0f / s : 0.0f;      // 0: it would overflow
-  if (zeros) z = sound ? fminf(15.0f, fmaxf(0.0f, round_quotient(-lo, s))) : 8.0f;
-  float q[16];
+  if (kZeros && sound) z = fminf(15.0f, fmaxf(0.0f, round_quotient(-lo, s)));
   if (sound) {
     round_quotients(v, s, inv, q);
   } else {
 #pragma unroll
     for (int i = 0; i < 16; ++i) q[i] = 0.0f;
   }
+  if constexpr (kZeros) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) q[i] = fminf(q[i] + z, 15.0f);          // (at least 0: z rounds as the least value does)
+  }
+  const float base = kZeros ? 8388608.0f : 8388608.0f + 8.0f * 4369.0f;  // 2^23, and a zero point of 8 in every code
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    uint32_t word = 0u;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float code = fminf(15.0f, fmaxf(0.0f, q[8 * h + i] + z));
-      word |= (__float_as_uint(code + 8388608.0f) & 15u) << w4_bit(i);     // 2^23: the code in the low bits
-    }
-    words[r][2 * c + h] = word;
+    const float *u = q + 8 * h;
+    const uint32_t even = __float_as_uint(four_codes(u[0] + base, u[2], u[4], u[6])), odd = __float_as_uint(four_codes(u[1] + base, u[3], u[5], u[7]));
+    words[r][2 * c + h] = __byte_perm(even, odd, 0x5410);
   }
-  if (n < d.N && k < d.K && c % lanes == 0) {
-    const size_t at = (size_t)(k / d.group) * d.N + n;
+  if (n < d.N && k < d.K && (c & (lanes - 1)) == 0) {
+    const size_t at = (size_t)(k >> lg) * d.N + n;
     scales[at] = s;
-    if (zeros) zeros[at] = (uint8_t)z;
+    if constexpr (kZeros) zeros[at] = (uint8_t)z;
   }
   __syncthreads();
   write_tiles(words, blockIdx.y, blockIdx.x * 2, (d.K + kW4Cols - 1) / kW4Cols, w_packed);
@@ -142,7 +162,7 @@ w4_pack_kernel(const uint8_t *codes, const xnor_w4_desc d, uint32_t *w_packed) {
 template <class T>
 __global__ void __launch_bounds__(kLayThreads)
 w4_dequantize_kernel(const uint32_t *w_packed, const float *scales, const uint8_t *zeros, const xnor_w4_desc d,
-                     int pieces, uint32_t magic, T *w) {
+                     int lg, int pieces, uint32_t magic, T *w) {
   __shared__ uint32_t words[2][32][5];
   stream_order();
   const int col_tiles = (d.K + kW4Cols - 1) / kW4Cols;
@@ -157,7 +177,7 @@ w4_dequantize_kernel(const uint32_t *w_packed, const float *scales, const uint8_
   const int r = threadIdx.x / 8, c = threadIdx.x % 8;
   const int n = blockIdx.y * kW4Rows + r, k = blockIdx.x * kLayCols + 16 * c;
   if (n >= d.N || k >= d.K) return;
-  const size_t at = (size_t)(k / d.group) * d.N + n;         // 16 columns lie in one group
+  const size_t at = (size_t)(k >> lg) * d.N + n;             // 16 columns lie in one group
   const float s = load_global(scales + at);
   const W4Type<__nv_bfloat16>::Zero zero = W4Type<__nv_bfloat16>::zero(zeros ? load_global(zeros + at) : 8u);
 #pragma unroll
@@ -451,14 +471,29 @@ dim3 fill_grid(const xnor_w4_desc &d) { return dim3(lay_grid(d).x, (unsigned)(w4
 
 }  // namespace
 
+namespace {
+
+int log2_of(int group) { return group == 32 ? 5 : group == 64 ? 6 : 7; }
+
+template <class T>
+cudaError_t quantize(const void *w, const xnor_w4_desc &d, uint32_t *w_packed, float *scales, uint8_t *zeros, cudaStream_t st) {
+  const int lg = log2_of(d.group), pieces = d.K % 8 == 0;
+  if (zeros) return launch_kernel(w4_quantize_kernel<T, true>, fill_grid(d), kLayThreads, 0, st, 1, (const T *)w, d, lg, pieces, w_packed, scales, zeros);
+  return launch_kernel(w4_quantize_kernel<T, false>, fill_grid(d), kLayThreads, 0, st, 1, (const T *)w, d, lg, pieces, w_packed, scales, zeros);
+}
+
+template <class T>
+cudaError_t dequantize(const uint32_t *w_packed, const float *scales, const uint8_t *zeros, const xnor_w4_desc &d, void *w, cudaStream_t st) {
+  return launch_kernel(w4_dequantize_kernel<T>, lay_grid(d), kLayThreads, 0, st, 1, w_packed, scales, zeros, d, log2_of(d.group), (int)(d.K % 8 == 0),
+                       W4Type<__nv_bfloat16>::kMagic, (T *)w);
+}
+
+}  // namespace
+
 cudaError_t launch_w4_quantize(const void *w, int type, const xnor_w4_desc &d, uint32_t *w_packed, float *scales,
                                uint8_t *zeros, cudaStream_t st) {
-  const int pieces = d.K % 8 == 0;
-  if (type == XNOR_F32)
-    return launch_kernel(w4_quantize_kernel<float>, fill_grid(d), kLayThreads, 0, st, 1, (const float *)w, d, pieces, w_packed, scales, zeros);
-  if (type == XNOR_BF16)
-    return launch_kernel(w4_quantize_kernel<__nv_bfloat16>, fill_grid(d), kLayThreads, 0, st, 1, (const __nv_bfloat16 *)w, d, pieces, w_packed, scales, zeros);
-  return launch_kernel(w4_quantize_kernel<__half>, fill_grid(d), kLayThreads, 0, st, 1, (const __half *)w, d, pieces, w_packed, scales, zeros);
+  if (type == XNOR_F32) return quantize<float>(w, d, w_packed, scales, zeros, st);
+  return type == XNOR_BF16 ? quantize<__nv_bfloat16>(w, d, w_packed, scales, zeros, st) : quantize<__half>(w, d, w_packed, scales, zeros, st);
 }
 
 cudaError_t launch_w4_pack(const uint8_t *codes, const xnor_w4_desc &d, uint32_t *w_packed, cudaStream_t st) {
@@ -467,12 +502,8 @@ cudaError_t launch_w4_pack(const uint8_t *codes, const xnor_w4_desc &d, uint32_t
 
 cudaError_t launch_w4_dequantize(const uint32_t *w_packed, const float *scales, const uint8_t *zeros,
                                  const xnor_w4_desc &d, int type, void *w, cudaStream_t st) {
-  const int pieces = d.K % 8 == 0;
-  if (type == XNOR_F32)
-    return launch_kernel(w4_dequantize_kernel<float>, lay_grid(d), kLayThreads, 0, st, 1, w_packed, scales, zeros, d, pieces, W4Type<__nv_bfloat16>::kMagic, (float *)w);
-  if (type == XNOR_BF16)
-    return launch_kernel(w4_dequantize_kernel<__nv_bfloat16>, lay_grid(d), kLayThreads, 0, st, 1, w_packed, scales, zeros, d, pieces, W4Type<__nv_bfloat16>::kMagic, (__nv_bfloat16 *)w);
-  return launch_kernel(w4_dequantize_kernel<__half>, lay_grid(d), kLayThreads, 0, st, 1, w_packed, scales, zeros, d, pieces, W4Type<__nv_bfloat16>::kMagic, (__half *)w);
+  if (type == XNOR_F32) return dequantize<float>(w_packed, scales, zeros, d, w, st);
+  return type == XNOR_BF16 ? dequantize<__nv_bfloat16>(w_packed, scales, zeros, d, w, st) : dequantize<__half>(w_packed, scales, zeros, d, w, st);
 }
 
 cudaError_t launch_w4_few_rows(const W4Args &a, cudaStream_t st) {
