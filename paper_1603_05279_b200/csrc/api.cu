@@ -551,7 +551,7 @@ xnor_status xnor_w4_matmul(const void *x, const float *x_scales, const uint32_t 
   if (large_w4(d) || r->rows > 16 * 65535 || r->x_type == XNOR_F32 || (bytes && r->x_group != 0 && r->x_group != d->group))
     return XNOR_ERR_UNSUPPORTED;
   const xnor::W4Args a = {x, x_scales, w_packed, scales, zeros, out, *d, *r};
-  return from_cuda(r->rows <= xnor::kW4FewRows ? xnor::launch_w4_few_rows(a, (cudaStream_t)cuda_stream)
+  return from_cuda(xnor::w4_few_rows(*d, r->rows) ? xnor::launch_w4_few_rows(a, (cudaStream_t)cuda_stream)
                                                : xnor::launch_w4_many_rows(a, (cudaStream_t)cuda_stream));
 }
 

@@ -166,6 +166,9 @@ struct W4Args {
 cudaError_t launch_w4_few_rows(const W4Args &a, cudaStream_t st);
 cudaError_t launch_w4_many_rows(const W4Args &a, cudaStream_t st);
 cudaError_t read_status_w4(int *status);   // of the kernel for many rows, as the others'
-constexpr int kW4FewRows = 8;              // up to here the kernel for few rows
+// Which kernel: up to 8 rows the one for few rows is never slower (8 rows times 16384x4096 12.0 us, 15.9 in the other); 9 to
+// 16 take it two passes' worth of registers, which pays for matrices that take a few microseconds only (12 rows times
+// 4096x4096 6.9 against 8.9, times 8192x4096 12.3 against 11.3).
+inline bool w4_few_rows(const xnor_w4_desc &d, int rows) { return rows <= 8 || (rows <= 16 && (long long)d.N * d.K <= 24ll << 20); }
 
 }  // namespace xnor

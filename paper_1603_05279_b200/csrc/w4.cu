@@ -11,18 +11,21 @@ namespace xnor {
 namespace {
 
 // ---- layout -------------------------------------------------------------------------------
-constexpr int kLayThreads = 128;
-constexpr int kLayCols = 2 * kW4Cols;      // a block: 16 rows x 128 columns, the largest group; a thread: 16 columns
-constexpr int kOctets = kLayCols / 8;
+// A block: 16 rows x 256 columns, two steps of 128 columns (the largest group) whose loads are under way together; a
+// thread: 16 columns of a row in each.
+constexpr int kLayThreads = 128, kLaySteps = 2;
+constexpr int kStepCols = 2 * kW4Cols, kLayCols = kLaySteps * kStepCols;
+constexpr int kOctets = kStepCols / 8;
+using LayWords = uint32_t[kLaySteps][kW4Rows][kOctets + 1];     // [steps][rows][groups of eight columns]
 
-// Words of the block, [16 rows][groups of eight columns], to the packed tiles.
-__device__ __forceinline__ void write_tiles(const uint32_t (&words)[kW4Rows][kOctets + 1], int row_tile, int col_tile0,
-                                            int col_tiles, uint32_t *w) {
+// Words of the block to the packed tiles: a warp, a tile.
+__device__ __forceinline__ void write_tiles(const LayWords &words, int row_tile, int col_tile0, int col_tiles, uint32_t *w) {
   const int tile = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  if (tile >= 2 || col_tile0 + tile >= col_tiles) return;
-  const int c = 8 * tile + (t ^ ((g >> 1) & 3));            // this place's columns
-  const uint32_t v[4] = {words[g][c], words[g][c + 4], words[g + 8][c], words[g + 8][c + 4]};
-  reinterpret_cast<uint4 *>(w)[(w4_tile(row_tile, col_tiles) + (size_t)(col_tile0 + tile) * kW4Panel) * 32 + lane] = make_uint4(v[0], v[1], v[2], v[3]);
+  if (col_tile0 + tile >= col_tiles) return;
+  const uint32_t (&s)[kW4Rows][kOctets + 1] = words[tile / 2];
+  const int c = 8 * (tile & 1) + (t ^ ((g >> 1) & 3));      // this place's columns
+  reinterpret_cast<uint4 *>(w)[(w4_tile(row_tile, col_tiles) + (size_t)(col_tile0 + tile) * kW4Panel) * 32 + lane] =
+      make_uint4(s[g][c], s[g][c + 4], s[g + 8][c], s[g + 8][c + 4]);
 }
 
 // w / s to the nearest whole number, ties to even, of the exact quotient (|w / s| below 2^20).  A first guess is off by one
@@ -56,8 +59,9 @@ __device__ __forceinline__ void round_quotients(const float (&w)[kN], float s, f
 }
 
 // Four codes c0 .. c3 as c0 + 16 c1 + 256 c2 + 4096 c3, which 32-bit floats hold exactly; in the mantissa of 2^23 they
-// lie as a word has them.  (Nine instructions a value in all; with a conversion, a shift and an OR for each
-// code 4096x4096 took 24.3 us, Q4US now.)
+// lie as a word has them.  (With a conversion, a shift and an OR for each code 4096x4096 bf16 took
+// 24.3 us, 18 to 20 so; what is left is instructions too, 26 a value, a third of them where quotients lie next to
+// borders, as those of bf16 weights often do.)
 __device__ __forceinline__ float four_codes(float first, float c1, float c2, float c3) {
   return fmaf(c3, 4096.0f, fmaf(c2, 256.0f, fmaf(c1, 16.0f, first)));
 }
@@ -67,135 +71,163 @@ __device__ __forceinline__ float four_codes(float first, float c1, float c2, flo
 template <class T, bool kZeros>
 __global__ void __launch_bounds__(kLayThreads)
 w4_quantize_kernel(const T *w, const xnor_w4_desc d, int lg, int pieces, uint32_t *w_packed, float *scales, uint8_t *zeros) {
-  __shared__ uint32_t words[kW4Rows][kOctets + 1];
+  __shared__ LayWords words;
   stream_order();
   const int r = threadIdx.x / 8, c = threadIdx.x % 8;
-  const int n = blockIdx.y * kW4Rows + r, k = blockIdx.x * kLayCols + 16 * c;
-  float v[16];
+  const int n = blockIdx.y * kW4Rows + r;
+  Chunk<T> in[kLaySteps][2];
   {
-    const T *from = w + (size_t)min(n, d.N - 1) * d.K + k;
+    const T *from = w + (size_t)min(n, d.N - 1) * d.K;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      Chunk<T> a;
-      a.load(from + 8 * i, pieces, n < d.N ? min(8, max(0, d.K - k - 8 * i)) : 0);
-      float (&half)[8] = *reinterpret_cast<float (*)[8]>(v + 8 * i);
-      a.to_float(half);
+    for (int step = 0; step < kLaySteps; ++step)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int k = blockIdx.x * kLayCols + step * kStepCols + 16 * c + 8 * i;
+        in[step][i].load(from + k, pieces, n < d.N ? min(8, max(0, d.K - k)) : 0);
+      }
+  }
+#pragma unroll
+  for (int step = 0; step < kLaySteps; ++step) {
+    const int k = blockIdx.x * kLayCols + step * kStepCols + 16 * c;
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) in[step][i].to_float(*reinterpret_cast<float (*)[8]>(v + 8 * i));
+    const int lanes = 1 << (lg - 4);
+    float s, z = 8.0f, lo = 0.0f, q[16];
+    if constexpr (kZeros) {
+      float hi = 0.0f, odd = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        lo = fminf(lo, v[i]);
+        hi = fmaxf(hi, v[i]);
+        odd = fmaf(v[i], 0.0f, odd);                     // NaN if any is NaN or infinite
+      }
+#pragma unroll
+      for (int o = 1; o < 8; o *= 2) {
+        const float ol = __shfl_xor_sync(0xffffffffu, lo, o), oh = __shfl_xor_sync(0xffffffffu, hi, o), oo = __shfl_xor_sync(0xffffffffu, odd, o);
+        if (o < lanes) { lo = fminf(lo, ol); hi = fmaxf(hi, oh); odd += oo; }
+      }
+      s = (float)(((double)hi - (double)lo) / 15.0);
+      if (odd != 0.0f && s <= 3.402823466e38f) s = odd;  // (infinite extremes have made it such)
+    } else {
+      uint32_t m = 0u;                                   // of bit patterns of magnitudes: a NaN is above every number
+#pragma unroll
+      for (int i = 0; i < 16; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+#pragma unroll
+      for (int o = 1; o < 8; o *= 2) {
+        const uint32_t om = __shfl_xor_sync(0xffffffffu, m, o);
+        if (o < lanes) m = max(m, om);
+      }
+      s = __fdiv_rn(__uint_as_float(m), 7.0f);
     }
-  }
-  const int lanes = 1 << (lg - 4);
-  float s, z = 8.0f, lo = 0.0f, q[16];
-  if constexpr (kZeros) {
-    float hi = 0.0f, odd = 0.0f;
+    const bool sound = s > 0.0f && s <= 3.402823466e38f;
+    const float inv = sound && s > 1e-37f ? 1.0f / s : 0.0f;      // 0: it would overflow
+    if (kZeros && sound) z = fminf(15.0f, fmaxf(0.0f, round_quotient(-lo, s)));
+    if (sound) {
+      round_quotients(v, s, inv, q);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      lo = fminf(lo, v[i]);
-      hi = fmaxf(hi, v[i]);
-      odd = fmaf(v[i], 0.0f, odd);                     // NaN if any is NaN or infinite
+      for (int i = 0; i < 16; ++i) q[i] = 0.0f;
     }
+    if constexpr (kZeros) {
 #pragma unroll
-    for (int o = 1; o < 8; o *= 2) {
-      const float ol = __shfl_xor_sync(0xffffffffu, lo, o), oh = __shfl_xor_sync(0xffffffffu, hi, o), oo = __shfl_xor_sync(0xffffffffu, odd, o);
-      if (o < lanes) { lo = fminf(lo, ol); hi = fmaxf(hi, oh); odd += oo; }
+      for (int i = 0; i < 16; ++i) q[i] = fminf(q[i] + z, 15.0f);          // (at least 0: z rounds as the least value does)
     }
-    s = (float)(((double)hi - (double)lo) / 15.0);
-    if (odd != 0.0f && s <= 3.402823466e38f) s = odd;  // (infinite extremes have made it such)
-  } else {
-    uint32_t m = 0u;                                   // of bit patterns of magnitudes: a NaN is above every number
+    const float base = kZeros ? 8388608.0f : 8388608.0f + 8.0f * 4369.0f;  // 2^23, and a zero point of 8 in every code
 #pragma unroll
-    for (int i = 0; i < 16; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-#pragma unroll
-    for (int o = 1; o < 8; o *= 2) {
-      const uint32_t om = __shfl_xor_sync(0xffffffffu, m, o);
-      if (o < lanes) m = max(m, om);
+    for (int h = 0; h < 2; ++h) {
+      const float *u = q + 8 * h;
+      const uint32_t even = __float_as_uint(four_codes(u[0] + base, u[2], u[4], u[6])), odd = __float_as_uint(four_codes(u[1] + base, u[3], u[5], u[7]));
+      words[step][r][2 * c + h] = __byte_perm(even, odd, 0x5410);
     }
-    s = __fdiv_rn(__uint_as_float(m), 7.0f);
-  }
-  const bool sound = s > 0.0f && s <= 3.402823466e38f;
-  const float inv = sound && s > 1e-37f ? 1.0f / s : 0.0f;      // 0: it would overflow
-  if (kZeros && sound) z = fminf(15.0f, fmaxf(0.0f, round_quotient(-lo, s)));
-  if (sound) {
-    round_quotients(v, s, inv, q);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) q[i] = 0.0f;
-  }
-  if constexpr (kZeros) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) q[i] = fminf(q[i] + z, 15.0f);          // (at least 0: z rounds as the least value does)
-  }
-  const float base = kZeros ? 8388608.0f : 8388608.0f + 8.0f * 4369.0f;  // 2^23, and a zero point of 8 in every code
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const float *u = q + 8 * h;
-    const uint32_t even = __float_as_uint(four_codes(u[0] + base, u[2], u[4], u[6])), odd = __float_as_uint(four_codes(u[1] + base, u[3], u[5], u[7]));
-    words[r][2 * c + h] = __byte_perm(even, odd, 0x5410);
-  }
-  if (n < d.N && k < d.K && (c & (lanes - 1)) == 0) {
-    const size_t at = (size_t)(k >> lg) * d.N + n;
-    scales[at] = s;
-    if constexpr (kZeros) zeros[at] = (uint8_t)z;
+    if (n < d.N && k < d.K && (c & (lanes - 1)) == 0) {
+      const size_t at = (size_t)(k >> lg) * d.N + n;
+      scales[at] = s;
+      if constexpr (kZeros) zeros[at] = (uint8_t)z;
+    }
   }
   __syncthreads();
-  write_tiles(words, blockIdx.y, blockIdx.x * 2, (d.K + kW4Cols - 1) / kW4Cols, w_packed);
+  write_tiles(words, blockIdx.y, blockIdx.x * (kLayCols / kW4Cols), (d.K + kW4Cols - 1) / kW4Cols, w_packed);
 }
 
 __global__ void __launch_bounds__(kLayThreads)
 w4_pack_kernel(const uint8_t *codes, const xnor_w4_desc d, uint32_t *w_packed) {
-  __shared__ uint32_t words[kW4Rows][kOctets + 1];
+  __shared__ LayWords words;
   stream_order();
   const int r = threadIdx.x / 8, c = threadIdx.x % 8;
-  const int n = blockIdx.y * kW4Rows + r, k = blockIdx.x * kLayCols + 16 * c;
+  const int n = blockIdx.y * kW4Rows + r;
+  const bool pieces = d.K % 8 == 0;
 #pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    uint32_t word = 0u;
+  for (int q = 0; q < 2 * kLaySteps; ++q) {
+    const int k = blockIdx.x * kLayCols + (q / 2) * kStepCols + 16 * c + 8 * (q & 1);
+    uint32_t word = 0x88888888u;
+    if (n < d.N && k < d.K) {
+      const uint8_t *from = codes + (size_t)n * d.K + k;
+      if (pieces) {
+        const uint2 v = load_global(reinterpret_cast<const uint2 *>(from));
+        const uint32_t a = v.x & 0x0F0F0F0Fu, b = v.y & 0x0F0F0F0Fu;         // codes 0 .. 3 and 4 .. 7, one in each byte
+        const uint32_t even = __byte_perm(a, b, 0x6420), odd = __byte_perm(a, b, 0x7531);
+        word = __byte_perm(even | even >> 4, odd | odd >> 4, 0x6420);
+      } else {
+        word = 0u;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int kk = k + 8 * q + i;
-      word |= (n < d.N && kk < d.K ? load_global(codes + (size_t)n * d.K + kk) & 15u : 8u) << w4_bit(i);
+        for (int i = 0; i < 8; ++i) word |= (k + i < d.K ? load_global(from + i) & 15u : 8u) << w4_bit(i);
+      }
     }
-    words[r][2 * c + q] = word;
+    words[q / 2][r][2 * c + (q & 1)] = word;
   }
   __syncthreads();
-  write_tiles(words, blockIdx.y, blockIdx.x * 2, (d.K + kW4Cols - 1) / kW4Cols, w_packed);
+  write_tiles(words, blockIdx.y, blockIdx.x * (kLayCols / kW4Cols), (d.K + kW4Cols - 1) / kW4Cols, w_packed);
 }
 
 template <class T>
 __global__ void __launch_bounds__(kLayThreads)
 w4_dequantize_kernel(const uint32_t *w_packed, const float *scales, const uint8_t *zeros, const xnor_w4_desc d,
                      int lg, int pieces, uint32_t magic, T *w) {
-  __shared__ uint32_t words[2][32][5];
+  __shared__ uint32_t words[kLayCols / kW4Cols][32][5];
   stream_order();
   const int col_tiles = (d.K + kW4Cols - 1) / kW4Cols;
-  if (threadIdx.x < 64) {
-    const int tile = threadIdx.x / 32, lane = threadIdx.x & 31, ct = blockIdx.x * 2 + tile;
+  {
+    const int tile = threadIdx.x / 32, lane = threadIdx.x & 31, ct = blockIdx.x * (kLayCols / kW4Cols) + tile;
     if (ct < col_tiles) {
       const uint4 v = load_global(reinterpret_cast<const uint4 *>(w_packed) + (w4_tile(blockIdx.y, col_tiles) + (size_t)ct * kW4Panel) * 32 + lane);
       words[tile][lane][0] = v.x; words[tile][lane][1] = v.y; words[tile][lane][2] = v.z; words[tile][lane][3] = v.w;
     }
   }
+  const int r = threadIdx.x / 8, c = threadIdx.x % 8, n = blockIdx.y * kW4Rows + r;
+  float s[kLaySteps];
+  uint32_t z[kLaySteps];
+#pragma unroll
+  for (int step = 0; step < kLaySteps; ++step) {
+    const int k = blockIdx.x * kLayCols + step * kStepCols + 16 * c;
+    const bool in = n < d.N && k < d.K;
+    const size_t at = in ? (size_t)(k >> lg) * d.N + n : 0;  // 16 columns lie in one group
+    s[step] = load_global(scales + at);
+    z[step] = zeros ? load_global(zeros + at) : 8u;
+  }
   __syncthreads();
-  const int r = threadIdx.x / 8, c = threadIdx.x % 8;
-  const int n = blockIdx.y * kW4Rows + r, k = blockIdx.x * kLayCols + 16 * c;
-  if (n >= d.N || k >= d.K) return;
-  const size_t at = (size_t)(k >> lg) * d.N + n;             // 16 columns lie in one group
-  const float s = load_global(scales + at);
-  const W4Type<__nv_bfloat16>::Zero zero = W4Type<__nv_bfloat16>::zero(zeros ? load_global(zeros + at) : 8u);
+  if (n >= d.N) return;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int col = 16 * (c & 3) + 8 * h;
-    const uint32_t word = words[c / 4][w4_place(r, col)][w4_word(r, col)];
-    uint32_t pair[4];
-    W4Type<__nv_bfloat16>::expand(word, zero, magic, pair);
-    float v[8];
+  for (int step = 0; step < kLaySteps; ++step) {
+    const int k = blockIdx.x * kLayCols + step * kStepCols + 16 * c;
+    if (k >= d.K) return;
+    const W4Type<__nv_bfloat16>::Zero zero = W4Type<__nv_bfloat16>::zero(z[step]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 f = pair_to_float(pair[i], __nv_bfloat16());
-      v[2 * i] = f.x * s;
-      v[2 * i + 1] = f.y * s;
+    for (int h = 0; h < 2; ++h) {
+      const int col = 16 * (c & 3) + 8 * h;
+      uint32_t pair[4];
+      W4Type<__nv_bfloat16>::expand(words[2 * step + c / 4][w4_place(r, col)][w4_word(r, col)], zero, magic, pair);
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 f = pair_to_float(pair[i], __nv_bfloat16());
+        v[2 * i] = f.x * s[step];
+        v[2 * i + 1] = f.y * s[step];
+      }
+      Chunk<T> a;
+      a.from_float(v);
+      a.store(w + (size_t)n * d.K + k + 8 * h, pieces, min(8, max(0, d.K - (k + 8 * h))));
     }
-    Chunk<T> a;
-    a.from_float(v);
-    a.store(w + (size_t)n * d.K + k + 8 * h, pieces, min(8, max(0, d.K - (k + 8 * h))));
   }
 }
 
@@ -239,7 +271,6 @@ w4_few_rows_kernel(const W4Args A, int pieces, uint32_t magic) {
   const int col_tiles = (K + kW4Cols - 1) / kW4Cols, row_tiles = (N + kW4Rows - 1) / kW4Rows, groups = (K + kGroup - 1) / kGroup;
   const int split = gridDim.x, rank = blockIdx.x;           // blocks of the cluster
   const int n0 = blockIdx.y * kOut;
-  const long long tok0 = (long long)blockIdx.z * kTok;
   // stages of two column tiles: this warp's
   const unsigned stages = (unsigned)(col_tiles + kU - 1) / kU, slice = (unsigned)(rank * kFewWarps + warp);
   const int lg = 31 - __clz(split * kFewWarps);             // a power of two of slices; fewer than 2^18 stages
@@ -247,7 +278,7 @@ w4_few_rows_kernel(const W4Args A, int pieces, uint32_t magic) {
   const uint8_t *x[kN];
 #pragma unroll
   for (int i = 0; i < kN; ++i)
-    x[i] = static_cast<const uint8_t *>(A.x) + min(tok0 + 8 * i + g, (long long)A.r.rows - 1) * A.r.x_stride * kB;
+    x[i] = static_cast<const uint8_t *>(A.x) + (long long)min(8 * i + g, A.r.rows - 1) * A.r.x_stride * kB;
   const uint4 *w[kR];
   int na[kR], nb[kR];                                       // this lane's weight rows, inside the matrix
 #pragma unroll
@@ -358,7 +389,7 @@ w4_few_rows_kernel(const W4Args A, int pieces, uint32_t magic) {
 #pragma unroll
         for (int n = 0; n < kN; ++n) {
           if (kB == 1 && x_groups) {
-            const long long last = (long long)A.r.rows - 1, t0 = min(tok0 + 8 * n + 2 * t, last), t1 = min(tok0 + 8 * n + 2 * t + 1, last);
+            const long long t0 = min(8 * n + 2 * t, A.r.rows - 1), t1 = min(8 * n + 2 * t + 1, A.r.rows - 1);
             const int at = min(st * kS + grp, groups - 1);
             const float s0 = load_global(A.x_scales + t0 * groups + at), s1 = load_global(A.x_scales + t1 * groups + at);
             acc[n][0] *= s0; acc[n][1] *= s1; acc[n][2] *= s0; acc[n][3] *= s1;
@@ -400,7 +431,7 @@ w4_few_rows_kernel(const W4Args A, int pieces, uint32_t magic) {
       p[kOut + 1 + 8] = total[i][n][3];
     }
   __syncthreads();
-  const int toks = (int)min((long long)kTok, A.r.rows - tok0);
+  const int toks = A.r.rows;
   for (int e = threadIdx.x; e < toks * kOut; e += kFewThreads) {
     const int n = e % kOut, tok = e / kOut;
     float s = part[tok * (kOut + 1) + n];
@@ -424,7 +455,7 @@ w4_few_rows_kernel(const W4Args A, int pieces, uint32_t magic) {
         s += v;
       }
     if (n0 + n >= N) continue;
-    const long long row = tok0 + e / kOut;
+    const long long row = e / kOut;
     if (A.x_scales != nullptr && !x_groups) s *= load_global(A.x_scales + row);
     const size_t at = (size_t)(row * A.r.out_stride) + n0 + n;
     if (A.r.out_type == XNOR_F32) static_cast<float *>(A.out)[at] = s;
@@ -436,7 +467,7 @@ w4_few_rows_kernel(const W4Args A, int pieces, uint32_t magic) {
 
 template <int kType, int kN, int kR, int kGroup, bool kZeros>
 cudaError_t few_rows(const W4Args &a, cudaStream_t st) {
-  constexpr int kTok = 8 * kN, kOut = kW4Rows * kR;
+  constexpr int kTok = 8 * kN, kOut = kW4Rows * kR;        // rows of x: kTok at most
   constexpr size_t kSmem = (size_t)(kFewWarps * kTok * (kOut + 1) + kTok * kOut) * sizeof(float);
   static_assert(kSmem <= 48 * 1024, "shared memory");
   const int blocks = (w4_row_tiles(a.d) + kR - 1) / kR, col_tiles = w4_col_tiles(a.d);
@@ -445,7 +476,7 @@ cudaError_t few_rows(const W4Args &a, cudaStream_t st) {
   int split = 1;
   while (split < kMaxSplit && blocks * split < sm_count_of_current_device() && col_tiles >= 4 * split * kFewWarps) split *= 2;
   const int pieces = rows_in_pieces(a.x, a.r.x_stride, 8, RowsOf<kType>::kBytes);
-  const dim3 grid((unsigned)split, (unsigned)blocks, (unsigned)((a.r.rows + kTok - 1) / kTok));
+  const dim3 grid((unsigned)split, (unsigned)blocks);
   return launch_kernel(w4_few_rows_kernel<kType, kN, kR, kGroup, kZeros>, grid, kFewThreads, kSmem, st, (unsigned)split, a, pieces,
                        W4Type<typename RowsOf<kType>::T>::kMagic);
 }
@@ -454,7 +485,7 @@ cudaError_t few_rows(const W4Args &a, cudaStream_t st) {
 template <int kType, int kN, int kGroup>
 cudaError_t few_rows(const W4Args &a, cudaStream_t st) {
   if (a.zeros) return few_rows<kType, kN, 1, kGroup, true>(a, st);
-  return few_rows<kType, kN, kGroup == 32 ? 1 : 2, kGroup, false>(a, st);
+  return few_rows<kType, kN, kGroup == 32 || kN == 2 ? 1 : 2, kGroup, false>(a, st);
 }
 template <int kType, int kN>
 cudaError_t few_rows(const W4Args &a, cudaStream_t st) {
@@ -465,7 +496,7 @@ cudaError_t few_rows(const W4Args &a, cudaStream_t st) {
   return a.r.rows <= 8 ? few_rows<kType, 1>(a, st) : few_rows<kType, 2>(a, st);
 }
 
-dim3 lay_grid(const xnor_w4_desc &d) { return dim3((unsigned)((w4_col_tiles(d) + 1) / 2), (unsigned)w4_row_tiles(d)); }
+dim3 lay_grid(const xnor_w4_desc &d) { return dim3((unsigned)((d.K + kLayCols - 1) / kLayCols), (unsigned)w4_row_tiles(d)); }
 // ... of every row tile of the panels
 dim3 fill_grid(const xnor_w4_desc &d) { return dim3(lay_grid(d).x, (unsigned)(w4_panels(d) * kW4Panel)); }
 

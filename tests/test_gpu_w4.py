@@ -142,7 +142,11 @@ def operands(T, N, K, group, zeros, xname, seed, x_groups=False):
 def product(x, xs, codes, scales, zs, group, out_type, pad=0):
     N, K = codes.shape
     d, G = X.make_w4_desc(N, K, group), Guards()
-    packed = pack_codes(codes.cpu().numpy()).cuda()
+    if N * K > 1 << 20:                          # (the library's own layout, which test_pack compares)
+        packed = X.alloc_w4(d)[0]
+        X.xnor_w4_pack(codes, d, packed)
+    else:
+        packed = pack_codes(codes.cpu().numpy()).cuda()
     out = G.rows(x.shape[0], N, out_type, pad)
     X.xnor_w4_matmul(x, xs, packed, scales, zs, d, out)
     X.xnor_check_device()
@@ -158,7 +162,7 @@ def check_product(x, each, codes, scales, zs, group, out):
     assert (off <= 0).all(), (off.max(), out.dtype)
 
 
-ROWS = [1, 2, 7, 8, 9, 16, 17, 33, 100]
+ROWS = [1, 2, 7, 8, 9, 16, 17, 33, 65, 100]
 
 
 @pytest.mark.parametrize("xname", ["bf16", "f16", "i8", "e4m3"])
@@ -182,6 +186,16 @@ def test_product_large(xname, T, N, K):
     x, xs, each, codes, scales, zs = operands(T, N, K, 128, T % 2 == 1, xname, T, T == 300)
     out = product(x, xs, codes, scales, zs, 128, torch.float32)
     check_product(x, each, codes, scales, zs, 128, out)
+
+
+@pytest.mark.parametrize("xname", ["bf16", "f16", "i8", "e4m3"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("T,N,K", [(300, 5000, 328), (193, 9500, 161), (384, 4800, 329), (12, 6200, 4160), (9, 128, 4096)])
+def test_product_of_every_kernel(xname, group, T, N, K):
+    """Shapes that the largest blocks take (whole and ragged columns, addresses for copies or not), and the smallest."""
+    x, xs, each, codes, scales, zs = operands(T, N, K, group, K % 2 == 0, xname, T, T == 300)
+    out = product(x, xs, codes, scales, zs, group, torch.bfloat16)
+    check_product(x, each, codes, scales, zs, group, out)
 
 
 @pytest.mark.parametrize("xname", ["bf16", "f16", "i8", "e4m3"])

@@ -102,7 +102,7 @@ no(lambda: Q(q=f(8, 64, t=i8)[::2]))                      # not dense
 no(lambda: Q(s=f(4, 1)))
 no(lambda: Q(g=0))
 R = lambda dw, wk, h=None: X.xnor_rmsnorm_backward(f(4, 64), None, f(4, 64) if h is None else h, None, f(4), f(4, 64), dw, wk, stream=0)
-no(lambda: R(f(64), f(255)))                              # work too small
+no(lambda: R(f(64), f(63)))                               # work too small
 no(lambda: R(f(63), f(256)))
 no(lambda: R(None, None, h=f(4, 64, t=bf)))
 d = X.make_w4_desc(40, 100, 64)
