@@ -431,6 +431,7 @@ typedef enum {
  *   rstd      out  fp32 [rows] or NULL: what the backward pass needs
  * xnor_rmsnorm_quant writes y in 8 bits instead, without rounding it in between:
  *   scale = max|y| / top over the group, q = y / scale to nearest even, top = 127 (I8) or 448 (E4M3)
+ *   (scale and quotient within a few fp32 roundings of that)
  *   q         out  q_type [rows][cols], dense
  *   scales    out  fp32 [rows][cols / group], dense; group = 0: one scale for a whole row, [rows]
  *   A group of zeros has the scale 0.  A group with an infinity or NaN in it has such a scale (so that
@@ -468,7 +469,8 @@ xnor_status xnor_rmsnorm_quant(const void *x, const void *residual, const void *
  *   rstd     in   fp32 [rows], from the forward call
  *   dx       out  type [rows][cols], stride sum_stride; may be the same buffer as dy or dsum
  *   dweight  out  fp32 [cols] or NULL (then work may be NULL too)
- *   work     scratch of xnor_rmsnorm_work_elems(rows, cols) floats
+ *   work     scratch of xnor_rmsnorm_work_elems(rows, cols) floats; calls that can overlap (other
+ *                 streams, two graphs) need one each
  * dweight is summed in a fixed order: the same inputs give the same bits.  d->eps is ignored.
  * Errors as above; xnor_rmsnorm_work_elems gives 0 for sizes out of range and for no rows.
  */
@@ -519,8 +521,11 @@ xnor_status xnor_w4_dequantize(const uint32_t *w_packed, const float *scales, co
  *   x_scales  in   fp32 [rows] (x_group = 0) or [rows][ceil(K/group)] (x_group = group), dense; only
  *                  with I8 and E4M3 rows (xnor_rmsnorm_quant makes them), else NULL
  *   w_packed, scales, zeros   as above
- *   out       out  out_type [rows][N]: F32, BF16, F16, rounded once
- * code - zero and x are exact operands; the sums of a group and over the groups are fp32.
+ *   out       out  out_type [rows][N]: F32, BF16, F16, rounded once; overlaps nothing that is read
+ * code - zero and x are exact operands; the sums of a group and over the groups are fp32, in an order
+ * that depends on the sizes alone.  Up to 16 rows run on warp-level products whose weights go straight
+ * into registers, more on the 5th-generation tensor cores.  Device-side waits are bounded as in
+ * xnor_conv2d_forward (xnor_check_device); so are those of xnor_rmsnorm_backward.
  * INVALID_ARG as above, and for x_scales that are missing or not wanted.  UNSUPPORTED: F32 rows, an
  * x_group that is neither 0 nor the weights' group, rows > 1048560.
  */

@@ -34,7 +34,7 @@ xnor_status from_cuda(cudaError_t e) { return e == cudaSuccess ? XNOR_OK : XNOR_
 
 extern "C" {
 
-int xnor_version(void) { return 200; }
+int xnor_version(void) { return 300; }
 
 int xnor_built_with_bounds_check(void) {
 #ifdef XNOR_BOUNDS_CHECK
@@ -474,7 +474,7 @@ xnor_status xnor_rmsnorm(const void *x, const void *residual, const void *weight
   if (s == XNOR_ERR_INVALID_ARG) return s;
   if (d->rows > 0 && bad_write(y, d->y_stride, d->rows, d->cols)) return XNOR_ERR_INVALID_ARG;
   if (s != XNOR_OK) return s;
-  return from_cuda(xnor::launch_rmsnorm({x, residual, weight, sum, y, rstd, nullptr, nullptr, 0, 0, *d},
+  return from_cuda(xnor::launch_rmsnorm({x, residual, weight, sum, y, rstd, nullptr, nullptr, 0, 0, *d, 1.0f / (float)d->cols},
                                         (cudaStream_t)cuda_stream));
 }
 
@@ -488,7 +488,7 @@ xnor_status xnor_rmsnorm_quant(const void *x, const void *residual, const void *
   if (d->rows > 0 && (bad_ptr(q) || bad_ptr(scales))) return XNOR_ERR_INVALID_ARG;
   if (s != XNOR_OK) return s;
   if (group != 0 && d->cols % group != 0) return XNOR_ERR_UNSUPPORTED;
-  return from_cuda(xnor::launch_rmsnorm({x, residual, weight, sum, nullptr, rstd, q, scales, q_type, group, *d},
+  return from_cuda(xnor::launch_rmsnorm({x, residual, weight, sum, nullptr, rstd, q, scales, q_type, group, *d, 1.0f / (float)d->cols},
                                         (cudaStream_t)cuda_stream));
 }
 
@@ -507,7 +507,7 @@ xnor_status xnor_rmsnorm_backward(const void *dy, const void *dsum, const void *
                       bad_ptr(rstd) || bad_write(dx, d->sum_stride, d->rows, d->cols) || (dweight && bad_ptr(work))))
     return XNOR_ERR_INVALID_ARG;
   if (s != XNOR_OK) return s;
-  return from_cuda(xnor::launch_rmsnorm_backward({dy, dsum, h, weight, rstd, dx, dweight, work, *d}, (cudaStream_t)cuda_stream));
+  return from_cuda(xnor::launch_rmsnorm_backward({dy, dsum, h, weight, rstd, dx, dweight, work, *d, 1.0f / (float)d->cols}, (cudaStream_t)cuda_stream));
 }
 
 size_t xnor_w4_packed_words(const xnor_w4_desc *d) {

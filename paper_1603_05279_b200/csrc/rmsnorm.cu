@@ -41,10 +41,23 @@ struct Team {
 };
 
 struct Add { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
-// Of bit patterns of magnitudes: a NaN is above every number and stays.
-struct Max { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); } };
+// The larger of two, a NaN if either is one.
+struct Max {
+  __device__ __forceinline__ float operator()(float a, float b) const {
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
+  }
+};
 
-__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+// 1 / sqrt(v): an approximation and one step of Newton's method, within two roundings; 0, infinite and NaN as they come.
+// (Every thread of a row forms it.)
+__device__ __forceinline__ float inverse_root(float v) {
+  float r;
+  asm("rsqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+  const float better = fmaf(0.5f * r, fmaf(-v * r, r, 1.0f), r);
+  return r > 0.0f && r <= 3.402823466e38f ? better : r;
+}
 
 // Eight weights: ones (kind 0), in 32 bits (1) or of the rows' type (2).
 template <class T>
@@ -67,18 +80,18 @@ int weight_kind(const void *w, const xnor_norm_desc &d) {
   return w == nullptr ? 0 : d.weight_type == XNOR_F32 ? 1 : 2;
 }
 
-// The scale of a group whose largest magnitude is m (as bits), and what its values are multiplied with.  Both are within
-// two roundings of m / top and its reciprocal, at a few instructions (two IEEE divisions took a tenth of the time of
+// The scale of a group whose largest magnitude is v, and what its values are multiplied with.  Both are within
+// two roundings of v / top and its reciprocal, at a few instructions (two IEEE divisions took a tenth of the time of
 // e4m3 rows); where the reciprocal would overflow or the scale lose bits, they are divided.
-__device__ __forceinline__ float scale_of(uint32_t m, bool i8, float &inv) {
-  const float v = __uint_as_float(m), top = i8 ? 127.0f : 448.0f;
-  if (m < 0x08800000u && m > 0u) {           // below 2^-110
+__device__ __forceinline__ float scale_of(float v, bool i8, float &inv) {
+  const float top = i8 ? 127.0f : 448.0f;
+  if (v < 0x1p-110f && v > 0.0f) {
     inv = -1.0f;
     return __fdiv_rn(v, top);
   }
   float r;
   asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
-  inv = m > 0u && m < 0x7F800000u ? top * r : 0.0f;        // a group of zeros, infinite or NaN: zeros (NaN)
+  inv = v > 0.0f && v <= 3.402823466e38f ? top * r : 0.0f;        // a group of zeros, infinite or NaN: zeros (NaN)
   return v * (i8 ? 1.0f / 127.0f : 1.0f / 448.0f);
 }
 __device__ __forceinline__ void divide(float (&y)[8], float s, float inv) {
@@ -106,7 +119,7 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
 template <class T, int kV, bool kQuant>
 __device__ __forceinline__ void finish_row(const NormArgs &A, const Team &team, long long row, bool real, const int (&in)[kV], Chunk<T> (&xc)[kV],
                                            const Chunk<T> (&rc)[kV], const float (&wc)[kV][8], int weights, int pieces, float *red,
-                                           uint32_t *red_max) {
+                                           float *red_max) {
   const int D = A.d.cols;
   // (16-bit values stay packed and are converted twice: half the registers, so twice the rows under way)
   float ss = 0.0f;
@@ -132,7 +145,7 @@ __device__ __forceinline__ void finish_row(const NormArgs &A, const Team &team, 
     for (int v = 0; v < kV; ++v) xc[v].store(sum + 8 * (team.rank + v * team.size), pieces, in[v]);
   }
   ss = team.reduce(ss, red, Add());
-  const float rstd = 1.0f / sqrtf(ss / (float)D + A.d.eps);
+  const float rstd = inverse_root(fmaf(ss, A.per_col, A.d.eps));
   if (A.rstd && real && team.rank == 0) A.rstd[row] = rstd;
   auto normed = [&](int v, float (&y)[8]) {
     xc[v].to_float(y);
@@ -154,20 +167,20 @@ __device__ __forceinline__ void finish_row(const NormArgs &A, const Team &team, 
   } else {
     const bool i8 = A.q_type == XNOR_I8;
     float u[kV <= 2 ? kV : 1][8];             // (many chunks: formed again)
-    uint32_t m[kV];
+    float m[kV];
 #pragma unroll
     for (int v = 0; v < kV; ++v) {
       float (&y)[8] = u[kV <= 2 ? v : 0];
       normed(v, y);
-      m[v] = 0u;
+      m[v] = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) m[v] = max(m[v], magnitude(y[i]));
+      for (int i = 0; i < 8; ++i) m[v] = Max()(m[v], fabsf(y[i]));
     }
     const int lanes = A.group / 8, lg = 31 - __clz(max(A.group, 1));      // threads of a group: 4, 8 or 16, in one warp
     if (A.group == 0) {
-      uint32_t all = m[0];
+      float all = m[0];
 #pragma unroll
-      for (int v = 1; v < kV; ++v) all = max(all, m[v]);
+      for (int v = 1; v < kV; ++v) all = Max()(all, m[v]);
       all = team.reduce(all, red_max, Max());
 #pragma unroll
       for (int v = 0; v < kV; ++v) m[v] = all;
@@ -176,8 +189,8 @@ __device__ __forceinline__ void finish_row(const NormArgs &A, const Team &team, 
       for (int v = 0; v < kV; ++v)
 #pragma unroll
         for (int o = 1; o < 16; o *= 2) {
-          const uint32_t other = __shfl_xor_sync(0xffffffffu, m[v], o);
-          if (o < lanes) m[v] = max(m[v], other);
+          const float other = __shfl_xor_sync(0xffffffffu, m[v], o);
+          if (o < lanes) m[v] = Max()(m[v], other);
         }
     }
     uint8_t *q = static_cast<uint8_t *>(A.q) + (real ? row * D : 0);
@@ -211,7 +224,7 @@ template <class T, int kV, int kMost, bool kQuant>
 __global__ void __launch_bounds__(kMost, kMost <= 512 && sizeof(T) == 2 ? 2 : 1)
 rmsnorm_kernel(const NormArgs A, int team_size, int weights, int pieces) {
   __shared__ float red[kMost / 32];
-  __shared__ uint32_t red_max[kMost / 32];
+  __shared__ float red_max[kMost / 32];
   const Team team(team_size);
   const int D = A.d.cols;
   const long long row = (long long)blockIdx.x * ((int)blockDim.x / team_size) + ((int)threadIdx.x / team_size);
@@ -369,7 +382,7 @@ rmsnorm_backward_kernel(const NormBackwardArgs A, int team_size, int weights, in
     for (int v = 0; v < kV; ++v) add_chunk<T>(hc[v], yc[v], wc[v], rstd, dot, dw[v]);
     dot = team.reduce(dot, red[turn], Add());
     if (!real) continue;
-    const float k = dot * (rstd * rstd / (float)D);
+    const float k = dot * (rstd * rstd * A.per_col);
     T *dx = static_cast<T *>(A.dx) + row * A.d.sum_stride;
 #pragma unroll
     for (int v = 0; v < kV; ++v)
@@ -440,7 +453,7 @@ rmsnorm_backward_ring_kernel(const NormBackwardArgs A, int weights, int stages) 
       add_chunk<T>(h, y, wc[v], rstd, dot, dw[v]);
     }
     dot = team.reduce(dot, red[i & 1], Add());
-    const float k = dot * (rstd * rstd / (float)A.d.cols);
+    const float k = dot * (rstd * rstd * A.per_col);
     T *dx = static_cast<T *>(A.dx) + ring.row(i) * A.d.sum_stride;
 #pragma unroll
     for (int v = 0; v < kV; ++v) {

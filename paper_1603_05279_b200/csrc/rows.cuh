@@ -33,7 +33,7 @@ __device__ __forceinline__ uint8_t load_global(const uint8_t *p) {
 }
 
 __device__ __forceinline__ float2 pair_to_float(uint32_t w, __nv_bfloat16) {
-  return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w));
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));      // (one instruction each)
 }
 __device__ __forceinline__ float2 pair_to_float(uint32_t w, __half) {
   return __half22float2(*reinterpret_cast<const __half2 *>(&w));
@@ -128,6 +128,7 @@ struct NormArgs {
   float *scales;
   int q_type, group;          // group 0: the whole row
   xnor_norm_desc d;
+  float per_col;              // 1 / cols
 };
 cudaError_t launch_rmsnorm(const NormArgs &a, cudaStream_t st);
 struct NormBackwardArgs {
@@ -136,6 +137,7 @@ struct NormBackwardArgs {
   void *dx;
   float *dweight, *work;
   xnor_norm_desc d;
+  float per_col;
 };
 cudaError_t launch_rmsnorm_backward(const NormBackwardArgs &a, cudaStream_t st);
 cudaError_t read_status_norm(int *status);

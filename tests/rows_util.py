@@ -78,9 +78,9 @@ def norm_error(D):
     """Relative error of y before its rounding, of fp32 sums and products.
 
     A row's squares are added by a thread in chains of up to 32, then by a tree of 5 steps and a chain over up to
-    32 warps, each addition and product off by U at most: 69 U for the sum, half of that for its root; division
-    by D, addition of eps, root, reciprocal and two products: 6 U more."""
-    return (69 / 2 + 6) * U
+    32 warps, each addition and product off by U at most: 69 U for the sum; the rounded reciprocal of D, its
+    product and the addition of eps: 3 U more.  Half of that for the root, which is within 2 U itself; two products: 2 U."""
+    return (72 / 2 + 4) * U
 
 
 def unpack_codes(packed, N, K):
