@@ -157,3 +157,38 @@ def test_training_step_of_the_norm():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(w, want[0]) and torch.equal(dx, want[1])
+
+
+FIRST_CALL = """
+import torch
+from paper_1603_05279_b200.runner import TokenBlock
+import paper_1603_05279_b200 as X
+b = TokenBlock(%d, 512, 640, quant=%r)
+w = torch.randn(640, 512, device="cuda").bfloat16()
+b.x.normal_()
+b.residual.normal_()
+start = b.residual.clone()
+torch.cuda.synchronize()
+side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph, stream=side):
+    b.load(w)
+    b.forward()
+graph.replay()
+torch.cuda.synchronize()
+got = b.out.clone()
+b.residual.copy_(start)
+b.load(w)
+b.forward()
+X.xnor_check_device()
+assert torch.equal(got, b.out) and torch.isfinite(got).all()
+"""
+
+
+@pytest.mark.parametrize("rows,q", [(3, None), (40, "i8"), (300, None)])
+def test_first_calls_inside_a_capture(rows, q):
+    """What a process's first calls look up and set may happen while a graph is being captured."""
+    import subprocess
+    import sys
+    from test_binding import ROOT
+    r = subprocess.run([sys.executable, "-c", FIRST_CALL % (rows, q)], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
