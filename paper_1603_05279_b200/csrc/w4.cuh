@@ -82,14 +82,19 @@ struct RowsOf {
 template <> struct RowsOf<XNOR_BF16> { using T = __nv_bfloat16; static constexpr int kBytes = 2; };
 template <> struct RowsOf<XNOR_F16> { using T = __half; static constexpr int kBytes = 2; };
 
+// Two of four values in 8 bits.
+template <int kType>
+__device__ __forceinline__ uint32_t x_pair(uint32_t four, int pair) {
+  if constexpr (kType == XNOR_I8) return i8_pair(four, pair);
+  else return e4m3_pair((four >> (16 * pair)) & 0xFFFFu);
+}
 // As four pairs; `raw` is what lies in memory.
 template <int kType>
 __device__ __forceinline__ void x8_pairs(const uint32_t (&raw)[2 * RowsOf<kType>::kBytes], uint32_t (&v)[4]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if constexpr (RowsOf<kType>::kBytes == 2) v[i] = raw[i];
-    else if constexpr (kType == XNOR_I8) v[i] = i8_pair(raw[i / 2], i & 1);
-    else v[i] = e4m3_pair((raw[i / 2] >> (16 * (i & 1))) & 0xFFFFu);
+    else v[i] = x_pair<kType>(raw[i / 2], i & 1);
   }
 }
 // Columns k .. k + 7 of a row of K as they lie in memory; some may not exist (zeros) or lie anywhere.

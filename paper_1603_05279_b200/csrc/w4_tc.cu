@@ -44,12 +44,12 @@ constexpr uint32_t kCtrlBytes = 1024;
 constexpr int kMaxSplitTc = 8;
 constexpr int kAhead = 8;                    // groups whose scales are under way
 
-template <int kRows, int kBytes>
+template <int kRows, bool kCopies>           // kCopies: the rows come by tensor copies
 struct Shape {
   static constexpr int kPromo = kRows > 64 ? 2 : 1;            // sets of four warps
   static constexpr int kUnit = kRows / kPromo;                 // rows of x of a set
   static constexpr int kExpand = kRows > 64 ? 2 : 4;           // sets of four warps
-  static constexpr int kOther = kBytes == 1 ? 8 : 4, kLoadWarps = kOther - 2;
+  static constexpr int kOther = kCopies ? 4 : 8, kLoadWarps = kOther - 2;
   static constexpr int kMmaWarp = 4 * (kPromo + kExpand), kWeightWarp = kMmaWarp + 1, kLoadWarp = kMmaWarp + 2;
   static constexpr int kThreads = 32 * (kMmaWarp + kOther);
   static constexpr int kATmem = kRows > 128 ? 2 * kRows : 256; // behind the two accumulators
@@ -59,8 +59,8 @@ struct Shape {
   static constexpr size_t kSmem = 1024 + kCtrlBytes + kScaleBytes + kWeightStages * kWeightStage + (size_t)kStages * kStage;   // (1024: to align the ring)
   // Registers per thread as launched, and after they are dealt out anew: the promotion's hold its sums.
   static constexpr int kRegs = kThreads == 640 ? 96 : kThreads == 768 ? 80 : 72;
-  static constexpr int kPromoRegs = kRows > 128 ? 144 : kRows > 64 ? (kBytes == 1 ? 112 : 128) : kRows > 32 ? 128 : 96;
-  static constexpr int kOtherRegs = kRows > 128 ? 64 : kRows > 64 ? (kBytes == 1 ? 64 : 72) : kBytes == 1 ? (kRows > 32 ? 56 : 64) : (kRows > 32 ? 64 : 72);
+  static constexpr int kPromoRegs = kRows > 128 ? 144 : kRows > 64 ? (kCopies ? 128 : 112) : kRows > 32 ? (kCopies ? 128 : 112) : 96;
+  static constexpr int kOtherRegs = kRows > 128 ? 64 : kRows > 64 ? (kCopies ? 72 : 64) : kCopies ? (kRows > 32 ? 64 : 72) : 64;
   static_assert(kPromo * 128 * kPromoRegs + (kThreads - kPromo * 128) * kOtherRegs <= kThreads * kRegs, "registers");
   static_assert(kSmem <= 232448 && kStages <= kMaxStages && (kStages & (kStages - 1)) == 0, "shared and tensor memory");
   static_assert((size_t)kStages * kStage >= (size_t)kRows * kTileN * 4 || kRows > 128, "room for the sums of a block");
@@ -70,7 +70,7 @@ struct TcParams {
   CUtensorMap x_map;                        // the rows of x, 64 columns x kRows rows at a time
   W4Args A;
   int col_tiles, row_tiles, token_tiles;    // chunks of columns; tiles of 128 outputs, of kRows rows
-  int split, pieces, copies;                // copies: x_map is there
+  int split, pieces;                        // pieces: rows in 8 bits can be read in pieces of eight
   uint32_t idesc, magic;                    // magic: W4Type's
 };
 
@@ -347,82 +347,162 @@ __device__ __forceinline__ void copy_role(const TcParams &P, const Smem &S, cons
   }
 }
 
-// Through registers: rows in 8 bits become 16-bit numbers, others are at addresses that tensor copies do not take.
-// The warps share every stage; a thread has eight columns of every (4 kLoadWarps)-th row, and where it can it loads them
-// a chunk ahead.
+// A stage that is filled through registers: free, and filled by this warp.
+template <class Sh>
+__device__ __forceinline__ bool start_rows(const Smem &S, const Parities<Sh::kStages> &par, int i) {
+  return wait_warp(S, S.empty + 8u * (i % Sh::kStages), par.of(i) ^ 1u);
+}
+template <class Sh>
+__device__ __forceinline__ void finish_rows(const Smem &S, int i, int lane) {
+  fence_proxy_async();
+  __syncwarp();
+  if (lane == 0) mbar_arrive(S.full + 8u * (i % Sh::kStages));
+}
+
+// Through registers: rows in 8 bits become 16-bit numbers.  The warps share every stage; a thread has eight columns of
+// every (4 kLoadWarps)-th row, and where it can it loads them a chunk ahead.
 template <class Sh, int kType, int kRows>
 __device__ __forceinline__ void load_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total, int w, int lane) {
-  constexpr int kB = RowsOf<kType>::kBytes, kStep = 4 * Sh::kLoadWarps, kPass = (kRows + kStep - 1) / kStep, kBatch = kPass < 6 ? kPass : 6;
+  constexpr int kStep = 4 * Sh::kLoadWarps, kPass = (kRows + kStep - 1) / kStep;
+  static_assert(RowsOf<kType>::kBytes == 1 && kPass <= 6, "a batch is a stage");
   const int K = P.A.d.K, n = span.c1 - span.c0, piece = lane & 7, row0 = 4 * w + (lane >> 3);
-  const long long row_bytes = P.A.r.x_stride * kB;
+  const long long row_bytes = P.A.r.x_stride;
   Parities<Sh::kStages> par(n);
   for (int tile = first; tile < total; tile += step, par.next_tile()) {
     const long long tok0 = (long long)(tile / P.row_tiles) * kRows;
     const int rows = (int)min((long long)kRows, P.A.r.rows - tok0);
     const uint8_t *x = static_cast<const uint8_t *>(P.A.x) + tok0 * row_bytes;
     // (a row that does not exist is its last one's: no output reads it)
-    struct Batch { uint32_t v[kBatch][2 * kB]; };
-    auto whole = [&](int i) { return P.pieces && (span.c0 + i + 1) * kChunk <= K; };
-    auto load = [&](int i, int p0, Batch &b) {       // of a whole chunk, at addresses for whole pieces: nothing but loads
+    struct Batch { uint32_t v[kPass][2]; };
+    auto whole = [&](int i) { return (span.c0 + i + 1) * kChunk <= K; };
+    auto load = [&](int i, Batch &b) {               // of a whole chunk: nothing but loads
       if (i >= n || !whole(i)) return;
-      const uint8_t *from = x + ((span.c0 + i) * kChunk + 8 * piece) * kB;
+      const uint8_t *from = x + ((span.c0 + i) * kChunk + 8 * piece);
 #pragma unroll
-      for (int p = 0; p < kBatch; ++p)
-        load_x8_raw<kType>(from + (long long)min(row0 + kStep * (p0 + p), rows - 1) * row_bytes, 0, INT_MAX, true, b.v[p]);
+      for (int p = 0; p < kPass; ++p)
+        load_x8_raw<kType>(from + (long long)min(row0 + kStep * p, rows - 1) * row_bytes, 0, INT_MAX, true, b.v[p]);
     };
-    auto put = [&](int i, int row, const uint32_t (&raw)[2 * kB]) {
+    auto put = [&](int i, int row, const uint32_t (&raw)[2]) {
       uint32_t v[4];
       x8_pairs<kType>(raw, v);
       if (row < kRows)
         sts128(S.ring + ((uint32_t)i % Sh::kStages) * Sh::kStage + (uint32_t)row * 128u + (uint32_t)((piece ^ (row & 7)) * 16), v[0], v[1], v[2], v[3]);
     };
-    auto store = [&](int i, int p0, const Batch &b) {
+    auto store = [&](int i, const Batch &b) {
       if (whole(i)) {
 #pragma unroll
-        for (int p = 0; p < kBatch; ++p) put(i, row0 + kStep * (p0 + p), b.v[p]);
+        for (int p = 0; p < kPass; ++p) put(i, row0 + kStep * p, b.v[p]);
       } else {
 #pragma unroll 1
-        for (int p = 0; p < kBatch; ++p) {
-          uint32_t raw[2 * kB];
-          const int row = row0 + kStep * (p0 + p);
-          load_x8_raw<kType>(x + (long long)min(row, rows - 1) * row_bytes, (span.c0 + i) * kChunk + 8 * piece, K, P.pieces, raw);
+        for (int p = 0; p < kPass; ++p) {
+          uint32_t raw[2];
+          const int row = row0 + kStep * p;
+          load_x8_raw<kType>(x + (long long)min(row, rows - 1) * row_bytes, (span.c0 + i) * kChunk + 8 * piece, K, true, raw);
           put(i, row, raw);
         }
       }
     };
-    auto start = [&](int i) { return wait_warp(S, S.empty + 8u * (i % Sh::kStages), par.of(i) ^ 1u); };
-    auto finish = [&](int i) {
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(S.full + 8u * (i % Sh::kStages));
-    };
-    if constexpr (kPass <= kBatch) {
-      Batch b0, b1;
-      load(0, 0, b0);
-      load(1, 0, b1);
+    Batch b0, b1;
+    load(0, b0);
+    load(1, b1);
 #pragma unroll 1
-      for (int i = 0; i < n; i += 2) {
-        if (!start(i)) return;
-        store(i, 0, b0);
-        finish(i);
+    for (int i = 0; i < n; i += 2) {
+      if (!start_rows<Sh>(S, par, i)) return;
+      store(i, b0);
+      finish_rows<Sh>(S, i, lane);
+      load(i + 2, b0);
+      if (i + 1 >= n) break;
+      if (!start_rows<Sh>(S, par, i + 1)) return;
+      store(i + 1, b1);
+      finish_rows<Sh>(S, i + 1, lane);
+      load(i + 3, b1);
+    }
+  }
+}
+
+// Through registers from any address, as rows of an odd number of columns have them: a thread loads one aligned word of
+// four bytes per row, so that a warp reads a chunk of one row (two in 8 bits) at once, and takes the bytes that belong to
+// its neighbour's word from there; what lies behind the warp's words, a thread per row loads.  (Value by value it took
+// 2035 us for 2048 rows times 4096x4095, and tensor copies take 73 for 4096x4096.)
+template <class Sh, int kType, int kRows>
+__device__ __forceinline__ void word_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total, int w, int lane) {
+  constexpr int kB = RowsOf<kType>::kBytes, kWords = kChunk * kB / 4, kAtOnce = 32 / kWords, kStep = kAtOnce * Sh::kLoadWarps;
+  constexpr int kPass = (kRows + kStep - 1) / kStep, kParts = kPass > 12 ? 2 : 1, kBatch = (kPass + kParts - 1) / kParts;
+  static_assert(kBatch * kAtOnce <= 31, "a thread for what lies behind each row, a bit for each load");
+  const int K = P.A.d.K, n = span.c1 - span.c0, word = lane % kWords, row0 = kAtOnce * w + lane / kWords;
+  const int behind = kAtOnce * w + lane % kAtOnce + kStep * (lane / kAtOnce);       // the row whose next word this thread loads
+  const long long row_bytes = P.A.r.x_stride * kB;
+  const uint8_t *end = static_cast<const uint8_t *>(P.A.x) + (P.A.r.rows - 1) * row_bytes + (size_t)K * kB;
+  uint32_t tail = 0u;                                // of the word in which the rows end
+  for (int i = 0; i < (int)((uintptr_t)end & 3u); ++i)
+    tail |= (uint32_t)load_global(reinterpret_cast<const uint8_t *>((uintptr_t)end & ~(uintptr_t)3) + i) << (8 * i);
+  Parities<Sh::kStages> par(n);
+  for (int tile = first; tile < total; tile += step, par.next_tile()) {
+    const long long tok0 = (long long)(tile / P.row_tiles) * kRows;
+    const int rows = (int)min((long long)kRows, P.A.r.rows - tok0);
+    const uint8_t *x = static_cast<const uint8_t *>(P.A.x) + tok0 * row_bytes;
+    struct Batch { uint32_t v[kBatch], next, tails; };               // tails: which loads are the last word
+    auto load = [&](int i, int part, Batch &b) {
+      if (i >= n) return;
+      const uint8_t *from = x + (size_t)(span.c0 + i) * (kChunk * kB);
+      b.tails = 0u;
+      auto one = [&](int row, int at, int bit, uint32_t &v) {
+        // (a row that does not exist is its last one's: no output reads it)
+        const uintptr_t p = ((uintptr_t)(from + (long long)min(row, rows - 1) * row_bytes) & ~(uintptr_t)3) + 4u * (unsigned)at;
+        if (p == ((uintptr_t)end & ~(uintptr_t)3)) b.tails |= 1u << bit;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.le.u64 p, %2, %3;\n\tmov.u32 %0, 0;\n\t@p ld.global.u32 %0, [%1];\n\t}"
+            : "=r"(v) : "l"(p), "l"(p + 4u), "l"(end) : "memory");
+      };
+      int r0 = row0 + kStep * kBatch * part;
+      asm volatile("" : "+r"(r0));                   // (the addresses of all rows at once do not fit the registers)
+#pragma unroll
+      for (int p = 0; p < kBatch; ++p) one(r0 + kStep * p, word, p, b.v[p]);
+      one(behind + kStep * kBatch * part, kWords, 31, b.next);
+    };
+    auto store = [&](int i, int part, const Batch &b) {
+      const int left = (K - (span.c0 + i) * kChunk) * kB - 4 * word;                 // bytes of this word that exist
+      const uint32_t mask = left >= 4 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+      const uint32_t next = b.tails >> 31 ? tail : b.next, low = (uint32_t)(uintptr_t)x;
+      const uint32_t stage = S.ring + ((uint32_t)i % Sh::kStages) * Sh::kStage;
+      int r0 = row0 + kStep * kBatch * part;
+      asm volatile("" : "+r"(r0));
+#pragma unroll
+      for (int p = 0; p < kBatch; ++p) {
+        const int row = r0 + kStep * p;
+        const uint32_t mine = (b.tails >> p) & 1u ? tail : b.v[p];
+        const uint32_t other = __shfl_down_sync(0xFFFFFFFFu, mine, 1), last = __shfl_sync(0xFFFFFFFFu, next, kAtOnce * p + lane / kWords);
+        const uint32_t turn = 8u * ((low + (uint32_t)min(row, rows - 1) * (uint32_t)row_bytes) & 3u);
+        const uint32_t v = __funnelshift_r(mine, word == kWords - 1 ? last : other, turn) & mask;
+        if (row >= kRows) continue;
+        const uint32_t to = stage + (uint32_t)row * 128u;
+        if constexpr (kB == 2)
+          asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + (uint32_t)(((word >> 2) ^ (row & 7)) * 16 + (word & 3) * 4)), "r"(v) : "memory");
+        else
+          asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to + (uint32_t)(((word >> 1) ^ (row & 7)) * 16 + (word & 1) * 8)),
+                       "r"(x_pair<kType>(v, 0)), "r"(x_pair<kType>(v, 1)) : "memory");
+      }
+    };
+    Batch b0, b1;
+    load(0, 0, b0);
+    load(kParts == 1 ? 1 : 0, kParts - 1, b1);
+#pragma unroll 1
+    for (int i = 0; i < n; i += 3 - kParts) {
+      if (!start_rows<Sh>(S, par, i)) return;
+      store(i, 0, b0);
+      if constexpr (kParts == 1) {
+        finish_rows<Sh>(S, i, lane);
         load(i + 2, 0, b0);
         if (i + 1 >= n) break;
-        if (!start(i + 1)) return;
+        if (!start_rows<Sh>(S, par, i + 1)) return;
         store(i + 1, 0, b1);
-        finish(i + 1);
+        finish_rows<Sh>(S, i + 1, lane);
         load(i + 3, 0, b1);
-      }
-    } else {
-      Batch b;
-#pragma unroll 1
-      for (int i = 0; i < n; ++i) {
-        if (!start(i)) return;
-#pragma unroll 1
-        for (int p0 = 0; p0 < kPass; p0 += kBatch) {
-          load(i, p0, b);
-          store(i, p0, b);
-        }
-        finish(i);
+      } else {
+        load(i + 1, 0, b0);
+        store(i, 1, b1);
+        finish_rows<Sh>(S, i, lane);
+        load(i + 1, 1, b1);
       }
     }
   }
@@ -590,23 +670,23 @@ __device__ __forceinline__ void cluster_barrier() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-template <int kType, int kRows>
-__global__ void __launch_bounds__(Shape<kRows, RowsOf<kType>::kBytes>::kThreads, 1)
+template <int kType, int kRows, bool kCopies>
+__global__ void __launch_bounds__(Shape<kRows, kCopies>::kThreads, 1)
 w4_tc_kernel(const __grid_constant__ TcParams P) {
-  using Sh = Shape<kRows, RowsOf<kType>::kBytes>;
+  using Sh = Shape<kRows, kCopies>;
   using T = typename RowsOf<kType>::T;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Smem S = carve(smem, Sh::kScaleBytes);
   if (threadIdx.x == 0) {
     // a stage is full with four expanding warps' arrivals and those that bring the rows
-    for (int i = 0; i < Sh::kStages; ++i) { mbar_init(S.full + 8u * i, 4 + (P.copies ? 1 : Sh::kLoadWarps)); mbar_init(S.empty + 8u * i, 1); }
+    for (int i = 0; i < Sh::kStages; ++i) { mbar_init(S.full + 8u * i, 4 + (kCopies ? 1 : Sh::kLoadWarps)); mbar_init(S.empty + 8u * i, 1); }
     for (int i = 0; i < kWeightStages; ++i) { mbar_init(S.wfull + 8u * i, 1); mbar_init(S.wempty + 8u * i, 8); }
     for (int i = 0; i < 2; ++i) { mbar_init(S.dfull + 8u * i, 1); mbar_init(S.dempty + 8u * i, 4 * Sh::kPromo); }
     *S.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == Sh::kLoadWarp && lane == 0 && P.copies)
+  if (kCopies && warp == Sh::kLoadWarp && lane == 0)
     asm volatile("prefetch.tensormap [%0];" ::"l"(&P.x_map) : "memory");
   if (warp == Sh::kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(S.tmem_slot)), "r"(512u) : "memory");
@@ -638,10 +718,14 @@ w4_tc_kernel(const __grid_constant__ TcParams P) {
       }
     } else if (warp == Sh::kWeightWarp) {
       if (elect_one()) weight_role(P, S, span, first, step, total);
-    } else if (!P.copies) {
-      load_role<Sh, kType, kRows>(P, S, span, first, step, total, warp - Sh::kLoadWarp, lane);
-    } else if (warp == Sh::kLoadWarp) {
-      if (elect_one()) copy_role<Sh, kRows>(P, S, span, first, step, total);
+    } else if constexpr (kCopies) {
+      if (warp == Sh::kLoadWarp && elect_one()) copy_role<Sh, kRows>(P, S, span, first, step, total);
+    } else {
+      bool done = false;
+      if constexpr (RowsOf<kType>::kBytes == 1) {
+        if (P.pieces) { load_role<Sh, kType, kRows>(P, S, span, first, step, total, warp - Sh::kLoadWarp, lane); done = true; }
+      }
+      if (!done) word_role<Sh, kType, kRows>(P, S, span, first, step, total, warp - Sh::kLoadWarp, lane);
     }
     __syncwarp();
   }
@@ -708,29 +792,32 @@ EncodeTiled encode_tiled() {
 
 // Whether the rows can be copied as they are, and their map.
 template <int kType>
+bool copied(const W4Args &a) {
+  return RowsOf<kType>::kBytes == 2 && rows_in_pieces(a.x, a.r.x_stride, 8, 2) && a.r.x_stride >= a.d.K && encode_tiled() != nullptr;
+}
+template <int kType>
 bool map_rows(const W4Args &a, int rows, CUtensorMap *map) {
-  if (RowsOf<kType>::kBytes != 2 || !rows_in_pieces(a.x, a.r.x_stride, 8, 2) || a.r.x_stride < a.d.K) return false;
-  const EncodeTiled encode = encode_tiled();
-  if (encode == nullptr) return false;
   const cuuint64_t size[2] = {(cuuint64_t)a.d.K, (cuuint64_t)a.r.rows}, stride[1] = {(cuuint64_t)a.r.x_stride * 2};
   const cuuint32_t box[2] = {kChunk, (cuuint32_t)rows}, each[2] = {1, 1};
-  return encode(map, kType == XNOR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
-                const_cast<void *>(a.x), size, stride, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return encode_tiled()(map, kType == XNOR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                        const_cast<void *>(a.x), size, stride, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int kType, int kRows>
+template <int kType, int kRows, bool kCopies>
 cudaError_t run(const W4Args &a, cudaStream_t st) {
-  using Sh = Shape<kRows, RowsOf<kType>::kBytes>;
+  using Sh = Shape<kRows, kCopies>;
   static bool attr_flags[64] = {};
   bool &attr_set = attr_done_for_current_device(attr_flags);
   if (!attr_set) {
-    const cudaError_t e = cudaFuncSetAttribute(w4_tc_kernel<kType, kRows>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Sh::kSmem);
+    const cudaError_t e = cudaFuncSetAttribute(w4_tc_kernel<kType, kRows, kCopies>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Sh::kSmem);
     if (e != cudaSuccess) { (void)cudaGetLastError(); return e; }
     attr_set = true;
   }
   TcParams P;
-  P.copies = map_rows<kType>(a, kRows, &P.x_map);
+  if constexpr (kCopies) {
+    if (!map_rows<kType>(a, kRows, &P.x_map)) return cudaErrorInvalidValue;
+  }
   P.A = a;
   P.magic = W4Type<typename RowsOf<kType>::T>::kMagic;
   P.col_tiles = w4_col_tiles(a.d);
@@ -745,19 +832,26 @@ cudaError_t run(const W4Args &a, cudaStream_t st) {
   const uint32_t format = kType == XNOR_BF16 ? 1u : 0u;
   P.idesc = (1u << 4) | (format << 7) | (format << 10) | ((uint32_t)(kRows >> 3) << 17) | ((uint32_t)(kTileN >> 4) << 24);
   const unsigned grid = P.split > 1 ? (unsigned)(total * P.split) : (unsigned)std::min(total, sms);
-  return launch_kernel(w4_tc_kernel<kType, kRows>, dim3(grid), Sh::kThreads, Sh::kSmem, st, (unsigned)P.split, P);
+  return launch_kernel(w4_tc_kernel<kType, kRows, kCopies>, dim3(grid), Sh::kThreads, Sh::kSmem, st, (unsigned)P.split, P);
 }
 
+template <int kType, bool kCopies>
+cudaError_t run_rows(const W4Args &a, cudaStream_t st) {
+  if (a.r.rows <= 16) return run<kType, 16, kCopies>(a, st);
+  if (a.r.rows <= 32) return run<kType, 32, kCopies>(a, st);
+  if (a.r.rows <= 64) return run<kType, 64, kCopies>(a, st);
+  return run<kType, 128, kCopies>(a, st);
+}
 template <int kType>
 cudaError_t run_type(const W4Args &a, cudaStream_t st) {
   if constexpr (RowsOf<kType>::kBytes == 2) {
-    const long long tiles = (a.d.N + kTileN - 1) / kTileN * ((a.r.rows + 191ll) / 192);
-    if (a.r.rows > 128 && 2 * tiles > sm_count_of_current_device()) return run<kType, 192>(a, st);
+    if (copied<kType>(a)) {
+      const long long tiles = (a.d.N + kTileN - 1) / kTileN * ((a.r.rows + 191ll) / 192);
+      if (a.r.rows > 128 && 2 * tiles > sm_count_of_current_device()) return run<kType, 192, true>(a, st);
+      return run_rows<kType, true>(a, st);
+    }
   }
-  if (a.r.rows <= 16) return run<kType, 16>(a, st);
-  if (a.r.rows <= 32) return run<kType, 32>(a, st);
-  if (a.r.rows <= 64) return run<kType, 64>(a, st);
-  return run<kType, 128>(a, st);
+  return run_rows<kType, false>(a, st);
 }
 
 }  // namespace

@@ -208,6 +208,23 @@ def test_product_of_rows_apart(xname, T):
         check_product(x, each, codes, scales, zs, 64, out)
 
 
+@pytest.mark.parametrize("xname", ["bf16", "f16", "i8", "e4m3"])
+@pytest.mark.parametrize("T", [2, 17, 33, 70, 129])
+def test_product_of_rows_at_odd_addresses(xname, T):
+    """Rows of an odd number of columns, from less than a word to several blocks of columns; NaN (int8: -100)
+    between them and behind the last one."""
+    for K, pad in ((1, 0), (3, 0), (5, 2), (63, 0), (64, 1), (65, 0), (129, 6), (191, 4), (701, 0), (1280, 3)):
+        x, xs, each, codes, scales, zs = operands(T, 130, K, 32, True, xname, K + T)
+        if xname in ("i8", "e4m3"):
+            buf = torch.full((T * (K + pad) + 40,), -100 if xname == "i8" else 127, dtype=torch.int8, device="cuda").view(x.dtype)
+        else:
+            buf = torch.full((T * (K + pad) + 40,), float("nan"), dtype=x.dtype, device="cuda")
+        rows = buf.view(torch.int8 if x.element_size() == 1 else torch.int16).as_strided((T, K), (K + pad, 1))
+        rows.copy_(x.view(rows.dtype))
+        out = product(rows.view(x.dtype), xs, codes, scales, zs, 32, torch.float32)
+        check_product(x, each, codes, scales, zs, 32, out)
+
+
 def _apart(x, pad):
     """x with its rows `pad` elements further apart, NaN (int8: 77) between them."""
     if not pad:
