@@ -13,7 +13,7 @@
 //   expansion  8: a thread expands one weight row, 64 columns at a time, from shared straight into tensor memory
 //   one issues the products, one copies the packed weights into a deep ring in shared memory (bulk copies), one the
 //   rows of x, by tensor copies, into the stages of 64 columns that the products read; rows that cannot be copied as
-//   they are, in 8 bits above all, come through the registers of two warps (six) instead
+//   they are, in 8 bits above all, come through the registers of six warps instead
 // Where the tiles are too few for the GPU, the blocks of a cluster divide the columns, and add their sums through
 // each other's shared memory in a fixed order.  Every wait is bounded; on expiry the block records
 // XNOR_ERR_TIMEOUT, stops and frees its tensor memory.
@@ -422,18 +422,19 @@ __device__ __forceinline__ void load_role(const TcParams &P, const Smem &S, cons
 
 // Through registers from any address, as rows of an odd number of columns have them: a thread loads one aligned word of
 // four bytes per row, so that a warp reads a chunk of one row (two in 8 bits) at once, and takes the bytes that belong to
-// its neighbour's word from there; what lies behind the warp's words, a thread per row loads.  (Value by value it took
-// 2035 us for 2048 rows times 4096x4095, and tensor copies take 73 for 4096x4096.)
+// its neighbour's word from there; what lies behind the warp's words, a thread per row loads.  2048 bf16
+// rows times 4096x4095: 537 us, 2035 value by value; tensor copies take 73 for 4096x4096.  Bound by the loads' latency:
+// more than twelve rows of a warp under way at once do not fit the registers and spill (593 us).
 template <class Sh, int kType, int kRows>
 __device__ __forceinline__ void word_role(const TcParams &P, const Smem &S, const Span &span, int first, int step, int total, int w, int lane) {
   constexpr int kB = RowsOf<kType>::kBytes, kWords = kChunk * kB / 4, kAtOnce = 32 / kWords, kStep = kAtOnce * Sh::kLoadWarps;
-  constexpr int kPass = (kRows + kStep - 1) / kStep, kParts = kPass > 12 ? 2 : 1, kBatch = (kPass + kParts - 1) / kParts;
-  static_assert(kBatch * kAtOnce <= 31, "a thread for what lies behind each row, a bit for each load");
+  constexpr int kPass = (kRows + kStep - 1) / kStep, kParts = kPass > 6 ? 2 * ((kPass + 11) / 12) : 1, kBatch = (kPass + kParts - 1) / kParts;
+  static_assert(kBatch * kAtOnce <= 32, "a thread for what lies behind each row");
   const int K = P.A.d.K, n = span.c1 - span.c0, word = lane % kWords, row0 = kAtOnce * w + lane / kWords;
   const int behind = kAtOnce * w + lane % kAtOnce + kStep * (lane / kAtOnce);       // the row whose next word this thread loads
   const long long row_bytes = P.A.r.x_stride * kB;
   const uint8_t *end = static_cast<const uint8_t *>(P.A.x) + (P.A.r.rows - 1) * row_bytes + (size_t)K * kB;
-  uint32_t tail = 0u;                                // of the word in which the rows end
+  uint32_t tail = 0u;                                // what exists of the word in which the rows end
   for (int i = 0; i < (int)((uintptr_t)end & 3u); ++i)
     tail |= (uint32_t)load_global(reinterpret_cast<const uint8_t *>((uintptr_t)end & ~(uintptr_t)3) + i) << (8 * i);
   Parities<Sh::kStages> par(n);
@@ -441,56 +442,71 @@ __device__ __forceinline__ void word_role(const TcParams &P, const Smem &S, cons
     const long long tok0 = (long long)(tile / P.row_tiles) * kRows;
     const int rows = (int)min((long long)kRows, P.A.r.rows - tok0);
     const uint8_t *x = static_cast<const uint8_t *>(P.A.x) + tok0 * row_bytes;
-    struct Batch { uint32_t v[kBatch], next, tails; };               // tails: which loads are the last word
-    auto load = [&](int i, int part, Batch &b) {
-      if (i >= n) return;
-      const uint8_t *from = x + (size_t)(span.c0 + i) * (kChunk * kB);
-      b.tails = 0u;
-      auto one = [&](int row, int at, int bit, uint32_t &v) {
-        // (a row that does not exist is its last one's: no output reads it)
-        const uintptr_t p = ((uintptr_t)(from + (long long)min(row, rows - 1) * row_bytes) & ~(uintptr_t)3) + 4u * (unsigned)at;
-        if (p == ((uintptr_t)end & ~(uintptr_t)3)) b.tails |= 1u << bit;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\tsetp.le.u64 p, %2, %3;\n\tmov.u32 %0, 0;\n\t@p ld.global.u32 %0, [%1];\n\t}"
-            : "=r"(v) : "l"(p), "l"(p + 4u), "l"(end) : "memory");
-      };
+    struct Batch { uint32_t v[kBatch], next; };
+    // Chunks that end a word and more before a row's last byte: no word can lie behind the rows.
+    auto inner = [&](int i) { return (span.c0 + i + 1) * kChunk * kB + 8 <= K * kB; };
+    // (a row that does not exist is its last one's: no output reads it)
+    auto place = [&](int i, int row, int at) {
+      return (uintptr_t)(x + (size_t)(span.c0 + i) * (kChunk * kB) + 4 * at + (long long)min(row, rows - 1) * row_bytes) & ~(uintptr_t)3;
+    };
+    auto load = [&](int i, int part, Batch &b) {     // of an inner chunk: nothing but loads
+      if (i >= n || !inner(i)) return;
       int r0 = row0 + kStep * kBatch * part;
       asm volatile("" : "+r"(r0));                   // (the addresses of all rows at once do not fit the registers)
 #pragma unroll
-      for (int p = 0; p < kBatch; ++p) one(r0 + kStep * p, word, p, b.v[p]);
-      one(behind + kStep * kBatch * part, kWords, 31, b.next);
+      for (int p = 0; p < kBatch; ++p) b.v[p] = load_global(reinterpret_cast<const uint32_t *>(place(i, r0 + kStep * p, word)));
+      b.next = load_global(reinterpret_cast<const uint32_t *>(place(i, behind + kStep * kBatch * part, kWords)));
+    };
+    const uint32_t low = 8u * (uint32_t)(uintptr_t)x, step8 = 8u * (uint32_t)row_bytes;
+    auto put = [&](int i, int row, uint32_t mine, uint32_t other, uint32_t mask) {
+      const uint32_t v = __funnelshift_r(mine, other, low + (uint32_t)row * step8) & mask;      // (by the address's bits modulo 32)
+      const uint32_t to = S.ring + ((uint32_t)i % Sh::kStages) * Sh::kStage + (uint32_t)row * 128u;
+      // (predicates, not branches: the shuffles of the next row would wait for the warp to join)
+      if constexpr (kB == 2)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.s32 p, %0, %1;\n\t@p st.shared.b32 [%2], %3;\n\t}"
+                     ::"r"(row), "n"(kRows), "r"(to + (uint32_t)(((word >> 2) ^ (row & 7)) * 16 + (word & 3) * 4)), "r"(v) : "memory");
+      else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.s32 p, %0, %1;\n\t@p st.shared.v2.b32 [%2], {%3, %4};\n\t}"
+                     ::"r"(row), "n"(kRows), "r"(to + (uint32_t)(((word >> 1) ^ (row & 7)) * 16 + (word & 1) * 8)),
+                     "r"(x_pair<kType>(v, 0)), "r"(x_pair<kType>(v, 1)) : "memory");
     };
     auto store = [&](int i, int part, const Batch &b) {
-      const int left = (K - (span.c0 + i) * kChunk) * kB - 4 * word;                 // bytes of this word that exist
-      const uint32_t mask = left >= 4 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
-      const uint32_t next = b.tails >> 31 ? tail : b.next, low = (uint32_t)(uintptr_t)x;
-      const uint32_t stage = S.ring + ((uint32_t)i % Sh::kStages) * Sh::kStage;
       int r0 = row0 + kStep * kBatch * part;
       asm volatile("" : "+r"(r0));
+      if (inner(i)) {
 #pragma unroll
-      for (int p = 0; p < kBatch; ++p) {
-        const int row = r0 + kStep * p;
-        const uint32_t mine = (b.tails >> p) & 1u ? tail : b.v[p];
-        const uint32_t other = __shfl_down_sync(0xFFFFFFFFu, mine, 1), last = __shfl_sync(0xFFFFFFFFu, next, kAtOnce * p + lane / kWords);
-        const uint32_t turn = 8u * ((low + (uint32_t)min(row, rows - 1) * (uint32_t)row_bytes) & 3u);
-        const uint32_t v = __funnelshift_r(mine, word == kWords - 1 ? last : other, turn) & mask;
-        if (row >= kRows) continue;
-        const uint32_t to = stage + (uint32_t)row * 128u;
-        if constexpr (kB == 2)
-          asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + (uint32_t)(((word >> 2) ^ (row & 7)) * 16 + (word & 3) * 4)), "r"(v) : "memory");
-        else
-          asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to + (uint32_t)(((word >> 1) ^ (row & 7)) * 16 + (word & 1) * 8)),
-                       "r"(x_pair<kType>(v, 0)), "r"(x_pair<kType>(v, 1)) : "memory");
+        for (int p = 0; p < kBatch; ++p) {
+          const uint32_t other = __shfl_down_sync(0xFFFFFFFFu, b.v[p], 1), last = __shfl_sync(0xFFFFFFFFu, b.next, kAtOnce * p + lane / kWords);
+          put(i, r0 + kStep * p, b.v[p], word == kWords - 1 ? last : other, 0xFFFFFFFFu);
+        }
+        return;
+      }
+      const int left = (K - (span.c0 + i) * kChunk) * kB - 4 * word;                 // bytes of this word that exist
+      const uint32_t mask = left >= 4 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+      auto read = [&](uintptr_t p) {
+        return p + 4u <= (uintptr_t)end ? load_global(reinterpret_cast<const uint32_t *>(p)) : p < (uintptr_t)end ? tail : 0u;
+      };
+#pragma unroll 1
+      for (int p0 = 0; p0 < kBatch; p0 += 2, r0 += 2 * kStep) {
+        uint32_t mine[2], other[2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          mine[p] = read(place(i, r0 + kStep * p, word));
+          other[p] = read(place(i, r0 + kStep * p, word + 1));
+        }
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+          if (p0 + p < kBatch) put(i, r0 + kStep * p, mine[p], other[p], mask);
       }
     };
     Batch b0, b1;
     load(0, 0, b0);
-    load(kParts == 1 ? 1 : 0, kParts - 1, b1);
+    load(kParts == 1 ? 1 : 0, kParts == 1 ? 0 : 1, b1);
 #pragma unroll 1
-    for (int i = 0; i < n; i += 3 - kParts) {
+    for (int i = 0; i < n; i += kParts == 1 ? 2 : 1) {
       if (!start_rows<Sh>(S, par, i)) return;
-      store(i, 0, b0);
       if constexpr (kParts == 1) {
+        store(i, 0, b0);
         finish_rows<Sh>(S, i, lane);
         load(i + 2, 0, b0);
         if (i + 1 >= n) break;
@@ -499,10 +515,15 @@ __device__ __forceinline__ void word_role(const TcParams &P, const Smem &S, cons
         finish_rows<Sh>(S, i + 1, lane);
         load(i + 3, 0, b1);
       } else {
-        load(i + 1, 0, b0);
-        store(i, 1, b1);
-        finish_rows<Sh>(S, i, lane);
-        load(i + 1, 1, b1);
+#pragma unroll
+        for (int q = 0; q < kParts; q += 2) {
+          const bool last = q + 2 == kParts;
+          store(i, q, b0);
+          load(last ? i + 1 : i, last ? 0 : q + 2, b0);
+          store(i, q + 1, b1);
+          if (last) finish_rows<Sh>(S, i, lane);
+          load(last ? i + 1 : i, last ? 1 : q + 3, b1);
+        }
       }
     }
   }
