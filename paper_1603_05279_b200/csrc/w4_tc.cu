@@ -8,7 +8,7 @@
 // rounded: scaling the weights before the product would round each to the operands' 8 or 11 bits.
 //
 // A block (one per SM, persistent) computes 128 outputs x kRows rows of x.  A unit of work is one group: its sums
-// have two buffers in tensor memory, so that the tensor core fills one while the other is drained.  Warps:
+// have two buffers in tensor memory (four up to 64 rows), so that the tensor core fills one while another is drained.  Warps:
 //   promotion  8 (4 up to 64 rows): a thread holds the sums of one output and up to 96 rows of x
 //   expansion  8: a thread expands one weight row, 64 columns at a time, from shared straight into tensor memory
 //   one issues the products, one copies the packed weights into a deep ring in shared memory (bulk copies), one the
@@ -37,7 +37,7 @@ using namespace umma;
 constexpr int kTileN = 128;                  // outputs (weight rows) of a tile: the lanes of tensor memory
 constexpr int kChunk = 64;                   // columns of a stage
 constexpr int kACols = kChunk / 2;           // tensor-memory columns of a chunk of expanded weights
-constexpr int kMaxStages = 8, kWeightStages = 8;
+constexpr int kMaxStages = 8, kWeightStages = 8, kMaxBufs = 4;
 constexpr uint32_t kWeightChunk = 4096;      // a chunk of packed weights: 8 tiles of 16 x 64
 constexpr uint32_t kWeightStage = 2 * kWeightChunk;            // chunks of two expanding sets
 constexpr uint32_t kCtrlBytes = 1024;
@@ -52,7 +52,8 @@ struct Shape {
   static constexpr int kOther = kCopies ? 4 : 8, kLoadWarps = kOther - 2;
   static constexpr int kMmaWarp = 4 * (kPromo + kExpand), kWeightWarp = kMmaWarp + 1, kLoadWarp = kMmaWarp + 2;
   static constexpr int kThreads = 32 * (kMmaWarp + kOther);
-  static constexpr int kATmem = kRows > 128 ? 2 * kRows : 256; // behind the two accumulators
+  static constexpr int kBufs = kRows > 64 ? 2 : 4;             // accumulators
+  static constexpr int kATmem = kRows > 128 ? 2 * kRows : 256; // behind them
   static constexpr int kStages = (512 - kATmem) / kACols;      // chunks: weights in tensor memory, rows of x in shared
   static constexpr uint32_t kStage = kRows * kChunk * 2;       // a row of x: 128 bytes, swizzled
   static constexpr uint32_t kScaleBytes = 8 * (512 + kAhead * 128);          // per promotion warp: a group's scales of x, its outputs' of groups ahead
@@ -86,8 +87,8 @@ __device__ __forceinline__ Smem carve(uint8_t *smem, uint32_t scale_bytes) {
   s.wfull = s.empty + 8 * kMaxStages;
   s.wempty = s.wfull + 8 * kWeightStages;
   s.dfull = s.wempty + 8 * kWeightStages;
-  s.dempty = s.dfull + 16;
-  s.tmem_slot = reinterpret_cast<uint32_t *>(smem + 16 * kMaxStages + 16 * kWeightStages + 32);
+  s.dempty = s.dfull + 8 * kMaxBufs;
+  s.tmem_slot = reinterpret_cast<uint32_t *>(smem + 16 * (kMaxStages + kWeightStages + kMaxBufs));
   s.abort_flag = reinterpret_cast<volatile int *>(s.tmem_slot + 1);
   s.scales = s.full + kCtrlBytes;
   s.weights = s.scales + scale_bytes;
@@ -175,7 +176,7 @@ __device__ __forceinline__ void mma_loop(const TcParams &P, const Smem &S, const
   const uint64_t desc0 = swizzled_desc(S.ring);
   const int n = span.c1 - span.c0, units = span.u1 - span.u0;
   Parities<Sh::kStages> par(n);
-  uint32_t dpar = 3u;                              // the accumulators: drained at first
+  uint32_t dpar = (1u << Sh::kBufs) - 1u;          // the accumulators: drained at first
   auto drained = [&](int buf) {
     const bool ok = wait(S, S.dempty + 8u * buf, (dpar >> buf) & 1u);
     dpar ^= 1u << buf;
@@ -195,17 +196,17 @@ __device__ __forceinline__ void mma_loop(const TcParams &P, const Smem &S, const
 #pragma unroll
       for (int s = 0; s < Sh::kStages; ++s) {
         if (c + s < n) {
-          const int buf = kGroup == 128 ? (s / 2) & 1 : s & 1;
-          if (kGroup == 32 ? !drained(0) : (kGroup == 64 || s % 2 == 0) && !drained(buf)) return;
+          const int buf = (kGroup == 128 ? s / 2 : kGroup == 64 ? s : 2 * s) % Sh::kBufs;
+          if ((kGroup != 128 || s % 2 == 0) && !drained(buf)) return;
           if (!wait(S, S.full + 8u * s, par.of(c + s))) return;
           tc_fence_after();
           if constexpr (kGroup == 32) {
-            products(s, 0, 0, 2, 0u);
-            umma_commit(S.dfull);
+            products(s, buf, 0, 2, 0u);
+            umma_commit(S.dfull + 8u * buf);
             if (2 * (c + s) + 1 < units) {
-              if (!drained(1)) return;
-              products(s, 1, 2, 2, 0u);
-              umma_commit(S.dfull + 8u);
+              if (!drained(buf + 1)) return;
+              products(s, buf + 1, 2, 2, 0u);
+              umma_commit(S.dfull + 8u * (buf + 1));
             }
           } else {
             products(s, buf, 0, 4, kGroup == 128 && s % 2 == 1 ? 1u : 0u);
@@ -617,7 +618,7 @@ __device__ __forceinline__ void promote_role(const TcParams &P, const Smem &S, c
         }
         __syncwarp();
       }
-      const uint32_t buf = (uint32_t)(u - span.u0) & 1u;
+      const uint32_t buf = (uint32_t)(u - span.u0) % Sh::kBufs;
       if (!__all_sync(0xFFFFFFFFu, wait_inline(S, S.dfull + 8u * buf, (dpar >> buf) & 1u))) {
         asm volatile("cp.async.wait_all;" ::: "memory");
         return;
@@ -703,7 +704,7 @@ w4_tc_kernel(const __grid_constant__ TcParams P) {
     // a stage is full with four expanding warps' arrivals and those that bring the rows
     for (int i = 0; i < Sh::kStages; ++i) { mbar_init(S.full + 8u * i, 4 + (kCopies ? 1 : Sh::kLoadWarps)); mbar_init(S.empty + 8u * i, 1); }
     for (int i = 0; i < kWeightStages; ++i) { mbar_init(S.wfull + 8u * i, 1); mbar_init(S.wempty + 8u * i, 8); }
-    for (int i = 0; i < 2; ++i) { mbar_init(S.dfull + 8u * i, 1); mbar_init(S.dempty + 8u * i, 4 * Sh::kPromo); }
+    for (int i = 0; i < Sh::kBufs; ++i) { mbar_init(S.dfull + 8u * i, 1); mbar_init(S.dempty + 8u * i, 4 * Sh::kPromo); }
     *S.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
