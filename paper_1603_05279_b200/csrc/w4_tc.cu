@@ -60,7 +60,7 @@ struct Shape {
   static constexpr size_t kSmem = 1024 + kCtrlBytes + kScaleBytes + kWeightStages * kWeightStage + (size_t)kStages * kStage;   // (1024: to align the ring)
   // Registers per thread as launched, and after they are dealt out anew: the promotion's hold its sums.
   static constexpr int kRegs = kThreads == 640 ? 96 : kThreads == 768 ? 80 : 72;
-  static constexpr int kPromoRegs = kRows > 128 ? 144 : kRows > 64 ? (kCopies ? 128 : 112) : kRows > 32 ? (kCopies ? 128 : 112) : 96;
+  static constexpr int kPromoRegs = kRows > 128 ? 144 : kRows > 64 ? (kCopies ? 128 : 112) : kRows > 32 ? (kCopies ? 128 : 112) : 120;
   static constexpr int kOtherRegs = kRows > 128 ? 64 : kRows > 64 ? (kCopies ? 72 : 64) : kCopies ? (kRows > 32 ? 64 : 72) : 64;
   static_assert(kPromo * 128 * kPromoRegs + (kThreads - kPromo * 128) * kOtherRegs <= kThreads * kRegs, "registers");
   static_assert(kSmem <= 232448 && kStages <= kMaxStages && (kStages & (kStages - 1)) == 0, "shared and tensor memory");
@@ -577,6 +577,8 @@ __device__ __forceinline__ void promote_role(const TcParams &P, const Smem &S, c
   // (32 rows times 16384x16384 69.9 -> 56.2 us, with four expanding sets).  Many rows have the time of one group's
   // products for a load from the L2, and no slots to spare (2048 rows times 8192x8192 234 us, 240 with the ring).
   constexpr bool kRing = kRows <= 64;
+  // Two groups at a time where their sums fit the registers: a group's waits and loads follow each other.
+  constexpr int kPair = kRows <= 32 ? 2 : 1;
   // A group's scale of this output, into its place of the ring; a copy or none, so that the copies count the groups
   auto ahead = [&](int u, int nc) {
     if (u < span.u1)
@@ -594,66 +596,100 @@ __device__ __forceinline__ void promote_role(const TcParams &P, const Smem &S, c
     float next = 0.0f;
     if constexpr (kRing) {
 #pragma unroll
-      for (int i = 0; i < kAhead - 1; ++i) ahead(span.u0 + i, nc);
+      for (int i = 0; i < kAhead - kPair; ++i) ahead(span.u0 + i, nc);
     } else {
       if (span.u0 < span.u1) next = load_global(A.scales + (size_t)span.u0 * N + nc);
     }
 #pragma unroll 1
-    for (int u = span.u0; u < span.u1; ++u) {
-      float s = next;
+    for (int u = span.u0; u < span.u1; u += kPair) {
+      float s[kPair];
+      s[0] = next;
       if constexpr (kRing) {
-        ahead(u + kAhead - 1, nc);
-        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
-        s = __uint_as_float(lds32(my_ring + 128u * ((uint32_t)u % kAhead)));  // (each lane reads what it copied)
+#pragma unroll
+        for (int h = 0; h < kPair; ++h) ahead(u + kAhead - kPair + h, nc);
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - kPair) : "memory");
+#pragma unroll
+        for (int h = 0; h < kPair; ++h) s[h] = __uint_as_float(lds32(my_ring + 128u * ((uint32_t)(u + h) % kAhead)));  // (each lane reads what it copied)
       } else {
         if (u + 1 < span.u1) next = load_global(A.scales + (size_t)(u + 1) * N + nc);
       }
+      const int count = kPair == 1 ? 1 : min(kPair, span.u1 - u);
       if (x_groups) {
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < (kUnit + 31) / 32; ++i) {
-          const int col = lane + 32 * i;
-          const float v = col < kUnit && tok0 + col < A.r.rows ? load_global(A.x_scales + (tok0 + col) * G + u) : 0.0f;
-          if (col < kUnit) sts32(my_scales + 4u * col, __float_as_uint(v));
+        for (int i = 0; i < (kPair * kUnit + 31) / 32; ++i) {
+          const int at = lane + 32 * i, col = at % kUnit, h = at / kUnit;
+          const float v = h < count && tok0 + col < A.r.rows ? load_global(A.x_scales + (tok0 + col) * G + u + h) : 0.0f;
+          if (h < kPair) sts32(my_scales + 4u * at, __float_as_uint(v));
         }
         __syncwarp();
       }
       const uint32_t buf = (uint32_t)(u - span.u0) % Sh::kBufs;
-      if (!__all_sync(0xFFFFFFFFu, wait_inline(S, S.dfull + 8u * buf, (dpar >> buf) & 1u))) {
+      bool ok = true;
+#pragma unroll
+      for (int h = 0; h < kPair; ++h)
+        if (h < count) {
+          ok = ok && wait_inline(S, S.dfull + 8u * (buf + h), (dpar >> (buf + h)) & 1u);
+          dpar ^= 1u << (buf + h);
+        }
+      if (!__all_sync(0xFFFFFFFFu, ok)) {
         asm volatile("cp.async.wait_all;" ::: "memory");
         return;
       }
-      dpar ^= 1u << buf;
       tc_fence_after();
-      // 16 values at a time; the next load is under way while these are added
       constexpr int kLoad = 16, kLoads = kUnit / kLoad;
       const uint32_t from = t_lane + buf * (uint32_t)kRows + (uint32_t)(set * kUnit);
-      int32_t vs[2][kLoad];
-      tmem_ld16(from, vs[0]);
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        int32_t (&v)[kLoad] = vs[j & 1];
-        tmem_wait16(v);
-        if (j + 1 < kLoads) {
-          tmem_ld16(from + (uint32_t)(kLoad * (j + 1)), vs[(j + 1) & 1]);
-        } else {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(S.dempty + 8u * buf);
-        }
+      auto release = [&](int h) {
+        if (lane == 0) mbar_arrive(S.dempty + 8u * (buf + h));
+      };
+      auto add = [&](int j, int h, const int32_t (&v)[kLoad]) {
         if (x_groups) {
 #pragma unroll
           for (int i = 0; i < kLoad / 4; ++i) {
-            const float4 f = lds_f4(my_scales + (uint32_t)(4 * kLoad * j + 16 * i));
+            const float4 f = lds_f4(my_scales + (uint32_t)(4 * kUnit * h + 4 * kLoad * j + 16 * i));
             float *to = acc + kLoad * j + 4 * i;
-            to[0] = fmaf(__int_as_float(v[4 * i]) * f.x, s, to[0]);
-            to[1] = fmaf(__int_as_float(v[4 * i + 1]) * f.y, s, to[1]);
-            to[2] = fmaf(__int_as_float(v[4 * i + 2]) * f.z, s, to[2]);
-            to[3] = fmaf(__int_as_float(v[4 * i + 3]) * f.w, s, to[3]);
+            to[0] = fmaf(__int_as_float(v[4 * i]) * f.x, s[h], to[0]);
+            to[1] = fmaf(__int_as_float(v[4 * i + 1]) * f.y, s[h], to[1]);
+            to[2] = fmaf(__int_as_float(v[4 * i + 2]) * f.z, s[h], to[2]);
+            to[3] = fmaf(__int_as_float(v[4 * i + 3]) * f.w, s[h], to[3]);
           }
         } else {
 #pragma unroll
-          for (int i = 0; i < kLoad; ++i) acc[kLoad * j + i] = fmaf(__int_as_float(v[i]), s, acc[kLoad * j + i]);
+          for (int i = 0; i < kLoad; ++i) acc[kLoad * j + i] = fmaf(__int_as_float(v[i]), s[h], acc[kLoad * j + i]);
+        }
+      };
+      if constexpr (kPair == 2) {
+        int32_t vs[2][kLoads][kLoad];
+#pragma unroll
+        for (int j = 0; j < 2 * kLoads; ++j)       // (a group that does not exist: the first again, not added)
+          tmem_ld16(from + (uint32_t)((j / kLoads < count ? j / kLoads : 0) * kRows + kLoad * (j % kLoads)), vs[j / kLoads][j % kLoads]);
+#pragma unroll
+        for (int j = 0; j < 2 * kLoads; ++j) tmem_wait16(vs[j / kLoads][j % kLoads]);
+        tc_fence_before();
+        __syncwarp();
+        release(0);
+        if (count == 2) release(1);
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) add(j, 0, vs[0][j]);
+        if (count == 2) {
+#pragma unroll
+          for (int j = 0; j < kLoads; ++j) add(j, 1, vs[1][j]);
+        }
+      } else {
+        // 16 values at a time; the next load is under way while these are added
+        int32_t vs[2][kLoad];
+        tmem_ld16(from, vs[0]);
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+          tmem_wait16(vs[j & 1]);
+          if (j + 1 < kLoads) {
+            tmem_ld16(from + (uint32_t)(kLoad * (j + 1)), vs[(j + 1) & 1]);
+          } else {
+            tc_fence_before();
+            __syncwarp();
+            release(0);
+          }
+          add(j, 0, vs[j & 1]);
         }
       }
     }
