@@ -199,6 +199,17 @@ def test_product_of_every_kernel(xname, group, T, N, K):
 
 
 @pytest.mark.parametrize("xname", ["bf16", "f16", "i8", "e4m3"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("T", [12, 30, 50, 100])
+def test_product_of_several_tiles_per_block(xname, group, T):
+    """More tiles than a GPU has SMs, with odd and even numbers of groups and of blocks of columns."""
+    for K in (97, 161, 200, 328):
+        x, xs, each, codes, scales, zs = operands(T, 20001, K, group, K % 2 == 0, xname, T + K, K > 180)
+        out = product(x, xs, codes, scales, zs, group, torch.float16 if xname == "f16" else torch.float32)
+        check_product(x, each, codes, scales, zs, group, out)
+
+
+@pytest.mark.parametrize("xname", ["bf16", "f16", "i8", "e4m3"])
 @pytest.mark.parametrize("T", [1, 5, 20, 70, 200])
 def test_product_of_rows_apart(xname, T):
     """Rows of x at strides that are and are not multiples of 16 bytes; what lies between out's rows stays."""
