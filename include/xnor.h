@@ -431,7 +431,11 @@ typedef enum {
  *   rstd      out  fp32 [rows] or NULL: what the backward pass needs
  * xnor_rmsnorm_quant writes y in 8 bits instead, without rounding it in between:
  *   scale = max|y| / top over the group, q = y / scale to nearest even, top = 127 (I8) or 448 (E4M3)
- *   (scale and quotient within a few fp32 roundings of that)
+ *   The scale is within a few fp32 roundings of that.  rstd is in y and in the scale, so q is formed without
+ *   it, from the fp32 products p = h weight: top p / max|p| is rounded to fp32 (correctly), then to q_type, ties to
+ *   even.  Where the products are exact (16-bit rows with weights of their type or none) quotients that lie
+ *   between two outputs are thus recognised as such.  (Groups whose norm stays below 2^-89 are divided by the
+ *   scale as it is stored.)
  *   q         out  q_type [rows][cols], dense
  *   scales    out  fp32 [rows][cols / group], dense; group = 0: one scale for a whole row, [rows]
  *   A group of zeros has the scale 0.  A group with an infinity or NaN in it has such a scale (so that

@@ -6,6 +6,7 @@
 // fewer warps for the same work).  The backward pass, which has the sums of the weight's gradient in its registers too,
 // needs that ring for long rows in numbers (4096x4096 39 -> 34 us): persistent blocks, one row at a time.
 #include <algorithm>
+#include <type_traits>
 
 #include "rows.cuh"
 #include "umma_common.cuh"
@@ -50,15 +51,6 @@ struct Max {
   }
 };
 
-// 1 / sqrt(v): an approximation and one step of Newton's method, within two roundings; 0, infinite and NaN as they come.
-// (Every thread of a row forms it.)
-__device__ __forceinline__ float inverse_root(float v) {
-  float r;
-  asm("rsqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
-  const float better = fmaf(0.5f * r, fmaf(-v * r, r, 1.0f), r);
-  return r > 0.0f && r <= 3.402823466e38f ? better : r;
-}
-
 // Eight weights: ones (kind 0), in 32 bits (1) or of the rows' type (2).
 template <class T>
 __device__ __forceinline__ void load_weights(const void *w, int kind, int c, int in, float (&v)[8]) {
@@ -80,29 +72,55 @@ int weight_kind(const void *w, const xnor_norm_desc &d) {
   return w == nullptr ? 0 : d.weight_type == XNOR_F32 ? 1 : 2;
 }
 
-// The scale of a group whose largest magnitude is v, and what its values are multiplied with.  Both are within
-// two roundings of v / top and its reciprocal, at a few instructions (two IEEE divisions took a tenth of the time of
-// e4m3 rows); where the reciprocal would overflow or the scale lose bits, they are divided.
-__device__ __forceinline__ float scale_of(float v, bool i8, float &inv) {
-  const float top = i8 ? 127.0f : 448.0f;
-  if (v < 0x1p-110f && v > 0.0f) {
-    inv = -1.0f;
-    return __fdiv_rn(v, top);
-  }
-  float r;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
-  inv = v > 0.0f && v <= 3.402823466e38f ? top * r : 0.0f;        // a group of zeros, infinite or NaN: zeros (NaN)
-  return v * (i8 ? 1.0f / 127.0f : 1.0f / 448.0f);
+// A row's root in two factors: the power of two that is in it, by which values are scaled without a rounding, and the rest,
+// 1 to 2.  0, infinite and NaN roots are the first.
+__device__ __forceinline__ float power_of(float rstd, float &rest) {
+  const bool sound = rstd > 0.0f && rstd <= 3.402823466e38f;
+  rest = sound ? __uint_as_float((__float_as_uint(rstd) & 0x007FFFFFu) | 0x3F800000u) : 1.0f;
+  return sound ? __uint_as_float(__float_as_uint(rstd) & 0x7F800000u) : rstd;
 }
-__device__ __forceinline__ void divide(float (&y)[8], float s, float inv) {
-  if (inv < 0.0f) {
+
+// The values of a group as 8-bit outputs want them.  u = h weight times a power of two, m = max|u|: the row's root is in both, so
+// that q is the rounding of top u / m.  16-bit h and weight often put that exactly between two outputs (243 of 2 M e4m3
+// quotients of normal bf16 rows), where an approximate quotient would decide by chance.  So quotients are rounded to fp32 correctly, by
+// Markstein's correction of an approximate one with its residual (1990), a multiply-add each.  Where top u has more than 24
+// bits (all but bf16 rows with bf16 weights or none) its rest is added to the residual.  (2048x4096 bf16 to e4m3 17.6 us, 16.3
+// with approximate quotients, 17.9 with the rest added throughout and the scale by an IEEE division.)
+struct Quotients {
+  float part, divisor, inv, scale;         // top and m, both 2^-9 of it; 1 / divisor
+  bool tiny;                               // the scale loses bits, or is near to that: divided by as it is
+  __device__ __forceinline__ Quotients(float m, float rest, bool i8) {
+    const float over = i8 ? 512.0f / 127.0f : 512.0f / 448.0f;
+    const bool sound = m > 0.0f && m <= 3.402823466e38f;                // else zeros (NaN)
+    tiny = m > 0.0f && m < 0x1p-90f;
+    part = (i8 ? 127.0f : 448.0f) * 0x1p-9f;
+    divisor = sound ? m * 0x1p-9f : 0.0f;
+    const float largest = divisor * rest, s = __fmul_rn(largest, over);
+    scale = sound ? __fmaf_rn(__fmaf_rn(-s, part, largest), over, s) : m;
+    if (tiny) scale = __fdiv_rn(m * rest, i8 ? 127.0f : 448.0f);
+    float r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(divisor));
+    inv = sound ? r : 0.0f;
+  }
+  __device__ __forceinline__ void divide(float (&u)[8], float rest, bool wide) const {
+    if (tiny) {
 #pragma unroll 1
-    for (int i = 0; i < 8; ++i) y[i] = s > 0.0f ? y[i] / s : 0.0f;
-    return;
-  }
+      for (int i = 0; i < 8; ++i) u[i] = scale > 0.0f ? __fdiv_rn(u[i] * rest, scale) : 0.0f;
+    } else if (wide) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] *= inv;
-}
+      for (int i = 0; i < 8; ++i) {
+        const float n = __fmul_rn(part, u[i]), t = __fmul_rn(n, inv);
+        u[i] = __fmaf_rn(__fadd_rn(__fmaf_rn(-t, divisor, n), __fmaf_rn(part, u[i], -n)), inv, t);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float n = __fmul_rn(part, u[i]), t = __fmul_rn(n, inv);
+        u[i] = __fmaf_rn(__fmaf_rn(-t, divisor, n), inv, t);
+      }
+    }
+  }
+};
 
 __device__ __forceinline__ uint32_t pack_i8(float a, float b, float c, float d) {
   auto q = [](float v) { return (uint32_t)(uint8_t)(int8_t)min(127, max(-127, __float2int_rn(v))); };
@@ -115,7 +133,7 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
 }
 
 // Forward: what follows the loads of a row.  Chunk c = rank + v * team of a row belongs to one thread; kV chunks per
-// thread cover the row.  `read` is called when every thread of the block has its values.
+// thread cover the row.
 template <class T, int kV, bool kQuant>
 __device__ __forceinline__ void finish_row(const NormArgs &A, const Team &team, long long row, bool real, const int (&in)[kV], Chunk<T> (&xc)[kV],
                                            const Chunk<T> (&rc)[kV], const float (&wc)[kV][8], int weights, int pieces, float *red,
@@ -145,15 +163,17 @@ __device__ __forceinline__ void finish_row(const NormArgs &A, const Team &team, 
     for (int v = 0; v < kV; ++v) xc[v].store(sum + 8 * (team.rank + v * team.size), pieces, in[v]);
   }
   ss = team.reduce(ss, red, Add());
-  const float rstd = inverse_root(fmaf(ss, A.per_col, A.d.eps));
+  const float rstd = __frsqrt_rn(fmaf(ss, A.per_col, A.d.eps));
   if (A.rstd && real && team.rank == 0) A.rstd[row] = rstd;
+  float rest = 1.0f;                          // (8 bits: of the row's root)
+  const float root = kQuant ? power_of(rstd, rest) : rstd;
   auto normed = [&](int v, float (&y)[8]) {
     xc[v].to_float(y);
     float late[8];
     if constexpr (kV > 2) load_weights<T>(A.weight, weights, 8 * (team.rank + v * team.size), in[v], late);     // (long rows: not held over the sum)
     const float *w = kV > 2 ? late : wc[v];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = y[i] * rstd * w[i];
+    for (int i = 0; i < 8; ++i) y[i] = y[i] * root * w[i];
   };
   if constexpr (!kQuant) {
     T *y = static_cast<T *>(A.y) + (real ? row * A.d.y_stride : 0);
@@ -197,16 +217,15 @@ __device__ __forceinline__ void finish_row(const NormArgs &A, const Team &team, 
 #pragma unroll
     for (int v = 0; v < kV; ++v) {
       const int chunk = team.rank + v * team.size;
-      float inv;
-      const float s = scale_of(m[v], i8, inv);
+      const Quotients of(m[v], rest, i8);
       if (A.group == 0) {
-        if (v == 0 && team.rank == 0 && real) A.scales[row] = s;
+        if (v == 0 && team.rank == 0 && real) A.scales[row] = of.scale;
       } else if (in[v] > 0 && (chunk & (lanes - 1)) == 0) {
-        A.scales[row * (D >> lg) + (chunk >> (lg - 3))] = s;
+        A.scales[row * (D >> lg) + (chunk >> (lg - 3))] = of.scale;
       }
       float (&y)[8] = u[kV <= 2 ? v : 0];
       if constexpr (kV > 2) normed(v, y);
-      divide(y, s, inv);
+      of.divide(y, rest, !std::is_same<T, __nv_bfloat16>::value || weights == 1);
       const uint32_t lo = i8 ? pack_i8(y[0], y[1], y[2], y[3]) : pack_e4m3(y[0], y[1], y[2], y[3]);
       const uint32_t hi = i8 ? pack_i8(y[4], y[5], y[6], y[7]) : pack_e4m3(y[4], y[5], y[6], y[7]);
       if ((D & 7) == 0) {
