@@ -497,7 +497,8 @@ xnor_status xnor_rmsnorm_backward(const void *dy, const void *dsum, const void *
  * xnor_w4_quantize   w type [N][K] (F32, BF16, F16) -> w_packed, scales, zeros.
  *     zeros NULL: scale = max|w| / 7, code = w / scale + 8; else with lo = min(w, 0) and hi = max(w, 0)
  *     over the group scale = (hi - lo) / 15, zero = -lo / scale, code = w / scale + zero.  scale is
- *     rounded to fp32, the quotients to the nearest whole number, exactly, ties to even.  A group of
+ *     rounded to fp32, the quotients to the nearest whole number, exactly, ties to even; codes and zeros
+ *     are held to 0 .. 15 (which matters where the scale is a few units of fp32's least number).  A group of
  *     zeros has the scale 0; one with an infinity or NaN such a scale.
  * xnor_w4_pack        codes u8 [N][K], 0 .. 15 (higher bits are ignored) -> w_packed: weights that
  *     were quantised elsewhere.

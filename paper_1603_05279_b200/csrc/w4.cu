@@ -37,12 +37,13 @@ __device__ __forceinline__ float mend_quotient(float q, float w, float s) {
 __device__ __forceinline__ float round_quotient(float w, float s) { return mend_quotient(rintf(w / s), w, s); }
 
 // The same of kN values.  With the reciprocal the guess is within 2e-6 of the quotient (at most 16), so only guesses that
-// close to a border can be wrong; all are mended then.  (inv = 0: it would overflow.)
+// close to a border can be wrong; all are mended then.  (inv = 0: it would overflow.  Such a scale may be a few units of
+// fp32's least number, so far from a seventh or a 15th that quotients leave the codes' range: -zero .. 15 - zero.)
 template <int kN>
-__device__ __forceinline__ void round_quotients(const float (&w)[kN], float s, float inv, float (&q)[kN]) {
+__device__ __forceinline__ void round_quotients(const float (&w)[kN], float s, float inv, float zero, float (&q)[kN]) {
   if (inv == 0.0f) {
 #pragma unroll 1
-    for (int i = 0; i < kN; ++i) q[i] = round_quotient(w[i], s);
+    for (int i = 0; i < kN; ++i) q[i] = fminf(15.0f - zero, fmaxf(-zero, round_quotient(w[i], s)));
     return;
   }
   float far = 0.0f;
@@ -124,14 +125,14 @@ w4_quantize_kernel(const T *w, const xnor_w4_desc d, int lg, int pieces, uint32_
     const float inv = sound && s > 1e-37f ? 1.0f / s : 0.0f;      // 0: it would overflow
     if (kZeros && sound) z = fminf(15.0f, fmaxf(0.0f, round_quotient(-lo, s)));
     if (sound) {
-      round_quotients(v, s, inv, q);
+      round_quotients(v, s, inv, z, q);
     } else {
 #pragma unroll
       for (int i = 0; i < 16; ++i) q[i] = 0.0f;
     }
     if constexpr (kZeros) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) q[i] = fminf(q[i] + z, 15.0f);          // (at least 0: z rounds as the least value does)
+      for (int i = 0; i < 16; ++i) q[i] = fminf(q[i] + z, 15.0f);          // (at least 0: z rounds as the least value does, or the quotient is cut)
     }
     const float base = kZeros ? 8388608.0f : 8388608.0f + 8.0f * 4369.0f;  // 2^23, and a zero point of 8 in every code
 #pragma unroll
