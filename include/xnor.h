@@ -426,8 +426,9 @@ typedef enum {
  *   residual  in   type [rows][cols] or NULL
  *   weight    in   weight_type [cols] or NULL (ones)
  *   sum       out  type [rows][cols] or NULL: h, what the next layers add to.  May be the same
- *                  buffer as x or residual (with the same stride)
- *   y         out  type [rows][cols]; may be the same buffer as x or residual
+ *                  buffer as x or residual, with the same stride
+ *   y         out  type [rows][cols]; likewise, but not the same buffer as sum
+ * Other overlaps of what is written with what is read or written are not allowed.
  *   rstd      out  fp32 [rows] or NULL: what the backward pass needs
  * xnor_rmsnorm_quant writes y in 8 bits instead, without rounding it in between:
  *   scale = max|y| / top over the group, q = y / scale to nearest even, top = 127 (I8) or 448 (E4M3)
@@ -442,7 +443,7 @@ typedef enum {
  *   all it stands for is NaN or infinite).
  *
  * INVALID_ARG: null (where not allowed) or misaligned pointer, rows < 0, cols < 1, a stride out of
- * range, type none of F32, BF16, F16, weight_type neither F32 nor type, eps negative or not a number,
+ * range, the same buffer with another stride or for sum and y, type none of F32, BF16, F16, weight_type neither F32 nor type, eps negative or not a number,
  * q_type neither I8 nor E4M3, group none of 0, 32, 64, 128.  UNSUPPORTED: cols > 32768; cols not a
  * multiple of group.
  */
@@ -471,7 +472,8 @@ xnor_status xnor_rmsnorm_quant(const void *x, const void *residual, const void *
  *   h        in   type [rows][cols], stride x_stride: the forward call's sum (x without a residual)
  *   weight   in   as in the forward call
  *   rstd     in   fp32 [rows], from the forward call
- *   dx       out  type [rows][cols], stride sum_stride; may be the same buffer as dy or dsum
+ *   dx       out  type [rows][cols], stride sum_stride; may be the same buffer as dy or dsum, with the
+ *                 same stride
  *   dweight  out  fp32 [cols] or NULL (then work may be NULL too)
  *   work     scratch of xnor_rmsnorm_work_elems(rows, cols) floats; calls that can overlap (other
  *                 streams, two graphs) need one each

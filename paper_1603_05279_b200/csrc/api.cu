@@ -460,6 +460,14 @@ xnor_status check_norm_forward(const void *x, const void *residual, const void *
   return s;
 }
 
+// Whether a tensor that is written in the place of one that is read has its rows elsewhere than that.
+bool other_rows(const void *out, long long out_stride, const void *in, long long in_stride, int rows) {
+  return out != nullptr && out == in && rows > 1 && out_stride != in_stride;
+}
+bool bad_place(const void *out, long long stride, const void *x, const void *residual, const xnor_norm_desc *d) {
+  return other_rows(out, stride, x, d->x_stride, d->rows) || other_rows(out, stride, residual, d->residual_stride, d->rows);
+}
+
 bool bad_w4(const xnor_w4_desc *d) {
   return !d || d->N < 1 || d->K < 1 || (d->group != 32 && d->group != 64 && d->group != 128);
 }
@@ -474,6 +482,8 @@ xnor_status xnor_rmsnorm(const void *x, const void *residual, const void *weight
   if (s == XNOR_ERR_INVALID_ARG) return s;
   if (d->rows > 0 && bad_write(y, d->y_stride, d->rows, d->cols)) return XNOR_ERR_INVALID_ARG;
   if (s != XNOR_OK) return s;
+  if (d->rows > 0 && (sum == y || bad_place(sum, d->sum_stride, x, residual, d) || bad_place(y, d->y_stride, x, residual, d)))
+    return XNOR_ERR_INVALID_ARG;
   return from_cuda(xnor::launch_rmsnorm({x, residual, weight, sum, y, rstd, nullptr, nullptr, 0, 0, *d, 1.0f / (float)d->cols},
                                         (cudaStream_t)cuda_stream));
 }
@@ -488,6 +498,7 @@ xnor_status xnor_rmsnorm_quant(const void *x, const void *residual, const void *
   if (d->rows > 0 && (bad_ptr(q) || bad_ptr(scales))) return XNOR_ERR_INVALID_ARG;
   if (s != XNOR_OK) return s;
   if (group != 0 && d->cols % group != 0) return XNOR_ERR_UNSUPPORTED;
+  if (bad_place(sum, d->sum_stride, x, residual, d)) return XNOR_ERR_INVALID_ARG;
   return from_cuda(xnor::launch_rmsnorm({x, residual, weight, sum, nullptr, rstd, q, scales, q_type, group, *d, 1.0f / (float)d->cols},
                                         (cudaStream_t)cuda_stream));
 }
@@ -507,6 +518,8 @@ xnor_status xnor_rmsnorm_backward(const void *dy, const void *dsum, const void *
                       bad_ptr(rstd) || bad_write(dx, d->sum_stride, d->rows, d->cols) || (dweight && bad_ptr(work))))
     return XNOR_ERR_INVALID_ARG;
   if (s != XNOR_OK) return s;
+  if (other_rows(dx, d->sum_stride, dy, d->y_stride, d->rows) || other_rows(dx, d->sum_stride, dsum, d->residual_stride, d->rows))
+    return XNOR_ERR_INVALID_ARG;
   return from_cuda(xnor::launch_rmsnorm_backward({dy, dsum, h, weight, rstd, dx, dweight, work, *d, 1.0f / (float)d->cols}, (cudaStream_t)cuda_stream));
 }
 

@@ -175,3 +175,21 @@ def test_layout_helpers_agree(group):
     for N, K in ((1, 1), (17, 65), (40, 200)):
         codes = rng.integers(0, 16, (N, K), dtype=np.uint8)
         assert (unpack_codes(pack_codes(codes), N, K) == codes).all()
+
+
+def test_the_same_buffer_wants_the_same_rows():
+    """Rows of one buffer at two strides would be read after others had been written over them.  (Nothing is launched here:
+    calls that are in order are made on a GPU by the tests of the operators.)"""
+    lib = X.load()
+    a, b, c, e = (ctypes.c_void_p(n << 20) for n in (1, 2, 3, 4))
+    fwd = lambda d, s, y: lib.xnor_rmsnorm(a, b, NULL, d, s, y, NULL, NULL)
+    for out, stride in ((a, "x_stride"), (b, "residual_stride")):
+        for apart in (0, 128):                        # one row for all, or rows apart
+            d = norm(**{stride: apart})
+            assert fwd(d, c, out) == INV and fwd(d, NULL, out) == INV and fwd(d, out, c) == INV
+            assert lib.xnor_rmsnorm_quant(a, b, NULL, d, B.XNOR_I8, 32, out, c, e, NULL, NULL) == INV
+    assert fwd(norm(), c, c) == INV                   # two results in one place
+    bwd = lambda d, dx: lib.xnor_rmsnorm_backward(a, b, c, NULL, e, d, dx, NULL, NULL, NULL)
+    for out, stride in ((a, "y_stride"), (b, "residual_stride")):
+        for apart in (0, 128):
+            assert bwd(norm(**{stride: apart}), out) == INV
