@@ -273,6 +273,10 @@ class TokenBlock:
     "i8_groups" or "e4m3_groups" (a scale for each of the weights' groups)."""
 
     def __init__(self, rows, K, N, group=128, zeros=False, quant=None, eps=1e-5, device="cuda"):
+        if quant not in (None, "i8", "e4m3", "i8_groups", "e4m3_groups"):
+            raise ValueError("quant: None, 'i8', 'e4m3', 'i8_groups' or 'e4m3_groups', not %r" % (quant,))
+        if quant is not None and quant.endswith("_groups") and K % group:
+            raise ValueError("scales of groups want K (%d) in whole groups of %d" % (K, group))
         bf16 = dict(dtype=torch.bfloat16, device=device)
         self.eps, self.d = eps, B.make_w4_desc(N, K, group)
         self.x, self.residual = torch.empty((rows, K), **bf16), torch.empty((rows, K), **bf16)

@@ -193,3 +193,19 @@ def test_the_same_buffer_wants_the_same_rows():
     for out, stride in ((a, "y_stride"), (b, "residual_stride")):
         for apart in (0, 128):
             assert bwd(norm(**{stride: apart}), out) == INV
+
+
+@pytest.mark.parametrize("quant", ["int8", "e4m3_rows", "", "E4M3", 8])
+def test_token_block_wants_a_known_kind_of_rows(quant):
+    from paper_1603_05279_b200.runner import TokenBlock
+    with pytest.raises(ValueError):
+        TokenBlock(2, 64, 32, group=32, quant=quant, device="cpu")
+
+
+def test_token_block_wants_whole_groups():
+    from paper_1603_05279_b200.runner import TokenBlock
+    for quant in ("i8_groups", "e4m3_groups"):
+        with pytest.raises(ValueError):
+            TokenBlock(2, 100, 32, group=64, quant=quant, device="cpu")
+        assert TokenBlock(2, 128, 32, group=64, quant=quant, device="cpu").q_scales.shape == (2, 2)
+    assert TokenBlock(2, 100, 32, group=64, quant="i8", device="cpu").q_scales.shape == (2, 1)
