@@ -533,7 +533,7 @@ xnor_status xnor_w4_dequantize(const uint32_t *w_packed, const float *scales, co
  * that depends on the sizes alone.  Up to 16 rows run on warp-level products whose weights go straight
  * into registers, more on the 5th-generation tensor cores.  Device-side waits are bounded as in
  * xnor_conv2d_forward (xnor_check_device); so are those of xnor_rmsnorm_backward.
- * INVALID_ARG as above, and for x_scales that are missing or not wanted.  UNSUPPORTED: F32 rows, an
+ * INVALID_ARG as above, for x_scales that are missing or not wanted, and for out in the place of x.  UNSUPPORTED: F32 rows, an
  * x_group that is neither 0 nor the weights' group, rows > 1048560.
  */
 typedef struct {

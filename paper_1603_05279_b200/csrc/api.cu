@@ -563,6 +563,7 @@ xnor_status xnor_w4_matmul(const void *x, const float *x_scales, const uint32_t 
     return XNOR_ERR_INVALID_ARG;
   if (large_w4(d) || r->rows > 16 * 65535 || r->x_type == XNOR_F32 || (bytes && r->x_group != 0 && r->x_group != d->group))
     return XNOR_ERR_UNSUPPORTED;
+  if (r->rows > 0 && out == x) return XNOR_ERR_INVALID_ARG;       // blocks write outputs of rows that others still read
   const xnor::W4Args a = {x, x_scales, w_packed, scales, zeros, out, *d, *r};
   return from_cuda(xnor::w4_few_rows(*d, r->rows) ? xnor::launch_w4_few_rows(a, (cudaStream_t)cuda_stream)
                                                : xnor::launch_w4_many_rows(a, (cudaStream_t)cuda_stream));

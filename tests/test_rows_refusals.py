@@ -209,3 +209,11 @@ def test_token_block_wants_whole_groups():
             TokenBlock(2, 100, 32, group=64, quant=quant, device="cpu")
         assert TokenBlock(2, 128, 32, group=64, quant=quant, device="cpu").q_scales.shape == (2, 2)
     assert TokenBlock(2, 100, 32, group=64, quant="i8", device="cpu").q_scales.shape == (2, 1)
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_a_product_in_the_place_of_its_rows(rows):
+    lib = X.load()
+    a, b, c, x = (ctypes.c_void_p(n << 20) for n in (1, 2, 3, 4))
+    r = ctypes.byref(B.xnor_w4_rows(rows, B.XNOR_BF16, 0, B.XNOR_BF16, 64, 64))
+    assert lib.xnor_w4_matmul(x, NULL, a, b, c, ctypes.byref(B.xnor_w4_desc(64, 64, 64)), r, x, NULL) == INV
