@@ -249,16 +249,6 @@ __device__ __forceinline__ void umma_commit_to(uint32_t bar) {
   else umma_commit_one(bar);
 }
 
-__device__ __forceinline__ uint32_t elect_one() {
-  uint32_t pred = 0;
-  asm volatile(
-      "{\n\t.reg .b32 rx;\n\t.reg .pred px;\n\t"
-      "elect.sync rx|px, %1;\n\t"
-      "@px mov.s32 %0, 1;\n\t}"
-      : "+r"(pred) : "r"(0xFFFFFFFFu));
-  return pred;
-}
-
 // 32 sign bits -> 32 e2m1 nibbles (sign in bit 3 of a nibble, magnitude code
 // 1 = 0.5, 2 = 1, 4 = 2).  Register r holds channels r, r+4, ...; a set bit is +.
 // kAct: magnitudes {2, 1, 0.5, 0.5}; otherwise {0.5, 1, 2, 2}.

@@ -84,16 +84,6 @@ __device__ __forceinline__ uint32_t fast_div(uint32_t n, uint32_t m, int s) {
   return (uint32_t)(((uint64_t)n * m) >> (31 + s));
 }
 
-__device__ __forceinline__ uint32_t elect_one() {
-  uint32_t pred = 0;
-  asm volatile(
-      "{\n\t.reg .b32 rx;\n\t.reg .pred px;\n\t"
-      "elect.sync rx|px, %1;\n\t"
-      "@px mov.s32 %0, 1;\n\t}"
-      : "+r"(pred) : "r"(0xFFFFFFFFu));
-  return pred;
-}
-
 // One MMA of 128 x NT x 16 (bf16).  One elected lane of the issuing warp runs the whole issue
 // loop (a predicate per MMA in a converged warp costs a divergence each time).
 __device__ __forceinline__ void umma_bf16(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi,

@@ -81,6 +81,17 @@ __device__ __forceinline__ uint32_t cluster_ctarank() {
   return r;
 }
 
+// 1 in one thread of the warp, whose threads all call it.
+__device__ __forceinline__ uint32_t elect_one() {
+  uint32_t pred = 0;
+  asm volatile(
+      "{\n\t.reg .b32 rx;\n\t.reg .pred px;\n\t"
+      "elect.sync rx|px, %1;\n\t"
+      "@px mov.s32 %0, 1;\n\t}"
+      : "+r"(pred) : "r"(0xFFFFFFFFu));
+  return pred;
+}
+
 // Barrier over all threads of the cluster (every thread of every CTA must reach it).
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;"

@@ -4,6 +4,7 @@
 #include <climits>
 #include <type_traits>
 
+#include "umma_common.cuh"
 #include "w4.cuh"
 
 namespace xnor {
@@ -440,7 +441,7 @@ w4_few_rows_kernel(const W4Args A, int pieces, uint32_t magic) {
     for (int i = 1; i < kFewWarps; ++i) s += part[(i * kTok + tok) * (kOut + 1) + n];
     sums[e] = s;
   }
-  if (split > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (split > 1) umma::cluster_sync();
   // (without a cluster every thread reads what it wrote itself)
   // the cluster's blocks write the outputs in turn; each adds the blocks' sums in the same order
   for (int e = rank * kFewThreads + threadIdx.x; e < toks * kOut; e += split * kFewThreads) {
@@ -463,7 +464,7 @@ w4_few_rows_kernel(const W4Args A, int pieces, uint32_t magic) {
     else if (A.r.out_type == XNOR_BF16) static_cast<__nv_bfloat16 *>(A.out)[at] = __float2bfloat16_rn(s);
     else static_cast<__half *>(A.out)[at] = __float2half_rn(s);
   }
-  if (split > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (split > 1) umma::cluster_sync();
 }
 
 template <int kType, int kN, int kR, int kGroup, bool kZeros>

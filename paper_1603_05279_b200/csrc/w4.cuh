@@ -23,8 +23,8 @@ __host__ __device__ __forceinline__ size_t w4_tile(int rt, int col_tiles) { retu
 
 __host__ __device__ __forceinline__ int w4_bit(int column) { return 4 * (column >> 1) + 16 * (column & 1); }
 
-// The eight values of a word, code - zero, as four pairs of 16-bit numbers, exact.  A code put into the mantissa of
-// 2^k is 2^k + code.  `magic` is kW4Magic of the type, but as a variable that the compiler does not know (a kernel's
+// The eight values of a word, code - zero, as four pairs of 16-bit numbers, exact.  Conversions of small whole numbers by way of
+// the mantissa are a known method: a code put into that of 2^k is 2^k + code.  `magic` is kW4Magic of the type, but as a variable that the compiler does not know (a kernel's
 // argument): a mask and an OR are one instruction if only one of them is a constant in it.  (One row times
 // 16384x8192: 24.0 -> 20.2 us.)
 template <class T>
@@ -120,12 +120,6 @@ __device__ __forceinline__ void load_x8_raw(const uint8_t *row, int k, int K, bo
     if constexpr (kB == 2) raw[i / 2] |= (uint32_t)load_global(reinterpret_cast<const uint16_t *>(p) + i) << (16 * (i & 1));
     else raw[i / 4] |= (uint32_t)load_global(p + i) << (8 * (i & 3));
   }
-}
-template <int kType>
-__device__ __forceinline__ void load_x8(const uint8_t *row, int k, int K, bool pieces, uint32_t (&v)[4]) {
-  uint32_t raw[2 * RowsOf<kType>::kBytes];
-  load_x8_raw<kType>(row, k, K, pieces, raw);
-  x8_pairs<kType>(raw, v);
 }
 
 }  // namespace xnor

@@ -153,16 +153,6 @@ __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uin
       ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-__device__ __forceinline__ uint32_t elect_one() {
-  uint32_t pred = 0;
-  asm volatile(
-      "{\n\t.reg .b32 rx;\n\t.reg .pred px;\n\t"
-      "elect.sync rx|px, %1;\n\t"
-      "@px mov.s32 %0, 1;\n\t}"
-      : "+r"(pred) : "r"(0xFFFFFFFFu));
-  return pred;
-}
-
 // ------------------------------------------------------------------ the issuing thread
 // Operand of the rows of x: 128-byte rows, swizzled in groups of eight (1024 bytes); 16 columns are 32 bytes on.
 __device__ __forceinline__ uint64_t swizzled_desc(uint32_t addr) {
@@ -724,10 +714,6 @@ __device__ __forceinline__ void promote_role(const TcParams &P, const Smem &S, c
   }
 }
 
-__device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
 template <int kType, int kRows, bool kCopies>
 __global__ void __launch_bounds__(Shape<kRows, kCopies>::kThreads, 1)
 w4_tc_kernel(const __grid_constant__ TcParams P) {
@@ -793,7 +779,7 @@ w4_tc_kernel(const __grid_constant__ TcParams P) {
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
   if (P.split == 1) return;
   // a cluster has one tile; its blocks write shares of the rows, each the sums of all in the same order
-  cluster_barrier();
+  cluster_sync();
   const int n0 = (first % P.row_tiles) * kTileN;
   const long long tok0 = (long long)(first / P.row_tiles) * kRows;
   const bool row_scale = P.A.x_scales != nullptr && P.A.r.x_group == 0;
@@ -824,7 +810,7 @@ w4_tc_kernel(const __grid_constant__ TcParams P) {
     else if (P.A.r.out_type == XNOR_BF16) store_four(s, static_cast<__nv_bfloat16 *>(P.A.out) + at, left);
     else store_four(s, static_cast<__half *>(P.A.out) + at, left);
   }
-  cluster_barrier();
+  cluster_sync();
 }
 
 // The driver's function that makes tensor maps, looked up once (no library is linked for it).
