@@ -504,7 +504,8 @@ xnor_status xnor_rmsnorm_backward(const void *dy, const void *dsum, const void *
  *     zeros has the scale 0; one with an infinity or NaN such a scale.
  * xnor_w4_pack        codes u8 [N][K], 0 .. 15 (higher bits are ignored) -> w_packed: weights that
  *     were quantised elsewhere.
- * xnor_w4_dequantize  w_packed, scales, zeros -> w type [N][K] (F32, BF16, F16), rounded once.
+ * xnor_w4_dequantize  w_packed, scales, zeros -> w type [N][K] (F32, BF16, F16): the product is rounded to
+ *     fp32, and that to the type.
  *
  * INVALID_ARG: null or misaligned pointer, N or K < 1, group none of 32, 64, 128, type out of range.
  * UNSUPPORTED: N > 1048448, K > 16777216.
@@ -530,9 +531,10 @@ xnor_status xnor_w4_dequantize(const uint32_t *w_packed, const float *scales, co
  *   w_packed, scales, zeros   as above
  *   out       out  out_type [rows][N]: F32, BF16, F16, rounded once; overlaps nothing that is read
  * code - zero and x are exact operands; the sums of a group and over the groups are fp32, in an order
- * that depends on the sizes alone.  Up to 16 rows run on warp-level products whose weights go straight
- * into registers, more on the 5th-generation tensor cores.  Device-side waits are bounded as in
- * xnor_conv2d_forward (xnor_check_device); so are those of xnor_rmsnorm_backward.
+ * that depends on the sizes, on how the rows lie and on the device's number of SMs.  Up to 8 rows, and up to 16 of matrices
+ * with N K <= 25165824, run on warp-level products whose weights go straight into registers, more on the
+ * 5th-generation tensor cores.  Device-side waits (of the latter) are bounded as in xnor_conv2d_forward
+ * (xnor_check_device); so are those of xnor_rmsnorm_backward.
  * INVALID_ARG as above, for x_scales that are missing or not wanted, and for out in the place of x.  UNSUPPORTED: F32 rows, an
  * x_group that is neither 0 nor the weights' group, rows > 1048560.
  */

@@ -524,8 +524,8 @@ struct Deal {
   int per_thread, most, team;       // team: a power of two of whole warps
 };
 enum Pass { kForward, kQuantized, kBackward };
-// Chunks per thread, measured: 8192x4096 with residual 59 us with one, 47 with two, 43.7 with four (32 bits: 51, 43.6,
-// 46.4); e4m3 2048x4096 23, 16.6, 19.2; backward 4096x4096 50 with one, 34 with two.
+// Chunks per thread, measured: 8192x4096 with residual 59 us with one, 47 with two, 43.7 with four (32 bits, 4096x4096: 51,
+// 43.6, 46.4); e4m3 2048x4096 23, 16.6, 19.2 (before its quotients were corrected); backward 4096x4096 50 with one, 34 with two.
 Deal deal(int cols, Pass pass, size_t elem) {
   const int chunks = (cols + 7) / 8;
   Deal d;
