@@ -48,8 +48,10 @@ typedef enum {
   XNOR_ERR_UNSUPPORTED = 2, /* a shape the kernels were not built for (see each call)       */
   XNOR_ERR_CUDA = 3,        /* the launch failed; the CUDA error was read and cleared        */
   XNOR_ERR_TIMEOUT = 4,     /* a bounded device-side wait gave up (see xnor_check_device)    */
-  XNOR_ERR_BOUNDS = 5       /* checking build only: a kernel computed an address outside its
-                               buffer; the access was skipped (see xnor_built_with_bounds_check) */
+  XNOR_ERR_BOUNDS = 5       /* a position, place or page in device memory lay outside its table or
+                               cache, and was left out; in the checking build also: a kernel computed
+                               an address outside its buffer; the access was skipped (see
+                               xnor_built_with_bounds_check) */
 } xnor_status;
 
 /* Geometry of one convolution layer.  Square or rectangular filters, one
@@ -547,6 +549,141 @@ xnor_status xnor_w4_matmul(const void *x, const float *x_scales, const uint32_t 
                            const xnor_w4_rows *r, void *out, void *cuda_stream);
 
 /*
+ * ---- Attention over a cache in 4 bits ------------------------------------------------------
+ * What lies between two products of a decoder's layer: norms and rotation of queries and keys, a
+ * paged cache of keys and values in 4 bits, and attention that reads it.  (No counterpart in the
+ * paper.)  Rows of heads are [rows][heads][dim], a token's heads one after the other, with a
+ * stride of their own, in elements, from row to row, as rows of tokens have: they may lie in the
+ * output of the product that made them.
+ *
+ * Positions, lengths and pages are read on the device.  What lies outside the table or the cache
+ * is left out there, and the next xnor_check_device then returns XNOR_ERR_BOUNDS once.
+ */
+
+/*
+ * Root-mean-square norm of every head of queries and keys, and the rotation by position:
+ *   x = h rstd weight, rstd = 1 / sqrt(mean over the head of h^2 + eps)   (x = h without norm),
+ *   pair i < rot / 2 of x turned by the angle that entry i of the position's row of `rope` has:
+ *   (u, v) -> (u cos - v sin, v cos + u sin); values from rot on stay.
+ * pairs = 0: pair i is values i and i + rot / 2; 1: values 2 i and 2 i + 1.  fp32, rounded once.
+ *
+ *   q, k        in   type [rows][q_heads][dim], [rows][k_heads][dim], strides q_stride, k_stride; of
+ *                    no heads: ignored
+ *   q_weight, k_weight   in   weight_type [dim] or NULL (ones); without norm ignored
+ *   positions   in   int32 [rows]; without rotation (rot = 0) ignored, as is rope
+ *   rope        in   fp32 [d->positions][rot], dense: the cosines of rot / 2 angles, then their sines
+ *   q_out, k_out  out   strides q_out_stride, k_out_stride; may be the same buffers as q and k, with
+ *                    the same strides.  Other overlaps are not allowed
+ * A token whose position is outside 0 .. d->positions - 1 is left as it is (see above).
+ *
+ * xnor_qk_norm_rope_backward: the gradients at q and k (q_out, k_out) from those at the outputs
+ * (dq_out, dk_out, strides dq_stride, dk_stride): with g = the gradient turned back, u = weight g,
+ *   dh = rstd (u - h rstd^2 mean(u h)),   dweight = sum over rows and heads of g h rstd.
+ *   dq_weight, dk_weight   out  fp32 [dim] or NULL; zeros without norm, and where there are no rows or heads
+ *   work      scratch of xnor_qk_work_elems(rows, q_heads, k_heads, dim) floats, NULL if neither is
+ *             wanted; calls that can overlap (other streams, two graphs) need one each
+ * q_out and k_out may be the same buffers as dq_out and dk_out, or as q and k, with the same strides.  dweight is
+ * summed in a fixed order: the same inputs give the same bits.  Tokens with positions outside the
+ * table add nothing to it.
+ *
+ * INVALID_ARG: null (where not allowed) or misaligned pointer, rows < 0, heads < 0 or none at all,
+ * dim < 2 or odd, rot odd or not in 0 .. dim, positions < 1 where they are read, a stride out of range (rows that are written
+ * overlap) or another one in the same place, type none of F32, BF16, F16, weight_type neither F32 nor type, eps negative or not a
+ * number.  UNSUPPORTED: dim > 512, rows > 2^24, heads > 65535.
+ */
+typedef struct {
+  int rows, dim;
+  int q_heads, k_heads;
+  int type, weight_type;      /* xnor_type */
+  int norm;                   /* 0: rotation alone */
+  float eps;
+  int rot, pairs, positions;
+  long long q_stride, k_stride, v_stride, q_out_stride, k_out_stride;   /* v: xnor_kv4_append's */
+  long long dq_stride, dk_stride;                                       /* the backward pass's */
+} xnor_heads_desc;
+xnor_status xnor_qk_norm_rope(const void *q, const void *k, const void *q_weight, const void *k_weight,
+                              const int32_t *positions, const float *rope, const xnor_heads_desc *d,
+                              void *q_out, void *k_out, void *cuda_stream);
+size_t xnor_qk_work_elems(int rows, int q_heads, int k_heads, int dim);       /* 0: nothing wanted, or out of range */
+xnor_status xnor_qk_norm_rope_backward(const void *dq_out, const void *dk_out, const void *q, const void *k,
+                                       const void *q_weight, const void *k_weight, const int32_t *positions,
+                                       const float *rope, const xnor_heads_desc *d, void *dq, void *dk,
+                                       float *dq_weight, float *dk_weight, float *work, void *cuda_stream);
+
+/*
+ * The cache: `pages` pages of `page` tokens (a multiple of 16) of kv_heads heads of dim values (64 or
+ * 128), keys and values, in 4 bits with a scale and a zero point for each token and head:
+ * value = (code - zero) scale.  Bytes [pages][kv_heads][page / 16][16 (dim + 8)]; of 16 tokens
+ *   keys' codes    [16][dim / 2]   column 2 i + h of eight in bits 4 i + 16 h and up of their word
+ *   values' codes  [16][dim / 2]
+ *   keys' words    u32 [16]        the scale in fp32, the zero point in the place of its last 4 bits
+ *   values' words  u32 [16]
+ * Sequence b has the rows starts[b] .. starts[b + 1] - 1 of the call's new tokens, which are its last
+ * ones: it has lens[b] tokens with them.  Token p of it lies at place p % page of page
+ * table[b][p / page].
+ *   starts  int32 [seqs + 1], from 0 or more, rising;  lens  int32 [seqs];  table  int32 [seqs][table_cols]
+ * Rows before starts[0] and from starts[seqs] on belong to no sequence, and what is written is left as it was
+ * there.  A sequence may have fewer tokens than rows: the first of its rows then come before its
+ * first token, are not stored, and see nothing.
+ *
+ * xnor_kv4_append stores the new tokens' keys, with norm and rotation by their places in the
+ * sequences, and values; and writes the queries with theirs to q_out (as xnor_qk_norm_rope does).
+ *   q, k, v   in   as in xnor_qk_norm_rope, h->k_heads = d->kv_heads, v_stride for v; h->q_heads = 0: no queries
+ *   rope      in   [h->positions][rot]; places from h->positions on are left out (see above)
+ * Norm and rotation of keys in 64 bits, rounded to fp32; then with lo = min(x, 0), hi = max(x, 0) over
+ * the head, scale = (hi - lo) / 15, rounded to fp32 and its last 4 bits cleared, zero = -lo / scale and
+ * code = x / scale + zero, the quotients to the nearest whole number, exactly, ties to even, held to
+ * 0 .. 15.  A head whose scale is 0 is all zeros; one with an infinity or NaN in it is all NaN once stored.
+ * Two sequences must not store to the same place in one call.
+ *
+ * xnor_kv4_read gives the new tokens' keys and values back, in `type`, each rounded once: the whole
+ * of the sequences where starts counts all of their tokens.  Rows that were not stored are left as they were.
+ *
+ * INVALID_ARG as in xnor_qk_norm_rope, and: null or misaligned cache, starts, lens, table; pages, kv_heads,
+ * seqs < 0 or < 1, page < 16 or not a multiple of 16, table_cols < 1; k_heads that are not d->kv_heads.
+ * UNSUPPORTED: dim neither 64 nor 128, rot no multiple of 16, page > 65536, kv_heads > 4096, seqs > 2^20.
+ */
+typedef struct {
+  int pages, page, kv_heads, dim;
+  int seqs, table_cols;
+} xnor_kv4_desc;
+size_t xnor_kv4_cache_bytes(const xnor_kv4_desc *d);      /* 0: bad descriptor (seqs and table_cols are ignored) */
+xnor_status xnor_kv4_append(const void *q, const void *k, const void *v, const void *q_weight,
+                            const void *k_weight, const float *rope, const int32_t *starts,
+                            const int32_t *lens, const int32_t *table, const xnor_heads_desc *h,
+                            const xnor_kv4_desc *d, void *q_out, void *cache, void *cuda_stream);
+xnor_status xnor_kv4_read(const void *cache, const int32_t *starts, const int32_t *lens, const int32_t *table,
+                          const xnor_kv4_desc *d, int type, int rows, void *k, long long k_stride, void *v,
+                          long long v_stride, void *cuda_stream);
+
+/*
+ * Attention of the new tokens' queries over the cache, causal: query head j reads head
+ * j / (q_heads / kv_heads) of the cache, and a token sees those of its sequence up to itself:
+ *   out = sum over p of exp(scale q k_p - lse) v_p,   lse = log of the sum over p of exp(scale q k_p)
+ *   q     in   BF16 or F16 [rows][q_heads][dim]
+ *   out   out  the same type; must not overlap q.  A row that sees nothing: zeros
+ *   lse   out  fp32 [rows][q_heads], dense, or NULL; -infinity for a row that sees nothing
+ *   most  no sequence has more new tokens than this (0: not known).  By it and the sizes the call
+ *         chooses its kernels; where it is too small, results are as good and may take longer
+ *   work  scratch of xnor_kv4_work_bytes(d, r) bytes, whatever is in it; calls that can overlap need one each
+ * Codes and queries are exact operands; products, sums and the softmax are fp32, but exp(..) times a value's
+ * scale, which is rounded to 11 bits (below 2^-26 of the largest scale to a step of 2^-36 of that) to meet the values' codes.  The order of
+ * the sums depends on the sizes, all sequences' lengths and the device's number of SMs: the same call gives the same bits.
+ * Device-side waits are bounded (xnor_check_device).  What lies outside the table or the cache is not seen.
+ * INVALID_ARG as above, and: q_heads no multiple of kv_heads, scale not finite, most < 0, out in the place of q.
+ * UNSUPPORTED as above, and: F32.
+ */
+typedef struct {
+  int rows, q_heads, type, most;
+  float scale;
+  long long q_stride, out_stride;
+} xnor_kv4_rows;
+size_t xnor_kv4_work_bytes(const xnor_kv4_desc *d, const xnor_kv4_rows *r);   /* 0: bad descriptors */
+xnor_status xnor_kv4_attention(const void *q, const void *cache, const int32_t *starts, const int32_t *lens,
+                               const int32_t *table, const xnor_kv4_desc *d, const xnor_kv4_rows *r,
+                               void *out, float *lse, void *work, void *cuda_stream);
+
+/*
  * Which BinConv engine xnor_conv2d_forward uses.  XNOR_ENGINE_AUTO (default)
  * picks by shape: the tensor-core engine where it applies, else the CUDA-core
  * one.  Meant for tests and measurements.  This is the library's only
@@ -609,8 +746,8 @@ xnor_status xnor_measure_peaks(double *mma_mac_per_clk_per_sm, double *popc_per_
  * shared-memory barrier) is bounded; a wait that expires records
  * XNOR_ERR_TIMEOUT there, the kernel stops issuing work, releases its tensor
  * memory and returns, and the outputs of that launch are undefined.  Returns
- * XNOR_OK, XNOR_ERR_TIMEOUT (the word is then cleared), XNOR_ERR_CUDA or, from a
- * checking build, XNOR_ERR_BOUNDS.
+ * XNOR_OK, XNOR_ERR_TIMEOUT (the word is then cleared), XNOR_ERR_CUDA or XNOR_ERR_BOUNDS
+ * (likewise).
  */
 xnor_status xnor_check_device(void *cuda_stream);
 

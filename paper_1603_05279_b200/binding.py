@@ -46,6 +46,8 @@ EXPORTS = [
     "xnor_bgrad_stream_elems", "xnor_binarize_weights_transposed", "xnor_binary_gradient_backward", "xnor_measure_peaks",
     "xnor_rmsnorm", "xnor_rmsnorm_quant", "xnor_rmsnorm_work_elems", "xnor_rmsnorm_backward",
     "xnor_w4_packed_words", "xnor_w4_quantize", "xnor_w4_pack", "xnor_w4_dequantize", "xnor_w4_matmul",
+    "xnor_qk_norm_rope", "xnor_qk_work_elems", "xnor_qk_norm_rope_backward",
+    "xnor_kv4_cache_bytes", "xnor_kv4_append", "xnor_kv4_read", "xnor_kv4_work_bytes", "xnor_kv4_attention",
 ]
 
 XNOR_F32 = 0
@@ -79,6 +81,22 @@ class xnor_w4_rows(ctypes.Structure):
         [(n, ctypes.c_longlong) for n in ("x_stride", "out_stride")]
 
 
+class xnor_heads_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("rows", "dim", "q_heads", "k_heads", "type", "weight_type", "norm")] + \
+        [("eps", ctypes.c_float)] + [(n, ctypes.c_int) for n in ("rot", "pairs", "positions")] + \
+        [(n, ctypes.c_longlong) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride", "k_out_stride", "dq_stride",
+                                          "dk_stride")]
+
+
+class xnor_kv4_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("pages", "page", "kv_heads", "dim", "seqs", "table_cols")]
+
+
+class xnor_kv4_rows(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("rows", "q_heads", "type", "most")] + [("scale", ctypes.c_float)] + \
+        [(n, ctypes.c_longlong) for n in ("q_stride", "out_stride")]
+
+
 class XnorError(RuntimeError):
     def __init__(self, status, where):
         self.status = int(status)
@@ -91,7 +109,8 @@ _MARSHALLED = ["binarize_weights", "binactiv", "conv2d_forward", "shortcut_conv1
                "conv2d_forward_binactiv", "binactiv_finish", "maxpool2d", "binactiv_kbit",
                "conv2d_forward_kbit", "bwn_prepare_input", "bwn_conv2d_forward",
                "binarize_weights_transposed", "binary_gradient_backward", "rmsnorm", "rmsnorm_quant",
-               "rmsnorm_backward", "w4_quantize", "w4_pack", "w4_dequantize", "w4_matmul"]
+               "rmsnorm_backward", "w4_quantize", "w4_pack", "w4_dequantize", "w4_matmul", "qk_norm_rope",
+               "qk_norm_rope_backward", "kv4_append", "kv4_read", "kv4_attention"]
 
 
 class _Unloaded:
@@ -194,6 +213,23 @@ def load():
     lib.xnor_w4_dequantize.argtypes = [vp, vp, vp, wd, ci, vp, vp]
     lib.xnor_w4_matmul.restype = ci
     lib.xnor_w4_matmul.argtypes = [vp, vp, vp, vp, vp, wd, ctypes.POINTER(xnor_w4_rows), vp, vp]
+    hd, kd, kr = ctypes.POINTER(xnor_heads_desc), ctypes.POINTER(xnor_kv4_desc), ctypes.POINTER(xnor_kv4_rows)
+    lib.xnor_qk_norm_rope.restype = ci
+    lib.xnor_qk_norm_rope.argtypes = [vp, vp, vp, vp, vp, vp, hd, vp, vp, vp]
+    lib.xnor_qk_work_elems.restype = cz
+    lib.xnor_qk_work_elems.argtypes = [ci, ci, ci, ci]
+    lib.xnor_qk_norm_rope_backward.restype = ci
+    lib.xnor_qk_norm_rope_backward.argtypes = [vp] * 8 + [hd] + [vp] * 6
+    lib.xnor_kv4_cache_bytes.restype = cz
+    lib.xnor_kv4_cache_bytes.argtypes = [kd]
+    lib.xnor_kv4_append.restype = ci
+    lib.xnor_kv4_append.argtypes = [vp] * 9 + [hd, kd, vp, vp, vp]
+    lib.xnor_kv4_read.restype = ci
+    lib.xnor_kv4_read.argtypes = [vp, vp, vp, vp, kd, ci, ci, vp, ctypes.c_longlong, vp, ctypes.c_longlong, vp]
+    lib.xnor_kv4_work_bytes.restype = cz
+    lib.xnor_kv4_work_bytes.argtypes = [kd, kr]
+    lib.xnor_kv4_attention.restype = ci
+    lib.xnor_kv4_attention.argtypes = [vp, vp, vp, vp, vp, kd, kr, vp, vp, vp, vp]
     try:
         from . import _pymarshal
     except ImportError as e:
@@ -202,6 +238,8 @@ def load():
     _pymarshal.bind([ctypes.cast(getattr(lib, "xnor_" + n), vp).value for n in _MARSHALLED], xnor_conv_desc,
                     _address)
     _pymarshal.describe(xnor_w4_desc, _describe, ctypes.cast(lib.xnor_rmsnorm_work_elems, vp).value)
+    _pymarshal.describe_kv4(xnor_kv4_desc, ctypes.cast(lib.xnor_qk_work_elems, vp).value,
+                            ctypes.cast(lib.xnor_kv4_work_bytes, vp).value)
     _m, _lib = _pymarshal, lib       # in this order: another thread that sees _lib goes on to use _m
     return lib
 
@@ -527,6 +565,89 @@ def xnor_w4_matmul(x, x_scales, w_packed, scales, zeros, d, out, stream=None):
     s = _m.w4_matmul(x, x_scales, w_packed, scales, zeros, d, out, stream)
     if s:
         raise XnorError(s, "xnor_w4_matmul")
+
+
+# ---- attention over a cache in 4 bits ---------------------------------------------------------
+# Heads are [rows][heads][dim] tensors, a row's heads contiguous, rows at any stride: views of a product's output too.
+def xnor_qk_norm_rope(q, k, q_weight, k_weight, eps, positions, rope, pairs, q_out, k_out, stream=None):
+    """Norm (eps None: none) and rotation by position (rope None: none) of queries' and keys' heads; q or k may be
+    None.  pairs: neighbours are rotated, else a value with the one half of the rotated ones further on."""
+    s = _m.qk_norm_rope(q, k, q_weight, k_weight, eps, positions, rope, pairs, q_out, k_out, stream)
+    if s:
+        raise XnorError(s, "xnor_qk_norm_rope")
+
+
+def xnor_qk_work_elems(rows, q_heads, k_heads, dim):
+    return int(load().xnor_qk_work_elems(int(rows), int(q_heads), int(k_heads), int(dim)))
+
+
+def xnor_qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, eps, positions, rope, pairs, dq, dk, dq_weight,
+                               dk_weight, work, stream=None):
+    """dq and dk from the gradients at q_out and k_out, and dq_weight and dk_weight (or None, with work)."""
+    s = _m.qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, eps, positions, rope, pairs, dq, dk, dq_weight,
+                                 dk_weight, work, stream)
+    if s:
+        raise XnorError(s, "xnor_qk_norm_rope_backward")
+
+
+def alloc_qk_backward(rows, q_heads, k_heads, dim, device="cuda"):
+    """(dq_weight [dim], dk_weight [dim], work scratch) for xnor_qk_norm_rope_backward."""
+    return tuple(torch.empty((n,), dtype=torch.float32, device=device)
+                 for n in (dim, dim, xnor_qk_work_elems(rows, q_heads, k_heads, dim)))
+
+
+def make_rope(positions, rot, base=10000.0, device="cuda"):
+    """The table of a rotation of `rot` values: cosines and sines of position base^(-2 i / rot), [positions][rot]."""
+    a = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * \
+        base ** (-torch.arange(0, rot, 2, dtype=torch.float64, device=device) / rot)
+    return torch.cat([a.cos(), a.sin()], 1).float()
+
+
+def make_kv4_desc(pages, page, kv_heads, dim):
+    """A cache of `pages` pages of `page` tokens; the calls take the number of sequences from the table they get."""
+    return xnor_kv4_desc(pages, page, kv_heads, dim, 0, 0)
+
+
+def xnor_kv4_cache_bytes(d):
+    return int(load().xnor_kv4_cache_bytes(ctypes.byref(d)))
+
+
+def alloc_kv4(d, device="cuda"):
+    """The cache of descriptor d."""
+    return torch.empty((d.pages, d.kv_heads, d.page // 16, 16 * (d.dim + 8)), dtype=torch.uint8, device=device)
+
+
+def xnor_kv4_append(q, k, v, q_weight, k_weight, eps, rope, pairs, starts, lens, table, d, q_out, cache, stream=None):
+    """New tokens' keys (norm, rotation) and values into the cache, their queries (may be None), rotated, into q_out."""
+    s = _m.kv4_append(q, k, v, q_weight, k_weight, eps, rope, pairs, starts, lens, table, d, q_out, cache, stream)
+    if s:
+        raise XnorError(s, "xnor_kv4_append")
+
+
+def xnor_kv4_read(cache, starts, lens, table, d, k, v, stream=None):
+    """The keys and values that the cache stands for, of the sequences' last tokens."""
+    s = _m.kv4_read(cache, starts, lens, table, d, k, v, stream)
+    if s:
+        raise XnorError(s, "xnor_kv4_read")
+
+
+def xnor_kv4_work_bytes(d, rows, q_heads, seqs=1, most=0, type=XNOR_BF16):
+    """Scratch of xnor_kv4_attention; most = 0 holds for any."""
+    kd, r = xnor_kv4_desc(d.pages, d.page, d.kv_heads, d.dim, seqs, 1), xnor_kv4_rows(rows, q_heads, type, most, 1.0, 0, 0)
+    return int(load().xnor_kv4_work_bytes(ctypes.byref(kd), ctypes.byref(r)))
+
+
+def alloc_kv4_work(d, rows, q_heads, seqs=1, device="cuda"):
+    """Scratch for xnor_kv4_attention of up to `rows` new tokens of `seqs` sequences, whatever `most` says."""
+    return torch.empty((xnor_kv4_work_bytes(d, rows, q_heads, seqs),), dtype=torch.uint8, device=device)
+
+
+def xnor_kv4_attention(q, cache, starts, lens, table, d, scale, most, out, lse, work, stream=None):
+    """Causal attention of the new tokens' queries over the cache; lse may be None.  most: the most new tokens of a
+    sequence, as far as known (0: not), by which the kernels are chosen."""
+    s = _m.kv4_attention(q, cache, starts, lens, table, d, scale, most, out, lse, work, stream)
+    if s:
+        raise XnorError(s, "xnor_kv4_attention")
 
 
 # ---- buffer helpers (allocation only; torch owns the memory) -------------------------------

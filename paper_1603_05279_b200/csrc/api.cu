@@ -3,7 +3,7 @@
 
 #include "bgrad.cuh"
 #include "kbit.cuh"
-#include "rows.cuh"
+#include "kv4.cuh"
 
 namespace {
 
@@ -335,16 +335,18 @@ xnor_status xnor_selftest_wait_timeout(void *cuda_stream) {
 }
 
 xnor_status xnor_check_device(void *cuda_stream) {
-  int st = 0, st2 = 0, st3 = 0, st4 = 0, st5 = 0, st6 = 0;
+  int st = 0, st2 = 0, st3 = 0, st4 = 0, st5 = 0, st6 = 0, st7 = 0, st8 = 0, st9 = 0;
   if (cudaStreamSynchronize((cudaStream_t)cuda_stream) != cudaSuccess ||
       xnor::read_status_tc(&st) != cudaSuccess || xnor::read_status_bwn(&st2) != cudaSuccess ||
       xnor::read_status_act(&st3) != cudaSuccess || xnor::read_status_pool(&st4) != cudaSuccess ||
-      xnor::read_status_w4(&st5) != cudaSuccess || xnor::read_status_norm(&st6) != cudaSuccess) {
+      xnor::read_status_w4(&st5) != cudaSuccess || xnor::read_status_norm(&st6) != cudaSuccess ||
+      xnor::read_status_heads(&st7) != cudaSuccess || xnor::read_status_kv4(&st8) != cudaSuccess ||
+      xnor::read_status_kv4_attention(&st9) != cudaSuccess) {
     (void)cudaGetLastError();
     return XNOR_ERR_CUDA;
   }
-  if (st >= 1000) return XNOR_ERR_BOUNDS;
-  return (st == 0 && st2 == 0 && st3 == 0 && st4 == 0 && st5 == 0 && st6 == 0) ? XNOR_OK : XNOR_ERR_TIMEOUT;
+  if (st >= 1000 || st7 == XNOR_ERR_BOUNDS || st8 == XNOR_ERR_BOUNDS || st9 == XNOR_ERR_BOUNDS) return XNOR_ERR_BOUNDS;
+  return (st == 0 && st2 == 0 && st3 == 0 && st4 == 0 && st5 == 0 && st6 == 0 && st9 == 0) ? XNOR_OK : XNOR_ERR_TIMEOUT;
 }
 
 xnor_status xnor_measure_peaks(double *mma_mac_per_clk_per_sm, double *popc_per_clk_per_sm,
@@ -473,6 +475,34 @@ bool bad_w4(const xnor_w4_desc *d) {
 }
 bool large_w4(const xnor_w4_desc *d) { return d->N > xnor::kW4Rows * 65528 || d->K > (1 << 24); }
 
+// Rows of heads that are written: `width` = heads x dim values each.
+bool bad_heads(const void *in, long long in_stride, const void *out, long long out_stride, int rows, int heads, int dim) {
+  return rows > 0 && heads > 0 &&
+         (bad_read(in, in_stride) || bad_ptr(out) || out_stride < 0 || (rows > 1 && out_stride < (long long)heads * dim) ||
+          other_rows(out, out_stride, in, in_stride, rows));
+}
+xnor_status check_heads(const xnor_heads_desc *d, const void *q_weight, const void *k_weight, const float *rope) {
+  if (!d || d->rows < 0 || d->dim < 2 || d->dim % 2 || d->q_heads < 0 || d->k_heads < 0 || (d->q_heads == 0 && d->k_heads == 0) || !real_type(d->type) ||
+      d->rot < 0 || d->rot > d->dim || d->rot % 2)
+    return XNOR_ERR_INVALID_ARG;
+  if (d->norm && (!(d->eps >= 0.0f) || misaligned(q_weight) || misaligned(k_weight) ||
+                  ((q_weight || k_weight) && d->weight_type != XNOR_F32 && d->weight_type != d->type)))
+    return XNOR_ERR_INVALID_ARG;
+  if (d->rot > 0 && (d->positions < 1 || (d->rows > 0 && bad_ptr(rope)))) return XNOR_ERR_INVALID_ARG;
+  return d->dim > xnor::kHeadsMaxDim || d->rows > (1 << 24) || d->q_heads > 65535 || d->k_heads > 65535 ? XNOR_ERR_UNSUPPORTED : XNOR_OK;
+}
+
+bool bad_kv4(const xnor_kv4_desc *d) { return !d || d->pages < 1 || d->page < 16 || d->page % 16 || d->kv_heads < 1 || d->dim < 1; }
+bool large_kv4(const xnor_kv4_desc *d) { return (d->dim != 64 && d->dim != 128) || d->page > 65536 || d->kv_heads > 4096; }
+xnor_status check_kv4(const xnor_kv4_desc *d, const void *cache, const int32_t *starts, const int32_t *lens, const int32_t *table) {
+  if (bad_kv4(d) || d->seqs < 1 || d->table_cols < 1 || bad_ptr(cache) || bad_ptr(starts) || bad_ptr(lens) || bad_ptr(table)) return XNOR_ERR_INVALID_ARG;
+  return large_kv4(d) || d->seqs > (1 << 20) ? XNOR_ERR_UNSUPPORTED : XNOR_OK;
+}
+bool bad_kv4_rows(const xnor_kv4_desc *d, const xnor_kv4_rows *r) {
+  return !r || r->rows < 0 || r->q_heads < 1 || r->q_heads % d->kv_heads || !real_type(r->type) || r->most < 0;
+}
+bool large_kv4_rows(const xnor_kv4_rows *r) { return r->type == XNOR_F32 || r->rows > (1 << 24) || r->q_heads > 65535; }
+
 }  // namespace
 
 xnor_status xnor_rmsnorm(const void *x, const void *residual, const void *weight,
@@ -567,6 +597,95 @@ xnor_status xnor_w4_matmul(const void *x, const float *x_scales, const uint32_t 
   const xnor::W4Args a = {x, x_scales, w_packed, scales, zeros, out, *d, *r};
   return from_cuda(xnor::w4_few_rows(*d, r->rows) ? xnor::launch_w4_few_rows(a, (cudaStream_t)cuda_stream)
                                                : xnor::launch_w4_many_rows(a, (cudaStream_t)cuda_stream));
+}
+
+xnor_status xnor_qk_norm_rope(const void *q, const void *k, const void *q_weight, const void *k_weight,
+                              const int32_t *positions, const float *rope, const xnor_heads_desc *d,
+                              void *q_out, void *k_out, void *cuda_stream) {
+  const xnor_status s = check_heads(d, q_weight, k_weight, rope);
+  if (s == XNOR_ERR_INVALID_ARG) return s;
+  if (bad_heads(q, d->q_stride, q_out, d->q_out_stride, d->rows, d->q_heads, d->dim) ||
+      bad_heads(k, d->k_stride, k_out, d->k_out_stride, d->rows, d->k_heads, d->dim) || (d->rows > 0 && d->rot > 0 && bad_ptr(positions)))
+    return XNOR_ERR_INVALID_ARG;
+  if (s != XNOR_OK) return s;
+  return from_cuda(xnor::launch_heads({q, k, q_weight, k_weight, positions, rope, q_out, k_out, nullptr, nullptr, nullptr, nullptr, nullptr, *d},
+                                      (cudaStream_t)cuda_stream));
+}
+
+size_t xnor_qk_work_elems(int rows, int q_heads, int k_heads, int dim) {
+  if (rows < 0 || rows > (1 << 24) || q_heads < 0 || k_heads < 0 || q_heads > 65535 || k_heads > 65535 || dim < 2 || dim % 2 || dim > xnor::kHeadsMaxDim) return 0;
+  return (size_t)xnor::heads_parts(rows, q_heads, k_heads) * (size_t)dim;
+}
+
+xnor_status xnor_qk_norm_rope_backward(const void *dq_out, const void *dk_out, const void *q, const void *k,
+                                       const void *q_weight, const void *k_weight, const int32_t *positions,
+                                       const float *rope, const xnor_heads_desc *d, void *dq, void *dk,
+                                       float *dq_weight, float *dk_weight, float *work, void *cuda_stream) {
+  const xnor_status s = check_heads(d, q_weight, k_weight, rope);
+  if (s == XNOR_ERR_INVALID_ARG) return s;
+  const bool reads = d->norm != 0;                      // without a norm q and k do not matter
+  if (bad_heads(dq_out, d->dq_stride, dq, d->q_out_stride, d->rows, d->q_heads, d->dim) ||
+      bad_heads(dk_out, d->dk_stride, dk, d->k_out_stride, d->rows, d->k_heads, d->dim) || (d->rows > 0 && d->rot > 0 && bad_ptr(positions)) ||
+      (d->rows > 0 && reads && ((d->q_heads > 0 && bad_read(q, d->q_stride)) || (d->k_heads > 0 && bad_read(k, d->k_stride)))) ||
+      misaligned(dq_weight) || misaligned(dk_weight) || (d->rows > 0 && reads && (dq_weight || dk_weight) && bad_ptr(work)))
+    return XNOR_ERR_INVALID_ARG;
+  if (reads && ((d->q_heads > 0 && other_rows(dq, d->q_out_stride, q, d->q_stride, d->rows)) ||
+                (d->k_heads > 0 && other_rows(dk, d->k_out_stride, k, d->k_stride, d->rows))))
+    return XNOR_ERR_INVALID_ARG;
+  if (s != XNOR_OK) return s;
+  return from_cuda(xnor::launch_heads_backward({q, k, q_weight, k_weight, positions, rope, dq, dk, dq_out, dk_out, dq_weight, dk_weight, work, *d},
+                                               (cudaStream_t)cuda_stream));
+}
+
+size_t xnor_kv4_cache_bytes(const xnor_kv4_desc *d) {
+  if (bad_kv4(d) || large_kv4(d)) return 0;
+  return (size_t)d->pages * d->kv_heads * (d->page / 16) * xnor::kv4_record(d->dim);
+}
+
+xnor_status xnor_kv4_append(const void *q, const void *k, const void *v, const void *q_weight,
+                            const void *k_weight, const float *rope, const int32_t *starts,
+                            const int32_t *lens, const int32_t *table, const xnor_heads_desc *h,
+                            const xnor_kv4_desc *d, void *q_out, void *cache, void *cuda_stream) {
+  const xnor_status s = check_heads(h, q_weight, k_weight, rope), s2 = check_kv4(d, cache, starts, lens, table);
+  if (s == XNOR_ERR_INVALID_ARG || s2 == XNOR_ERR_INVALID_ARG || h->k_heads != d->kv_heads || h->dim != d->dim) return XNOR_ERR_INVALID_ARG;
+  if (bad_heads(q, h->q_stride, q_out, h->q_out_stride, h->rows, h->q_heads, h->dim) ||
+      (h->rows > 0 && (bad_read(k, h->k_stride) || bad_read(v, h->v_stride))))
+    return XNOR_ERR_INVALID_ARG;
+  if (s != XNOR_OK || s2 != XNOR_OK || h->rot % 16) return XNOR_ERR_UNSUPPORTED;
+  return from_cuda(xnor::launch_kv4_append({{h->q_heads > 0 ? q : nullptr, k, q_weight, k_weight, nullptr, rope, h->q_heads > 0 ? q_out : nullptr, nullptr,
+                                             nullptr, nullptr, nullptr, nullptr, nullptr, *h},
+                                            v, {starts, lens, table, *d}, static_cast<uint8_t *>(cache)},
+                                           (cudaStream_t)cuda_stream));
+}
+
+xnor_status xnor_kv4_read(const void *cache, const int32_t *starts, const int32_t *lens, const int32_t *table,
+                          const xnor_kv4_desc *d, int type, int rows, void *k, long long k_stride, void *v,
+                          long long v_stride, void *cuda_stream) {
+  const xnor_status s = check_kv4(d, cache, starts, lens, table);
+  if (s == XNOR_ERR_INVALID_ARG || !real_type(type) || rows < 0) return XNOR_ERR_INVALID_ARG;
+  const long long width = (long long)d->kv_heads * d->dim;
+  auto bad = [&](const void *p, long long stride) { return bad_ptr(p) || stride < 0 || (rows > 1 && stride < width); };
+  if (rows > 0 && (bad(k, k_stride) || bad(v, v_stride) || k == v)) return XNOR_ERR_INVALID_ARG;
+  if (s != XNOR_OK || rows > (1 << 24)) return XNOR_ERR_UNSUPPORTED;
+  return from_cuda(xnor::launch_kv4_read({static_cast<const uint8_t *>(cache), {starts, lens, table, *d}, type, rows, k, v, k_stride, v_stride},
+                                         (cudaStream_t)cuda_stream));
+}
+
+size_t xnor_kv4_work_bytes(const xnor_kv4_desc *d, const xnor_kv4_rows *r) {
+  if (bad_kv4(d) || large_kv4(d) || bad_kv4_rows(d, r) || large_kv4_rows(r)) return 0;
+  return xnor::kv4_work_bytes(*d, *r);
+}
+
+xnor_status xnor_kv4_attention(const void *q, const void *cache, const int32_t *starts, const int32_t *lens,
+                               const int32_t *table, const xnor_kv4_desc *d, const xnor_kv4_rows *r,
+                               void *out, float *lse, void *work, void *cuda_stream) {
+  const xnor_status s = check_kv4(d, cache, starts, lens, table);
+  if (s == XNOR_ERR_INVALID_ARG || bad_kv4_rows(d, r) || !(r->scale >= -3.402823466e38f && r->scale <= 3.402823466e38f)) return XNOR_ERR_INVALID_ARG;
+  if (r->rows > 0 && (bad_read(q, r->q_stride) || bad_ptr(out) || r->out_stride < 0 || (r->rows > 1 && r->out_stride < (long long)r->q_heads * d->dim) ||
+                      misaligned(lse) || bad_ptr(work) || out == q))
+    return XNOR_ERR_INVALID_ARG;
+  if (s != XNOR_OK || large_kv4_rows(r)) return XNOR_ERR_UNSUPPORTED;
+  return from_cuda(xnor::launch_kv4_attention({q, static_cast<const uint8_t *>(cache), {starts, lens, table, *d}, *r, out, lse, work}, (cudaStream_t)cuda_stream));
 }
 
 xnor_status xnor_shortcut_conv1x1(const float *x, const float *w, int N, int C_in, int H, int W,

@@ -1,0 +1,84 @@
+// The layout of the cache in 4 bits, and the sequences in it (internal).
+//
+// 16 tokens of a head are a record: the keys' codes, 16 rows of dim / 2 bytes, the values', and a word for each row, 16
+// of keys, 16 of values: its scale, whose last four bits are its zero point.  Records lie together by page and
+// head, so that one bulk copy brings 16 tokens, whatever a page holds; and a token is written without reading.
+// Codes lie in a word as those of 4-bit weights do (w4.cuh): a mask brings neighbours to where two 16-bit values have them.
+#pragma once
+#include "heads.cuh"
+#include "w4.cuh"
+
+namespace xnor {
+
+constexpr int kKvTokens = 16;                // of a record
+__host__ __device__ constexpr uint32_t kv4_record(int dim) { return (uint32_t)(kKvTokens * (dim + 8)); }
+__host__ __device__ constexpr uint32_t kv4_codes(int dim, bool values) { return values ? (uint32_t)(8 * dim) : 0u; }
+__host__ __device__ constexpr uint32_t kv4_words(int dim, bool values) { return (uint32_t)(16 * dim + (values ? 64 : 0)); }
+
+__device__ __forceinline__ float kv4_scale(uint32_t word) { return __uint_as_float(word & ~15u); }
+
+// What says where tokens lie.
+struct Kv4Where {
+  const int *starts, *lens, *table;
+  xnor_kv4_desc d;
+};
+
+__device__ __forceinline__ int load_int(const int *p) { return (int)load_global(reinterpret_cast<const uint32_t *>(p)); }
+
+// Record `rec` of sequence b (16 of its tokens), head h: its number in the cache.  -1: outside the table or the cache.
+__device__ __forceinline__ long long kv4_find(const Kv4Where &W, int b, int rec, int h) {
+  const int per_page = W.d.page / kKvTokens, at = rec / per_page;
+  if (at >= W.d.table_cols) return -1;
+  const int page = load_int(W.table + (size_t)b * W.d.table_cols + at);
+  if (page < 0 || page >= W.d.pages) return -1;
+  return ((long long)page * W.d.kv_heads + h) * per_page + (rec - at * per_page);
+}
+
+// The sequence of a row, for all threads of a warp; false: it belongs to none.  Thirty-two threads look at once.
+__device__ __forceinline__ bool find_sequence(const Kv4Where &W, int row, int lane, int &b, int &place) {
+  int lo = 0, hi = W.d.seqs;                  // the first sequence that ends behind the row is in lo .. hi (hi: none)
+  while (lo < hi) {
+    const int step = (hi - lo + 31) / 32, i = lo + (lane + 1) * step - 1;
+    const bool before = i < hi && load_int(W.starts + i + 1) <= row;
+    const int k = __popc(__ballot_sync(0xffffffffu, before));
+    hi = min(hi, lo + (k + 1) * step - 1);
+    lo = min(hi, lo + k * step);
+  }
+  b = lo;
+  if (b >= W.d.seqs) return false;
+  const int end = load_int(W.starts + b + 1);
+  if (load_int(W.starts + b) > row || end <= row) return false;
+  place = load_int(W.lens + b) - (end - row);
+  return true;
+}
+
+struct Kv4AppendArgs {
+  HeadsArgs h;                // pos is not used
+  const void *v;
+  Kv4Where w;
+  uint8_t *cache;
+};
+cudaError_t launch_kv4_append(const Kv4AppendArgs &a, cudaStream_t st);
+struct Kv4ReadArgs {
+  const uint8_t *cache;
+  Kv4Where w;
+  int type, rows;
+  void *k, *v;
+  long long k_stride, v_stride;
+};
+cudaError_t launch_kv4_read(const Kv4ReadArgs &a, cudaStream_t st);
+struct Kv4Args {
+  const void *q;
+  const uint8_t *cache;
+  Kv4Where w;
+  xnor_kv4_rows r;
+  void *out;
+  float *lse;
+  void *work;
+};
+cudaError_t launch_kv4_attention(const Kv4Args &a, cudaStream_t st);
+size_t kv4_work_bytes(const xnor_kv4_desc &d, const xnor_kv4_rows &r);
+cudaError_t read_status_kv4(int *status);
+cudaError_t read_status_kv4_attention(int *status);
+
+}  // namespace xnor

@@ -1,0 +1,648 @@
+// Attention over the cache in 4 bits for few new tokens of a sequence: warp-level products, the context shared out over
+// the GPU, and joined.
+//
+// A unit of work is a record (16 tokens of a head) for a tile of rows (queries of that head's group).  The units of all
+// sequences, heads and tiles stand in one row, and every block takes an equal share of it, found on the device from the
+// lengths; so a batch of any lengths keeps all SMs reading.  The tokens are the matrix operand (16 rows of m16n8k16) and the
+// queries, up to 8 kTiles of them, the other: S^T = K Q^T, then O^T += V^T P^T, whose codes - zero come straight from
+// a record's words, exactly.  A key's scale multiplies its row of S^T, a value's its row of P^T, which a matrix transposition
+// within the warp (movmatrix) makes the second operand.  The softmax is one pass: a running maximum, raised (and
+// the sums rescaled) only when it is exceeded by more than 2^3, and sums in fp32.
+// P, times the values' scales, is rounded to F16, 11 bits, relative to the largest scale so far (a power of two 2^e
+// above it) and times 2^12: at most 2^15, and with all 11 bits down to 2^-26 of that scale.  (As bfloat16 it gave outputs
+// in bfloat16 half as much again of error.)
+//
+// A block: one warp copies records into a ring in shared memory, a thread a stage, and eight or four warps take every
+// so-many-th unit each; at an item's end (the units of a tile) they add their sums.  An item that lies in
+// several blocks' shares leaves partial sums in the workspace, which a second kernel joins.
+#include <algorithm>
+
+#include "kv4.cuh"
+#include "umma_common.cuh"
+
+namespace xnor {
+
+__device__ int g_status_kv4_attention = 0;
+
+namespace {
+
+using namespace umma;
+
+constexpr int kWarps = 4, kStages = 16;
+constexpr int kPerSm = 3;
+constexpr int kMaxWorkers = kPerSm * 160;    // blocks, at most (a B200 has 148 SMs)
+constexpr int kLeastUnits = 2 * kWarps;      // of a block's share
+constexpr float kRaise = 3.0f;               // the maximum is left behind by 2^3 at most
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// The row of units.  A sequence of n new tokens and L in all has kv_heads x ceil(n group / rows) items of max(1, ceil(L / 16)) units.
+struct Sequence {
+  int start, n, len;           // first row, rows, tokens that the table has room for
+  int lead;                    // a row's last visible token, less the row
+  int tiles, units;            // units: of an item
+  __device__ __forceinline__ void load(const Kv4Where &W, int b, int group, int rows, int total_rows) {
+    const int end = load_int(W.starts + b + 1), all = load_int(W.lens + b);
+    start = max(0, load_int(W.starts + b));
+    n = max(0, min(total_rows, end) - start);
+    len = (int)min((long long)max(0, all), (long long)W.d.table_cols * W.d.page);
+    lead = all - end;
+    if (n > 0 && all > len) atomicMax(&g_status_kv4_attention, (int)XNOR_ERR_BOUNDS);
+    tiles = (int)(((long long)n * group + rows - 1) / rows);
+    units = max(1, (len + kKvTokens - 1) / kKvTokens);
+  }
+  __device__ __forceinline__ long long all(int kv_heads) const { return (long long)kv_heads * tiles * units; }
+};
+
+// What the threads of a warp know of the row: each the sum over its own run of sequences, and the sum before them.
+struct Row {
+  int per;                     // sequences of a thread
+  long long before, total;
+  long long workers;
+  __device__ __forceinline__ Row(const Kv4Where &W, int group, int rows, int total_rows, int lane, int most) {
+    per = (W.d.seqs + 31) / 32;
+    long long mine = 0;
+#pragma unroll 4
+    for (int i = 0; i < per; ++i) {
+      const int b = lane * per + i;
+      if (b >= W.d.seqs) break;
+      Sequence s;
+      s.load(W, b, group, rows, total_rows);
+      mine += s.all(W.d.kv_heads);
+    }
+    long long sum = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const long long v = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += v;
+    }
+    before = sum - mine;
+    total = __shfl_sync(0xffffffffu, sum, 31);
+    workers = max(1ll, min((long long)most, total / kLeastUnits));
+  }
+  __device__ __forceinline__ long long first_of(long long worker) const { return worker * total / workers; }
+  __device__ __forceinline__ int worker_of(long long unit) const { return (int)(((unit + 1) * workers - 1) / total); }
+  // The sum before sequence b; the same for all threads.
+  __device__ __forceinline__ long long before_sequence(const Kv4Where &W, int b, int group, int rows, int total_rows, int lane) const {
+    long long v = before;
+    if (lane == b / per)
+      for (int i = lane * per; i < b; ++i) {
+        Sequence s;
+        s.load(W, i, group, rows, total_rows);
+        v += s.all(W.d.kv_heads);
+      }
+    return __shfl_sync(0xffffffffu, v, b / per);
+  }
+  // The sequence of a unit (below total), and the sum before it.
+  __device__ __forceinline__ int sequence_of(const Kv4Where &W, long long unit, int group, int rows, int total_rows, int lane, long long &sum) const {
+    const uint32_t later = __ballot_sync(0xffffffffu, before > unit);
+    const int owner = later == 0 ? 31 : __ffs((int)later) - 2;       // the last thread whose sum before it is no more
+    int b = 0;
+    long long v = before;
+    if (lane == owner) {
+      for (b = lane * per; b + 1 < W.d.seqs; ++b) {
+        Sequence s;
+        s.load(W, b, group, rows, total_rows);
+        const long long u = s.all(W.d.kv_heads);
+        if (v + u > unit) break;
+        v += u;
+      }
+    }
+    sum = __shfl_sync(0xffffffffu, v, owner);
+    return __shfl_sync(0xffffffffu, b, owner);
+  }
+};
+
+// A place in the row: item (sequence, head, tile) and record.
+struct Place {
+  int b, head, tile, rec;
+  Sequence s;
+  __device__ __forceinline__ void set(long long in_sequence) {
+    const long long item = in_sequence / s.units;
+    rec = (int)(in_sequence - item * s.units);
+    head = (int)(item / s.tiles);
+    tile = (int)(item - (long long)head * s.tiles);
+  }
+};
+
+// ---- shared memory -----------------------------------------------------------------------------------------------
+template <int kDim, int kTiles>
+struct Layout {
+  static constexpr uint32_t kRecord = kv4_record(kDim);
+  static constexpr int kRows = 8 * kTiles;
+  static constexpr int kSumRow = kDim + 4;                          // floats
+  static constexpr uint32_t kFull = 0, kEmpty = 8 * kStages, kValid = 16 * kStages, kAbort = kValid + 4 * kStages;
+  static constexpr uint32_t kStats = 512;                           // [kWarps][kRows] maxima and sums
+  static constexpr uint32_t kSums = kStats + 8 * kWarps * kRows;    // [kWarps][kRows][kSumRow]
+  static constexpr uint32_t kRing = (kSums + 4u * kWarps * kRows * kSumRow + 127u) & ~127u;
+  static constexpr uint32_t kBytes = kRing + kStages * kRecord;
+  static_assert(kAbort + 4 <= kStats, "control words");
+};
+
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// 2^i; 0 below fp32's normal numbers.
+__device__ __forceinline__ float power_of_two(int i) { return i < -126 ? 0.0f : __uint_as_float((uint32_t)(i + 127) << 23); }
+// The power of two above a scale, within limits that keep all its uses normal numbers.  Infinity and NaN do not count.
+constexpr int kLeastScale = -100, kMostScale = 127;
+__device__ __forceinline__ int scale_above(float s) {
+  const int i = (int)(__float_as_uint(s) >> 23) & 255;
+  return i == 255 ? kLeastScale : min(kMostScale, max(kLeastScale, i - 126));
+}
+
+// Which token of a record is row i of the products (neighbours are neighbours): keys and values then meet in the fewest banks.
+__device__ __forceinline__ int token_of(int i) { return i ^ ((i >> 1) & 1); }
+
+struct Params {
+  Kv4Args A;
+  int group, workers, q_pieces, out_words;      // q can be read in 16-byte pieces, out written in words
+  uint32_t magic, magic16;     // W4Type's of the queries' type and of F16
+};
+
+// Waits of a warp's threads for their own barriers; false: gave up.
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
+  return mbar_wait(bar, parity, abort_flag, &g_status_kv4_attention);
+}
+
+// ---- the copying warp --------------------------------------------------------------------------------------------
+// Thread i fills stage i, of every kStages-th unit of the share.  It finds the next unit's record before it waits for the stage.
+template <class L>
+__device__ __forceinline__ void copy_role(const Params &P, const Row &row, long long u0, long long u1, int b0, long long sum0, uint32_t smem,
+                                          volatile int *abort_flag, int lane) {
+  const Kv4Where &W = P.A.w;
+  if (lane >= kStages) return;
+  Place p;
+  p.b = b0;
+  p.s.load(W, b0, P.group, L::kRows, P.A.r.rows);
+  long long sum = sum0;
+  struct Next { long long record; int valid; };
+  auto find = [&](long long u) {
+    Next n = {-1, 0};
+    if (u >= u1) return n;
+    while (u >= sum + p.s.all(W.d.kv_heads)) {
+      sum += p.s.all(W.d.kv_heads);
+      p.s.load(W, ++p.b, P.group, L::kRows, P.A.r.rows);
+    }
+    p.set(u - sum);
+    n.valid = min(kKvTokens, p.s.len - p.rec * kKvTokens);
+    if (n.valid > 0) n.record = kv4_find(W, p.b, p.rec, p.head);
+    return n;
+  };
+  const uint32_t full = smem + L::kFull + 8u * lane, empty = smem + L::kEmpty + 8u * lane;
+  Next next = find(u0 + lane);
+  uint32_t parity = 1u;
+  bool in_flight = false;
+  for (long long u = u0 + lane; u < u1; u += kStages, parity ^= 1u) {
+    const Next now = next;
+    next = find(u + kStages);
+    if (!wait_for(empty, parity, abort_flag)) {
+      // gave up: the copy in flight must land before the block's shared memory is released
+      for (int i = 0; in_flight && i < (1 << 12) && !mbar_try(full, parity); ++i) {}
+      return;
+    }
+    const bool there = now.record >= 0;
+    if (!there && now.valid > 0) atomicMax(&g_status_kv4_attention, (int)XNOR_ERR_BOUNDS);
+    asm volatile("st.shared.b32 [%0], %1;" ::"r"(smem + L::kValid + 4u * lane), "r"(there ? now.valid : 0) : "memory");
+    if (there) {
+      mbar_arrive_expect_tx(full, L::kRecord);
+      bulk_copy_g2s(smem + L::kRing + (uint32_t)lane * L::kRecord, P.A.cache + (size_t)now.record * L::kRecord, L::kRecord, full);
+    } else {
+      mbar_arrive(full);
+    }
+    in_flight = there;
+  }
+}
+
+// ---- the computing warps -----------------------------------------------------------------------------------------
+__device__ __forceinline__ void block_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory"); }
+
+// A row of the tile: where its query and its outputs are; -1: none.
+struct TileRow {
+  long long q, out;
+  long long lse;
+  int limit;                   // the last token that it sees; below 0: none
+  bool in;
+  __device__ __forceinline__ TileRow(const Params &P, const Place &p, int rows, int i, int dim) {
+    const long long r = (long long)p.tile * rows + i;
+    const int token = (int)(r / P.group), head = p.head * P.group + (int)(r - (long long)token * P.group);
+    in = token < p.s.n;
+    q = (p.s.start + token) * P.A.r.q_stride + (long long)head * dim;
+    out = (p.s.start + token) * P.A.r.out_stride + (long long)head * dim;
+    lse = (long long)(p.s.start + token) * P.A.r.q_heads + head;
+    limit = p.s.lead + p.s.start + token;
+  }
+};
+
+// A warp's row of outputs, kDim / 32 columns a thread.
+template <class T, int kDim>
+__device__ __forceinline__ void store_row(T *row, const float (&acc)[kDim / 32], float inv, bool blind, bool words, int lane) {
+#pragma unroll
+  for (int c = 0; c < kDim / 64; ++c) {
+    const uint32_t v = blind ? 0u : float_to_pair(acc[2 * c] * inv, acc[2 * c + 1] * inv, T());
+    T *to = row + lane * (kDim / 32) + 2 * c;
+    if (words) {
+      *reinterpret_cast<uint32_t *>(to) = v;
+    } else {
+      reinterpret_cast<uint16_t *>(to)[0] = (uint16_t)v;
+      reinterpret_cast<uint16_t *>(to)[1] = (uint16_t)(v >> 16);
+    }
+  }
+}
+
+__host__ __device__ constexpr size_t slot_floats(int rows, int dim) { return (size_t)rows * (dim + 2); }
+
+template <class T, int kDim, int kTiles>
+__device__ __forceinline__ void compute_role(const Params &P, const Row &row, int worker, long long u0, long long u1, int b0, long long sum0,
+                                             uint32_t smem, uint8_t *smem_ptr, volatile int *abort_flag, int warp, int lane) {
+  using L = Layout<kDim, kTiles>;
+  constexpr int kRows = L::kRows, kWords = kDim / 32, kVWords = kDim / 64, kMTiles = kDim / 16;      // of a thread: key words, value words of a token; tiles of O^T
+  const Kv4Where &W = P.A.w;
+  const int g = lane >> 2, t = lane & 3;
+  float *stats = reinterpret_cast<float *>(smem_ptr + L::kStats), *sums = reinterpret_cast<float *>(smem_ptr + L::kSums);
+  const float scale2 = P.A.r.scale * kLog2e;
+  const int tok0 = token_of(g), tok1 = token_of(g + 8);                    // this thread's rows of S^T
+  Place p;
+  p.b = b0;
+  p.s.load(W, b0, P.group, kRows, P.A.r.rows);
+  long long u = u0, sum = sum0;
+  bool alive = true;
+  while (u < u1) {
+    while (u >= sum + p.s.all(W.d.kv_heads)) {
+      sum += p.s.all(W.d.kv_heads);
+      p.s.load(W, ++p.b, P.group, kRows, P.A.r.rows);
+    }
+    p.set(u - sum);
+    const long long item0 = u - p.rec;                                     // the item's units
+    const int rec_end = (int)min((long long)p.s.units, p.rec + (u1 - u));
+    // Q: thread (g, t) has row g's columns kDim / 4 t .., as its words of keys have them
+    uint32_t q[kTiles][kWords][4];
+    int limit[kTiles][2], least = 0x7FFFFFFF;
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+      const TileRow r(P, p, kRows, 8 * n + g, kDim);
+#pragma unroll
+      for (int w = 0; w < kWords; ++w) {
+        Chunk<T> c;
+        c.load(static_cast<const T *>(P.A.q) + r.q + t * (kDim / 4) + 8 * w, P.q_pieces, r.in ? 8 : 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[n][w][i] = c.w[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const TileRow s(P, p, kRows, 8 * n + 2 * t + i, kDim);
+        limit[n][i] = s.in ? s.limit : 0x7FFFFFFF;                         // (rows that do not exist compute something)
+        least = min(least, limit[n][i]);
+      }
+    }
+    least = __reduce_min_sync(0xffffffffu, least);
+    float o[kTiles][kMTiles][4], m[kTiles][2], l[kTiles][2];
+    int e = kLeastScale;                                                   // 2^e: the values' scales are below it
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) { m[n][i] = -INFINITY; l[n][i] = 0.0f; }
+#pragma unroll
+      for (int j = 0; j < kMTiles; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[n][j][i] = 0.0f;
+    }
+    // every kWarps-th unit of the share is this warp's
+    const int skip = (int)((warp - (u - u0)) & (kWarps - 1));
+#pragma unroll 1
+    for (int rec = p.rec + skip; alive && rec < rec_end; rec += kWarps) {
+      const long long i = item0 + rec - u0;                                // the unit's number in the share
+      const uint32_t stage = (uint32_t)(i % kStages), base = smem + L::kRing + stage * L::kRecord;
+      alive = __all_sync(0xffffffffu, wait_for(smem + L::kFull + 8u * stage, (uint32_t)(i / kStages) & 1u, abort_flag));
+      if (!alive) break;
+      const int valid = (int)lds32(smem + L::kValid + 4u * stage);
+      // ---- S^T
+      float s[kTiles][4];
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[n][j] = 0.0f;
+      const uint32_t kw0 = lds32(base + kv4_words(kDim, false) + 4u * tok0), kw1 = lds32(base + kv4_words(kDim, false) + 4u * tok1);
+      {
+        const typename W4Type<T>::Zero z0 = W4Type<T>::zero(kw0 & 15u), z1 = W4Type<T>::zero(kw1 & 15u);
+        uint32_t c0[kWords], c1[kWords];
+        const uint32_t from = base + (uint32_t)(t * (kDim / 8));
+        if constexpr (kWords == 4) {
+          lds128(from + tok0 * (kDim / 2), c0);
+          lds128(from + tok1 * (kDim / 2), c1);
+        } else {
+          lds64(from + tok0 * (kDim / 2), c0[0], c0[1]);
+          lds64(from + tok1 * (kDim / 2), c1[0], c1[1]);
+        }
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) {
+          uint32_t e0[4], e1[4];
+          W4Type<T>::expand(c0[w], z0, P.magic, e0);
+          W4Type<T>::expand(c1[w], z1, P.magic, e1);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t a[4] = {e0[2 * k], e1[2 * k], e0[2 * k + 1], e1[2 * k + 1]};
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) mma16816(s[n], a, q[n][w][2 * k], q[n][w][2 * k + 1], T());
+          }
+        }
+      }
+      // ---- the softmax: s[n][0], [1]: token tok0 for rows 2 t, 2 t + 1; [2], [3]: token tok1
+      const float ks0 = kv4_scale(kw0) * scale2, ks1 = kv4_scale(kw1) * scale2;
+      const int p0 = rec * kKvTokens;
+      const bool whole = valid == kKvTokens && p0 + kKvTokens - 1 <= least;
+      bool raise = false;
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int tok = j < 2 ? tok0 : tok1;
+          s[n][j] *= j < 2 ? ks0 : ks1;
+          if (!whole && (tok >= valid || p0 + tok > limit[n][j & 1])) s[n][j] = -INFINITY;
+          raise = raise || s[n][j] > m[n][j & 1] + kRaise;
+        }
+      const uint32_t vw0 = lds32(base + kv4_words(kDim, true) + 4u * tok0), vw1 = lds32(base + kv4_words(kDim, true) + 4u * tok1);
+      float vs0 = kv4_scale(vw0), vs1 = kv4_scale(vw1);
+      const int e0 = tok0 < valid ? scale_above(vs0) : kLeastScale, e1 = tok1 < valid ? scale_above(vs1) : kLeastScale;
+      raise = raise || max(e0, e1) > e;
+      if (__any_sync(0xffffffffu, raise)) {
+        const int above = __reduce_max_sync(0xffffffffu, max(e, max(e0, e1)));
+        const float down = power_of_two(e - above);
+        e = above;
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float top = fmaxf(m[n][i], fmaxf(s[n][i], s[n][i + 2]));
+#pragma unroll
+            for (int x = 4; x < 32; x *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+            const float f = top == -INFINITY ? 1.0f : exp2_fast(m[n][i] - top);
+            m[n][i] = top;
+            l[n][i] *= f;
+#pragma unroll
+            for (int j = 0; j < kMTiles; ++j) {
+              o[n][j][i] *= f * down;
+              o[n][j][i + 2] *= f * down;
+            }
+          }
+      }
+      vs0 *= power_of_two(12 - e);
+      vs1 *= power_of_two(12 - e);
+      uint32_t b[kTiles][2];                                               // P^T: tokens 0 .. 7 and 8 .. 15 of the rows
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n) {
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float top = m[n][j & 1];
+          x[j] = exp2_fast(s[n][j] - (top == -INFINITY ? 0.0f : top));
+          l[n][j & 1] += x[j];
+          x[j] = s[n][j] == -INFINITY ? 0.0f : x[j] * (j < 2 ? vs0 : vs1); // (a token that is not seen may stand for anything)
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) b[n][h] = transpose8x8(float_to_pair(x[2 * h], x[2 * h + 1], __half()));
+      }
+      // ---- O^T: thread (g, t) has columns kDim / 8 g .. of tokens 2 t, 2 t + 1 and 8 more
+      {
+        using V = W4Type<__half>;
+        uint32_t c[2][2][kVWords];
+        V::Zero z[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int ta = token_of(2 * t + 8 * h), tb = token_of(2 * t + 1 + 8 * h);
+          const uint32_t codes = base + kv4_codes(kDim, true) + (uint32_t)(g * (kDim / 16)), words = base + kv4_words(kDim, true);
+          const uint32_t zeros = (lds32(words + 4u * ta) & 15u) | (lds32(words + 4u * tb) & 15u) << 16;
+          z[h] = {0x64006400u | zeros, 0xD400D400u | zeros << 4};
+          if constexpr (kVWords == 2) {
+            lds64(codes + ta * (kDim / 2), c[h][0][0], c[h][0][1]);
+            lds64(codes + tb * (kDim / 2), c[h][1][0], c[h][1][1]);
+          } else {
+            c[h][0][0] = lds32(codes + ta * (kDim / 2));
+            c[h][1][0] = lds32(codes + tb * (kDim / 2));
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem + L::kEmpty + 8u * stage);
+#pragma unroll
+        for (int w = 0; w < kVWords; ++w) {
+          uint32_t x[2][2][4];                                             // [half of the tokens][even, odd columns][pairs]
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            V::expand(__byte_perm(c[h][0][w], c[h][1][w], 0x5410), z[h], P.magic16, x[h][0]);
+            V::expand(__byte_perm(c[h][0][w], c[h][1][w], 0x7632), z[h], P.magic16, x[h][1]);
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t a[4] = {x[0][0][k], x[0][1][k], x[1][0][k], x[1][1][k]};
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) {
+              mma16816(o[n][4 * w + k], a, b[n][0], b[n][1], __half());
+            }
+          }
+        }
+      }
+    }
+    // ---- the warps' sums together
+    const float back = power_of_two(e - 12);
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int x = 4; x < 32; x *= 2) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], x);
+        const int r = 8 * n + 2 * t + i;
+        if (g == 0) {
+          stats[2 * (warp * kRows + r)] = m[n][i];
+          stats[2 * (warp * kRows + r) + 1] = l[n][i];
+        }
+        float *to = sums + (size_t)(warp * kRows + r) * L::kSumRow + g * (kDim / 8);
+#pragma unroll
+        for (int w = 0; w < kVWords; ++w)
+#pragma unroll
+          for (int k = 0; k < 4; k += 2)
+            *reinterpret_cast<float4 *>(to + 8 * w + 2 * k) = make_float4(back * o[n][4 * w + k][i], back * o[n][4 * w + k][i + 2], back * o[n][4 * w + k + 1][i], back * o[n][4 * w + k + 1][i + 2]);
+      }
+    block_sync();
+    alive = *abort_flag == 0;
+    const bool first = p.rec == 0, last = rec_end == p.s.units;
+    float *slot = static_cast<float *>(P.A.work) + (size_t)(2 * worker + (first ? 1 : 0)) * slot_floats(kRows, kDim);
+    // a warp's rows; a thread has kDim / 32 columns
+#pragma unroll 1
+    for (int r = warp; r < kRows; r += kWarps) {
+      const TileRow at(P, p, kRows, r, kDim);
+      if (!at.in) break;
+      float top = -INFINITY, total = 0.0f, f[kWarps], acc[kDim / 32] = {};
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) top = fmaxf(top, stats[2 * (i * kRows + r)]);
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) {
+        f[i] = top == -INFINITY ? 0.0f : exp2_fast(stats[2 * (i * kRows + r)] - top);
+        total = fmaf(f[i], stats[2 * (i * kRows + r) + 1], total);
+      }
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i)
+#pragma unroll
+        for (int c = 0; c < kDim / 32; ++c) acc[c] = fmaf(f[i], sums[(size_t)(i * kRows + r) * L::kSumRow + lane * (kDim / 32) + c], acc[c]);
+      if (first && last) {
+        const bool blind = at.limit < 0;
+        const float inv = blind ? 0.0f : 1.0f / total;
+        store_row<T, kDim>(static_cast<T *>(P.A.out) + at.out, acc, inv, blind, P.out_words, lane);
+        if (lane == 0 && P.A.lse) P.A.lse[at.lse] = blind ? -INFINITY : (top + log2f(total)) * kLn2;
+      } else {
+#pragma unroll
+        for (int c = 0; c < kDim / 32; ++c) slot[(size_t)r * kDim + lane * (kDim / 32) + c] = acc[c];
+        if (lane == 0) {
+          slot[(size_t)kRows * kDim + 2 * r] = top;
+          slot[(size_t)kRows * kDim + 2 * r + 1] = total;
+        }
+      }
+    }
+    block_sync();
+    u += rec_end - p.rec;
+  }
+}
+
+template <class T, int kDim, int kTiles>
+__global__ void __launch_bounds__(32 * (kWarps + 1))
+kv4_few_kernel(const Params P) {
+  using L = Layout<kDim, kTiles>;
+  extern __shared__ __align__(128) uint8_t smem_ptr[];
+  const uint32_t smem = smem_u32(smem_ptr);
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(smem_ptr + L::kAbort);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(smem + L::kFull + 8u * i, 1);
+      mbar_init(smem + L::kEmpty + 8u * i, 1);
+    }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  stream_order();
+  const Row row(P.A.w, P.group, L::kRows, P.A.r.rows, lane, P.workers);
+  if (row.total == 0 || (long long)blockIdx.x >= row.workers) return;
+  const long long u0 = row.first_of(blockIdx.x), u1 = row.first_of(blockIdx.x + 1);
+  long long sum;
+  const int b = row.sequence_of(P.A.w, u0, P.group, L::kRows, P.A.r.rows, lane, sum);
+  if (warp == kWarps)
+    copy_role<L>(P, row, u0, u1, b, sum, smem, abort_flag, lane);
+  else
+    compute_role<T, kDim, kTiles>(P, row, blockIdx.x, u0, u1, b, sum, smem, smem_ptr, abort_flag, warp, lane);
+}
+
+// Joins the partial sums of items that lie in several blocks' shares: a warp has a row (token and head).
+constexpr int kJoinWarps = 4;
+template <class T, int kDim>
+__global__ void __launch_bounds__(32 * kJoinWarps)
+kv4_join_kernel(const Params P, int rows) {
+  const int lane = threadIdx.x & 31;
+  const long long item = (long long)blockIdx.x * kJoinWarps + threadIdx.x / 32;
+  stream_order();
+  const int token = (int)(item / P.A.r.q_heads), head = (int)(item % P.A.r.q_heads);
+  if (token >= P.A.r.rows) return;
+  const Kv4Where &W = P.A.w;
+  int b, place;
+  if (!find_sequence(W, token, lane, b, place)) return;
+  const Row row(W, P.group, rows, P.A.r.rows, lane, P.workers);
+  const long long before = row.before_sequence(W, b, P.group, rows, P.A.r.rows, lane);
+  Sequence s;
+  s.load(W, b, P.group, rows, P.A.r.rows);
+  const long long r = (long long)(token - s.start) * P.group + head % P.group;
+  const int tile = (int)(r / rows), at = (int)(r - (long long)tile * rows);
+  const long long u0 = before + ((long long)(head / P.group) * s.tiles + tile) * s.units;
+  const int w0 = row.worker_of(u0), w1 = row.worker_of(u0 + s.units - 1);
+  if (w0 == w1) return;
+  const float *work = static_cast<const float *>(P.A.work);
+  auto slot = [&](int w) { return work + (size_t)(2 * w + (w == w0 ? 1 : 0)) * slot_floats(rows, kDim); };
+  float top = -INFINITY;
+  for (int w = w0 + lane; w <= w1; w += 32) top = fmaxf(top, load_global(slot(w) + (size_t)rows * kDim + 2 * at));
+#pragma unroll
+  for (int x = 16; x > 0; x /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+  float total = 0.0f, acc[kDim / 32] = {};
+#pragma unroll 4
+  for (int w = w0; w <= w1; ++w) {
+    const float *from = slot(w);
+    const float m = load_global(from + (size_t)rows * kDim + 2 * at), l = load_global(from + (size_t)rows * kDim + 2 * at + 1);
+    const float f = top == -INFINITY ? 0.0f : exp2_fast(m - top);
+    total = fmaf(f, l, total);
+#pragma unroll
+    for (int c = 0; c < kDim / 32; ++c) acc[c] = fmaf(f, load_global(from + (size_t)at * kDim + lane * (kDim / 32) + c), acc[c]);
+  }
+  const bool blind = place < 0;
+  const float inv = 1.0f / total;
+  store_row<T, kDim>(static_cast<T *>(P.A.out) + token * P.A.r.out_stride + (long long)head * kDim, acc, inv, blind, P.out_words, lane);
+  if (lane == 0 && P.A.lse) P.A.lse[(long long)token * P.A.r.q_heads + head] = blind ? -INFINITY : (top + log2f(total)) * kLn2;
+}
+
+template <class K>
+cudaError_t allow_shared(K *kernel, size_t bytes, bool (&flags)[64]) {
+  bool &set = attr_done_for_current_device(flags);
+  if (set) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e != cudaSuccess) (void)cudaGetLastError();
+  set = e == cudaSuccess;
+  return e;
+}
+
+int tiles_for(const xnor_kv4_desc &d, const xnor_kv4_rows &r) {
+  const long long rows = (long long)(r.most > 0 ? std::min(r.most, r.rows) : r.rows) * (r.q_heads / d.kv_heads);
+  return rows <= 8 ? 1 : 2;
+}
+
+template <class T, int kDim, int kTiles>
+cudaError_t run(const Kv4Args &a, cudaStream_t st) {
+  using L = Layout<kDim, kTiles>;
+  static bool flags[64] = {};
+  cudaError_t e = allow_shared(kv4_few_kernel<T, kDim, kTiles>, L::kBytes, flags);
+  if (e != cudaSuccess) return e;
+  const int workers = std::min(kMaxWorkers, kPerSm * sm_count_of_current_device());
+  const Params P = {a, a.r.q_heads / a.w.d.kv_heads, workers, rows_in_pieces(a.q, a.r.q_stride, kDim, 2), a.r.out_stride % 2 == 0, W4Type<T>::kMagic, W4Type<__half>::kMagic};
+  e = launch_kernel(kv4_few_kernel<T, kDim, kTiles>, dim3((unsigned)workers), 32 * (kWarps + 1), L::kBytes, st, 1, P);
+  if (e != cudaSuccess) return e;
+  const long long rows = (long long)a.r.rows * a.r.q_heads;
+  return launch_kernel(kv4_join_kernel<T, kDim>, dim3((unsigned)((rows + kJoinWarps - 1) / kJoinWarps)), 32 * kJoinWarps, 0, st, 1, P, L::kRows);
+}
+template <class T>
+cudaError_t run_type(const Kv4Args &a, cudaStream_t st) {
+  const int tiles = tiles_for(a.w.d, a.r);
+  if (a.w.d.dim == 64) return tiles == 1 ? run<T, 64, 1>(a, st) : run<T, 64, 2>(a, st);
+  return tiles == 1 ? run<T, 128, 1>(a, st) : run<T, 128, 2>(a, st);
+}
+
+}  // namespace
+
+size_t kv4_work_bytes(const xnor_kv4_desc &d, const xnor_kv4_rows &r) {
+  return 2 * (size_t)kMaxWorkers * slot_floats(8 * tiles_for(d, r), d.dim) * sizeof(float);
+}
+
+cudaError_t read_status_kv4_attention(int *status) {
+  cudaError_t e = cudaMemcpyFromSymbol(status, g_status_kv4_attention, sizeof(int));
+  if (e == cudaSuccess && *status != 0) {
+    const int zero = 0;
+    e = cudaMemcpyToSymbol(g_status_kv4_attention, &zero, sizeof(int));
+  }
+  return e;
+}
+
+cudaError_t launch_kv4_attention(const Kv4Args &a, cudaStream_t st) {
+  if (a.r.rows == 0) return cudaSuccess;
+  return a.r.type == XNOR_BF16 ? run_type<__nv_bfloat16>(a, st) : run_type<__half>(a, st);
+}
+
+}  // namespace xnor

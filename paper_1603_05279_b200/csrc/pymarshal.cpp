@@ -42,11 +42,17 @@ struct Entry {
   decltype(&xnor_w4_pack) w4_pack;
   decltype(&xnor_w4_dequantize) w4_dequantize;
   decltype(&xnor_w4_matmul) w4_matmul;
+  decltype(&xnor_qk_norm_rope) qk_norm_rope;
+  decltype(&xnor_qk_norm_rope_backward) qk_norm_rope_backward;
+  decltype(&xnor_kv4_append) kv4_append;
+  decltype(&xnor_kv4_read) kv4_read;
+  decltype(&xnor_kv4_attention) kv4_attention;
 } E;
 constexpr Py_ssize_t kEntries = sizeof(Entry) / sizeof(void *);
 PyObject *desc_type = nullptr;         // the ctypes structure xnor_conv_desc
 PyObject *py_address = nullptr;        // (object, type name) -> its checked address through Python attributes
 PyObject *w4_desc_type = nullptr;      // the ctypes structure xnor_w4_desc
+PyObject *kv4_desc_type = nullptr;     // the ctypes structure xnor_kv4_desc
 PyObject *py_describe = nullptr;       // object -> (address, type, shape, strides, device) through Python attributes
 
 // Arguments of one call, converted in order; the first failure sets a Python error and sticks.
@@ -610,6 +616,212 @@ XNOR_PY(w4_matmul) {                 // x, x_scales, w_packed, scales, zeros, d,
   return A.run([&] { return E.w4_matmul(x.p, (const float *)xs.p, (const uint32_t *)in.packed.p, (const float *)in.scales.p, (const uint8_t *)in.zeros.p, &d, &r, out.p, st); });
 }
 
+// ---- tensors of heads ---------------------------------------------------------------------
+decltype(&xnor_qk_work_elems) qk_work_elems = nullptr;             // queries, as above
+decltype(&xnor_kv4_work_bytes) kv4_work_bytes = nullptr;
+
+// [rows][heads][dim], a row's heads and values contiguous.
+Dense heads(RowArgs &A, int i, const char *name, long long *stride) {
+  const Dense d = A.tensor(i, name);
+  *stride = 0;
+  if (!A.ok) return d;
+  if (d.dims != 3) A.bad(name, "expected a tensor of 3 dimensions");
+  else if (d.size[2] < 1) A.bad(name, "heads of no values");
+  else if ((d.size[2] > 1 && d.stride[2] != 1) || (d.size[1] > 1 && d.stride[1] != d.size[2])) A.bad(name, "a row's heads must be contiguous");
+  *stride = d.size[0] > 1 ? d.stride[0] : d.size[1] * d.size[2];
+  return d;
+}
+Dense heads_like(RowArgs &A, int i, const char *name, const Dense &other, long long *stride) {
+  const Dense d = heads(A, i, name, stride);
+  if (A.ok && (d.size[0] != other.size[0] || d.size[1] != other.size[1] || d.size[2] != other.size[2])) A.bad(name, "another shape than the rows that it belongs to");
+  if (A.ok) A.want_type(d, name, (at::ScalarType)other.type);
+  return d;
+}
+
+// Queries and keys (either may be None), their weights, eps (None: no norm), the table of the rotation (None: none).
+struct HeadsIn {
+  xnor_heads_desc d = {};
+  Dense any, q, k, q_weight, k_weight, rope;
+  HeadsIn(RowArgs &A, int q_at, int k_at, int weights_at, int eps_at, int rope_at, int pairs_at) {
+    if (!A.ok) return;
+    if (!A.none(q_at)) any = q = heads(A, q_at, "q", &d.q_stride);
+    if (A.ok && !A.none(k_at)) {
+      k = heads(A, k_at, "k", &d.k_stride);
+      if (A.ok && q.there() && (k.size[0] != q.size[0] || k.size[2] != q.size[2])) A.bad("k", "other rows or heads than q has");
+      if (A.ok && q.there()) A.want_type(k, "k", (at::ScalarType)q.type);
+      if (!any.there()) any = k;
+    }
+    if (A.ok && !any.there()) A.bad("q", "neither queries nor keys");
+    if (!A.ok) return;
+    d.rows = (int)any.size[0];
+    d.dim = (int)any.size[2];
+    d.q_heads = q.there() ? (int)q.size[1] : 0;
+    d.k_heads = k.there() ? (int)k.size[1] : 0;
+    d.type = A.xnor_type_of(any, "q", false);
+    d.weight_type = XNOR_F32;
+    if (!A.none(eps_at)) {
+      d.norm = 1;
+      d.eps = (float)A.number(eps_at);
+      int type = -1;
+      for (int i = 0; i < 2; ++i) {
+        if (!A.ok || A.none(weights_at + i)) continue;
+        Dense &w = i == 0 ? q_weight : k_weight;
+        const char *name = i == 0 ? "q_weight" : "k_weight";
+        w = A.tensor(weights_at + i, name);
+        if (!A.ok) return;
+        w = A.dense(weights_at + i, name, w.type == any.type ? (at::ScalarType)any.type : at::kFloat, {any.size[2]});
+        if (A.ok && type >= 0 && type != w.type) A.bad(name, "another type than q_weight");
+        type = w.type;
+        if (A.ok) d.weight_type = A.xnor_type_of(w, name, false);
+      }
+    }
+    if (A.ok && !A.none(rope_at)) {
+      rope = A.tensor(rope_at, "rope");
+      if (A.ok && (rope.dims != 2 || rope.size[1] < 2 || rope.size[1] % 2 || rope.size[1] > d.dim)) A.bad("rope", "expected [positions][rotated values], an even number of up to the heads' values");
+      if (A.ok) rope = A.dense(rope_at, "rope", at::kFloat, {rope.size[0], rope.size[1]});
+      if (!A.ok) return;
+      d.positions = (int)rope.size[0];
+      d.rot = (int)rope.size[1];
+    }
+    const int pairs = A.ok ? PyObject_IsTrue(A.a[pairs_at]) : 0;
+    if (pairs < 0) A.ok = false;
+    d.pairs = pairs > 0;
+  }
+};
+
+XNOR_PY(qk_norm_rope) {              // q, k, q_weight, k_weight, eps, positions, rope, pairs, q_out, k_out, stream
+  RowArgs A(args, nargs, 11);
+  if (!A.ok) return nullptr;
+  HeadsIn in(A, 0, 1, 2, 4, 6, 7);
+  Dense pos, q_out, k_out;
+  if (A.ok && in.rope.there()) pos = A.dense(5, "positions", at::kInt, {in.any.size[0]});
+  if (A.ok && in.q.there()) q_out = heads_like(A, 8, "q_out", in.q, &in.d.q_out_stride);
+  if (A.ok && in.k.there()) k_out = heads_like(A, 9, "k_out", in.k, &in.d.k_out_stride);
+  void *st = A.stream(10);
+  return A.run([&] { return E.qk_norm_rope(in.q.p, in.k.p, in.q_weight.p, in.k_weight.p, (const int32_t *)pos.p, (const float *)in.rope.p, &in.d, q_out.p, k_out.p, st); });
+}
+
+XNOR_PY(qk_norm_rope_backward) {     // dq_out, dk_out, q, k, q_weight, k_weight, eps, positions, rope, pairs, dq, dk, dq_weight, dk_weight, work, stream
+  RowArgs A(args, nargs, 16);
+  if (!A.ok) return nullptr;
+  HeadsIn in(A, 2, 3, 4, 6, 8, 9);
+  Dense pos, dq_out, dk_out, dq, dk, dqw, dkw, work;
+  if (A.ok && in.rope.there()) pos = A.dense(7, "positions", at::kInt, {in.any.size[0]});
+  if (A.ok && in.q.there()) {
+    dq_out = heads_like(A, 0, "dq_out", in.q, &in.d.dq_stride);
+    dq = heads_like(A, 10, "dq", in.q, &in.d.q_out_stride);
+  }
+  if (A.ok && in.k.there()) {
+    dk_out = heads_like(A, 1, "dk_out", in.k, &in.d.dk_stride);
+    dk = heads_like(A, 11, "dk", in.k, &in.d.k_out_stride);
+  }
+  if (A.ok && !A.none(12)) dqw = A.dense(12, "dq_weight", at::kFloat, {in.d.dim});
+  if (A.ok && !A.none(13)) dkw = A.dense(13, "dk_weight", at::kFloat, {in.d.dim});
+  if (A.ok && (dqw.there() || dkw.there()) && !A.none(14)) {
+    work = A.tensor(14, "work");
+    if (A.ok) work = A.dense(14, "work", at::kFloat, {work.numel});
+    if (A.ok && work.numel < (long long)qk_work_elems(in.d.rows, in.d.q_heads, in.d.k_heads, in.d.dim)) A.bad("work", "too few elements");
+  }
+  void *st = A.stream(15);
+  return A.run([&] { return E.qk_norm_rope_backward(dq_out.p, dk_out.p, in.q.p, in.k.p, in.q_weight.p, in.k_weight.p, (const int32_t *)pos.p, (const float *)in.rope.p,
+                                                    &in.d, dq.p, dk.p, (float *)dqw.p, (float *)dkw.p, (float *)work.p, st); });
+}
+
+// The cache's descriptor, and what says where tokens lie.
+struct Kv4In {
+  xnor_kv4_desc d = {};
+  Dense cache, starts, lens, table;
+  Kv4In(RowArgs &A, int d_at, int cache_at, int where_at) {
+    if (!A.ok) return;
+    Py_buffer b;
+    const int is = PyObject_IsInstance(A.a[d_at], kv4_desc_type);
+    if (is == 0) PyErr_Format(PyExc_TypeError, "expected an xnor_kv4_desc, got %S", (PyObject *)Py_TYPE(A.a[d_at]));
+    if (is != 1 || PyObject_GetBuffer(A.a[d_at], &b, PyBUF_SIMPLE) != 0) { A.ok = false; return; }
+    memcpy(&d, b.buf, std::min((size_t)b.len, sizeof(d)));
+    PyBuffer_Release(&b);
+    if (d.pages < 1 || d.page < 16 || d.page % 16 || d.kv_heads < 1 || d.dim < 1 || d.dim > 4096) { A.bad("d", "not a descriptor of a cache"); return; }
+    cache = A.dense(cache_at, "cache", at::kByte, {d.pages, d.kv_heads, d.page / 16, 16ll * (d.dim + 8)});
+    table = A.tensor(where_at + 2, "table");
+    if (A.ok && table.dims != 2) A.bad("table", "expected a tensor of 2 dimensions");
+    if (A.ok) table = A.dense(where_at + 2, "table", at::kInt, {table.size[0], table.size[1]});
+    if (!A.ok) return;
+    d.seqs = (int)table.size[0];
+    d.table_cols = (int)table.size[1];
+    starts = A.dense(where_at, "starts", at::kInt, {d.seqs + 1ll});
+    lens = A.dense(where_at + 1, "lens", at::kInt, {d.seqs});
+  }
+  const int32_t *at_starts() const { return (const int32_t *)starts.p; }
+  const int32_t *at_lens() const { return (const int32_t *)lens.p; }
+  const int32_t *at_table() const { return (const int32_t *)table.p; }
+};
+
+XNOR_PY(kv4_append) {                // q, k, v, q_weight, k_weight, eps, rope, pairs, starts, lens, table, d, q_out, cache, stream
+  RowArgs A(args, nargs, 15);
+  if (!A.ok) return nullptr;
+  if (A.none(1)) A.bad("k", "no keys");
+  HeadsIn in(A, 0, 1, 3, 5, 6, 7);
+  Dense v, q_out;
+  if (A.ok) v = heads_like(A, 2, "v", in.k, &in.d.v_stride);
+  if (A.ok && in.q.there()) q_out = heads_like(A, 12, "q_out", in.q, &in.d.q_out_stride);
+  Kv4In kv(A, 11, 13, 8);
+  if (A.ok && (in.d.k_heads != kv.d.kv_heads || in.d.dim != kv.d.dim)) A.bad("k", "other heads than the cache has");
+  void *st = A.stream(14);
+  return A.run([&] { return E.kv4_append(in.q.p, in.k.p, v.p, in.q_weight.p, in.k_weight.p, (const float *)in.rope.p, kv.at_starts(), kv.at_lens(), kv.at_table(),
+                                         &in.d, &kv.d, q_out.p, kv.cache.p, st); });
+}
+
+XNOR_PY(kv4_read) {                  // cache, starts, lens, table, d, k, v, stream
+  RowArgs A(args, nargs, 8);
+  if (!A.ok) return nullptr;
+  Kv4In kv(A, 4, 0, 1);
+  long long k_stride = 0, v_stride = 0;
+  Dense k, v;
+  if (A.ok) k = heads(A, 5, "k", &k_stride);
+  if (A.ok && (k.size[1] != kv.d.kv_heads || k.size[2] != kv.d.dim)) A.bad("k", "other heads than the cache has");
+  if (A.ok) v = heads_like(A, 6, "v", k, &v_stride);
+  const int type = A.ok ? A.xnor_type_of(k, "k", false) : 0;
+  void *st = A.stream(7);
+  return A.run([&] { return E.kv4_read(kv.cache.p, kv.at_starts(), kv.at_lens(), kv.at_table(), &kv.d, type, (int)k.size[0], k.p, k_stride, v.p, v_stride, st); });
+}
+
+XNOR_PY(kv4_attention) {             // q, cache, starts, lens, table, d, scale, most, out, lse, work, stream
+  RowArgs A(args, nargs, 12);
+  if (!A.ok) return nullptr;
+  xnor_kv4_rows r = {};
+  const Dense q = heads(A, 0, "q", &r.q_stride);
+  Kv4In kv(A, 5, 1, 2);
+  Dense out, lse, work;
+  if (A.ok && q.size[2] != kv.d.dim) A.bad("q", "other heads than the cache has");
+  if (A.ok && (q.size[1] < 1 || q.size[1] % kv.d.kv_heads)) A.bad("q", "the cache's heads do not divide its heads");
+  if (A.ok) out = heads_like(A, 8, "out", q, &r.out_stride);
+  if (A.ok && !A.none(9)) lse = A.dense(9, "lse", at::kFloat, {q.size[0], q.size[1]});
+  if (!A.ok) return nullptr;
+  r.rows = (int)q.size[0];
+  r.q_heads = (int)q.size[1];
+  r.type = A.xnor_type_of(q, "q", false);
+  r.scale = (float)A.number(6);
+  r.most = A.whole(7);
+  if (A.ok) work = A.tensor(10, "work");
+  if (A.ok) work = A.dense(10, "work", at::kByte, {work.numel});
+  if (A.ok && work.numel < (long long)kv4_work_bytes(&kv.d, &r)) A.bad("work", "too few bytes");
+  void *st = A.stream(11);
+  return A.run([&] { return E.kv4_attention(q.p, kv.cache.p, kv.at_starts(), kv.at_lens(), kv.at_table(), &kv.d, &r, out.p, (float *)lse.p, work.p, st); });
+}
+
+// describe_kv4(class, addresses): the cache's descriptor, xnor_qk_work_elems and xnor_kv4_work_bytes
+PyObject *describe_kv4(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+  if (nargs != 3) return PyErr_Format(PyExc_TypeError, "expected 3 arguments, got %zd", nargs);
+  void *p[2];
+  for (int i = 0; i < 2; ++i) {
+    p[i] = PyLong_AsVoidPtr(args[1 + i]);
+    if (p[i] == nullptr) { if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address"); return nullptr; }
+  }
+  qk_work_elems = (decltype(&xnor_qk_work_elems))p[0];
+  kv4_work_bytes = (decltype(&xnor_kv4_work_bytes))p[1];
+  Py_XSETREF(kv4_desc_type, Py_NewRef(args[0]));
+  Py_RETURN_NONE;
+}
+
 // describe(class, function, address): the descriptor of 4-bit weights, the Python description of what is not exactly
 // a tensor, and xnor_rmsnorm_work_elems
 PyObject *describe(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
@@ -653,6 +865,8 @@ PyMethodDef methods[] = {
     {"describe", (PyCFunction)(void (*)(void))describe, METH_FASTCALL, nullptr},
     XNOR_FAST(rmsnorm), XNOR_FAST(rmsnorm_quant), XNOR_FAST(rmsnorm_backward), XNOR_FAST(w4_quantize), XNOR_FAST(w4_pack),
     XNOR_FAST(w4_dequantize), XNOR_FAST(w4_matmul),
+    {"describe_kv4", (PyCFunction)(void (*)(void))describe_kv4, METH_FASTCALL, nullptr},
+    XNOR_FAST(qk_norm_rope), XNOR_FAST(qk_norm_rope_backward), XNOR_FAST(kv4_append), XNOR_FAST(kv4_read), XNOR_FAST(kv4_attention),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pymarshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

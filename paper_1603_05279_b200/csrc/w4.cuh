@@ -61,6 +61,45 @@ struct W4Type<__half> {
   }
 };
 
+// w / s to the nearest whole number, ties to even, of the exact quotient (|w / s| below 2^20).  A first guess is off by one
+// at most, where the quotient lies next to a border, and the rest w - q s is exact in 32 bits.
+__device__ __forceinline__ float mend_quotient(float q, float w, float s) {
+  const float r = fmaf(-q, s, w), twice = 2.0f * fabsf(r);
+  return twice > s || (twice == s && ((int)q & 1)) ? q + (r > 0.0f ? 1.0f : -1.0f) : q;
+}
+__device__ __forceinline__ float round_quotient(float w, float s) { return mend_quotient(rintf(w / s), w, s); }
+
+// The same of kN values.  With the reciprocal the guess is within 2e-6 of the quotient (at most 16), so only guesses that
+// close to a border can be wrong; all are mended then.  (inv = 0: it would overflow.  Such a scale may be a few units of
+// fp32's least number, so far from a seventh or a 15th that quotients leave the codes' range: -zero .. 15 - zero.)
+template <int kN>
+__device__ __forceinline__ void round_quotients(const float (&w)[kN], float s, float inv, float zero, float (&q)[kN]) {
+  if (inv == 0.0f) {
+#pragma unroll 1
+    for (int i = 0; i < kN; ++i) q[i] = fminf(15.0f - zero, fmaxf(-zero, round_quotient(w[i], s)));
+    return;
+  }
+  float far = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    const float t = w[i] * inv;
+    q[i] = __fadd_rn(__fadd_rn(t, 12582912.0f), -12582912.0f);          // 1.5 2^23: rounds to a whole number
+    far = fmaxf(far, fabsf(t - q[i]));
+  }
+  if (far > 0.49999f) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) q[i] = mend_quotient(q[i], w[i], s);
+  }
+}
+
+// Four codes c0 .. c3 as c0 + 16 c1 + 256 c2 + 4096 c3, which 32-bit floats hold exactly; in the mantissa of 2^23 they
+// lie as a word has them.  (With a conversion, a shift and an OR for each code 4096x4096 bf16 took
+// 24.3 us, 18 to 20 so; what is left is 26 instructions a value, a third of them where quotients lie next to borders, as
+// those of bf16 weights often do, at 2.6 a clock: blocks that load, wait, compute and store, half of the warps an SM can have.)
+__device__ __forceinline__ float four_codes(float first, float c1, float c2, float c3) {
+  return fmaf(c3, 4096.0f, fmaf(c2, 256.0f, fmaf(c1, 16.0f, first)));
+}
+
 // Eight values of a row in 8 bits as 16-bit numbers, exact.  The code of an int8 with its sign bit turned is
 // 128 + value; in the mantissa of 1024 it is 1152 + value.
 __device__ __forceinline__ uint32_t i8_pair(uint32_t four, int pair) {

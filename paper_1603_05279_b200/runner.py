@@ -305,3 +305,44 @@ class TokenBlock:
         B.xnor_w4_matmul(self.y if self.q is None else self.q, self.q_scales, self.packed, self.scales, self.zeros,
                          self.d, self.out, stream)
         return self.out
+
+
+class TokenAttention:
+    """Buffers and calls of the attention in a decoder's layer, on bfloat16 rows between two TokenBlocks' products: norms
+    and rotation of queries and keys, the new tokens into a cache in 4 bits, and attention over it.
+
+    `seqs` sequences of up to `context` tokens each, in pages of `page`; up to `rows` new tokens in a call, up to `most`
+    of a sequence (0: any).  rot: rotated values of a head (None: all, 0: none)."""
+
+    def __init__(self, rows, seqs, context, q_heads, kv_heads, dim, page=64, most=0, norm=True, rot=None, base=10000.0,
+                 pairs=False, eps=1e-6, device="cuda"):
+        cols = -(-context // page)
+        self.q_heads, self.kv_heads, self.dim, self.most, self.pairs = q_heads, kv_heads, dim, most, pairs
+        self.d = B.make_kv4_desc(seqs * cols, page, kv_heads, dim)
+        self.cache = B.alloc_kv4(self.d, device)
+        self.table = torch.arange(seqs * cols, dtype=torch.int32, device=device).view(seqs, cols)
+        self.starts = torch.zeros((seqs + 1,), dtype=torch.int32, device=device)
+        self.lens = torch.zeros((seqs,), dtype=torch.int32, device=device)
+        rot = dim if rot is None else rot
+        self.rope = B.make_rope(context, rot, base, device) if rot else None
+        self.eps = eps if norm else None
+        self.q_weight, self.k_weight = (torch.ones((dim,), dtype=torch.float32, device=device) if norm else None for _ in "qk")
+        self.q = torch.empty((rows, q_heads, dim), dtype=torch.bfloat16, device=device)
+        self.out = torch.empty((rows, q_heads * dim), dtype=torch.bfloat16, device=device)
+        self.work = B.alloc_kv4_work(self.d, rows, q_heads, seqs, device)
+
+    def grow(self, new):
+        """The next forward() brings new[b] more tokens of sequence b (int32 on the device), in the sequences' order."""
+        torch.cumsum(new, 0, dtype=torch.int32, out=self.starts[1:])
+        self.lens += new
+
+    def forward(self, qkv, stream=None):
+        """qkv: rows [q_heads dim | kv_heads dim | kv_heads dim] of one product; gives rows [q_heads dim]."""
+        rows, n, m = qkv.shape[0], self.q_heads, self.kv_heads
+        q, k, v = (t.unflatten(1, (-1, self.dim)) for t in qkv.split([n * self.dim, m * self.dim, m * self.dim], 1))
+        out = self.out[:rows]
+        B.xnor_kv4_append(q, k, v, self.q_weight, self.k_weight, self.eps, self.rope, self.pairs, self.starts, self.lens,
+                          self.table, self.d, self.q[:rows], self.cache, stream)
+        B.xnor_kv4_attention(self.q[:rows], self.cache, self.starts, self.lens, self.table, self.d, self.dim ** -0.5,
+                             self.most, out.unflatten(1, (n, self.dim)), None, self.work, stream)
+        return out
