@@ -79,6 +79,16 @@ struct Kv4Args {
 cudaError_t launch_kv4_attention(const Kv4Args &a, cudaStream_t st);
 size_t kv4_work_bytes(const xnor_kv4_desc &d, const xnor_kv4_rows &r);
 cudaError_t read_status_kv4(int *status);
-cudaError_t read_status_kv4_attention(int *status);
+// Its two kernels: of sequences with at most so many rows (new tokens x queries of a head), and of those with more.
+cudaError_t launch_kv4_few(const Kv4Args &a, int most_rows, cudaStream_t st);
+size_t kv4_few_work_bytes(const xnor_kv4_desc &d, const xnor_kv4_rows &r);
+cudaError_t read_status_kv4_few(int *status);
+cudaError_t launch_kv4_prompt(const Kv4Args &a, int least_rows, cudaStream_t st);
+size_t kv4_prompt_work_bytes(const xnor_kv4_desc &d, const xnor_kv4_rows &r);
+cudaError_t read_status_kv4_prompt(int *status);
+// Rows of a sequence, at most, as far as the caller knows.
+inline long long kv4_most_rows(const xnor_kv4_desc &d, const xnor_kv4_rows &r) {
+  return (long long)(r.most > 0 && r.most < r.rows ? r.most : r.rows) * (r.q_heads / d.kv_heads);
+}
 
 }  // namespace xnor

@@ -1,0 +1,77 @@
+// What the kernels of attention over the cache in 4 bits have in common (internal).
+#pragma once
+#include "kv4.cuh"
+#include "umma_common.cuh"
+
+namespace xnor {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kRaise = 3.0f;               // a row's maximum is left behind by 2^3 at most
+
+struct Sequence;
+// How a call's rows are cut: tiles of `rows` queries of a head's group, units of `tokens`; of sequences with more than
+// `least` and at most `most` rows.
+struct Tiling {
+  int group, rows, tokens, total_rows;
+  int least, most;
+  // Records lengths that the table has no room for; for all threads of a warp.
+  __device__ __forceinline__ void check_lengths(const Kv4Where &W, int lane, int *status) const;
+};
+
+// A sequence of n new tokens and L in all has kv_heads x ceil(n group / rows) items of max(1, ceil(L / tokens)) units.
+struct Sequence {
+  int start, n, len;           // first row, rows (0: not of this kernel's), tokens that the table has room for
+  int lead;                    // a row's last visible token, less the row
+  int tiles, units;            // units: of an item
+  bool cut;                    // longer than the table has room for
+  __device__ __forceinline__ void load(const Kv4Where &W, const Tiling &T, int b) {
+    const int end = load_int(W.starts + b + 1), all = load_int(W.lens + b);
+    start = max(0, load_int(W.starts + b));
+    n = max(0, min(T.total_rows, end) - start);
+    const long long r = (long long)n * T.group;
+    if (r <= T.least || r > T.most) n = 0;
+    len = (int)min((long long)max(0, all), (long long)W.d.table_cols * W.d.page);
+    lead = all - end;
+    cut = n > 0 && all > len;
+    tiles = n > 0 ? (int)((r + T.rows - 1) / T.rows) : 0;
+    units = max(1, (len + T.tokens - 1) / T.tokens);
+  }
+  __device__ __forceinline__ long long all(int kv_heads) const { return (long long)kv_heads * tiles * units; }
+};
+
+__device__ __forceinline__ void Tiling::check_lengths(const Kv4Where &W, int lane, int *status) const {
+  bool cut = false;
+  for (int b = (int)blockIdx.x * 32 + lane; b < W.d.seqs; b += (int)gridDim.x * 32) {
+    Sequence s;
+    s.load(W, *this, b);
+    cut = cut || s.cut;
+  }
+  if (cut) atomicMax(status, (int)XNOR_ERR_BOUNDS);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// 2^i; 0 below fp32's normal numbers.
+__device__ __forceinline__ float power_of_two(int i) { return i < -126 ? 0.0f : __uint_as_float((uint32_t)(i + 127) << 23); }
+// The power of two above a scale, within limits that keep all its uses normal numbers.  Infinity and NaN do not count.
+constexpr int kLeastScale = -100, kMostScale = 127;
+__device__ __forceinline__ int scale_above(float s) {
+  const int i = (int)(__float_as_uint(s) >> 23) & 255;
+  return i == 255 ? kLeastScale : min(kMostScale, max(kLeastScale, i - 126));
+}
+
+template <class K>
+cudaError_t allow_shared(K *kernel, size_t bytes, bool (&flags)[64]) {
+  bool &set = attr_done_for_current_device(flags);
+  if (set) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e != cudaSuccess) (void)cudaGetLastError();
+  set = e == cudaSuccess;
+  return e;
+}
+
+}  // namespace xnor

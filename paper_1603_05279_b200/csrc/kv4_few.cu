@@ -17,12 +17,11 @@
 // several blocks' shares leaves partial sums in the workspace, which a second kernel joins.
 #include <algorithm>
 
-#include "kv4.cuh"
-#include "umma_common.cuh"
+#include "kv4_attention.cuh"
 
 namespace xnor {
 
-__device__ int g_status_kv4_attention = 0;
+__device__ int g_status_kv4_few = 0;
 
 namespace {
 
@@ -32,33 +31,13 @@ constexpr int kWarps = 4, kStages = 16;
 constexpr int kPerSm = 3;
 constexpr int kMaxWorkers = kPerSm * 160;    // blocks, at most (a B200 has 148 SMs)
 constexpr int kLeastUnits = 2 * kWarps;      // of a block's share
-constexpr float kRaise = 3.0f;               // the maximum is left behind by 2^3 at most
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-// The row of units.  A sequence of n new tokens and L in all has kv_heads x ceil(n group / rows) items of max(1, ceil(L / 16)) units.
-struct Sequence {
-  int start, n, len;           // first row, rows, tokens that the table has room for
-  int lead;                    // a row's last visible token, less the row
-  int tiles, units;            // units: of an item
-  __device__ __forceinline__ void load(const Kv4Where &W, int b, int group, int rows, int total_rows) {
-    const int end = load_int(W.starts + b + 1), all = load_int(W.lens + b);
-    start = max(0, load_int(W.starts + b));
-    n = max(0, min(total_rows, end) - start);
-    len = (int)min((long long)max(0, all), (long long)W.d.table_cols * W.d.page);
-    lead = all - end;
-    if (n > 0 && all > len) atomicMax(&g_status_kv4_attention, (int)XNOR_ERR_BOUNDS);
-    tiles = (int)(((long long)n * group + rows - 1) / rows);
-    units = max(1, (len + kKvTokens - 1) / kKvTokens);
-  }
-  __device__ __forceinline__ long long all(int kv_heads) const { return (long long)kv_heads * tiles * units; }
-};
 
 // What the threads of a warp know of the row: each the sum over its own run of sequences, and the sum before them.
 struct Row {
   int per;                     // sequences of a thread
   long long before, total;
   long long workers;
-  __device__ __forceinline__ Row(const Kv4Where &W, int group, int rows, int total_rows, int lane, int most) {
+  __device__ __forceinline__ Row(const Kv4Where &W, const Tiling &T, int lane, int most) {
     per = (W.d.seqs + 31) / 32;
     long long mine = 0;
 #pragma unroll 4
@@ -66,7 +45,7 @@ struct Row {
       const int b = lane * per + i;
       if (b >= W.d.seqs) break;
       Sequence s;
-      s.load(W, b, group, rows, total_rows);
+      s.load(W, T, b);
       mine += s.all(W.d.kv_heads);
     }
     long long sum = mine;
@@ -82,18 +61,18 @@ struct Row {
   __device__ __forceinline__ long long first_of(long long worker) const { return worker * total / workers; }
   __device__ __forceinline__ int worker_of(long long unit) const { return (int)(((unit + 1) * workers - 1) / total); }
   // The sum before sequence b; the same for all threads.
-  __device__ __forceinline__ long long before_sequence(const Kv4Where &W, int b, int group, int rows, int total_rows, int lane) const {
+  __device__ __forceinline__ long long before_sequence(const Kv4Where &W, const Tiling &T, int b, int lane) const {
     long long v = before;
     if (lane == b / per)
       for (int i = lane * per; i < b; ++i) {
         Sequence s;
-        s.load(W, i, group, rows, total_rows);
+        s.load(W, T, i);
         v += s.all(W.d.kv_heads);
       }
     return __shfl_sync(0xffffffffu, v, b / per);
   }
   // The sequence of a unit (below total), and the sum before it.
-  __device__ __forceinline__ int sequence_of(const Kv4Where &W, long long unit, int group, int rows, int total_rows, int lane, long long &sum) const {
+  __device__ __forceinline__ int sequence_of(const Kv4Where &W, const Tiling &T, long long unit, int lane, long long &sum) const {
     const uint32_t later = __ballot_sync(0xffffffffu, before > unit);
     const int owner = later == 0 ? 31 : __ffs((int)later) - 2;       // the last thread whose sum before it is no more
     int b = 0;
@@ -101,7 +80,7 @@ struct Row {
     if (lane == owner) {
       for (b = lane * per; b + 1 < W.d.seqs; ++b) {
         Sequence s;
-        s.load(W, b, group, rows, total_rows);
+        s.load(W, T, b);
         const long long u = s.all(W.d.kv_heads);
         if (v + u > unit) break;
         v += u;
@@ -151,33 +130,19 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-// 2^i; 0 below fp32's normal numbers.
-__device__ __forceinline__ float power_of_two(int i) { return i < -126 ? 0.0f : __uint_as_float((uint32_t)(i + 127) << 23); }
-// The power of two above a scale, within limits that keep all its uses normal numbers.  Infinity and NaN do not count.
-constexpr int kLeastScale = -100, kMostScale = 127;
-__device__ __forceinline__ int scale_above(float s) {
-  const int i = (int)(__float_as_uint(s) >> 23) & 255;
-  return i == 255 ? kLeastScale : min(kMostScale, max(kLeastScale, i - 126));
-}
-
 // Which token of a record is row i of the products (neighbours are neighbours): keys and values then meet in the fewest banks.
 __device__ __forceinline__ int token_of(int i) { return i ^ ((i >> 1) & 1); }
 
 struct Params {
   Kv4Args A;
-  int group, workers, q_pieces, out_words;      // q can be read in 16-byte pieces, out written in words
+  Tiling T;
+  int workers, q_pieces, out_words;      // q can be read in 16-byte pieces, out written in words
   uint32_t magic, magic16;     // W4Type's of the queries' type and of F16
 };
 
 // Waits of a warp's threads for their own barriers; false: gave up.
 __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
-  return mbar_wait(bar, parity, abort_flag, &g_status_kv4_attention);
+  return mbar_wait(bar, parity, abort_flag, &g_status_kv4_few);
 }
 
 // ---- the copying warp --------------------------------------------------------------------------------------------
@@ -189,7 +154,7 @@ __device__ __forceinline__ void copy_role(const Params &P, const Row &row, long 
   if (lane >= kStages) return;
   Place p;
   p.b = b0;
-  p.s.load(W, b0, P.group, L::kRows, P.A.r.rows);
+  p.s.load(W, P.T, b0);
   long long sum = sum0;
   struct Next { long long record; int valid; };
   auto find = [&](long long u) {
@@ -197,7 +162,7 @@ __device__ __forceinline__ void copy_role(const Params &P, const Row &row, long 
     if (u >= u1) return n;
     while (u >= sum + p.s.all(W.d.kv_heads)) {
       sum += p.s.all(W.d.kv_heads);
-      p.s.load(W, ++p.b, P.group, L::kRows, P.A.r.rows);
+      p.s.load(W, P.T, ++p.b);
     }
     p.set(u - sum);
     n.valid = min(kKvTokens, p.s.len - p.rec * kKvTokens);
@@ -217,7 +182,7 @@ __device__ __forceinline__ void copy_role(const Params &P, const Row &row, long 
       return;
     }
     const bool there = now.record >= 0;
-    if (!there && now.valid > 0) atomicMax(&g_status_kv4_attention, (int)XNOR_ERR_BOUNDS);
+    if (!there && now.valid > 0) atomicMax(&g_status_kv4_few, (int)XNOR_ERR_BOUNDS);
     asm volatile("st.shared.b32 [%0], %1;" ::"r"(smem + L::kValid + 4u * lane), "r"(there ? now.valid : 0) : "memory");
     if (there) {
       mbar_arrive_expect_tx(full, L::kRecord);
@@ -240,7 +205,7 @@ struct TileRow {
   bool in;
   __device__ __forceinline__ TileRow(const Params &P, const Place &p, int rows, int i, int dim) {
     const long long r = (long long)p.tile * rows + i;
-    const int token = (int)(r / P.group), head = p.head * P.group + (int)(r - (long long)token * P.group);
+    const int token = (int)(r / P.T.group), head = p.head * P.T.group + (int)(r - (long long)token * P.T.group);
     in = token < p.s.n;
     q = (p.s.start + token) * P.A.r.q_stride + (long long)head * dim;
     out = (p.s.start + token) * P.A.r.out_stride + (long long)head * dim;
@@ -279,13 +244,13 @@ __device__ __forceinline__ void compute_role(const Params &P, const Row &row, in
   const int tok0 = token_of(g), tok1 = token_of(g + 8);                    // this thread's rows of S^T
   Place p;
   p.b = b0;
-  p.s.load(W, b0, P.group, kRows, P.A.r.rows);
+  p.s.load(W, P.T, b0);
   long long u = u0, sum = sum0;
   bool alive = true;
   while (u < u1) {
     while (u >= sum + p.s.all(W.d.kv_heads)) {
       sum += p.s.all(W.d.kv_heads);
-      p.s.load(W, ++p.b, P.group, kRows, P.A.r.rows);
+      p.s.load(W, P.T, ++p.b);
     }
     p.set(u - sum);
     const long long item0 = u - p.rec;                                     // the item's units
@@ -535,11 +500,12 @@ kv4_few_kernel(const Params P) {
   }
   __syncthreads();
   stream_order();
-  const Row row(P.A.w, P.group, L::kRows, P.A.r.rows, lane, P.workers);
+  const Row row(P.A.w, P.T, lane, P.workers);
+  if (threadIdx.x < 32) P.T.check_lengths(P.A.w, lane, &g_status_kv4_few);
   if (row.total == 0 || (long long)blockIdx.x >= row.workers) return;
   const long long u0 = row.first_of(blockIdx.x), u1 = row.first_of(blockIdx.x + 1);
   long long sum;
-  const int b = row.sequence_of(P.A.w, u0, P.group, L::kRows, P.A.r.rows, lane, sum);
+  const int b = row.sequence_of(P.A.w, P.T, u0, lane, sum);
   if (warp == kWarps)
     copy_role<L>(P, row, u0, u1, b, sum, smem, abort_flag, lane);
   else
@@ -559,13 +525,14 @@ kv4_join_kernel(const Params P, int rows) {
   const Kv4Where &W = P.A.w;
   int b, place;
   if (!find_sequence(W, token, lane, b, place)) return;
-  const Row row(W, P.group, rows, P.A.r.rows, lane, P.workers);
-  const long long before = row.before_sequence(W, b, P.group, rows, P.A.r.rows, lane);
   Sequence s;
-  s.load(W, b, P.group, rows, P.A.r.rows);
-  const long long r = (long long)(token - s.start) * P.group + head % P.group;
+  s.load(W, P.T, b);
+  if (s.n == 0) return;
+  const Row row(W, P.T, lane, P.workers);
+  const long long before = row.before_sequence(W, P.T, b, lane);
+  const long long r = (long long)(token - s.start) * P.T.group + head % P.T.group;
   const int tile = (int)(r / rows), at = (int)(r - (long long)tile * rows);
-  const long long u0 = before + ((long long)(head / P.group) * s.tiles + tile) * s.units;
+  const long long u0 = before + ((long long)(head / P.T.group) * s.tiles + tile) * s.units;
   const int w0 = row.worker_of(u0), w1 = row.worker_of(u0 + s.units - 1);
   if (w0 == w1) return;
   const float *work = static_cast<const float *>(P.A.work);
@@ -590,59 +557,45 @@ kv4_join_kernel(const Params P, int rows) {
   if (lane == 0 && P.A.lse) P.A.lse[(long long)token * P.A.r.q_heads + head] = blind ? -INFINITY : (top + log2f(total)) * kLn2;
 }
 
-template <class K>
-cudaError_t allow_shared(K *kernel, size_t bytes, bool (&flags)[64]) {
-  bool &set = attr_done_for_current_device(flags);
-  if (set) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-  if (e != cudaSuccess) (void)cudaGetLastError();
-  set = e == cudaSuccess;
-  return e;
-}
-
-int tiles_for(const xnor_kv4_desc &d, const xnor_kv4_rows &r) {
-  const long long rows = (long long)(r.most > 0 ? std::min(r.most, r.rows) : r.rows) * (r.q_heads / d.kv_heads);
-  return rows <= 8 ? 1 : 2;
-}
+int tiles_for(const xnor_kv4_desc &d, const xnor_kv4_rows &r) { return kv4_most_rows(d, r) <= 8 ? 1 : 2; }
 
 template <class T, int kDim, int kTiles>
-cudaError_t run(const Kv4Args &a, cudaStream_t st) {
+cudaError_t run(const Kv4Args &a, int most_rows, cudaStream_t st) {
   using L = Layout<kDim, kTiles>;
   static bool flags[64] = {};
   cudaError_t e = allow_shared(kv4_few_kernel<T, kDim, kTiles>, L::kBytes, flags);
   if (e != cudaSuccess) return e;
   const int workers = std::min(kMaxWorkers, kPerSm * sm_count_of_current_device());
-  const Params P = {a, a.r.q_heads / a.w.d.kv_heads, workers, rows_in_pieces(a.q, a.r.q_stride, kDim, 2), a.r.out_stride % 2 == 0, W4Type<T>::kMagic, W4Type<__half>::kMagic};
+  const Params P = {a, {a.r.q_heads / a.w.d.kv_heads, L::kRows, kKvTokens, a.r.rows, 0, most_rows}, workers, rows_in_pieces(a.q, a.r.q_stride, kDim, 2), a.r.out_stride % 2 == 0, W4Type<T>::kMagic, W4Type<__half>::kMagic};
   e = launch_kernel(kv4_few_kernel<T, kDim, kTiles>, dim3((unsigned)workers), 32 * (kWarps + 1), L::kBytes, st, 1, P);
   if (e != cudaSuccess) return e;
   const long long rows = (long long)a.r.rows * a.r.q_heads;
   return launch_kernel(kv4_join_kernel<T, kDim>, dim3((unsigned)((rows + kJoinWarps - 1) / kJoinWarps)), 32 * kJoinWarps, 0, st, 1, P, L::kRows);
 }
 template <class T>
-cudaError_t run_type(const Kv4Args &a, cudaStream_t st) {
+cudaError_t run_type(const Kv4Args &a, int most_rows, cudaStream_t st) {
   const int tiles = tiles_for(a.w.d, a.r);
-  if (a.w.d.dim == 64) return tiles == 1 ? run<T, 64, 1>(a, st) : run<T, 64, 2>(a, st);
-  return tiles == 1 ? run<T, 128, 1>(a, st) : run<T, 128, 2>(a, st);
+  if (a.w.d.dim == 64) return tiles == 1 ? run<T, 64, 1>(a, most_rows, st) : run<T, 64, 2>(a, most_rows, st);
+  return tiles == 1 ? run<T, 128, 1>(a, most_rows, st) : run<T, 128, 2>(a, most_rows, st);
 }
 
 }  // namespace
 
-size_t kv4_work_bytes(const xnor_kv4_desc &d, const xnor_kv4_rows &r) {
+size_t kv4_few_work_bytes(const xnor_kv4_desc &d, const xnor_kv4_rows &r) {
   return 2 * (size_t)kMaxWorkers * slot_floats(8 * tiles_for(d, r), d.dim) * sizeof(float);
 }
 
-cudaError_t read_status_kv4_attention(int *status) {
-  cudaError_t e = cudaMemcpyFromSymbol(status, g_status_kv4_attention, sizeof(int));
+cudaError_t read_status_kv4_few(int *status) {
+  cudaError_t e = cudaMemcpyFromSymbol(status, g_status_kv4_few, sizeof(int));
   if (e == cudaSuccess && *status != 0) {
     const int zero = 0;
-    e = cudaMemcpyToSymbol(g_status_kv4_attention, &zero, sizeof(int));
+    e = cudaMemcpyToSymbol(g_status_kv4_few, &zero, sizeof(int));
   }
   return e;
 }
 
-cudaError_t launch_kv4_attention(const Kv4Args &a, cudaStream_t st) {
-  if (a.r.rows == 0) return cudaSuccess;
-  return a.r.type == XNOR_BF16 ? run_type<__nv_bfloat16>(a, st) : run_type<__half>(a, st);
+cudaError_t launch_kv4_few(const Kv4Args &a, int most_rows, cudaStream_t st) {
+  return a.r.type == XNOR_BF16 ? run_type<__nv_bfloat16>(a, most_rows, st) : run_type<__half>(a, most_rows, st);
 }
 
 }  // namespace xnor
