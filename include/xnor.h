@@ -667,7 +667,7 @@ xnor_status xnor_kv4_read(const void *cache, const int32_t *starts, const int32_
  *         chooses its kernels; where it is too small, results are as good and may take longer
  *   work  scratch of xnor_kv4_work_bytes(d, r) bytes, whatever is in it; calls that can overlap need one each
  * Codes and queries are exact operands; products, sums and the softmax are fp32, but exp(..) times a value's
- * scale, which is rounded to 11 bits (below 2^-26 of the largest scale to a step of 2^-36 of that) to meet the values' codes.  The order of
+ * scale, which is rounded to 11 bits (below 2^-21 of the largest scale to a step of 2^-31 of that) to meet the values' codes.  The order of
  * the sums depends on the sizes, all sequences' lengths and the device's number of SMs: the same call gives the same bits.
  * Device-side waits are bounded (xnor_check_device).  What lies outside the table or the cache is not seen.
  * INVALID_ARG as above, and: q_heads no multiple of kv_heads, scale not finite, most < 0, out in the place of q.

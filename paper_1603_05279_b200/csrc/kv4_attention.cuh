@@ -6,7 +6,11 @@
 namespace xnor {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kRaise = 3.0f;               // a row's maximum is left behind by 2^3 at most
+// A row's maximum is left behind by 2^8 at most: then P, up to 2^8 times a value's scale, is rounded to F16, relative to a
+// power of two 2^e above the largest scale so far and times 2^7.  That is at most 2^15, and has all 11 bits
+// down to 2^-21 of that scale.  (As bfloat16 it gave outputs in bfloat16 half as much again of error.)
+constexpr float kRaise = 8.0f;
+constexpr int kLift = 7;
 
 struct Sequence;
 // How a call's rows are cut: tiles of `rows` queries of a head's group, units of `tokens`; of sequences with more than

@@ -7,10 +7,7 @@
 // queries, up to 8 kTiles of them, the other: S^T = K Q^T, then O^T += V^T P^T, whose codes - zero come straight from
 // a record's words, exactly.  A key's scale multiplies its row of S^T, a value's its row of P^T, which a matrix transposition
 // within the warp (movmatrix) makes the second operand.  The softmax is one pass: a running maximum, raised (and
-// the sums rescaled) only when it is exceeded by more than 2^3, and sums in fp32.
-// P, times the values' scales, is rounded to F16, 11 bits, relative to the largest scale so far (a power of two 2^e
-// above it) and times 2^12: at most 2^15, and with all 11 bits down to 2^-26 of that scale.  (As bfloat16 it gave outputs
-// in bfloat16 half as much again of error.)
+// the sums rescaled) only when it is exceeded by more than 2^8, and sums in fp32.
 //
 // A block: one warp copies records into a ring in shared memory, a thread a stage, and eight or four warps take every
 // so-many-th unit each; at an item's end (the units of a tile) they add their sums.  An item that lies in
@@ -366,8 +363,8 @@ __device__ __forceinline__ void compute_role(const Params &P, const Row &row, in
             }
           }
       }
-      vs0 *= power_of_two(12 - e);
-      vs1 *= power_of_two(12 - e);
+      vs0 *= power_of_two(kLift - e);
+      vs1 *= power_of_two(kLift - e);
       uint32_t b[kTiles][2];                                               // P^T: tokens 0 .. 7 and 8 .. 15 of the rows
 #pragma unroll
       for (int n = 0; n < kTiles; ++n) {
@@ -423,7 +420,7 @@ __device__ __forceinline__ void compute_role(const Params &P, const Row &row, in
       }
     }
     // ---- the warps' sums together
-    const float back = power_of_two(e - 12);
+    const float back = power_of_two(e - kLift);
 #pragma unroll
     for (int n = 0; n < kTiles; ++n)
 #pragma unroll

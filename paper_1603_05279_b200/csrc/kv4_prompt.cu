@@ -1,15 +1,17 @@
 // Attention over the cache in 4 bits for many new tokens of a sequence, on the 5th-generation tensor cores.
 //
 // A block computes one item: up to 256 rows (queries of a head's group, token by token) in two halves of 128, over their
-// context in tiles of 128 tokens.  S = Q K^T (128 x 128) and O += P V run on tcgen05.mma kind::f16 with fp32 sums in tensor memory:
-// S and O of both halves fill it, and P, in F16, lies where S lay.  Keys and values become code - zero, exactly, in shared
+// context in tiles of 128 tokens, 64 at a step.  S = Q K^T (128 x 64) and O += P V run on tcgen05.mma kind::f16 with fp32 sums in tensor
+// memory: two S and an O of both halves fill it, and P, in F16, lies where S lay.  Two S, so that the products of a step run while the
+// softmax is busy with another (one S of 128 tokens left the tensor cores idle while both halves weighed: 545 us for two
+// prompts of 4096 tokens).  Keys and values become code - zero, exactly, in shared
 // memory; a key's scale multiplies its column of S, a value's its column of P (rounded to F16 as in the kernel for few
-// rows).  The softmax is one pass with a running maximum that may be left behind by 2^3, so that O is rescaled rarely.
+// rows).  The softmax is one pass with a running maximum that may be left behind by 2^8, so that O is rescaled rarely.
 //
 // Warps: 0 - 7  softmax: a thread has a row of its half; it also brings the row's query and takes its output away
-//        8 - 11 expansion: 4-bit records into operands of 128 tokens (three stages), and the columns' scales
-//        12     issues the products: while one half's softmax runs, the other half's P V and the next Q K^T
-//        13     copies records into a ring in shared memory, a thread a record
+//        8 - 11 keys from 4-bit records into operands of 128 tokens (three stages), and the columns' scales; 12 - 15 values
+//        16     issues the products
+//        17     copies records into a ring in shared memory, a thread a record
 // Where there are too few items for the GPU, the blocks of an item divide its context, and a second kernel joins
 // their sums.  Every wait is bounded; on expiry the block records XNOR_ERR_TIMEOUT, stops and frees its tensor memory.
 #include <algorithm>
@@ -27,10 +29,11 @@ using namespace umma;
 
 constexpr int kHalf = 128, kItemRows = 2 * kHalf;
 constexpr int kTokens = 128, kRecords = kTokens / kKvTokens;     // of a tile
+constexpr int kStep = 64, kStepRecords = kStep / kKvTokens;
 constexpr int kOperands = 3, kRawStages = 2, kScaleBufs = 4;
-constexpr int kExpandWarp = 8, kMmaWarp = 12, kCopyWarp = 13, kThreads = 16 * 32;
-constexpr int kSoftmaxRegs = 184, kOtherRegs = 72, kLaunchRegs = 128;
-static_assert(8 * 32 * (kSoftmaxRegs + kOtherRegs) <= kThreads * kLaunchRegs, "registers");
+constexpr int kKeyWarp = 8, kValueWarp = 12, kMmaWarp = 16, kCopyWarp = 17, kThreads = 20 * 32;
+constexpr int kSoftmaxRegs = 144, kOtherRegs = 64, kLaunchRegs = 96;
+static_assert(kKeyWarp * 32 * kSoftmaxRegs + (kThreads - kKeyWarp * 32) * kOtherRegs <= kThreads * kLaunchRegs, "registers");
 constexpr int kMaxSplits = 8;
 
 template <int kDim>
@@ -38,7 +41,7 @@ struct Layout {
   static constexpr uint32_t kOperand = kTokens * kDim * 2;       // also of 128 queries
   static constexpr uint32_t kRaw = kRecords * kv4_record(kDim);
   static constexpr uint32_t kRawFull = 0, kRawEmpty = kRawFull + 8 * kRawStages, kFull = kRawEmpty + 8 * kRawStages, kEmpty = kFull + 8 * kOperands;
-  static constexpr uint32_t kSFull = kEmpty + 8 * kOperands, kPFull = kSFull + 16, kQFull = kPFull + 16;
+  static constexpr uint32_t kSFull = kEmpty + 8 * kOperands, kPFull = kSFull + 32, kODone = kPFull + 32, kLast = kODone + 16, kQFull = kLast + 16;      // [half][S]
   static constexpr uint32_t kScaled = kQFull + 16, kTmem = kScaled + 8 * kScaleBufs, kAbort = kTmem + 4, kItem = kAbort + 4, kMask = kItem + 32, kExponent = kMask + 4 * kRawStages;
   static constexpr uint32_t kThere = kExponent + 4 * kScaleBufs;
   static constexpr uint32_t kScales = 512, kRing = kScales + kScaleBufs * 2 * kTokens * 4;
@@ -111,7 +114,7 @@ __device__ __forceinline__ int rank_of(const Params &P, int b, int tile, int lan
 
 // An item's tiles of context, and the share of them that one of its blocks has.
 struct Span {
-  int tiles, splits, first, last;
+  int tiles, splits, first, last, steps;
   __device__ __forceinline__ Span(const Params &P, const Sequence &s, int tile, int split) {
     const long long end_row = min((long long)s.n * P.T.group, (long long)(tile + 1) * kItemRows);
     const int last_token = (int)((end_row - 1) / P.T.group);
@@ -120,6 +123,7 @@ struct Span {
     splits = min(P.splits, max(1, tiles / 4));
     first = (int)((long long)tiles * split / splits);
     last = (int)((long long)tiles * (split + 1) / splits);
+    steps = (min(last * kTokens, seen) - first * kTokens + kStep - 1) / kStep;
   }
 };
 
@@ -128,9 +132,9 @@ __device__ __forceinline__ size_t partial_floats(int dim) { return (size_t)kItem
 struct Block {                // what all roles know
   const Params &P;
   Sequence s;
-  int b, head, tile, first, last;
+  int b, head, tile, first, last, steps;
   bool two, direct;           // both halves have rows; the block has the whole context
-  uint32_t smem, q, operands, tmem;
+  uint32_t smem, q, operands;
   uint8_t *ptr;
   volatile int *abort_flag;
   float *partial;
@@ -194,23 +198,22 @@ __device__ __forceinline__ void copy_role(const Block &B, int lane) {
 // token.  Values: a row is a column of O, its values tokens; so eight tokens' codes are transposed on the way, by
 // choosing bytes of two tokens at a time.
 template <class T, int kDim>
-__device__ __forceinline__ void expand_role(const Block &B, int id) {
+__device__ __forceinline__ void key_role(const Block &B, int id) {
   using L = Layout<kDim>;
-  using V = W4Type<__half>;
   constexpr uint32_t kRecord = kv4_record(kDim);
   constexpr int kQuads = kDim / 32;                        // of words in a token's codes
   const int lane = id & 31;
   const float scale2 = B.P.A.r.scale * kLog2e;
   float *scales = reinterpret_cast<float *>(B.ptr + L::kScales);
   int e = kLeastScale;
-  uint32_t op = 0u;                                        // operands so far
+#pragma unroll 1
   for (int t = B.first; t < B.last; ++t) {
     const int i = t - B.first;
+    const uint32_t op = 2u * (uint32_t)i, stage = op % kOperands;
     const uint32_t slot = (uint32_t)i % kRawStages, raw = B.smem + L::kRing + slot * L::kRaw, buf = (uint32_t)i % kScaleBufs;
     if (!wait_warp(B, B.smem + L::kRawFull + 8u * slot, (uint32_t)(i / kRawStages) & 1u)) return;
-    const uint32_t there = lds32(B.smem + L::kMask + 4u * slot);
-    uint32_t stage = op % kOperands;
     if (!wait_warp(B, B.smem + L::kEmpty + 8u * stage, ((op / kOperands) & 1u) ^ 1u)) return;
+    const uint32_t there = lds32(B.smem + L::kMask + 4u * slot);
     {
       // the columns' scales; all warps find the largest value's
       int above = e;
@@ -224,7 +227,7 @@ __device__ __forceinline__ void expand_role(const Block &B, int id) {
       const bool in = (there >> (id / kKvTokens) & 1u) && t * kTokens + id < B.s.len;
       const uint32_t words = raw + (uint32_t)(id / kKvTokens) * kRecord + 4u * (id % kKvTokens);
       scales[(2 * buf) * kTokens + id] = in ? kv4_scale(lds32(words + kv4_words(kDim, false))) * scale2 : 0.0f;
-      scales[(2 * buf + 1) * kTokens + id] = in ? kv4_scale(lds32(words + kv4_words(kDim, true))) * power_of_two(12 - e) : 0.0f;
+      scales[(2 * buf + 1) * kTokens + id] = in ? kv4_scale(lds32(words + kv4_words(kDim, true))) * power_of_two(kLift - e) : 0.0f;
       if (id == 0) {
         sts32(B.smem + L::kExponent + 4u * buf, (uint32_t)e);
         sts32(B.smem + L::kThere + 4u * buf, there);
@@ -254,9 +257,25 @@ __device__ __forceinline__ void expand_role(const Block &B, int id) {
     }
     fence_proxy_async();
     __syncwarp();
-    if (lane == 0) mbar_arrive(B.smem + L::kFull + 8u * stage);
-    ++op;
-    stage = op % kOperands;
+    if (lane == 0) {
+      mbar_arrive(B.smem + L::kFull + 8u * stage);
+      mbar_arrive(B.smem + L::kRawEmpty + 8u * slot);
+    }
+  }
+}
+
+template <int kDim>
+__device__ __forceinline__ void value_role(const Block &B, int id) {
+  using L = Layout<kDim>;
+  using V = W4Type<__half>;
+  constexpr uint32_t kRecord = kv4_record(kDim);
+  constexpr int kQuads = kDim / 32;
+#pragma unroll 1
+  for (int t = B.first; t < B.last; ++t) {
+    const int i = t - B.first;
+    const uint32_t op = 2u * (uint32_t)i + 1u, stage = op % kOperands;
+    const uint32_t slot = (uint32_t)i % kRawStages, raw = B.smem + L::kRing + slot * L::kRaw;
+    if (!wait_warp(B, B.smem + L::kRawFull + 8u * slot, (uint32_t)(i / kRawStages) & 1u)) return;
     if (!wait_warp(B, B.smem + L::kEmpty + 8u * stage, ((op / kOperands) & 1u) ^ 1u)) return;
     {
       const uint32_t to = B.operands + stage * L::kOperand;
@@ -300,11 +319,10 @@ __device__ __forceinline__ void expand_role(const Block &B, int id) {
     }
     fence_proxy_async();
     __syncwarp();
-    if (lane == 0) {
+    if ((id & 31) == 0) {
       mbar_arrive(B.smem + L::kFull + 8u * stage);
       mbar_arrive(B.smem + L::kRawEmpty + 8u * slot);
     }
-    ++op;
   }
 }
 
@@ -312,17 +330,25 @@ __device__ __forceinline__ void expand_role(const Block &B, int id) {
 __device__ __forceinline__ uint64_t swizzled_desc(uint32_t addr) {
   return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
-__device__ __forceinline__ void mma_shared(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// The whole warp runs the loop, and one thread issues: so what the instructions take stays in uniform registers.  (Run by one thread
+// alone, each product cost it 60 cycles, as many as the tensor core.)
+__device__ __forceinline__ void mma_shared(uint32_t leader, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
 }
-__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void mma_tmem(uint32_t leader, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t leader, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+      ::"r"(bar), "r"(leader) : "memory");
 }
 // D fp32, A and B of one 16-bit type, both K-major, M = 128.
 __host__ __device__ constexpr uint32_t instruction(bool bf16, int n) {
@@ -332,87 +358,84 @@ __host__ __device__ constexpr uint32_t instruction(bool bf16, int n) {
 template <class T, int kDim>
 __device__ __forceinline__ void mma_role(const Block &B) {
   using L = Layout<kDim>;
-  constexpr uint32_t kSDesc = instruction(std::is_same<T, __nv_bfloat16>::value, kTokens), kODesc = instruction(false, kDim);
-  const int n = B.last - B.first, halves = B.two ? 2 : 1;
+  constexpr uint32_t kSDesc = instruction(std::is_same<T, __nv_bfloat16>::value, kStep), kODesc = instruction(false, kDim);
+  const int n = B.steps, halves = B.two ? 2 : 1;
+  const uint32_t leader = elect_one();
   const uint64_t q0 = swizzled_desc(B.q), op0 = swizzled_desc(B.operands);
-  auto qk = [&](int half, uint32_t stage) {
+  auto full = [&](uint32_t op) {
+    const bool ok = wait_warp(B, B.smem + L::kFull + 8u * (op % kOperands), (op / kOperands) & 1u);
+    tc_fence_after();
+    return ok;
+  };
+  auto free_operand = [&](uint32_t op) { commit(leader, B.smem + L::kEmpty + 8u * (op % kOperands)); };
+  // S of step j, of half h
+  auto qk = [&](int h, int j) {
+    const uint32_t op = (uint32_t)j & ~1u, sub = (uint32_t)j & 1u;
+    if (sub == 0u && h == 0 && !full(op)) return false;
+    const uint64_t queries = q0 + (uint64_t)((uint32_t)h * (L::kOperand / 16)), keys = op0 + (uint64_t)((op % kOperands) * (L::kOperand / 16) + sub * (kStep * 128 / 16));
+    const uint32_t to = (uint32_t)h * kTokens + sub * kStep;
 #pragma unroll
     for (int k = 0; k < kDim / 16; ++k) {
       const uint64_t step = (uint64_t)((uint32_t)(k / 4) * (kTokens * 128 / 16) + 2u * (uint32_t)(k % 4));
-      mma_shared(B.tmem + (uint32_t)(half * kTokens), q0 + (uint64_t)((uint32_t)half * (L::kOperand / 16)) + step, op0 + (uint64_t)(stage * (L::kOperand / 16)) + step, kSDesc,
-                 k > 0 ? 1u : 0u);
+      mma_shared(leader, to, queries + step, keys + step, kSDesc, k > 0 ? 1u : 0u);
     }
-    umma_commit(B.smem + L::kSFull + 8u * half);
+    commit(leader, B.smem + L::kSFull + 16u * h + 8u * sub);
+    if (h + 1 == halves && (sub == 1u || j + 1 == n)) free_operand(op);
+    return true;
   };
-  auto pv = [&](int half, uint32_t stage, bool first) {
-#pragma unroll
-    for (int k = 0; k < kTokens / 16; ++k) {
-      const uint64_t step = (uint64_t)((uint32_t)(k / 4) * (kDim * 128 / 16) + 2u * (uint32_t)(k % 4));
-      mma_tmem(B.tmem + L::kO + (uint32_t)(half * kDim), B.tmem + (uint32_t)(half * kTokens + 8 * k), op0 + (uint64_t)(stage * (L::kOperand / 16)) + step, kODesc,
-               first && k == 0 ? 0u : 1u);
-    }
-  };
-  auto full = [&](uint32_t op) { return wait(B, B.smem + L::kFull + 8u * (op % kOperands), (op / kOperands) & 1u); };
   for (int h = 0; h < halves; ++h)
-    if (!wait(B, B.smem + L::kQFull + 8u * h, 0u)) return;
-  if (!full(0u)) return;
-  tc_fence_after();
-  for (int h = 0; h < halves; ++h) qk(h, 0u);
-  umma_commit(B.smem + L::kEmpty);
+    if (!wait_warp(B, B.smem + L::kQFull + 8u * h, 0u)) return;
+  for (int j = 0; j < min(n, 2); ++j)
+    for (int h = 0; h < halves; ++h)
+      if (!qk(h, j)) return;
 #pragma unroll 1
-  for (int i = 0; i < n; ++i) {
-    const uint32_t values = 2u * (uint32_t)i + 1u, keys = values + 1u;
-    if (!full(values)) return;
+  for (int j = 0; j < n; ++j) {
+    const uint32_t op = (uint32_t)j | 1u, sub = (uint32_t)j & 1u;
+    if (sub == 0u && !full(op)) return;
+    const uint64_t values = op0 + (uint64_t)((op % kOperands) * (L::kOperand / 16) + sub * (kDim * 128 / 16));
+#pragma unroll 1
     for (int h = 0; h < halves; ++h) {
-      if (!wait(B, B.smem + L::kPFull + 8u * h, (uint32_t)i & 1u)) return;
+      if (!wait_warp(B, B.smem + L::kPFull + 16u * h + 8u * sub, (uint32_t)(j >> 1) & 1u)) return;
       tc_fence_after();
-      pv(h, values % kOperands, i == 0);
-      if (h + 1 == halves) umma_commit(B.smem + L::kEmpty + 8u * (values % kOperands));
-      if (i + 1 < n) {
-        if (h == 0 && !full(keys)) return;
-        tc_fence_after();
-        qk(h, keys % kOperands);                           // (behind P V, whose P it overwrites)
-        if (h + 1 == halves) umma_commit(B.smem + L::kEmpty + 8u * (keys % kOperands));
-      } else {
-        umma_commit(B.smem + L::kSFull + 8u * h);          // O is done
-      }
+      const uint32_t to = L::kO + (uint32_t)h * kDim, weights = (uint32_t)h * kTokens + sub * kStep;
+#pragma unroll
+      for (int k = 0; k < kStep / 16; ++k) mma_tmem(leader, to, weights + 8u * k, values + (uint64_t)(2 * k), kODesc, j == 0 && k == 0 ? 0u : 1u);
+      if (j + 2 >= n) commit(leader, B.smem + (j + 1 < n ? L::kODone : L::kLast) + 8u * h);
+      if (h + 1 == halves && (sub == 1u || j + 1 == n)) free_operand(op);
+      if (j + 2 < n && !qk(h, j + 2)) return;              // (behind P V, whose P it overwrites)
     }
   }
 }
 
 // ---- softmax -------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
+// S and O leave tensor memory with two neighbouring columns of a row in a thread (rows g and g + 8 of 16, columns 2 t and
+// 2 t + 1 of eight, for lane 4 g + t), and P goes back likewise: so a thread has four rows, which share the scales that it reads.
+// (A row a thread took as many bytes of scales from shared memory as there are values of S, in competition with the products.)
+__device__ __forceinline__ void tmem_ld_rows(uint32_t taddr, uint32_t (&r)[16]) {      // 16 rows x 32 columns
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
-        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr) : "memory");
 }
-// Every tcgen05.ld of this thread has returned; the registers are operands so that nothing uses them before.
-__device__ __forceinline__ void tmem_wait32(uint32_t (&r)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
-                 "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]),
-                 "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
-               :: "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+__device__ __forceinline__ void tmem_st_rows(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_rows(uint32_t (&r)[16]) { tmem_wait16(*reinterpret_cast<int32_t (*)[16]>(&r)); }
+// P of 16 rows x 64 columns, in 32 columns of tensor memory.
+__device__ __forceinline__ void tmem_st_weights(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], "
       "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
       ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-__device__ __forceinline__ float4 lds_float4(uint32_t addr) {
-  uint32_t v[4];
-  lds128(addr, v);
-  return make_float4(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3]));
-}
 
 // Two fp32 operations at once.
 __device__ __forceinline__ uint64_t pack2(float a, float b) {
@@ -430,184 +453,289 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pack2(a.x, a.y)), "l"(pack2(b.x, b.y)));
   return unpack2(r);
 }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pack2(a.x, a.y)), "l"(pack2(b.x, b.y)), "l"(pack2(c.x, c.y)));
+  return unpack2(r);
+}
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   uint64_t r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pack2(a.x, a.y)), "l"(pack2(b.x, b.y)));
   return unpack2(r);
+}
+__device__ __forceinline__ float2 lds_float2(uint32_t addr) {
+  uint32_t a, b;
+  lds64(addr, a, b);
+  return make_float2(__uint_as_float(a), __uint_as_float(b));
+}
+
+// The weights of a step, against the rows' maxima m: p = exp2(s ks - m) times the values' scales, as pairs of F16; their sums before
+// that; and the largest s ks - m, each of this thread's columns (2 t and 2 t + 1 of eight, of rows g, g + 8, g + 16 and g + 24 of 32;
+// scales: theirs).  kMasked: columns from `seen` on (counted from 2 t) are not seen, nor are records that are
+// missing; and s ks is rounded before m is taken from it, so that the maximum itself gives 0 whatever its size.
+struct Scales { float2 k[kStep / 8], v[kStep / 8]; };
+template <bool kMasked>
+__device__ __forceinline__ void weigh(uint32_t S, const Scales &scales, const float (&m)[4], const int (&seen)[4], uint32_t there, uint32_t (&p)[2][16],
+                                      float (&sum)[4], float (&top)[4]) {
+  float2 sums[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    sums[r] = make_float2(0.0f, 0.0f);
+    top[r] = -INFINITY;
+  }
+  uint32_t raw[2][2][16];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    tmem_ld_rows(S + 32u * c, raw[c][0]);
+    tmem_ld_rows(S + (16u << 16) + 32u * c, raw[c][1]);
+  }
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    tmem_wait_rows(raw[c][0]);
+    tmem_wait_rows(raw[c][1]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int column = 32 * c + 8 * k;
+      const float2 f = scales.k[4 * c + k], g = scales.v[4 * c + k];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const uint32_t *x = raw[c][r >> 1] + 4 * k + 2 * (r & 1);
+        float2 u = make_float2(__uint_as_float(x[0]), __uint_as_float(x[1]));
+        const int end = !kMasked ? 0 : (there >> (column / kKvTokens) & 1u) ? seen[r] : INT_MIN;
+        if (kMasked) {
+          u = make_float2(__fadd_rn(__fmul_rn(u.x, f.x), -m[r]), __fadd_rn(__fmul_rn(u.y, f.y), -m[r]));
+          if (column >= end) u.x = -INFINITY;
+          if (column + 1 >= end) u.y = -INFINITY;
+        } else {
+          u = fma2(u, f, make_float2(-m[r], -m[r]));
+        }
+        top[r] = fmaxf(fmaxf(u.x, u.y), top[r]);
+        u = make_float2(exp2_fast(u.x), exp2_fast(u.y));
+        sums[r] = add2(sums[r], u);
+        u = mul2(u, g);
+        if (kMasked) {                                     // (a token that is not seen may stand for anything)
+          if (column >= end) u.x = 0.0f;
+          if (column + 1 >= end) u.y = 0.0f;
+        }
+        p[r >> 1][2 * (4 * c + k) + (r & 1)] = float_to_pair(u.x, u.y, __half());
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) sum[r] = sums[r].x + sums[r].y;
+}
+
+// Of four values for rows g, g + 8, .. that a thread has, the one for row `lane`.
+__device__ __forceinline__ float of_row(const float (&v)[4], int lane) {
+  float got = 0.0f;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const float x = __shfl_sync(0xffffffffu, v[r], 4 * (lane & 7));
+    got = lane >> 3 == r ? x : got;
+  }
+  return got;
 }
 
 template <class T, int kDim>
 __device__ __forceinline__ void softmax_role(const Block &B, int half, int quarter, int lane) {
   using L = Layout<kDim>;
   const Params &P = B.P;
-  const int in_tile = 32 * quarter + lane;
+  const int in_tile = 32 * quarter + lane, g = lane >> 2, t = lane & 3;
+  if (half == 1 && !B.two) return;
   const long long r = (long long)B.tile * kItemRows + half * kHalf + in_tile;
   const int token = (int)(r / P.T.group), head = B.head * P.T.group + (int)(r - (long long)token * P.T.group);
   const bool in = token < B.s.n;
   const long long row = B.s.start + token;
-  const int limit = in ? min(B.s.lead + B.s.start + token, B.s.len - 1) : INT_MAX;        // the last token that it sees
-  if (half == 1 && !B.two) return;
-  // the query, 64 columns a block
+  const int limit = in ? min(B.s.lead + B.s.start + token, B.s.len - 1) : INT_MAX;        // the last token that the row of this lane sees
+  // the queries, 64 columns a block: kDim / 8 lanes a row
   {
-    const T *q = static_cast<const T *>(P.A.q) + (in ? row * P.A.r.q_stride + (long long)head * kDim : 0);
-    const uint32_t to = B.q + (uint32_t)half * L::kOperand + (uint32_t)in_tile * 128u;
+    constexpr int kLanes = kDim / 8, kRows = 32 / kLanes;
+    const long long from = in ? row * P.A.r.q_stride + (long long)head * kDim : -1;
+    const uint32_t to = B.q + (uint32_t)half * L::kOperand;
+    const int c = lane % kLanes;
 #pragma unroll
-    for (int c = 0; c < kDim / 8; ++c) {
-      Chunk<T> v;
-      v.load(q + 8 * c, P.q_pieces, in ? 8 : 0);
-      sts128(to + (uint32_t)(c / 8) * (kTokens * 128) + (uint32_t)(((c & 7) ^ (in_tile & 7)) * 16), v.w[0], v.w[1], v.w[2], v.w[3]);
+    for (int j = 0; j < 32 / kRows; j += 16 / (128 / kDim)) {
+      constexpr int kAtOnce = 16 / (128 / kDim);
+      Chunk<T> v[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const long long at = __shfl_sync(0xffffffffu, from, (j + i) * kRows + lane / kLanes);
+        v[i].load(static_cast<const T *>(P.A.q) + max(at, 0ll) + 8 * c, P.q_pieces, at >= 0 ? 8 : 0);
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int r = 32 * quarter + (j + i) * kRows + lane / kLanes;
+        sts128(to + (uint32_t)(c / 8) * (kTokens * 128) + (uint32_t)(r * 128 + ((c & 7) ^ (r & 7)) * 16), v[i].w[0], v[i].w[1], v[i].w[2], v[i].w[3]);
+      }
     }
     fence_proxy_async();
     __syncwarp();
     if (lane == 0) mbar_arrive(B.smem + L::kQFull + 8u * half);
   }
-  const uint32_t lanes = B.tmem + ((uint32_t)(32 * quarter) << 16), S = lanes + (uint32_t)(half * kTokens), O = lanes + L::kO + (uint32_t)(half * kDim);
-  const int n = B.last - B.first, least = __reduce_min_sync(0xffffffffu, limit);
-  float m = -INFINITY, l = 0.0f;
-  int e = kLeastScale;
+  const uint32_t lanes = (uint32_t)(32 * quarter) << 16, S = lanes + (uint32_t)(half * kTokens), O = lanes + L::kO + (uint32_t)(half * kDim);
+  const int n = B.steps, least = __reduce_min_sync(0xffffffffu, limit);
+  // a row's maximum so far, 0 where it has seen nothing (`unset`: a bit for each), and the sum of its weights
+  float m[4], l[4];
+  int limits[4], unset = 15, e = kLeastScale;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    m[j] = l[j] = 0.0f;
+    limits[j] = __shfl_sync(0xffffffffu, limit, g + 8 * j);
+  }
+  bool calm = false;           // all of the warp's rows have a maximum, below 2^20 (from there on what rounding leaves of s ks - m would count)
 #pragma unroll 1
   for (int i = 0; i < n; ++i) {
-    const uint32_t buf = (uint32_t)i % kScaleBufs;
-    if (!wait_inline(B, B.smem + L::kSFull + 8u * half, (uint32_t)i & 1u) ||
-        !wait_inline(B, B.smem + L::kScaled + 8u * buf, (uint32_t)(i / kScaleBufs) & 1u))
-      return;
-    tc_fence_after();
-    const uint32_t ks = B.smem + L::kScales + 2u * buf * kTokens * 4u, vs = ks + kTokens * 4u;
+    const uint32_t tile = (uint32_t)(i >> 1), sub = (uint32_t)i & 1u, buf = tile % kScaleBufs;
+    if (sub == 0u && !wait_inline(B, B.smem + L::kScaled + 8u * buf, (tile / kScaleBufs) & 1u)) return;
+    Scales scales;
+    const uint32_t ks = B.smem + L::kScales + 4u * (2u * buf * kTokens + sub * kStep) + 8u * t;
+#pragma unroll
+    for (int k = 0; k < kStep / 8; ++k) {
+      scales.k[k] = lds_float2(ks + 32u * k);
+      scales.v[k] = lds_float2(ks + 4u * kTokens + 32u * k);
+    }
     const int e_now = (int)lds32(B.smem + L::kExponent + 4u * buf);
-    const uint32_t there = lds32(B.smem + L::kThere + 4u * buf);
-    const int t0 = (B.first + i) * kTokens;
-    float2 x[kTokens / 2];
-    float top = -INFINITY;
-    const bool whole = there == (1u << kRecords) - 1u && t0 + kTokens - 1 <= least;
-    {
-      uint32_t a[32], b[32];
-      auto scaled = [&](int c, const uint32_t (&raw)[32]) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float4 f = lds_float4(ks + 16u * (uint32_t)(8 * c + j));
-          x[16 * c + 2 * j] = mul2(make_float2(__uint_as_float(raw[4 * j]), __uint_as_float(raw[4 * j + 1])), make_float2(f.x, f.y));
-          x[16 * c + 2 * j + 1] = mul2(make_float2(__uint_as_float(raw[4 * j + 2]), __uint_as_float(raw[4 * j + 3])), make_float2(f.z, f.w));
-        }
-      };
-      tmem_ld32(S, a);
-      tmem_wait32(a);
-      tmem_ld32(S + 32u, b);
-      scaled(0, a);
-      tmem_wait32(b);
-      tmem_ld32(S + 64u, a);
-      scaled(1, b);
-      tmem_wait32(a);
-      tmem_ld32(S + 96u, b);
-      scaled(2, a);
-      tmem_wait32(b);
-      scaled(3, b);
+    const uint32_t there = lds32(B.smem + L::kThere + 4u * buf) >> (kStepRecords * sub) & ((1u << kStepRecords) - 1u);
+    if (!wait_inline(B, B.smem + L::kSFull + 16u * half + 8u * sub, tile & 1u)) return;
+    tc_fence_after();
+    const uint32_t here = S + sub * kStep;
+    const int t0 = B.first * kTokens + i * kStep;
+    const int none[4] = {};
+    uint32_t p[2][16];
+    float sum[4], top[4];
+    bool good = false;
+    if (calm && there == (1u << kStepRecords) - 1u && t0 + kStep - 1 <= least && e_now == e) {
+      weigh<false>(here, scales, m, none, 0u, p, sum, top);
+      good = !__any_sync(0xffffffffu, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) > kRaise);
     }
-    if (!whole) {
+    if (!good) {
+      // What is masked, and where a maximum is left too far behind: that is raised, and the step weighed again (once; where numbers are so
+      // large that rounding moves the maximum again, once more).
+#pragma unroll 1
+      for (int attempt = 0;; ++attempt) {
+        int seen[4];
 #pragma unroll
-      for (int j = 0; j < kTokens / 2; ++j) {
-        const bool here = there >> (2 * j / kKvTokens) & 1u;
-        if (!here || t0 + 2 * j > limit) x[j].x = -INFINITY;
-        if (!here || t0 + 2 * j + 1 > limit) x[j].y = -INFINITY;
+        for (int j = 0; j < 4; ++j) seen[j] = (limits[j] < t0 ? 0 : min(limits[j] - t0, kStep) + 1) - 2 * t;
+        weigh<true>(here, scales, m, seen, there, p, sum, top);
+        int up = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+          for (int x = 1; x < 4; x *= 2) top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], x));
+          if (unset >> j & 1 ? top[j] > -INFINITY : top[j] > kRaise) up |= 1 << j;
+        }
+        const bool again = attempt < 3 && __any_sync(0xffffffffu, up != 0);
+        if (!again && e_now == e) break;
+        const float down = power_of_two(e - e_now);
+        float f[4];
+        calm = true;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          f[j] = 1.0f;
+          if (again && (up >> j & 1)) {
+            const float above = m[j] + top[j];
+            f[j] = unset >> j & 1 ? 0.0f : exp2_fast(m[j] - above);
+            m[j] = above;
+          }
+          l[j] *= f[j];
+          f[j] *= down;
+          calm = calm && fabsf(m[j]) < 1048576.0f;
+        }
+        if (again) unset &= ~up;
+        calm = __all_sync(0xffffffffu, calm && unset == 0);
+        e = e_now;
+        if (i > 0) {
+          // P V of the last step has to be done: the next step's S comes behind it
+          if (!(i + 1 < n ? wait_inline(B, B.smem + L::kSFull + 16u * half + 8u * (sub ^ 1u), (uint32_t)((i + 1) >> 1) & 1u) : wait_inline(B, B.smem + L::kODone + 8u * half, 0u))) return;
+          tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < kDim / 16; ++c) {
+            const uint32_t at = O + (uint32_t)(c & 1) * (16u << 16) + 32u * (c / 2);
+            const float f0 = c & 1 ? f[2] : f[0], f1 = c & 1 ? f[3] : f[1];
+            uint32_t o[16];
+            tmem_ld_rows(at, o);
+            tmem_wait_rows(o);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * (j & 2 ? f1 : f0));
+            tmem_st_rows(at, o);
+          }
+        }
+        if (!again) break;
       }
     }
-    float top1 = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < kTokens / 2; j += 2) {
-      top = fmaxf(top, fmaxf(x[j].x, x[j].y));
-      top1 = fmaxf(top1, fmaxf(x[j + 1].x, x[j + 1].y));
-    }
-    top = fmaxf(top, top1);
-    // (m = -infinity: any number exceeds it)
-    if (__any_sync(0xffffffffu, top > m + kRaise || e_now > e)) {
-      const float above = top > m + kRaise ? top : m;
-      const float f = above == -INFINITY ? 1.0f : exp2_fast(m - above), down = f * power_of_two(e - e_now);
-      m = above;
-      e = e_now;
-      l *= f;
-      if (i > 0) {                                         // (S of this tile came behind P V of the last one: O is there)
-#pragma unroll
-        for (int c = 0; c < kDim / 16; ++c) {
-          int32_t o[16];
-          uint32_t scaled[16];
-          tmem_ld16(O + 16u * c, o);
-          tmem_wait16(o);
-#pragma unroll
-          for (int j = 0; j < 16; ++j) scaled[j] = __float_as_uint(__int_as_float(o[j]) * down);
-          tmem_st16(O + 16u * c, scaled);
-        }
-      }
-    }
-    const float base = m == -INFINITY ? 0.0f : -m;
-    const float2 base2 = make_float2(base, base);
-    float2 sum = make_float2(0.0f, 0.0f), sum1 = sum;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      uint32_t p[16];
-#pragma unroll
-      for (int j = 0; j < 16; j += 2) {
-        const float4 f = lds_float4(vs + 16u * (uint32_t)(8 * c + j / 2));
-        float2 u = add2(x[16 * c + j], base2), v = add2(x[16 * c + j + 1], base2);
-        u = make_float2(exp2_fast(u.x), exp2_fast(u.y));
-        v = make_float2(exp2_fast(v.x), exp2_fast(v.y));
-        sum = add2(sum, u);
-        sum1 = add2(sum1, v);
-        u = mul2(u, make_float2(f.x, f.y));
-        v = mul2(v, make_float2(f.z, f.w));
-        if (!whole) {                                      // (a token that is not seen may stand for anything)
-          if (x[16 * c + j].x == -INFINITY) u.x = 0.0f;
-          if (x[16 * c + j].y == -INFINITY) u.y = 0.0f;
-          if (x[16 * c + j + 1].x == -INFINITY) v.x = 0.0f;
-          if (x[16 * c + j + 1].y == -INFINITY) v.y = 0.0f;
-        }
-        p[j] = float_to_pair(u.x, u.y, __half());
-        p[j + 1] = float_to_pair(v.x, v.y, __half());
-      }
-      tmem_st16(S + 16u * c, p);
-    }
-    l += (sum.x + sum.y) + (sum1.x + sum1.y);
+    for (int j = 0; j < 4; ++j) l[j] += sum[j];
+    tmem_st_weights(here, p[0]);
+    tmem_st_weights(here + (16u << 16), p[1]);
     tmem_wait_st();
     tc_fence_before();
     __syncwarp();
-    if (lane == 0) mbar_arrive(B.smem + L::kPFull + 8u * half);
+    if (lane == 0) mbar_arrive(B.smem + L::kPFull + 16u * half + 8u * sub);
   }
-  // ---- the row's output, or its sums for the kernel that joins them
+  // ---- a row a thread: its output, or its sums for the kernel that joins them
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int x = 1; x < 4; x *= 2) l[j] += __shfl_xor_sync(0xffffffffu, l[j], x);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) m[j] = unset >> j & 1 ? -INFINITY : m[j];
+  const float m_row = of_row(m, lane), l_row = of_row(l, lane);
   if (n > 0) {
-    if (!wait_inline(B, B.smem + L::kSFull + 8u * half, (uint32_t)n & 1u)) return;
+    if (!wait_inline(B, B.smem + L::kLast + 8u * half, 0u)) return;
     tc_fence_after();
   }
   const bool blind = limit < 0 || n == 0;
-  const float back = power_of_two(e - 12), inv = B.direct ? back / l : back;
-  T *out = static_cast<T *>(P.A.out) + row * P.A.r.out_stride + (long long)head * kDim;
+  const float back = power_of_two(e - kLift), inv = B.direct ? back / l_row : back;
   float *partial = B.partial + (size_t)(half * kHalf + in_tile) * kDim, *stats = B.partial + (size_t)kItemRows * kDim + 2 * (half * kHalf + in_tile);
+  int32_t o[kDim / 16][16];
+  if (n > 0) {
 #pragma unroll
-  for (int c = 0; c < kDim / 32; ++c) {
-    uint32_t o[32];
-    if (n > 0) {
-      tmem_ld32(O + 32u * c, o);
-      tmem_wait32(o);
+    for (int c = 0; c < kDim / 16; ++c) tmem_ld16(O + 16u * c, o[c]);
+#pragma unroll
+    for (int c = 0; c < kDim / 16; ++c) tmem_wait16(o[c]);
+  }
+  const bool zero = n == 0 || (B.direct && blind);
+  if (B.direct) {
+    // by way of where the queries were (all products are done), so that lanes write neighbouring pieces of a row
+    const uint32_t at = B.q + (uint32_t)half * L::kOperand;
+#pragma unroll
+    for (int c = 0; c < kDim / 8; ++c) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = zero ? 0.0f : __int_as_float(o[c / 2][8 * (c & 1) + j]) * inv;
+      Chunk<T> w;
+      w.from_float(v);
+      sts128(at + (uint32_t)(c / 8) * (kTokens * 128) + (uint32_t)(in_tile * 128 + ((c & 7) ^ (in_tile & 7)) * 16), w.w[0], w.w[1], w.w[2], w.w[3]);
     }
-    if (!in) continue;
+    __syncwarp();
+    constexpr int kLanes = kDim / 8, kRows = 32 / kLanes;
+    const long long to = in ? row * P.A.r.out_stride + (long long)head * kDim : -1;
+    const int c = lane % kLanes;
 #pragma unroll
-    for (int j = 0; j < 32; ++j) o[j] = n > 0 && !(B.direct && blind) ? __float_as_uint(__uint_as_float(o[j]) * inv) : 0u;
-    if (B.direct) {
+    for (int j = 0; j < 32 / kRows; ++j) {
+      const int r = j * kRows + lane / kLanes;
+      const long long place = __shfl_sync(0xffffffffu, to, r);
+      Chunk<T> w;
+      lds128(at + (uint32_t)(c / 8) * (kTokens * 128) + (uint32_t)((32 * quarter + r) * 128 + ((c & 7) ^ (r & 7)) * 16), w.w);
+      if (place >= 0) w.store(static_cast<T *>(P.A.out) + place + 8 * c, P.out_pieces, 8);
+    }
+  } else if (in) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        Chunk<T> v;
-        v.from_float(*reinterpret_cast<const float (*)[8]>(o + 8 * j));
-        v.store(out + 32 * c + 8 * j, P.out_pieces, 8);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        reinterpret_cast<uint4 *>(partial + 32 * c)[j] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+    for (int c = 0; c < kDim / 4; ++c) {
+      float4 v;
+      v.x = zero ? 0.0f : __int_as_float(o[c / 4][4 * (c & 3)]) * inv;
+      v.y = zero ? 0.0f : __int_as_float(o[c / 4][4 * (c & 3) + 1]) * inv;
+      v.z = zero ? 0.0f : __int_as_float(o[c / 4][4 * (c & 3) + 2]) * inv;
+      v.w = zero ? 0.0f : __int_as_float(o[c / 4][4 * (c & 3) + 3]) * inv;
+      reinterpret_cast<float4 *>(partial)[c] = v;
     }
   }
   if (!in) return;
   if (B.direct) {
-    if (P.A.lse) P.A.lse[row * P.A.r.q_heads + head] = blind ? -INFINITY : (m + log2f(l)) * kLn2;
+    if (P.A.lse) P.A.lse[row * P.A.r.q_heads + head] = blind ? -INFINITY : (m_row + log2f(l_row)) * kLn2;
   } else {
-    stats[0] = m;
-    stats[1] = l;
+    stats[0] = m_row;
+    stats[1] = l_row;
   }
 }
 
@@ -622,10 +750,11 @@ kv4_prompt_kernel(const __grid_constant__ Params P) {
   int *found = reinterpret_cast<int *>(smem_ptr + L::kItem);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(smem_ptr + L::kAbort);
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kRawStages; ++i) { mbar_init(smem + L::kRawFull + 8u * i, 1); mbar_init(smem + L::kRawEmpty + 8u * i, 4); }
+    for (int i = 0; i < kRawStages; ++i) { mbar_init(smem + L::kRawFull + 8u * i, 1); mbar_init(smem + L::kRawEmpty + 8u * i, 8); }
     for (int i = 0; i < kOperands; ++i) { mbar_init(smem + L::kFull + 8u * i, 4); mbar_init(smem + L::kEmpty + 8u * i, 1); }
     for (int i = 0; i < kScaleBufs; ++i) mbar_init(smem + L::kScaled + 8u * i, 4);
-    for (int i = 0; i < 2; ++i) { mbar_init(smem + L::kSFull + 8u * i, 1); mbar_init(smem + L::kPFull + 8u * i, 4); mbar_init(smem + L::kQFull + 8u * i, 4); }
+    for (int i = 0; i < 4; ++i) { mbar_init(smem + L::kSFull + 8u * i, 1); mbar_init(smem + L::kPFull + 8u * i, 4); }
+    for (int i = 0; i < 2; ++i) { mbar_init(smem + L::kODone + 8u * i, 1); mbar_init(smem + L::kLast + 8u * i, 1); mbar_init(smem + L::kQFull + 8u * i, 4); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -639,21 +768,28 @@ kv4_prompt_kernel(const __grid_constant__ Params P) {
   const int split = (int)(blockIdx.x % (unsigned)P.splits), at = (int)(blockIdx.x / (unsigned)P.splits);
   if (warp == kCopyWarp) {
     const Item item = item_of(P, at / P.A.w.d.kv_heads, lane);
-    if (lane == 0) { found[0] = item.b; found[1] = item.tile; found[2] = item.there; }
+    Sequence s = {};
+    if (item.there) s.load(P.A.w, P.T, item.b);
+    if (lane == 0) {
+      found[0] = item.b; found[1] = item.tile; found[2] = item.there;
+      found[3] = s.start; found[4] = s.n; found[5] = s.len; found[6] = s.lead;
+      if (*tmem_slot != 0u) *abort_flag = 1;               // (all of it was taken: its addresses begin at 0)
+    }
   } else if (warp == kMmaWarp) {
     P.T.check_lengths(P.A.w, lane, &g_status_kv4_prompt);
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  Block B = {P, {}, found[0], at % P.A.w.d.kv_heads, found[1], 0, 0, false, false, smem, 0u, 0u, *tmem_slot, smem_ptr, abort_flag, nullptr};
+  Block B = {P, {}, found[0], at % P.A.w.d.kv_heads, found[1], 0, 0, 0, false, false, smem, 0u, 0u, smem_ptr, abort_flag, nullptr};
   bool work = found[2] != 0;
   if (work) {
-    B.s.load(P.A.w, P.T, B.b);
+    B.s.start = found[3]; B.s.n = found[4]; B.s.len = found[5]; B.s.lead = found[6];
     const Span span(P, B.s, B.tile, split);
     work = split < span.splits;
     B.first = span.first;
     B.last = span.last;
+    B.steps = span.steps;
     B.two = (long long)B.s.n * P.T.group - (long long)B.tile * kItemRows > kHalf;
     B.direct = span.splits == 1;
     B.q = (smem + L::kQ + 1023u) & ~1023u;
@@ -661,16 +797,18 @@ kv4_prompt_kernel(const __grid_constant__ Params P) {
     B.partial = static_cast<float *>(P.A.work) + (size_t)blockIdx.x * partial_floats(kDim);
   }
   if (work) {
-    if (warp < kExpandWarp) {
+    if (warp < kKeyWarp) {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
       softmax_role<T, kDim>(B, warp >> 2, warp & 3, lane);
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
       if (B.first < B.last) {
-        if (warp < kMmaWarp) {
-          expand_role<T, kDim>(B, (int)threadIdx.x - 32 * kExpandWarp);
+        if (warp < kValueWarp) {
+          key_role<T, kDim>(B, (int)threadIdx.x - 32 * kKeyWarp);
+        } else if (warp < kMmaWarp) {
+          value_role<kDim>(B, (int)threadIdx.x - 32 * kValueWarp);
         } else if (warp == kMmaWarp) {
-          if (elect_one()) mma_role<T, kDim>(B);
+          mma_role<T, kDim>(B);
         } else if (warp == kCopyWarp) {
           copy_role<kDim>(B, lane);
         }
@@ -681,7 +819,7 @@ kv4_prompt_kernel(const __grid_constant__ Params P) {
   tc_fence_before();
   __syncthreads();
   if (warp == kMmaWarp)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(B.tmem), "r"(512u) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(*tmem_slot), "r"(512u) : "memory");
 }
 
 // Joins the sums of an item's blocks: a warp has a row (token and head).

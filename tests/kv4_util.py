@@ -178,8 +178,8 @@ def attention64(batch, q, scale):
 
     Off by: a logit's products are exact and added one by one (2 U each, cut off), then scaled (4 U), of sums of magnitudes; the exponent's argument, up
     to its size x, 4 U x, and exp2 itself 2^-21; so a weight's relative error e, twice (its sum's too), with the sum's chain of up to L/64 + 64 additions.
-    A weight times the value's scale is rounded to F16's 11 bits, off by half a step, torch.finfo(torch.float16).eps / 2 = 2^-11, or to a fixed step of 2^-37 of the largest scale (F16's subnormals after the
-    product with 2^12), times codes up to 15.  O's additions like the logits', 2 U each."""
+    A weight times the value's scale is rounded to F16's 11 bits, off by half a step, torch.finfo(torch.float16).eps / 2 = 2^-11, or by 2^-32 of the largest scale (half a step of
+    F16's subnormals, 2^-25, after the product with 2^7), times codes up to 15.  O's additions like the logits', 2 U each."""
     T, Hq, D = q.shape
     G = Hq // batch.heads
     out, lse = torch.zeros(T, Hq, D, dtype=torch.float64, device="cuda"), torch.full((T, Hq), math.nan, dtype=torch.float64, device="cuda")
@@ -214,7 +214,7 @@ def attention64(batch, q, scale):
         lse[rows] = torch.where(has[:, None, None], x, -math.inf).flatten(1, 2)
         lse_off[rows] = (e + 4 * U * x.abs().nan_to_num(0, 0, 0)).flatten(1, 2)
         out[rows] = torch.where(has[:, None, None, None], o, 0.0).flatten(1, 2)
-        step = 2.0 ** -37 * 2 * 15 * top[None, :, None] * length
+        step = 2.0 ** -32 * 2 * 15 * top[None, :, None] * length
         off[rows] = (sz * (e[..., None] + 2.0 ** -11 + (length / 16 + 64) * 2 * U) + step[..., None]).flatten(1, 2)
     t = q.dtype
     off += half_step(t) * (out.abs() + off) + least(t)
