@@ -671,7 +671,7 @@ xnor_status xnor_kv4_read(const void *cache, const int32_t *starts, const int32_
  * the sums depends on the sizes, all sequences' lengths and the device's number of SMs: the same call gives the same bits.
  * Device-side waits are bounded (xnor_check_device).  What lies outside the table or the cache is not seen.
  * INVALID_ARG as above, and: q_heads no multiple of kv_heads, scale not finite, most < 0, out in the place of q.
- * UNSUPPORTED as above, and: F32.
+ * UNSUPPORTED as above, and: F32, rows q_heads > 2^30.
  */
 typedef struct {
   int rows, q_heads, type, most;

@@ -503,7 +503,7 @@ xnor_status check_kv4(const xnor_kv4_desc *d, const void *cache, const int32_t *
 bool bad_kv4_rows(const xnor_kv4_desc *d, const xnor_kv4_rows *r) {
   return !r || r->rows < 0 || r->q_heads < 1 || r->q_heads % d->kv_heads || !real_type(r->type) || r->most < 0;
 }
-bool large_kv4_rows(const xnor_kv4_rows *r) { return r->type == XNOR_F32 || r->rows > (1 << 24) || r->q_heads > 65535; }
+bool large_kv4_rows(const xnor_kv4_rows *r) { return r->type == XNOR_F32 || r->rows > (1 << 24) || r->q_heads > 65535 || (long long)r->rows * r->q_heads > (1ll << 30); }
 
 }  // namespace
 

@@ -201,8 +201,7 @@ struct TileRow {
   int limit;                   // the last token that it sees; below 0: none
   bool in;
   __device__ __forceinline__ TileRow(const Params &P, const Place &p, int rows, int i, int dim) {
-    const long long r = (long long)p.tile * rows + i;
-    const int token = (int)(r / P.T.group), head = p.head * P.T.group + (int)(r - (long long)token * P.T.group);
+    const int r = p.tile * rows + i, token = r / P.T.group, head = p.head * P.T.group + r % P.T.group;
     in = token < p.s.n;
     q = (p.s.start + token) * P.A.r.q_stride + (long long)head * dim;
     out = (p.s.start + token) * P.A.r.out_stride + (long long)head * dim;

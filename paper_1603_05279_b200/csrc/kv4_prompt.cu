@@ -42,7 +42,7 @@ struct Layout {
   static constexpr uint32_t kRaw = kRecords * kv4_record(kDim);
   static constexpr uint32_t kRawFull = 0, kRawEmpty = kRawFull + 8 * kRawStages, kFull = kRawEmpty + 8 * kRawStages, kEmpty = kFull + 8 * kOperands;
   static constexpr uint32_t kSFull = kEmpty + 8 * kOperands, kPFull = kSFull + 32, kODone = kPFull + 32, kLast = kODone + 16, kQFull = kLast + 16;      // [half][S]
-  static constexpr uint32_t kScaled = kQFull + 16, kTmem = kScaled + 8 * kScaleBufs, kAbort = kTmem + 4, kItem = kAbort + 4, kMask = kItem + 32, kExponent = kMask + 4 * kRawStages;
+  static constexpr uint32_t kScaled = kQFull + 16, kTmem = kScaled + 8 * kScaleBufs, kAbort = kTmem + 4, kItem = kAbort + 4, kMask = kItem + 48, kExponent = kMask + 4 * kRawStages;
   static constexpr uint32_t kThere = kExponent + 4 * kScaleBufs;
   static constexpr uint32_t kScales = 512, kRing = kScales + kScaleBufs * 2 * kTokens * 4;
   static constexpr uint32_t kQ = kRing + kRawStages * kRaw;      // (rounded up to 1024 in memory)
@@ -115,14 +115,14 @@ __device__ __forceinline__ int rank_of(const Params &P, int b, int tile, int lan
 // An item's tiles of context, and the share of them that one of its blocks has.
 struct Span {
   int tiles, splits, first, last, steps;
+  Span() = default;
   __device__ __forceinline__ Span(const Params &P, const Sequence &s, int tile, int split) {
-    const long long end_row = min((long long)s.n * P.T.group, (long long)(tile + 1) * kItemRows);
-    const int last_token = (int)((end_row - 1) / P.T.group);
+    const int last_token = (min(s.n * P.T.group, (tile + 1) * kItemRows) - 1) / P.T.group;
     const int seen = min(s.len, max(0, s.lead + s.start + last_token + 1));            // tokens that any of its rows sees
     tiles = (seen + kTokens - 1) / kTokens;
     splits = min(P.splits, max(1, tiles / 4));
-    first = (int)((long long)tiles * split / splits);
-    last = (int)((long long)tiles * (split + 1) / splits);
+    first = tiles / splits * split + min(split, tiles % splits);
+    last = first + tiles / splits + (split < tiles % splits ? 1 : 0);
     steps = (min(last * kTokens, seen) - first * kTokens + kStep - 1) / kStep;
   }
 };
@@ -542,8 +542,7 @@ __device__ __forceinline__ void softmax_role(const Block &B, int half, int quart
   const Params &P = B.P;
   const int in_tile = 32 * quarter + lane, g = lane >> 2, t = lane & 3;
   if (half == 1 && !B.two) return;
-  const long long r = (long long)B.tile * kItemRows + half * kHalf + in_tile;
-  const int token = (int)(r / P.T.group), head = B.head * P.T.group + (int)(r - (long long)token * P.T.group);
+  const int r = B.tile * kItemRows + half * kHalf + in_tile, token = r / P.T.group, head = B.head * P.T.group + r % P.T.group;
   const bool in = token < B.s.n;
   const long long row = B.s.start + token;
   const int limit = in ? min(B.s.lead + B.s.start + token, B.s.len - 1) : INT_MAX;        // the last token that the row of this lane sees
@@ -768,12 +767,18 @@ kv4_prompt_kernel(const __grid_constant__ Params P) {
   const int split = (int)(blockIdx.x % (unsigned)P.splits), at = (int)(blockIdx.x / (unsigned)P.splits);
   if (warp == kCopyWarp) {
     const Item item = item_of(P, at / P.A.w.d.kv_heads, lane);
-    Sequence s = {};
-    if (item.there) s.load(P.A.w, P.T, item.b);
     if (lane == 0) {
-      found[0] = item.b; found[1] = item.tile; found[2] = item.there;
+      Sequence s = {};
+      Span span = {};
+      if (item.there) {
+        s.load(P.A.w, P.T, item.b);
+        span = Span(P, s, item.tile, split);
+      }
+      found[0] = item.b; found[1] = item.tile; found[2] = item.there && split < span.splits && *tmem_slot == 0u;      // (all of it was taken: its addresses begin at 0)
       found[3] = s.start; found[4] = s.n; found[5] = s.len; found[6] = s.lead;
-      if (*tmem_slot != 0u) *abort_flag = 1;               // (all of it was taken: its addresses begin at 0)
+      found[7] = span.first; found[8] = span.last; found[9] = span.steps;
+      found[10] = s.n * P.T.group - item.tile * kItemRows > kHalf;
+      found[11] = span.splits == 1;
     }
   } else if (warp == kMmaWarp) {
     P.T.check_lengths(P.A.w, lane, &g_status_kv4_prompt);
@@ -782,20 +787,14 @@ kv4_prompt_kernel(const __grid_constant__ Params P) {
   __syncthreads();
   tc_fence_after();
   Block B = {P, {}, found[0], at % P.A.w.d.kv_heads, found[1], 0, 0, 0, false, false, smem, 0u, 0u, smem_ptr, abort_flag, nullptr};
-  bool work = found[2] != 0;
-  if (work) {
-    B.s.start = found[3]; B.s.n = found[4]; B.s.len = found[5]; B.s.lead = found[6];
-    const Span span(P, B.s, B.tile, split);
-    work = split < span.splits;
-    B.first = span.first;
-    B.last = span.last;
-    B.steps = span.steps;
-    B.two = (long long)B.s.n * P.T.group - (long long)B.tile * kItemRows > kHalf;
-    B.direct = span.splits == 1;
-    B.q = (smem + L::kQ + 1023u) & ~1023u;
-    B.operands = B.q + 2u * L::kOperand;
-    B.partial = static_cast<float *>(P.A.work) + (size_t)blockIdx.x * partial_floats(kDim);
-  }
+  const bool work = found[2] != 0;
+  B.s.start = found[3]; B.s.n = found[4]; B.s.len = found[5]; B.s.lead = found[6];
+  B.first = found[7]; B.last = found[8]; B.steps = found[9];
+  B.two = found[10] != 0;
+  B.direct = found[11] != 0;
+  B.q = (smem + L::kQ + 1023u) & ~1023u;
+  B.operands = B.q + 2u * L::kOperand;
+  B.partial = static_cast<float *>(P.A.work) + (size_t)blockIdx.x * partial_floats(kDim);
   if (work) {
     if (warp < kKeyWarp) {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));

@@ -105,6 +105,7 @@ def test_cache():
     for kw in (dict(q=NULL), dict(q=ODD), dict(c=NULL), dict(s=NULL), dict(l=ODD), dict(t=NULL), dict(o=NULL), dict(o=P), dict(ls=ODD), dict(w=NULL)):
         assert m(kv4(), rows(), **kw) == INV, kw
     assert m(kv4(), rows(type=B.XNOR_F32)) == UNS and m(kv4(), rows(rows=(1 << 24) + 1)) == UNS
+    assert m(kv4(), rows(rows=1 << 20, q_heads=2048, q_stride=1 << 17, out_stride=1 << 17)) == UNS
     assert m(kv4(), rows(rows=0), q=NULL, o=NULL, w=NULL) == OK
 
 
