@@ -9,10 +9,11 @@
 // within the warp (movmatrix) makes the second operand.  The softmax is one pass: a running maximum, raised (and
 // the sums rescaled) only when it is exceeded by more than 2^8, and sums in fp32.
 //
-// A block: one warp copies records into a ring in shared memory, a thread a stage, and eight or four warps take every
-// so-many-th unit each; at an item's end (the units of a tile) they add their sums.  An item that lies in
+// A block: one warp copies records into a ring in shared memory, a thread a stage, and seven warps take every
+// seventh unit each; at an item's end (the units of a tile) they add their sums.  An item that lies in
 // several blocks' shares leaves partial sums in the workspace, which a second kernel joins.
 #include <algorithm>
+#include <type_traits>
 
 #include "kv4_attention.cuh"
 
@@ -24,9 +25,10 @@ namespace {
 
 using namespace umma;
 
-constexpr int kWarps = 4, kStages = 16;
-constexpr int kPerSm = 3;
-constexpr int kMaxWorkers = kPerSm * 160;    // blocks, at most (a B200 has 148 SMs)
+// Seven computing warps and one that copies: 256 threads, so that two blocks have 128 registers a thread.
+constexpr int kWarps = 7, kTurns = 4, kStages = kTurns * kWarps;      // kTurns: stages of a warp
+constexpr int per_sm(int tiles) { return tiles == 1 ? 2 : 1; }          // blocks: by their registers
+constexpr int kMaxWorkers = 2 * 160;         // blocks, at most (a B200 has 148 SMs)
 constexpr int kLeastUnits = 2 * kWarps;      // of a block's share
 
 // What the threads of a warp know of the row: each the sum over its own run of sequences, and the sum before them.
@@ -34,6 +36,7 @@ struct Row {
   int per;                     // sequences of a thread
   long long before, total;
   long long workers;
+  Sequence own;                // with one sequence a thread: that
   __device__ __forceinline__ Row(const Kv4Where &W, const Tiling &T, int lane, int most) {
     per = (W.d.seqs + 31) / 32;
     long long mine = 0;
@@ -41,9 +44,8 @@ struct Row {
     for (int i = 0; i < per; ++i) {
       const int b = lane * per + i;
       if (b >= W.d.seqs) break;
-      Sequence s;
-      s.load(W, T, b);
-      mine += s.all(W.d.kv_heads);
+      own.load(W, T, b);
+      mine += own.all(W.d.kv_heads);
     }
     long long sum = mine;
 #pragma unroll
@@ -60,7 +62,7 @@ struct Row {
   // The sum before sequence b; the same for all threads.
   __device__ __forceinline__ long long before_sequence(const Kv4Where &W, const Tiling &T, int b, int lane) const {
     long long v = before;
-    if (lane == b / per)
+    if (per > 1 && lane == b / per)
       for (int i = lane * per; i < b; ++i) {
         Sequence s;
         s.load(W, T, i);
@@ -69,12 +71,13 @@ struct Row {
     return __shfl_sync(0xffffffffu, v, b / per);
   }
   // The sequence of a unit (below total), and the sum before it.
-  __device__ __forceinline__ int sequence_of(const Kv4Where &W, const Tiling &T, long long unit, int lane, long long &sum) const {
+  __device__ __forceinline__ int sequence_of(const Kv4Where &W, const Tiling &T, long long unit, int lane, long long &sum, Sequence &found) const {
     const uint32_t later = __ballot_sync(0xffffffffu, before > unit);
     const int owner = later == 0 ? 31 : __ffs((int)later) - 2;       // the last thread whose sum before it is no more
-    int b = 0;
+    int b = lane;
     long long v = before;
-    if (lane == owner) {
+    found = own;
+    if (per > 1 && lane == owner) {
       for (b = lane * per; b + 1 < W.d.seqs; ++b) {
         Sequence s;
         s.load(W, T, b);
@@ -84,7 +87,18 @@ struct Row {
       }
     }
     sum = __shfl_sync(0xffffffffu, v, owner);
-    return __shfl_sync(0xffffffffu, b, owner);
+    b = __shfl_sync(0xffffffffu, b, owner);
+    if (per > 1) {
+      found.load(W, T, b);
+    } else {
+      found.start = __shfl_sync(0xffffffffu, found.start, owner);
+      found.n = __shfl_sync(0xffffffffu, found.n, owner);
+      found.len = __shfl_sync(0xffffffffu, found.len, owner);
+      found.lead = __shfl_sync(0xffffffffu, found.lead, owner);
+      found.tiles = __shfl_sync(0xffffffffu, found.tiles, owner);
+      found.units = __shfl_sync(0xffffffffu, found.units, owner);
+    }
+    return b;
   }
 };
 
@@ -107,7 +121,7 @@ struct Layout {
   static constexpr int kRows = 8 * kTiles;
   static constexpr int kSumRow = kDim + 4;                          // floats
   static constexpr uint32_t kFull = 0, kEmpty = 8 * kStages, kValid = 16 * kStages, kAbort = kValid + 4 * kStages;
-  static constexpr uint32_t kStats = 512;                           // [kWarps][kRows] maxima and sums
+  static constexpr uint32_t kStats = 1024;                          // [kWarps][kRows] maxima and sums
   static constexpr uint32_t kSums = kStats + 8 * kWarps * kRows;    // [kWarps][kRows][kSumRow]
   static constexpr uint32_t kRing = (kSums + 4u * kWarps * kRows * kSumRow + 127u) & ~127u;
   static constexpr uint32_t kBytes = kRing + kStages * kRecord;
@@ -145,13 +159,12 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile
 // ---- the copying warp --------------------------------------------------------------------------------------------
 // Thread i fills stage i, of every kStages-th unit of the share.  It finds the next unit's record before it waits for the stage.
 template <class L>
-__device__ __forceinline__ void copy_role(const Params &P, const Row &row, long long u0, long long u1, int b0, long long sum0, uint32_t smem,
+__device__ __forceinline__ void copy_role(const Params &P, long long u0, long long u1, int b0, const Sequence &s0, long long sum0, uint32_t smem,
                                           volatile int *abort_flag, int lane) {
   const Kv4Where &W = P.A.w;
-  if (lane >= kStages) return;
   Place p;
   p.b = b0;
-  p.s.load(W, P.T, b0);
+  p.s = s0;
   long long sum = sum0;
   struct Next { long long record; int valid; };
   auto find = [&](long long u) {
@@ -167,27 +180,40 @@ __device__ __forceinline__ void copy_role(const Params &P, const Row &row, long 
     return n;
   };
   const uint32_t full = smem + L::kFull + 8u * lane, empty = smem + L::kEmpty + 8u * lane;
-  Next next = find(u0 + lane);
+  const bool mine = lane < kStages;
+  Next next = find(mine ? u0 + lane : u1);
   uint32_t parity = 1u;
-  bool in_flight = false;
-  for (long long u = u0 + lane; u < u1; u += kStages, parity ^= 1u) {
+  bool in_flight = false, alive = true;
+#pragma unroll 1
+  for (long long u = u0; alive && u < u1; u += kStages, parity ^= 1u) {
     const Next now = next;
-    next = find(u + kStages);
-    if (!wait_for(empty, parity, abort_flag)) {
-      // gave up: the copy in flight must land before the block's shared memory is released
-      for (int i = 0; in_flight && i < (1 << 12) && !mbar_try(full, parity); ++i) {}
-      return;
+    next = find(mine ? u + lane + kStages : u1);
+    // a stage of each warp at a time: the others' units stay under way meanwhile (all at once the ring ran empty: 107 us for
+    // 64 sequences of up to 8192 tokens)
+#pragma unroll 1
+    for (int turn = 0; alive && turn < kTurns; ++turn) {
+      if (lane / kWarps == turn && mine && u + lane < u1) {
+        alive = wait_for(empty, parity, abort_flag);
+        if (alive) {
+          const bool there = now.record >= 0;
+          if (!there && now.valid > 0) atomicMax(&g_status_kv4_few, (int)XNOR_ERR_BOUNDS);
+          asm volatile("st.shared.b32 [%0], %1;" ::"r"(smem + L::kValid + 4u * lane), "r"(there ? now.valid : 0) : "memory");
+          if (there) {
+            mbar_arrive_expect_tx(full, L::kRecord);
+            bulk_copy_g2s(smem + L::kRing + (uint32_t)lane * L::kRecord, P.A.cache + (size_t)now.record * L::kRecord, L::kRecord, full);
+          } else {
+            mbar_arrive(full);
+          }
+          in_flight = there;
+        }
+      }
+      alive = __all_sync(0xffffffffu, alive);
     }
-    const bool there = now.record >= 0;
-    if (!there && now.valid > 0) atomicMax(&g_status_kv4_few, (int)XNOR_ERR_BOUNDS);
-    asm volatile("st.shared.b32 [%0], %1;" ::"r"(smem + L::kValid + 4u * lane), "r"(there ? now.valid : 0) : "memory");
-    if (there) {
-      mbar_arrive_expect_tx(full, L::kRecord);
-      bulk_copy_g2s(smem + L::kRing + (uint32_t)lane * L::kRecord, P.A.cache + (size_t)now.record * L::kRecord, L::kRecord, full);
-    } else {
-      mbar_arrive(full);
-    }
-    in_flight = there;
+  }
+  // gave up: the copies in flight must land before the block's shared memory is released
+  if (!alive && in_flight) {
+    const long long t0 = clock64();
+    while (clock64() - t0 < (1 << 20)) {}
   }
 }
 
@@ -229,7 +255,7 @@ __device__ __forceinline__ void store_row(T *row, const float (&acc)[kDim / 32],
 __host__ __device__ constexpr size_t slot_floats(int rows, int dim) { return (size_t)rows * (dim + 2); }
 
 template <class T, int kDim, int kTiles>
-__device__ __forceinline__ void compute_role(const Params &P, const Row &row, int worker, long long u0, long long u1, int b0, long long sum0,
+__device__ __forceinline__ void compute_role(const Params &P, int worker, long long u0, long long u1, int b0, const Sequence &s0, long long sum0,
                                              uint32_t smem, uint8_t *smem_ptr, volatile int *abort_flag, int warp, int lane) {
   using L = Layout<kDim, kTiles>;
   constexpr int kRows = L::kRows, kWords = kDim / 32, kVWords = kDim / 64, kMTiles = kDim / 16;      // of a thread: key words, value words of a token; tiles of O^T
@@ -240,9 +266,11 @@ __device__ __forceinline__ void compute_role(const Params &P, const Row &row, in
   const int tok0 = token_of(g), tok1 = token_of(g + 8);                    // this thread's rows of S^T
   Place p;
   p.b = b0;
-  p.s.load(W, P.T, b0);
+  p.s = s0;
   long long u = u0, sum = sum0;
   bool alive = true;
+  uint32_t use = 0u;                                                       // units that this warp has had: unit warp + kWarps use of the share is next
+  const uint32_t turned = t & 1 ? 0x1054u : 0x5410u;                       // (tokens 2 t and 2 t + 1 are the other way round there)
   while (u < u1) {
     while (u >= sum + p.s.all(W.d.kv_heads)) {
       sum += p.s.all(W.d.kv_heads);
@@ -272,37 +300,35 @@ __device__ __forceinline__ void compute_role(const Params &P, const Row &row, in
       }
     }
     least = __reduce_min_sync(0xffffffffu, least);
+    // sums, a row's maximum so far, 0 where nothing was seen (`settled`: all of the warp's rows have one), and the sum of its weights
     float o[kTiles][kMTiles][4], m[kTiles][2], l[kTiles][2];
+    uint32_t unset = (1u << (2 * kTiles)) - 1u;
+    bool settled = false;
     int e = kLeastScale;                                                   // 2^e: the values' scales are below it
+    float largest = 0.0f, lift = 0.0f;                                     // 2^e, 2^(kLift - e); 0: not known
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) { m[n][i] = -INFINITY; l[n][i] = 0.0f; }
+      for (int i = 0; i < 2; ++i) m[n][i] = l[n][i] = 0.0f;
 #pragma unroll
       for (int j = 0; j < kMTiles; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[n][j][i] = 0.0f;
     }
     // every kWarps-th unit of the share is this warp's
-    const int skip = (int)((warp - (u - u0)) & (kWarps - 1));
+    const int skip = (int)((warp + kWarps - (u - u0) % kWarps) % kWarps);
 #pragma unroll 1
-    for (int rec = p.rec + skip; alive && rec < rec_end; rec += kWarps) {
-      const long long i = item0 + rec - u0;                                // the unit's number in the share
-      const uint32_t stage = (uint32_t)(i % kStages), base = smem + L::kRing + stage * L::kRecord;
-      alive = __all_sync(0xffffffffu, wait_for(smem + L::kFull + 8u * stage, (uint32_t)(i / kStages) & 1u, abort_flag));
+    for (int rec = p.rec + skip; alive && rec < rec_end; rec += kWarps, ++use) {
+      const uint32_t stage = (uint32_t)warp + kWarps * (use % kTurns), base = smem + L::kRing + stage * L::kRecord;
+      alive = __all_sync(0xffffffffu, wait_for(smem + L::kFull + 8u * stage, (use / kTurns) & 1u, abort_flag));
       if (!alive) break;
+      // all of the record that this thread needs
       const int valid = (int)lds32(smem + L::kValid + 4u * stage);
-      // ---- S^T
-      float s[kTiles][4];
-#pragma unroll
-      for (int n = 0; n < kTiles; ++n)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s[n][j] = 0.0f;
       const uint32_t kw0 = lds32(base + kv4_words(kDim, false) + 4u * tok0), kw1 = lds32(base + kv4_words(kDim, false) + 4u * tok1);
+      const uint32_t vw0 = lds32(base + kv4_words(kDim, true) + 4u * tok0), vw1 = lds32(base + kv4_words(kDim, true) + 4u * tok1);
+      uint32_t c0[kWords], c1[kWords], c[2][2][kVWords], zeros[2];
       {
-        const typename W4Type<T>::Zero z0 = W4Type<T>::zero(kw0 & 15u), z1 = W4Type<T>::zero(kw1 & 15u);
-        uint32_t c0[kWords], c1[kWords];
-        const uint32_t from = base + (uint32_t)(t * (kDim / 8));
+        const uint32_t from = base + (uint32_t)(t * (kDim / 8)), codes = base + kv4_codes(kDim, true) + (uint32_t)(g * (kDim / 16));
         if constexpr (kWords == 4) {
           lds128(from + tok0 * (kDim / 2), c0);
           lds128(from + tok1 * (kDim / 2), c1);
@@ -310,6 +336,31 @@ __device__ __forceinline__ void compute_role(const Params &P, const Row &row, in
           lds64(from + tok0 * (kDim / 2), c0[0], c0[1]);
           lds64(from + tok1 * (kDim / 2), c1[0], c1[1]);
         }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int ta = token_of(2 * t + 8 * h), tb = token_of(2 * t + 1 + 8 * h);
+          if constexpr (kVWords == 2) {
+            lds64(codes + ta * (kDim / 2), c[h][0][0], c[h][0][1]);
+            lds64(codes + tb * (kDim / 2), c[h][1][0], c[h][1][1]);
+          } else {
+            c[h][0][0] = lds32(codes + ta * (kDim / 2));
+            c[h][1][0] = lds32(codes + tb * (kDim / 2));
+          }
+          uint32_t wa, wb;
+          lds64(base + kv4_words(kDim, true) + 32u * h + 8u * t, wa, wb);
+          zeros[h] = __byte_perm(wa, wb, turned) & 0x000F000Fu;
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem + L::kEmpty + 8u * stage);
+      // ---- S^T
+      float s[kTiles][4];
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[n][j] = 0.0f;
+      {
+        const typename W4Type<T>::Zero z0 = W4Type<T>::zero(kw0 & 15u), z1 = W4Type<T>::zero(kw1 & 15u);
 #pragma unroll
         for (int w = 0; w < kWords; ++w) {
           uint32_t e0[4], e1[4];
@@ -325,99 +376,106 @@ __device__ __forceinline__ void compute_role(const Params &P, const Row &row, in
       }
       // ---- the softmax: s[n][0], [1]: token tok0 for rows 2 t, 2 t + 1; [2], [3]: token tok1
       const float ks0 = kv4_scale(kw0) * scale2, ks1 = kv4_scale(kw1) * scale2;
+      float vs0 = kv4_scale(vw0), vs1 = kv4_scale(vw1), over = -INFINITY, x[kTiles][4];
       const int p0 = rec * kKvTokens;
-      const bool whole = valid == kKvTokens && p0 + kKvTokens - 1 <= least;
-      bool raise = false;
+      const bool masked = valid < kKvTokens || p0 + kKvTokens - 1 > least;
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[n][j] *= j < 2 ? ks0 : ks1;
+      if (masked) {
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int tok = j < 2 ? tok0 : tok1;
+            if (tok >= valid || p0 + tok > limit[n][j & 1]) s[n][j] = -INFINITY;
+          }
+      }
 #pragma unroll
       for (int n = 0; n < kTiles; ++n)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int tok = j < 2 ? tok0 : tok1;
-          s[n][j] *= j < 2 ? ks0 : ks1;
-          if (!whole && (tok >= valid || p0 + tok > limit[n][j & 1])) s[n][j] = -INFINITY;
-          raise = raise || s[n][j] > m[n][j & 1] + kRaise;
+          x[n][j] = s[n][j] - m[n][j & 1];
+          over = fmaxf(over, x[n][j]);
         }
-      const uint32_t vw0 = lds32(base + kv4_words(kDim, true) + 4u * tok0), vw1 = lds32(base + kv4_words(kDim, true) + 4u * tok1);
-      float vs0 = kv4_scale(vw0), vs1 = kv4_scale(vw1);
-      const int e0 = tok0 < valid ? scale_above(vs0) : kLeastScale, e1 = tok1 < valid ? scale_above(vs1) : kLeastScale;
-      raise = raise || max(e0, e1) > e;
-      if (__any_sync(0xffffffffu, raise)) {
-        const int above = __reduce_max_sync(0xffffffffu, max(e, max(e0, e1)));
+      if (!settled || __any_sync(0xffffffffu, over > kRaise || fmaxf(vs0, vs1) > largest)) {
+        const int above = __reduce_max_sync(0xffffffffu, max(e, max(tok0 < valid ? scale_above(vs0) : kLeastScale, tok1 < valid ? scale_above(vs1) : kLeastScale)));
         const float down = power_of_two(e - above);
         e = above;
+        largest = power_of_two(e);
+        lift = power_of_two(kLift - e);
 #pragma unroll
         for (int n = 0; n < kTiles; ++n)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            float top = fmaxf(m[n][i], fmaxf(s[n][i], s[n][i + 2]));
+            float top = fmaxf(s[n][i], s[n][i + 2]), f = 1.0f;
 #pragma unroll
-            for (int x = 4; x < 32; x *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-            const float f = top == -INFINITY ? 1.0f : exp2_fast(m[n][i] - top);
-            m[n][i] = top;
+            for (int y = 4; y < 32; y *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
+            const uint32_t bit = 1u << (2 * n + i);
+            if (unset & bit ? top > -INFINITY : top > m[n][i] + kRaise) {
+              f = unset & bit ? 0.0f : exp2_fast(m[n][i] - top);
+              m[n][i] = top;
+              unset &= ~bit;
+            }
             l[n][i] *= f;
 #pragma unroll
             for (int j = 0; j < kMTiles; ++j) {
               o[n][j][i] *= f * down;
               o[n][j][i + 2] *= f * down;
             }
+            x[n][i] = s[n][i] - m[n][i];
+            x[n][i + 2] = s[n][i + 2] - m[n][i];
           }
+        settled = __all_sync(0xffffffffu, unset == 0u);
       }
-      vs0 *= power_of_two(kLift - e);
-      vs1 *= power_of_two(kLift - e);
+      vs0 *= lift;
+      vs1 *= lift;
       uint32_t b[kTiles][2];                                               // P^T: tokens 0 .. 7 and 8 .. 15 of the rows
 #pragma unroll
       for (int n = 0; n < kTiles; ++n) {
-        float x[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float top = m[n][j & 1];
-          x[j] = exp2_fast(s[n][j] - (top == -INFINITY ? 0.0f : top));
-          l[n][j & 1] += x[j];
-          x[j] = s[n][j] == -INFINITY ? 0.0f : x[j] * (j < 2 ? vs0 : vs1); // (a token that is not seen may stand for anything)
+          x[n][j] = exp2_fast(x[n][j]);
+          l[n][j & 1] += x[n][j];
+          x[n][j] *= j < 2 ? vs0 : vs1;
+        }
+        if (masked) {                                                      // (a token that is not seen may stand for anything)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (s[n][j] == -INFINITY) x[n][j] = 0.0f;
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) b[n][h] = transpose8x8(float_to_pair(x[2 * h], x[2 * h + 1], __half()));
+        for (int h = 0; h < 2; ++h) b[n][h] = transpose8x8(float_to_pair(x[n][2 * h], x[n][2 * h + 1], __half()));
       }
       // ---- O^T: thread (g, t) has columns kDim / 8 g .. of tokens 2 t, 2 t + 1 and 8 more
       {
         using V = W4Type<__half>;
-        uint32_t c[2][2][kVWords];
         V::Zero z[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int ta = token_of(2 * t + 8 * h), tb = token_of(2 * t + 1 + 8 * h);
-          const uint32_t codes = base + kv4_codes(kDim, true) + (uint32_t)(g * (kDim / 16)), words = base + kv4_words(kDim, true);
-          const uint32_t zeros = (lds32(words + 4u * ta) & 15u) | (lds32(words + 4u * tb) & 15u) << 16;
-          z[h] = {0x64006400u | zeros, 0xD400D400u | zeros << 4};
-          if constexpr (kVWords == 2) {
-            lds64(codes + ta * (kDim / 2), c[h][0][0], c[h][0][1]);
-            lds64(codes + tb * (kDim / 2), c[h][1][0], c[h][1][1]);
-          } else {
-            c[h][0][0] = lds32(codes + ta * (kDim / 2));
-            c[h][1][0] = lds32(codes + tb * (kDim / 2));
-          }
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem + L::kEmpty + 8u * stage);
+        for (int h = 0; h < 2; ++h) z[h] = {P.magic16 | zeros[h], 0xD400D400u | zeros[h] << 4};
 #pragma unroll
         for (int w = 0; w < kVWords; ++w) {
-          uint32_t x[2][2][4];                                             // [half of the tokens][even, odd columns][pairs]
+          uint32_t v[2][2][4];                                             // [half of the tokens][even, odd columns][pairs]
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            V::expand(__byte_perm(c[h][0][w], c[h][1][w], 0x5410), z[h], P.magic16, x[h][0]);
-            V::expand(__byte_perm(c[h][0][w], c[h][1][w], 0x7632), z[h], P.magic16, x[h][1]);
+            V::expand(__byte_perm(c[h][0][w], c[h][1][w], 0x5410), z[h], P.magic16, v[h][0]);
+            V::expand(__byte_perm(c[h][0][w], c[h][1][w], 0x7632), z[h], P.magic16, v[h][1]);
           }
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const uint32_t a[4] = {x[0][0][k], x[0][1][k], x[1][0][k], x[1][1][k]};
+            const uint32_t a[4] = {v[0][0][k], v[0][1][k], v[1][0][k], v[1][1][k]};
 #pragma unroll
-            for (int n = 0; n < kTiles; ++n) {
-              mma16816(o[n][4 * w + k], a, b[n][0], b[n][1], __half());
-            }
+            for (int n = 0; n < kTiles; ++n) mma16816(o[n][4 * w + k], a, b[n][0], b[n][1], __half());
           }
         }
       }
     }
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (unset >> (2 * n + i) & 1u) m[n][i] = -INFINITY;
     // ---- the warps' sums together
     const float back = power_of_two(e - kLift);
 #pragma unroll
@@ -479,7 +537,7 @@ __device__ __forceinline__ void compute_role(const Params &P, const Row &row, in
 }
 
 template <class T, int kDim, int kTiles>
-__global__ void __launch_bounds__(32 * (kWarps + 1))
+__global__ void __launch_bounds__(32 * (kWarps + 1), per_sm(kTiles))
 kv4_few_kernel(const Params P) {
   using L = Layout<kDim, kTiles>;
   extern __shared__ __align__(128) uint8_t smem_ptr[];
@@ -501,11 +559,18 @@ kv4_few_kernel(const Params P) {
   if (row.total == 0 || (long long)blockIdx.x >= row.workers) return;
   const long long u0 = row.first_of(blockIdx.x), u1 = row.first_of(blockIdx.x + 1);
   long long sum;
-  const int b = row.sequence_of(P.A.w, P.T, u0, lane, sum);
+  Sequence first;
+  const int b = row.sequence_of(P.A.w, P.T, u0, lane, sum, first);
   if (warp == kWarps)
-    copy_role<L>(P, row, u0, u1, b, sum, smem, abort_flag, lane);
+    copy_role<L>(P, u0, u1, b, first, sum, smem, abort_flag, lane);
   else
-    compute_role<T, kDim, kTiles>(P, row, blockIdx.x, u0, u1, b, sum, smem, smem_ptr, abort_flag, warp, lane);
+    compute_role<T, kDim, kTiles>(P, blockIdx.x, u0, u1, b, first, sum, smem, smem_ptr, abort_flag, warp, lane);
+}
+
+__device__ __forceinline__ float4 load_piece(const float4 *p) { return load_global(p); }
+__device__ __forceinline__ float2 load_piece(const float2 *p) {
+  const uint2 v = load_global(reinterpret_cast<const uint2 *>(p));
+  return make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
 }
 
 // Joins the partial sums of items that lie in several blocks' shares: a warp has a row (token and head).
@@ -537,15 +602,27 @@ kv4_join_kernel(const Params P, int rows) {
   for (int w = w0 + lane; w <= w1; w += 32) top = fmaxf(top, load_global(slot(w) + (size_t)rows * kDim + 2 * at));
 #pragma unroll
   for (int x = 16; x > 0; x /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+  // eight shares' loads under way at a time
+  using Piece = std::conditional_t<kDim == 128, float4, float2>;
   float total = 0.0f, acc[kDim / 32] = {};
-#pragma unroll 4
-  for (int w = w0; w <= w1; ++w) {
-    const float *from = slot(w);
-    const float m = load_global(from + (size_t)rows * kDim + 2 * at), l = load_global(from + (size_t)rows * kDim + 2 * at + 1);
-    const float f = top == -INFINITY ? 0.0f : exp2_fast(m - top);
-    total = fmaf(f, l, total);
+  for (int w = w0; w <= w1; w += 8) {
+    Piece v[8];
+    float ml[8][2];
 #pragma unroll
-    for (int c = 0; c < kDim / 32; ++c) acc[c] = fmaf(f, load_global(from + (size_t)at * kDim + lane * (kDim / 32) + c), acc[c]);
+    for (int i = 0; i < 8; ++i) {
+      const float *from = slot(min(w + i, w1));
+      ml[i][0] = load_global(from + (size_t)rows * kDim + 2 * at);
+      ml[i][1] = load_global(from + (size_t)rows * kDim + 2 * at + 1);
+      v[i] = load_piece(reinterpret_cast<const Piece *>(from + (size_t)at * kDim) + lane);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float f = top == -INFINITY || w + i > w1 ? 0.0f : exp2_fast(ml[i][0] - top);
+      if (f == 0.0f) continue;                             // (a share that saw nothing)
+      total = fmaf(f, ml[i][1], total);
+#pragma unroll
+      for (int c = 0; c < kDim / 32; ++c) acc[c] = fmaf(f, reinterpret_cast<const float *>(&v[i])[c], acc[c]);
+    }
   }
   const bool blind = place < 0;
   const float inv = 1.0f / total;
@@ -561,7 +638,7 @@ cudaError_t run(const Kv4Args &a, int most_rows, cudaStream_t st) {
   static bool flags[64] = {};
   cudaError_t e = allow_shared(kv4_few_kernel<T, kDim, kTiles>, L::kBytes, flags);
   if (e != cudaSuccess) return e;
-  const int workers = std::min(kMaxWorkers, kPerSm * sm_count_of_current_device());
+  const int workers = std::min(kMaxWorkers, per_sm(kTiles) * sm_count_of_current_device());
   const Params P = {a, {a.r.q_heads / a.w.d.kv_heads, L::kRows, kKvTokens, a.r.rows, 0, most_rows}, workers, rows_in_pieces(a.q, a.r.q_stride, kDim, 2), a.r.out_stride % 2 == 0, W4Type<T>::kMagic, W4Type<__half>::kMagic};
   e = launch_kernel(kv4_few_kernel<T, kDim, kTiles>, dim3((unsigned)workers), 32 * (kWarps + 1), L::kBytes, st, 1, P);
   if (e != cudaSuccess) return e;
