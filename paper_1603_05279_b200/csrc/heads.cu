@@ -66,7 +66,7 @@ struct TwoChunks {
 };
 
 template <class T, int kDim, bool kPairs>
-__global__ void __launch_bounds__(32 * kWarps)
+__global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 4 ? 2 : 3)
 heads_kernel(const HeadsArgs A, int parts) {
   const HeadLane<kDim> lane(threadIdx.x & 31, A.d.rot, kPairs);
   const HeadUnits<T, kDim> U(A.d);
@@ -91,7 +91,7 @@ heads_kernel(const HeadsArgs A, int parts) {
         float s = 0.0f, w[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) s = fmaf(v[i], v[i], s);
-        const float r = 1.0f / sqrtf(lane.sum(s) * (1.0f / kDim) + A.d.eps);
+        const float r = __frsqrt_rn(lane.sum(s) * (1.0f / kDim) + A.d.eps);
         const void *weight = U.keys(u) ? A.k_weight : A.q_weight;
         load_head_weights<T>(weight, f32, lane.a, w);
         load_head_weights<T>(weight, f32, lane.b, w + 8);
@@ -138,7 +138,7 @@ constexpr int kBackwardEach = 4;
 // g = the gradient turned back, u = weight g:  dx = rstd (u - x rstd^2 mean(u x)),  dweight += g x rstd.  A thread adds up its
 // sixteen columns' dweight over all its heads, the block adds its threads' in a fixed order, and leaves a row of `work`.
 template <class T, int kDim, bool kPairs>
-__global__ void __launch_bounds__(32 * kWarps)
+__global__ void __launch_bounds__(32 * kWarps, 2)
 heads_backward_kernel(const HeadsArgs A, int q_blocks) {
   using Lane = HeadLane<kDim>;
   __shared__ float sums[kWarps * Lane::kHeads][kDim + 4];
@@ -179,7 +179,7 @@ heads_backward_kernel(const HeadsArgs A, int q_blocks) {
         for (int j = 0; j < 16; ++j) s = fmaf(x[j], x[j], s);
 #pragma unroll
         for (int j = 0; j < 16; ++j) dot = fmaf(g[j] * w[j], x[j], dot);
-        const float r = 1.0f / sqrtf(lane.sum(s) * (1.0f / kDim) + A.d.eps);
+        const float r = __frsqrt_rn(lane.sum(s) * (1.0f / kDim) + A.d.eps);
         const float k = lane.sum(dot) * (r * r * (1.0f / kDim));
 #pragma unroll
         for (int j = 0; j < 16; ++j) {

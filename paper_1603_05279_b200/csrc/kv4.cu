@@ -55,7 +55,7 @@ __device__ __forceinline__ void store_codes(const float (&v)[16], const HeadLane
 
 // As the kernel of norms and rotations (heads.cu): a warp has a token, and its units of queries, then of keys, then of values.
 template <class T, int kDim, bool kPairs>
-__global__ void __launch_bounds__(32 * kWarps)
+__global__ void __launch_bounds__(32 * kWarps, 2)
 kv4_append_kernel(const Kv4AppendArgs A, int parts, int pieces) {
   using Lane = HeadLane<kDim>;
   const xnor_heads_desc &d = A.h.d;
@@ -68,26 +68,34 @@ kv4_append_kernel(const Kv4AppendArgs A, int parts, int pieces) {
   stream_order();
   for (long long item = (long long)blockIdx.x * kWarps + threadIdx.x / 32; item < items; item += (long long)gridDim.x * kWarps) {
     const int t = (int)(item / parts);
+    const T *q = static_cast<const T *>(A.h.q) + t * d.q_stride, *k = static_cast<const T *>(A.h.k) + t * d.k_stride;
+    const T *v_row = static_cast<const T *>(A.v) + t * d.v_stride;
+    auto kind_of = [&](int u) { return u < q_units ? 0 : u < q_units + k_units ? 1 : 2; };
+    auto head_of = [&](int u) { return (u < q_units ? u : u < q_units + k_units ? u - q_units : u - q_units - k_units) * Lane::kHeads + lane.sub; };
+    auto fetch = [&](int u, Chunk<T> &ca, Chunk<T> &cb) {
+      const int kind = kind_of(u), head = head_of(u);
+      const bool in = u < q_units + 2 * k_units && head < (kind == 0 ? d.q_heads : d.k_heads);
+      const T *from = (kind == 0 ? q : kind == 1 ? k : v_row) + (in ? head : 0) * kDim;
+      ca.load(from + lane.a, pieces, in ? 8 : 0);
+      cb.load(from + lane.b, pieces, in ? 8 : 0);
+    };
+    // (the first values are under way while the token's place is looked up, then the next ones while these are worked on)
+    const int first = (int)(item % parts);
+    Chunk<T> xa, xb, ya, yb;
+    fetch(first, xa, xb);
     int b, place;
     if (!find_sequence(A.w, t, id, b, place) || place < 0) continue;
-    long long record = kv4_find(A.w, b, place / kKvTokens, 0);
+    const long long record = kv4_find(A.w, b, place / kKvTokens, 0);
     const bool angles_there = d.rot == 0 || place < d.positions;
     if ((record < 0 || !angles_there) && id == 0) atomicMax(&g_status_kv4, (int)XNOR_ERR_BOUNDS);
     if (!angles_there) continue;
-    const T *q = static_cast<const T *>(A.h.q) + t * d.q_stride, *k = static_cast<const T *>(A.h.k) + t * d.k_stride;
-    const T *v_row = static_cast<const T *>(A.v) + t * d.v_stride;
     T *q_out = static_cast<T *>(A.h.q_out) + t * d.q_out_stride;
     Angles angles;
     if (lane.turns) angles.load(A.h.table + (size_t)place * d.rot, d.rot, lane.which);
-    for (int u = (int)(item % parts); u < q_units + 2 * k_units; u += parts) {
-      const int kind = u < q_units ? 0 : u < q_units + k_units ? 1 : 2;
-      if (kind > 0 && record < 0) break;
-      const int head = (kind == 0 ? u : kind == 1 ? u - q_units : u - q_units - k_units) * Lane::kHeads + lane.sub;
+    auto finish = [&](int u, Chunk<T> &ca, Chunk<T> &cb) {
+      const int kind = kind_of(u), head = head_of(u);
+      if (kind > 0 && record < 0) return;
       const bool in = head < (kind == 0 ? d.q_heads : d.k_heads);
-      const T *from = (kind == 0 ? q : kind == 1 ? k : v_row) + (in ? head : 0) * kDim;
-      Chunk<T> ca, cb;
-      ca.load(from + lane.a, pieces, in ? 8 : 0);
-      cb.load(from + lane.b, pieces, in ? 8 : 0);
       float v[16];
       ca.to_float(*reinterpret_cast<float (*)[8]>(v));
       cb.to_float(*reinterpret_cast<float (*)[8]>(v + 8));
@@ -102,7 +110,7 @@ kv4_append_kernel(const Kv4AppendArgs A, int parts, int pieces) {
           float s = 0.0f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) s = fmaf(v[i], v[i], s);
-          const float r = 1.0f / sqrtf(lane.sum(s) * (1.0f / kDim) + d.eps);
+          const float r = __frsqrt_rn(lane.sum(s) * (1.0f / kDim) + d.eps);
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[i] *= r * w[i];
         }
@@ -113,7 +121,7 @@ kv4_append_kernel(const Kv4AppendArgs A, int parts, int pieces) {
           ca.store(q_out + head * kDim + lane.a, pieces, 8);
           cb.store(q_out + head * kDim + lane.b, pieces, 8);
         }
-        continue;
+        return;
       }
       if (kind == 1 && (d.norm || d.rot > 0)) {
         // Keys in 64 bits: a code is that of the exact key, wherever it lies next to a border.
@@ -134,6 +142,14 @@ kv4_append_kernel(const Kv4AppendArgs A, int parts, int pieces) {
       }
       uint8_t *to = A.cache + (size_t)(record + (long long)(in ? head : 0) * per_page) * kv4_record(kDim);
       store_codes<kDim>(v, lane, to, place % kKvTokens, kind == 2, in);
+    };
+#pragma unroll 1
+    for (int u = first; u < q_units + 2 * k_units; u += 2 * parts) {
+      fetch(u + parts, ya, yb);
+      finish(u, xa, xb);
+      if (u + parts >= q_units + 2 * k_units) break;
+      fetch(u + 2 * parts, xa, xb);
+      finish(u + parts, ya, yb);
     }
   }
 }

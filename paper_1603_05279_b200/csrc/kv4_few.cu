@@ -5,7 +5,8 @@
 // sequences, heads and tiles stand in one row, and every block takes an equal share of it, found on the device from the
 // lengths; so a batch of any lengths keeps all SMs reading.  The tokens are the matrix operand (16 rows of m16n8k16) and the
 // queries, up to 8 kTiles of them, the other: S^T = K Q^T, then O^T += V^T P^T, whose codes - zero come straight from
-// a record's words, exactly.  A key's scale multiplies its row of S^T, a value's its row of P^T, which a matrix transposition
+// a record's words, exactly, as F16 (whose expansion takes two instructions in eleven fewer than bfloat16's; so queries in bfloat16
+// become F16, times a power of two).  A key's scale multiplies its row of S^T, a value's its row of P^T, which a matrix transposition
 // within the warp (movmatrix) makes the second operand.  The softmax is one pass: a running maximum, raised (and
 // the sums rescaled) only when it is exceeded by more than 2^8, and sums in fp32.
 //
@@ -128,11 +129,7 @@ struct Layout {
   static_assert(kAbort + 4 <= kStats, "control words");
 };
 
-__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half) {
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -148,7 +145,7 @@ struct Params {
   Kv4Args A;
   Tiling T;
   int workers, q_pieces, out_words;      // q can be read in 16-byte pieces, out written in words
-  uint32_t magic, magic16;     // W4Type's of the queries' type and of F16
+  uint32_t magic;              // W4Type's
 };
 
 // Waits of a warp's threads for their own barriers; false: gave up.
@@ -193,7 +190,7 @@ __device__ __forceinline__ void copy_role(const Params &P, long long u0, long lo
 #pragma unroll 1
     for (int turn = 0; alive && turn < kTurns; ++turn) {
       if (lane / kWarps == turn && mine && u + lane < u1) {
-        alive = wait_for(empty, parity, abort_flag);
+        alive = mbar_wait_relaxed(empty, parity, abort_flag, &g_status_kv4_few, 100);     // (the issue slots are the others')
         if (alive) {
           const bool there = now.record >= 0;
           if (!there && now.valid > 0) atomicMax(&g_status_kv4_few, (int)XNOR_ERR_BOUNDS);
@@ -263,7 +260,8 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
   const int g = lane >> 2, t = lane & 3;
   float *stats = reinterpret_cast<float *>(smem_ptr + L::kStats), *sums = reinterpret_cast<float *>(smem_ptr + L::kSums);
   const float scale2 = P.A.r.scale * kLog2e;
-  const int tok0 = token_of(g), tok1 = token_of(g + 8);                    // this thread's rows of S^T
+  const int tok0 = token_of(g), tok1 = tok0 + 8;                           // this thread's rows of S^T
+  const int pair = token_of(2 * t);                                        // and of P^T: this, its neighbour, and eight on
   Place p;
   p.b = b0;
   p.s = s0;
@@ -282,16 +280,44 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
     // Q: thread (g, t) has row g's columns kDim / 4 t .., as its words of keys have them
     uint32_t q[kTiles][kWords][4];
     int limit[kTiles][2], least = 0x7FFFFFFF;
+    float row_scale[kTiles][2];                                            // of logits: scale, log2 e and what the query was multiplied by
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
       const TileRow r(P, p, kRows, 8 * n + g, kDim);
+      Chunk<T> c[kWords];
 #pragma unroll
-      for (int w = 0; w < kWords; ++w) {
-        Chunk<T> c;
-        c.load(static_cast<const T *>(P.A.q) + r.q + t * (kDim / 4) + 8 * w, P.q_pieces, r.in ? 8 : 0);
+      for (int w = 0; w < kWords; ++w) c[w].load(static_cast<const T *>(P.A.q) + r.q + t * (kDim / 4) + 8 * w, P.q_pieces, r.in ? 8 : 0);
+      float lifted = 1.0f;
+      if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        // bfloat16 as F16, times a power of two that brings the row's largest value to 2^14: exact but for values below 2^-31 of that
+        uint32_t top = 0u;                                                 // (bit patterns of magnitudes; infinity and NaN stay what they are)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[n][w][i] = c.w[i];
+        for (int w = 0; w < kWords; ++w)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = c[w].w[i] & 0x7FFFu, hi = c[w].w[i] >> 16 & 0x7FFFu;
+            top = max(top, max(lo < 0x7F80u ? lo : 0u, hi < 0x7F80u ? hi : 0u));
+          }
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int up = min(126, max(-112, 14 - ((int)(top >> 7) - 127)));
+        const float f = power_of_two(up);
+        lifted = power_of_two(-up);
+#pragma unroll
+        for (int w = 0; w < kWords; ++w)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 v = pair_to_float(c[w].w[i], T());
+            q[n][w][i] = float_to_pair(v.x * f, v.y * f, __half());
+          }
+      } else {
+#pragma unroll
+        for (int w = 0; w < kWords; ++w)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) q[n][w][i] = c[w].w[i];
       }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) row_scale[n][i] = scale2 * __shfl_sync(0xffffffffu, lifted, 4 * (2 * t + i));
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const TileRow s(P, p, kRows, 8 * n + 2 * t + i, kDim);
@@ -326,9 +352,9 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
       const int valid = (int)lds32(smem + L::kValid + 4u * stage);
       const uint32_t kw0 = lds32(base + kv4_words(kDim, false) + 4u * tok0), kw1 = lds32(base + kv4_words(kDim, false) + 4u * tok1);
       const uint32_t vw0 = lds32(base + kv4_words(kDim, true) + 4u * tok0), vw1 = lds32(base + kv4_words(kDim, true) + 4u * tok1);
-      uint32_t c0[kWords], c1[kWords], c[2][2][kVWords], zeros[2];
+      uint32_t c0[kWords], c1[kWords];
       {
-        const uint32_t from = base + (uint32_t)(t * (kDim / 8)), codes = base + kv4_codes(kDim, true) + (uint32_t)(g * (kDim / 16));
+        const uint32_t from = base + (uint32_t)(t * (kDim / 8));
         if constexpr (kWords == 4) {
           lds128(from + tok0 * (kDim / 2), c0);
           lds128(from + tok1 * (kDim / 2), c1);
@@ -336,9 +362,35 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
           lds64(from + tok0 * (kDim / 2), c0[0], c0[1]);
           lds64(from + tok1 * (kDim / 2), c1[0], c1[1]);
         }
+      }
+      // ---- S^T
+      // (two chains of products: one waits eight times for a product of 30 cycles and more)
+      float s[kTiles][4], s2[kTiles][4];
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[n][j] = s2[n][j] = 0.0f;
+      {
+        const W4Type<__half>::Zero z0 = W4Type<__half>::zero(kw0 & 15u), z1 = W4Type<__half>::zero(kw1 & 15u);
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) {
+          uint32_t e0[4], e1[4];
+          W4Type<__half>::expand(c0[w], z0, P.magic, e0);
+          W4Type<__half>::expand(c1[w], z1, P.magic, e1);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t a[4] = {e0[2 * k], e1[2 * k], e0[2 * k + 1], e1[2 * k + 1]};
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) mma16816(k == 0 ? s[n] : s2[n], a, q[n][w][2 * k], q[n][w][2 * k + 1]);
+          }
+        }
+      }
+      uint32_t c[2][2][kVWords], zeros[2];                                 // (under way during the softmax)
+      {
+        const uint32_t codes = base + kv4_codes(kDim, true) + (uint32_t)(g * (kDim / 16));
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int ta = token_of(2 * t + 8 * h), tb = token_of(2 * t + 1 + 8 * h);
+          const int ta = pair + 8 * h, tb = (pair ^ 1) + 8 * h;
           if constexpr (kVWords == 2) {
             lds64(codes + ta * (kDim / 2), c[h][0][0], c[h][0][1]);
             lds64(codes + tb * (kDim / 2), c[h][1][0], c[h][1][1]);
@@ -353,36 +405,15 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(smem + L::kEmpty + 8u * stage);
-      // ---- S^T
-      float s[kTiles][4];
-#pragma unroll
-      for (int n = 0; n < kTiles; ++n)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s[n][j] = 0.0f;
-      {
-        const typename W4Type<T>::Zero z0 = W4Type<T>::zero(kw0 & 15u), z1 = W4Type<T>::zero(kw1 & 15u);
-#pragma unroll
-        for (int w = 0; w < kWords; ++w) {
-          uint32_t e0[4], e1[4];
-          W4Type<T>::expand(c0[w], z0, P.magic, e0);
-          W4Type<T>::expand(c1[w], z1, P.magic, e1);
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const uint32_t a[4] = {e0[2 * k], e1[2 * k], e0[2 * k + 1], e1[2 * k + 1]};
-#pragma unroll
-            for (int n = 0; n < kTiles; ++n) mma16816(s[n], a, q[n][w][2 * k], q[n][w][2 * k + 1], T());
-          }
-        }
-      }
       // ---- the softmax: s[n][0], [1]: token tok0 for rows 2 t, 2 t + 1; [2], [3]: token tok1
-      const float ks0 = kv4_scale(kw0) * scale2, ks1 = kv4_scale(kw1) * scale2;
+      const float ks0 = kv4_scale(kw0), ks1 = kv4_scale(kw1);
       float vs0 = kv4_scale(vw0), vs1 = kv4_scale(vw1), over = -INFINITY, x[kTiles][4];
       const int p0 = rec * kKvTokens;
       const bool masked = valid < kKvTokens || p0 + kKvTokens - 1 > least;
 #pragma unroll
       for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[n][j] *= j < 2 ? ks0 : ks1;
+        for (int j = 0; j < 4; ++j) s[n][j] = (s[n][j] + s2[n][j]) * row_scale[n][j & 1] * (j < 2 ? ks0 : ks1);
       if (masked) {
 #pragma unroll
         for (int n = 0; n < kTiles; ++n)
@@ -453,20 +484,20 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
         using V = W4Type<__half>;
         V::Zero z[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) z[h] = {P.magic16 | zeros[h], 0xD400D400u | zeros[h] << 4};
+        for (int h = 0; h < 2; ++h) z[h] = {P.magic | zeros[h], 0xD400D400u | zeros[h] << 4};
 #pragma unroll
         for (int w = 0; w < kVWords; ++w) {
           uint32_t v[2][2][4];                                             // [half of the tokens][even, odd columns][pairs]
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            V::expand(__byte_perm(c[h][0][w], c[h][1][w], 0x5410), z[h], P.magic16, v[h][0]);
-            V::expand(__byte_perm(c[h][0][w], c[h][1][w], 0x7632), z[h], P.magic16, v[h][1]);
+            V::expand(__byte_perm(c[h][0][w], c[h][1][w], 0x5410), z[h], P.magic, v[h][0]);
+            V::expand(__byte_perm(c[h][0][w], c[h][1][w], 0x7632), z[h], P.magic, v[h][1]);
           }
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const uint32_t a[4] = {v[0][0][k], v[0][1][k], v[1][0][k], v[1][1][k]};
 #pragma unroll
-            for (int n = 0; n < kTiles; ++n) mma16816(o[n][4 * w + k], a, b[n][0], b[n][1], __half());
+            for (int n = 0; n < kTiles; ++n) mma16816(o[n][4 * w + k], a, b[n][0], b[n][1]);
           }
         }
       }
@@ -639,7 +670,7 @@ cudaError_t run(const Kv4Args &a, int most_rows, cudaStream_t st) {
   cudaError_t e = allow_shared(kv4_few_kernel<T, kDim, kTiles>, L::kBytes, flags);
   if (e != cudaSuccess) return e;
   const int workers = std::min(kMaxWorkers, per_sm(kTiles) * sm_count_of_current_device());
-  const Params P = {a, {a.r.q_heads / a.w.d.kv_heads, L::kRows, kKvTokens, a.r.rows, 0, most_rows}, workers, rows_in_pieces(a.q, a.r.q_stride, kDim, 2), a.r.out_stride % 2 == 0, W4Type<T>::kMagic, W4Type<__half>::kMagic};
+  const Params P = {a, {a.r.q_heads / a.w.d.kv_heads, L::kRows, kKvTokens, a.r.rows, 0, most_rows}, workers, rows_in_pieces(a.q, a.r.q_stride, kDim, 2), a.r.out_stride % 2 == 0, W4Type<__half>::kMagic};
   e = launch_kernel(kv4_few_kernel<T, kDim, kTiles>, dim3((unsigned)workers), 32 * (kWarps + 1), L::kBytes, st, 1, P);
   if (e != cudaSuccess) return e;
   const long long rows = (long long)a.r.rows * a.r.q_heads;
