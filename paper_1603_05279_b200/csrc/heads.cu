@@ -79,42 +79,48 @@ heads_kernel(const HeadsArgs A, int parts) {
     if (!angles_of(A, t, row)) continue;
     const T *q = static_cast<const T *>(A.q) + t * A.d.q_stride, *k = static_cast<const T *>(A.k) + t * A.d.k_stride;
     T *q_out = static_cast<T *>(A.q_out) + t * A.d.q_out_stride, *k_out = static_cast<T *>(A.k_out) + t * A.d.k_out_stride;
-    auto fetch = [&](int u, TwoChunks<T> &x) {
-      const int h = U.head(A.d, lane, u);
-      x.load((U.keys(u) ? k : q) + max(h, 0) * kDim, lane, h >= 0);
-    };
     Angles angles;
-    auto finish = [&](int u, TwoChunks<T> &x) {
-      float v[16];
-      x.to_float(v);
+    // units of one kind, `first`, first + parts, ..: their weights stay in registers
+    auto run = [&](int first, int units, int heads, const T *from, T *to, const void *weight, bool start) {
+      if (first >= units) return;
+      const int step = parts * HeadLane<kDim>::kHeads;
+      int h = first * HeadLane<kDim>::kHeads + lane.sub;
+      TwoChunks<T> x, y;
+      x.load(from + h * kDim, lane, h < heads);
+      if (start && lane.turns) angles.load(row, A.d.rot, lane.which);
+      float w[16];
       if (A.d.norm) {
-        float s = 0.0f, w[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s = fmaf(v[i], v[i], s);
-        const float r = __frsqrt_rn(lane.sum(s) * (1.0f / kDim) + A.d.eps);
-        const void *weight = U.keys(u) ? A.k_weight : A.q_weight;
         load_head_weights<T>(weight, f32, lane.a, w);
         load_head_weights<T>(weight, f32, lane.b, w + 8);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] *= r * w[i];
       }
-      if (lane.turns) turn<kPairs, 1>(v, angles);
-      x.from_float(v);
-      const int h = U.head(A.d, lane, u);
-      if (h >= 0) x.store((U.keys(u) ? k_out : q_out) + h * kDim, lane);
-    };
-    TwoChunks<T> x, y;
-    const int first = (int)(item % parts);
-    fetch(first, x);
-    if (lane.turns) angles.load(row, A.d.rot, lane.which);
+      auto finish = [&](int h, TwoChunks<T> &x) {
+        float v[16];
+        x.to_float(v);
+        if (A.d.norm) {
+          float s = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s = fmaf(v[i], v[i], s);
+          const float r = __frsqrt_rn(lane.sum(s) * (1.0f / kDim) + A.d.eps);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] *= r * w[i];
+        }
+        if (lane.turns) turn<kPairs, 1>(v, angles);
+        x.from_float(v);
+        if (h < heads) x.store(to + h * kDim, lane);
+      };
 #pragma unroll 1
-    for (int u = first; u < U.units; u += 2 * parts) {
-      fetch(u + parts, y);
-      finish(u, x);
-      if (u + parts >= U.units) break;
-      fetch(u + 2 * parts, x);
-      finish(u + parts, y);
-    }
+      for (int u = first; u < units; u += 2 * parts, h += 2 * step) {
+        y.load(from + (h + step) * kDim, lane, u + parts < units && h + step < heads);
+        finish(h, x);
+        if (u + parts >= units) break;
+        x.load(from + (h + 2 * step) * kDim, lane, u + 2 * parts < units && h + 2 * step < heads);
+        finish(h + step, y);
+      }
+    };
+    const int first = (int)(item % parts);
+    run(first, U.q_units, A.d.q_heads, q, q_out, A.q_weight, true);
+    const int later = first >= U.q_units ? first - U.q_units : (first - U.q_units % parts + parts) % parts;      // its first unit of keys
+    run(later, U.units - U.q_units, A.d.k_heads, k, k_out, A.k_weight, first >= U.q_units);
   }
 }
 

@@ -27,13 +27,15 @@ __device__ __forceinline__ void store_codes(const float (&v)[16], const HeadLane
     hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
     odd += __shfl_xor_sync(0xffffffffu, odd, o);
   }
-  const uint32_t bits = __float_as_uint((float)(((double)hi - (double)lo) / 15.0)) & ~15u;
+  // a fifteenth in 64 bits, the quotient mended by its rest (Markstein): a division by a variable takes 100 instructions
+  const double range = (double)hi - (double)lo, fifteenth = range * (1.0 / 15.0);
+  const uint32_t bits = __float_as_uint((float)fma(fma(-15.0, fifteenth, range), 1.0 / 15.0, fifteenth)) & ~15u;
   const float s = __uint_as_float(bits);
   const bool sound = odd == 0.0f && s > 0.0f;
   const float inv = sound && s > 1e-37f ? 1.0f / s : 0.0f;        // 0: it would overflow
   float z = 8.0f, q[16];
   if (sound) {
-    z = fminf(15.0f, fmaxf(0.0f, round_quotient(-lo, s)));
+    z = fminf(15.0f, fmaxf(0.0f, inv == 0.0f ? round_quotient(-lo, s) : mend_quotient(rintf(-lo * inv), -lo, s)));
     round_quotients(v, s, inv, z, q);
 #pragma unroll
     for (int i = 0; i < 16; ++i) q[i] = fminf(15.0f, fmaxf(0.0f, q[i] + z));
@@ -85,13 +87,13 @@ kv4_append_kernel(const Kv4AppendArgs A, int parts, int pieces) {
     fetch(first, xa, xb);
     int b, place;
     if (!find_sequence(A.w, t, id, b, place) || place < 0) continue;
-    const long long record = kv4_find(A.w, b, place / kKvTokens, 0);
     const bool angles_there = d.rot == 0 || place < d.positions;
+    Angles angles;
+    if (lane.turns && angles_there) angles.load(A.h.table + (size_t)place * d.rot, d.rot, lane.which);
+    const long long record = kv4_find(A.w, b, place / kKvTokens, 0);
     if ((record < 0 || !angles_there) && id == 0) atomicMax(&g_status_kv4, (int)XNOR_ERR_BOUNDS);
     if (!angles_there) continue;
     T *q_out = static_cast<T *>(A.h.q_out) + t * d.q_out_stride;
-    Angles angles;
-    if (lane.turns) angles.load(A.h.table + (size_t)place * d.rot, d.rot, lane.which);
     auto finish = [&](int u, Chunk<T> &ca, Chunk<T> &cb) {
       const int kind = kind_of(u), head = head_of(u);
       if (kind > 0 && record < 0) return;

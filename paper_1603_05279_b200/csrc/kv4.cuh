@@ -34,21 +34,31 @@ __device__ __forceinline__ long long kv4_find(const Kv4Where &W, int b, int rec,
   return ((long long)page * W.d.kv_heads + h) * per_page + (rec - at * per_page);
 }
 
-// The sequence of a row, for all threads of a warp; false: it belongs to none.  Thirty-two threads look at once.
+// The sequence of a row and the row's token in it, for all threads of a warp; false: it belongs to none.  Thirty-two threads look
+// at once, in the last round at all that a sequence has, so that up to 32 sequences take one load's latency.
 __device__ __forceinline__ bool find_sequence(const Kv4Where &W, int row, int lane, int &b, int &place) {
   int lo = 0, hi = W.d.seqs;                  // the first sequence that ends behind the row is in lo .. hi (hi: none)
-  while (lo < hi) {
+  while (hi - lo > 32) {
     const int step = (hi - lo + 31) / 32, i = lo + (lane + 1) * step - 1;
     const bool before = i < hi && load_int(W.starts + i + 1) <= row;
     const int k = __popc(__ballot_sync(0xffffffffu, before));
     hi = min(hi, lo + (k + 1) * step - 1);
     lo = min(hi, lo + k * step);
   }
-  b = lo;
-  if (b >= W.d.seqs) return false;
-  const int end = load_int(W.starts + b + 1);
-  if (load_int(W.starts + b) > row || end <= row) return false;
-  place = load_int(W.lens + b) - (end - row);
+  const int i = min(lo + lane, W.d.seqs - 1);
+  const int start = load_int(W.starts + i), end = load_int(W.starts + i + 1), len = load_int(W.lens + i);
+  const uint32_t has = __ballot_sync(0xffffffffu, lo + lane <= hi && lo + lane < W.d.seqs && start <= row && end > row);
+  // (sequences up to hi: with 32 in between, hi itself has a thread of its own only if there are fewer)
+  if (has == 0u) {
+    if (hi - lo < 32 || hi >= W.d.seqs) return false;
+    const int s = load_int(W.starts + hi), e = load_int(W.starts + hi + 1);
+    b = hi;
+    place = load_int(W.lens + hi) - (e - row);
+    return s <= row && e > row;
+  }
+  const int who = __ffs((int)has) - 1;
+  b = lo + who;
+  place = __shfl_sync(0xffffffffu, len - (end - row), who);
   return true;
 }
 
