@@ -616,7 +616,7 @@ xnor_status xnor_qk_norm_rope_backward(const void *dq_out, const void *dk_out, c
  * value = (code - zero) scale.  Bytes [pages][kv_heads][page / 16][16 (dim + 8)]; of 16 tokens
  *   keys' codes    [16][dim / 2]   column 2 i + h of eight in bits 4 i + 16 h and up of their word
  *   values' codes  [16][dim / 2]
- *   keys' words    u32 [16]        the scale in fp32, the zero point in the place of its last 4 bits
+ *   keys' words    u32 [16]        the scale in fp32, 0 or more, the zero point in the place of its last 4 bits
  *   values' words  u32 [16]
  * Sequence b has the rows starts[b] .. starts[b + 1] - 1 of the call's new tokens, which are its last
  * ones: it has lens[b] tokens with them.  Token p of it lies at place p % page of page
@@ -641,7 +641,8 @@ xnor_status xnor_qk_norm_rope_backward(const void *dq_out, const void *dk_out, c
  *
  * INVALID_ARG as in xnor_qk_norm_rope, and: null or misaligned cache, starts, lens, table; pages, kv_heads,
  * seqs < 0 or < 1, page < 16 or not a multiple of 16, table_cols < 1; k_heads that are not d->kv_heads.
- * UNSUPPORTED: dim neither 64 nor 128, rot no multiple of 16, page > 65536, kv_heads > 4096, seqs > 2^20.
+ * UNSUPPORTED: dim neither 64 nor 128, rot no multiple of 16, page > 65536, kv_heads > 4096, seqs > 2^20,
+ * table_cols page > 2^31 - 256.
  */
 typedef struct {
   int pages, page, kv_heads, dim;
@@ -665,10 +666,12 @@ xnor_status xnor_kv4_read(const void *cache, const int32_t *starts, const int32_
  *   lse   out  fp32 [rows][q_heads], dense, or NULL; -infinity for a row that sees nothing
  *   most  no sequence has more new tokens than this (0: not known).  By it and the sizes the call
  *         chooses its kernels; where it is too small, results are as good and may take longer
- *   work  scratch of xnor_kv4_work_bytes(d, r) bytes, whatever is in it; calls that can overlap need one each
- * Codes and queries are exact operands; products, sums and the softmax are fp32, but exp(..) times a value's
- * scale, which is rounded to 11 bits (below 2^-21 of the largest scale to a step of 2^-31 of that) to meet the values' codes.  The order of
- * the sums depends on the sizes, all sequences' lengths and the device's number of SMs: the same call gives the same bits.
+ *   work  scratch of xnor_kv4_work_bytes(d, r) bytes, whatever is in it, which is enough for calls with fewer rows, fewer
+ *         sequences or a smaller `most` as well; calls that can overlap need one each
+ * Codes are exact operands, and so are queries (in BF16, where rows are few, but for values below 2^-31 of the row's
+ * largest, which are rounded to a step of 2^-38 of that); products, sums and the softmax are fp32, but exp(..) times
+ * a value's scale, which is rounded to 11 bits (below 2^-21 of the largest scale to a step of 2^-31 of that) to meet the
+ * values' codes.  The order of the sums depends on the sizes, all sequences' lengths and the device's number of SMs: the same call gives the same bits.
  * Device-side waits are bounded (xnor_check_device).  What lies outside the table or the cache is not seen.
  * INVALID_ARG as above, and: q_heads no multiple of kv_heads, scale not finite, most < 0, out in the place of q.
  * UNSUPPORTED as above, and: F32, rows q_heads > 2^30.

@@ -345,10 +345,9 @@ xnor_status xnor_check_device(void *cuda_stream) {
     (void)cudaGetLastError();
     return XNOR_ERR_CUDA;
   }
-  if (st >= 1000 || st7 == XNOR_ERR_BOUNDS || st8 == XNOR_ERR_BOUNDS || st9 == XNOR_ERR_BOUNDS ||
-      st10 == XNOR_ERR_BOUNDS)
-    return XNOR_ERR_BOUNDS;
-  return (st == 0 && st2 == 0 && st3 == 0 && st4 == 0 && st5 == 0 && st6 == 0 && st9 == 0 && st10 == 0) ? XNOR_OK : XNOR_ERR_TIMEOUT;
+  if (st >= 1000) return XNOR_ERR_BOUNDS;
+  if (st || st2 || st3 || st4 || st5 || st6 || st9 == XNOR_ERR_TIMEOUT || st10 == XNOR_ERR_TIMEOUT) return XNOR_ERR_TIMEOUT;
+  return st7 || st8 || st9 || st10 ? XNOR_ERR_BOUNDS : XNOR_OK;
 }
 
 xnor_status xnor_measure_peaks(double *mma_mac_per_clk_per_sm, double *popc_per_clk_per_sm,
@@ -496,9 +495,10 @@ xnor_status check_heads(const xnor_heads_desc *d, const void *q_weight, const vo
 
 bool bad_kv4(const xnor_kv4_desc *d) { return !d || d->pages < 1 || d->page < 16 || d->page % 16 || d->kv_heads < 1 || d->dim < 1; }
 bool large_kv4(const xnor_kv4_desc *d) { return (d->dim != 64 && d->dim != 128) || d->page > 65536 || d->kv_heads > 4096; }
+constexpr long long kMostTokens = (1ll << 31) - 256;      // of a sequence: rounded up to whole tiles an int
 xnor_status check_kv4(const xnor_kv4_desc *d, const void *cache, const int32_t *starts, const int32_t *lens, const int32_t *table) {
   if (bad_kv4(d) || d->seqs < 1 || d->table_cols < 1 || bad_ptr(cache) || bad_ptr(starts) || bad_ptr(lens) || bad_ptr(table)) return XNOR_ERR_INVALID_ARG;
-  return large_kv4(d) || d->seqs > (1 << 20) ? XNOR_ERR_UNSUPPORTED : XNOR_OK;
+  return large_kv4(d) || d->seqs > (1 << 20) || (long long)d->table_cols * d->page > kMostTokens ? XNOR_ERR_UNSUPPORTED : XNOR_OK;
 }
 bool bad_kv4_rows(const xnor_kv4_desc *d, const xnor_kv4_rows *r) {
   return !r || r->rows < 0 || r->q_heads < 1 || r->q_heads % d->kv_heads || !real_type(r->type) || r->most < 0;

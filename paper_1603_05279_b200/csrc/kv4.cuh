@@ -34,8 +34,8 @@ __device__ __forceinline__ long long kv4_find(const Kv4Where &W, int b, int rec,
   return ((long long)page * W.d.kv_heads + h) * per_page + (rec - at * per_page);
 }
 
-// The sequence of a row and the row's token in it, for all threads of a warp; false: it belongs to none.  Thirty-two threads look
-// at once, in the last round at all that a sequence has, so that up to 32 sequences take one load's latency.
+// The sequence of a row and the row's token in it (below 0: before its first), for all threads of a warp; false: it belongs to
+// none.  Thirty-two threads look at once, and in the last round each at a whole sequence, so that up to 32 of them take one load's latency.
 __device__ __forceinline__ bool find_sequence(const Kv4Where &W, int row, int lane, int &b, int &place) {
   int lo = 0, hi = W.d.seqs;                  // the first sequence that ends behind the row is in lo .. hi (hi: none)
   while (hi - lo > 32) {
@@ -46,14 +46,14 @@ __device__ __forceinline__ bool find_sequence(const Kv4Where &W, int row, int la
     lo = min(hi, lo + k * step);
   }
   const int i = min(lo + lane, W.d.seqs - 1);
-  const int start = load_int(W.starts + i), end = load_int(W.starts + i + 1), len = load_int(W.lens + i);
+  const int start = load_int(W.starts + i), end = load_int(W.starts + i + 1), len = max(0, load_int(W.lens + i));
   const uint32_t has = __ballot_sync(0xffffffffu, lo + lane <= hi && lo + lane < W.d.seqs && start <= row && end > row);
-  // (sequences up to hi: with 32 in between, hi itself has a thread of its own only if there are fewer)
+  // (it is one of lo .. hi; where 32 lie before hi, hi itself has no thread and is looked at by all)
   if (has == 0u) {
     if (hi - lo < 32 || hi >= W.d.seqs) return false;
     const int s = load_int(W.starts + hi), e = load_int(W.starts + hi + 1);
     b = hi;
-    place = load_int(W.lens + hi) - (e - row);
+    place = max(0, load_int(W.lens + hi)) - (e - row);
     return s <= row && e > row;
   }
   const int who = __ffs((int)has) - 1;

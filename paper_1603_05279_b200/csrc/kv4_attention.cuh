@@ -12,6 +12,9 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 8.0f;
 constexpr int kLift = 7;
 
+// (a wait that gave up is the graver: that is written over this, and this not over that)
+__device__ __forceinline__ void record_bounds(int *status) { atomicCAS(status, 0, (int)XNOR_ERR_BOUNDS); }
+
 struct Sequence;
 // How a call's rows are cut: tiles of `rows` queries of a head's group, units of `tokens`; of sequences with more than
 // `least` and at most `most` rows.
@@ -35,7 +38,7 @@ struct Sequence {
     const long long r = (long long)n * T.group;
     if (r <= T.least || r > T.most) n = 0;
     len = (int)min((long long)max(0, all), (long long)W.d.table_cols * W.d.page);
-    lead = all - end;
+    lead = max(0, all) - end;
     cut = n > 0 && all > len;
     tiles = n > 0 ? (int)((r + T.rows - 1) / T.rows) : 0;
     units = max(1, (len + T.tokens - 1) / T.tokens);
@@ -50,7 +53,7 @@ __device__ __forceinline__ void Tiling::check_lengths(const Kv4Where &W, int lan
     s.load(W, *this, b);
     cut = cut || s.cut;
   }
-  if (cut) atomicMax(status, (int)XNOR_ERR_BOUNDS);
+  if (cut) record_bounds(status);
 }
 
 __device__ __forceinline__ float exp2_fast(float x) {

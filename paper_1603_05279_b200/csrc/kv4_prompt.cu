@@ -175,14 +175,9 @@ __device__ __forceinline__ void copy_role(const Block &B, int lane) {
     const uint32_t slot = (uint32_t)i % kRawStages, parity = (uint32_t)(i / kRawStages) & 1u, full = B.smem + L::kRawFull + 8u * slot;
     const long long now = next;
     next = find(t + 1);
-    if (!wait_warp(B, B.smem + L::kRawEmpty + 8u * slot, parity ^ 1u)) {
-      // gave up: copies in flight must land before the block's shared memory is released
-      const long long t0 = clock64();
-      while (clock64() - t0 < (1 << 20)) {}
-      return;
-    }
+    if (!wait_warp(B, B.smem + L::kRawEmpty + 8u * slot, parity ^ 1u)) return;
     const uint32_t there = __ballot_sync(0xffffffffu, now >= 0);
-    if (now == -1) atomicMax(&g_status_kv4_prompt, (int)XNOR_ERR_BOUNDS);
+    if (now == -1) record_bounds(&g_status_kv4_prompt);
     if (lane == 0) {
       sts32(B.smem + L::kMask + 4u * slot, there);
       mbar_arrive_expect_tx(full, (uint32_t)__popc(there) * kv4_record(kDim));
@@ -330,8 +325,7 @@ __device__ __forceinline__ void value_role(const Block &B, int id) {
 __device__ __forceinline__ uint64_t swizzled_desc(uint32_t addr) {
   return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
-// The whole warp runs the loop, and one thread issues: so what the instructions take stays in uniform registers.  (Run by one thread
-// alone, each product cost it 60 cycles, as many as the tensor core.)
+// The whole warp runs the loop, and one thread issues: so the warp's waits and fences need no second meeting.
 __device__ __forceinline__ void mma_shared(uint32_t leader, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
@@ -472,7 +466,8 @@ __device__ __forceinline__ float2 lds_float2(uint32_t addr) {
 // The weights of a step, against the rows' maxima m: p = exp2(s ks - m) times the values' scales, as pairs of F16; their sums before
 // that; and the largest s ks - m, each of this thread's columns (2 t and 2 t + 1 of eight, of rows g, g + 8, g + 16 and g + 24 of 32;
 // scales: theirs).  kMasked: columns from `seen` on (counted from 2 t) are not seen, nor are records that are
-// missing; and s ks is rounded before m is taken from it, so that the maximum itself gives 0 whatever its size.
+// missing; and s ks is rounded before m is taken from it, and the largest s ks itself is given, so that as the
+// maximum it gives a weight of 1 whatever its size.
 struct Scales { float2 k[kStep / 8], v[kStep / 8]; };
 template <bool kMasked>
 __device__ __forceinline__ void weigh(uint32_t S, const Scales &scales, const float (&m)[4], const int (&seen)[4], uint32_t there, uint32_t (&p)[2][16],
@@ -503,13 +498,15 @@ __device__ __forceinline__ void weigh(uint32_t S, const Scales &scales, const fl
         float2 u = make_float2(__uint_as_float(x[0]), __uint_as_float(x[1]));
         const int end = !kMasked ? 0 : (there >> (column / kKvTokens) & 1u) ? seen[r] : INT_MIN;
         if (kMasked) {
-          u = make_float2(__fadd_rn(__fmul_rn(u.x, f.x), -m[r]), __fadd_rn(__fmul_rn(u.y, f.y), -m[r]));
+          u = mul2(u, f);
           if (column >= end) u.x = -INFINITY;
           if (column + 1 >= end) u.y = -INFINITY;
+          top[r] = fmaxf(fmaxf(u.x, u.y), top[r]);
+          u = add2(u, make_float2(-m[r], -m[r]));
         } else {
           u = fma2(u, f, make_float2(-m[r], -m[r]));
+          top[r] = fmaxf(fmaxf(u.x, u.y), top[r]);
         }
-        top[r] = fmaxf(fmaxf(u.x, u.y), top[r]);
         u = make_float2(exp2_fast(u.x), exp2_fast(u.y));
         sums[r] = add2(sums[r], u);
         u = mul2(u, g);
@@ -608,8 +605,7 @@ __device__ __forceinline__ void softmax_role(const Block &B, int half, int quart
       good = !__any_sync(0xffffffffu, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) > kRaise);
     }
     if (!good) {
-      // What is masked, and where a maximum is left too far behind: that is raised, and the step weighed again (once; where numbers are so
-      // large that rounding moves the maximum again, once more).
+      // What is masked, and where a maximum is left too far behind: that is raised, and the step weighed once more.
 #pragma unroll 1
       for (int attempt = 0;; ++attempt) {
         int seen[4];
@@ -621,9 +617,9 @@ __device__ __forceinline__ void softmax_role(const Block &B, int half, int quart
         for (int j = 0; j < 4; ++j) {
 #pragma unroll
           for (int x = 1; x < 4; x *= 2) top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], x));
-          if (unset >> j & 1 ? top[j] > -INFINITY : top[j] > kRaise) up |= 1 << j;
+          if (top[j] > (unset >> j & 1 ? -INFINITY : m[j] + kRaise)) up |= 1 << j;
         }
-        const bool again = attempt < 3 && __any_sync(0xffffffffu, up != 0);
+        const bool again = attempt == 0 && __any_sync(0xffffffffu, up != 0);
         if (!again && e_now == e) break;
         const float down = power_of_two(e - e_now);
         float f[4];
@@ -632,9 +628,8 @@ __device__ __forceinline__ void softmax_role(const Block &B, int half, int quart
         for (int j = 0; j < 4; ++j) {
           f[j] = 1.0f;
           if (again && (up >> j & 1)) {
-            const float above = m[j] + top[j];
-            f[j] = unset >> j & 1 ? 0.0f : exp2_fast(m[j] - above);
-            m[j] = above;
+            f[j] = unset >> j & 1 ? 0.0f : exp2_fast(m[j] - top[j]);
+            m[j] = top[j];
           }
           l[j] *= f[j];
           f[j] *= down;
@@ -817,6 +812,12 @@ kv4_prompt_kernel(const __grid_constant__ Params P) {
   }
   tc_fence_before();
   __syncthreads();
+  if (*abort_flag != 0) {
+    // gave up: copies and products in flight must land before the block's memory is released
+    const long long t0 = clock64();
+    while (clock64() - t0 < (1 << 20)) {}
+    __syncthreads();
+  }
   if (warp == kMmaWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(*tmem_slot), "r"(512u) : "memory");
 }
@@ -892,14 +893,21 @@ cudaError_t run(const Kv4Args &a, int least_rows, cudaStream_t st) {
 template <class T>
 cudaError_t run_type(const Kv4Args &a, int least_rows, cudaStream_t st) { return a.w.d.dim == 64 ? run<T, 64>(a, least_rows, st) : run<T, 128>(a, least_rows, st); }
 
-// From how many rows of a sequence on the tensor cores take it.
-constexpr int kFewRows = 64;
+// Up to how many rows of a sequence (new tokens x queries of a head) the kernel for few takes it: that one reads the context once
+// for every 16 rows, this one once for 256.  us for 16, 32, 64, 96, 128 rows of every head, few against this, dim 128:
+//   64 sequences of 4000 tokens, 8 heads   139 259 502 746 988   315 317 323 328 333
+//   16 of 2000, 8 heads                     29  46  82 115 148    51  52  51  52  52
+//   3 of 8000, 8 heads                      25  34  52  70  93    45  46  47  56  57     (blocks share an item)
+//   1 of 4000, 8 heads                      19  19  22  25  28    23  23  24  25  26
+//   4 of 1000, 4 heads                      17  17  19  21  23    27  27  29  30  30
+int few_rows(const xnor_kv4_desc &d) { return (long long)d.seqs * d.kv_heads > 16 ? 32 : 96; }
 
 }  // namespace
 
 size_t kv4_prompt_work_bytes(const xnor_kv4_desc &d, const xnor_kv4_rows &r) {
-  const Plan p = plan(d, r);
-  return p.splits == 1 ? 0 : (size_t)(p.items * d.kv_heads * p.splits) * kItemRows * (d.dim + 2) * sizeof(float);
+  // (enough for any call of fewer rows too: where blocks share items, they are no more than there are SMs)
+  const long long blocks = std::min<long long>(kSms, plan(d, r).items * d.kv_heads * kMaxSplits);
+  return (size_t)blocks * kItemRows * (d.dim + 2) * sizeof(float);
 }
 
 cudaError_t launch_kv4_prompt(const Kv4Args &a, int least_rows, cudaStream_t st) {
@@ -918,15 +926,16 @@ cudaError_t read_status_kv4_prompt(int *status) {
 // Sequences of few rows go to one kernel, those of many to the other; which there are, only the device knows, but no
 // sequence has more than `most`, and one alone may have any number.
 size_t kv4_work_bytes(const xnor_kv4_desc &d, const xnor_kv4_rows &r) {
-  return std::max(kv4_few_work_bytes(d, r), kv4_most_rows(d, r) > kFewRows ? kv4_prompt_work_bytes(d, r) : 0);
+  return std::max(kv4_few_work_bytes(d, r), kv4_most_rows(d, r) > few_rows(d) ? kv4_prompt_work_bytes(d, r) : 0);
 }
 
 cudaError_t launch_kv4_attention(const Kv4Args &a, cudaStream_t st) {
   if (a.r.rows == 0) return cudaSuccess;
-  if (kv4_most_rows(a.w.d, a.r) <= kFewRows) return launch_kv4_few(a, INT_MAX, st);
+  const int few = few_rows(a.w.d);
+  if (kv4_most_rows(a.w.d, a.r) <= few) return launch_kv4_few(a, INT_MAX, st);
   if (a.w.d.seqs == 1) return launch_kv4_prompt(a, 0, st);
-  const cudaError_t e = launch_kv4_few(a, kFewRows, st);
-  return e == cudaSuccess ? launch_kv4_prompt(a, kFewRows, st) : e;
+  const cudaError_t e = launch_kv4_few(a, few, st);
+  return e == cudaSuccess ? launch_kv4_prompt(a, few, st) : e;
 }
 
 }  // namespace xnor

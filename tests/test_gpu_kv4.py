@@ -19,6 +19,8 @@ CASES = [
     ([2, 40, 0, 9], [5, 3, 2, 9], 3, 2, 64, 16, 64, False, True, "f32"),      # more rows than tokens
     ([1000], [1000], 1, 8, 128, 256, 128, True, True, "f16"),
     ([30] * 70, [1, 2] * 35, 2, 1, 64, 16, 16, False, True, "bf16"),
+    ([3] * 33, [1] * 33, 1, 1, 64, 16, 16, False, True, "bf16"),              # how sequences are found: 32 at a time
+    ([2] * 1100, [1, 0, 2, 0] * 275, 1, 1, 64, 16, 16, False, True, "f16"),
 ]
 
 

@@ -4,8 +4,8 @@ import torch
 
 import paper_1603_05279_b200 as X
 from paper_1603_05279_b200 import binding as B
-from kv4_util import TYPES, Batch, attention64
-from rows_util import Guards, gen, randn
+from kv4_util import TYPES, Batch, attention64, put, quantized
+from rows_util import Guards, U, gen, half_step, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -177,3 +177,60 @@ def test_sequences_that_share_pages():
     batch.table[1, :10] = batch.table[0, :10]
     q = randn((2, 4, 64), gen(63), torch.bfloat16)
     check(batch, q, 0.2, *run(batch, q, 0.2, 1))
+
+
+@pytest.mark.parametrize("new,most", [(3, 3), (150, 150)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_logits_of_any_size(new, most, D):
+    """Keys of 10^30, and the largest of them ever later: a row is then the value of one token."""
+    L, H, G = 700, 2, 2
+    for rising in (False, True):
+        batch = Batch([L], [new], H, D, 16, 71).fill(72)
+        words = batch.cache[..., 16 * D:].view(torch.int32)
+        page, slot = batch.place(0, torch.arange(L, device="cuda"))
+        size = 1e30 * (1 + torch.arange(L, device="cuda")) ** 2 if rising else torch.full((L,), 1e30, device="cuda")
+        words[page, :, slot // 16, slot % 16] = (size.float().view(torch.int32) & ~15)[:, None] | (words[page, :, slot // 16, slot % 16] & 15)
+        q = randn((new, H * G, D), gen(73), torch.bfloat16)
+        out, lse = run(batch, q, 0.1, most)
+        assert out.isfinite().all() and lse.isfinite().all()
+        K, V = batch.read64(0)
+        S = 0.1 * torch.einsum("nhgd,lhd->nhgl", q.double().unflatten(1, (H, G)), K)
+        mass = 0.1 * torch.einsum("nhgd,lhd->nhgl", q.double().abs().unflatten(1, (H, G)), K.abs())
+        hidden = torch.arange(L, device="cuda") > torch.arange(L - new, L, device="cuda")[:, None]
+        S = S.masked_fill(hidden[:, None, None], -float("inf"))
+        two, at = S.topk(2, -1)
+        # a logit's products and sums are off by (2 D + 5) U of their magnitudes' sum: where the first is ahead by more than both are off, and 100
+        clear = two[..., 0] - two[..., 1] > 100 + 2 * (2 * D + 5) * U * mass.masked_fill(hidden[:, None, None], 0.0).amax(-1)
+        assert clear.float().mean() > 0.9
+        want = V[at[..., 0], torch.arange(H, device="cuda")[:, None]]                 # [new][H][G][D]
+        # a weight of 1 (the rest together below 700 e^-100) times the scale, to 11 bits: off by 2^-11
+        off = want.abs() * (2.0 ** -11 + 64 * U)
+        off = off + half_step(torch.bfloat16) * (want.abs() + off)
+        assert ((out.double().unflatten(1, (H, G)) - want).abs() <= off)[clear].all()
+        assert ((lse.double().unflatten(1, (H, G)) - two[..., 0]).abs() <= (2 * D + 10) * U * mass.masked_fill(hidden[:, None, None], 0.0).amax(-1)).all()
+
+
+@pytest.mark.parametrize("new,most", [(4, 4), (150, 150)])
+def test_queries_of_a_wide_range(new, most):
+    """bfloat16 queries with values 2^26 apart, the large ones where all keys are zero; rows of very small ones."""
+    batch, D, H = Batch([300], [new], 2, 64, 16, 81).fill(82), 64, 2
+    page, slot = batch.place(0, torch.arange(300, device="cuda"))
+    x = randn((300, H, D), gen(83))
+    x[..., 5] = x[..., 40] = 0
+    put(batch.cache, D, False, page, slot, *quantized(x))
+    q = randn((new, 4, D), gen(84), torch.bfloat16)
+    q[0] *= 2.0 ** -60
+    q[1] *= 2.0 ** -126
+    q[..., 5] = 2.0 ** 20
+    q[2:, :, 40] = -1.5 * 2.0 ** 26
+    q[1, :, 5] = 0
+    check(batch, q, 0.3, *run(batch, q, 0.3, most))
+
+
+@pytest.mark.parametrize("seqs,heads", [(3, 2), (40, 4)])
+def test_sequences_of_all_sizes_in_one_call(seqs, heads):
+    """Some of a batch's sequences have few new tokens, some many, on both sides of where the kernels meet."""
+    new = [(1, 130, 16, 47, 33, 48, 0, 17, 49)[i % 9] for i in range(seqs)]
+    batch = Batch([n + 150 - 3 * i for i, n in enumerate(new)], new, heads, 64, 16, 91).fill(92)
+    q = randn((batch.T, 2 * heads, 64), gen(93), torch.float16)
+    check(batch, q, 0.2, *run(batch, q, 0.2, 0))

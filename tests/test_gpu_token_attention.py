@@ -1,5 +1,6 @@
 """A decoder's layer in a run of calls: projection, norms and rotation, cache, attention, projection; graphs, streams and threads."""
 import threading
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -201,3 +202,13 @@ def test_gradients_through_a_run():
     torch.cuda.synchronize()
     assert all(torch.equal(t, e) for t, e in zip((b, dx, *dw), eager))
     X.xnor_check_device()
+
+
+def test_room_for_many_rows_is_room_for_few():
+    """A layer made for prompts of thousands of tokens gets one of 200, whose context is shared by many blocks."""
+    A = TokenAttention(5000, 2, 5200, 8, 8, 64, page=16)
+    A.grow(torch.tensor([200, 1], dtype=torch.int32, device="cuda"))
+    qkv = randn((201, 24 * 64), gen(3), torch.bfloat16)
+    A.forward(qkv)
+    X.xnor_check_device()
+    check_attention(SimpleNamespace(attention=A, qkv=SimpleNamespace(out=qkv)), [200, 1], [200, 1])

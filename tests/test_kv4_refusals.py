@@ -83,7 +83,7 @@ def test_cache():
 
     for kw in (dict(pages=0), dict(page=8), dict(page=24), dict(kv_heads=0), dict(dim=0), dict(seqs=0), dict(table_cols=0)):
         assert a(heads(), kv4(**kw)) == INV and r(kv4(**kw)) == INV and m(kv4(**kw), rows()) == INV, kw
-    for kw in (dict(page=65552), dict(seqs=(1 << 20) + 1)):
+    for kw in (dict(page=65552), dict(seqs=(1 << 20) + 1), dict(page=32768, table_cols=65536), dict(page=16, table_cols=(1 << 27) - 15)):
         assert a(heads(), kv4(**kw)) == UNS and r(kv4(**kw)) == UNS and m(kv4(**kw), rows()) == UNS, kw
     assert a(heads(dim=96, rot=64, q_stride=400, k_stride=400, q_out_stride=400), kv4(dim=96)) == UNS
     assert r(kv4(dim=96), ks=192, vs=192) == UNS and m(kv4(dim=96), rows(q_stride=400, out_stride=400)) == UNS
@@ -107,6 +107,21 @@ def test_cache():
     assert m(kv4(), rows(type=B.XNOR_F32)) == UNS and m(kv4(), rows(rows=(1 << 24) + 1)) == UNS
     assert m(kv4(), rows(rows=1 << 20, q_heads=2048, q_stride=1 << 17, out_stride=1 << 17)) == UNS
     assert m(kv4(), rows(rows=0), q=NULL, o=NULL, w=NULL) == OK
+
+
+def test_scratch_of_a_call_is_enough_for_smaller_ones():
+    for heads, kv_heads, dim in ((32, 8, 128), (4, 4, 64), (64, 1, 128), (7, 1, 64)):
+        d, most_bytes = X.make_kv4_desc(64, 64, kv_heads, dim), {}
+        for seqs in (1, 2, 3, 18, 64, 1000):
+            for most in (1, 2, 9, 40, 100, 1000, 0):
+                before = 0
+                for rows in (1, 2, 3, 8, 9, 33, 64, 65, 100, 129, 257, 600, 1025, 4096, 40000):
+                    n = X.xnor_kv4_work_bytes(d, rows, heads, seqs, most)
+                    key = (rows, most if most else 1 << 30)
+                    assert n >= before and all(n >= v for (r, m), v in most_bytes.items() if r <= key[0] and m <= key[1])
+                    before = most_bytes[key] = max(n, most_bytes.get(key, 0))
+    sizes = [X.xnor_qk_work_elems(rows, 32, 8, 128) for rows in range(1, 3000)]
+    assert sizes == sorted(sizes)
 
 
 def test_the_binding_checks_tensors_against_each_other():
