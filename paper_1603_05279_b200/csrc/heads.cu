@@ -30,64 +30,38 @@ __device__ __forceinline__ bool angles_of(const HeadsArgs &A, int t, const float
 // parts-th unit, the next one's values under way.  Few tokens are shared by many warps.
 template <class T, int kDim>
 struct HeadUnits {
-  using Lane = HeadLane<kDim>;
   int q_units, units;
   __device__ __forceinline__ explicit HeadUnits(const xnor_heads_desc &d)
-      : q_units((d.q_heads + Lane::kHeads - 1) / Lane::kHeads), units(q_units + (d.k_heads + Lane::kHeads - 1) / Lane::kHeads) {}
-  __device__ __forceinline__ bool keys(int u) const { return u >= q_units; }
-  // This thread's head of unit u; -1: none.
-  __device__ __forceinline__ int head(const xnor_heads_desc &d, const Lane &lane, int u) const {
-    const int h = (keys(u) ? u - q_units : u) * Lane::kHeads + lane.sub;
-    return u < units && h < (keys(u) ? d.k_heads : d.q_heads) ? h : -1;
-  }
-};
-
-template <class T>
-struct TwoChunks {
-  Chunk<T> a, b;
-  template <class Lane>
-  __device__ __forceinline__ void load(const T *head, const Lane &lane, bool in) {
-    a.load(head + lane.a, true, in ? 8 : 0);
-    b.load(head + lane.b, true, in ? 8 : 0);
-  }
-  template <class Lane>
-  __device__ __forceinline__ void store(T *head, const Lane &lane) const {
-    a.store(head + lane.a, true, 8);
-    b.store(head + lane.b, true, 8);
-  }
-  __device__ __forceinline__ void to_float(float (&v)[16]) const {
-    a.to_float(*reinterpret_cast<float (*)[8]>(v));
-    b.to_float(*reinterpret_cast<float (*)[8]>(v + 8));
-  }
-  __device__ __forceinline__ void from_float(const float (&v)[16]) {
-    a.from_float(*reinterpret_cast<const float (*)[8]>(v));
-    b.from_float(*reinterpret_cast<const float (*)[8]>(v + 8));
-  }
+      : q_units((d.q_heads + HeadLane<kDim>::kHeads - 1) / HeadLane<kDim>::kHeads), units(q_units + (d.k_heads + HeadLane<kDim>::kHeads - 1) / HeadLane<kDim>::kHeads) {}
 };
 
 template <class T, int kDim, bool kPairs>
-__global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 4 ? 2 : 3)
+__global__ void __launch_bounds__(32 * kWarps, 2)
 heads_kernel(const HeadsArgs A, int parts) {
-  const HeadLane<kDim> lane(threadIdx.x & 31, A.d.rot, kPairs);
+  using Lane = HeadLane<kDim>;
+  const Lane lane(threadIdx.x & 31, A.d.rot, kPairs);
   const HeadUnits<T, kDim> U(A.d);
   const bool f32 = A.d.weight_type == XNOR_F32;
-  const long long items = (long long)A.d.rows * parts;
+  const int items = A.d.rows * parts, step = parts * Lane::kHeads;
   stream_order();
-  for (long long item = (long long)blockIdx.x * kWarps + threadIdx.x / 32; item < items; item += (long long)gridDim.x * kWarps) {
-    const int t = (int)(item / parts);
+  for (int item = (int)blockIdx.x * kWarps + (int)threadIdx.x / 32; item < items; item += (int)gridDim.x * kWarps) {
+    const int t = item / parts, first = item - t * parts;
+    const int first_k = first >= U.q_units ? first - U.q_units : (parts - (U.q_units - first) % parts) % parts;      // its first unit of keys
+    const T *q = static_cast<const T *>(A.q) + t * A.d.q_stride, *k = static_cast<const T *>(A.k) + t * A.d.k_stride;
+    if (A.d.q_heads == 0) q = k;                             // (read, but not used)
+    if (A.d.k_heads == 0) k = q;
+    auto fetch = [&](const T *from, int heads, int h, TwoChunks<T> &x) { x.load(from + (h < heads ? h : 0) * kDim, lane); };
+    // the first units are under way while the token's angles are looked up
+    TwoChunks<T> x_q, x_k;
+    fetch(q, A.d.q_heads, first * Lane::kHeads + lane.sub, x_q);
+    fetch(k, A.d.k_heads, first_k * Lane::kHeads + lane.sub, x_k);
     const float *row;
     if (!angles_of(A, t, row)) continue;
-    const T *q = static_cast<const T *>(A.q) + t * A.d.q_stride, *k = static_cast<const T *>(A.k) + t * A.d.k_stride;
-    T *q_out = static_cast<T *>(A.q_out) + t * A.d.q_out_stride, *k_out = static_cast<T *>(A.k_out) + t * A.d.k_out_stride;
     Angles angles;
-    // units of one kind, `first`, first + parts, ..: their weights stay in registers
-    auto run = [&](int first, int units, int heads, const T *from, T *to, const void *weight, bool start) {
+    if (lane.turns) angles.load(row, A.d.rot, lane.which);
+    // units of one kind, `first`, first + parts, ..: their weights stay in registers, the next one's values are under way
+    auto run = [&](int first, int units, int heads, const T *from, T *to, const void *weight, TwoChunks<T> &x) {
       if (first >= units) return;
-      const int step = parts * HeadLane<kDim>::kHeads;
-      int h = first * HeadLane<kDim>::kHeads + lane.sub;
-      TwoChunks<T> x, y;
-      x.load(from + h * kDim, lane, h < heads);
-      if (start && lane.turns) angles.load(row, A.d.rot, lane.which);
       float w[16];
       if (A.d.norm) {
         load_head_weights<T>(weight, f32, lane.a, w);
@@ -108,19 +82,19 @@ heads_kernel(const HeadsArgs A, int parts) {
         x.from_float(v);
         if (h < heads) x.store(to + h * kDim, lane);
       };
+      TwoChunks<T> y;
+      int h = first * Lane::kHeads + lane.sub;
 #pragma unroll 1
       for (int u = first; u < units; u += 2 * parts, h += 2 * step) {
-        y.load(from + (h + step) * kDim, lane, u + parts < units && h + step < heads);
+        fetch(from, heads, h + step, y);
         finish(h, x);
         if (u + parts >= units) break;
-        x.load(from + (h + 2 * step) * kDim, lane, u + 2 * parts < units && h + 2 * step < heads);
+        fetch(from, heads, h + 2 * step, x);
         finish(h + step, y);
       }
     };
-    const int first = (int)(item % parts);
-    run(first, U.q_units, A.d.q_heads, q, q_out, A.q_weight, true);
-    const int later = first >= U.q_units ? first - U.q_units : (first - U.q_units % parts + parts) % parts;      // its first unit of keys
-    run(later, U.units - U.q_units, A.d.k_heads, k, k_out, A.k_weight, first >= U.q_units);
+    run(first, U.q_units, A.d.q_heads, q, static_cast<T *>(A.q_out) + t * A.d.q_out_stride, A.q_weight, x_q);
+    run(first_k, U.units - U.q_units, A.d.k_heads, k, static_cast<T *>(A.k_out) + t * A.d.k_out_stride, A.k_weight, x_k);
   }
 }
 
@@ -161,20 +135,20 @@ heads_backward_kernel(const HeadsArgs A, int q_blocks) {
   load_head_weights<T>(weight, A.d.weight_type == XNOR_F32, lane.a, w);
   load_head_weights<T>(weight, A.d.weight_type == XNOR_F32, lane.b, w + 8);
   for (long long item = (long long)I.block * kWarps + threadIdx.x / 32; item < I.items; item += (long long)I.blocks * kWarps) {
-    const int t = (int)(item / I.per_token);
+    const int t = (int)divide(item, I.per_token);
     const float *row;
     if (!angles_of(A, t, row)) continue;
     const T *x_row = x_all + t * x_stride, *dy_row = dy_all + t * dy_stride;
     T *dx_row = dx_all + t * dx_stride;
-    const int h0 = (int)(item % I.per_token) * kBackwardEach * Lane::kHeads + lane.sub;
+    const int h0 = (int)(item - (long long)t * I.per_token) * kBackwardEach * Lane::kHeads + lane.sub;
     auto fetch = [&](int i, TwoChunks<T> &x, TwoChunks<T> &dy) {
       const int h = h0 + i * Lane::kHeads;
-      const bool in = i < kBackwardEach && h < I.heads;
-      x.load(x_row + (in ? h : 0) * kDim, lane, in);
-      dy.load(dy_row + (in ? h : 0) * kDim, lane, in);
+      x.load(x_row + (h < I.heads ? h : 0) * kDim, lane);
+      dy.load(dy_row + (h < I.heads ? h : 0) * kDim, lane);
     };
     Angles angles;
     auto finish = [&](int i, const TwoChunks<T> &xc, TwoChunks<T> &yc) {
+      const int h = h0 + i * Lane::kHeads;
       float x[16], g[16];
       yc.to_float(g);
       if (lane.turns) turn<kPairs, -1>(g, angles);
@@ -186,15 +160,14 @@ heads_backward_kernel(const HeadsArgs A, int q_blocks) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) dot = fmaf(g[j] * w[j], x[j], dot);
         const float r = __frsqrt_rn(lane.sum(s) * (1.0f / kDim) + A.d.eps);
-        const float k = lane.sum(dot) * (r * r * (1.0f / kDim));
+        const float k = lane.sum(dot) * (r * r * (1.0f / kDim)), once = h < I.heads ? r : 0.0f;
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          dw[j] = fmaf(g[j] * r, x[j], dw[j]);
+          dw[j] = fmaf(g[j] * once, x[j], dw[j]);
           g[j] = r * fmaf(-x[j], k, g[j] * w[j]);
         }
       }
       yc.from_float(g);
-      const int h = h0 + i * Lane::kHeads;
       if (h < I.heads) yc.store(dx_row + h * kDim, lane);
     };
     TwoChunks<T> x0, y0, x1, y1;
@@ -205,6 +178,7 @@ heads_backward_kernel(const HeadsArgs A, int q_blocks) {
       fetch(i + 1, x1, y1);
       finish(i, x0, y0);
       if (i + 2 < kBackwardEach) fetch(i + 2, x0, y0);
+      if (h0 - lane.sub + (i + 1) * Lane::kHeads >= I.heads) break;
       finish(i + 1, x1, y1);
     }
   }

@@ -32,6 +32,11 @@ cudaError_t read_status_heads(int *status);
 // that 16-byte pieces can be read.
 inline bool heads_in_chunks(const xnor_heads_desc &d) { return (d.dim == 64 || d.dim == 128 || d.dim == 256) && d.rot % 16 == 0; }
 
+// a / b of numbers that are not negative, for the most part below 2^32 (in 64 bits it takes 100 instructions).
+__device__ __forceinline__ long long divide(long long a, long long b) {
+  return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 template <int kDim>
 struct HeadLane {
   static constexpr int kLanes = kDim / 16, kHeads = 32 / kLanes;      // threads of a head, heads of a warp
@@ -53,6 +58,31 @@ struct HeadLane {
 #pragma unroll
     for (int o = kLanes / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
+  }
+};
+
+// A thread's values of a head.  Loads have no condition, so that nothing waits for them before their values are used: what
+// does not exist is read elsewhere.
+template <class T>
+struct TwoChunks {
+  Chunk<T> a, b;
+  template <bool kPieces = true, class Lane>
+  __device__ __forceinline__ void load(const T *head, const Lane &lane) {
+    a.load(head + lane.a, kPieces, 8);
+    b.load(head + lane.b, kPieces, 8);
+  }
+  template <bool kPieces = true, class Lane>
+  __device__ __forceinline__ void store(T *head, const Lane &lane) const {
+    a.store(head + lane.a, kPieces, 8);
+    b.store(head + lane.b, kPieces, 8);
+  }
+  __device__ __forceinline__ void to_float(float (&v)[16]) const {
+    a.to_float(*reinterpret_cast<float (*)[8]>(v));
+    b.to_float(*reinterpret_cast<float (*)[8]>(v + 8));
+  }
+  __device__ __forceinline__ void from_float(const float (&v)[16]) {
+    a.from_float(*reinterpret_cast<const float (*)[8]>(v));
+    b.from_float(*reinterpret_cast<const float (*)[8]>(v + 8));
   }
 };
 

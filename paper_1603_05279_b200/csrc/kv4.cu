@@ -55,36 +55,31 @@ __device__ __forceinline__ void store_codes(const float (&v)[16], const HeadLane
     *reinterpret_cast<uint32_t *>(record + kv4_words(kDim, values) + 4 * slot) = (odd == 0.0f ? bits : 0x7FFFFFF0u) | (uint32_t)z;
 }
 
-// As the kernel of norms and rotations (heads.cu): a warp has a token, and its units of queries, then of keys, then of values.
-template <class T, int kDim, bool kPairs>
+// As the kernel of norms and rotations (heads.cu): a warp has a token, and its units of queries, then of keys, then of values,
+// every parts-th of the three together.  The first of each kind are under way while the token's place is looked up.
+template <class T, int kDim, bool kPairs, bool kPieces>
 __global__ void __launch_bounds__(32 * kWarps, 2)
-kv4_append_kernel(const Kv4AppendArgs A, int parts, int pieces) {
+kv4_append_kernel(const Kv4AppendArgs A, int parts) {
   using Lane = HeadLane<kDim>;
   const xnor_heads_desc &d = A.h.d;
   const int id = threadIdx.x & 31;
   const Lane lane(id, d.rot, kPairs);
   const bool f32 = d.weight_type == XNOR_F32;
   const int q_units = (d.q_heads + Lane::kHeads - 1) / Lane::kHeads, k_units = (d.k_heads + Lane::kHeads - 1) / Lane::kHeads;
-  const int per_page = A.w.d.page / kKvTokens;
-  const long long items = (long long)d.rows * parts;
+  const int per_page = A.w.d.page / kKvTokens, step = parts * Lane::kHeads;
+  const int items = d.rows * parts;                          // (rows, or a few thousand)
   stream_order();
-  for (long long item = (long long)blockIdx.x * kWarps + threadIdx.x / 32; item < items; item += (long long)gridDim.x * kWarps) {
-    const int t = (int)(item / parts);
-    const T *q = static_cast<const T *>(A.h.q) + t * d.q_stride, *k = static_cast<const T *>(A.h.k) + t * d.k_stride;
-    const T *v_row = static_cast<const T *>(A.v) + t * d.v_stride;
-    auto kind_of = [&](int u) { return u < q_units ? 0 : u < q_units + k_units ? 1 : 2; };
-    auto head_of = [&](int u) { return (u < q_units ? u : u < q_units + k_units ? u - q_units : u - q_units - k_units) * Lane::kHeads + lane.sub; };
-    auto fetch = [&](int u, Chunk<T> &ca, Chunk<T> &cb) {
-      const int kind = kind_of(u), head = head_of(u);
-      const bool in = u < q_units + 2 * k_units && head < (kind == 0 ? d.q_heads : d.k_heads);
-      const T *from = (kind == 0 ? q : kind == 1 ? k : v_row) + (in ? head : 0) * kDim;
-      ca.load(from + lane.a, pieces, in ? 8 : 0);
-      cb.load(from + lane.b, pieces, in ? 8 : 0);
-    };
-    // (the first values are under way while the token's place is looked up, then the next ones while these are worked on)
-    const int first = (int)(item % parts);
-    Chunk<T> xa, xb, ya, yb;
-    fetch(first, xa, xb);
+  for (int item = (int)blockIdx.x * kWarps + (int)threadIdx.x / 32; item < items; item += (int)gridDim.x * kWarps) {
+    const int t = item / parts, first = item - t * parts;
+    const int first_k = first >= q_units ? first - q_units : (parts - (q_units - first) % parts) % parts;
+    const int first_v = first >= q_units + k_units ? first - q_units - k_units : (parts - (q_units + k_units - first) % parts) % parts;
+    const T *k = static_cast<const T *>(A.h.k) + t * d.k_stride, *v_row = static_cast<const T *>(A.v) + t * d.v_stride;
+    const T *q = d.q_heads > 0 ? static_cast<const T *>(A.h.q) + t * d.q_stride : k;      // (read, but not used)
+    auto fetch = [&](const T *from, int heads, int h, TwoChunks<T> &x) { x.template load<kPieces>(from + (h < heads ? h : 0) * kDim, lane); };
+    TwoChunks<T> x_q, x_k, x_v;
+    fetch(q, d.q_heads, first * Lane::kHeads + lane.sub, x_q);
+    fetch(k, d.k_heads, first_k * Lane::kHeads + lane.sub, x_k);
+    fetch(v_row, d.k_heads, first_v * Lane::kHeads + lane.sub, x_v);
     int b, place;
     if (!find_sequence(A.w, t, id, b, place) || place < 0) continue;
     const bool angles_there = d.rot == 0 || place < d.positions;
@@ -93,21 +88,31 @@ kv4_append_kernel(const Kv4AppendArgs A, int parts, int pieces) {
     const long long record = kv4_find(A.w, b, place / kKvTokens, 0);
     if ((record < 0 || !angles_there) && id == 0) atomicMax(&g_status_kv4, (int)XNOR_ERR_BOUNDS);
     if (!angles_there) continue;
-    T *q_out = static_cast<T *>(A.h.q_out) + t * d.q_out_stride;
-    auto finish = [&](int u, Chunk<T> &ca, Chunk<T> &cb) {
-      const int kind = kind_of(u), head = head_of(u);
-      if (kind > 0 && record < 0) return;
-      const bool in = head < (kind == 0 ? d.q_heads : d.k_heads);
-      float v[16];
-      ca.to_float(*reinterpret_cast<float (*)[8]>(v));
-      cb.to_float(*reinterpret_cast<float (*)[8]>(v + 8));
-      float w[16];
-      if (kind < 2 && d.norm) {
-        const void *weight = kind == 0 ? A.h.q_weight : A.h.k_weight;
-        load_head_weights<T>(weight, f32, lane.a, w);
-        load_head_weights<T>(weight, f32, lane.b, w + 8);
+    // units first, first + parts, .. of one kind, the next one's values under way
+    auto run = [&](const T *from, int units, int heads, int first, TwoChunks<T> &x, auto finish) {
+      TwoChunks<T> y;
+      int h = first * Lane::kHeads + lane.sub;
+#pragma unroll 1
+      for (int u = first; u < units; u += 2 * parts, h += 2 * step) {
+        fetch(from, heads, h + step, y);
+        finish(h, x);
+        if (u + parts >= units) break;
+        fetch(from, heads, h + 2 * step, x);
+        finish(h + step, y);
       }
-      if (kind == 0) {
+    };
+    float w[16];
+    auto weights = [&](const void *weight) {
+      if (!d.norm) return;
+      load_head_weights<T>(weight, f32, lane.a, w);
+      load_head_weights<T>(weight, f32, lane.b, w + 8);
+    };
+    if (first < q_units) {
+      T *q_out = static_cast<T *>(A.h.q_out) + t * d.q_out_stride;
+      weights(A.h.q_weight);
+      run(q, q_units, d.q_heads, first, x_q, [&](int h, TwoChunks<T> &x) {
+        float v[16];
+        x.to_float(v);
         if (d.norm) {
           float s = 0.0f;
 #pragma unroll
@@ -117,42 +122,42 @@ kv4_append_kernel(const Kv4AppendArgs A, int parts, int pieces) {
           for (int i = 0; i < 16; ++i) v[i] *= r * w[i];
         }
         if (lane.turns) turn<kPairs, 1>(v, angles);
-        ca.from_float(*reinterpret_cast<const float (*)[8]>(v));
-        cb.from_float(*reinterpret_cast<const float (*)[8]>(v + 8));
-        if (in) {
-          ca.store(q_out + head * kDim + lane.a, pieces, 8);
-          cb.store(q_out + head * kDim + lane.b, pieces, 8);
-        }
-        return;
-      }
-      if (kind == 1 && (d.norm || d.rot > 0)) {
-        // Keys in 64 bits: a code is that of the exact key, wherever it lies next to a border.
-        double x[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = (double)v[i];
-        if (d.norm) {
-          double s = 0.0;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s = fma(x[i], x[i], s);
-          const double r = 1.0 / sqrt(lane.sum(s) * (1.0 / kDim) + (double)d.eps);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) x[i] = x[i] * r * (double)w[i];
-        }
-        if (lane.turns) turn<kPairs, 1>(x, angles);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = (float)x[i];
-      }
-      uint8_t *to = A.cache + (size_t)(record + (long long)(in ? head : 0) * per_page) * kv4_record(kDim);
-      store_codes<kDim>(v, lane, to, place % kKvTokens, kind == 2, in);
-    };
-#pragma unroll 1
-    for (int u = first; u < q_units + 2 * k_units; u += 2 * parts) {
-      fetch(u + parts, ya, yb);
-      finish(u, xa, xb);
-      if (u + parts >= q_units + 2 * k_units) break;
-      fetch(u + 2 * parts, xa, xb);
-      finish(u + parts, ya, yb);
+        x.from_float(v);
+        if (h < d.q_heads) x.template store<kPieces>(q_out + h * kDim, lane);
+      });
     }
+    if (record < 0) continue;
+    auto record_of = [&](int h) { return A.cache + (size_t)(record + (long long)(h < d.k_heads ? h : 0) * per_page) * kv4_record(kDim); };
+    if (first_k < k_units) {
+      weights(A.h.k_weight);
+      run(k, k_units, d.k_heads, first_k, x_k, [&](int h, TwoChunks<T> &c) {
+        float v[16];
+        c.to_float(v);
+        if (d.norm || d.rot > 0) {
+          // Keys in 64 bits: a code is that of the exact key, wherever it lies next to a border.
+          double x[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[i] = (double)v[i];
+          if (d.norm) {
+            double s = 0.0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s = fma(x[i], x[i], s);
+            const double r = 1.0 / sqrt(lane.sum(s) * (1.0 / kDim) + (double)d.eps);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = x[i] * r * (double)w[i];
+          }
+          if (lane.turns) turn<kPairs, 1>(x, angles);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = (float)x[i];
+        }
+        store_codes<kDim>(v, lane, record_of(h), place % kKvTokens, false, h < d.k_heads);
+      });
+    }
+    run(v_row, k_units, d.k_heads, first_v, x_v, [&](int h, TwoChunks<T> &c) {
+      float v[16];
+      c.to_float(v);
+      store_codes<kDim>(v, lane, record_of(h), place % kKvTokens, true, h < d.k_heads);
+    });
   }
 }
 
@@ -164,10 +169,10 @@ kv4_read_kernel(const Kv4ReadArgs A, uint32_t magic, int parts, int pieces) {
   const int id = threadIdx.x & 31, heads = A.w.d.kv_heads, k_units = (heads + Lane::kHeads - 1) / Lane::kHeads;
   const Lane lane(id, 0, 0);
   const int per_page = A.w.d.page / kKvTokens;
-  const long long items = (long long)A.rows * parts;
+  const int items = A.rows * parts;
   stream_order();
-  for (long long item = (long long)blockIdx.x * kWarps + threadIdx.x / 32; item < items; item += (long long)gridDim.x * kWarps) {
-    const int t = (int)(item / parts);
+  for (int item = (int)blockIdx.x * kWarps + (int)threadIdx.x / 32; item < items; item += (int)gridDim.x * kWarps) {
+    const int t = item / parts;
     int b, place;
     if (!find_sequence(A.w, t, id, b, place) || place < 0) continue;
     const long long record = kv4_find(A.w, b, place / kKvTokens, 0);
@@ -176,7 +181,7 @@ kv4_read_kernel(const Kv4ReadArgs A, uint32_t magic, int parts, int pieces) {
       continue;
     }
     const int slot = place % kKvTokens;
-    for (int u = (int)(item % parts); u < 2 * k_units; u += parts) {
+    for (int u = item - t * parts; u < 2 * k_units; u += parts) {
       const bool values = u >= k_units;
       const int head = (values ? u - k_units : u) * Lane::kHeads + lane.sub;
       if (head >= heads) continue;
@@ -212,12 +217,13 @@ template <class T, int kDim>
 cudaError_t append(const Kv4AppendArgs &a, cudaStream_t st) {
   constexpr int kHeads = HeadLane<kDim>::kHeads;
   const xnor_heads_desc &d = a.h.d;
-  const int pieces = rows_in_pieces(a.h.q, d.q_stride, kDim, sizeof(T)) && rows_in_pieces(a.h.k, d.k_stride, kDim, sizeof(T)) &&
+  const bool pieces = rows_in_pieces(a.h.q, d.q_stride, kDim, sizeof(T)) && rows_in_pieces(a.h.k, d.k_stride, kDim, sizeof(T)) &&
                      rows_in_pieces(a.v, d.v_stride, kDim, sizeof(T)) && rows_in_pieces(a.h.q_out, d.q_out_stride, kDim, sizeof(T));
   const int parts = parts_for((d.q_heads + kHeads - 1) / kHeads + 2 * ((d.k_heads + kHeads - 1) / kHeads), d.rows);
   const dim3 grid(blocks_for((long long)d.rows * parts));
-  return d.pairs ? launch_kernel(kv4_append_kernel<T, kDim, true>, grid, 32 * kWarps, 0, st, 1, a, parts, pieces)
-                 : launch_kernel(kv4_append_kernel<T, kDim, false>, grid, 32 * kWarps, 0, st, 1, a, parts, pieces);
+  auto *kernel = d.pairs ? (pieces ? kv4_append_kernel<T, kDim, true, true> : kv4_append_kernel<T, kDim, true, false>)
+                         : (pieces ? kv4_append_kernel<T, kDim, false, true> : kv4_append_kernel<T, kDim, false, false>);
+  return launch_kernel(kernel, grid, 32 * kWarps, 0, st, 1, a, parts);
 }
 template <class T>
 cudaError_t append_type(const Kv4AppendArgs &a, cudaStream_t st) { return a.h.d.dim == 64 ? append<T, 64>(a, st) : append<T, 128>(a, st); }

@@ -58,8 +58,8 @@ struct Row {
     total = __shfl_sync(0xffffffffu, sum, 31);
     workers = max(1ll, min((long long)most, total / kLeastUnits));
   }
-  __device__ __forceinline__ long long first_of(long long worker) const { return worker * total / workers; }
-  __device__ __forceinline__ int worker_of(long long unit) const { return (int)(((unit + 1) * workers - 1) / total); }
+  __device__ __forceinline__ long long first_of(long long worker) const { return divide(worker * total, workers); }
+  __device__ __forceinline__ int worker_of(long long unit) const { return (int)divide((unit + 1) * workers - 1, total); }
   // The sum before sequence b; the same for all threads.
   __device__ __forceinline__ long long before_sequence(const Kv4Where &W, const Tiling &T, int b, int lane) const {
     long long v = before;
@@ -108,9 +108,9 @@ struct Place {
   int b, head, tile, rec;
   Sequence s;
   __device__ __forceinline__ void set(long long in_sequence) {
-    const long long item = in_sequence / s.units;
+    const long long item = divide(in_sequence, s.units);
     rec = (int)(in_sequence - item * s.units);
-    head = (int)(item / s.tiles);
+    head = (int)divide(item, s.tiles);
     tile = (int)(item - (long long)head * s.tiles);
   }
 };
@@ -610,9 +610,9 @@ template <class T, int kDim>
 __global__ void __launch_bounds__(32 * kJoinWarps)
 kv4_join_kernel(const Params P, int rows) {
   const int lane = threadIdx.x & 31;
-  const long long item = (long long)blockIdx.x * kJoinWarps + threadIdx.x / 32;
+  const uint32_t item = blockIdx.x * kJoinWarps + threadIdx.x / 32;        // (up to 2^30)
   stream_order();
-  const int token = (int)(item / P.A.r.q_heads), head = (int)(item % P.A.r.q_heads);
+  const int token = (int)(item / (uint32_t)P.A.r.q_heads), head = (int)(item % (uint32_t)P.A.r.q_heads);
   if (token >= P.A.r.rows) return;
   const Kv4Where &W = P.A.w;
   int b, place;
@@ -623,7 +623,7 @@ kv4_join_kernel(const Params P, int rows) {
   const Row row(W, P.T, lane, P.workers);
   const long long before = row.before_sequence(W, P.T, b, lane);
   const long long r = (long long)(token - s.start) * P.T.group + head % P.T.group;
-  const int tile = (int)(r / rows), at = (int)(r - (long long)tile * rows);
+  const int tile = (int)divide(r, rows), at = (int)(r - (long long)tile * rows);
   const long long u0 = before + ((long long)(head / P.T.group) * s.tiles + tile) * s.units;
   const int w0 = row.worker_of(u0), w1 = row.worker_of(u0 + s.units - 1);
   if (w0 == w1) return;

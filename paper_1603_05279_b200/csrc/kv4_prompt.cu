@@ -828,9 +828,9 @@ template <class T, int kDim>
 __global__ void __launch_bounds__(32 * kJoinWarps)
 kv4_prompt_join_kernel(const Params P) {
   const int lane = threadIdx.x & 31;
-  const long long item = (long long)blockIdx.x * kJoinWarps + threadIdx.x / 32;
+  const uint32_t item = blockIdx.x * kJoinWarps + threadIdx.x / 32;        // (up to 2^30)
   stream_order();
-  const int token = (int)(item / P.A.r.q_heads), head = (int)(item % P.A.r.q_heads), kv_head = head / P.T.group;
+  const int token = (int)(item / (uint32_t)P.A.r.q_heads), head = (int)(item % (uint32_t)P.A.r.q_heads), kv_head = head / P.T.group;
   if (token >= P.A.r.rows) return;
   int b, place;
   if (!find_sequence(P.A.w, token, lane, b, place)) return;
