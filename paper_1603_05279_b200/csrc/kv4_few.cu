@@ -37,62 +37,74 @@ constexpr int per_sm(int tiles) { return tiles == 1 ? 2 : 1; }          // block
 constexpr int kMaxWorkers = 2 * 160;         // blocks, at most (a B200 has 148 SMs)
 constexpr int kLeastUnits = 2 * kWarps;      // of a block's share
 
-// What the threads of a warp know of the row: each the sum over its own run of sequences, and the sum before them.
+// Shares are cut in a row in which an item has kEnd places more than units, before its first: its end, where the warps meet, and its
+// start take a block about as long as so many units.  us for 0, 10, 24, 36, 56: 64 sequences of 300 to 8192 tokens
+// 101 99 90.8 89.6 91.8; 16 of up to 1500, whole step, 26.4 23.1 22.2 22.4 23.3; one of 5000 17.1 15.4 15.3 15.5 15.6.
+constexpr int kEnd = 32;
+
+// What the threads of a warp know of the row: each the sums over its own run of sequences, and before them, of units and of places.
 struct Row {
   int per;                     // sequences of a thread
-  long long before, total;
+  long long before, total;     // units
+  long long places_before, places;
   long long workers;
   Sequence own;                // with one sequence a thread: that
+  __device__ __forceinline__ static long long places_of(const Sequence &s, int kv_heads) { return (long long)kv_heads * s.tiles * (s.units + kEnd); }
   __device__ __forceinline__ Row(const Kv4Where &W, const Tiling &T, int lane, int most) {
     per = (W.d.seqs + 31) / 32;
-    long long mine = 0;
+    long long mine = 0, my_places = 0;
 #pragma unroll 4
     for (int i = 0; i < per; ++i) {
       const int b = lane * per + i;
       if (b >= W.d.seqs) break;
       own.load(W, T, b);
       mine += own.all(W.d.kv_heads);
+      my_places += places_of(own, W.d.kv_heads);
     }
-    long long sum = mine;
+    long long sum = mine, place_sum = my_places;
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) {
-      const long long v = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += v;
+      const long long v = __shfl_up_sync(0xffffffffu, sum, o), w = __shfl_up_sync(0xffffffffu, place_sum, o);
+      if (lane >= o) { sum += v; place_sum += w; }
     }
     before = sum - mine;
     total = __shfl_sync(0xffffffffu, sum, 31);
+    places_before = place_sum - my_places;
+    places = __shfl_sync(0xffffffffu, place_sum, 31);
     workers = max(1ll, min((long long)most, total / kLeastUnits));
   }
-  __device__ __forceinline__ long long first_of(long long worker) const { return divide(worker * total, workers); }
-  __device__ __forceinline__ int worker_of(long long unit) const { return (int)divide((unit + 1) * workers - 1, total); }
-  // The sum before sequence b; the same for all threads.
-  __device__ __forceinline__ long long before_sequence(const Kv4Where &W, const Tiling &T, int b, int lane) const {
-    long long v = before;
+  __device__ __forceinline__ int worker_of(long long place) const { return (int)divide((place + 1) * workers - 1, places); }
+  // The places before sequence b; the same for all threads.
+  __device__ __forceinline__ long long places_before_sequence(const Kv4Where &W, const Tiling &T, int b, int lane) const {
+    long long v = places_before;
     if (per > 1 && lane == b / per)
       for (int i = lane * per; i < b; ++i) {
         Sequence s;
         s.load(W, T, i);
-        v += s.all(W.d.kv_heads);
+        v += places_of(s, W.d.kv_heads);
       }
     return __shfl_sync(0xffffffffu, v, b / per);
   }
-  // The sequence of a unit (below total), and the sum before it.
-  __device__ __forceinline__ int sequence_of(const Kv4Where &W, const Tiling &T, long long unit, int lane, long long &sum, Sequence &found) const {
-    const uint32_t later = __ballot_sync(0xffffffffu, before > unit);
-    const int owner = later == 0 ? 31 : __ffs((int)later) - 2;       // the last thread whose sum before it is no more
-    int b = lane;
-    long long v = before;
+  // The first unit of a worker's share (that worker's first place's, or the next one's that is a unit's), its sequence, and the units before that.
+  __device__ __forceinline__ long long first_of(const Kv4Where &W, const Tiling &T, long long worker, int lane, int &b, long long &sum, Sequence &found) const {
+    const long long place = divide(worker * places, workers);
+    const uint32_t later = __ballot_sync(0xffffffffu, places_before > place);
+    const int owner = later == 0 ? 31 : __ffs((int)later) - 2;       // the last thread with no more places before it
+    long long u = before, v = places_before;
+    b = lane;
     found = own;
     if (per > 1 && lane == owner) {
       for (b = lane * per; b + 1 < W.d.seqs; ++b) {
         Sequence s;
         s.load(W, T, b);
-        const long long u = s.all(W.d.kv_heads);
-        if (v + u > unit) break;
-        v += u;
+        const long long n = places_of(s, W.d.kv_heads);
+        if (v + n > place) break;
+        v += n;
+        u += s.all(W.d.kv_heads);
       }
     }
-    sum = __shfl_sync(0xffffffffu, v, owner);
+    sum = __shfl_sync(0xffffffffu, u, owner);
+    v = __shfl_sync(0xffffffffu, v, owner);
     b = __shfl_sync(0xffffffffu, b, owner);
     if (per > 1) {
       found.load(W, T, b);
@@ -104,7 +116,9 @@ struct Row {
       found.tiles = __shfl_sync(0xffffffffu, found.tiles, owner);
       found.units = __shfl_sync(0xffffffffu, found.units, owner);
     }
-    return b;
+    const int length = found.units + kEnd;
+    const long long item = divide(place - v, length);
+    return sum + item * found.units + max(0, (int)(place - v - item * length) - kEnd);
   }
 };
 
@@ -126,12 +140,12 @@ struct Layout {
   static constexpr uint32_t kRecord = kv4_record(kDim);
   static constexpr int kRows = 8 * kTiles;
   static constexpr int kSumRow = kDim + 4;                          // floats
-  static constexpr uint32_t kFull = 0, kEmpty = 8 * kStages, kValid = 16 * kStages, kAbort = kValid + 4 * kStages;
+  static constexpr uint32_t kFull = 0, kEmpty = 8 * kStages, kValid = 16 * kStages, kAbort = kValid + 4 * kStages, kRead = kAbort + 8;
   static constexpr uint32_t kStats = 1024;                          // [kWarps][kRows] maxima and sums
   static constexpr uint32_t kSums = kStats + 8 * kWarps * kRows;    // [kWarps][kRows][kSumRow]
   static constexpr uint32_t kRing = (kSums + 4u * kWarps * kRows * kSumRow + 127u) & ~127u;
   static constexpr uint32_t kBytes = kRing + kStages * kRecord;
-  static_assert(kAbort + 4 <= kStats, "control words");
+  static_assert(kRead % 8 == 0 && kRead + 8 <= kStats, "control words");
 };
 
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -272,6 +286,7 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
   p.s = s0;
   long long u = u0, sum = sum0;
   bool alive = true;
+  uint32_t read = 1u;                                                      // parity of kRead's next phase to wait for; at first there is nothing to
   uint32_t use = 0u;                                                       // units that this warp has had: unit warp + kWarps use of the share is next
   const uint32_t turned = t & 1 ? 0x1054u : 0x5410u;                       // (tokens 2 t and 2 t + 1 are the other way round there)
   while (u < u1) {
@@ -513,6 +528,9 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
       for (int i = 0; i < 2; ++i)
         if (unset >> (2 * n + i) & 1u) m[n][i] = -INFINITY;
     // ---- the warps' sums together
+    // (all have read the last item's; who gives up goes on to the next meeting all the same)
+    if (!wait_for(smem + L::kRead, read, abort_flag)) alive = false;
+    read ^= 1u;
     const float back = power_of_two(e - kLift);
 #pragma unroll
     for (int n = 0; n < kTiles; ++n)
@@ -567,7 +585,8 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
         }
       }
     }
-    block_sync();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem + L::kRead);
     u += rec_end - p.rec;
   }
 }
@@ -585,6 +604,7 @@ kv4_few_kernel(const Params P) {
       mbar_init(smem + L::kFull + 8u * i, 1);
       mbar_init(smem + L::kEmpty + 8u * i, 1);
     }
+    mbar_init(smem + L::kRead, kWarps);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -593,10 +613,11 @@ kv4_few_kernel(const Params P) {
   const Row row(P.A.w, P.T, lane, P.workers);
   if (threadIdx.x < 32) P.T.check_lengths(P.A.w, lane, &g_status_kv4_few);
   if (row.total == 0 || (long long)blockIdx.x >= row.workers) return;
-  const long long u0 = row.first_of(blockIdx.x), u1 = row.first_of(blockIdx.x + 1);
-  long long sum;
+  long long sum, u1 = row.total;
   Sequence first;
-  const int b = row.sequence_of(P.A.w, P.T, u0, lane, sum, first);
+  int b;
+  if (blockIdx.x + 1 < row.workers) u1 = row.first_of(P.A.w, P.T, blockIdx.x + 1, lane, b, sum, first);
+  const long long u0 = row.first_of(P.A.w, P.T, blockIdx.x, lane, b, sum, first);
   if (warp == kWarps)
     copy_role<L>(P, u0, u1, b, first, sum, smem, abort_flag, lane);
   else
@@ -626,11 +647,11 @@ kv4_join_kernel(const Params P, int rows) {
   s.load(W, P.T, b);
   if (s.n == 0) return;
   const Row row(W, P.T, lane, P.workers);
-  const long long before = row.before_sequence(W, P.T, b, lane);
+  const long long before = row.places_before_sequence(W, P.T, b, lane);
   const long long r = (long long)(token - s.start) * P.T.group + head % P.T.group;
   const int tile = (int)divide(r, rows), at = (int)(r - (long long)tile * rows);
-  const long long u0 = before + ((long long)(head / P.T.group) * s.tiles + tile) * s.units;
-  const int w0 = row.worker_of(u0), w1 = row.worker_of(u0 + s.units - 1);
+  const long long first = before + ((long long)(head / P.T.group) * s.tiles + tile) * (s.units + kEnd) + kEnd;
+  const int w0 = row.worker_of(first), w1 = row.worker_of(first + s.units - 1);
   if (w0 == w1) return;
   const float *work = static_cast<const float *>(P.A.work);
   auto slot = [&](int w) { return work + (size_t)(2 * w + (w == w0 ? 1 : 0)) * slot_floats(rows, kDim); };
