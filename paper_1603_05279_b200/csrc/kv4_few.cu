@@ -14,9 +14,9 @@
 // seventh unit each; at an item's end (the units of a tile) they add their sums.  An item that lies in
 // several blocks' shares leaves partial sums in the workspace, which a second kernel joins.
 //
-// 64 sequences of 300 to 8192 tokens, 8 heads of 128 with four queries each: 99 us with the join (294 MB, 0.46 of a copy's rate), at
-// 2.4 instructions per clock, half of the ALU's: the expansion of the codes and the softmax, 380 instructions a record of 4096 codes.  Single
-// tokens of short batches are latency: 5000 tokens 16 us with the join.  Two blocks per SM: one of 14 warps took 130 us (they
+// 64 sequences of 300 to 8192 tokens, 8 heads of 128 with four queries each: 88.6 us with the join (294 MB, 0.51 of a copy's rate), at
+// 2.4 instructions per clock and more, half of the ALU's: the expansion of the codes and the softmax, 380 instructions a record of 4096 codes.  Single
+// tokens of short batches are latency: 5000 tokens 15.3 us with the join.  Two blocks per SM: one of 14 warps took 130 us (they
 // meet at every item's end), three spilled, 146.
 #include <algorithm>
 #include <type_traits>
