@@ -43,6 +43,17 @@ struct Sequence {
     tiles = n > 0 ? (int)((r + T.rows - 1) / T.rows) : 0;
     units = max(1, (len + T.tokens - 1) / T.tokens);
   }
+  // What thread `lane` of the warp has.
+  __device__ __forceinline__ Sequence of(int lane) const {
+    Sequence r = *this;
+    r.start = __shfl_sync(0xffffffffu, start, lane);
+    r.n = __shfl_sync(0xffffffffu, n, lane);
+    r.len = __shfl_sync(0xffffffffu, len, lane);
+    r.lead = __shfl_sync(0xffffffffu, lead, lane);
+    r.tiles = __shfl_sync(0xffffffffu, tiles, lane);
+    r.units = __shfl_sync(0xffffffffu, units, lane);
+    return r;
+  }
   __device__ __forceinline__ long long all(int kv_heads) const { return (long long)kv_heads * tiles * units; }
 };
 

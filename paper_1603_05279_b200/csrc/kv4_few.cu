@@ -92,7 +92,6 @@ struct Row {
     const int owner = later == 0 ? 31 : __ffs((int)later) - 2;       // the last thread with no more places before it
     long long u = before, v = places_before;
     b = lane;
-    found = own;
     if (per > 1 && lane == owner) {
       for (b = lane * per; b + 1 < W.d.seqs; ++b) {
         Sequence s;
@@ -106,16 +105,8 @@ struct Row {
     sum = __shfl_sync(0xffffffffu, u, owner);
     v = __shfl_sync(0xffffffffu, v, owner);
     b = __shfl_sync(0xffffffffu, b, owner);
-    if (per > 1) {
-      found.load(W, T, b);
-    } else {
-      found.start = __shfl_sync(0xffffffffu, found.start, owner);
-      found.n = __shfl_sync(0xffffffffu, found.n, owner);
-      found.len = __shfl_sync(0xffffffffu, found.len, owner);
-      found.lead = __shfl_sync(0xffffffffu, found.lead, owner);
-      found.tiles = __shfl_sync(0xffffffffu, found.tiles, owner);
-      found.units = __shfl_sync(0xffffffffu, found.units, owner);
-    }
+    if (per > 1) found.load(W, T, b);
+    else found = own.of(owner);
     const int length = found.units + kEnd;
     const long long item = divide(place - v, length);
     return sum + item * found.units + max(0, (int)(place - v - item * length) - kEnd);
@@ -641,13 +632,23 @@ kv4_join_kernel(const Params P, int rows) {
   const int token = (int)(item / (uint32_t)P.A.r.q_heads), head = (int)(item % (uint32_t)P.A.r.q_heads);
   if (token >= P.A.r.rows) return;
   const Kv4Where &W = P.A.w;
-  int b, place;
-  if (!find_sequence(W, token, lane, b, place)) return;
-  Sequence s;
-  s.load(W, P.T, b);
-  if (s.n == 0) return;
   const Row row(W, P.T, lane, P.workers);
-  const long long before = row.places_before_sequence(W, P.T, b, lane);
+  int b, place;
+  Sequence s;
+  long long before;
+  if (row.per == 1) {                                      // (a thread has read all of a sequence's numbers)
+    const uint32_t has = __ballot_sync(0xffffffffu, lane < W.d.seqs && token >= row.own.start && token - row.own.start < row.own.n);
+    if (has == 0u) return;
+    b = __ffs((int)has) - 1;
+    s = row.own.of(b);
+    place = s.lead + token;
+    before = __shfl_sync(0xffffffffu, row.places_before, b);
+  } else {
+    if (!find_sequence(W, token, lane, b, place)) return;
+    s.load(W, P.T, b);
+    if (s.n == 0) return;
+    before = row.places_before_sequence(W, P.T, b, lane);
+  }
   const long long r = (long long)(token - s.start) * P.T.group + head % P.T.group;
   const int tile = (int)divide(r, rows), at = (int)(r - (long long)tile * rows);
   const long long first = before + ((long long)(head / P.T.group) * s.tiles + tile) * (s.units + kEnd) + kEnd;
@@ -655,16 +656,11 @@ kv4_join_kernel(const Params P, int rows) {
   if (w0 == w1) return;
   const float *work = static_cast<const float *>(P.A.work);
   auto slot = [&](int w) { return work + (size_t)(2 * w + (w == w0 ? 1 : 0)) * slot_floats(rows, kDim); };
-  float top = -INFINITY;
-  for (int w = w0 + lane; w <= w1; w += 32) top = fmaxf(top, load_global(slot(w) + (size_t)rows * kDim + 2 * at));
-#pragma unroll
-  for (int x = 16; x > 0; x /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-  // eight shares' loads under way at a time
+  // eight shares' loads under way at a time, the first before the maximum is known
   using Piece = std::conditional_t<kDim == 128, float4, float2>;
-  float total = 0.0f, acc[kDim / 32] = {};
-  for (int w = w0; w <= w1; w += 8) {
-    Piece v[8];
-    float ml[8][2];
+  Piece v[8];
+  float ml[8][2], top = -INFINITY;
+  auto fetch = [&](int w) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float *from = slot(min(w + i, w1));
@@ -672,6 +668,19 @@ kv4_join_kernel(const Params P, int rows) {
       ml[i][1] = load_global(from + (size_t)rows * kDim + 2 * at + 1);
       v[i] = load_piece(reinterpret_cast<const Piece *>(from + (size_t)at * kDim) + lane);
     }
+  };
+  fetch(w0);
+  if (w1 - w0 < 8) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, ml[i][0]);
+  } else {
+    for (int w = w0 + lane; w <= w1; w += 32) top = fmaxf(top, load_global(slot(w) + (size_t)rows * kDim + 2 * at));
+#pragma unroll
+    for (int x = 16; x > 0; x /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+  }
+  float total = 0.0f, acc[kDim / 32] = {};
+  for (int w = w0; w <= w1; w += 8) {
+    if (w > w0) fetch(w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float f = top == -INFINITY || w + i > w1 ? 0.0f : exp2_fast(ml[i][0] - top);
