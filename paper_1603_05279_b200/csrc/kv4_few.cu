@@ -14,9 +14,9 @@
 // seventh unit each; at an item's end (the units of a tile) they add their sums.  An item that lies in
 // several blocks' shares leaves partial sums in the workspace, which a second kernel joins.
 //
-// 64 sequences of 300 to 8192 tokens, 8 heads of 128 with four queries each: 88.6 us with the join (294 MB, 0.51 of a copy's rate), at
+// 64 sequences of 300 to 8192 tokens, 8 heads of 128 with four queries each: 87.8 us with the join (294 MB, 0.52 of a copy's rate), at
 // 2.4 instructions per clock and more, half of the ALU's: the expansion of the codes and the softmax, 380 instructions a record of 4096 codes.  Single
-// tokens of short batches are latency: 5000 tokens 15.3 us with the join.  Two blocks per SM: one of 14 warps took 130 us (they
+// tokens of short batches are latency: 5000 tokens 13.3 us with the join.  Two blocks per SM: one of 14 warps took 130 us (they
 // meet at every item's end), three spilled, 146.
 #include <algorithm>
 #include <type_traits>
@@ -35,7 +35,7 @@ using namespace umma;
 constexpr int kWarps = 7, kTurns = 4, kStages = kTurns * kWarps;      // kTurns: stages of a warp
 constexpr int per_sm(int tiles) { return tiles == 1 ? 2 : 1; }          // blocks: by their registers
 constexpr int kMaxWorkers = 2 * 160;         // blocks, at most (a B200 has 148 SMs)
-constexpr int kLeastUnits = 2 * kWarps;      // of a block's share
+constexpr int kLeastUnits = 3 * kWarps;      // of a block's share, where items are few: us for 14, 21, 28 with one sequence of 1000 tokens, 8 heads, 11.2 12.2 13.0, of 5000 15.2 13.3 14.0
 
 // Shares are cut in a row in which an item has kEnd places more than units, before its first: its end, where the warps meet, and its
 // start take a block about as long as so many units.  us for 0, 10, 24, 36, 56: 64 sequences of 300 to 8192 tokens
@@ -71,7 +71,7 @@ struct Row {
     total = __shfl_sync(0xffffffffu, sum, 31);
     places_before = place_sum - my_places;
     places = __shfl_sync(0xffffffffu, place_sum, 31);
-    workers = max(1ll, min((long long)most, total / kLeastUnits));
+    workers = max(1ll, min((long long)most, max((places - total) / kEnd, total / kLeastUnits)));      // (a block an item at least: 100 tokens 11.2 -> 8.9 us)
   }
   __device__ __forceinline__ int worker_of(long long place) const { return (int)divide((place + 1) * workers - 1, places); }
   // The places before sequence b; the same for all threads.
