@@ -14,11 +14,12 @@
 // seventh unit each; at an item's end (the units of a tile) they add their sums.  An item that lies in
 // several blocks' shares leaves partial sums in the workspace, which a second kernel joins.
 //
-// 64 sequences of 300 to 8192 tokens, 8 heads of 128 with four queries each: 87.8 us with the join (294 MB, 0.52 of a copy's rate), at
+// 64 sequences of 300 to 8192 tokens, 8 heads of 128 with four queries each: 88 us with the join (294 MB, 0.52 of a copy's rate), at
 // 2.4 instructions per clock and more, half of the ALU's: the expansion of the codes and the softmax, 380 instructions a record of 4096 codes.  Single
-// tokens of short batches are latency: 5000 tokens 13.3 us with the join.  Two blocks per SM: one of 14 warps took 130 us (they
+// tokens of short batches are latency: 5000 tokens 13.5 us with the join.  Two blocks per SM: one of 14 warps took 130 us (they
 // meet at every item's end), three spilled, 146.
 #include <algorithm>
+#include <climits>
 #include <type_traits>
 
 #include "kv4_attention.cuh"
@@ -621,22 +622,39 @@ __device__ __forceinline__ float2 load_piece(const float2 *p) {
   return make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
 }
 
-// Joins the partial sums of items that lie in several blocks' shares: a warp has a row (token and head).
+// Joins the partial sums of items that lie in several blocks' shares: a warp has a row (token and head).  limit > 0: it has row
+// i < limit of a sequence and head of the cache instead, which are fewer where most tokens belong to long prompts (two of 4096
+// tokens, none of them this kernel's, took 33 us).
 constexpr int kJoinWarps = 4;
 template <class T, int kDim>
 __global__ void __launch_bounds__(32 * kJoinWarps)
-kv4_join_kernel(const Params P, int rows) {
+kv4_join_kernel(const Params P, int rows, int limit) {
   const int lane = threadIdx.x & 31;
   const uint32_t item = blockIdx.x * kJoinWarps + threadIdx.x / 32;        // (up to 2^30)
   stream_order();
-  const int token = (int)(item / (uint32_t)P.A.r.q_heads), head = (int)(item % (uint32_t)P.A.r.q_heads);
-  if (token >= P.A.r.rows) return;
   const Kv4Where &W = P.A.w;
-  const Row row(W, P.T, lane, P.workers);
-  int b, place;
+  int token, head, b, place;
   Sequence s;
   long long before;
-  if (row.per == 1) {                                      // (a thread has read all of a sequence's numbers)
+  if (limit > 0) {
+    const uint32_t of_sequence = (uint32_t)W.d.kv_heads * (uint32_t)limit, rest = item % of_sequence;
+    b = (int)(item / of_sequence);
+    if (b >= W.d.seqs) return;
+    s.load(W, P.T, b);
+    const int r = (int)(rest % (uint32_t)limit);
+    if (r >= s.n * P.T.group) return;
+    token = s.start + r / P.T.group;
+    head = (int)(rest / (uint32_t)limit) * P.T.group + r % P.T.group;
+    place = s.lead + token;
+  } else {
+    token = (int)(item / (uint32_t)P.A.r.q_heads);
+    head = (int)(item % (uint32_t)P.A.r.q_heads);
+    if (token >= P.A.r.rows) return;
+  }
+  const Row row(W, P.T, lane, P.workers);
+  if (limit > 0) {
+    before = row.places_before_sequence(W, P.T, b, lane);
+  } else if (row.per == 1) {                               // (a thread has read all of a sequence's numbers)
     const uint32_t has = __ballot_sync(0xffffffffu, lane < W.d.seqs && token >= row.own.start && token - row.own.start < row.own.n);
     if (has == 0u) return;
     b = __ffs((int)has) - 1;
@@ -709,8 +727,10 @@ cudaError_t run(const Kv4Args &a, int most_rows, cudaStream_t st) {
   const Params P = {a, {a.r.q_heads / a.w.d.kv_heads, L::kRows, kKvTokens, a.r.rows, 0, most_rows}, workers, rows_in_pieces(a.q, a.r.q_stride, kDim, 2), a.r.out_stride % 2 == 0, W4Type<__half>::kMagic};
   e = launch_kernel(kv4_few_kernel<T, kDim, kTiles>, dim3((unsigned)workers), 32 * (kWarps + 1), L::kBytes, st, 1, P);
   if (e != cudaSuccess) return e;
-  const long long rows = (long long)a.r.rows * a.r.q_heads;
-  return launch_kernel(kv4_join_kernel<T, kDim>, dim3((unsigned)((rows + kJoinWarps - 1) / kJoinWarps)), 32 * kJoinWarps, 0, st, 1, P, L::kRows);
+  // (by most_rows, which the kernel holds to, not by what the caller says)
+  const long long rows = (long long)a.r.rows * a.r.q_heads, places = most_rows == INT_MAX ? rows : (long long)most_rows * a.w.d.kv_heads * a.w.d.seqs;
+  return launch_kernel(kv4_join_kernel<T, kDim>, dim3((unsigned)((std::min(rows, places) + kJoinWarps - 1) / kJoinWarps)), 32 * kJoinWarps, 0, st, 1, P, L::kRows,
+                       places < rows ? most_rows : 0);
 }
 template <class T>
 cudaError_t run_type(const Kv4Args &a, int most_rows, cudaStream_t st) {

@@ -12,10 +12,10 @@
 //        8 - 11 keys from 4-bit records into operands of 128 tokens (three stages), and the columns' scales; 12 - 15 values
 //        16     issues the products
 //        17     copies records into a ring in shared memory, a thread a record
-// Two prompts of 4096 tokens, 32 heads of 128 on 8: 470 us, 571 TFLOP/s of what is not masked, 0.34 of a matrix product's rate; the tensor
+// Two prompts of 4096 tokens, 32 heads of 128 on 8: 427 us with the other kernel's launches, 629 TFLOP/s of what is not masked, 0.37 of a matrix product's rate; the tensor
 // pipe is busy 30 % of the time.  An item of two halves takes 2800 clocks for 128 tokens, of which the products alone would take
 // 1600, and 27,000 before its first and after its last (its place, its queries, the first records, its output).  Tried: turns of the
-// halves by barriers 583 us, one block that goes on from item to item 582 (it spills), two chains of products no change.
+// halves by barriers 583 us against 470 at the time, one block that goes on from item to item 582 (it spills), two chains of products no change.
 // Where there are too few items for the GPU, the blocks of an item divide its context, and a second kernel joins
 // their sums.  Every wait is bounded; on expiry the block records XNOR_ERR_TIMEOUT, stops and frees its tensor memory.
 #include <algorithm>

@@ -234,3 +234,12 @@ def test_sequences_of_all_sizes_in_one_call(seqs, heads):
     batch = Batch([n + 150 - 3 * i for i, n in enumerate(new)], new, heads, 64, 16, 91).fill(92)
     q = randn((batch.T, 2 * heads, 64), gen(93), torch.float16)
     check(batch, q, 0.2, *run(batch, q, 0.2, 0))
+
+
+@pytest.mark.parametrize("most", [0, 700])
+def test_short_sequences_beside_long_prompts(most):
+    """Rows of short ones, whose context many blocks share, next to prompts that make up nearly all of the call's rows."""
+    lens, new = [700, 3000, 1, 650, 2500, 0], [700, 1, 1, 650, 24, 0]
+    batch = Batch(lens, new, 2, 64, 32, 101).fill(102)
+    q = randn((batch.T, 8, 64), gen(103), torch.bfloat16)
+    check(batch, q, 0.2, *run(batch, q, 0.2, most))
