@@ -701,8 +701,9 @@ kv4_join_kernel(const Params P, int rows, int limit) {
     if (w > w0) fetch(w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float f = top == -INFINITY || w + i > w1 ? 0.0f : exp2_fast(ml[i][0] - top);
-      if (f == 0.0f) continue;                             // (a share that saw nothing)
+      if (w + i > w1) continue;
+      // (a share that saw nothing has zeros; one whose sums are NaN has them whatever its maximum is, which NaN does not raise)
+      const float f = top == -INFINITY ? 0.0f : exp2_fast(ml[i][0] - top);
       total = fmaf(f, ml[i][1], total);
 #pragma unroll
       for (int c = 0; c < kDim / 32; ++c) acc[c] = fmaf(f, reinterpret_cast<const float *>(&v[i])[c], acc[c]);

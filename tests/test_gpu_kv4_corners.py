@@ -1,0 +1,63 @@
+"""Attention over the cache in 4 bits where a token or a page spoils a row, against the definition in 64 bits."""
+import pytest
+import torch
+
+import paper_1603_05279_b200 as X
+from kv4_util import TYPES, Batch, attention64
+from rows_util import gen, randn
+
+pytestmark = pytest.mark.gpu
+
+
+def attend(batch, q, scale, most, table=None):
+    T, Hq, D = q.shape
+    out, lse = torch.full_like(q, 3.0), torch.full((T, Hq), 3.0, device="cuda")
+    d = X.make_kv4_desc(batch.pages, batch.page, batch.heads, D)
+    X.xnor_kv4_attention(q, batch.cache, batch.starts, batch.lens, batch.table if table is None else table, d, scale, most, out, lse,
+                         X.alloc_kv4_work(d, T, Hq, len(batch.len_list)))
+    return out, lse
+
+
+# lens, new, sequence and token that is NaN.  The first: two blocks' shares of five records are cut before the only one that has the token.
+NAN_CASES = [
+    ([33, 17], [1, 1], 0, 32),
+    ([33, 17], [1, 1], 0, 3),
+    ([5000], [1], 0, 4999),
+    ([5000], [1], 0, 0),
+    ([3000, 1, 40], [2, 1, 3], 0, 2998),
+    ([3000], [300], 0, 2700),
+]
+
+
+@pytest.mark.parametrize("case", NAN_CASES, ids=lambda c: "%s-%s-%d-%d" % c)
+@pytest.mark.parametrize("D,t", [(64, "f16"), (128, "bf16")])
+@pytest.mark.parametrize("which", ["key", "value"])
+def test_nan_reaches_every_row_that_sees_it(case, D, t, which):
+    """However the context is cut: the outputs of rows that see a key or a value of NaN are NaN; lse is with keys."""
+    lens, new, b, p = case
+    H, G = 1, 4
+    batch = Batch(lens, new, H, D, 16, 201).fill(202)
+    q = randn((batch.T, H * G, D), gen(203), TYPES[t])
+    want, x, off, lse_off = attention64(batch, q, 0.1)
+    page, slot = batch.place(b, torch.tensor(p, device="cuda"))
+    batch.cache[..., 16 * D:].view(torch.int32)[page, 0, slot // 16, (0 if which == "key" else 16) + slot % 16] = 0x7FFFFFF8
+    out, lse = attend(batch, q, 0.1, max(new))
+    X.xnor_check_device()
+    r0, first = sum(new[:b]), max(0, p - (lens[b] - new[b]))
+    hit = torch.zeros(batch.T, dtype=torch.bool, device="cuda")
+    hit[r0 + first:r0 + new[b]] = True
+    assert out[hit].isnan().all()
+    assert ((out.double() - want).abs() <= off)[~hit].all() and ((lse.double() - x).abs() <= lse_off)[~hit].all()
+    assert lse[hit].isnan().all() if which == "key" else ((lse.double() - x).abs() <= lse_off)[hit].all()
+
+
+@pytest.mark.parametrize("lens,new", [([5000], [1]), ([33, 17], [1, 1]), ([3000], [300])])
+def test_a_query_of_nan(lens, new):
+    batch = Batch(lens, new, 1, 64, 16, 211).fill(212)
+    q = randn((batch.T, 2, 64), gen(213), torch.bfloat16)
+    q[0, 1, 7] = float("nan")
+    out, lse = attend(batch, q, 0.1, max(new))
+    X.xnor_check_device()
+    bad = torch.zeros(batch.T, 2, dtype=torch.bool, device="cuda")
+    bad[0, 1] = True
+    assert torch.equal(lse.isnan(), bad) and torch.equal(out.isnan(), bad[..., None].expand_as(out))
