@@ -662,7 +662,8 @@ xnor_status xnor_kv4_read(const void *cache, const int32_t *starts, const int32_
  * j / (q_heads / kv_heads) of the cache, and a token sees those of its sequence up to itself:
  *   out = sum over p of exp(scale q k_p - lse) v_p,   lse = log of the sum over p of exp(scale q k_p)
  *   q     in   BF16 or F16 [rows][q_heads][dim]
- *   out   out  the same type; must not overlap q.  A row that sees nothing: zeros
+ *   out   out  the same type; must not overlap q.  A row that sees nothing (no token before it, or all of them
+ *              outside the cache; logits of -infinity count as not seen): zeros
  *   lse   out  fp32 [rows][q_heads], dense, or NULL; -infinity for a row that sees nothing
  *   most  no sequence has more new tokens than this (0: not known).  By it and the sizes the call
  *         chooses its kernels; where it is too small, results are as good and may take longer

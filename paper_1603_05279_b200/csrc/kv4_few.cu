@@ -564,8 +564,8 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
 #pragma unroll
         for (int c = 0; c < kDim / 32; ++c) acc[c] = fmaf(f[i], sums[(size_t)(i * kRows + r) * L::kSumRow + lane * (kDim / 32) + c], acc[c]);
       if (first && last) {
-        const bool blind = at.limit < 0;
-        const float inv = blind ? 0.0f : 1.0f / total;
+        const bool blind = total == 0.0f;                    // no token before it, or all of them outside the cache
+        const float inv = 1.0f / total;
         store_row<T, kDim>(static_cast<T *>(P.A.out) + at.out, acc, inv, blind, P.out_words, lane);
         if (lane == 0 && P.A.lse) P.A.lse[at.lse] = blind ? -INFINITY : (top + log2f(total)) * kLn2;
       } else {
@@ -633,7 +633,7 @@ kv4_join_kernel(const Params P, int rows, int limit) {
   const uint32_t item = blockIdx.x * kJoinWarps + threadIdx.x / 32;        // (up to 2^30)
   stream_order();
   const Kv4Where &W = P.A.w;
-  int token, head, b, place;
+  int token, head, b;
   Sequence s;
   long long before;
   if (limit > 0) {
@@ -645,7 +645,6 @@ kv4_join_kernel(const Params P, int rows, int limit) {
     if (r >= s.n * P.T.group) return;
     token = s.start + r / P.T.group;
     head = (int)(rest / (uint32_t)limit) * P.T.group + r % P.T.group;
-    place = s.lead + token;
   } else {
     token = (int)(item / (uint32_t)P.A.r.q_heads);
     head = (int)(item % (uint32_t)P.A.r.q_heads);
@@ -659,9 +658,9 @@ kv4_join_kernel(const Params P, int rows, int limit) {
     if (has == 0u) return;
     b = __ffs((int)has) - 1;
     s = row.own.of(b);
-    place = s.lead + token;
     before = __shfl_sync(0xffffffffu, row.places_before, b);
   } else {
+    int place;
     if (!find_sequence(W, token, lane, b, place)) return;
     s.load(W, P.T, b);
     if (s.n == 0) return;
@@ -709,7 +708,7 @@ kv4_join_kernel(const Params P, int rows, int limit) {
       for (int c = 0; c < kDim / 32; ++c) acc[c] = fmaf(f, reinterpret_cast<const float *>(&v[i])[c], acc[c]);
     }
   }
-  const bool blind = place < 0;
+  const bool blind = total == 0.0f;                        // no token before it, or all of them outside the cache
   const float inv = 1.0f / total;
   store_row<T, kDim>(static_cast<T *>(P.A.out) + token * P.A.r.out_stride + (long long)head * kDim, acc, inv, blind, P.out_words, lane);
   if (lane == 0 && P.A.lse) P.A.lse[(long long)token * P.A.r.q_heads + head] = blind ? -INFINITY : (top + log2f(total)) * kLn2;

@@ -682,7 +682,7 @@ __device__ __forceinline__ void softmax_role(const Block &B, int half, int quart
     if (!wait_inline(B, B.smem + L::kLast + 8u * half, 0u)) return;
     tc_fence_after();
   }
-  const bool blind = limit < 0 || n == 0;
+  const bool blind = l_row == 0.0f;                        // no token before it, or all of them outside the cache
   const float back = power_of_two(e - kLift), inv = B.direct ? back / l_row : back;
   float *partial = B.partial + (size_t)(half * kHalf + in_tile) * kDim, *stats = B.partial + (size_t)kItemRows * kDim + 2 * (half * kHalf + in_tile);
   int32_t o[kDim / 16][16];
@@ -859,7 +859,7 @@ kv4_prompt_join_kernel(const Params P) {
 #pragma unroll
     for (int c = 0; c < kDim / 32; ++c) acc[c] = fmaf(f, load_global(part(i) + (size_t)in_tile * kDim + lane + 32 * c), acc[c]);
   }
-  const bool blind = place < 0;
+  const bool blind = total == 0.0f;                        // no token before it, or all of them outside the cache
   const float inv = 1.0f / total;
   T *out = static_cast<T *>(P.A.out) + token * P.A.r.out_stride + (long long)head * kDim;
 #pragma unroll

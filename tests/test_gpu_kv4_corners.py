@@ -1,12 +1,17 @@
 """Attention over the cache in 4 bits where a token or a page spoils a row, against the definition in 64 bits."""
+import copy
+
 import pytest
 import torch
 
 import paper_1603_05279_b200 as X
+from paper_1603_05279_b200 import binding as B
 from kv4_util import TYPES, Batch, attention64
 from rows_util import gen, randn
 
 pytestmark = pytest.mark.gpu
+
+INF = float("inf")
 
 
 def attend(batch, q, scale, most, table=None):
@@ -61,3 +66,45 @@ def test_a_query_of_nan(lens, new):
     bad = torch.zeros(batch.T, 2, dtype=torch.bool, device="cuda")
     bad[0, 1] = True
     assert torch.equal(lse.isnan(), bad) and torch.equal(out.isnan(), bad[..., None].expand_as(out))
+
+
+# lens, new, kv heads, queries a head, the pages of sequence 0 that are in the cache (from the end; 0: none)
+BLIND_CASES = [
+    ([20], [1], 1, 4, 0),
+    ([5000], [1], 2, 4, 0),                    # cut among blocks
+    ([33, 17], [1, 1], 1, 4, 0),
+    ([300, 50], [6, 2], 2, 2, 0),
+    ([100], [40], 2, 2, 1),                    # rows before the page that is there
+    ([200], [200], 2, 2, 0),
+    ([200], [200], 2, 2, 5),
+    ([3000, 30], [300, 1], 1, 8, 0),           # cut among blocks
+    ([3000], [300], 1, 8, 4),
+]
+
+
+@pytest.mark.parametrize("case", BLIND_CASES, ids=str)
+@pytest.mark.parametrize("D,t", [(64, "bf16"), (128, "f16")])
+def test_rows_whose_visible_tokens_are_all_outside_the_cache(case, D, t):
+    """They see nothing: zeros and -infinity.  The others see what is there."""
+    lens, new, H, G, there = case
+    batch = Batch(lens, new, H, D, 16, 221).fill(222)
+    q = randn((batch.T, H * G, D), gen(223), TYPES[t])
+    pages = -(-lens[0] // 16)
+    table = batch.table.clone()
+    table[0, :pages - there] = torch.where(torch.arange(pages - there, device="cuda") % 2 == 0, batch.pages, -1).int()
+    out, lse = attend(batch, q, 0.1, max(new), table)
+    with pytest.raises(X.XnorError) as e:
+        X.xnor_check_device()
+    assert e.value.status == B.XNOR_ERR_BOUNDS
+    X.xnor_check_device()
+    n, first = new[0], (pages - there) * 16
+    blind = torch.arange(lens[0] - n, lens[0], device="cuda") < first
+    assert (out[:n][blind] == 0).all() and (lse[:n][blind] == -INF).all()
+    if there:
+        # a sequence of the tokens that are there, whose first rows come before them
+        rest = copy.copy(batch)
+        rest.table, rest.len_list, rest.new_list = batch.table[:, pages - there:], [lens[0] - first] + lens[1:], new
+        want, x, off, lse_off = attention64(rest, q, 0.1)
+        assert ((out.double() - want).abs() <= off)[:n].all() and ((lse.double() - x).abs() <= lse_off)[:n][~blind].all()
+    want, x, off, lse_off = attention64(batch, q, 0.1)
+    assert ((out.double() - want).abs() <= off)[n:].all() and ((lse.double() - x).abs() <= lse_off)[n:].all()
