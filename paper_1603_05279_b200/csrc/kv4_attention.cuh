@@ -7,7 +7,7 @@ namespace xnor {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // A row's maximum is left behind by 2^8 at most: then P, up to 2^8 times a value's scale, is rounded to F16, relative to a
-// power of two 2^e above the largest scale so far and times 2^7.  That is at most 2^15, and has all 11 bits
+// power of two 2^e above the largest scale so far that the row sees and times 2^7.  That is at most 2^15, and has all 11 bits
 // down to 2^-21 of that scale.  (As bfloat16 it gave outputs in bfloat16 half as much again of error.)
 constexpr float kRaise = 8.0f;
 constexpr int kLift = 7;
@@ -75,6 +75,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
 
 // 2^i; 0 below fp32's normal numbers.
 __device__ __forceinline__ float power_of_two(int i) { return i < -126 ? 0.0f : __uint_as_float((uint32_t)(i + 127) << 23); }
+// 1 / 2^i, of a normal number whose inverse is one.
+__device__ __forceinline__ float inverse_power(float v) { return __uint_as_float((254u << 23) - __float_as_uint(v)); }
 // The power of two above a scale, within limits that keep all its uses normal numbers.  Infinity and NaN do not count.
 constexpr int kLeastScale = -100, kMostScale = 127;
 __device__ __forceinline__ int scale_above(float s) {

@@ -342,12 +342,16 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
     float o[kTiles][kMTiles][4], m[kTiles][2], l[kTiles][2];
     uint32_t unset = (1u << (2 * kTiles)) - 1u;
     bool settled = false;
-    int e = kLeastScale;                                                   // 2^e: the values' scales are below it
-    float largest = 0.0f, lift = 0.0f;                                     // 2^e, 2^(kLift - e); 0: not known
+    // 2^(kLift - e), 2^e above the scales of the values that the row has seen: of each row, for the tokens behind it may have any (up to
+    // the first record that is masked all rows have seen the same); and the least 2^e (0: not known)
+    float lift[kTiles][2], largest = 0.0f;
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) m[n][i] = l[n][i] = 0.0f;
+      for (int i = 0; i < 2; ++i) {
+        m[n][i] = l[n][i] = 0.0f;
+        lift[n][i] = power_of_two(kLift - kLeastScale);
+      }
 #pragma unroll
       for (int j = 0; j < kMTiles; ++j)
 #pragma unroll
@@ -419,7 +423,8 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
       if (lane == 0) mbar_arrive(smem + L::kEmpty + 8u * stage);
       // ---- the softmax: s[n][0], [1]: token tok0 for rows 2 t, 2 t + 1; [2], [3]: token tok1
       const float ks0 = kv4_scale(kw0), ks1 = kv4_scale(kw1);
-      float vs0 = kv4_scale(vw0), vs1 = kv4_scale(vw1), over = -INFINITY, x[kTiles][4];
+      float vs0 = kv4_scale(vw0), vs1 = kv4_scale(vw1);
+      float over = -INFINITY, x[kTiles][4];
       const int p0 = rec * kKvTokens;
       const bool masked = valid < kKvTokens || p0 + kKvTokens - 1 > least;
 #pragma unroll
@@ -443,18 +448,23 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
           over = fmaxf(over, x[n][j]);
         }
       if (!settled || __any_sync(0xffffffffu, over > kRaise || fmaxf(vs0, vs1) > largest)) {
-        const int above = __reduce_max_sync(0xffffffffu, max(e, max(tok0 < valid ? scale_above(vs0) : kLeastScale, tok1 < valid ? scale_above(vs1) : kLeastScale)));
-        const float down = power_of_two(e - above);
-        e = above;
-        largest = power_of_two(e);
-        lift = power_of_two(kLift - e);
+        const float lift0 = power_of_two(kLift - scale_above(vs0)), lift1 = power_of_two(kLift - scale_above(vs1));
+        float most = 0.0f;
 #pragma unroll
         for (int n = 0; n < kTiles; ++n)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            float top = fmaxf(s[n][i], s[n][i + 2]), f = 1.0f;
+            float top = fmaxf(s[n][i], s[n][i + 2]), f = 1.0f, now = lift[n][i];
+            if (!masked || s[n][i] != -INFINITY) now = fminf(now, lift0);
+            if (!masked || s[n][i + 2] != -INFINITY) now = fminf(now, lift1);
 #pragma unroll
-            for (int y = 4; y < 32; y *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
+            for (int y = 4; y < 32; y *= 2) {
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
+              now = fminf(now, __shfl_xor_sync(0xffffffffu, now, y));
+            }
+            const float down = now * inverse_power(lift[n][i]);
+            lift[n][i] = now;
+            most = fmaxf(most, now);
             const uint32_t bit = 1u << (2 * n + i);
             if (unset & bit ? top > -INFINITY : top > m[n][i] + kRaise) {
               f = unset & bit ? 0.0f : exp2_fast(m[n][i] - top);
@@ -470,10 +480,13 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
             x[n][i] = s[n][i] - m[n][i];
             x[n][i + 2] = s[n][i + 2] - m[n][i];
           }
+        largest = power_of_two(kLift) * inverse_power(most);
         settled = __all_sync(0xffffffffu, unset == 0u);
       }
-      vs0 *= lift;
-      vs1 *= lift;
+      if (!masked) {
+        vs0 *= lift[0][0];
+        vs1 *= lift[0][0];
+      }
       uint32_t b[kTiles][2];                                               // P^T: tokens 0 .. 7 and 8 .. 15 of the rows
 #pragma unroll
       for (int n = 0; n < kTiles; ++n) {
@@ -481,12 +494,11 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
         for (int j = 0; j < 4; ++j) {
           x[n][j] = exp2_fast(x[n][j]);
           l[n][j & 1] += x[n][j];
-          x[n][j] *= j < 2 ? vs0 : vs1;
+          if (!masked) x[n][j] *= j < 2 ? vs0 : vs1;
         }
         if (masked) {                                                      // (a token that is not seen may stand for anything)
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (s[n][j] == -INFINITY) x[n][j] = 0.0f;
+          for (int j = 0; j < 4; ++j) x[n][j] = s[n][j] == -INFINITY ? 0.0f : x[n][j] * ((j < 2 ? vs0 : vs1) * lift[n][j & 1]);
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) b[n][h] = transpose8x8(float_to_pair(x[n][2 * h], x[n][2 * h + 1], __half()));
@@ -523,11 +535,11 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
     // (all have read the last item's; who gives up goes on to the next meeting all the same)
     if (!wait_for(smem + L::kRead, read, abort_flag)) alive = false;
     read ^= 1u;
-    const float back = power_of_two(e - kLift);
 #pragma unroll
     for (int n = 0; n < kTiles; ++n)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
+        const float back = inverse_power(lift[n][i]);
 #pragma unroll
         for (int x = 4; x < 32; x *= 2) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], x);
         const int r = 8 * n + 2 * t + i;

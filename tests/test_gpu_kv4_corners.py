@@ -108,3 +108,55 @@ def test_rows_whose_visible_tokens_are_all_outside_the_cache(case, D, t):
         assert ((out.double() - want).abs() <= off)[:n].all() and ((lse.double() - x).abs() <= lse_off)[:n][~blind].all()
     want, x, off, lse_off = attention64(batch, q, 0.1)
     assert ((out.double() - want).abs() <= off)[n:].all() and ((lse.double() - x).abs() <= lse_off)[n:].all()
+
+
+def row_by_row(batch, q, scale):
+    """attention64 of each row with the tokens that it sees, and no others, in its sequence."""
+    got = []
+    for b, (length, n) in enumerate(zip(batch.len_list, batch.new_list)):
+        for i in range(n):
+            one = copy.copy(batch)
+            one.len_list, one.new_list, one.table, one.gap = [length - n + i + 1], [1], batch.table[b:b + 1], 0
+            row = sum(batch.new_list[:b]) + i
+            got.append(attention64(one, q[row:row + 1], scale))
+    return [torch.cat(v) for v in zip(*got)]
+
+
+def set_value_scales(batch, b, first, factors):
+    """Values of tokens first .. of sequence b times powers of two."""
+    page, slot = batch.place(b, first + torch.arange(factors.numel(), device="cuda"))
+    words = batch.cache[..., 16 * batch.dim:].view(torch.int32)
+    at = (page, slice(None), slot // 16, 16 + slot % 16)
+    w = words[at]
+    words[at] = ((w & ~15).view(torch.float32) * factors[:, None]).view(torch.int32) | (w & 15)
+
+
+# lens, new, kv heads, queries a head, token of sequence 0 whose values are large
+FEW = [
+    ([16], [16], 1, 1, 9),
+    ([400], [4], 2, 4, 398),
+    ([400], [4], 2, 4, 399),
+    ([403, 20], [16, 16], 1, 1, 400),
+    ([400, 90], [8, 2], 2, 2, 393),
+    ([5000], [3], 1, 5, 4998),
+]
+
+
+@pytest.mark.parametrize("case", FEW, ids=lambda c: "%s-%s-%d-%d-%d" % c)
+@pytest.mark.parametrize("D", [64, 128])
+def test_values_of_later_tokens_in_a_call_of_few(case, D):
+    """A row is as exact as if the tokens behind it did not exist, however large their values are: one of them 2^40 times the
+    others, and all of them growing from token to token."""
+    lens, new, H, G, p = case
+    first = lens[0] - new[0]
+    grow = 2.0 ** (3.0 * torch.arange(new[0], device="cuda")).clamp(max=80)
+    for at, factors in ((p, torch.full((1,), 2.0 ** 40, device="cuda")), (first, grow)):
+        batch = Batch(lens, new, H, D, 16, 231).fill(232, v_scale=2.0 ** -10)
+        set_value_scales(batch, 0, at, factors)
+        q = randn((batch.T, H * G, D), gen(233), torch.bfloat16)
+        out, lse = attend(batch, q, 0.1, max(new))
+        X.xnor_check_device()
+        want, x, off, lse_off = row_by_row(batch, q, 0.1)
+        assert ((lse.double() - x).abs() <= lse_off).all()
+        worst = ((out.double() - want).abs() / off).amax((1, 2))
+        assert (worst <= 1).all(), (worst.argmax(), worst.max())
