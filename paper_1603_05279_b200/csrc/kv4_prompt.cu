@@ -9,9 +9,14 @@
 // rows).  The softmax is one pass with a running maximum that may be left behind by 2^8, so that O is rescaled rarely.
 //
 // Warps: 0 - 7  softmax of 32 rows each, whose queries they bring and whose output they take away
-//        8 - 11 keys from 4-bit records into operands of 128 tokens (three stages), and the columns' scales; 12 - 15 values
+//        8 - 11 keys from 4-bit records into operands of 128 tokens (three stages); 12 - 15 values
 //        16     issues the products
 //        17     copies records into a ring in shared memory, a thread a record
+//        18     the columns' scales, and what the values' are rounded by (done by the warps of keys, which others wait for: 437 us for 394)
+// Steps that all of an item's rows see whole, and those with masked tokens, are two loops: in the latter each row has a power of two of its
+// own that P is rounded by, for it must not go by tokens that the row does not see (as one loop, whose registers did not do: 419 us for 408
+// for two prompts of 4000 tokens and 30 single ones; one prompt of 128 tokens, which has no other steps, takes 1 us more than when
+// rows shared it).
 // Two prompts of 4096 tokens, 32 heads of 128 on 8: 427 us with the other kernel's launches, 629 TFLOP/s of what is not masked, 0.37 of a matrix product's rate; the tensor
 // pipe is busy 30 % of the time.  An item of two halves takes 2800 clocks for 128 tokens, of which the products alone would take
 // 1600, and 27,000 before its first and after its last (its place, its queries, the first records, its output).  Tried: turns of the
@@ -20,6 +25,7 @@
 // their sums.  Every wait is bounded; on expiry the block records XNOR_ERR_TIMEOUT, stops and frees its tensor memory.
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "kv4_attention.cuh"
 
@@ -35,7 +41,7 @@ constexpr int kHalf = 128, kItemRows = 2 * kHalf;
 constexpr int kTokens = 128, kRecords = kTokens / kKvTokens;     // of a tile
 constexpr int kStep = 64, kStepRecords = kStep / kKvTokens;
 constexpr int kOperands = 3, kRawStages = 2, kScaleBufs = 4;
-constexpr int kKeyWarp = 8, kValueWarp = 12, kMmaWarp = 16, kCopyWarp = 17, kThreads = 20 * 32;
+constexpr int kKeyWarp = 8, kValueWarp = 12, kMmaWarp = 16, kCopyWarp = 17, kScaleWarp = 18, kThreads = 20 * 32;
 constexpr int kSoftmaxRegs = 144, kOtherRegs = 64, kLaunchRegs = 96;
 static_assert(kKeyWarp * 32 * kSoftmaxRegs + (kThreads - kKeyWarp * 32) * kOtherRegs <= kThreads * kLaunchRegs, "registers");
 constexpr int kMaxSplits = 8;
@@ -47,8 +53,8 @@ struct Layout {
   static constexpr uint32_t kRawFull = 0, kRawEmpty = kRawFull + 8 * kRawStages, kFull = kRawEmpty + 8 * kRawStages, kEmpty = kFull + 8 * kOperands;
   static constexpr uint32_t kSFull = kEmpty + 8 * kOperands, kPFull = kSFull + 32, kODone = kPFull + 32, kLast = kODone + 16, kQFull = kLast + 16;      // [half][S]
   static constexpr uint32_t kScaled = kQFull + 16, kTmem = kScaled + 8 * kScaleBufs, kAbort = kTmem + 4, kItem = kAbort + 4, kMask = kItem + 48, kExponent = kMask + 4 * kRawStages;
-  static constexpr uint32_t kThere = kExponent + 4 * kScaleBufs;
-  static constexpr uint32_t kScales = 512, kRing = kScales + kScaleBufs * 2 * kTokens * 4;
+  static constexpr uint32_t kThere = kExponent + 8 * kScaleBufs;
+  static constexpr uint32_t kScales = 512, kUpTo = kScales + kScaleBufs * 2 * kTokens * 4, kRing = kUpTo + kScaleBufs * kTokens * 4;
   static constexpr uint32_t kQ = kRing + kRawStages * kRaw;      // (rounded up to 1024 in memory)
   static constexpr uint32_t kBytes = kQ + 1024 + 2 * kOperand + kOperands * kOperand;
   static_assert(kThere + 4 * kScaleBufs <= kScales && kBytes <= 232448, "shared memory");
@@ -137,6 +143,7 @@ struct Block {                // what all roles know
   const Params &P;
   Sequence s;
   int b, head, tile, first, last, steps;
+  int whole;                  // steps, from the first on, whose tokens all of the item's rows see
   bool two, direct;           // both halves have rows; the block has the whole context
   uint32_t smem, q, operands;
   uint8_t *ptr;
@@ -192,6 +199,70 @@ __device__ __forceinline__ void copy_role(const Block &B, int lane) {
   }
 }
 
+// Exponents of powers of two above values' scales, of a thread's four rows: a signed byte each.
+__device__ __forceinline__ constexpr uint32_t four_times(int e) { return ((uint32_t)e & 255u) * 0x01010101u; }
+__device__ __forceinline__ int exponent(uint32_t e, int row) { return (int)(int8_t)(e >> (8 * row)); }
+
+// ---- scales --------------------------------------------------------------------------------------------------------
+// The columns' scales, four tokens a thread.  The values' are given relative to a power of two 2^e above the largest so far, in a step that
+// all rows see whole; of others they are as they are in the cache, with the exponent up to each token beside them, and a row takes
+// that of the last token that it sees.  (Buffers are free: a tile's records come after the values of the tile four before it were used.)
+template <int kDim>
+__device__ __forceinline__ void scale_role(const Block &B, int lane) {
+  using L = Layout<kDim>;
+  const float scale2 = B.P.A.r.scale * kLog2e;
+  int e = kLeastScale;
+#pragma unroll 1
+  for (int t = B.first; t < B.last; ++t) {
+    const int i = t - B.first;
+    const uint32_t slot = (uint32_t)i % kRawStages, buf = (uint32_t)i % kScaleBufs;
+    if (!wait_warp(B, B.smem + L::kRawFull + 8u * slot, (uint32_t)(i / kRawStages) & 1u)) return;
+    const uint32_t there = lds32(B.smem + L::kMask + 4u * slot);
+    const uint32_t words = B.smem + L::kRing + slot * L::kRaw + (uint32_t)(lane / 4) * kv4_record(kDim) + 16u * (lane % 4);
+    uint32_t k[4], v[4], upto[4];
+    lds128(words + kv4_words(kDim, false), k);
+    lds128(words + kv4_words(kDim, true), v);
+    int above = kLeastScale;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool in = (there >> (lane / 4) & 1u) && t * kTokens + 4 * lane + j < B.s.len;
+      k[j] = in ? __float_as_uint(kv4_scale(k[j]) * scale2) : 0u;
+      v[j] = in ? __float_as_uint(kv4_scale(v[j])) : 0u;
+      above = max(above, scale_above(__uint_as_float(v[j])));
+      upto[j] = (uint32_t)above;
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const int x = __shfl_up_sync(0xffffffffu, above, o);
+      if (lane >= o) above = max(above, x);
+    }
+    const int x = __shfl_up_sync(0xffffffffu, above, 1), before = lane > 0 ? max(e, x) : e;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) upto[j] = (uint32_t)max((int)upto[j], before);
+    const int half = max(e, __shfl_sync(0xffffffffu, above, 15));
+    e = max(e, __shfl_sync(0xffffffffu, above, 31));
+    const bool first = 2 * i < B.whole, second = 2 * i + 1 < B.whole;
+    const int e0 = second ? e : half;
+    const float lift = lane < 16 ? (first ? power_of_two(kLift - e0) : 1.0f) : second ? power_of_two(kLift - e) : 1.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * lift);
+    const uint32_t to = B.smem + L::kScales + 4u * (2u * buf * kTokens + 4u * lane);
+    sts128(to, k[0], k[1], k[2], k[3]);
+    sts128(to + 4u * kTokens, v[0], v[1], v[2], v[3]);
+    sts128(B.smem + L::kUpTo + 4u * (buf * kTokens + 4u * lane), upto[0], upto[1], upto[2], upto[3]);
+    if (lane == 0) {
+      sts32(B.smem + L::kExponent + 8u * buf, (uint32_t)e0);
+      sts32(B.smem + L::kExponent + 8u * buf + 4u, (uint32_t)e);
+      sts32(B.smem + L::kThere + 4u * buf, there);
+    }
+    __syncwarp();
+    if (lane == 0) {
+      mbar_arrive(B.smem + L::kScaled + 8u * buf);
+      mbar_arrive(B.smem + L::kRawEmpty + 8u * slot);
+    }
+  }
+}
+
 // ---- expansion -------------------------------------------------------------------------------------------------------
 // Operands: rows of 64 values (128 bytes), swizzled in groups of eight; blocks of 64 columns one after the other.  Keys: a row is a
 // token.  Values: a row is a column of O, its values tokens; so eight tokens' codes are transposed on the way, by
@@ -202,38 +273,13 @@ __device__ __forceinline__ void key_role(const Block &B, int id) {
   constexpr uint32_t kRecord = kv4_record(kDim);
   constexpr int kQuads = kDim / 32;                        // of words in a token's codes
   const int lane = id & 31;
-  const float scale2 = B.P.A.r.scale * kLog2e;
-  float *scales = reinterpret_cast<float *>(B.ptr + L::kScales);
-  int e = kLeastScale;
 #pragma unroll 1
   for (int t = B.first; t < B.last; ++t) {
     const int i = t - B.first;
     const uint32_t op = 2u * (uint32_t)i, stage = op % kOperands;
-    const uint32_t slot = (uint32_t)i % kRawStages, raw = B.smem + L::kRing + slot * L::kRaw, buf = (uint32_t)i % kScaleBufs;
+    const uint32_t slot = (uint32_t)i % kRawStages, raw = B.smem + L::kRing + slot * L::kRaw;
     if (!wait_warp(B, B.smem + L::kRawFull + 8u * slot, (uint32_t)(i / kRawStages) & 1u)) return;
     if (!wait_warp(B, B.smem + L::kEmpty + 8u * stage, ((op / kOperands) & 1u) ^ 1u)) return;
-    const uint32_t there = lds32(B.smem + L::kMask + 4u * slot);
-    {
-      // the columns' scales; all warps find the largest value's
-      int above = e;
-#pragma unroll
-      for (int k = 0; k < kTokens / 32; ++k) {
-        const int tok = lane + 32 * k;
-        const bool in = (there >> (tok / kKvTokens) & 1u) && t * kTokens + tok < B.s.len;
-        if (in) above = max(above, scale_above(kv4_scale(lds32(raw + (uint32_t)(tok / kKvTokens) * kRecord + kv4_words(kDim, true) + 4u * (tok % kKvTokens)))));
-      }
-      e = __reduce_max_sync(0xffffffffu, above);
-      const bool in = (there >> (id / kKvTokens) & 1u) && t * kTokens + id < B.s.len;
-      const uint32_t words = raw + (uint32_t)(id / kKvTokens) * kRecord + 4u * (id % kKvTokens);
-      scales[(2 * buf) * kTokens + id] = in ? kv4_scale(lds32(words + kv4_words(kDim, false))) * scale2 : 0.0f;
-      scales[(2 * buf + 1) * kTokens + id] = in ? kv4_scale(lds32(words + kv4_words(kDim, true))) * power_of_two(kLift - e) : 0.0f;
-      if (id == 0) {
-        sts32(B.smem + L::kExponent + 4u * buf, (uint32_t)e);
-        sts32(B.smem + L::kThere + 4u * buf, there);
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(B.smem + L::kScaled + 8u * buf);
-    }
     {
       const uint32_t to = B.operands + stage * L::kOperand;
 #pragma unroll
@@ -469,13 +515,14 @@ __device__ __forceinline__ float2 lds_float2(uint32_t addr) {
 
 // The weights of a step, against the rows' maxima m: p = exp2(s ks - m) times the values' scales, as pairs of F16; their sums before
 // that; and the largest s ks - m, each of this thread's columns (2 t and 2 t + 1 of eight, of rows g, g + 8, g + 16 and g + 24 of 32;
-// scales: theirs).  kMasked: columns from `seen` on (counted from 2 t) are not seen, nor are records that are
-// missing; and s ks is rounded before m is taken from it, and the largest s ks itself is given, so that as the
-// maximum it gives a weight of 1 whatever its size.
+// scales: theirs).  kCareful: records may be missing; and s ks is rounded before m is taken from it, and the largest s ks itself is
+// given, so that as the maximum it gives a weight of 1 whatever its size.  kOwn: besides, columns from `seen` on (counted from 2 t)
+// are not seen, and the values' scales are those of the cache, which each row takes times a power of two of its own (lifts: the exponents).
 struct Scales { float2 k[kStep / 8], v[kStep / 8]; };
-template <bool kMasked>
-__device__ __forceinline__ void weigh(uint32_t S, const Scales &scales, const float (&m)[4], const int (&seen)[4], uint32_t there, uint32_t (&p)[2][16],
-                                      float (&sum)[4], float (&top)[4]) {
+enum Care { kPlain, kCareful, kOwn };
+template <Care kCare>
+__device__ __forceinline__ void weigh(uint32_t S, const Scales &scales, const float (&m)[4], const int (&seen)[4], uint32_t lifts, uint32_t there,
+                                      uint32_t (&p)[2][16], float (&sum)[4], float (&top)[4]) {
   float2 sums[4];
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
@@ -500,8 +547,8 @@ __device__ __forceinline__ void weigh(uint32_t S, const Scales &scales, const fl
       for (int r = 0; r < 4; ++r) {
         const uint32_t *x = raw[c][r >> 1] + 4 * k + 2 * (r & 1);
         float2 u = make_float2(__uint_as_float(x[0]), __uint_as_float(x[1]));
-        const int end = !kMasked ? 0 : (there >> (column / kKvTokens) & 1u) ? seen[r] : INT_MIN;
-        if (kMasked) {
+        const int end = (there >> (column / kKvTokens) & 1u) ? (kCare == kOwn ? seen[r] : INT_MAX) : INT_MIN;
+        if (kCare != kPlain) {
           u = mul2(u, f);
           if (column >= end) u.x = -INFINITY;
           if (column + 1 >= end) u.y = -INFINITY;
@@ -513,8 +560,13 @@ __device__ __forceinline__ void weigh(uint32_t S, const Scales &scales, const fl
         }
         u = make_float2(exp2_fast(u.x), exp2_fast(u.y));
         sums[r] = add2(sums[r], u);
-        u = mul2(u, g);
-        if (kMasked) {                                     // (a token that is not seen may stand for anything)
+        if (kCare == kOwn) {
+          const float lift = __uint_as_float((uint32_t)(exponent(lifts, r) + 127) << 23);
+          u = mul2(u, make_float2(g.x * lift, g.y * lift));
+        } else {
+          u = mul2(u, g);
+        }
+        if (kCare != kPlain) {                             // (a token that is not seen may stand for anything)
           if (column >= end) u.x = 0.0f;
           if (column + 1 >= end) u.y = 0.0f;
         }
@@ -573,20 +625,20 @@ __device__ __forceinline__ void softmax_role(const Block &B, int half, int quart
     if (lane == 0) mbar_arrive(B.smem + L::kQFull + 8u * half);
   }
   const uint32_t lanes = (uint32_t)(32 * quarter) << 16, S = lanes + (uint32_t)(half * kTokens), O = lanes + L::kO + (uint32_t)(half * kDim);
-  const int n = B.steps, least = __reduce_min_sync(0xffffffffu, limit);
+  const int n = B.steps;
   // a row's maximum so far, 0 where it has seen nothing (`unset`: a bit for each), and the sum of its weights
   float m[4], l[4];
-  int limits[4], unset = 15, e = kLeastScale;
+  int unset = 15;
+  int e = kLeastScale;         // the values' scales so far are below 2^e: those of the steps that all rows see,
+  uint32_t own = 0u;           // and from then on those that each row sees
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    m[j] = l[j] = 0.0f;
-    limits[j] = __shfl_sync(0xffffffffu, limit, g + 8 * j);
-  }
+  for (int j = 0; j < 4; ++j) m[j] = l[j] = 0.0f;
   bool calm = false;           // all of the warp's rows have a maximum, below 2^20 (from there on what rounding leaves of s ks - m would count)
-#pragma unroll 1
-  for (int i = 0; i < n; ++i) {
+  // Step i; false: gave up.
+  auto step = [&](auto kOwnTag, int i) {
+    constexpr bool kRowsOwn = decltype(kOwnTag)::value;
     const uint32_t tile = (uint32_t)(i >> 1), sub = (uint32_t)i & 1u, buf = tile % kScaleBufs;
-    if (sub == 0u && !wait_inline(B, B.smem + L::kScaled + 8u * buf, (tile / kScaleBufs) & 1u)) return;
+    if (sub == 0u && !wait_inline(B, B.smem + L::kScaled + 8u * buf, (tile / kScaleBufs) & 1u)) return false;
     Scales scales;
     const uint32_t ks = B.smem + L::kScales + 4u * (2u * buf * kTokens + sub * kStep) + 8u * t;
 #pragma unroll
@@ -594,28 +646,42 @@ __device__ __forceinline__ void softmax_role(const Block &B, int half, int quart
       scales.k[k] = lds_float2(ks + 32u * k);
       scales.v[k] = lds_float2(ks + 4u * kTokens + 32u * k);
     }
-    const int e_now = (int)lds32(B.smem + L::kExponent + 4u * buf);
+    const int e_now = (int)lds32(B.smem + L::kExponent + 8u * buf + 4u * sub);
     const uint32_t there = lds32(B.smem + L::kThere + 4u * buf) >> (kStepRecords * sub) & ((1u << kStepRecords) - 1u);
-    if (!wait_inline(B, B.smem + L::kSFull + 16u * half + 8u * sub, tile & 1u)) return;
+    if (!wait_inline(B, B.smem + L::kSFull + 16u * half + 8u * sub, tile & 1u)) return false;
     tc_fence_after();
     const uint32_t here = S + sub * kStep;
-    const int t0 = B.first * kTokens + i * kStep;
-    const int none[4] = {};
-    uint32_t p[2][16];
+    int seen[4] = {};
+    uint32_t lifts = 0u, p[2][16], own_now = 0u;
     float sum[4], top[4];
     bool good = false;
-    if (calm && there == (1u << kStepRecords) - 1u && t0 + kStep - 1 <= least && e_now == e) {
-      weigh<false>(here, scales, m, none, 0u, p, sum, top);
+    if (!kRowsOwn && calm && there == (1u << kStepRecords) - 1u && e_now == e) {
+      weigh<kPlain>(here, scales, m, seen, 0u, 0u, p, sum, top);
       good = !__any_sync(0xffffffffu, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) > kRaise);
     }
     if (!good) {
-      // What is masked, and where a maximum is left too far behind: that is raised, and the step weighed once more.
+      // Where a maximum is left too far behind: that is raised, and the step weighed once more.  And steps with tokens that are missing or
+      // masked: of the latter each row's powers of two are those up to its last token.
+      bool moved;
+      if constexpr (kRowsOwn) {
+        const int t0 = B.first * kTokens + i * kStep;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int last = __shfl_sync(0xffffffffu, limit, g + 8 * j) - t0;      // in the step; below 0: none of it
+          seen[j] = (last < 0 ? 0 : min(last, kStep) + 1) - 2 * t;
+          const int in_tile = min(last + (int)sub * kStep, kTokens - 1);           // (the tile's, so that both of its steps have the same)
+          const int v = in_tile < 0 ? exponent(own, j) : (int)lds32(B.smem + L::kUpTo + 4u * (buf * kTokens + (uint32_t)in_tile));
+          own_now |= ((uint32_t)v & 255u) << (8 * j);
+        }
+        lifts = __vsub4(four_times(kLift), own_now);
+        moved = __any_sync(0xffffffffu, own_now != own);
+      } else {
+        moved = e_now != e;
+      }
 #pragma unroll 1
       for (int attempt = 0;; ++attempt) {
-        int seen[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) seen[j] = (limits[j] < t0 ? 0 : min(limits[j] - t0, kStep) + 1) - 2 * t;
-        weigh<true>(here, scales, m, seen, there, p, sum, top);
+        asm volatile("" : "+r"(lifts));                    // (else products with it are worked out before the loop, and spilled)
+        weigh<kRowsOwn ? kOwn : kCareful>(here, scales, m, seen, lifts, there, p, sum, top);
         int up = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -624,8 +690,7 @@ __device__ __forceinline__ void softmax_role(const Block &B, int half, int quart
           if (top[j] > (unset >> j & 1 ? -INFINITY : m[j] + kRaise)) up |= 1 << j;
         }
         const bool again = attempt == 0 && __any_sync(0xffffffffu, up != 0);
-        if (!again && e_now == e) break;
-        const float down = power_of_two(e - e_now);
+        if (!again && !moved) break;
         float f[4];
         calm = true;
 #pragma unroll
@@ -636,15 +701,17 @@ __device__ __forceinline__ void softmax_role(const Block &B, int half, int quart
             m[j] = top[j];
           }
           l[j] *= f[j];
-          f[j] *= down;
+          if (moved) f[j] *= kRowsOwn ? power_of_two(exponent(own, j) - exponent(own_now, j)) : power_of_two(e - e_now);
           calm = calm && fabsf(m[j]) < 1048576.0f;
         }
         if (again) unset &= ~up;
         calm = __all_sync(0xffffffffu, calm && unset == 0);
-        e = e_now;
+        if (kRowsOwn) own = own_now;
+        else e = e_now;
+        moved = false;
         if (i > 0) {
           // P V of the last step has to be done: the next step's S comes behind it
-          if (!(i + 1 < n ? wait_inline(B, B.smem + L::kSFull + 16u * half + 8u * (sub ^ 1u), (uint32_t)((i + 1) >> 1) & 1u) : wait_inline(B, B.smem + L::kODone + 8u * half, 0u))) return;
+          if (!(i + 1 < n ? wait_inline(B, B.smem + L::kSFull + 16u * half + 8u * (sub ^ 1u), (uint32_t)((i + 1) >> 1) & 1u) : wait_inline(B, B.smem + L::kODone + 8u * half, 0u))) return false;
           tc_fence_after();
 #pragma unroll 1
           for (int c = 0; c < kDim / 16; ++c) {
@@ -669,7 +736,15 @@ __device__ __forceinline__ void softmax_role(const Block &B, int half, int quart
     tc_fence_before();
     __syncwarp();
     if (lane == 0) mbar_arrive(B.smem + L::kPFull + 16u * half + 8u * sub);
-  }
+    return true;
+  };
+#pragma unroll 1
+  for (int i = 0; i < B.whole; ++i)
+    if (!step(std::false_type(), i)) return;
+  own = four_times(e);
+#pragma unroll 1
+  for (int i = B.whole; i < n; ++i)
+    if (!step(std::true_type(), i)) return;
   // ---- a row a thread: its output, or its sums for the kernel that joins them
 #pragma unroll
   for (int j = 0; j < 4; ++j)
@@ -677,13 +752,16 @@ __device__ __forceinline__ void softmax_role(const Block &B, int half, int quart
     for (int x = 1; x < 4; x *= 2) l[j] += __shfl_xor_sync(0xffffffffu, l[j], x);
 #pragma unroll
   for (int j = 0; j < 4; ++j) m[j] = unset >> j & 1 ? -INFINITY : m[j];
-  const float m_row = of_row(m, lane), l_row = of_row(l, lane);
+  float lifted[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) lifted[j] = power_of_two(exponent(own, j) - kLift);
+  const float m_row = of_row(m, lane), l_row = of_row(l, lane), back = of_row(lifted, lane);
   if (n > 0) {
     if (!wait_inline(B, B.smem + L::kLast + 8u * half, 0u)) return;
     tc_fence_after();
   }
   const bool blind = l_row == 0.0f;                        // no token before it, or all of them outside the cache
-  const float back = power_of_two(e - kLift), inv = B.direct ? back / l_row : back;
+  const float inv = B.direct ? back / l_row : back;
   float *partial = B.partial + (size_t)(half * kHalf + in_tile) * kDim, *stats = B.partial + (size_t)kItemRows * kDim + 2 * (half * kHalf + in_tile);
   int32_t o[kDim / 16][16];
   if (n > 0) {
@@ -748,9 +826,9 @@ kv4_prompt_kernel(const __grid_constant__ Params P) {
   int *found = reinterpret_cast<int *>(smem_ptr + L::kItem);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(smem_ptr + L::kAbort);
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kRawStages; ++i) { mbar_init(smem + L::kRawFull + 8u * i, 1); mbar_init(smem + L::kRawEmpty + 8u * i, 8); }
+    for (int i = 0; i < kRawStages; ++i) { mbar_init(smem + L::kRawFull + 8u * i, 1); mbar_init(smem + L::kRawEmpty + 8u * i, 9); }
     for (int i = 0; i < kOperands; ++i) { mbar_init(smem + L::kFull + 8u * i, 4); mbar_init(smem + L::kEmpty + 8u * i, 1); }
-    for (int i = 0; i < kScaleBufs; ++i) mbar_init(smem + L::kScaled + 8u * i, 4);
+    for (int i = 0; i < kScaleBufs; ++i) mbar_init(smem + L::kScaled + 8u * i, 1);
     for (int i = 0; i < 4; ++i) { mbar_init(smem + L::kSFull + 8u * i, 1); mbar_init(smem + L::kPFull + 8u * i, 4); }
     for (int i = 0; i < 2; ++i) { mbar_init(smem + L::kODone + 8u * i, 1); mbar_init(smem + L::kLast + 8u * i, 1); mbar_init(smem + L::kQFull + 8u * i, 4); }
     *abort_flag = 0;
@@ -785,10 +863,11 @@ kv4_prompt_kernel(const __grid_constant__ Params P) {
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  Block B = {P, {}, found[0], at % P.A.w.d.kv_heads, found[1], 0, 0, 0, false, false, smem, 0u, 0u, smem_ptr, abort_flag, nullptr};
+  Block B = {P, {}, found[0], at % P.A.w.d.kv_heads, found[1], 0, 0, 0, 0, false, false, smem, 0u, 0u, smem_ptr, abort_flag, nullptr};
   const bool work = found[2] != 0;
   B.s.start = found[3]; B.s.n = found[4]; B.s.len = found[5]; B.s.lead = found[6];
   B.first = found[7]; B.last = found[8]; B.steps = found[9];
+  B.whole = min(B.steps, max(0, min(B.s.lead + B.s.start + B.tile * kItemRows / P.T.group, B.s.len - 1) + 1 - B.first * kTokens) / kStep);
   B.two = found[10] != 0;
   B.direct = found[11] != 0;
   B.q = (smem + L::kQ + 1023u) & ~1023u;
@@ -809,6 +888,8 @@ kv4_prompt_kernel(const __grid_constant__ Params P) {
           mma_role<T, kDim>(B);
         } else if (warp == kCopyWarp) {
           copy_role<kDim>(B, lane);
+        } else if (warp == kScaleWarp) {
+          scale_role<kDim>(B, lane);
         }
       }
       __syncwarp();

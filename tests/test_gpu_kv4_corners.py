@@ -140,11 +140,19 @@ FEW = [
     ([400, 90], [8, 2], 2, 2, 393),
     ([5000], [3], 1, 5, 4998),
 ]
+MANY = [
+    ([150], [150], 2, 1, 70),
+    ([150], [150], 2, 4, 149),
+    ([400], [200], 2, 4, 290),
+    ([400, 30], [200, 3], 1, 16, 399),
+    ([300], [300], 1, 1, 140),
+    ([3000], [130], 1, 8, 2999),
+]
 
 
-@pytest.mark.parametrize("case", FEW, ids=lambda c: "%s-%s-%d-%d-%d" % c)
+@pytest.mark.parametrize("case", FEW + MANY, ids=lambda c: "%s-%s-%d-%d-%d" % c)
 @pytest.mark.parametrize("D", [64, 128])
-def test_values_of_later_tokens_in_a_call_of_few(case, D):
+def test_values_of_later_tokens(case, D):
     """A row is as exact as if the tokens behind it did not exist, however large their values are: one of them 2^40 times the
     others, and all of them growing from token to token."""
     lens, new, H, G, p = case
