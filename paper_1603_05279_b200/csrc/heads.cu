@@ -166,10 +166,11 @@ heads_backward_kernel(const HeadsArgs A, int q_blocks) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) dot = fmaf(g[j] * w[j], x[j], dot);
         const float r = __frsqrt_rn(lane.sum(s) * (1.0f / kDim) + A.d.eps);
-        const float k = lane.sum(dot) * (r * r * (1.0f / kDim)), once = h < I.heads ? r : 0.0f;
+        const float k = lane.sum(dot) * (r * r * (1.0f / kDim));
+        // (what a thread without a head has read is another's, and may be its gradient already, even infinite)
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          dw[j] = fmaf(g[j] * once, x[j], dw[j]);
+          if (h < I.heads) dw[j] = fmaf(g[j] * r, x[j], dw[j]);
           g[j] = r * fmaf(-x[j], k, g[j] * w[j]);
         }
       }
