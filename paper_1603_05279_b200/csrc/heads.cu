@@ -468,6 +468,12 @@ cudaError_t launch_heads(const HeadsArgs &a, cudaStream_t st) {
 cudaError_t launch_heads_backward(const HeadsArgs &args, cudaStream_t st) {
   HeadsArgs a = args;
   if (!a.d.norm || (a.dq_weight == nullptr && a.dk_weight == nullptr)) a.work = nullptr;
+  if (!a.d.norm) {
+    // values and weights are not given then, and the kernel for whole chunks reads them all the same: the gradients stand in
+    a.q = a.dq_out; a.d.q_stride = a.d.dq_stride;
+    a.k = a.dk_out; a.d.k_stride = a.d.dk_stride;
+    a.q_weight = a.k_weight = nullptr;
+  }
   BackwardBlocks b = {0, 0};
   if (a.d.rows > 0) {
     b = backward_blocks(a.d.rows, a.d.q_heads, a.d.k_heads);
