@@ -495,10 +495,11 @@ xnor_status check_heads(const xnor_heads_desc *d, const void *q_weight, const vo
 
 bool bad_kv4(const xnor_kv4_desc *d) { return !d || d->pages < 1 || d->page < 16 || d->page % 16 || d->kv_heads < 1 || d->dim < 1; }
 bool large_kv4(const xnor_kv4_desc *d) { return (d->dim != 64 && d->dim != 128) || d->page > 65536 || d->kv_heads > 4096; }
+constexpr int kMostSeqs = 1 << 20;
 constexpr long long kMostTokens = (1ll << 31) - 256;      // of a sequence: rounded up to whole tiles an int
 xnor_status check_kv4(const xnor_kv4_desc *d, const void *cache, const int32_t *starts, const int32_t *lens, const int32_t *table) {
   if (bad_kv4(d) || d->seqs < 1 || d->table_cols < 1 || bad_ptr(cache) || bad_ptr(starts) || bad_ptr(lens) || bad_ptr(table)) return XNOR_ERR_INVALID_ARG;
-  return large_kv4(d) || d->seqs > (1 << 20) || (long long)d->table_cols * d->page > kMostTokens ? XNOR_ERR_UNSUPPORTED : XNOR_OK;
+  return large_kv4(d) || d->seqs > kMostSeqs || (long long)d->table_cols * d->page > kMostTokens ? XNOR_ERR_UNSUPPORTED : XNOR_OK;
 }
 bool bad_kv4_rows(const xnor_kv4_desc *d, const xnor_kv4_rows *r) {
   return !r || r->rows < 0 || r->q_heads < 1 || r->q_heads % d->kv_heads || !real_type(r->type) || r->most < 0;
@@ -674,7 +675,7 @@ xnor_status xnor_kv4_read(const void *cache, const int32_t *starts, const int32_
 }
 
 size_t xnor_kv4_work_bytes(const xnor_kv4_desc *d, const xnor_kv4_rows *r) {
-  if (bad_kv4(d) || large_kv4(d) || bad_kv4_rows(d, r) || large_kv4_rows(r)) return 0;
+  if (bad_kv4(d) || large_kv4(d) || d->seqs < 1 || d->seqs > kMostSeqs || bad_kv4_rows(d, r) || large_kv4_rows(r)) return 0;
   return xnor::kv4_work_bytes(*d, *r);
 }
 
