@@ -8,9 +8,13 @@ namespace xnor {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // A row's maximum is left behind by 2^8 at most: then P, up to 2^8 times a value's scale, is rounded to F16, relative to a
 // power of two 2^e above the largest scale so far that the row sees and times 2^7.  That is at most 2^15, and has all 11 bits
-// down to 2^-21 of that scale.  (As bfloat16 it gave outputs in bfloat16 half as much again of error.)
+// down to 2^-21 of that scale.  (As bfloat16 it gave outputs in bfloat16 half as much again of error.)  Outputs in F16 would show it: there
+// what the rounding left is a second operand, and 22 bits are kept (16 sequences of 2000 tokens, five new: error 0.0003 -> 0.0002, which is
+// the output's own rounding, 20.2 -> 21.2 us; prompts of 2000, 1000 and 333 tokens, 40 heads of 128 on 8, 115 -> 135 us).
 constexpr float kRaise = 8.0f;
 constexpr int kLift = 7;
+template <class T> constexpr bool kTwoParts = false;
+template <> constexpr bool kTwoParts<__half> = true;
 
 // (a wait that gave up is the graver: that is written over this, and this not over that)
 __device__ __forceinline__ void record_bounds(int *status) { atomicCAS(status, 0, (int)XNOR_ERR_BOUNDS); }

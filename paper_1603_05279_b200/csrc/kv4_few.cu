@@ -487,7 +487,7 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
         vs0 *= lift[0][0];
         vs1 *= lift[0][0];
       }
-      uint32_t b[kTiles][2];                                               // P^T: tokens 0 .. 7 and 8 .. 15 of the rows
+      uint32_t b[kTiles][2], rest[kTiles][2];                              // P^T: tokens 0 .. 7 and 8 .. 15 of the rows; what its rounding left
 #pragma unroll
       for (int n = 0; n < kTiles; ++n) {
 #pragma unroll
@@ -501,7 +501,14 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
           for (int j = 0; j < 4; ++j) x[n][j] = s[n][j] == -INFINITY ? 0.0f : x[n][j] * ((j < 2 ? vs0 : vs1) * lift[n][j & 1]);
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) b[n][h] = transpose8x8(float_to_pair(x[n][2 * h], x[n][2 * h + 1], __half()));
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t w = float_to_pair(x[n][2 * h], x[n][2 * h + 1], __half());
+          b[n][h] = transpose8x8(w);
+          if constexpr (kTwoParts<T>) {
+            const float2 f = pair_to_float(w, __half());
+            rest[n][h] = transpose8x8(float_to_pair(x[n][2 * h] - f.x, x[n][2 * h + 1] - f.y, __half()));
+          }
+        }
       }
       // ---- O^T: thread (g, t) has columns kDim / 8 g .. of tokens 2 t, 2 t + 1 and 8 more
       {
@@ -521,7 +528,10 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
           for (int k = 0; k < 4; ++k) {
             const uint32_t a[4] = {v[0][0][k], v[0][1][k], v[1][0][k], v[1][1][k]};
 #pragma unroll
-            for (int n = 0; n < kTiles; ++n) mma16816(o[n][4 * w + k], a, b[n][0], b[n][1]);
+            for (int n = 0; n < kTiles; ++n) {
+              mma16816(o[n][4 * w + k], a, b[n][0], b[n][1]);
+              if constexpr (kTwoParts<T>) mma16816(o[n][4 * w + k], a, rest[n][0], rest[n][1]);
+            }
           }
         }
       }

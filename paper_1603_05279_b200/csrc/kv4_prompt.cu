@@ -2,7 +2,7 @@
 //
 // A block computes one item: up to 256 rows (queries of a head's group, token by token) in two halves of 128, over their
 // context in tiles of 128 tokens, 64 at a step.  S = Q K^T (128 x 64) and O += P V run on tcgen05.mma kind::f16 with fp32 sums in tensor
-// memory: two S and an O of both halves fill it, and P, in F16, lies where S lay.  Two S, so that the products of a step run while the
+// memory: two S and an O of both halves fill it, and P, in F16 (in one part or two), lies where S lay.  Two S, so that the products of a step run while the
 // softmax is busy with another (one S of 128 tokens left the tensor cores idle while both halves weighed: 545 us for two
 // prompts of 4096 tokens).  Keys and values become code - zero, exactly, in shared
 // memory; a key's scale multiplies its column of S, a value's its column of P (rounded to F16 as in the kernel for few
@@ -444,6 +444,10 @@ __device__ __forceinline__ void mma_role(const Block &B) {
       const uint32_t to = L::kO + (uint32_t)h * kDim, weights = (uint32_t)h * kTokens + sub * kStep;
 #pragma unroll
       for (int k = 0; k < kStep / 16; ++k) mma_tmem(leader, to, weights + 8u * k, values + (uint64_t)(2 * k), kODesc, j == 0 && k == 0 ? 0u : 1u);
+      if constexpr (kTwoParts<T>) {
+#pragma unroll
+        for (int k = 0; k < kStep / 16; ++k) mma_tmem(leader, to, weights + kStep / 2 + 8u * k, values + (uint64_t)(2 * k), kODesc, 1u);
+      }
       if (j + 2 >= n) commit(leader, B.smem + (j + 1 < n ? L::kODone : L::kLast) + 8u * h);
       if (h + 1 == halves && (sub == 1u || j + 1 == n)) free_operand(op);
       if (j + 2 < n && !qk(h, j + 2)) return;              // (behind P V, whose P it overwrites)
@@ -520,9 +524,10 @@ __device__ __forceinline__ float2 lds_float2(uint32_t addr) {
 // are not seen, and the values' scales are those of the cache, which each row takes times a power of two of its own (lifts: the exponents).
 struct Scales { float2 k[kStep / 8], v[kStep / 8]; };
 enum Care { kPlain, kCareful, kOwn };
-template <Care kCare>
+// Two parts: p has what the rounding left behind the rounded weights.
+template <Care kCare, int kParts>
 __device__ __forceinline__ void weigh(uint32_t S, const Scales &scales, const float (&m)[4], const int (&seen)[4], uint32_t lifts, uint32_t there,
-                                      uint32_t (&p)[2][16], float (&sum)[4], float (&top)[4]) {
+                                      uint32_t (&p)[kParts][2][16], float (&sum)[4], float (&top)[4]) {
   float2 sums[4];
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
@@ -570,7 +575,12 @@ __device__ __forceinline__ void weigh(uint32_t S, const Scales &scales, const fl
           if (column >= end) u.x = 0.0f;
           if (column + 1 >= end) u.y = 0.0f;
         }
-        p[r >> 1][2 * (4 * c + k) + (r & 1)] = float_to_pair(u.x, u.y, __half());
+        uint32_t &w = p[0][r >> 1][2 * (4 * c + k) + (r & 1)];
+        w = float_to_pair(u.x, u.y, __half());
+        if constexpr (kParts == 2) {
+          const float2 f = pair_to_float(w, __half());
+          p[1][r >> 1][2 * (4 * c + k) + (r & 1)] = float_to_pair(u.x - f.x, u.y - f.y, __half());
+        }
       }
     }
   }
@@ -652,7 +662,7 @@ __device__ __forceinline__ void softmax_role(const Block &B, int half, int quart
     tc_fence_after();
     const uint32_t here = S + sub * kStep;
     int seen[4] = {};
-    uint32_t lifts = 0u, p[2][16], own_now = 0u;
+    uint32_t lifts = 0u, p[kTwoParts<T> ? 2 : 1][2][16], own_now = 0u;
     float sum[4], top[4];
     bool good = false;
     if (!kRowsOwn && calm && there == (1u << kStepRecords) - 1u && e_now == e) {
@@ -730,8 +740,12 @@ __device__ __forceinline__ void softmax_role(const Block &B, int half, int quart
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) l[j] += sum[j];
-    tmem_st_weights(here, p[0]);
-    tmem_st_weights(here + (16u << 16), p[1]);
+    tmem_st_weights(here, p[0][0]);
+    tmem_st_weights(here + (16u << 16), p[0][1]);
+    if constexpr (kTwoParts<T>) {
+      tmem_st_weights(here + kStep / 2, p[1][0]);
+      tmem_st_weights(here + kStep / 2 + (16u << 16), p[1][1]);
+    }
     tmem_wait_st();
     tc_fence_before();
     __syncwarp();

@@ -7,7 +7,7 @@ import torch
 import paper_1603_05279_b200 as X
 from paper_1603_05279_b200 import binding as B
 from kv4_util import TYPES, Batch, attention64
-from rows_util import gen, randn
+from rows_util import U, gen, half_step, least, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -168,3 +168,44 @@ def test_values_of_later_tokens(case, D):
         assert ((lse.double() - x).abs() <= lse_off).all()
         worst = ((out.double() - want).abs() / off).amax((1, 2))
         assert (worst <= 1).all(), (worst.argmax(), worst.max())
+
+
+# lens, new, kv heads, queries a head, most
+FINE = [
+    ([1, 2, 3, 5, 17], [1] * 5, 2, 1, 1),
+    ([4, 1, 9], [4, 1, 5], 2, 4, 5),
+    ([40, 700], [2, 1], 3, 8, 2),
+    ([3000], [1], 1, 2, 1),                      # cut among blocks
+    ([150, 130], [150, 130], 1, 1, 150),
+    ([130, 200], [130, 4], 2, 4, 130),
+    ([2500], [200], 1, 4, 200),                  # cut among blocks
+]
+
+
+@pytest.mark.parametrize("case", FINE, ids=str)
+@pytest.mark.parametrize("D", [64, 128])
+def test_outputs_in_f16_are_off_by_their_own_rounding(case, D):
+    """As attention64 derives it, but weights times scales are rounded in two parts: what F16 leaves of a value x, at most 2^-11 x and exact in
+    fp32, is rounded to F16 in its turn, so that 2^-22 x is left, or half a step of the least numbers, 2^-32 of the largest scale.
+    Small logits, so that fp32's share is small too."""
+    lens, new, H, G, most = case
+    batch = Batch(lens, new, H, D, 16, 241).fill(242)
+    q = randn((batch.T, H * G, D), gen(243), torch.float16, 0.05)
+    scale = 0.125
+    out, lse = attend(batch, q, scale, most)
+    X.xnor_check_device()
+    for b, (length, n) in enumerate(zip(lens, new)):
+        K, V = batch.read64(b)
+        rows = slice(sum(new[:b]), sum(new[:b]) + n)
+        Q = q[rows].double().unflatten(1, (H, G))
+        S = torch.einsum("nhgd,lhd->nhgl", Q, K) * scale
+        size = torch.einsum("nhgd,lhd->nhgl", Q.abs(), K.abs()).amax(-1) * scale
+        hidden = torch.arange(length, device="cuda") > torch.arange(length - n, length, device="cuda")[:, None]
+        w = torch.softmax(S.masked_fill(hidden[:, None, None], -INF), -1)
+        want, mass = torch.einsum("nhgl,lhd->nhgd", w, V), torch.einsum("nhgl,lhd->nhgd", w, V.abs())
+        # logits (2 D + 4) U of their size, their distances below 10: 4 U each, exp2 2^-21; twice, and the sums' chains
+        e = 2 * (size * (2 * D + 4) * U + 40 * U + 2.0 ** -21) + (length / 64 + 64) * 2 * U
+        off = mass * (e[..., None] + 2.0 ** -22 + (length / 16 + 64) * 2 * U) + 2.0 ** -32 * 2 * 15 * length * V.abs().amax()
+        off = off + half_step(torch.float16) * (want.abs() + off) + least(torch.float16)
+        worst = ((out[rows].double().unflatten(1, (H, G)) - want).abs() / off).max().item()
+        assert worst <= 1, (b, worst)
