@@ -672,7 +672,8 @@ xnor_status xnor_kv4_read(const void *cache, const int32_t *starts, const int32_
  * Codes are exact operands, and so are queries (in BF16, where rows are few, but for values below 2^-31 of the row's
  * largest, which are rounded to a step of 2^-38 of that); products, sums and the softmax are fp32, but exp(..) times
  * a value's scale, which is rounded to 11 bits for outputs in BF16, to 22 for F16 (both of them no finer than to a step of 2^-31
- * of the largest scale that the row sees), to meet the values' codes.  The order of the sums depends on the sizes, all sequences' lengths and the device's number of SMs: the same call gives the same bits.
+ * of the largest scale that the row sees), to meet the values' codes.  (So values, summed over the context
+ * with weights of up to 2^8, have to stay within fp32.)  The order of the sums depends on the sizes, all sequences' lengths and the device's number of SMs: the same call gives the same bits.
  * Device-side waits are bounded (xnor_check_device).  What lies outside the table or the cache is not seen.
  * INVALID_ARG as above, and: q_heads no multiple of kv_heads, scale not finite, most < 0, out in the place of q.
  * UNSUPPORTED as above, and: F32, rows q_heads > 2^30.

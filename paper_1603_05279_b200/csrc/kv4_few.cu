@@ -14,9 +14,9 @@
 // seventh unit each; at an item's end (the units of a tile) they add their sums.  An item that lies in
 // several blocks' shares leaves partial sums in the workspace, which a second kernel joins.
 //
-// 64 sequences of 300 to 8192 tokens, 8 heads of 128 with four queries each: 88 us with the join (294 MB, 0.52 of a copy's rate), at
-// 2.4 instructions per clock and more, half of the ALU's: the expansion of the codes and the softmax, 380 instructions a record of 4096 codes.  Single
-// tokens of short batches are latency: 5000 tokens 13.5 us with the join.  Two blocks per SM: one of 14 warps took 130 us (they
+// 64 sequences of 300 to 8192 tokens, 8 heads of 128 with four queries each: 88 us with the join (294 MB, 0.51 of a copy's rate), at
+// 2.5 instructions per clock, half of the ALU's: the expansion of the codes and the softmax, 390 instructions a record of 4096 codes.  Single
+// tokens of short batches are latency: 5000 tokens 12.9 us with the join.  Two blocks per SM: one of 14 warps took 130 us (they
 // meet at every item's end), three spilled, 146.
 #include <algorithm>
 #include <climits>
@@ -287,7 +287,6 @@ __device__ __forceinline__ void compute_role(const Params &P, int worker, long l
       p.s.load(W, P.T, ++p.b);
     }
     p.set(u - sum);
-    const long long item0 = u - p.rec;                                     // the item's units
     const int rec_end = (int)min((long long)p.s.units, p.rec + (u1 - u));
     // Q: thread (g, t) has row g's columns kDim / 4 t .., as its words of keys have them
     uint32_t q[kTiles][kWords][4];

@@ -17,8 +17,8 @@
 // own that P is rounded by, for it must not go by tokens that the row does not see (as one loop, whose registers did not do: 419 us for 408
 // for two prompts of 4000 tokens and 30 single ones; one prompt of 128 tokens, which has no other steps, takes 1 us more than when
 // rows shared it).
-// Two prompts of 4096 tokens, 32 heads of 128 on 8: 427 us with the other kernel's launches, 629 TFLOP/s of what is not masked, 0.37 of a matrix product's rate; the tensor
-// pipe is busy 30 % of the time.  An item of two halves takes 2800 clocks for 128 tokens, of which the products alone would take
+// Two prompts of 4096 tokens, 32 heads of 128 on 8: 393 us with the other kernel's launches, 684 TFLOP/s of what is not masked, 0.40 of a matrix product's rate; the tensor
+// pipe is busy 33 % of the time.  When it took 427 an item of two halves took 2800 clocks for 128 tokens, of which the products alone would take
 // 1600, and 27,000 before its first and after its last (its place, its queries, the first records, its output).  Tried: turns of the
 // halves by barriers 583 us against 470 at the time, one block that goes on from item to item 582 (it spills), two chains of products no change.
 // Where there are too few items for the GPU, the blocks of an item divide its context, and a second kernel joins
@@ -993,12 +993,14 @@ template <class T>
 cudaError_t run_type(const Kv4Args &a, int least_rows, cudaStream_t st) { return a.w.d.dim == 64 ? run<T, 64>(a, least_rows, st) : run<T, 128>(a, least_rows, st); }
 
 // Up to how many rows of a sequence (new tokens x queries of a head) the kernel for few takes it: that one reads the context once
-// for every 16 rows, this one once for 256.  us for 16, 32, 64, 96, 128 rows of every head, few against this, dim 128:
-//   64 sequences of 4000 tokens, 8 heads   139 259 502 746 988   315 317 323 328 333
-//   16 of 2000, 8 heads                     29  46  82 115 148    51  52  51  52  52
-//   3 of 8000, 8 heads                      25  34  52  70  93    45  46  47  56  57     (blocks share an item)
-//   1 of 4000, 8 heads                      19  19  22  25  28    23  23  24  25  26
-//   4 of 1000, 4 heads                      17  17  19  21  23    27  27  29  30  30
+// for every 16 rows, this one once for 256.  us for 16, 32, 64, 96, 128 rows of every head, few against this:
+//                                          dim 128, bfloat16                             dim 64
+//   64 sequences of 4000 tokens, 8 heads   137 255 496 736 977   319 319 322 323 324     111 203 386 569 753   287 287 287 288 288
+//   16 of 2000, 8 heads                     28  46  78 111 144    52  53  51  51  51      23  36  61  85 109    46  46  44  45  45
+//   3 of 8000, 8 heads                      22  32  51  70  90    45  46  46  56  57      19  27  42  57  73    41  41  42  50  51   (blocks share an item)
+//   1 of 4000, 8 heads                      16  17  19  23  26    21  21  22  23  24      13  14  17  19  21    19  19  19  20  20
+//   4 of 1000, 4 heads                      15  15  17  20  22    25  26  28  29  29      13  13  15  16  19    23  24  26  27  26
+// F16 moves both: 64 sequences 137 259 503 747 991, 364 366 368 370 372.
 int few_rows(const xnor_kv4_desc &d) { return (long long)d.seqs * d.kv_heads > 16 ? 32 : 96; }
 
 }  // namespace
