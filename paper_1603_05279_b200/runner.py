@@ -311,8 +311,9 @@ class TokenAttention:
     """Buffers and calls of the attention in a decoder's layer, on bfloat16 rows between two TokenBlocks' products: norms
     and rotation of queries and keys, the new tokens into a cache in 4 bits, and attention over it.
 
-    `seqs` sequences of up to `context` tokens each, in pages of `page`; up to `rows` new tokens in a call, up to `most`
-    of a sequence (0: any).  rot: rotated values of a head (None: all, 0: none)."""
+    `seqs` sequences of up to `context` tokens each, in pages of `page` (tokens behind that are left out, and the next
+    xnor_check_device says so); up to `rows` new tokens in a call, up to `most` of a sequence (0: any; a call of few takes
+    longer then).  rot: rotated values of a head (None: all, 0: none)."""
 
     def __init__(self, rows, seqs, context, q_heads, kv_heads, dim, page=64, most=0, norm=True, rot=None, base=10000.0,
                  pairs=False, eps=1e-6, device="cuda"):
